@@ -448,7 +448,9 @@ heddle_status heddle_get_tables(heddle_ctx* ctx, int64_t* q, int64_t* p2p);
  * device first, then clears them): bit 0 a table-staging wait timed out,
  * bit 1 a search exceeded its iteration bound, bit 2 an internal
  * consistency check failed, bit 3 (bounds-checked builds only) an index
- * test failed and the access was skipped.  0 in normal operation. */
+ * test failed and the access was skipped, bit 4 a wait inside a layer
+ * operator ran out (its outputs are not valid), bit 5 a position outside its
+ * rotation table.  0 in normal operation. */
 heddle_status heddle_device_errors(heddle_ctx* ctx, uint32_t* flags);
 
 /* PartitionLayers search.  AUTO (default) uses the equal-layer closed form
@@ -532,6 +534,221 @@ heddle_status heddle_work_counters(heddle_ctx* ctx, uint64_t out[3]);
 heddle_status heddle_time_phases(heddle_ctx* ctx, int32_t enable);
 heddle_status heddle_phase_times(heddle_ctx* ctx, double ms[HEDDLE_N_PHASES],
                                  int64_t launches[HEDDLE_N_PHASES]);
+
+/* ----------------------------------------------------- layer operators */
+
+/* A transformer layer's operators, forward and backward, so that the profile
+ * entries that heddle_load_model takes (§5.2: seconds of one layer at each
+ * degree) can be measured on the GPU at hand, at the shapes of each degree's
+ * shard.  The paper takes such profiles from elsewhere and names no operator.
+ *
+ * Matrices are row-major with a row stride (ld, in elements, at least the
+ * columns); weights are [outputs][inputs].  Element types: HEDDLE_BF16,
+ * HEDDLE_FP16 (products, sums, statistics and saved activations are held in
+ * 32 bits, each result is rounded once) and, where named, HEDDLE_FP32.
+ * Buffers are device memory and any alignment of the element type is taken;
+ * products run from laid-out copies in the context's scratch where a base or
+ * row stride is no multiple of 16 bytes.  An output must not overlap an
+ * input unless named.  All calls are asynchronous on `stream`, results do not
+ * depend on the launch configuration of other calls and repeat bit for bit.
+ * Scratch belongs to the context and grows on first use of a larger size
+ * (E_NOMEM if that fails): before a stream capture, make the call once.
+ * Calls on one context must not overlap on the GPU.
+ * Errors of all: E_ARG (a null pointer, a negative size, a bad stride, type
+ * or activation), E_LIMIT (a size beyond the limits named), E_CUDA, E_NOMEM;
+ * nothing is launched then.  A call whose outputs are empty is a no-op; a
+ * sum over an empty dimension is zero.  Sizes are at most 2^31 - 1. */
+#define HEDDLE_BF16 0
+#define HEDDLE_FP16 1
+#define HEDDLE_FP32 2
+
+#define HEDDLE_ACT_NONE 0
+#define HEDDLE_ACT_RELU 1
+#define HEDDLE_ACT_SILU 2 /* z / (1 + exp(-z)) */
+#define HEDDLE_ACT_GELU 3 /* z (1 + erf(z / sqrt 2)) / 2 */
+
+/* y[m][n] = act(x[m][k] w[n][k]^T + bias[n]) + residual[m][n].
+ * bias, residual: nullable, of the same type.  residual may be y itself
+ * (same stride).  pre (nullable, float [m][n], row stride ldp): receives the
+ * sum before the activation, which the backward pass needs if act is not
+ * NONE.  dtype BF16 or FP16. */
+typedef struct {
+    int64_t m, n, k;
+    int32_t dtype, act;
+    const void* x;
+    int64_t ldx;
+    const void* w;
+    int64_t ldw;
+    const void* bias;
+    const void* residual;
+    int64_t ldr;
+    void* y;
+    int64_t ldy;
+    float* pre;
+    int64_t ldp;
+} heddle_linear_args;
+heddle_status heddle_linear(heddle_ctx* ctx, const heddle_linear_args* args, void* stream);
+
+/* Gradients of heddle_linear from dy = dL/dy: with dz = dy act'(pre),
+ *   dx[m][k] = dz w,  dw[n][k] = dz^T x,  dbias[n] = sum over rows of dz
+ * (the residual's gradient is dy).  Each output is nullable: not computed.
+ * x is read for dw, w for dx, pre unless act is NONE; the others may be
+ * null.  dz is rounded to the element type for the products, dbias sums it
+ * in 32 bits. */
+typedef struct {
+    int64_t m, n, k;
+    int32_t dtype, act;
+    const void* dy;
+    int64_t lddy;
+    const void* x;
+    int64_t ldx;
+    const void* w;
+    int64_t ldw;
+    const float* pre;
+    int64_t ldp;
+    void* dx;
+    int64_t lddx;
+    void* dw;
+    int64_t lddw;
+    void* dbias;
+} heddle_linear_grad_args;
+heddle_status heddle_linear_backward(heddle_ctx* ctx, const heddle_linear_grad_args* args, void* stream);
+
+/* Gated feed-forward block: gate = x w_gate^T, up = x w_up^T (both weights
+ * [n][k]), y[m][n] = act(gate) up, in one kernel.  gate, up (nullable
+ * together, float [m][n], row stride lds): receive both products for the
+ * backward pass.  dtype BF16 or FP16; any activation. */
+typedef struct {
+    int64_t m, n, k;
+    int32_t dtype, act;
+    const void* x;
+    int64_t ldx;
+    const void* w_gate;
+    int64_t ldg;
+    const void* w_up;
+    int64_t ldu;
+    void* y;
+    int64_t ldy;
+    float* gate;
+    float* up;
+    int64_t lds;
+} heddle_gated_ffn_args;
+heddle_status heddle_gated_ffn(heddle_ctx* ctx, const heddle_gated_ffn_args* args, void* stream);
+
+/* Gradients of heddle_gated_ffn from dy: with dg = dy up act'(gate) and
+ * du = dy act(gate),  dx = dg w_gate + du w_up,  dw_gate = dg^T x,
+ * dw_up = du^T x.  dx is nullable, dw_gate and dw_up are together; x is read
+ * for the weights' gradients, the weights for dx.  dg and du are rounded to
+ * the element type for the products. */
+typedef struct {
+    int64_t m, n, k;
+    int32_t dtype, act;
+    const void* dy;
+    int64_t lddy;
+    const void* x;
+    int64_t ldx;
+    const void* w_gate;
+    int64_t ldg;
+    const void* w_up;
+    int64_t ldu;
+    const float* gate;
+    const float* up;
+    int64_t lds;
+    void* dx;
+    int64_t lddx;
+    void* dw_gate;
+    void* dw_up;
+    int64_t lddw;
+} heddle_gated_ffn_grad_args;
+heddle_status heddle_gated_ffn_backward(heddle_ctx* ctx, const heddle_gated_ffn_grad_args* args, void* stream);
+
+/* A tensor of heads: element d of head h of token t of sequence b is at
+ * data[b * batch_stride + t * token_stride + h * head_stride + d]. */
+typedef struct {
+    void* data;
+    int64_t batch_stride, token_stride, head_stride;
+} heddle_heads;
+
+/* Root-mean-square norm of every head of the queries and keys and the
+ * rotation of its first rot_dim values by its token's position, in one pass:
+ *   v = x / sqrt(mean(x^2) + eps) * weight
+ *   (a, b) -> (a cos - b sin, b cos + a sin) for each pair (a, b) i of v
+ * pair i: values i and i + rot_dim / 2, or 2i and 2i + 1 (interleaved).
+ * wq, wk: [head_dim], of the same type.  positions: int32 [tokens], rows of
+ * cos and sin (float [table_len][rot_dim / 2]); a token whose position is
+ * outside the table raises bit 5 of heddle_device_errors and gets zeros
+ * (and gives no gradient).
+ * Outputs may be the inputs themselves (same strides).  Tokens are a single
+ * axis: batch strides are not read.  dtype BF16, FP16 or FP32;
+ * 1 <= head_dim <= 256, rot_dim even and at most head_dim (0: no rotation,
+ * positions, cos and sin not read); q_heads or k_heads may be 0. */
+typedef struct {
+    int64_t tokens, table_len;
+    int32_t q_heads, k_heads, head_dim, rot_dim;
+    int32_t dtype, interleaved;
+    float eps;
+    int32_t reserved;
+    heddle_heads q, k;
+    const void* wq;
+    const void* wk;
+    const int32_t* positions;
+    const float* cos;
+    const float* sin;
+    heddle_heads q_out, k_out;
+} heddle_qk_norm_rope_args;
+heddle_status heddle_qk_norm_rope(heddle_ctx* ctx, const heddle_qk_norm_rope_args* args, void* stream);
+
+/* Gradients of heddle_qk_norm_rope: fwd as in the forward call, except that
+ * q_out and k_out hold the gradients of the outputs.  dq, dk: gradients of
+ * the inputs (may be q_out and k_out themselves).  dwq, dwk: float
+ * [head_dim], the weights' gradients summed over all tokens and heads in a
+ * fixed order. */
+typedef struct {
+    heddle_qk_norm_rope_args fwd;
+    heddle_heads dq, dk;
+    float* dwq;
+    float* dwk;
+} heddle_qk_norm_rope_grad_args;
+heddle_status heddle_qk_norm_rope_backward(heddle_ctx* ctx, const heddle_qk_norm_rope_grad_args* args, void* stream);
+
+/* Attention of queries over keys with shared key heads (query head h reads
+ * key head h / (q_heads / kv_heads)), a sliding window and first tokens that
+ * stay visible.  Sequence b has q_lens[b] queries and kv_lens[b] keys
+ * (nullable device int32 [batch]: q_len and kv_len; values outside
+ * [0, q_len] and [0, kv_len] count as the nearer end); its query i stands at
+ * p = kv_lens[b] - q_lens[b] + i and sees key j if
+ *   j <= p  and  (p - j < window  or  j < sinks)
+ * (window 0: every key j <= p).  s_ij = scale q_i . k_j, P = softmax over the
+ * visible keys, o_i = sum_j P_ij v_j, lse_i = log sum exp s_ij (float
+ * [batch][q_heads][q_len], nullable).  A query that sees nothing, and rows
+ * past a sequence's queries, get o = 0 and lse = -infinity.  Keys and values
+ * past kv_lens are not used, whatever they hold; those within must be
+ * finite.  P is rounded to the element type for its product with v, its sum
+ * is not.  One query against many keys is split along the keys.
+ * dtype BF16 or FP16; 1 <= head_dim <= 256; kv_heads divides q_heads;
+ * batch * q_heads * q_len and batch * kv_heads * kv_len below 2^31. */
+typedef struct {
+    int64_t batch, q_len, kv_len;
+    int32_t q_heads, kv_heads, head_dim, dtype;
+    int64_t window, sinks;
+    float scale;
+    int32_t reserved;
+    heddle_heads q, k, v, o;
+    float* lse;
+    const int32_t* q_lens;
+    const int32_t* kv_lens;
+} heddle_attention_args;
+heddle_status heddle_attention(heddle_ctx* ctx, const heddle_attention_args* args, void* stream);
+
+/* Gradients of heddle_attention: fwd as in the forward call with its o and
+ * lse (both required, read), d_o = dL/do.  dq, dk, dv are all written (the
+ * shared heads' sums included; zeros where a row sees nothing or is past its
+ * sequence).  Sums run in a fixed order. */
+typedef struct {
+    heddle_attention_args fwd;
+    heddle_heads d_o, dq, dk, dv;
+} heddle_attention_grad_args;
+heddle_status heddle_attention_backward(heddle_ctx* ctx, const heddle_attention_grad_args* args, void* stream);
 
 #ifdef __cplusplus
 }

@@ -1,0 +1,200 @@
+// heddle_attn.cu -- attention with a sliding window and first tokens that
+// stay visible, one warp per row: any head_dim, stride and alignment.
+
+#include "heddle_ops.cuh"
+
+namespace hd {
+namespace {
+
+constexpr int kWarps = 8;
+constexpr int kVals = 8;  // values of a head a lane holds: head_dim <= 256
+
+// Queries and keys of a sequence, and how far positions are from query indices.
+struct Span {
+    int64_t ql, kl, off;
+};
+__device__ __forceinline__ Span span_of(const heddle_attention_args& a, int64_t b) {
+    Span s{a.q_len, a.kv_len, 0};
+    if (a.q_lens) s.ql = max((int64_t)0, min((int64_t)a.q_lens[b], a.q_len));
+    if (a.kv_lens) s.kl = max((int64_t)0, min((int64_t)a.kv_lens[b], a.kv_len));
+    s.off = s.kl - s.ql;
+    return s;
+}
+
+template <class T>
+__device__ __forceinline__ const T* at(const heddle_heads& t, int64_t b, int64_t i, int64_t h) {
+    return static_cast<const T*>(t.data) + b * t.batch_stride + i * t.token_stride + h * t.head_stride;
+}
+template <class T>
+__device__ __forceinline__ T* out_at(const heddle_heads& t, int64_t b, int64_t i, int64_t h) {
+    return static_cast<T*>(t.data) + b * t.batch_stride + i * t.token_stride + h * t.head_stride;
+}
+
+template <class T>
+__device__ __forceinline__ void load_row(const T* p, int D, int lane, float (&v)[kVals]) {
+#pragma unroll
+    for (int j = 0; j < kVals; ++j) v[j] = lane + 32 * j < D ? to_float(p[lane + 32 * j]) : 0.0f;
+}
+template <class T>
+__device__ __forceinline__ void store_row(T* p, int D, int lane, const float (&v)[kVals], float f) {
+#pragma unroll
+    for (int j = 0; j < kVals; ++j)
+        if (lane + 32 * j < D) p[lane + 32 * j] = from_float<T>(v[j] * f);
+}
+__device__ __forceinline__ float dot_rows(const float (&a)[kVals], const float (&b)[kVals]) {
+    float s = 0.0f;
+#pragma unroll
+    for (int j = 0; j < kVals; ++j) s += a[j] * b[j];
+    return warp_sum(s);
+}
+
+template <class T>
+__global__ void __launch_bounds__(kWarps * 32) attn_row_kernel(heddle_attention_args a) {
+    const int lane = threadIdx.x % 32, D = a.head_dim;
+    const int64_t rows = a.batch * a.q_heads * a.q_len;
+    for (int64_t r = (int64_t)blockIdx.x * kWarps + threadIdx.x / 32; r < rows; r += (int64_t)gridDim.x * kWarps) {
+        const int64_t b = r / (a.q_heads * a.q_len), h = r / a.q_len % a.q_heads, i = r % a.q_len;
+        const int64_t hk = h / (a.q_heads / a.kv_heads);
+        const Span s = span_of(a, b);
+        const int64_t p = i < s.ql ? s.off + i : -1;
+        float q[kVals], o[kVals] = {}, m = -INFINITY, l = 0.0f;
+        load_row(at<T>(a.q, b, i, h), D, lane, q);
+        const int64_t low = a.window && p - a.window + 1 > 0 ? p - a.window + 1 : 0;
+        for (int64_t j = 0; j <= p; ++j) {
+            if (j < low && j >= a.sinks) j = low;
+            float k[kVals], v[kVals];
+            load_row(at<T>(a.k, b, j, hk), D, lane, k);
+            load_row(at<T>(a.v, b, j, hk), D, lane, v);
+            const float sc = dot_rows(q, k) * a.scale;
+            const float top = fmaxf(m, sc);
+            const float keep = m == -INFINITY ? 0.0f : expf(m - top), w = expf(sc - top);
+            l = l * keep + w;
+#pragma unroll
+            for (int x = 0; x < kVals; ++x) o[x] = o[x] * keep + w * v[x];
+            m = top;
+        }
+        store_row(out_at<T>(a.o, b, i, h), D, lane, o, l > 0.0f ? 1.0f / l : 0.0f);
+        if (a.lse && lane == 0) a.lse[r] = l > 0.0f ? m + logf(l) : -INFINITY;
+    }
+}
+
+// delta_i = do_i . o_i
+template <class T>
+__global__ void __launch_bounds__(kWarps * 32) attn_delta_kernel(heddle_attention_grad_args g, float* delta) {
+    const heddle_attention_args& a = g.fwd;
+    const int lane = threadIdx.x % 32, D = a.head_dim;
+    const int64_t rows = a.batch * a.q_heads * a.q_len;
+    for (int64_t r = (int64_t)blockIdx.x * kWarps + threadIdx.x / 32; r < rows; r += (int64_t)gridDim.x * kWarps) {
+        const int64_t b = r / (a.q_heads * a.q_len), h = r / a.q_len % a.q_heads, i = r % a.q_len;
+        float o[kVals], d[kVals];
+        load_row(at<T>(a.o, b, i, h), D, lane, o);
+        load_row(at<T>(g.d_o, b, i, h), D, lane, d);
+        const float s = dot_rows(o, d);
+        if (lane == 0) delta[r] = s;
+    }
+}
+
+template <class T>
+__global__ void __launch_bounds__(kWarps * 32) attn_dq_row_kernel(heddle_attention_grad_args g, const float* delta) {
+    const heddle_attention_args& a = g.fwd;
+    const int lane = threadIdx.x % 32, D = a.head_dim;
+    const int64_t rows = a.batch * a.q_heads * a.q_len;
+    for (int64_t r = (int64_t)blockIdx.x * kWarps + threadIdx.x / 32; r < rows; r += (int64_t)gridDim.x * kWarps) {
+        const int64_t b = r / (a.q_heads * a.q_len), h = r / a.q_len % a.q_heads, i = r % a.q_len;
+        const int64_t hk = h / (a.q_heads / a.kv_heads);
+        const Span s = span_of(a, b);
+        const int64_t p = i < s.ql ? s.off + i : -1;
+        float q[kVals], d[kVals], dq[kVals] = {};
+        load_row(at<T>(a.q, b, i, h), D, lane, q);
+        load_row(at<T>(g.d_o, b, i, h), D, lane, d);
+        const float lse = a.lse[r], dl = delta[r];
+        const int64_t low = a.window && p - a.window + 1 > 0 ? p - a.window + 1 : 0;
+        for (int64_t j = 0; j <= p; ++j) {
+            if (j < low && j >= a.sinks) j = low;
+            float k[kVals], v[kVals];
+            load_row(at<T>(a.k, b, j, hk), D, lane, k);
+            load_row(at<T>(a.v, b, j, hk), D, lane, v);
+            const float w = expf(dot_rows(q, k) * a.scale - lse);
+            const float ds = w * (dot_rows(d, v) - dl) * a.scale;
+#pragma unroll
+            for (int x = 0; x < kVals; ++x) dq[x] += ds * k[x];
+        }
+        store_row(out_at<T>(g.dq, b, i, h), D, lane, dq, 1.0f);
+    }
+}
+
+template <class T>
+__global__ void __launch_bounds__(kWarps * 32) attn_dkv_row_kernel(heddle_attention_grad_args g, const float* delta) {
+    const heddle_attention_args& a = g.fwd;
+    const int lane = threadIdx.x % 32, D = a.head_dim;
+    const int64_t rows = a.batch * a.kv_heads * a.kv_len, group = a.q_heads / a.kv_heads;
+    for (int64_t r = (int64_t)blockIdx.x * kWarps + threadIdx.x / 32; r < rows; r += (int64_t)gridDim.x * kWarps) {
+        const int64_t b = r / (a.kv_heads * a.kv_len), hk = r / a.kv_len % a.kv_heads, j = r % a.kv_len;
+        const Span s = span_of(a, b);
+        float k[kVals], v[kVals], dk[kVals] = {}, dv[kVals] = {};
+        load_row(at<T>(a.k, b, j, hk), D, lane, k);
+        load_row(at<T>(a.v, b, j, hk), D, lane, v);
+        const int64_t first = max((int64_t)0, j - s.off);
+        int64_t last = j < s.kl ? s.ql : 0;
+        if (a.window && j >= a.sinks) last = min(last, j + a.window - s.off);
+        for (int64_t h = hk * group; h < (hk + 1) * group; ++h)
+            for (int64_t i = first; i < last; ++i) {
+                float q[kVals], d[kVals];
+                load_row(at<T>(a.q, b, i, h), D, lane, q);
+                load_row(at<T>(g.d_o, b, i, h), D, lane, d);
+                const int64_t at_row = (b * a.q_heads + h) * a.q_len + i;
+                const float w = expf(dot_rows(q, k) * a.scale - a.lse[at_row]);
+                const float ds = w * (dot_rows(d, v) - delta[at_row]) * a.scale;
+#pragma unroll
+                for (int x = 0; x < kVals; ++x) {
+                    dv[x] += w * d[x];
+                    dk[x] += ds * q[x];
+                }
+            }
+        store_row(out_at<T>(g.dk, b, j, hk), D, lane, dk, 1.0f);
+        store_row(out_at<T>(g.dv, b, j, hk), D, lane, dv, 1.0f);
+    }
+}
+
+unsigned row_blocks(const OpContext& x, int64_t rows) {
+    const int64_t most = (int64_t)x.num_sms * 64;
+    return (unsigned)(ceil_div(rows, kWarps) < most ? ceil_div(rows, kWarps) : most);
+}
+
+template <class T>
+cudaError_t attention_grad(const OpContext& x, const heddle_attention_grad_args& g, float* delta, cudaStream_t st) {
+    const heddle_attention_args& a = g.fwd;
+    const int64_t rows = a.batch * a.q_heads * a.q_len, keys = a.batch * a.kv_heads * a.kv_len;
+    if (rows) {
+        attn_delta_kernel<T><<<row_blocks(x, rows), kWarps * 32, 0, st>>>(g, delta);
+        attn_dq_row_kernel<T><<<row_blocks(x, rows), kWarps * 32, 0, st>>>(g, delta);
+    }
+    if (keys) attn_dkv_row_kernel<T><<<row_blocks(x, keys), kWarps * 32, 0, st>>>(g, delta);
+    return cudaGetLastError();
+}
+
+}  // namespace
+
+size_t attention_scratch(const OpContext&, const heddle_attention_args&) { return 0; }
+
+cudaError_t launch_attention(const OpContext& x, const heddle_attention_args& a, unsigned char*, cudaStream_t st) {
+    const unsigned grid = row_blocks(x, a.batch * a.q_heads * a.q_len);
+    if (a.dtype == HEDDLE_BF16)
+        attn_row_kernel<__nv_bfloat16><<<grid, kWarps * 32, 0, st>>>(a);
+    else
+        attn_row_kernel<__half><<<grid, kWarps * 32, 0, st>>>(a);
+    return cudaGetLastError();
+}
+
+size_t attention_grad_scratch(const OpContext&, const heddle_attention_grad_args& g) {
+    return align256(sizeof(float) * (size_t)(g.fwd.batch * g.fwd.q_heads * g.fwd.q_len));
+}
+
+cudaError_t launch_attention_grad(const OpContext& x, const heddle_attention_grad_args& g, unsigned char* ws,
+                                  cudaStream_t st) {
+    float* delta = reinterpret_cast<float*>(ws);
+    return g.fwd.dtype == HEDDLE_BF16 ? attention_grad<__nv_bfloat16>(x, g, delta, st)
+                                      : attention_grad<__half>(x, g, delta, st);
+}
+
+}  // namespace hd

@@ -9,6 +9,7 @@
 #include <algorithm>
 #include <vector>
 
+#include "heddle_ops.cuh"
 #include "heddle_tiled.cuh"
 
 using hd::Layout;
@@ -17,6 +18,7 @@ struct heddle_ctx {
     int device = 0;
     int num_sms = 0;
     char msg[512] = {0};
+    hd::OpContext op;  // the layer operators' part
     // host copies of the descriptions
     std::vector<heddle_gpu_type> types;
     std::vector<heddle_node> nodes;
@@ -465,6 +467,8 @@ void free_worklist(heddle_ctx::Worklist& w) {
 
 }  // namespace
 
+hd::OpContext* heddle_op_context(heddle_ctx* x) { return &x->op; }
+
 extern "C" {
 
 heddle_status heddle_create(heddle_ctx** out, int32_t device) {
@@ -496,6 +500,11 @@ heddle_status heddle_create(heddle_ctx** out, int32_t device) {
     if (e == cudaSuccess) e = cudaMalloc(&x->d_meet, meet);
     if (e == cudaSuccess) e = cudaMemset(x->d_meet, 0, meet);
 
+    x->op.device = device;
+    x->op.num_sms = x->num_sms;
+    x->op.err = x->d_flags + 1;
+    x->op.msg = x->msg;
+    x->op.msg_size = sizeof(x->msg);
     if (e != cudaSuccess) {
         heddle_destroy(x);
         return HEDDLE_E_CUDA;
@@ -549,6 +558,7 @@ void heddle_destroy(heddle_ctx* x) {
         cudaFree(x->lv_status[i]);
         cudaFree(x->lv_bounds[i]);
     }
+    cudaFree(x->op.ws);
     cudaFree(x->d_timg);
     cudaFree(x->d_node_type);
     cudaFree(x->d_node_gpus);

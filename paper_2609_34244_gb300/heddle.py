@@ -76,13 +76,73 @@ class heddle_topk_state(C.Structure):
 
 TOPK_STATE_BYTES = C.sizeof(heddle_topk_state)
 
+# layer operators
+BF16, FP16, FP32 = 0, 1, 2
+ACT_NONE, ACT_RELU, ACT_SILU, ACT_GELU = 0, 1, 2, 3
+ACTIVATIONS = {"none": ACT_NONE, "relu": ACT_RELU, "silu": ACT_SILU, "gelu": ACT_GELU}
+
+
+def _fields(spec):
+    kinds = {"q": C.c_int64, "i": C.c_int32, "f": C.c_float, "p": C.c_void_p}
+    return [(name, kinds[kind] if isinstance(kind, str) else kind)
+            for kind, names in spec for name in names.split()]
+
+
+class heddle_linear_args(C.Structure):
+    _fields_ = _fields([("q", "m n k"), ("i", "dtype act"), ("p", "x"), ("q", "ldx"), ("p", "w"), ("q", "ldw"),
+                        ("p", "bias residual"), ("q", "ldr"), ("p", "y"), ("q", "ldy"), ("p", "pre"), ("q", "ldp")])
+
+
+class heddle_linear_grad_args(C.Structure):
+    _fields_ = _fields([("q", "m n k"), ("i", "dtype act"), ("p", "dy"), ("q", "lddy"), ("p", "x"), ("q", "ldx"),
+                        ("p", "w"), ("q", "ldw"), ("p", "pre"), ("q", "ldp"), ("p", "dx"), ("q", "lddx"),
+                        ("p", "dw"), ("q", "lddw"), ("p", "dbias")])
+
+
+class heddle_gated_ffn_args(C.Structure):
+    _fields_ = _fields([("q", "m n k"), ("i", "dtype act"), ("p", "x"), ("q", "ldx"), ("p", "w_gate"), ("q", "ldg"),
+                        ("p", "w_up"), ("q", "ldu"), ("p", "y"), ("q", "ldy"), ("p", "gate up"), ("q", "lds")])
+
+
+class heddle_gated_ffn_grad_args(C.Structure):
+    _fields_ = _fields([("q", "m n k"), ("i", "dtype act"), ("p", "dy"), ("q", "lddy"), ("p", "x"), ("q", "ldx"),
+                        ("p", "w_gate"), ("q", "ldg"), ("p", "w_up"), ("q", "ldu"), ("p", "gate up"), ("q", "lds"),
+                        ("p", "dx"), ("q", "lddx"), ("p", "dw_gate dw_up"), ("q", "lddw")])
+
+
+class heddle_heads(C.Structure):
+    _fields_ = _fields([("p", "data"), ("q", "batch_stride token_stride head_stride")])
+
+
+class heddle_qk_norm_rope_args(C.Structure):
+    _fields_ = _fields([("q", "tokens table_len"), ("i", "q_heads k_heads head_dim rot_dim dtype interleaved"),
+                        ("f", "eps"), ("i", "reserved"), (heddle_heads, "q k"), ("p", "wq wk positions cos sin"),
+                        (heddle_heads, "q_out k_out")])
+
+
+class heddle_qk_norm_rope_grad_args(C.Structure):
+    _fields_ = [("fwd", heddle_qk_norm_rope_args), ("dq", heddle_heads), ("dk", heddle_heads),
+                ("dwq", C.c_void_p), ("dwk", C.c_void_p)]
+
+
+class heddle_attention_args(C.Structure):
+    _fields_ = _fields([("q", "batch q_len kv_len"), ("i", "q_heads kv_heads head_dim dtype"), ("q", "window sinks"),
+                        ("f", "scale"), ("i", "reserved"), (heddle_heads, "q k v o"), ("p", "lse q_lens kv_lens")])
+
+
+class heddle_attention_grad_args(C.Structure):
+    _fields_ = [("fwd", heddle_attention_args), ("d_o", heddle_heads), ("dq", heddle_heads), ("dk", heddle_heads),
+                ("dv", heddle_heads)]
+
 EXPORTS = ["heddle_create", "heddle_destroy", "heddle_last_error", "heddle_load_cluster",
            "heddle_load_model", "heddle_price_candidates", "heddle_topk_reset", "heddle_topk",
            "heddle_price_topk_host", "heddle_get_tables", "heddle_device_errors",
            "heddle_count_next", "heddle_work_counters", "heddle_set_search", "heddle_get_search", "heddle_set_thread_search_min",
            "heddle_price_topk", "heddle_topk_noalloc", "heddle_time_phases", "heddle_phase_times",
            "heddle_load_mbs", "heddle_price_mbs", "heddle_price_plans", "heddle_load_experts",
-           "heddle_price_tiled", "heddle_set_chunk"]
+           "heddle_price_tiled", "heddle_set_chunk",
+           "heddle_linear", "heddle_linear_backward", "heddle_gated_ffn", "heddle_gated_ffn_backward",
+           "heddle_qk_norm_rope", "heddle_qk_norm_rope_backward", "heddle_attention", "heddle_attention_backward"]
 MAX_MBS_LEVELS = 4
 PHASES = ("screen", "search", "topk")
 TOPK_NOALLOC_MAX_N = 4194304
@@ -127,6 +187,14 @@ def load_library(path: str = LIB_PATH):
         "heddle_price_tiled": (i32, [p, p, p, p, p]),
         "heddle_set_chunk": (i32, [p, i64]),
         "heddle_phase_times": (i32, [p, C.POINTER(C.c_double), C.POINTER(C.c_int64)]),
+        "heddle_linear": (i32, [p, p, p]),
+        "heddle_linear_backward": (i32, [p, p, p]),
+        "heddle_gated_ffn": (i32, [p, p, p]),
+        "heddle_gated_ffn_backward": (i32, [p, p, p]),
+        "heddle_qk_norm_rope": (i32, [p, p, p]),
+        "heddle_qk_norm_rope_backward": (i32, [p, p, p]),
+        "heddle_attention": (i32, [p, p, p]),
+        "heddle_attention_backward": (i32, [p, p, p]),
     }
     for name, (res, args) in sig.items():
         f = getattr(L, name)
@@ -404,6 +472,207 @@ def heddle_get_search(ctx) -> int:
     m = C.c_int32(0)
     _check(ctx, load_library().heddle_get_search(ctx, C.byref(m)))
     return int(m.value)
+
+
+# ------------------------------------------------------- layer operators
+#
+# Tensors are torch CUDA tensors of one element type (named outputs and saved
+# values float32), their last axis contiguous; every output is given by the
+# caller.  Shapes and types are checked here, since the C structs carry only
+# one set of sizes; everything else is checked by the library.
+
+_OP_TYPES = {}
+
+
+def _op_dtype(t) -> int:
+    if not _OP_TYPES:
+        import torch
+        _OP_TYPES.update({torch.bfloat16: BF16, torch.float16: FP16, torch.float32: FP32})
+    code = _OP_TYPES.get(t.dtype)
+    if code is None:
+        raise HeddleError(E_ARG, "unsupported element type %s" % t.dtype)
+    return code
+
+
+def _bad(what, t, shape, dtype):
+    raise HeddleError(E_ARG, "%s: expected a CUDA tensor %s of %s with a contiguous last axis, got %s of %s on %s"
+                      % (what, tuple(shape), dtype, tuple(t.shape), t.dtype, t.device))
+
+
+def _mat(what, t, rows, cols, dtype, device):
+    """(address, row stride) of a [rows][cols] tensor; (None, 0) for None."""
+    if t is None:
+        return None, 0
+    if t.dtype != dtype or t.device != device or tuple(t.shape) != (rows, cols):
+        _bad(what, t, (rows, cols), dtype)
+    ld, inner = t.stride()
+    if inner != 1 and cols > 1:
+        _bad(what, t, (rows, cols), dtype)
+    return t.data_ptr(), ld if rows > 1 else max(ld, cols)
+
+
+def _vec(what, t, n, dtype, device):
+    if t is None:
+        return None
+    if t.dtype != dtype or t.device != device or tuple(t.shape) != (n,) or (n > 1 and t.stride(0) != 1):
+        _bad(what, t, (n,), dtype)
+    return t.data_ptr()
+
+
+def _heads(what, t, shape, dtype, device):
+    """heddle_heads of a [batch][tokens][heads][head_dim] tensor, or one
+    without the batch axis."""
+    if t.dtype != dtype or t.device != device or t.shape != shape:
+        _bad(what, t, shape, dtype)
+    st = t.stride()
+    if st[-1] != 1 and shape[-1] > 1:
+        _bad(what, t, shape, dtype)
+    return heddle_heads(t.data_ptr(), st[0] if len(st) == 4 else 0, st[-3], st[-2])
+
+
+def _two_axes(what, t):
+    if t.dim() != 2 or not t.is_cuda:
+        raise HeddleError(E_ARG, "%s: expected a CUDA tensor of two axes, got %s on %s"
+                          % (what, tuple(t.shape), t.device))
+    return t.shape
+
+
+def heddle_linear(ctx, x, w, y, bias=None, residual=None, act=ACT_NONE, pre=None, stream=None):
+    """y = act(x w^T + bias) + residual; ``pre`` receives the sum before act."""
+    (m, k), (n, _) = _two_axes("x", x), _two_axes("w", w)
+    dt, dev = x.dtype, x.device
+    a = heddle_linear_args(m, n, k, _op_dtype(x), act, *_mat("x", x, m, k, dt, dev), *_mat("w", w, n, k, dt, dev),
+                           _vec("bias", bias, n, dt, dev), *_mat("residual", residual, m, n, dt, dev),
+                           *_mat("y", y, m, n, dt, dev), *_mat("pre", pre, m, n, _f32(), dev))
+    _check(ctx, load_library().heddle_linear(ctx, C.byref(a), _stream(stream)))
+
+
+def _f32():
+    import torch
+    return torch.float32
+
+
+def heddle_linear_backward(ctx, dy, x, w, act=ACT_NONE, pre=None, dx=None, dw=None, dbias=None, stream=None):
+    """Gradients of heddle_linear; an output that is None is not computed."""
+    (m, k), (n, _) = _two_axes("x", x), _two_axes("w", w)
+    dt, dev = x.dtype, x.device
+    a = heddle_linear_grad_args(m, n, k, _op_dtype(x), act, *_mat("dy", dy, m, n, dt, dev),
+                                *_mat("x", x, m, k, dt, dev), *_mat("w", w, n, k, dt, dev),
+                                *_mat("pre", pre, m, n, _f32(), dev), *_mat("dx", dx, m, k, dt, dev),
+                                *_mat("dw", dw, n, k, dt, dev), _vec("dbias", dbias, n, dt, dev))
+    _check(ctx, load_library().heddle_linear_backward(ctx, C.byref(a), _stream(stream)))
+
+
+def _same_stride(what, a, b):
+    if a[1] != b[1]:
+        raise HeddleError(E_ARG, "%s have different row strides" % what)
+    return a[0], b[0], a[1]
+
+
+def heddle_gated_ffn(ctx, x, w_gate, w_up, y, act=ACT_SILU, gate=None, up=None, stream=None):
+    """y = act(x w_gate^T) * (x w_up^T); ``gate`` and ``up`` receive the products."""
+    (m, k), (n, _) = _two_axes("x", x), _two_axes("w_gate", w_gate)
+    dt, dev = x.dtype, x.device
+    saved = _same_stride("gate and up", _mat("gate", gate, m, n, _f32(), dev), _mat("up", up, m, n, _f32(), dev))
+    a = heddle_gated_ffn_args(m, n, k, _op_dtype(x), act, *_mat("x", x, m, k, dt, dev),
+                              *_mat("w_gate", w_gate, n, k, dt, dev), *_mat("w_up", w_up, n, k, dt, dev),
+                              *_mat("y", y, m, n, dt, dev), *saved)
+    _check(ctx, load_library().heddle_gated_ffn(ctx, C.byref(a), _stream(stream)))
+
+
+def heddle_gated_ffn_backward(ctx, dy, x, w_gate, w_up, gate, up, act=ACT_SILU, dx=None, dwg=None, dwu=None,
+                              stream=None):
+    """Gradients of heddle_gated_ffn (dwg and dwu, those of w_gate and
+    w_up, together); an output
+    that is None is not computed."""
+    (m, k), (n, _) = _two_axes("x", x), _two_axes("w_gate", w_gate)
+    dt, dev = x.dtype, x.device
+    saved = _same_stride("gate and up", _mat("gate", gate, m, n, _f32(), dev), _mat("up", up, m, n, _f32(), dev))
+    dw = _same_stride("dwg and dwu", _mat("dwg", dwg, n, k, dt, dev),
+                      _mat("dwu", dwu, n, k, dt, dev))
+    a = heddle_gated_ffn_grad_args(m, n, k, _op_dtype(x), act, *_mat("dy", dy, m, n, dt, dev),
+                                   *_mat("x", x, m, k, dt, dev), *_mat("w_gate", w_gate, n, k, dt, dev),
+                                   *_mat("w_up", w_up, n, k, dt, dev), *saved, *_mat("dx", dx, m, k, dt, dev), *dw)
+    _check(ctx, load_library().heddle_gated_ffn_backward(ctx, C.byref(a), _stream(stream)))
+
+
+def _norm_rope_args(q, k, wq, wk, q_out, k_out, positions, cos, sin, eps, interleaved):
+    if q.dim() != 3 or k.dim() != 3 or not q.is_cuda:
+        raise HeddleError(E_ARG, "q and k: expected CUDA tensors [tokens][heads][head_dim]")
+    dt, dev = q.dtype, q.device
+    t, hq, d = q.shape
+    hk = k.shape[1]
+    rot = table = 0
+    ptrs = (None, None, None)
+    if positions is not None:
+        import torch
+        table, half = _two_axes("cos", cos)
+        rot = 2 * half
+        if not (cos.is_contiguous() and sin.is_contiguous()):
+            raise HeddleError(E_ARG, "cos and sin are contiguous")
+        ptrs = (_vec("positions", positions, t, torch.int32, dev), _mat("cos", cos, table, half, _f32(), dev)[0],
+                _mat("sin", sin, table, half, _f32(), dev)[0])
+    return heddle_qk_norm_rope_args(t, table, hq, hk, d, rot, _op_dtype(q), int(bool(interleaved)), eps, 0,
+                                    _heads("q", q, q.shape, dt, dev), _heads("k", k, (t, hk, d), dt, dev),
+                                    _vec("wq", wq, d, dt, dev), _vec("wk", wk, d, dt, dev), *ptrs,
+                                    _heads("q_out", q_out, q.shape, dt, dev), _heads("k_out", k_out, k.shape, dt, dev))
+
+
+def heddle_qk_norm_rope(ctx, q, k, wq, wk, q_out, k_out, positions=None, cos=None, sin=None, eps=1e-6,
+                        interleaved=False, stream=None):
+    """Norms and rotation of q and k ([tokens][heads][head_dim]); cos and sin
+    are float32 [table_len][rot_dim / 2], no rotation without positions."""
+    a = _norm_rope_args(q, k, wq, wk, q_out, k_out, positions, cos, sin, eps, interleaved)
+    _check(ctx, load_library().heddle_qk_norm_rope(ctx, C.byref(a), _stream(stream)))
+
+
+def heddle_qk_norm_rope_backward(ctx, dq_out, dk_out, q, k, wq, wk, dq, dk, dwq, dwk, positions=None, cos=None,
+                                 sin=None, eps=1e-6, interleaved=False, stream=None):
+    """Gradients of heddle_qk_norm_rope from those of its outputs; dwq and dwk
+    are float32 [head_dim]."""
+    f = _norm_rope_args(q, k, wq, wk, dq_out, dk_out, positions, cos, sin, eps, interleaved)
+    dt, dev, d = q.dtype, q.device, q.shape[2]
+    a = heddle_qk_norm_rope_grad_args(f, _heads("dq", dq, q.shape, dt, dev), _heads("dk", dk, k.shape, dt, dev),
+                                      _vec("dwq", dwq, d, _f32(), dev), _vec("dwk", dwk, d, _f32(), dev))
+    _check(ctx, load_library().heddle_qk_norm_rope_backward(ctx, C.byref(a), _stream(stream)))
+
+
+def _attention_args(q, k, v, o, lse, q_lens, kv_lens, window, sinks, scale):
+    if q.dim() != 4 or k.dim() != 4 or not q.is_cuda:
+        raise HeddleError(E_ARG, "q and k: expected CUDA tensors [batch][tokens][heads][head_dim]")
+    dt, dev = q.dtype, q.device
+    b, tq, hq, d = q.shape
+    tk, hk = k.shape[1:3]
+    keys = (b, tk, hk, d)
+    if lse is not None and (lse.dtype != _f32() or lse.device != dev or lse.shape != (b, hq, tq)
+                            or not lse.is_contiguous()):
+        _bad("lse", lse, (b, hq, tq), "float32")
+    lens = (None, None)
+    if q_lens is not None or kv_lens is not None:
+        import torch
+        lens = (_vec("q_lens", q_lens, b, torch.int32, dev), _vec("kv_lens", kv_lens, b, torch.int32, dev))
+    return heddle_attention_args(b, tq, tk, hq, hk, d, _op_dtype(q), window, sinks,
+                                 d ** -0.5 if scale is None else scale, 0,
+                                 _heads("q", q, q.shape, dt, dev), _heads("k", k, keys, dt, dev),
+                                 _heads("v", v, keys, dt, dev), _heads("o", o, q.shape, dt, dev), _ptr(lse), *lens)
+
+
+def heddle_attention(ctx, q, k, v, o, lse=None, q_lens=None, kv_lens=None, window=0, sinks=0, scale=None,
+                     stream=None):
+    """Causal attention of q over k and v ([batch][tokens][heads][head_dim])
+    with a sliding window (0: none) and sinks; scale None: head_dim ** -0.5."""
+    a = _attention_args(q, k, v, o, lse, q_lens, kv_lens, window, sinks, scale)
+    _check(ctx, load_library().heddle_attention(ctx, C.byref(a), _stream(stream)))
+
+
+def heddle_attention_backward(ctx, do, q, k, v, o, lse, dq, dk, dv, q_lens=None, kv_lens=None, window=0, sinks=0,
+                              scale=None, stream=None):
+    """Gradients of heddle_attention from ``do``, with its o and lse."""
+    f = _attention_args(q, k, v, o, lse, q_lens, kv_lens, window, sinks, scale)
+    dt, dev = q.dtype, q.device
+    a = heddle_attention_grad_args(f, _heads("do", do, q.shape, dt, dev), _heads("dq", dq, q.shape, dt, dev),
+                                   _heads("dk", dk, k.shape, dt, dev), _heads("dv", dv, k.shape, dt, dev))
+    _check(ctx, load_library().heddle_attention_backward(ctx, C.byref(a), _stream(stream)))
 
 
 # ------------------------------------------------------------- marshalling helpers

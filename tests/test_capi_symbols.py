@@ -82,3 +82,23 @@ def test_missing_library_fails_loudly(tmp_path):
                        timeout=300)
     assert p.returncode == 0, p.stderr[-2000:]
     assert "raised:" in p.stdout and "not built" in p.stdout
+
+
+def test_operator_struct_layouts_match_header(heddle_lib, tmp_path):
+    import ctypes as C
+    names = ["linear_args", "linear_grad_args", "gated_ffn_args", "gated_ffn_grad_args", "heads",
+             "qk_norm_rope_args", "qk_norm_rope_grad_args", "attention_args", "attention_grad_args"]
+    lines, want = [], []
+    for n in names:
+        t = getattr(heddle_lib, "heddle_" + n)
+        lines.append('printf("%%zu\\n", sizeof(heddle_%s));' % n)
+        want.append(C.sizeof(t))
+        for field, _ in t._fields_:
+            lines.append('printf("%%zu\\n", offsetof(heddle_%s, %s));' % (n, field))
+            want.append(getattr(t, field).offset)
+    src = tmp_path / "op.c"
+    src.write_text('#include <stdio.h>\n#include <stddef.h>\n#include "heddle.h"\nint main(void) {\n%s\nreturn 0; }\n'
+                   % "\n".join(lines))
+    exe = tmp_path / "op"
+    subprocess.check_call(["gcc", "-std=c11", "-I", os.path.join(ROOT, "include"), str(src), "-o", str(exe)])
+    assert [int(v) for v in subprocess.check_output([str(exe)], text=True).split()] == want
