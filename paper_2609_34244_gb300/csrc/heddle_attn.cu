@@ -1,25 +1,13 @@
 // heddle_attn.cu -- attention with a sliding window and first tokens that
 // stay visible, one warp per row: any head_dim, stride and alignment.
 
-#include "heddle_ops.cuh"
+#include "heddle_attn.cuh"
 
 namespace hd {
 namespace {
 
 constexpr int kWarps = 8;
 constexpr int kVals = 8;  // values of a head a lane holds: head_dim <= 256
-
-// Queries and keys of a sequence, and how far positions are from query indices.
-struct Span {
-    int64_t ql, kl, off;
-};
-__device__ __forceinline__ Span span_of(const heddle_attention_args& a, int64_t b) {
-    Span s{a.q_len, a.kv_len, 0};
-    if (a.q_lens) s.ql = max((int64_t)0, min((int64_t)a.q_lens[b], a.q_len));
-    if (a.kv_lens) s.kl = max((int64_t)0, min((int64_t)a.kv_lens[b], a.kv_len));
-    s.off = s.kl - s.ql;
-    return s;
-}
 
 template <class T>
 __device__ __forceinline__ const T* at(const heddle_heads& t, int64_t b, int64_t i, int64_t h) {
@@ -165,8 +153,12 @@ template <class T>
 cudaError_t attention_grad(const OpContext& x, const heddle_attention_grad_args& g, float* delta, cudaStream_t st) {
     const heddle_attention_args& a = g.fwd;
     const int64_t rows = a.batch * a.q_heads * a.q_len, keys = a.batch * a.kv_heads * a.kv_len;
+    if (rows) attn_delta_kernel<T><<<row_blocks(x, rows), kWarps * 32, 0, st>>>(g, delta);
+    if (attn_tc_takes_grad(g)) {
+        const cudaError_t e = cudaGetLastError();
+        return e == cudaSuccess ? launch_attn_tc_grad(x, g, delta, st) : e;
+    }
     if (rows) {
-        attn_delta_kernel<T><<<row_blocks(x, rows), kWarps * 32, 0, st>>>(g, delta);
         attn_dq_row_kernel<T><<<row_blocks(x, rows), kWarps * 32, 0, st>>>(g, delta);
     }
     if (keys) attn_dkv_row_kernel<T><<<row_blocks(x, keys), kWarps * 32, 0, st>>>(g, delta);
@@ -175,9 +167,12 @@ cudaError_t attention_grad(const OpContext& x, const heddle_attention_grad_args&
 
 }  // namespace
 
-size_t attention_scratch(const OpContext&, const heddle_attention_args&) { return 0; }
+size_t attention_scratch(const OpContext& x, const heddle_attention_args& a) {
+    return attn_tc_takes(a) ? attn_tc_scratch(x, a) : 0;
+}
 
-cudaError_t launch_attention(const OpContext& x, const heddle_attention_args& a, unsigned char*, cudaStream_t st) {
+cudaError_t launch_attention(const OpContext& x, const heddle_attention_args& a, unsigned char* ws, cudaStream_t st) {
+    if (attn_tc_takes(a)) return launch_attn_tc(x, a, ws, st);
     const unsigned grid = row_blocks(x, a.batch * a.q_heads * a.q_len);
     if (a.dtype == HEDDLE_BF16)
         attn_row_kernel<__nv_bfloat16><<<grid, kWarps * 32, 0, st>>>(a);

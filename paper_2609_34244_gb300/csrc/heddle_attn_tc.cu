@@ -1,0 +1,1001 @@
+// heddle_attn_tc.cu -- attention with a sliding window and first tokens that
+// stay visible on the tensor cores, forward and backward.
+//
+// A tile's 128 rows are the queries of consecutive tokens under one key head:
+// row r is query head r % G of the group's G on token r / G, so that a key
+// tile read once serves the whole group.  Rows past G * (128 / G) are empty.
+// Scores and their gradients stay in tensor memory: the weights P (and dS)
+// are written back over the scores as the 16-bit left operand of the next
+// product.
+
+#include "heddle_attn.cuh"
+#include "heddle_tc.cuh"
+
+namespace hd {
+namespace {
+
+using namespace tc;
+
+constexpr int kTile = 128;
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.69314718055994531f;
+// A row's maximum is kept until a score passes it by this many powers of two:
+// weights stay below 2^8, far inside the range of 16-bit types, and the sums
+// are rarely scaled again.
+constexpr float kSlack = 8.0f;
+
+__device__ __forceinline__ float exp2_fast(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+
+// Two floats to 16-bit values, the first in the low half.
+template <class T>
+__device__ __forceinline__ uint32_t pack_two(float lo, float hi);
+template <>
+__device__ __forceinline__ uint32_t pack_two<__nv_bfloat16>(float lo, float hi) {
+    uint32_t r;
+    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+template <>
+__device__ __forceinline__ uint32_t pack_two<__half>(float lo, float hi) {
+    uint32_t r;
+    asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+
+struct Params {
+    heddle_attention_args a;
+    heddle_heads d_o, dq, dk, dv;
+    const float* delta;
+    int32_t group, tokens;  // G, tokens of a tile
+    int32_t q_tiles, kv_tiles;
+    int32_t splits;
+    float scale_log2;
+    float* part_o;    // [splits][batch * q_heads * q_len][head_dim]
+    float* part_lse;  // [splits][batch * q_heads * q_len]
+    uint32_t* err;
+};
+
+// The key tiles that a range of queries sees: those of the first tokens ahead
+// of the window's, then the window's.
+struct KeyTiles {
+    int lead, first, count;  // lead tiles from 0, then from `first` on; count of both
+    __device__ int at(int j) const { return j < lead ? j : first + j - lead; }
+};
+__device__ __forceinline__ KeyTiles key_tiles(const Params& p, const Span& s, int64_t i0, int64_t i1) {
+    KeyTiles k{0, 0, 0};
+    i1 = min(i1, s.ql);
+    if (i0 >= i1) return k;
+    const int64_t hi = min(s.off + i1 - 1, s.kl - 1);
+    if (hi < 0) return k;
+    int64_t lo = 0;
+    if (p.a.window) lo = max((int64_t)0, s.off + i0 - p.a.window + 1);
+    k.first = (int)(lo / kTile);
+    const int last = (int)(hi / kTile);
+    const int64_t sinks = min(p.a.sinks, hi + 1);
+    k.lead = min((int)((sinks + kTile - 1) / kTile), k.first);
+    k.count = k.lead + last - k.first + 1;
+    return k;
+}
+
+// What the query at a position sees; positions below -1 see nothing either.
+struct RowMask {
+    int pos, low, sinks;
+    __device__ RowMask(int64_t at, const heddle_attention_args& a)
+        : pos((int)max(at, (int64_t)-1)), low(a.window ? pos - (int)a.window + 1 : INT32_MIN), sinks((int)a.sinks) {}
+    __device__ bool sees(int key) const { return key <= pos && (key >= low || key < sinks); }
+};
+
+// Every query of tokens i0 .. i1 - 1 sees every key of the tile at k0.
+__device__ __forceinline__ bool all_visible(const Params& p, const Span& s, int64_t i0, int64_t i1, int64_t k0) {
+    return s.off + i0 >= k0 + kTile - 1 &&
+           (p.a.window == 0 || s.off + i1 - 1 - k0 < p.a.window || k0 + kTile <= p.a.sinks);
+}
+
+// Rows [from, 128) of a tile in shared memory to zero, a row a thread; the
+// products read them after the next barrier.
+template <int DP>
+__device__ __forceinline__ void clear_rows(unsigned char* tile, int row, int64_t from) {
+    if (row >= from)
+#pragma unroll
+        for (int h = 0; h < DP / 64; ++h)
+#pragma unroll
+            for (int c = 0; c < 8; ++c)
+                *reinterpret_cast<uint4*>(tile + h * 16384 + row * 128 + c * 16) = make_uint4(0, 0, 0, 0);
+}
+
+// A D[128][N] = A B^T step over head_dim (operands' rows run along it).
+template <int DP>
+__device__ __forceinline__ void mma_dims(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc) {
+#pragma unroll
+    for (int k = 0; k < DP / 16; ++k) {
+        const uint32_t at = (k / 4) * 16384 + (k % 4) * 32;
+        mma_ss(d, smem_desc(a + at, 16384), smem_desc(b + at, 16384), idesc, k != 0);
+    }
+}
+// D[128][DP] (+)= W B over 128 rows of B: W in tensor memory, its upper 64
+// columns `gap` columns after its lower ones.
+__device__ __forceinline__ void mma_rows(uint32_t d, uint32_t w, int gap, uint32_t b, uint32_t idesc, bool add) {
+#pragma unroll
+    for (int k = 0; k < 8; ++k)
+        mma_ts(d, w + (k % 4) * 8 + (k / 4) * gap, smem_desc(b + k * 2048, 16384), idesc, add || k);
+}
+
+template <int DP>
+__device__ __forceinline__ void load_q_tile(uint32_t dst, const CUtensorMap* m, uint32_t bar, const Params& p,
+                                            int64_t t0, int hk, int b) {
+#pragma unroll
+    for (int h = 0; h < DP / 64; ++h) load_4d(dst + h * 16384, m, bar, h * 64, hk * p.group, (int)t0, b);
+}
+template <int DP>
+__device__ __forceinline__ void load_kv_tile(uint32_t dst, const CUtensorMap* m, uint32_t bar, int64_t k0, int hk,
+                                             int b) {
+#pragma unroll
+    for (int h = 0; h < DP / 64; ++h) load_4d(dst + h * 16384, m, bar, h * 64, hk, (int)k0, b);
+}
+
+// One row of DP sums times f from tensor memory to memory: 16 bytes at a time
+// where the row allows.
+template <class T, int DP>
+__device__ __forceinline__ void store_row(uint32_t tmem, T* out, bool live, int D, float f) {
+    const bool wide = ((uintptr_t)out & 15) == 0;
+#pragma unroll 1
+    for (int c = 0; c < DP; c += 32) {
+        __syncwarp();
+        uint32_t v[32];
+        tmem_ld32(tmem + c, v);
+        wait_ld();
+        if (!live) continue;
+        if (wide && c + 32 <= D) {
+#pragma unroll
+            for (int j = 0; j < 32; j += 8) {
+                uint4 u;
+                u.x = pack_two<T>(__uint_as_float(v[j]) * f, __uint_as_float(v[j + 1]) * f);
+                u.y = pack_two<T>(__uint_as_float(v[j + 2]) * f, __uint_as_float(v[j + 3]) * f);
+                u.z = pack_two<T>(__uint_as_float(v[j + 4]) * f, __uint_as_float(v[j + 5]) * f);
+                u.w = pack_two<T>(__uint_as_float(v[j + 6]) * f, __uint_as_float(v[j + 7]) * f);
+                *reinterpret_cast<uint4*>(out + c + j) = u;
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < 32; ++j)
+                if (c + j < D) out[c + j] = from_float<T>(__uint_as_float(v[j]) * f);
+        }
+    }
+}
+template <class T>
+__device__ __forceinline__ void zero_row(T* out, int D) {
+    for (int c = 0; c < D; ++c) out[c] = from_float<T>(0.0f);
+}
+
+// ------------------------------------------------------------------- forward
+
+// NT query tiles of a key head against the key tiles that they see, one
+// group of four warps each.  While one tile's warps turn scores into weights
+// the tensor cores run the other's products.
+template <int DP, int NT>
+struct Forward {
+    static constexpr int kTileBytes = kTile * DP * 2;
+    static constexpr int kRoom = 227 * 1024 - 1024 - 256 - NT * kTileBytes;
+    static constexpr int kSlots = kRoom / kTileBytes < 8 ? kRoom / kTileBytes : 8;  // K and V tiles by turns
+    static constexpr int kBytes = 1024 + (NT + kSlots) * kTileBytes + 256;
+    static constexpr int kThreads = 128 + NT * 128;
+    static constexpr int kCols = NT * (kTile + DP) <= 256 ? 256 : 512;
+};
+
+template <class T, int DP, int NT>
+__global__ void __launch_bounds__(Forward<DP, NT>::kThreads, 1)
+    attn_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUtensorMap mk,
+                const __grid_constant__ CUtensorMap mv, const __grid_constant__ Params p) {
+    using F = Forward<DP, NT>;
+    extern __shared__ unsigned char raw[];
+    unsigned char* base = raw + ((1024 - (smem_u32(raw) & 1023)) & 1023);
+    unsigned char* ring = base + NT * F::kTileBytes;
+    uint64_t* bars = reinterpret_cast<uint64_t*>(ring + F::kSlots * F::kTileBytes);
+    const uint32_t full = smem_u32(bars), empty = full + 8 * F::kSlots, q_full = empty + 8 * F::kSlots,
+                   s_full = q_full + 16, p_ready = s_full + 16, o_done = p_ready + 16;
+    volatile uint32_t* gave_up = reinterpret_cast<uint32_t*>(bars + 2 * F::kSlots + 8);
+    uint32_t* tmem_at = const_cast<uint32_t*>(gave_up) + 1;
+    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+
+    // the last queries see the most keys: their tiles start first
+    const int heads = p.a.kv_heads;
+    int64_t id = blockIdx.x;
+    const int split = (int)(id % p.splits);
+    id /= p.splits;
+    const int hk = (int)(id % heads);
+    id /= heads;
+    const int b = (int)(id % p.a.batch);
+    const int block = (int)((p.q_tiles + NT - 1) / NT - 1 - id / p.a.batch);
+    const Span s = span_of(p.a, b);
+    const int64_t t0 = (int64_t)block * NT * p.tokens;
+    const KeyTiles keys = key_tiles(p, s, t0, t0 + NT * p.tokens);
+    const int j0 = (int)((int64_t)keys.count * split / p.splits),
+              j1 = (int)((int64_t)keys.count * (split + 1) / p.splits);
+    // each tile's own first and last visible tile among them
+    int from[NT], to[NT];
+#pragma unroll
+    for (int q = 0; q < NT; ++q) {
+        const KeyTiles own = key_tiles(p, s, t0 + q * p.tokens, t0 + (q + 1) * p.tokens);
+        from[q] = to[q] = j0;
+        // the window's tiles of its own in the common order; leading tiles are common to both
+        if (own.count) {
+            const int last = keys.lead + own.first + own.count - own.lead - 1 - keys.first;
+            to[q] = max(j0, min(j1, last + 1));
+        }
+    }
+
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < F::kSlots; ++i) {
+            mbar_init(full + 8 * i, 1);
+            mbar_init(empty + 8 * i, 1);
+        }
+        for (int q = 0; q < 2; ++q) {
+            mbar_init(q_full + 8 * q, 1);
+            mbar_init(s_full + 8 * q, 1);
+            mbar_init(p_ready + 8 * q, 4);
+            mbar_init(o_done + 8 * q, 1);
+        }
+        *gave_up = 0;
+        mbar_fence_init();
+    }
+    if (warp == 2) tmem_alloc(smem_u32(tmem_at), F::kCols);
+    fence_before();
+    __syncthreads();
+    fence_after();
+    const uint32_t tmem = *tmem_at;
+    int last_to = j0;
+#pragma unroll
+    for (int q = 0; q < NT; ++q) last_to = max(last_to, to[q]);
+    const int n = last_to - j0;
+
+    if (warp == 0 && n > 0 && elect_one()) {
+        const uint32_t q_bytes = p.group * p.tokens * DP * 2;
+#pragma unroll
+        for (int q = 0; q < NT; ++q)
+            if (to[q] > from[q]) {
+                mbar_expect(q_full + 8 * q, q_bytes);
+                load_q_tile<DP>(smem_u32(base + q * F::kTileBytes), &mq, q_full + 8 * q, p, t0 + q * p.tokens, hk, b);
+            }
+        for (int i = 0; i < 2 * n; ++i) {
+            const int slot = i % F::kSlots;
+            if (!mbar_wait(empty + 8 * slot, (i / F::kSlots & 1) ^ 1, gave_up)) break;
+            mbar_expect(full + 8 * slot, F::kTileBytes);
+            load_kv_tile<DP>(smem_u32(ring + slot * F::kTileBytes), i & 1 ? &mv : &mk, full + 8 * slot,
+                             (int64_t)keys.at(j0 + i / 2) * kTile, hk, b);
+        }
+    } else if (warp == 1 && n > 0 && elect_one()) {
+        const uint32_t bf = p.a.dtype == HEDDLE_BF16;
+        const uint32_t id_s = instr_desc(bf, false, false, kTile), id_o = instr_desc(bf, false, true, DP);
+        bool go = true;
+        for (int j = -1; go && j < n; ++j) {
+            const int iv = 2 * j + 1, ik = 2 * j + 2;  // V of step j, K of step j + 1
+            const int sv = iv % F::kSlots, sk = ik % F::kSlots;
+            if (j + 1 < n) go = mbar_wait(full + 8 * sk, ik / F::kSlots & 1, gave_up);
+            if (go && j >= 0) go = mbar_wait(full + 8 * sv, iv / F::kSlots & 1, gave_up);
+            if (!go) break;
+            fence_after();
+#pragma unroll
+            for (int q = 0; q < NT; ++q) {
+                const uint32_t ts = tmem + q * kTile, to_acc = tmem + NT * kTile + q * DP;
+                if (j >= 0 && j0 + j < to[q]) {
+                    if (!(go = mbar_wait(p_ready + 8 * q, j & 1, gave_up))) break;
+                    fence_after();
+                    mma_rows(to_acc, ts, 32, smem_u32(ring + sv * F::kTileBytes), id_o, j > 0);
+                    if (j0 + j + 1 == to[q]) commit(o_done + 8 * q);
+                }
+                if (j0 + j + 1 < to[q]) {
+                    if (j < 0 && !(go = mbar_wait(q_full + 8 * q, 0, gave_up))) break;
+                    mma_dims<DP>(ts, smem_u32(base + q * F::kTileBytes), smem_u32(ring + sk * F::kTileBytes), id_s);
+                    commit(s_full + 8 * q);
+                }
+            }
+            if (!go) break;
+            if (j >= 0) commit(empty + 8 * sv);
+            if (j + 1 < n) commit(empty + 8 * sk);
+        }
+    } else if (warp >= 4) {
+        const int q = (warp - 4) / 4, row = (warp % 4) * 32 + lane;
+        const uint32_t lanes = (uint32_t)(warp % 4 * 32) << 16;
+        const uint32_t ts = tmem + lanes + q * kTile, to_acc = tmem + lanes + NT * kTile + q * DP;
+        const int64_t i0 = t0 + (int64_t)q * p.tokens, i1 = i0 + p.tokens;
+        const int64_t i = i0 + row / p.group;
+        const int64_t h = (int64_t)hk * p.group + row % p.group;
+        const RowMask mask(s.off + i, p.a);
+        const float c = p.scale_log2;
+        float top = -INFINITY, sum = 0.0f;
+        const int mine = to[q] - j0;
+        bool go = true;
+        for (int j = 0; j < mine; ++j) {
+            const int64_t k0 = (int64_t)keys.at(j0 + j) * kTile;
+            if (!(go = __all_sync(~0u, mbar_wait(s_full + 8 * q, j & 1, gave_up)))) break;
+            fence_after();
+            uint32_t v[4][32];
+#pragma unroll
+            for (int x = 0; x < 4; ++x) tmem_ld32(ts + 32 * x, v[x]);
+            wait_ld();
+            if (!all_visible(p, s, i0, min(i1, s.ql), k0)) {
+#pragma unroll
+                for (int x = 0; x < 4; ++x)
+#pragma unroll
+                    for (int y = 0; y < 32; ++y)
+                        if (!mask.sees((int)k0 + 32 * x + y)) v[x][y] = 0xff800000u;  // -infinity
+            }
+            float m4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+            for (int x = 0; x < 4; ++x)
+#pragma unroll
+                for (int y = 0; y < 32; ++y) m4[y % 4] = fmaxf(m4[y % 4], __uint_as_float(v[x][y]));
+            const float high = fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3]));
+            float keep = 1.0f;
+            if (high > top && (top == -INFINITY || (high - top) * c > kSlack)) {
+                keep = top == -INFINITY ? 0.0f : exp2_fast((top - high) * c);
+                top = high;
+                sum *= keep;
+            }
+            if (j > 0 && __any_sync(~0u, keep != 1.0f)) {
+                // the product of the step before has completed: the scores'
+                // barrier was committed after it
+#pragma unroll 1
+                for (int x = 0; x < DP; x += 32) {
+                    uint32_t o[32];
+                    tmem_ld32(to_acc + x, o);
+                    wait_ld();
+#pragma unroll
+                    for (int y = 0; y < 32; ++y) o[y] = __float_as_uint(__uint_as_float(o[y]) * keep);
+                    tmem_st32(to_acc + x, o);
+                }
+            }
+            const float sub = top == -INFINITY ? 0.0f : top * c;
+            float s4[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+            for (int x = 0; x < 4; x += 2) {
+                uint32_t w[32];
+#pragma unroll
+                for (int y = 0; y < 64; y += 2) {
+                    const float lo = exp2_fast(fmaf(__uint_as_float(v[x + y / 32][y % 32]), c, -sub));
+                    const float hi = exp2_fast(fmaf(__uint_as_float(v[x + y / 32][y % 32 + 1]), c, -sub));
+                    s4[y % 4] += lo;
+                    s4[y % 4 + 1] += hi;
+                    w[y / 2] = pack_two<T>(lo, hi);
+                }
+                tmem_st32(ts + 16 * x, w);
+            }
+            sum += (s4[0] + s4[1]) + (s4[2] + s4[3]);
+            if (s.kl < p.a.kv_len && k0 + kTile > s.kl) {  // values past the sequence
+                const int iv = 2 * j + 1, sv = iv % F::kSlots;
+                if (!(go = __all_sync(~0u, mbar_wait(full + 8 * sv, iv / F::kSlots & 1, gave_up)))) break;
+                clear_rows<DP>(ring + sv * F::kTileBytes, row, s.kl - k0);
+                fence_async_shared();
+            }
+            wait_st();
+            fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(p_ready + 8 * q);
+        }
+        if (go && mine > 0) go = __all_sync(~0u, mbar_wait(o_done + 8 * q, 0, gave_up));
+        fence_after();
+        if (go) {
+            const bool inside = row < p.group * p.tokens && i < p.a.q_len;
+            const bool some = mine > 0 && i < s.ql && !(sum == 0.0f);
+            const float f = some ? 1.0f / sum : 0.0f;
+            const float lse = some ? (top * c + log2f(sum)) * kLn2 : -INFINITY;
+            const int64_t r = ((int64_t)b * p.a.q_heads + h) * p.a.q_len + i;
+            const int D = p.a.head_dim;
+            if (p.splits > 1) {
+                const int64_t at = (int64_t)split * p.a.batch * p.a.q_heads * p.a.q_len + r;
+                if (inside) p.part_lse[at] = lse;
+#pragma unroll 1
+                for (int x = 0; x < DP; x += 32) {
+                    __syncwarp();
+                    uint32_t o[32];
+                    if (mine > 0) {
+                        tmem_ld32(to_acc + x, o);
+                        wait_ld();
+                    }
+                    if (!inside || !some) continue;  // a part of no weight is not read
+#pragma unroll
+                    for (int y = 0; y < 32; y += 4)
+                        if (x + y < D)
+                            *reinterpret_cast<float4*>(p.part_o + at * D + x + y) =
+                                make_float4(__uint_as_float(o[y]) * f, __uint_as_float(o[y + 1]) * f,
+                                            __uint_as_float(o[y + 2]) * f, __uint_as_float(o[y + 3]) * f);
+                }
+            } else {
+                T* out = static_cast<T*>(p.a.o.data) + b * p.a.o.batch_stride + i * p.a.o.token_stride +
+                         h * p.a.o.head_stride;
+                if (mine > 0) store_row<T, DP>(to_acc, out, inside && some, D, f);
+                if (inside && !some) zero_row(out, D);
+                if (inside && p.a.lse) p.a.lse[r] = lse;
+            }
+        }
+    }
+    fence_before();
+    __syncthreads();
+    if (*gave_up) {
+        if (threadIdx.x == 0) atomicOr(p.err, kErrOpWait);
+        drain();
+        __syncthreads();
+    }
+    if (warp == 2) tmem_free(tmem, F::kCols);
+}
+
+// Joins the parts of rows split along the keys, one warp a row.
+template <class T>
+__global__ void __launch_bounds__(256) attn_join_kernel(const __grid_constant__ Params p) {
+    const int lane = threadIdx.x % 32, D = p.a.head_dim;
+    const int64_t rows = p.a.batch * p.a.q_heads * p.a.q_len;
+    const int64_t r = (int64_t)blockIdx.x * 8 + threadIdx.x / 32;
+    if (r >= rows) return;
+    const float mine = lane < p.splits ? p.part_lse[lane * rows + r] : -INFINITY;
+    float top = mine;
+#pragma unroll
+    for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, o));
+    const float e = top == -INFINITY ? 0.0f : expf(mine - top);
+    const float total = warp_sum(e);
+    const float w = total > 0.0f ? e / total : 0.0f;
+    float acc[4] = {};
+    for (int x = 0; x < p.splits; ++x) {
+        const float f = __shfl_sync(~0u, w, x);
+        if (f == 0.0f) continue;
+        const float* o = p.part_o + ((int64_t)x * rows + r) * D;
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            if (lane + 32 * j < D) acc[j] += f * o[lane + 32 * j];
+    }
+    const int64_t b = r / (p.a.q_heads * p.a.q_len), h = r / p.a.q_len % p.a.q_heads, i = r % p.a.q_len;
+    T* out = static_cast<T*>(p.a.o.data) + b * p.a.o.batch_stride + i * p.a.o.token_stride + h * p.a.o.head_stride;
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+        if (lane + 32 * j < D) out[lane + 32 * j] = from_float<T>(acc[j]);
+    if (p.a.lse && lane == 0) p.a.lse[r] = total > 0.0f ? top + logf(total) : -INFINITY;
+}
+
+// ------------------------------------------------------------------ backward
+
+constexpr int kGradThreads = 128 + 256;
+
+// Bars of a backward kernel, in the order that follows its tiles.
+struct GradBars {
+    uint32_t held, full, full2, empty, a_full, b_full, a_ready, b_ready, stats, done;
+    __device__ explicit GradBars(uint32_t at)
+        : held(at), full(at + 8), full2(at + 24), empty(at + 40), a_full(at + 56), b_full(at + 64), a_ready(at + 72),
+          b_ready(at + 80), stats(at + 96), done(at + 104) {}
+    __device__ void init() const {
+        mbar_init(held, 1);
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(full + 8 * i, 1);
+            mbar_init(full2 + 8 * i, 1);
+            mbar_init(empty + 8 * i, 1);
+        }
+        mbar_init(a_full, 1);
+        mbar_init(b_full, 1);
+        mbar_init(a_ready, 8);
+        mbar_init(b_ready, 8);
+        mbar_init(b_ready + 8, 8);
+        mbar_init(stats, 8);
+        mbar_init(done, 1);
+    }
+};
+constexpr int kGradBarBytes = 128;
+
+// dq of a query tile: dq = scale sum over key tiles of dS K with
+// S = Q K^T, dP = dO V^T, dS = P (dP - delta).  Q and dO stay in shared
+// memory, K and V tiles come in two stages.  Scores of the next tile are
+// computed while this one's are turned into dS (two buffers).
+template <int DP>
+struct GradShape {
+    static constexpr int kTileBytes = kTile * DP * 2;
+    static constexpr int kStats = 3 * kTile * 12;
+    static constexpr int kBytes = 1024 + 6 * kTileBytes + kGradBarBytes + 64 + kStats;
+};
+
+template <class T, int DP>
+__global__ void __launch_bounds__(kGradThreads, 1)
+    attn_dq_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUtensorMap mk,
+                   const __grid_constant__ CUtensorMap mv, const __grid_constant__ CUtensorMap mdo,
+                   const __grid_constant__ Params p) {
+    using G = GradShape<DP>;
+    extern __shared__ unsigned char raw[];
+    unsigned char* base = raw + ((1024 - (smem_u32(raw) & 1023)) & 1023);
+    unsigned char *sq = base, *sdo = base + G::kTileBytes, *stage = base + 2 * G::kTileBytes;  // K, V, K, V
+    unsigned char* tail = base + 6 * G::kTileBytes;
+    const GradBars bar(smem_u32(tail));
+    volatile uint32_t* gave_up = reinterpret_cast<uint32_t*>(tail + kGradBarBytes);
+    uint32_t* tmem_at = const_cast<uint32_t*>(gave_up) + 1;
+    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+
+    int64_t id = blockIdx.x;
+    const int hk = (int)(id % p.a.kv_heads);
+    id /= p.a.kv_heads;
+    const int b = (int)(id % p.a.batch);
+    const int block = (int)(p.q_tiles - 1 - id / p.a.batch);
+    const Span s = span_of(p.a, b);
+    const int64_t t0 = (int64_t)block * p.tokens, t1 = min(t0 + p.tokens, s.ql);
+    const KeyTiles keys = key_tiles(p, s, t0, t0 + p.tokens);
+    const int n = keys.count;
+
+    if (threadIdx.x == 0) {
+        bar.init();
+        *gave_up = 0;
+        mbar_fence_init();
+    }
+    if (warp == 2) tmem_alloc(smem_u32(tmem_at), 512);
+    fence_before();
+    __syncthreads();
+    fence_after();
+    const uint32_t tmem = *tmem_at;
+    const uint32_t at_s = tmem, at_dp = tmem + 128, at_dq = tmem + 256, at_ds = tmem + 256 + DP;  // two of 64 columns
+
+    if (warp == 0 && n > 0 && elect_one()) {
+        mbar_expect(bar.held, 2 * p.group * p.tokens * DP * 2);
+        load_q_tile<DP>(smem_u32(sq), &mq, bar.held, p, t0, hk, b);
+        load_q_tile<DP>(smem_u32(sdo), &mdo, bar.held, p, t0, hk, b);
+        for (int j = 0; j < n; ++j) {
+            const int st = j & 1;
+            if (!mbar_wait(bar.empty + 8 * st, (j / 2 & 1) ^ 1, gave_up)) break;
+            mbar_expect(bar.full + 8 * st, 2 * G::kTileBytes);
+            const int64_t k0 = (int64_t)keys.at(j) * kTile;
+            load_kv_tile<DP>(smem_u32(stage + 2 * st * G::kTileBytes), &mk, bar.full + 8 * st, k0, hk, b);
+            load_kv_tile<DP>(smem_u32(stage + (2 * st + 1) * G::kTileBytes), &mv, bar.full + 8 * st, k0, hk, b);
+        }
+    } else if (warp == 1 && n > 0 && elect_one()) {
+        const uint32_t bf = p.a.dtype == HEDDLE_BF16;
+        const uint32_t id_s = instr_desc(bf, false, false, kTile), id_d = instr_desc(bf, false, true, DP);
+        bool go = mbar_wait(bar.held, 0, gave_up);
+        for (int j = -1; go && j < n; ++j) {
+            if (j + 1 < n) {
+                const int st = (j + 1) & 1;
+                if (!(go = mbar_wait(bar.full + 8 * st, (j + 1) / 2 & 1, gave_up))) break;
+                if (j >= 0 && !(go = mbar_wait(bar.a_ready, j & 1, gave_up))) break;  // scores of step j are read
+                fence_after();
+                mma_dims<DP>(at_s, smem_u32(sq), smem_u32(stage + 2 * st * G::kTileBytes), id_s);
+                mma_dims<DP>(at_dp, smem_u32(sdo), smem_u32(stage + (2 * st + 1) * G::kTileBytes), id_s);
+                commit(bar.a_full);
+            }
+            if (j >= 0) {
+                const int st = j & 1;
+                if (!(go = mbar_wait(bar.b_ready + 8 * st, j / 2 & 1, gave_up))) break;
+                fence_after();
+                mma_rows(at_dq, at_ds + 64 * st, 32, smem_u32(stage + 2 * st * G::kTileBytes), id_d, j > 0);
+                commit(bar.empty + 8 * st);
+            }
+        }
+        if (go) commit(bar.done);
+    } else if (warp >= 4) {
+        const int side = (warp - 4) / 4, row = (warp % 4) * 32 + lane;  // which 64 of a tile's 128 keys
+        const uint32_t lanes = (uint32_t)(warp % 4 * 32) << 16;
+        const int64_t i = t0 + row / p.group, h = (int64_t)hk * p.group + row % p.group;
+        const bool inside = row < p.group * p.tokens && i < p.a.q_len;
+        const int64_t r = ((int64_t)b * p.a.q_heads + h) * p.a.q_len + i;
+        const RowMask mask(i < s.ql ? s.off + i : -1, p.a);
+        float lse = inside ? p.a.lse[r] : INFINITY;
+        lse = lse == -INFINITY ? INFINITY : lse * kLog2e;  // weights of a row that sees nothing are zero
+        const float delta = inside ? p.delta[r] : 0.0f, c = p.scale_log2;
+        bool go = true;
+        for (int j = 0; j < n; ++j) {
+            const int64_t k0 = (int64_t)keys.at(j) * kTile;
+            if (!(go = __all_sync(~0u, mbar_wait(bar.a_full, j & 1, gave_up)))) break;
+            fence_after();
+            uint32_t v[2][32], d[2][32];
+#pragma unroll
+            for (int x = 0; x < 2; ++x) {
+                tmem_ld32(at_s + lanes + side * 64 + 32 * x, v[x]);
+                tmem_ld32(at_dp + lanes + side * 64 + 32 * x, d[x]);
+            }
+            wait_ld();
+            fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar.a_ready);
+            const bool whole = t0 + p.tokens <= s.ql && all_visible(p, s, t0, t1, k0);
+            uint32_t w[32];
+#pragma unroll
+            for (int x = 0; x < 2; ++x)
+#pragma unroll
+                for (int y = 0; y < 32; ++y) {
+                    float e = exp2_fast(fmaf(__uint_as_float(v[x][y]), c, -lse));
+                    if (!whole && !mask.sees((int)k0 + side * 64 + 32 * x + y)) e = 0.0f;
+                    // a product with what lies in hidden places must not count
+                    v[x][y] = __float_as_uint(e == 0.0f ? 0.0f : e * (__uint_as_float(d[x][y]) - delta));
+                }
+#pragma unroll
+            for (int y = 0; y < 32; ++y)
+                w[y] = pack_two<T>(__uint_as_float(v[y / 16][2 * y % 32]), __uint_as_float(v[y / 16][2 * y % 32 + 1]));
+            tmem_st32(at_ds + 64 * (j & 1) + lanes + side * 32, w);
+            if (side == 0 && s.kl < p.a.kv_len && k0 + kTile > s.kl) {  // keys past the sequence
+                clear_rows<DP>(stage + 2 * (j & 1) * G::kTileBytes, row, s.kl - k0);
+                fence_async_shared();
+            }
+            wait_st();
+            fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar.b_ready + 8 * (j & 1));  // a warp may be a step ahead of another
+        }
+        if (go && n > 0) go = __all_sync(~0u, mbar_wait(bar.done, 0, gave_up));
+        fence_after();
+        if (go && side == 0) {
+            T* out = static_cast<T*>(p.dq.data) + b * p.dq.batch_stride + i * p.dq.token_stride + h * p.dq.head_stride;
+            if (n > 0)
+                store_row<T, DP>(at_dq + lanes, out, inside, p.a.head_dim, p.a.scale);
+            else if (inside)
+                zero_row(out, p.a.head_dim);
+        }
+    }
+    fence_before();
+    __syncthreads();
+    if (*gave_up) {
+        if (threadIdx.x == 0) atomicOr(p.err, kErrOpWait);
+        drain();
+        __syncthreads();
+    }
+    if (warp == 2) tmem_free(tmem, 512);
+}
+
+// dk and dv of a key tile, over every query tile that sees it, the group's
+// heads among its rows.  The scores are computed transposed, keys along the
+// lanes, so that P^T and dS^T are left operands in tensor memory as they come:
+// S^T = K Q^T, dP^T = V dO^T, dv += P^T dO, dk += dS^T Q.
+template <class T, int DP>
+__global__ void __launch_bounds__(kGradThreads, 1)
+    attn_dkv_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUtensorMap mk,
+                    const __grid_constant__ CUtensorMap mv, const __grid_constant__ CUtensorMap mdo,
+                    const __grid_constant__ Params p) {
+    using G = GradShape<DP>;
+    extern __shared__ unsigned char raw[];
+    unsigned char* base = raw + ((1024 - (smem_u32(raw) & 1023)) & 1023);
+    unsigned char *sk = base, *sv = base + G::kTileBytes, *stage = base + 2 * G::kTileBytes;  // Q, dO, Q, dO
+    unsigned char* tail = base + 6 * G::kTileBytes;
+    const GradBars bar(smem_u32(tail));
+    volatile uint32_t* gave_up = reinterpret_cast<uint32_t*>(tail + kGradBarBytes);
+    uint32_t* tmem_at = const_cast<uint32_t*>(gave_up) + 1;
+    float2* stat = reinterpret_cast<float2*>(tail + kGradBarBytes + 64);     // [3][128] lse, delta
+    int* pos = reinterpret_cast<int*>(stat + 3 * kTile);                     // [3][128] positions
+    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+
+    int64_t id = blockIdx.x;
+    const int hk = (int)(id % p.a.kv_heads);
+    id /= p.a.kv_heads;
+    const int b = (int)(id % p.a.batch);
+    const int64_t k0 = id / p.a.batch * kTile;  // the first keys are seen by the most queries
+    const Span s = span_of(p.a, b);
+    // query tiles that see a key of the tile
+    int first = 0, n = 0;
+    if (k0 < s.kl) {
+        const int64_t lo = max((int64_t)0, k0 - s.off);
+        int64_t hi = s.ql;
+        if (p.a.window && k0 >= p.a.sinks) hi = min(hi, k0 + kTile - 1 + p.a.window - s.off);
+        if (lo < hi) {
+            first = (int)(lo / p.tokens);
+            n = (int)((hi - 1) / p.tokens) - first + 1;
+        }
+    }
+
+    if (threadIdx.x == 0) {
+        bar.init();
+        *gave_up = 0;
+        mbar_fence_init();
+    }
+    if (warp == 2) tmem_alloc(smem_u32(tmem_at), 512);
+    if (warp >= 4) {  // rows that no copy writes are zero throughout
+        const int row = threadIdx.x & 127, rows = p.group * p.tokens;
+        for (int x = 0; x < 4; ++x) clear_rows<DP>(stage + x * G::kTileBytes, row, rows);
+        fence_async_shared();
+    }
+    fence_before();
+    __syncthreads();
+    fence_after();
+    const uint32_t tmem = *tmem_at;
+    const uint32_t at_s = tmem, at_dp = tmem + 128, at_dv = tmem + 256, at_dk = tmem + 256 + DP;
+
+    if (warp == 0 && n > 0 && elect_one()) {
+        mbar_expect(bar.held, 2 * G::kTileBytes);
+        load_kv_tile<DP>(smem_u32(sk), &mk, bar.held, k0, hk, b);
+        load_kv_tile<DP>(smem_u32(sv), &mv, bar.held, k0, hk, b);
+        const uint32_t bytes = p.group * p.tokens * DP * 2;
+        for (int j = 0; j < n; ++j) {
+            const int st = j & 1;
+            if (!mbar_wait(bar.empty + 8 * st, (j / 2 & 1) ^ 1, gave_up)) break;
+            const int64_t t = (int64_t)(first + j) * p.tokens;
+            mbar_expect(bar.full + 8 * st, bytes);
+            load_q_tile<DP>(smem_u32(stage + 2 * st * G::kTileBytes), &mq, bar.full + 8 * st, p, t, hk, b);
+            mbar_expect(bar.full2 + 8 * st, bytes);
+            load_q_tile<DP>(smem_u32(stage + (2 * st + 1) * G::kTileBytes), &mdo, bar.full2 + 8 * st, p, t, hk, b);
+        }
+    } else if (warp == 1 && n > 0 && elect_one()) {
+        const uint32_t bf = p.a.dtype == HEDDLE_BF16;
+        const uint32_t id_s = instr_desc(bf, false, false, kTile), id_d = instr_desc(bf, false, true, DP);
+        bool go = mbar_wait(bar.held, 0, gave_up);
+        for (int j = -1; go && j < n; ++j) {
+            const int st = j & 1, nx = (j + 1) & 1;
+            const uint32_t tq = smem_u32(stage + 2 * st * G::kTileBytes), nq = smem_u32(stage + 2 * nx * G::kTileBytes);
+            if (j >= 0) {
+                if (!(go = mbar_wait(bar.a_ready, j & 1, gave_up))) break;
+                fence_after();
+                mma_rows(at_dv, at_s, 64, tq + G::kTileBytes, id_d, j > 0);
+            }
+            if (j + 1 < n) {
+                if (!(go = mbar_wait(bar.full + 8 * nx, (j + 1) / 2 & 1, gave_up))) break;
+                fence_after();
+                mma_dims<DP>(at_s, smem_u32(sk), nq, id_s);
+                commit(bar.a_full);
+            }
+            if (j >= 0) {
+                if (!(go = mbar_wait(bar.b_ready, j & 1, gave_up))) break;
+                fence_after();
+                mma_rows(at_dk, at_dp, 64, tq, id_d, j > 0);
+                commit(bar.empty + 8 * st);
+            }
+            if (j + 1 < n) {
+                if (!(go = mbar_wait(bar.full2 + 8 * nx, (j + 1) / 2 & 1, gave_up))) break;
+                fence_after();
+                mma_dims<DP>(at_dp, smem_u32(sv), nq + G::kTileBytes, id_s);
+                commit(bar.b_full);
+            }
+        }
+        if (go) commit(bar.done);
+    } else if (warp >= 4) {
+        const int side = (warp - 4) / 4, row = (warp % 4) * 32 + lane;  // which 64 of a tile's 128 queries
+        const uint32_t lanes = (uint32_t)(warp % 4 * 32) << 16;
+        const int64_t key = k0 + row;
+        const float c = p.scale_log2;
+
+        // statistics of query tile j to buffer j % 3: written a step ahead,
+        // while the slowest warp may still read those of the step before
+        auto put_stats = [&](int j) {
+            const int64_t i = (int64_t)(first + j) * p.tokens + row / p.group;
+            const int64_t h = (int64_t)hk * p.group + row % p.group;
+            const int64_t r = ((int64_t)b * p.a.q_heads + h) * p.a.q_len + i;
+            const bool live = row < p.group * p.tokens && i < s.ql;
+            float2* to = stat + (j % 3) * kTile + row;
+            if (side == 0) {
+                const float l = live ? p.a.lse[r] : INFINITY;
+                to->x = l == -INFINITY ? INFINITY : l * kLog2e;
+                pos[(j % 3) * kTile + row] = live ? (int)max(s.off + i, (int64_t)-1) : -1;
+            } else {
+                to->y = live ? p.delta[r] : 0.0f;
+            }
+        };
+        bool go = true;
+        if (n > 0) {
+            put_stats(0);
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar.stats);
+        }
+        for (int j = 0; j < n; ++j) {
+            if (!(go = __all_sync(~0u, mbar_wait(bar.stats, j & 1, gave_up)))) break;
+            if (j + 1 < n) {
+                put_stats(j + 1);
+                __syncwarp();
+                if (lane == 0) mbar_arrive(bar.stats);
+            }
+            const int64_t t0 = (int64_t)(first + j) * p.tokens, t1 = t0 + p.tokens;
+            const float2* st = stat + (j % 3) * kTile + side * 64;
+            const int* at = pos + (j % 3) * kTile + side * 64;
+            const bool whole = t1 <= s.ql && all_visible(p, s, t0, t1, k0);
+            if (!(go = __all_sync(~0u, mbar_wait(bar.a_full, j & 1, gave_up)))) break;
+            fence_after();
+            uint32_t v[2][32];
+            tmem_ld32(at_s + lanes + side * 64, v[0]);
+            tmem_ld32(at_s + lanes + side * 64 + 32, v[1]);
+            wait_ld();
+            uint32_t w[32];
+#pragma unroll
+            for (int x = 0; x < 2; ++x)
+#pragma unroll
+                for (int y = 0; y < 32; ++y) {
+                    float e = exp2_fast(fmaf(__uint_as_float(v[x][y]), c, -st[32 * x + y].x));
+                    if (!whole) {
+                        const RowMask mask(at[32 * x + y], p.a);
+                        if (!mask.sees((int)key)) e = 0.0f;
+                    }
+                    v[x][y] = __float_as_uint(e);
+                }
+#pragma unroll
+            for (int y = 0; y < 32; ++y)
+                w[y] = pack_two<T>(__uint_as_float(v[y / 16][2 * y % 32]), __uint_as_float(v[y / 16][2 * y % 32 + 1]));
+            tmem_st32(at_s + lanes + side * 64, w);
+            if (s.ql < p.a.q_len && t1 > s.ql) {  // queries past the sequence: side 0 clears Q, side 1 dO
+                const int st2 = j & 1;
+                const uint32_t loaded = side ? bar.full2 : bar.full;
+                if (!(go = __all_sync(~0u, mbar_wait(loaded + 8 * st2, j / 2 & 1, gave_up)))) break;
+                clear_rows<DP>(stage + (2 * st2 + side) * G::kTileBytes, row, (s.ql - t0) * p.group);
+                fence_async_shared();
+            }
+            wait_st();
+            fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar.a_ready);
+
+            if (!(go = __all_sync(~0u, mbar_wait(bar.b_full, j & 1, gave_up)))) break;
+            fence_after();
+            uint32_t d[2][32];
+            tmem_ld32(at_dp + lanes + side * 64, d[0]);
+            tmem_ld32(at_dp + lanes + side * 64 + 32, d[1]);
+            wait_ld();
+#pragma unroll
+            for (int x = 0; x < 2; ++x)
+#pragma unroll
+                for (int y = 0; y < 32; ++y) {
+                    const float e = __uint_as_float(v[x][y]);
+                    d[x][y] = __float_as_uint(e == 0.0f ? 0.0f : e * (__uint_as_float(d[x][y]) - st[32 * x + y].y));
+                }
+#pragma unroll
+            for (int y = 0; y < 32; ++y)
+                w[y] = pack_two<T>(__uint_as_float(d[y / 16][2 * y % 32]), __uint_as_float(d[y / 16][2 * y % 32 + 1]));
+            tmem_st32(at_dp + lanes + side * 64, w);
+            wait_st();
+            fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar.b_ready);
+        }
+        if (go && n > 0) go = __all_sync(~0u, mbar_wait(bar.done, 0, gave_up));
+        fence_after();
+        if (go) {
+            const heddle_heads& t = side ? p.dk : p.dv;
+            T* out = static_cast<T*>(t.data) + b * t.batch_stride + key * t.token_stride + hk * t.head_stride;
+            const bool inside = key < p.a.kv_len;
+            if (n > 0)
+                store_row<T, DP>((side ? at_dk : at_dv) + lanes, out, inside, p.a.head_dim, side ? p.a.scale : 1.0f);
+            else if (inside)
+                zero_row(out, p.a.head_dim);
+        }
+    }
+    fence_before();
+    __syncthreads();
+    if (*gave_up) {
+        if (threadIdx.x == 0) atomicOr(p.err, kErrOpWait);
+        drain();
+        __syncthreads();
+    }
+    if (warp == 2) tmem_free(tmem, 512);
+}
+
+// --------------------------------------------------------------------- host
+
+bool copies(const heddle_heads& t, int64_t b, int64_t n, int64_t h) {
+    auto fits = [](int64_t extent, int64_t stride) {
+        return extent == 1 || (stride > 0 && stride % 8 == 0 && stride < ((int64_t)1 << 39));
+    };
+    return (uintptr_t)t.data % 16 == 0 && fits(b, t.batch_stride) && fits(n, t.token_stride) &&
+           fits(h, t.head_stride);
+}
+
+cudaError_t heads_map(CUtensorMap* m, const heddle_heads& t, const heddle_attention_args& a, int64_t n, int64_t h,
+                      int box_heads, int box_tokens) {
+    const uint64_t row = (uint64_t)(a.head_dim + 7) / 8 * 16;  // where an axis has one entry
+    const uint64_t dims[4] = {(uint64_t)a.head_dim, (uint64_t)h, (uint64_t)n, (uint64_t)a.batch};
+    const uint64_t strides[3] = {h == 1 ? row : (uint64_t)t.head_stride * 2, n == 1 ? row : (uint64_t)t.token_stride * 2,
+                                 a.batch == 1 ? row : (uint64_t)t.batch_stride * 2};
+    const uint32_t box[4] = {64, (uint32_t)box_heads, (uint32_t)box_tokens, 1};
+    return make_map(m, t.data, a.dtype, 4, dims, strides, box);
+}
+
+int tiles_per_block(const heddle_attention_args& a) {
+    const int group = a.q_heads / a.kv_heads;
+    return a.q_len > kTile / group ? 2 : 1;
+}
+
+Params params_of(const OpContext& x, const heddle_attention_args& a) {
+    Params p{};
+    p.a = a;
+    p.group = a.q_heads / a.kv_heads;
+    p.tokens = kTile / p.group;
+    p.q_tiles = (int32_t)ceil_div(a.q_len, p.tokens);
+    p.kv_tiles = (int32_t)ceil_div(a.kv_len, kTile);
+    p.scale_log2 = a.scale * kLog2e;
+    p.err = x.err;
+    // Parts along the keys where the query tiles are too few for the SMs: at
+    // least two key tiles each, at most 32 (the join holds one a lane).
+    const int nt = tiles_per_block(a);
+    const int64_t blocks = ceil_div(p.q_tiles, nt) * a.kv_heads * a.batch;
+    int64_t keys = a.kv_len;
+    if (a.window) {
+        const int64_t reach = a.window + (a.q_len < nt * p.tokens ? a.q_len : nt * p.tokens) + a.sinks + 2 * kTile;
+        if (reach < keys) keys = reach;
+    }
+    int64_t parts = x.num_sms / blocks;
+    const int64_t most = keys / (2 * kTile);
+    parts = parts < most ? parts : most;
+    p.splits = (int32_t)(parts < 1 ? 1 : parts > 32 ? 32 : parts);
+    return p;
+}
+
+template <class T, int DP, int NT>
+cudaError_t forward(const Params& p, const CUtensorMap& q, const CUtensorMap& k, const CUtensorMap& v,
+                    cudaStream_t st) {
+    using F = Forward<DP, NT>;
+    static_assert(F::kSlots >= 4, "two steps of K and V");
+    auto* f = attn_kernel<T, DP, NT>;
+    cudaError_t e = cudaFuncSetAttribute(f, cudaFuncAttributeMaxDynamicSharedMemorySize, F::kBytes);
+    if (e != cudaSuccess) return e;
+    const int64_t grid = ceil_div(p.q_tiles, NT) * p.a.batch * p.a.kv_heads * p.splits;
+    f<<<(unsigned)grid, F::kThreads, F::kBytes, st>>>(q, k, v, p);
+    if (p.splits > 1) {
+        const int64_t rows = p.a.batch * p.a.q_heads * p.a.q_len;
+        attn_join_kernel<T><<<(unsigned)ceil_div(rows, 8), 256, 0, st>>>(p);
+    }
+    return cudaGetLastError();
+}
+
+template <class T, int DP>
+cudaError_t backward(const Params& p, const CUtensorMap& q, const CUtensorMap& k, const CUtensorMap& v,
+                     const CUtensorMap& d_o, cudaStream_t st) {
+    using G = GradShape<DP>;
+    cudaError_t e = cudaFuncSetAttribute(attn_dq_kernel<T, DP>, cudaFuncAttributeMaxDynamicSharedMemorySize, G::kBytes);
+    if (e == cudaSuccess)
+        e = cudaFuncSetAttribute(attn_dkv_kernel<T, DP>, cudaFuncAttributeMaxDynamicSharedMemorySize, G::kBytes);
+    if (e != cudaSuccess) return e;
+    const int64_t heads = p.a.batch * p.a.kv_heads;
+    attn_dkv_kernel<T, DP><<<(unsigned)(p.kv_tiles * heads), kGradThreads, G::kBytes, st>>>(q, k, v, d_o, p);
+    attn_dq_kernel<T, DP><<<(unsigned)(p.q_tiles * heads), kGradThreads, G::kBytes, st>>>(q, k, v, d_o, p);
+    return cudaGetLastError();
+}
+
+template <class T>
+cudaError_t forward_of(const Params& p, const CUtensorMap& q, const CUtensorMap& k, const CUtensorMap& v,
+                       cudaStream_t st) {
+    const bool two = tiles_per_block(p.a) == 2;
+    if (p.a.head_dim <= 64) return two ? forward<T, 64, 2>(p, q, k, v, st) : forward<T, 64, 1>(p, q, k, v, st);
+    return two ? forward<T, 128, 2>(p, q, k, v, st) : forward<T, 128, 1>(p, q, k, v, st);
+}
+
+cudaError_t input_maps(const Params& p, CUtensorMap* q, CUtensorMap* k, CUtensorMap* v) {
+    const heddle_attention_args& a = p.a;
+    cudaError_t e = heads_map(q, a.q, a, a.q_len, a.q_heads, p.group, p.tokens);
+    if (e == cudaSuccess) e = heads_map(k, a.k, a, a.kv_len, a.kv_heads, 1, kTile);
+    if (e == cudaSuccess) e = heads_map(v, a.v, a, a.kv_len, a.kv_heads, 1, kTile);
+    return e;
+}
+
+}  // namespace
+
+// head_dim in whole 16-byte units, at most 128, and bases and strides that
+// bulk tensor copies take; a scale whose sign keeps the order of scores.
+bool attn_tc_takes(const heddle_attention_args& a) {
+    return a.head_dim % 8 == 0 && a.head_dim <= 128 && a.q_heads / a.kv_heads <= kTile && a.scale > 0.0f &&
+           a.q_len > 0 && a.kv_len > 0 && copies(a.q, a.batch, a.q_len, a.q_heads) &&
+           copies(a.k, a.batch, a.kv_len, a.kv_heads) && copies(a.v, a.batch, a.kv_len, a.kv_heads);
+}
+bool attn_tc_takes_grad(const heddle_attention_grad_args& g) {
+    return attn_tc_takes(g.fwd) && copies(g.d_o, g.fwd.batch, g.fwd.q_len, g.fwd.q_heads);
+}
+
+size_t attn_tc_scratch(const OpContext& x, const heddle_attention_args& a) {
+    const Params p = params_of(x, a);
+    if (p.splits == 1) return 0;
+    const size_t rows = (size_t)(a.batch * a.q_heads * a.q_len) * p.splits;
+    return align256(rows * a.head_dim * 4) + align256(rows * 4);
+}
+
+cudaError_t launch_attn_tc(const OpContext& x, const heddle_attention_args& a, unsigned char* ws, cudaStream_t st) {
+    Params p = params_of(x, a);
+    if (p.splits > 1) {
+        const size_t rows = (size_t)(a.batch * a.q_heads * a.q_len) * p.splits;
+        p.part_o = reinterpret_cast<float*>(ws);
+        p.part_lse = reinterpret_cast<float*>(ws + align256(rows * a.head_dim * 4));
+    }
+    CUtensorMap q, k, v;
+    const cudaError_t e = input_maps(p, &q, &k, &v);
+    if (e != cudaSuccess) return e;
+    return a.dtype == HEDDLE_BF16 ? forward_of<__nv_bfloat16>(p, q, k, v, st) : forward_of<__half>(p, q, k, v, st);
+}
+
+cudaError_t launch_attn_tc_grad(const OpContext& x, const heddle_attention_grad_args& g, const float* delta,
+                                cudaStream_t st) {
+    const heddle_attention_args& a = g.fwd;
+    Params p = params_of(x, a);
+    p.d_o = g.d_o, p.dq = g.dq, p.dk = g.dk, p.dv = g.dv;
+    p.delta = delta;
+    CUtensorMap q, k, v, d_o;
+    cudaError_t e = input_maps(p, &q, &k, &v);
+    if (e == cudaSuccess) e = heads_map(&d_o, g.d_o, a, a.q_len, a.q_heads, p.group, p.tokens);
+    if (e != cudaSuccess) return e;
+    const bool narrow = a.head_dim <= 64;
+    if (a.dtype == HEDDLE_BF16)
+        return narrow ? backward<__nv_bfloat16, 64>(p, q, k, v, d_o, st) : backward<__nv_bfloat16, 128>(p, q, k, v, d_o, st);
+    return narrow ? backward<__half, 64>(p, q, k, v, d_o, st) : backward<__half, 128>(p, q, k, v, d_o, st);
+}
+
+}  // namespace hd
