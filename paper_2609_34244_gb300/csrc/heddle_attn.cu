@@ -66,6 +66,35 @@ __global__ void __launch_bounds__(kWarps * 32) attn_row_kernel(heddle_attention_
     }
 }
 
+// delta_i = do_i . o_i for heads of whole 16-byte units: GL lanes a row, 16
+// bytes a lane, rows in the order of memory.
+template <class T, int GL>
+__global__ void __launch_bounds__(256) attn_delta_wide_kernel(const __grid_constant__ heddle_attention_grad_args g,
+                                                              float* delta) {
+    const heddle_attention_args& a = g.fwd;
+    const int lane = threadIdx.x % GL;
+    const uint32_t r = blockIdx.x * (256 / GL) + threadIdx.x / GL;  // (b, i, h)
+    const uint32_t heads = a.q_heads, n = (uint32_t)a.q_len;
+    if (r >= a.batch * heads * n) return;
+    const uint32_t h = r % heads, bi = r / heads, i = bi % n, b = bi / n;
+    float s = 0.0f;
+    if (lane * 8 < a.head_dim) {
+        const uint4 u = *reinterpret_cast<const uint4*>(at<T>(a.o, b, i, h) + lane * 8);
+        const uint4 w = *reinterpret_cast<const uint4*>(at<T>(g.d_o, b, i, h) + lane * 8);
+        const T *x = reinterpret_cast<const T*>(&u), *y = reinterpret_cast<const T*>(&w);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) s += to_float(x[j]) * to_float(y[j]);
+    }
+    const uint32_t mask = ((1ull << GL) - 1) << (threadIdx.x % 32 / GL * GL);
+#pragma unroll
+    for (int o = GL / 2; o; o >>= 1) s += __shfl_xor_sync(mask, s, o, GL);
+    if (lane == 0) delta[((int64_t)b * heads + h) * n + i] = s;
+}
+
+bool units16(const heddle_heads& t) {
+    return (uintptr_t)t.data % 16 == 0 && t.batch_stride % 8 == 0 && t.token_stride % 8 == 0 && t.head_stride % 8 == 0;
+}
+
 // delta_i = do_i . o_i
 template <class T>
 __global__ void __launch_bounds__(kWarps * 32) attn_delta_kernel(heddle_attention_grad_args g, float* delta) {
@@ -153,7 +182,14 @@ template <class T>
 cudaError_t attention_grad(const OpContext& x, const heddle_attention_grad_args& g, float* delta, cudaStream_t st) {
     const heddle_attention_args& a = g.fwd;
     const int64_t rows = a.batch * a.q_heads * a.q_len, keys = a.batch * a.kv_heads * a.kv_len;
-    if (rows) attn_delta_kernel<T><<<row_blocks(x, rows), kWarps * 32, 0, st>>>(g, delta);
+    if (rows && a.head_dim % 8 == 0 && a.head_dim <= 128 && units16(a.o) && units16(g.d_o)) {
+        if (a.head_dim <= 64)
+            attn_delta_wide_kernel<T, 8><<<(unsigned)ceil_div(rows, 32), 256, 0, st>>>(g, delta);
+        else
+            attn_delta_wide_kernel<T, 16><<<(unsigned)ceil_div(rows, 16), 256, 0, st>>>(g, delta);
+    } else if (rows) {
+        attn_delta_kernel<T><<<row_blocks(x, rows), kWarps * 32, 0, st>>>(g, delta);
+    }
     if (attn_tc_takes_grad(g)) {
         const cudaError_t e = cudaGetLastError();
         return e == cudaSuccess ? launch_attn_tc_grad(x, g, delta, st) : e;

@@ -115,12 +115,12 @@ __device__ __forceinline__ void mma_dims(uint32_t d, uint32_t a, uint32_t b, uin
         mma_ss(d, smem_desc(a + at, 16384), smem_desc(b + at, 16384), idesc, k != 0);
     }
 }
-// D[128][DP] (+)= W B over 128 rows of B: W in tensor memory, its upper 64
-// columns `gap` columns after its lower ones.
+// D[128][DP] (+)= W B over 128 rows of B: W in tensor memory, 16 columns for
+// every 32 rows, `gap` columns from one 16 to the next.
 __device__ __forceinline__ void mma_rows(uint32_t d, uint32_t w, int gap, uint32_t b, uint32_t idesc, bool add) {
 #pragma unroll
     for (int k = 0; k < 8; ++k)
-        mma_ts(d, w + (k % 4) * 8 + (k / 4) * gap, smem_desc(b + k * 2048, 16384), idesc, add || k);
+        mma_ts(d, w + (k % 2) * 8 + (k / 2) * gap, smem_desc(b + k * 2048, 16384), idesc, add || k);
 }
 
 template <int DP>
@@ -283,7 +283,7 @@ __global__ void __launch_bounds__(Forward<DP, NT>::kThreads, 1)
                 if (j >= 0 && j0 + j < to[q]) {
                     if (!(go = mbar_wait(p_ready + 8 * q, j & 1, gave_up))) break;
                     fence_after();
-                    mma_rows(to_acc, ts, 32, smem_u32(ring + sv * F::kTileBytes), id_o, j > 0);
+                    mma_rows(to_acc, ts, 16, smem_u32(ring + sv * F::kTileBytes), id_o, j > 0);
                     if (j0 + j + 1 == to[q]) commit(o_done + 8 * q);
                 }
                 if (j0 + j + 1 < to[q]) {
@@ -455,7 +455,10 @@ __global__ void __launch_bounds__(256) attn_join_kernel(const __grid_constant__ 
 
 // ------------------------------------------------------------------ backward
 
-constexpr int kGradThreads = 128 + 256;
+// Sixteen warps turn scores into dS, four for every quarter of a tile's
+// columns: with eight, each scheduler's two warps left it idle two thirds of
+// the time.
+constexpr int kGradWarps = 16, kGradThreads = 128 + 32 * kGradWarps;
 
 // Bars of a backward kernel, in the order that follows its tiles.
 struct GradBars {
@@ -472,10 +475,10 @@ struct GradBars {
         }
         mbar_init(a_full, 1);
         mbar_init(b_full, 1);
-        mbar_init(a_ready, 8);
-        mbar_init(b_ready, 8);
-        mbar_init(b_ready + 8, 8);
-        mbar_init(stats, 8);
+        mbar_init(a_ready, kGradWarps);
+        mbar_init(b_ready, kGradWarps);
+        mbar_init(b_ready + 8, kGradWarps);
+        mbar_init(stats, kGradWarps);
         mbar_init(done, 1);
     }
 };
@@ -559,13 +562,13 @@ __global__ void __launch_bounds__(kGradThreads, 1)
                 const int st = j & 1;
                 if (!(go = mbar_wait(bar.b_ready + 8 * st, j / 2 & 1, gave_up))) break;
                 fence_after();
-                mma_rows(at_dq, at_ds + 64 * st, 32, smem_u32(stage + 2 * st * G::kTileBytes), id_d, j > 0);
+                mma_rows(at_dq, at_ds + 64 * st, 16, smem_u32(stage + 2 * st * G::kTileBytes), id_d, j > 0);
                 commit(bar.empty + 8 * st);
             }
         }
         if (go) commit(bar.done);
     } else if (warp >= 4) {
-        const int side = (warp - 4) / 4, row = (warp % 4) * 32 + lane;  // which 64 of a tile's 128 keys
+        const int side = (warp - 4) / 4, row = (warp % 4) * 32 + lane;  // which 32 of a tile's 128 keys
         const uint32_t lanes = (uint32_t)(warp % 4 * 32) << 16;
         const int64_t i = t0 + row / p.group, h = (int64_t)hk * p.group + row % p.group;
         const bool inside = row < p.group * p.tokens && i < p.a.q_len;
@@ -577,33 +580,35 @@ __global__ void __launch_bounds__(kGradThreads, 1)
         bool go = true;
         for (int j = 0; j < n; ++j) {
             const int64_t k0 = (int64_t)keys.at(j) * kTile;
+            const bool whole = t0 + p.tokens <= s.ql && all_visible(p, s, t0, t1, k0);
             if (!(go = __all_sync(~0u, mbar_wait(bar.a_full, j & 1, gave_up)))) break;
             fence_after();
-            uint32_t v[2][32], d[2][32];
-#pragma unroll
-            for (int x = 0; x < 2; ++x) {
-                tmem_ld32(at_s + lanes + side * 64 + 32 * x, v[x]);
-                tmem_ld32(at_dp + lanes + side * 64 + 32 * x, d[x]);
-            }
+            uint32_t v[32], d[32], w[16];
+            tmem_ld32(at_s + lanes + side * 32, v);
+            tmem_ld32(at_dp + lanes + side * 32, d);
             wait_ld();
             fence_before();
             __syncwarp();
             if (lane == 0) mbar_arrive(bar.a_ready);
-            const bool whole = t0 + p.tokens <= s.ql && all_visible(p, s, t0, t1, k0);
-            uint32_t w[32];
-#pragma unroll
-            for (int x = 0; x < 2; ++x)
-#pragma unroll
-                for (int y = 0; y < 32; ++y) {
-                    float e = exp2_fast(fmaf(__uint_as_float(v[x][y]), c, -lse));
-                    if (!whole && !mask.sees((int)k0 + side * 64 + 32 * x + y)) e = 0.0f;
-                    // a product with what lies in hidden places must not count
-                    v[x][y] = __float_as_uint(e == 0.0f ? 0.0f : e * (__uint_as_float(d[x][y]) - delta));
-                }
 #pragma unroll
             for (int y = 0; y < 32; ++y)
-                w[y] = pack_two<T>(__uint_as_float(v[y / 16][2 * y % 32]), __uint_as_float(v[y / 16][2 * y % 32 + 1]));
-            tmem_st32(at_ds + 64 * (j & 1) + lanes + side * 32, w);
+                v[y] = __float_as_uint(exp2_fast(fmaf(__uint_as_float(v[y]), c, -lse)));
+            if (whole) {
+#pragma unroll
+                for (int y = 0; y < 32; ++y)
+                    d[y] = __float_as_uint(__uint_as_float(v[y]) * (__uint_as_float(d[y]) - delta));
+            } else {
+                // a product with what lies in hidden places must not count
+#pragma unroll
+                for (int y = 0; y < 32; ++y) {
+                    const float e = mask.sees((int)k0 + side * 32 + y) ? __uint_as_float(v[y]) : 0.0f;
+                    d[y] = __float_as_uint(e == 0.0f ? 0.0f : e * (__uint_as_float(d[y]) - delta));
+                }
+            }
+#pragma unroll
+            for (int y = 0; y < 16; ++y)
+                w[y] = pack_two<T>(__uint_as_float(d[2 * y]), __uint_as_float(d[2 * y + 1]));
+            tmem_st16(at_ds + 64 * (j & 1) + lanes + side * 16, w);
             if (side == 0 && s.kl < p.a.kv_len && k0 + kTile > s.kl) {  // keys past the sequence
                 clear_rows<DP>(stage + 2 * (j & 1) * G::kTileBytes, row, s.kl - k0);
                 fence_async_shared();
@@ -680,7 +685,7 @@ __global__ void __launch_bounds__(kGradThreads, 1)
     if (warp == 2) tmem_alloc(smem_u32(tmem_at), 512);
     if (warp >= 4) {  // rows that no copy writes are zero throughout
         const int row = threadIdx.x & 127, rows = p.group * p.tokens;
-        for (int x = 0; x < 4; ++x) clear_rows<DP>(stage + x * G::kTileBytes, row, rows);
+        clear_rows<DP>(stage + (threadIdx.x - 128) / 128 * G::kTileBytes, row, rows);
         fence_async_shared();
     }
     fence_before();
@@ -713,7 +718,7 @@ __global__ void __launch_bounds__(kGradThreads, 1)
             if (j >= 0) {
                 if (!(go = mbar_wait(bar.a_ready, j & 1, gave_up))) break;
                 fence_after();
-                mma_rows(at_dv, at_s, 64, tq + G::kTileBytes, id_d, j > 0);
+                mma_rows(at_dv, at_s, 32, tq + G::kTileBytes, id_d, j > 0);
             }
             if (j + 1 < n) {
                 if (!(go = mbar_wait(bar.full + 8 * nx, (j + 1) / 2 & 1, gave_up))) break;
@@ -724,7 +729,7 @@ __global__ void __launch_bounds__(kGradThreads, 1)
             if (j >= 0) {
                 if (!(go = mbar_wait(bar.b_ready, j & 1, gave_up))) break;
                 fence_after();
-                mma_rows(at_dk, at_dp, 64, tq, id_d, j > 0);
+                mma_rows(at_dk, at_dp, 32, tq, id_d, j > 0);
                 commit(bar.empty + 8 * st);
             }
             if (j + 1 < n) {
@@ -736,13 +741,14 @@ __global__ void __launch_bounds__(kGradThreads, 1)
         }
         if (go) commit(bar.done);
     } else if (warp >= 4) {
-        const int side = (warp - 4) / 4, row = (warp % 4) * 32 + lane;  // which 64 of a tile's 128 queries
+        const int side = (warp - 4) / 4, row = (warp % 4) * 32 + lane;  // which 32 of a tile's 128 queries
         const uint32_t lanes = (uint32_t)(warp % 4 * 32) << 16;
         const int64_t key = k0 + row;
         const float c = p.scale_log2;
 
-        // statistics of query tile j to buffer j % 3: written a step ahead,
-        // while the slowest warp may still read those of the step before
+        // statistics of query tile j to buffer j % 3, by the first two sides:
+        // written a step ahead, while the slowest warp may still read those of
+        // the step before
         auto put_stats = [&](int j) {
             const int64_t i = (int64_t)(first + j) * p.tokens + row / p.group;
             const int64_t h = (int64_t)hk * p.group + row % p.group;
@@ -751,10 +757,11 @@ __global__ void __launch_bounds__(kGradThreads, 1)
             float2* to = stat + (j % 3) * kTile + row;
             if (side == 0) {
                 const float l = live ? p.a.lse[r] : INFINITY;
-                to->x = l == -INFINITY ? INFINITY : l * kLog2e;
-                pos[(j % 3) * kTile + row] = live ? (int)max(s.off + i, (int64_t)-1) : -1;
-            } else {
+                to->x = l == -INFINITY ? -INFINITY : -l * kLog2e;
+            } else if (side == 1) {
                 to->y = live ? p.delta[r] : 0.0f;
+            } else if (side == 2) {
+                pos[(j % 3) * kTile + row] = live ? (int)max(s.off + i, (int64_t)-1) : -1;
             }
         };
         bool go = true;
@@ -771,32 +778,30 @@ __global__ void __launch_bounds__(kGradThreads, 1)
                 if (lane == 0) mbar_arrive(bar.stats);
             }
             const int64_t t0 = (int64_t)(first + j) * p.tokens, t1 = t0 + p.tokens;
-            const float2* st = stat + (j % 3) * kTile + side * 64;
-            const int* at = pos + (j % 3) * kTile + side * 64;
+            const float4* st = reinterpret_cast<const float4*>(stat + (j % 3) * kTile + side * 32);
             const bool whole = t1 <= s.ql && all_visible(p, s, t0, t1, k0);
             if (!(go = __all_sync(~0u, mbar_wait(bar.a_full, j & 1, gave_up)))) break;
             fence_after();
-            uint32_t v[2][32];
-            tmem_ld32(at_s + lanes + side * 64, v[0]);
-            tmem_ld32(at_s + lanes + side * 64 + 32, v[1]);
+            uint32_t v[32], w[16];
+            tmem_ld32(at_s + lanes + side * 32, v);
             wait_ld();
-            uint32_t w[32];
 #pragma unroll
-            for (int x = 0; x < 2; ++x)
+            for (int y = 0; y < 32; y += 2) {
+                const float4 f = st[y / 2];
+                v[y] = __float_as_uint(exp2_fast(fmaf(__uint_as_float(v[y]), c, f.x)));
+                v[y + 1] = __float_as_uint(exp2_fast(fmaf(__uint_as_float(v[y + 1]), c, f.z)));
+            }
+            if (!whole) {
+                const int* at = pos + (j % 3) * kTile + side * 32;
 #pragma unroll
-                for (int y = 0; y < 32; ++y) {
-                    float e = exp2_fast(fmaf(__uint_as_float(v[x][y]), c, -st[32 * x + y].x));
-                    if (!whole) {
-                        const RowMask mask(at[32 * x + y], p.a);
-                        if (!mask.sees((int)key)) e = 0.0f;
-                    }
-                    v[x][y] = __float_as_uint(e);
-                }
+                for (int y = 0; y < 32; ++y)
+                    if (!RowMask(at[y], p.a).sees((int)key)) v[y] = 0;
+            }
 #pragma unroll
-            for (int y = 0; y < 32; ++y)
-                w[y] = pack_two<T>(__uint_as_float(v[y / 16][2 * y % 32]), __uint_as_float(v[y / 16][2 * y % 32 + 1]));
-            tmem_st32(at_s + lanes + side * 64, w);
-            if (s.ql < p.a.q_len && t1 > s.ql) {  // queries past the sequence: side 0 clears Q, side 1 dO
+            for (int y = 0; y < 16; ++y)
+                w[y] = pack_two<T>(__uint_as_float(v[2 * y]), __uint_as_float(v[2 * y + 1]));
+            tmem_st16(at_s + lanes + side * 32, w);
+            if (side < 2 && s.ql < p.a.q_len && t1 > s.ql) {  // queries past the sequence: side 0 clears Q, 1 dO
                 const int st2 = j & 1;
                 const uint32_t loaded = side ? bar.full2 : bar.full;
                 if (!(go = __all_sync(~0u, mbar_wait(loaded + 8 * st2, j / 2 & 1, gave_up)))) break;
@@ -810,21 +815,24 @@ __global__ void __launch_bounds__(kGradThreads, 1)
 
             if (!(go = __all_sync(~0u, mbar_wait(bar.b_full, j & 1, gave_up)))) break;
             fence_after();
-            uint32_t d[2][32];
-            tmem_ld32(at_dp + lanes + side * 64, d[0]);
-            tmem_ld32(at_dp + lanes + side * 64 + 32, d[1]);
+            uint32_t d[32];
+            tmem_ld32(at_dp + lanes + side * 32, d);
             wait_ld();
 #pragma unroll
-            for (int x = 0; x < 2; ++x)
+            for (int y = 0; y < 32; y += 2) {
+                const float4 f = st[y / 2];
+                d[y] = __float_as_uint(__uint_as_float(v[y]) * (__uint_as_float(d[y]) - f.y));
+                d[y + 1] = __float_as_uint(__uint_as_float(v[y + 1]) * (__uint_as_float(d[y + 1]) - f.w));
+            }
+            if (!whole) {  // a product with what lies in hidden places must not count
 #pragma unroll
-                for (int y = 0; y < 32; ++y) {
-                    const float e = __uint_as_float(v[x][y]);
-                    d[x][y] = __float_as_uint(e == 0.0f ? 0.0f : e * (__uint_as_float(d[x][y]) - st[32 * x + y].y));
-                }
+                for (int y = 0; y < 32; ++y)
+                    if (__uint_as_float(v[y]) == 0.0f) d[y] = 0;
+            }
 #pragma unroll
-            for (int y = 0; y < 32; ++y)
-                w[y] = pack_two<T>(__uint_as_float(d[y / 16][2 * y % 32]), __uint_as_float(d[y / 16][2 * y % 32 + 1]));
-            tmem_st32(at_dp + lanes + side * 64, w);
+            for (int y = 0; y < 16; ++y)
+                w[y] = pack_two<T>(__uint_as_float(d[2 * y]), __uint_as_float(d[2 * y + 1]));
+            tmem_st16(at_dp + lanes + side * 32, w);
             wait_st();
             fence_before();
             __syncwarp();
@@ -832,7 +840,7 @@ __global__ void __launch_bounds__(kGradThreads, 1)
         }
         if (go && n > 0) go = __all_sync(~0u, mbar_wait(bar.done, 0, gave_up));
         fence_after();
-        if (go) {
+        if (go && side < 2) {
             const heddle_heads& t = side ? p.dk : p.dv;
             T* out = static_cast<T*>(t.data) + b * t.batch_stride + key * t.token_stride + hk * t.head_stride;
             const bool inside = key < p.a.kv_len;
