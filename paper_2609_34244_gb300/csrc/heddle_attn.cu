@@ -179,7 +179,8 @@ unsigned row_blocks(const OpContext& x, int64_t rows) {
 }
 
 template <class T>
-cudaError_t attention_grad(const OpContext& x, const heddle_attention_grad_args& g, float* delta, cudaStream_t st) {
+cudaError_t attention_grad(const OpContext& x, const heddle_attention_grad_args& g, float* delta, unsigned char* rest,
+                           cudaStream_t st) {
     const heddle_attention_args& a = g.fwd;
     const int64_t rows = a.batch * a.q_heads * a.q_len, keys = a.batch * a.kv_heads * a.kv_len;
     if (rows && a.head_dim % 8 == 0 && a.head_dim <= 128 && units16(a.o) && units16(g.d_o)) {
@@ -192,7 +193,7 @@ cudaError_t attention_grad(const OpContext& x, const heddle_attention_grad_args&
     }
     if (attn_tc_takes_grad(g)) {
         const cudaError_t e = cudaGetLastError();
-        return e == cudaSuccess ? launch_attn_tc_grad(x, g, delta, st) : e;
+        return e == cudaSuccess ? launch_attn_tc_grad(x, g, delta, rest, st) : e;
     }
     if (rows) {
         attn_dq_row_kernel<T><<<row_blocks(x, rows), kWarps * 32, 0, st>>>(g, delta);
@@ -217,15 +218,20 @@ cudaError_t launch_attention(const OpContext& x, const heddle_attention_args& a,
     return cudaGetLastError();
 }
 
-size_t attention_grad_scratch(const OpContext&, const heddle_attention_grad_args& g) {
-    return align256(sizeof(float) * (size_t)(g.fwd.batch * g.fwd.q_heads * g.fwd.q_len));
+static size_t delta_bytes(const heddle_attention_args& a) {
+    return align256(sizeof(float) * (size_t)(a.batch * a.q_heads * a.q_len));
+}
+
+size_t attention_grad_scratch(const OpContext& x, const heddle_attention_grad_args& g) {
+    return delta_bytes(g.fwd) + (attn_tc_takes_grad(g) ? attn_tc_grad_scratch(x, g.fwd) : 0);
 }
 
 cudaError_t launch_attention_grad(const OpContext& x, const heddle_attention_grad_args& g, unsigned char* ws,
                                   cudaStream_t st) {
     float* delta = reinterpret_cast<float*>(ws);
-    return g.fwd.dtype == HEDDLE_BF16 ? attention_grad<__nv_bfloat16>(x, g, delta, st)
-                                      : attention_grad<__half>(x, g, delta, st);
+    unsigned char* rest = ws + delta_bytes(g.fwd);
+    return g.fwd.dtype == HEDDLE_BF16 ? attention_grad<__nv_bfloat16>(x, g, delta, rest, st)
+                                      : attention_grad<__half>(x, g, delta, rest, st);
 }
 
 }  // namespace hd

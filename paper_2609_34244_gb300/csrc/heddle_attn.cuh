@@ -23,7 +23,8 @@ bool attn_tc_takes(const heddle_attention_args& a);
 bool attn_tc_takes_grad(const heddle_attention_grad_args& g);
 size_t attn_tc_scratch(const OpContext& x, const heddle_attention_args& a);
 cudaError_t launch_attn_tc(const OpContext& x, const heddle_attention_args& a, unsigned char* ws, cudaStream_t st);
+size_t attn_tc_grad_scratch(const OpContext& x, const heddle_attention_args& a);
 cudaError_t launch_attn_tc_grad(const OpContext& x, const heddle_attention_grad_args& g, const float* delta,
-                                cudaStream_t st);
+                                unsigned char* ws, cudaStream_t st);
 
 }  // namespace hd

@@ -55,6 +55,10 @@ struct Params {
     float scale_log2;
     float* part_o;    // [splits][batch * q_heads * q_len][head_dim]
     float* part_lse;  // [splits][batch * q_heads * q_len]
+    // backward over keys: the first `lead` key tiles in lead_parts parts along
+    // the queries, the others in rest_parts; sums of parts as floats
+    int32_t lead, lead_parts, rest_parts;
+    float *part_dk, *part_dv;  // [slots][128][head_dim]
     uint32_t* err;
 };
 
@@ -115,12 +119,13 @@ __device__ __forceinline__ void mma_dims(uint32_t d, uint32_t a, uint32_t b, uin
         mma_ss(d, smem_desc(a + at, 16384), smem_desc(b + at, 16384), idesc, k != 0);
     }
 }
-// D[128][DP] (+)= W B over 128 rows of B: W in tensor memory, 16 columns for
-// every 32 rows, `gap` columns from one 16 to the next.
-__device__ __forceinline__ void mma_rows(uint32_t d, uint32_t w, int gap, uint32_t b, uint32_t idesc, bool add) {
+// D[128][DP] (+)= W B over 128 rows of B: W in tensor memory, 64 columns in
+// runs of RUN, the next one `GAP` columns further.
+template <int RUN, int GAP>
+__device__ __forceinline__ void mma_rows(uint32_t d, uint32_t w, uint32_t b, uint32_t idesc, bool add) {
 #pragma unroll
     for (int k = 0; k < 8; ++k)
-        mma_ts(d, w + (k % 2) * 8 + (k / 2) * gap, smem_desc(b + k * 2048, 16384), idesc, add || k);
+        mma_ts(d, w + k * 8 % RUN + k * 8 / RUN * GAP, smem_desc(b + k * 2048, 16384), idesc, add || k);
 }
 
 template <int DP>
@@ -165,6 +170,23 @@ __device__ __forceinline__ void store_row(uint32_t tmem, T* out, bool live, int 
         }
     }
 }
+template <int COLS>
+__device__ __forceinline__ void store_floats(uint32_t tmem, float* out, bool live, int D, float f) {
+#pragma unroll 1
+    for (int c = 0; c < COLS; c += 32) {
+        __syncwarp();
+        uint32_t v[32];
+        tmem_ld32(tmem + c, v);
+        wait_ld();
+        if (!live) continue;
+#pragma unroll
+        for (int j = 0; j < 32; j += 4)
+            if (c + j < D)  // whole units of four: head_dim is a multiple of eight
+                *reinterpret_cast<float4*>(out + c + j) =
+                    make_float4(__uint_as_float(v[j]) * f, __uint_as_float(v[j + 1]) * f, __uint_as_float(v[j + 2]) * f,
+                                __uint_as_float(v[j + 3]) * f);
+    }
+}
 template <class T>
 __device__ __forceinline__ void zero_row(T* out, int D) {
     for (int c = 0; c < D; ++c) out[c] = from_float<T>(0.0f);
@@ -172,16 +194,18 @@ __device__ __forceinline__ void zero_row(T* out, int D) {
 
 // ------------------------------------------------------------------- forward
 
-// NT query tiles of a key head against the key tiles that they see, one
-// group of four warps each.  While one tile's warps turn scores into weights
-// the tensor cores run the other's products.
+// NT query tiles of a key head against the key tiles that they see, eight
+// warps each: two threads a row, half of the columns each (one warp a row
+// left its scheduler idle most of the time).  While one tile's warps turn
+// scores into weights the tensor cores run the other's products.
 template <int DP, int NT>
 struct Forward {
     static constexpr int kTileBytes = kTile * DP * 2;
-    static constexpr int kRoom = 227 * 1024 - 1024 - 256 - NT * kTileBytes;
+    static constexpr int kHigh = 2 * NT * 2 * kTile * 4;  // the halves' maxima, by turns
+    static constexpr int kRoom = 227 * 1024 - 1024 - 512 - kHigh - NT * kTileBytes;
     static constexpr int kSlots = kRoom / kTileBytes < 8 ? kRoom / kTileBytes : 8;  // K and V tiles by turns
-    static constexpr int kBytes = 1024 + (NT + kSlots) * kTileBytes + 256;
-    static constexpr int kThreads = 128 + NT * 128;
+    static constexpr int kBytes = 1024 + (NT + kSlots) * kTileBytes + 512 + kHigh;
+    static constexpr int kThreads = 128 + NT * 256;
     static constexpr int kCols = NT * (kTile + DP) <= 256 ? 256 : 512;
 };
 
@@ -195,9 +219,10 @@ __global__ void __launch_bounds__(Forward<DP, NT>::kThreads, 1)
     unsigned char* ring = base + NT * F::kTileBytes;
     uint64_t* bars = reinterpret_cast<uint64_t*>(ring + F::kSlots * F::kTileBytes);
     const uint32_t full = smem_u32(bars), empty = full + 8 * F::kSlots, q_full = empty + 8 * F::kSlots,
-                   s_full = q_full + 16, p_ready = s_full + 16, o_done = p_ready + 16;
-    volatile uint32_t* gave_up = reinterpret_cast<uint32_t*>(bars + 2 * F::kSlots + 8);
+                   s_full = q_full + 16, p_ready = s_full + 16, o_done = p_ready + 16, met = o_done + 16;
+    volatile uint32_t* gave_up = reinterpret_cast<uint32_t*>(bars + 2 * F::kSlots + 16);
     uint32_t* tmem_at = const_cast<uint32_t*>(gave_up) + 1;
+    float* highs = reinterpret_cast<float*>(reinterpret_cast<unsigned char*>(bars) + 512);  // [2][NT][2][128]
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
 
     // the last queries see the most keys: their tiles start first
@@ -235,9 +260,10 @@ __global__ void __launch_bounds__(Forward<DP, NT>::kThreads, 1)
         for (int q = 0; q < 2; ++q) {
             mbar_init(q_full + 8 * q, 1);
             mbar_init(s_full + 8 * q, 1);
-            mbar_init(p_ready + 8 * q, 4);
+            mbar_init(p_ready + 8 * q, 8);
             mbar_init(o_done + 8 * q, 1);
         }
+        for (int q = 0; q < 8; ++q) mbar_init(met + 8 * q, 2);
         *gave_up = 0;
         mbar_fence_init();
     }
@@ -283,7 +309,7 @@ __global__ void __launch_bounds__(Forward<DP, NT>::kThreads, 1)
                 if (j >= 0 && j0 + j < to[q]) {
                     if (!(go = mbar_wait(p_ready + 8 * q, j & 1, gave_up))) break;
                     fence_after();
-                    mma_rows(to_acc, ts, 16, smem_u32(ring + sv * F::kTileBytes), id_o, j > 0);
+                    mma_rows<32, 64>(to_acc, ts, smem_u32(ring + sv * F::kTileBytes), id_o, j > 0);
                     if (j0 + j + 1 == to[q]) commit(o_done + 8 * q);
                 }
                 if (j0 + j + 1 < to[q]) {
@@ -297,9 +323,10 @@ __global__ void __launch_bounds__(Forward<DP, NT>::kThreads, 1)
             if (j + 1 < n) commit(empty + 8 * sk);
         }
     } else if (warp >= 4) {
-        const int q = (warp - 4) / 4, row = (warp % 4) * 32 + lane;
+        const int q = (warp - 4) / 8, side = (warp - 4) / 4 % 2, row = (warp % 4) * 32 + lane;
         const uint32_t lanes = (uint32_t)(warp % 4 * 32) << 16;
         const uint32_t ts = tmem + lanes + q * kTile, to_acc = tmem + lanes + NT * kTile + q * DP;
+        const uint32_t pair = met + 8 * (q * 4 + warp % 4);  // this warp and the one of the rows' other half
         const int64_t i0 = t0 + (int64_t)q * p.tokens, i1 = i0 + p.tokens;
         const int64_t i = i0 + row / p.group;
         const int64_t h = (int64_t)hk * p.group + row % p.group;
@@ -308,27 +335,39 @@ __global__ void __launch_bounds__(Forward<DP, NT>::kThreads, 1)
         float top = -INFINITY, sum = 0.0f;
         const int mine = to[q] - j0;
         bool go = true;
+        // the other half's value for the row, and this one's for it
+        auto swap = [&](int turn, float v) {
+            float* at = highs + ((turn & 1) * NT + q) * 2 * kTile + row;
+            at[side * kTile] = v;
+            __syncwarp();
+            if (lane == 0) mbar_arrive(pair);
+            go = __all_sync(~0u, mbar_wait(pair, turn & 1, gave_up));
+            return at[(side ^ 1) * kTile];
+        };
         for (int j = 0; j < mine; ++j) {
-            const int64_t k0 = (int64_t)keys.at(j0 + j) * kTile;
+            const int k0 = keys.at(j0 + j) * kTile;
+            const bool whole = all_visible(p, s, i0, min(i1, s.ql), k0);
             if (!(go = __all_sync(~0u, mbar_wait(s_full + 8 * q, j & 1, gave_up)))) break;
             fence_after();
-            uint32_t v[4][32];
+            uint32_t v[2][32];
 #pragma unroll
-            for (int x = 0; x < 4; ++x) tmem_ld32(ts + 32 * x, v[x]);
+            for (int x = 0; x < 2; ++x) tmem_ld32(ts + 64 * side + 32 * x, v[x]);
             wait_ld();
-            if (!all_visible(p, s, i0, min(i1, s.ql), k0)) {
+            if (!whole) {
 #pragma unroll
-                for (int x = 0; x < 4; ++x)
+                for (int x = 0; x < 2; ++x)
 #pragma unroll
                     for (int y = 0; y < 32; ++y)
-                        if (!mask.sees((int)k0 + 32 * x + y)) v[x][y] = 0xff800000u;  // -infinity
+                        if (!mask.sees(k0 + 64 * side + 32 * x + y)) v[x][y] = 0xff800000u;  // -infinity
             }
             float m4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
-            for (int x = 0; x < 4; ++x)
+            for (int x = 0; x < 2; ++x)
 #pragma unroll
                 for (int y = 0; y < 32; ++y) m4[y % 4] = fmaxf(m4[y % 4], __uint_as_float(v[x][y]));
-            const float high = fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3]));
+            float high = fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3]));
+            high = fmaxf(high, swap(j, high));
+            if (!go) break;
             float keep = 1.0f;
             if (high > top && (top == -INFINITY || (high - top) * c > kSlack)) {
                 keep = top == -INFINITY ? 0.0f : exp2_fast((top - high) * c);
@@ -339,32 +378,32 @@ __global__ void __launch_bounds__(Forward<DP, NT>::kThreads, 1)
                 // the product of the step before has completed: the scores'
                 // barrier was committed after it
 #pragma unroll 1
-                for (int x = 0; x < DP; x += 32) {
-                    uint32_t o[32];
-                    tmem_ld32(to_acc + x, o);
+                for (int x = 0; x < DP / 2; x += 16) {
+                    uint32_t o[16];
+                    tmem_ld16(to_acc + side * (DP / 2) + x, o);
                     wait_ld();
 #pragma unroll
-                    for (int y = 0; y < 32; ++y) o[y] = __float_as_uint(__uint_as_float(o[y]) * keep);
-                    tmem_st32(to_acc + x, o);
+                    for (int y = 0; y < 16; ++y) o[y] = __float_as_uint(__uint_as_float(o[y]) * keep);
+                    tmem_st16(to_acc + side * (DP / 2) + x, o);
                 }
             }
             const float sub = top == -INFINITY ? 0.0f : top * c;
             float s4[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-            for (int x = 0; x < 4; x += 2) {
-                uint32_t w[32];
+            for (int x = 0; x < 2; ++x) {
+                uint32_t w[16];
 #pragma unroll
-                for (int y = 0; y < 64; y += 2) {
-                    const float lo = exp2_fast(fmaf(__uint_as_float(v[x + y / 32][y % 32]), c, -sub));
-                    const float hi = exp2_fast(fmaf(__uint_as_float(v[x + y / 32][y % 32 + 1]), c, -sub));
+                for (int y = 0; y < 32; y += 2) {
+                    const float lo = exp2_fast(fmaf(__uint_as_float(v[x][y]), c, -sub));
+                    const float hi = exp2_fast(fmaf(__uint_as_float(v[x][y + 1]), c, -sub));
                     s4[y % 4] += lo;
                     s4[y % 4 + 1] += hi;
                     w[y / 2] = pack_two<T>(lo, hi);
                 }
-                tmem_st32(ts + 16 * x, w);
+                tmem_st16(ts + 64 * side + 16 * x, w);  // over scores that this warp itself has read
             }
             sum += (s4[0] + s4[1]) + (s4[2] + s4[3]);
-            if (s.kl < p.a.kv_len && k0 + kTile > s.kl) {  // values past the sequence
+            if (side == 0 && s.kl < p.a.kv_len && k0 + kTile > s.kl) {  // values past the sequence
                 const int iv = 2 * j + 1, sv = iv % F::kSlots;
                 if (!(go = __all_sync(~0u, mbar_wait(full + 8 * sv, iv / F::kSlots & 1, gave_up)))) break;
                 clear_rows<DP>(ring + sv * F::kTileBytes, row, s.kl - k0);
@@ -375,7 +414,10 @@ __global__ void __launch_bounds__(Forward<DP, NT>::kThreads, 1)
             __syncwarp();
             if (lane == 0) mbar_arrive(p_ready + 8 * q);
         }
-        if (go && mine > 0) go = __all_sync(~0u, mbar_wait(o_done + 8 * q, 0, gave_up));
+        if (go && mine > 0) {
+            sum += swap(mine, sum);
+            if (go) go = __all_sync(~0u, mbar_wait(o_done + 8 * q, 0, gave_up));
+        }
         fence_after();
         if (go) {
             const bool inside = row < p.group * p.tokens && i < p.a.q_len;
@@ -383,32 +425,18 @@ __global__ void __launch_bounds__(Forward<DP, NT>::kThreads, 1)
             const float f = some ? 1.0f / sum : 0.0f;
             const float lse = some ? (top * c + log2f(sum)) * kLn2 : -INFINITY;
             const int64_t r = ((int64_t)b * p.a.q_heads + h) * p.a.q_len + i;
-            const int D = p.a.head_dim;
+            const int D = p.a.head_dim, d0 = side * (DP / 2);
             if (p.splits > 1) {
                 const int64_t at = (int64_t)split * p.a.batch * p.a.q_heads * p.a.q_len + r;
-                if (inside) p.part_lse[at] = lse;
-#pragma unroll 1
-                for (int x = 0; x < DP; x += 32) {
-                    __syncwarp();
-                    uint32_t o[32];
-                    if (mine > 0) {
-                        tmem_ld32(to_acc + x, o);
-                        wait_ld();
-                    }
-                    if (!inside || !some) continue;  // a part of no weight is not read
-#pragma unroll
-                    for (int y = 0; y < 32; y += 4)
-                        if (x + y < D)
-                            *reinterpret_cast<float4*>(p.part_o + at * D + x + y) =
-                                make_float4(__uint_as_float(o[y]) * f, __uint_as_float(o[y + 1]) * f,
-                                            __uint_as_float(o[y + 2]) * f, __uint_as_float(o[y + 3]) * f);
-                }
+                if (inside && side == 0) p.part_lse[at] = lse;
+                // a part of no weight is not read
+                if (mine > 0) store_floats<DP / 2>(to_acc + d0, p.part_o + at * D + d0, inside && some, D - d0, f);
             } else {
                 T* out = static_cast<T*>(p.a.o.data) + b * p.a.o.batch_stride + i * p.a.o.token_stride +
-                         h * p.a.o.head_stride;
-                if (mine > 0) store_row<T, DP>(to_acc, out, inside && some, D, f);
-                if (inside && !some) zero_row(out, D);
-                if (inside && p.a.lse) p.a.lse[r] = lse;
+                         h * p.a.o.head_stride + d0;
+                if (mine > 0) store_row<T, DP / 2>(to_acc + d0, out, inside && some, D - d0, f);
+                if (inside && !some) zero_row(out, min(D - d0, DP / 2));
+                if (inside && side == 0 && p.a.lse) p.a.lse[r] = lse;
             }
         }
     }
@@ -562,7 +590,7 @@ __global__ void __launch_bounds__(kGradThreads, 1)
                 const int st = j & 1;
                 if (!(go = mbar_wait(bar.b_ready + 8 * st, j / 2 & 1, gave_up))) break;
                 fence_after();
-                mma_rows(at_dq, at_ds + 64 * st, 16, smem_u32(stage + 2 * st * G::kTileBytes), id_d, j > 0);
+                mma_rows<64, 64>(at_dq, at_ds + 64 * st, smem_u32(stage + 2 * st * G::kTileBytes), id_d, j > 0);
                 commit(bar.empty + 8 * st);
             }
         }
@@ -638,8 +666,16 @@ __global__ void __launch_bounds__(kGradThreads, 1)
     if (warp == 2) tmem_free(tmem, 512);
 }
 
-// dk and dv of a key tile, over every query tile that sees it, the group's
-// heads among its rows.  The scores are computed transposed, keys along the
+// Where the sums of a key tile's part go.
+__device__ __forceinline__ int64_t dkv_slot(const Params& p, bool lead, int tile, int hb, int part) {
+    const int64_t heads = p.a.batch * p.a.kv_heads;
+    if (lead) return (tile * heads + hb) * p.lead_parts + part;
+    return (p.lead_parts > 1 ? heads * p.lead * p.lead_parts : 0) + (tile * heads + hb) * p.rest_parts + part;
+}
+
+// dk and dv of a key tile, over every query tile that sees it (or a part of
+// them: the first tokens of a windowed call are seen by every query, and few
+// key tiles alone would leave SMs idle), the group's heads among its rows.  The scores are computed transposed, keys along the
 // lanes, so that P^T and dS^T are left operands in tensor memory as they come:
 // S^T = K Q^T, dP^T = V dO^T, dv += P^T dO, dk += dS^T Q.
 template <class T, int DP>
@@ -659,11 +695,17 @@ __global__ void __launch_bounds__(kGradThreads, 1)
     int* pos = reinterpret_cast<int*>(stat + 3 * kTile);                     // [3][128] positions
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
 
-    int64_t id = blockIdx.x;
-    const int hk = (int)(id % p.a.kv_heads);
-    id /= p.a.kv_heads;
-    const int b = (int)(id % p.a.batch);
-    const int64_t k0 = id / p.a.batch * kTile;  // the first keys are seen by the most queries
+    // the first keys are seen by the most queries
+    const int64_t heads = p.a.batch * p.a.kv_heads, lead_blocks = heads * p.lead * p.lead_parts;
+    const bool lead = blockIdx.x < lead_blocks;
+    const int parts = lead ? p.lead_parts : p.rest_parts;
+    int64_t id = lead ? blockIdx.x : blockIdx.x - lead_blocks;
+    const int part = (int)(id % parts);
+    id /= parts;
+    const int hb = (int)(id % heads), hk = hb % p.a.kv_heads, b = hb / p.a.kv_heads;
+    const int tile = (int)(id / heads);
+    const int64_t k0 = (int64_t)(lead ? tile : p.lead + tile) * kTile;
+    const int64_t slot = dkv_slot(p, lead, tile, hb, part);
     const Span s = span_of(p.a, b);
     // query tiles that see a key of the tile
     int first = 0, n = 0;
@@ -674,6 +716,9 @@ __global__ void __launch_bounds__(kGradThreads, 1)
         if (lo < hi) {
             first = (int)(lo / p.tokens);
             n = (int)((hi - 1) / p.tokens) - first + 1;
+            const int from = (int)((int64_t)n * part / parts);
+            n = (int)((int64_t)n * (part + 1) / parts) - from;
+            first += from;
         }
     }
 
@@ -718,7 +763,7 @@ __global__ void __launch_bounds__(kGradThreads, 1)
             if (j >= 0) {
                 if (!(go = mbar_wait(bar.a_ready, j & 1, gave_up))) break;
                 fence_after();
-                mma_rows(at_dv, at_s, 32, tq + G::kTileBytes, id_d, j > 0);
+                mma_rows<16, 32>(at_dv, at_s, tq + G::kTileBytes, id_d, j > 0);
             }
             if (j + 1 < n) {
                 if (!(go = mbar_wait(bar.full + 8 * nx, (j + 1) / 2 & 1, gave_up))) break;
@@ -729,7 +774,7 @@ __global__ void __launch_bounds__(kGradThreads, 1)
             if (j >= 0) {
                 if (!(go = mbar_wait(bar.b_ready, j & 1, gave_up))) break;
                 fence_after();
-                mma_rows(at_dk, at_dp, 32, tq, id_d, j > 0);
+                mma_rows<16, 32>(at_dk, at_dp, tq, id_d, j > 0);
                 commit(bar.empty + 8 * st);
             }
             if (j + 1 < n) {
@@ -844,7 +889,13 @@ __global__ void __launch_bounds__(kGradThreads, 1)
             const heddle_heads& t = side ? p.dk : p.dv;
             T* out = static_cast<T*>(t.data) + b * t.batch_stride + key * t.token_stride + hk * t.head_stride;
             const bool inside = key < p.a.kv_len;
-            if (n > 0)
+            if (parts > 1) {
+                float* to = (side ? p.part_dk : p.part_dv) + (slot * kTile + row) * p.a.head_dim;
+                if (n > 0)
+                    store_floats<DP>((side ? at_dk : at_dv) + lanes, to, true, p.a.head_dim, side ? p.a.scale : 1.0f);
+                else
+                    for (int x = 0; x < p.a.head_dim; ++x) to[x] = 0.0f;
+            } else if (n > 0)
                 store_row<T, DP>((side ? at_dk : at_dv) + lanes, out, inside, p.a.head_dim, side ? p.a.scale : 1.0f);
             else if (inside)
                 zero_row(out, p.a.head_dim);
@@ -858,6 +909,32 @@ __global__ void __launch_bounds__(kGradThreads, 1)
         __syncthreads();
     }
     if (warp == 2) tmem_free(tmem, 512);
+}
+
+// Adds up the parts of key tiles, in order: a block for 8 rows of one.
+template <class T>
+__global__ void __launch_bounds__(256) attn_dkv_join_kernel(const __grid_constant__ Params p, int is_lead) {
+    const int lane = threadIdx.x % 32, D = p.a.head_dim;
+    const int parts = is_lead ? p.lead_parts : p.rest_parts;
+    const int64_t heads = p.a.batch * p.a.kv_heads, unit = blockIdx.x / 16;
+    const int hb = (int)(unit % heads), tile = (int)(unit / heads);
+    const int row = blockIdx.x % 16 * 8 + threadIdx.x / 32;
+    const int64_t key = (int64_t)(is_lead ? tile : p.lead + tile) * kTile + row;
+    if (key >= p.a.kv_len || lane * 4 >= D) return;
+    const int64_t slot = dkv_slot(p, is_lead, tile, hb, 0);
+    for (int side = 0; side < 2; ++side) {
+        const float* from = (side ? p.part_dk : p.part_dv) + (slot * kTile + row) * D + lane * 4;
+        float4 sum = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        for (int i = 0; i < parts; ++i) {
+            const float4 f = *reinterpret_cast<const float4*>(from + (int64_t)i * kTile * D);
+            sum.x += f.x, sum.y += f.y, sum.z += f.z, sum.w += f.w;
+        }
+        const heddle_heads& t = side ? p.dk : p.dv;
+        T* out = static_cast<T*>(t.data) + (hb / p.a.kv_heads) * t.batch_stride + key * t.token_stride +
+                 (hb % p.a.kv_heads) * t.head_stride + lane * 4;
+        out[0] = from_float<T>(sum.x), out[1] = from_float<T>(sum.y);
+        out[2] = from_float<T>(sum.z), out[3] = from_float<T>(sum.w);
+    }
 }
 
 // --------------------------------------------------------------------- host
@@ -907,7 +984,27 @@ Params params_of(const OpContext& x, const heddle_attention_args& a) {
     const int64_t most = keys / (2 * kTile);
     parts = parts < most ? parts : most;
     p.splits = (int32_t)(parts < 1 ? 1 : parts > 32 ? 32 : parts);
+    // Backward over keys: blocks enough for the SMs, of four query tiles at
+    // least; the tiles of the first tokens, which every query sees, in parts
+    // of about the query tiles that a window's key tile has.
+    const int64_t heads = (int64_t)a.batch * a.kv_heads;
+    const int64_t near = a.window ? ceil_div(a.window + kTile, p.tokens) + 1 : p.q_tiles;
+    const int64_t each = near < p.q_tiles ? near : p.q_tiles;
+    int64_t rest = 3 * (int64_t)x.num_sms / (2 * heads * p.kv_tiles);
+    rest = rest < each / 4 ? rest : each / 4;
+    p.rest_parts = (int32_t)(rest < 1 ? 1 : rest > 32 ? 32 : rest);
+    const int64_t sinks = a.sinks < a.kv_len ? a.sinks : a.kv_len;
+    p.lead = a.window ? (int32_t)ceil_div(sinks, kTile) : 0;
+    const int64_t lead = p.rest_parts * p.q_tiles / (each < 8 ? 8 : each);
+    p.lead_parts = (int32_t)(lead < p.rest_parts ? p.rest_parts : lead > 64 ? 64 : lead);
     return p;
+}
+
+// Slots of partial sums of the backward pass over keys.
+int64_t dkv_slots(const Params& p) {
+    const int64_t heads = (int64_t)p.a.batch * p.a.kv_heads;
+    return heads * ((p.lead_parts > 1 ? (int64_t)p.lead * p.lead_parts : 0) +
+                    (p.rest_parts > 1 ? (int64_t)(p.kv_tiles - p.lead) * p.rest_parts : 0));
 }
 
 template <class T, int DP, int NT>
@@ -936,7 +1033,12 @@ cudaError_t backward(const Params& p, const CUtensorMap& q, const CUtensorMap& k
         e = cudaFuncSetAttribute(attn_dkv_kernel<T, DP>, cudaFuncAttributeMaxDynamicSharedMemorySize, G::kBytes);
     if (e != cudaSuccess) return e;
     const int64_t heads = p.a.batch * p.a.kv_heads;
-    attn_dkv_kernel<T, DP><<<(unsigned)(p.kv_tiles * heads), kGradThreads, G::kBytes, st>>>(q, k, v, d_o, p);
+    const int64_t blocks = heads * (p.lead * p.lead_parts + (int64_t)(p.kv_tiles - p.lead) * p.rest_parts);
+    attn_dkv_kernel<T, DP><<<(unsigned)blocks, kGradThreads, G::kBytes, st>>>(q, k, v, d_o, p);
+    if (p.lead_parts > 1 && p.lead)
+        attn_dkv_join_kernel<T><<<(unsigned)(heads * p.lead * 16), 256, 0, st>>>(p, 1);
+    if (p.rest_parts > 1 && p.kv_tiles > p.lead)
+        attn_dkv_join_kernel<T><<<(unsigned)(heads * (p.kv_tiles - p.lead) * 16), 256, 0, st>>>(p, 0);
     attn_dq_kernel<T, DP><<<(unsigned)(p.q_tiles * heads), kGradThreads, G::kBytes, st>>>(q, k, v, d_o, p);
     return cudaGetLastError();
 }
@@ -990,10 +1092,16 @@ cudaError_t launch_attn_tc(const OpContext& x, const heddle_attention_args& a, u
     return a.dtype == HEDDLE_BF16 ? forward_of<__nv_bfloat16>(p, q, k, v, st) : forward_of<__half>(p, q, k, v, st);
 }
 
+size_t attn_tc_grad_scratch(const OpContext& x, const heddle_attention_args& a) {
+    return 2 * align256((size_t)dkv_slots(params_of(x, a)) * kTile * a.head_dim * 4);
+}
+
 cudaError_t launch_attn_tc_grad(const OpContext& x, const heddle_attention_grad_args& g, const float* delta,
-                                cudaStream_t st) {
+                                unsigned char* ws, cudaStream_t st) {
     const heddle_attention_args& a = g.fwd;
     Params p = params_of(x, a);
+    p.part_dk = reinterpret_cast<float*>(ws);
+    p.part_dv = reinterpret_cast<float*>(ws + attn_tc_grad_scratch(x, a) / 2);
     p.d_o = g.d_o, p.dq = g.dq, p.dk = g.dk, p.dv = g.dv;
     p.delta = delta;
     CUtensorMap q, k, v, d_o;
