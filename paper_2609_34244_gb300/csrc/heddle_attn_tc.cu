@@ -1008,12 +1008,13 @@ int64_t dkv_slots(const Params& p) {
 }
 
 template <class T, int DP, int NT>
-cudaError_t forward(const Params& p, const CUtensorMap& q, const CUtensorMap& k, const CUtensorMap& v,
+cudaError_t forward(int device, const Params& p, const CUtensorMap& q, const CUtensorMap& k, const CUtensorMap& v,
                     cudaStream_t st) {
     using F = Forward<DP, NT>;
     static_assert(F::kSlots >= 4, "two steps of K and V");
     auto* f = attn_kernel<T, DP, NT>;
-    cudaError_t e = cudaFuncSetAttribute(f, cudaFuncAttributeMaxDynamicSharedMemorySize, F::kBytes);
+    static std::atomic<uint64_t> asked{0};
+    const cudaError_t e = allow_shared(f, F::kBytes, device, asked);
     if (e != cudaSuccess) return e;
     const int64_t grid = ceil_div(p.q_tiles, NT) * p.a.batch * p.a.kv_heads * p.splits;
     f<<<(unsigned)grid, F::kThreads, F::kBytes, st>>>(q, k, v, p);
@@ -1025,12 +1026,12 @@ cudaError_t forward(const Params& p, const CUtensorMap& q, const CUtensorMap& k,
 }
 
 template <class T, int DP>
-cudaError_t backward(const Params& p, const CUtensorMap& q, const CUtensorMap& k, const CUtensorMap& v,
+cudaError_t backward(int device, const Params& p, const CUtensorMap& q, const CUtensorMap& k, const CUtensorMap& v,
                      const CUtensorMap& d_o, cudaStream_t st) {
     using G = GradShape<DP>;
-    cudaError_t e = cudaFuncSetAttribute(attn_dq_kernel<T, DP>, cudaFuncAttributeMaxDynamicSharedMemorySize, G::kBytes);
-    if (e == cudaSuccess)
-        e = cudaFuncSetAttribute(attn_dkv_kernel<T, DP>, cudaFuncAttributeMaxDynamicSharedMemorySize, G::kBytes);
+    static std::atomic<uint64_t> asked_q{0}, asked_kv{0};
+    cudaError_t e = allow_shared(attn_dq_kernel<T, DP>, G::kBytes, device, asked_q);
+    if (e == cudaSuccess) e = allow_shared(attn_dkv_kernel<T, DP>, G::kBytes, device, asked_kv);
     if (e != cudaSuccess) return e;
     const int64_t heads = p.a.batch * p.a.kv_heads;
     const int64_t blocks = heads * (p.lead * p.lead_parts + (int64_t)(p.kv_tiles - p.lead) * p.rest_parts);
@@ -1044,11 +1045,11 @@ cudaError_t backward(const Params& p, const CUtensorMap& q, const CUtensorMap& k
 }
 
 template <class T>
-cudaError_t forward_of(const Params& p, const CUtensorMap& q, const CUtensorMap& k, const CUtensorMap& v,
+cudaError_t forward_of(int device, const Params& p, const CUtensorMap& q, const CUtensorMap& k, const CUtensorMap& v,
                        cudaStream_t st) {
     const bool two = tiles_per_block(p.a) == 2;
-    if (p.a.head_dim <= 64) return two ? forward<T, 64, 2>(p, q, k, v, st) : forward<T, 64, 1>(p, q, k, v, st);
-    return two ? forward<T, 128, 2>(p, q, k, v, st) : forward<T, 128, 1>(p, q, k, v, st);
+    if (p.a.head_dim <= 64) return two ? forward<T, 64, 2>(device, p, q, k, v, st) : forward<T, 64, 1>(device, p, q, k, v, st);
+    return two ? forward<T, 128, 2>(device, p, q, k, v, st) : forward<T, 128, 1>(device, p, q, k, v, st);
 }
 
 cudaError_t input_maps(const Params& p, CUtensorMap* q, CUtensorMap* k, CUtensorMap* v) {
@@ -1089,7 +1090,7 @@ cudaError_t launch_attn_tc(const OpContext& x, const heddle_attention_args& a, u
     CUtensorMap q, k, v;
     const cudaError_t e = input_maps(p, &q, &k, &v);
     if (e != cudaSuccess) return e;
-    return a.dtype == HEDDLE_BF16 ? forward_of<__nv_bfloat16>(p, q, k, v, st) : forward_of<__half>(p, q, k, v, st);
+    return a.dtype == HEDDLE_BF16 ? forward_of<__nv_bfloat16>(x.device, p, q, k, v, st) : forward_of<__half>(x.device, p, q, k, v, st);
 }
 
 size_t attn_tc_grad_scratch(const OpContext& x, const heddle_attention_args& a) {
@@ -1110,8 +1111,8 @@ cudaError_t launch_attn_tc_grad(const OpContext& x, const heddle_attention_grad_
     if (e != cudaSuccess) return e;
     const bool narrow = a.head_dim <= 64;
     if (a.dtype == HEDDLE_BF16)
-        return narrow ? backward<__nv_bfloat16, 64>(p, q, k, v, d_o, st) : backward<__nv_bfloat16, 128>(p, q, k, v, d_o, st);
-    return narrow ? backward<__half, 64>(p, q, k, v, d_o, st) : backward<__half, 128>(p, q, k, v, d_o, st);
+        return narrow ? backward<__nv_bfloat16, 64>(x.device, p, q, k, v, d_o, st) : backward<__nv_bfloat16, 128>(x.device, p, q, k, v, d_o, st);
+    return narrow ? backward<__half, 64>(x.device, p, q, k, v, d_o, st) : backward<__half, 128>(x.device, p, q, k, v, d_o, st);
 }
 
 }  // namespace hd

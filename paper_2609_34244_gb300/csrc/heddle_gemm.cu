@@ -415,7 +415,8 @@ cudaError_t run(const OpContext& x, const CUtensorMap (&a)[2], const CUtensorMap
     p.n_tiles = (int)ceil_div(p.g.N, kOut);
     p.tiles = (int64_t)p.m_tiles * p.n_tiles * (KIND == kGemmPair ? p.g.count : 1);
     auto* k = gemm_kernel<BN, KIND>;
-    cudaError_t e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kBytes);
+    static std::atomic<uint64_t> asked{0};
+    const cudaError_t e = allow_shared(k, S::kBytes, x.device, asked);
     if (e != cudaSuccess) return e;
     const unsigned grid = (unsigned)(p.tiles < x.num_sms ? p.tiles : x.num_sms);
     k<<<grid, kThreads, S::kBytes, st>>>(a[0], a[1], b[0], b[1], p);

@@ -4,6 +4,8 @@
 
 #include <cuda.h>
 
+#include <atomic>
+
 #include "heddle_ops.cuh"
 
 namespace hd {
@@ -191,6 +193,17 @@ __device__ __forceinline__ uint32_t instr_desc(bool bf16, bool a_across, bool b_
 }
 
 }  // namespace tc
+
+// Lets a kernel take `bytes` of dynamic shared memory; asked for once a
+// device, since every call would pay for it on the host.
+template <class K>
+cudaError_t allow_shared(K* kernel, int bytes, int device, std::atomic<uint64_t>& asked) {
+    const uint64_t bit = 1ull << (device & 63);
+    if (device < 64 && (asked.load(std::memory_order_relaxed) & bit)) return cudaSuccess;
+    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    if (e == cudaSuccess) asked.fetch_or(bit, std::memory_order_relaxed);
+    return e;
+}
 
 // A tensor map of 16-bit values: `rank` axes, the first contiguous, byte
 // strides of the others, 128-byte swizzle, zeros outside.

@@ -481,17 +481,48 @@ def heddle_get_search(ctx) -> int:
 # caller.  Shapes and types are checked here, since the C structs carry only
 # one set of sizes; everything else is checked by the library.
 
+_torch = None
 _OP_TYPES = {}
+_raw_stream = None
 
 
-def _op_dtype(t) -> int:
-    if not _OP_TYPES:
-        import torch
-        _OP_TYPES.update({torch.bfloat16: BF16, torch.float16: FP16, torch.float32: FP32})
+def _op_setup():
+    """What the operators need of torch, looked up once: a call of a few
+    microseconds on the GPU notices every one on the host."""
+    global _torch, _raw_stream
+    import torch
+    _OP_TYPES.update({torch.bfloat16: BF16, torch.float16: FP16, torch.float32: FP32})
+    _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or \
+        (lambda device: torch.cuda.current_stream(device).cuda_stream)
+    _torch = torch
+
+
+def _first(what, t, axes):
+    """(shape, element type, its code, device index) of a call's first tensor."""
+    if _torch is None:
+        _op_setup()
     code = _OP_TYPES.get(t.dtype)
     if code is None:
-        raise HeddleError(E_ARG, "unsupported element type %s" % t.dtype)
-    return code
+        raise HeddleError(E_ARG, "unsupported element type %s of %s" % (t.dtype, what))
+    shape = t.shape
+    device = t.get_device()
+    if len(shape) != axes or device < 0:
+        raise HeddleError(E_ARG, "%s: expected a CUDA tensor of %d axes, got %s on %s"
+                          % (what, axes, tuple(shape), t.device))
+    return shape, t.dtype, code, device
+
+
+def _axes(what, t, axes):
+    shape = t.shape
+    if len(shape) != axes:
+        raise HeddleError(E_ARG, "%s: expected %d axes, got %s" % (what, axes, tuple(shape)))
+    return shape
+
+
+def _op_call(ctx, fn, args, device, stream):
+    st = fn(ctx, C.byref(args), _raw_stream(device) if stream is None else getattr(stream, "cuda_stream", stream))
+    if st:
+        _check(ctx, st)
 
 
 def _bad(what, t, shape, dtype):
@@ -499,22 +530,24 @@ def _bad(what, t, shape, dtype):
                       % (what, tuple(shape), dtype, tuple(t.shape), t.dtype, t.device))
 
 
-def _mat(what, t, rows, cols, dtype, device):
+def _mat(what, t, shape, dtype, device):
     """(address, row stride) of a [rows][cols] tensor; (None, 0) for None."""
     if t is None:
         return None, 0
-    if t.dtype != dtype or t.device != device or tuple(t.shape) != (rows, cols):
-        _bad(what, t, (rows, cols), dtype)
+    if t.dtype is not dtype or t.shape != shape or t.get_device() != device:
+        _bad(what, t, shape, dtype)
     ld, inner = t.stride()
-    if inner != 1 and cols > 1:
-        _bad(what, t, (rows, cols), dtype)
-    return t.data_ptr(), ld if rows > 1 else max(ld, cols)
+    if inner != 1 and shape[1] > 1:
+        _bad(what, t, shape, dtype)
+    if ld < shape[1] and shape[0] <= 1:
+        ld = shape[1]
+    return t.data_ptr(), ld
 
 
 def _vec(what, t, n, dtype, device):
     if t is None:
         return None
-    if t.dtype != dtype or t.device != device or tuple(t.shape) != (n,) or (n > 1 and t.stride(0) != 1):
+    if t.dtype is not dtype or t.shape != (n,) or t.get_device() != device or (n > 1 and t.stride(0) != 1):
         _bad(what, t, (n,), dtype)
     return t.data_ptr()
 
@@ -522,45 +555,12 @@ def _vec(what, t, n, dtype, device):
 def _heads(what, t, shape, dtype, device):
     """heddle_heads of a [batch][tokens][heads][head_dim] tensor, or one
     without the batch axis."""
-    if t.dtype != dtype or t.device != device or t.shape != shape:
+    if t.dtype is not dtype or t.shape != shape or t.get_device() != device:
         _bad(what, t, shape, dtype)
     st = t.stride()
     if st[-1] != 1 and shape[-1] > 1:
         _bad(what, t, shape, dtype)
     return heddle_heads(t.data_ptr(), st[0] if len(st) == 4 else 0, st[-3], st[-2])
-
-
-def _two_axes(what, t):
-    if t.dim() != 2 or not t.is_cuda:
-        raise HeddleError(E_ARG, "%s: expected a CUDA tensor of two axes, got %s on %s"
-                          % (what, tuple(t.shape), t.device))
-    return t.shape
-
-
-def heddle_linear(ctx, x, w, y, bias=None, residual=None, act=ACT_NONE, pre=None, stream=None):
-    """y = act(x w^T + bias) + residual; ``pre`` receives the sum before act."""
-    (m, k), (n, _) = _two_axes("x", x), _two_axes("w", w)
-    dt, dev = x.dtype, x.device
-    a = heddle_linear_args(m, n, k, _op_dtype(x), act, *_mat("x", x, m, k, dt, dev), *_mat("w", w, n, k, dt, dev),
-                           _vec("bias", bias, n, dt, dev), *_mat("residual", residual, m, n, dt, dev),
-                           *_mat("y", y, m, n, dt, dev), *_mat("pre", pre, m, n, _f32(), dev))
-    _check(ctx, load_library().heddle_linear(ctx, C.byref(a), _stream(stream)))
-
-
-def _f32():
-    import torch
-    return torch.float32
-
-
-def heddle_linear_backward(ctx, dy, x, w, act=ACT_NONE, pre=None, dx=None, dw=None, dbias=None, stream=None):
-    """Gradients of heddle_linear; an output that is None is not computed."""
-    (m, k), (n, _) = _two_axes("x", x), _two_axes("w", w)
-    dt, dev = x.dtype, x.device
-    a = heddle_linear_grad_args(m, n, k, _op_dtype(x), act, *_mat("dy", dy, m, n, dt, dev),
-                                *_mat("x", x, m, k, dt, dev), *_mat("w", w, n, k, dt, dev),
-                                *_mat("pre", pre, m, n, _f32(), dev), *_mat("dx", dx, m, k, dt, dev),
-                                *_mat("dw", dw, n, k, dt, dev), _vec("dbias", dbias, n, dt, dev))
-    _check(ctx, load_library().heddle_linear_backward(ctx, C.byref(a), _stream(stream)))
 
 
 def _same_stride(what, a, b):
@@ -569,110 +569,127 @@ def _same_stride(what, a, b):
     return a[0], b[0], a[1]
 
 
+def heddle_linear(ctx, x, w, y, bias=None, residual=None, act=ACT_NONE, pre=None, stream=None):
+    """y = act(x w^T + bias) + residual; ``pre`` receives the sum before act."""
+    (m, k), dt, code, dev = _first("x", x, 2)
+    n = _axes("w", w, 2)[0]
+    mn = (m, n)
+    a = heddle_linear_args(m, n, k, code, act, *_mat("x", x, (m, k), dt, dev), *_mat("w", w, (n, k), dt, dev),
+                           _vec("bias", bias, n, dt, dev), *_mat("residual", residual, mn, dt, dev),
+                           *_mat("y", y, mn, dt, dev), *_mat("pre", pre, mn, _torch.float32, dev))
+    _op_call(ctx, load_library().heddle_linear, a, dev, stream)
+
+
+def heddle_linear_backward(ctx, dy, x, w, act=ACT_NONE, pre=None, dx=None, dw=None, dbias=None, stream=None):
+    """Gradients of heddle_linear; an output that is None is not computed."""
+    (m, k), dt, code, dev = _first("x", x, 2)
+    n = _axes("w", w, 2)[0]
+    mn, mk, nk = (m, n), (m, k), (n, k)
+    a = heddle_linear_grad_args(m, n, k, code, act, *_mat("dy", dy, mn, dt, dev), *_mat("x", x, mk, dt, dev),
+                                *_mat("w", w, nk, dt, dev), *_mat("pre", pre, mn, _torch.float32, dev),
+                                *_mat("dx", dx, mk, dt, dev), *_mat("dw", dw, nk, dt, dev),
+                                _vec("dbias", dbias, n, dt, dev))
+    _op_call(ctx, load_library().heddle_linear_backward, a, dev, stream)
+
+
 def heddle_gated_ffn(ctx, x, w_gate, w_up, y, act=ACT_SILU, gate=None, up=None, stream=None):
     """y = act(x w_gate^T) * (x w_up^T); ``gate`` and ``up`` receive the products."""
-    (m, k), (n, _) = _two_axes("x", x), _two_axes("w_gate", w_gate)
-    dt, dev = x.dtype, x.device
-    saved = _same_stride("gate and up", _mat("gate", gate, m, n, _f32(), dev), _mat("up", up, m, n, _f32(), dev))
-    a = heddle_gated_ffn_args(m, n, k, _op_dtype(x), act, *_mat("x", x, m, k, dt, dev),
-                              *_mat("w_gate", w_gate, n, k, dt, dev), *_mat("w_up", w_up, n, k, dt, dev),
-                              *_mat("y", y, m, n, dt, dev), *saved)
-    _check(ctx, load_library().heddle_gated_ffn(ctx, C.byref(a), _stream(stream)))
+    (m, k), dt, code, dev = _first("x", x, 2)
+    n = _axes("w_gate", w_gate, 2)[0]
+    mn, nk, f32 = (m, n), (n, k), _torch.float32
+    saved = _same_stride("gate and up", _mat("gate", gate, mn, f32, dev), _mat("up", up, mn, f32, dev))
+    a = heddle_gated_ffn_args(m, n, k, code, act, *_mat("x", x, (m, k), dt, dev),
+                              *_mat("w_gate", w_gate, nk, dt, dev), *_mat("w_up", w_up, nk, dt, dev),
+                              *_mat("y", y, mn, dt, dev), *saved)
+    _op_call(ctx, load_library().heddle_gated_ffn, a, dev, stream)
 
 
 def heddle_gated_ffn_backward(ctx, dy, x, w_gate, w_up, gate, up, act=ACT_SILU, dx=None, dwg=None, dwu=None,
                               stream=None):
-    """Gradients of heddle_gated_ffn (dwg and dwu, those of w_gate and
-    w_up, together); an output
-    that is None is not computed."""
-    (m, k), (n, _) = _two_axes("x", x), _two_axes("w_gate", w_gate)
-    dt, dev = x.dtype, x.device
-    saved = _same_stride("gate and up", _mat("gate", gate, m, n, _f32(), dev), _mat("up", up, m, n, _f32(), dev))
-    dw = _same_stride("dwg and dwu", _mat("dwg", dwg, n, k, dt, dev),
-                      _mat("dwu", dwu, n, k, dt, dev))
-    a = heddle_gated_ffn_grad_args(m, n, k, _op_dtype(x), act, *_mat("dy", dy, m, n, dt, dev),
-                                   *_mat("x", x, m, k, dt, dev), *_mat("w_gate", w_gate, n, k, dt, dev),
-                                   *_mat("w_up", w_up, n, k, dt, dev), *saved, *_mat("dx", dx, m, k, dt, dev), *dw)
-    _check(ctx, load_library().heddle_gated_ffn_backward(ctx, C.byref(a), _stream(stream)))
+    """Gradients of heddle_gated_ffn; dx, or dwg and dwu (those of w_gate and
+    w_up) together, are not computed where they are None."""
+    (m, k), dt, code, dev = _first("x", x, 2)
+    n = _axes("w_gate", w_gate, 2)[0]
+    mn, mk, nk, f32 = (m, n), (m, k), (n, k), _torch.float32
+    saved = _same_stride("gate and up", _mat("gate", gate, mn, f32, dev), _mat("up", up, mn, f32, dev))
+    dw = _same_stride("dwg and dwu", _mat("dwg", dwg, nk, dt, dev), _mat("dwu", dwu, nk, dt, dev))
+    a = heddle_gated_ffn_grad_args(m, n, k, code, act, *_mat("dy", dy, mn, dt, dev), *_mat("x", x, mk, dt, dev),
+                                   *_mat("w_gate", w_gate, nk, dt, dev), *_mat("w_up", w_up, nk, dt, dev), *saved,
+                                   *_mat("dx", dx, mk, dt, dev), *dw)
+    _op_call(ctx, load_library().heddle_gated_ffn_backward, a, dev, stream)
 
 
 def _norm_rope_args(q, k, wq, wk, q_out, k_out, positions, cos, sin, eps, interleaved):
-    if q.dim() != 3 or k.dim() != 3 or not q.is_cuda:
-        raise HeddleError(E_ARG, "q and k: expected CUDA tensors [tokens][heads][head_dim]")
-    dt, dev = q.dtype, q.device
-    t, hq, d = q.shape
-    hk = k.shape[1]
+    shape, dt, code, dev = _first("q", q, 3)
+    t, hq, d = shape
+    keys = (t, _axes("k", k, 3)[1], d)
     rot = table = 0
     ptrs = (None, None, None)
     if positions is not None:
-        import torch
-        table, half = _two_axes("cos", cos)
+        table, half = angles = _axes("cos", cos, 2)
         rot = 2 * half
+        ptrs = (_vec("positions", positions, t, _torch.int32, dev), _mat("cos", cos, angles, _torch.float32, dev)[0],
+                _mat("sin", sin, angles, _torch.float32, dev)[0])
         if not (cos.is_contiguous() and sin.is_contiguous()):
             raise HeddleError(E_ARG, "cos and sin are contiguous")
-        ptrs = (_vec("positions", positions, t, torch.int32, dev), _mat("cos", cos, table, half, _f32(), dev)[0],
-                _mat("sin", sin, table, half, _f32(), dev)[0])
-    return heddle_qk_norm_rope_args(t, table, hq, hk, d, rot, _op_dtype(q), int(bool(interleaved)), eps, 0,
-                                    _heads("q", q, q.shape, dt, dev), _heads("k", k, (t, hk, d), dt, dev),
-                                    _vec("wq", wq, d, dt, dev), _vec("wk", wk, d, dt, dev), *ptrs,
-                                    _heads("q_out", q_out, q.shape, dt, dev), _heads("k_out", k_out, k.shape, dt, dev))
+    a = heddle_qk_norm_rope_args(t, table, hq, keys[1], d, rot, code, 1 if interleaved else 0, eps, 0,
+                                 _heads("q", q, shape, dt, dev), _heads("k", k, keys, dt, dev),
+                                 _vec("wq", wq, d, dt, dev), _vec("wk", wk, d, dt, dev), *ptrs,
+                                 _heads("q_out", q_out, shape, dt, dev), _heads("k_out", k_out, keys, dt, dev))
+    return a, shape, keys, dt, dev
 
 
 def heddle_qk_norm_rope(ctx, q, k, wq, wk, q_out, k_out, positions=None, cos=None, sin=None, eps=1e-6,
                         interleaved=False, stream=None):
     """Norms and rotation of q and k ([tokens][heads][head_dim]); cos and sin
     are float32 [table_len][rot_dim / 2], no rotation without positions."""
-    a = _norm_rope_args(q, k, wq, wk, q_out, k_out, positions, cos, sin, eps, interleaved)
-    _check(ctx, load_library().heddle_qk_norm_rope(ctx, C.byref(a), _stream(stream)))
+    a, _, _, _, dev = _norm_rope_args(q, k, wq, wk, q_out, k_out, positions, cos, sin, eps, interleaved)
+    _op_call(ctx, load_library().heddle_qk_norm_rope, a, dev, stream)
 
 
 def heddle_qk_norm_rope_backward(ctx, dq_out, dk_out, q, k, wq, wk, dq, dk, dwq, dwk, positions=None, cos=None,
                                  sin=None, eps=1e-6, interleaved=False, stream=None):
     """Gradients of heddle_qk_norm_rope from those of its outputs; dwq and dwk
     are float32 [head_dim]."""
-    f = _norm_rope_args(q, k, wq, wk, dq_out, dk_out, positions, cos, sin, eps, interleaved)
-    dt, dev, d = q.dtype, q.device, q.shape[2]
-    a = heddle_qk_norm_rope_grad_args(f, _heads("dq", dq, q.shape, dt, dev), _heads("dk", dk, k.shape, dt, dev),
-                                      _vec("dwq", dwq, d, _f32(), dev), _vec("dwk", dwk, d, _f32(), dev))
-    _check(ctx, load_library().heddle_qk_norm_rope_backward(ctx, C.byref(a), _stream(stream)))
+    f, shape, keys, dt, dev = _norm_rope_args(q, k, wq, wk, dq_out, dk_out, positions, cos, sin, eps, interleaved)
+    d, f32 = shape[2], _torch.float32
+    a = heddle_qk_norm_rope_grad_args(f, _heads("dq", dq, shape, dt, dev), _heads("dk", dk, keys, dt, dev),
+                                      _vec("dwq", dwq, d, f32, dev), _vec("dwk", dwk, d, f32, dev))
+    _op_call(ctx, load_library().heddle_qk_norm_rope_backward, a, dev, stream)
 
 
 def _attention_args(q, k, v, o, lse, q_lens, kv_lens, window, sinks, scale):
-    if q.dim() != 4 or k.dim() != 4 or not q.is_cuda:
-        raise HeddleError(E_ARG, "q and k: expected CUDA tensors [batch][tokens][heads][head_dim]")
-    dt, dev = q.dtype, q.device
-    b, tq, hq, d = q.shape
-    tk, hk = k.shape[1:3]
+    shape, dt, code, dev = _first("q", q, 4)
+    b, tq, hq, d = shape
+    _, tk, hk, _ = _axes("k", k, 4)
     keys = (b, tk, hk, d)
-    if lse is not None and (lse.dtype != _f32() or lse.device != dev or lse.shape != (b, hq, tq)
+    if lse is not None and (lse.dtype is not _torch.float32 or lse.shape != (b, hq, tq) or lse.get_device() != dev
                             or not lse.is_contiguous()):
         _bad("lse", lse, (b, hq, tq), "float32")
-    lens = (None, None)
-    if q_lens is not None or kv_lens is not None:
-        import torch
-        lens = (_vec("q_lens", q_lens, b, torch.int32, dev), _vec("kv_lens", kv_lens, b, torch.int32, dev))
-    return heddle_attention_args(b, tq, tk, hq, hk, d, _op_dtype(q), window, sinks,
-                                 d ** -0.5 if scale is None else scale, 0,
-                                 _heads("q", q, q.shape, dt, dev), _heads("k", k, keys, dt, dev),
-                                 _heads("v", v, keys, dt, dev), _heads("o", o, q.shape, dt, dev), _ptr(lse), *lens)
+    i32 = _torch.int32
+    a = heddle_attention_args(b, tq, tk, hq, hk, d, code, window, sinks, d ** -0.5 if scale is None else scale, 0,
+                              _heads("q", q, shape, dt, dev), _heads("k", k, keys, dt, dev),
+                              _heads("v", v, keys, dt, dev), _heads("o", o, shape, dt, dev),
+                              None if lse is None else lse.data_ptr(), _vec("q_lens", q_lens, b, i32, dev),
+                              _vec("kv_lens", kv_lens, b, i32, dev))
+    return a, shape, keys, dt, dev
 
 
 def heddle_attention(ctx, q, k, v, o, lse=None, q_lens=None, kv_lens=None, window=0, sinks=0, scale=None,
                      stream=None):
     """Causal attention of q over k and v ([batch][tokens][heads][head_dim])
     with a sliding window (0: none) and sinks; scale None: head_dim ** -0.5."""
-    a = _attention_args(q, k, v, o, lse, q_lens, kv_lens, window, sinks, scale)
-    _check(ctx, load_library().heddle_attention(ctx, C.byref(a), _stream(stream)))
+    a, _, _, _, dev = _attention_args(q, k, v, o, lse, q_lens, kv_lens, window, sinks, scale)
+    _op_call(ctx, load_library().heddle_attention, a, dev, stream)
 
 
 def heddle_attention_backward(ctx, do, q, k, v, o, lse, dq, dk, dv, q_lens=None, kv_lens=None, window=0, sinks=0,
                               scale=None, stream=None):
     """Gradients of heddle_attention from ``do``, with its o and lse."""
-    f = _attention_args(q, k, v, o, lse, q_lens, kv_lens, window, sinks, scale)
-    dt, dev = q.dtype, q.device
-    a = heddle_attention_grad_args(f, _heads("do", do, q.shape, dt, dev), _heads("dq", dq, q.shape, dt, dev),
-                                   _heads("dk", dk, k.shape, dt, dev), _heads("dv", dv, k.shape, dt, dev))
-    _check(ctx, load_library().heddle_attention_backward(ctx, C.byref(a), _stream(stream)))
+    f, shape, keys, dt, dev = _attention_args(q, k, v, o, lse, q_lens, kv_lens, window, sinks, scale)
+    a = heddle_attention_grad_args(f, _heads("do", do, shape, dt, dev), _heads("dq", dq, shape, dt, dev),
+                                   _heads("dk", dk, keys, dt, dev), _heads("dv", dv, keys, dt, dev))
+    _op_call(ctx, load_library().heddle_attention_backward, a, dev, stream)
 
 
 # ------------------------------------------------------------- marshalling helpers
