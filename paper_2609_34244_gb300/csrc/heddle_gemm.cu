@@ -1,11 +1,15 @@
 // heddle_gemm.cu -- the products of the layer operators with their epilogues
 // on the tensor cores.
 //
-// A persistent CTA per SM computes 128 x BN tiles of C.  One thread streams
-// operand tiles of 64 steps into a ring of shared-memory stages by bulk
-// tensor copies, one issues the products (128 x BN x 16, sums in tensor
-// memory), four warps read finished sums back and run the epilogue while the
-// next tile's products fill the other half of tensor memory.
+// A persistent CTA per SM computes 128 x BN tiles of C, or a pair of CTAs
+// 256 x 256 tiles, each with half of the rows of A and of B in its shared
+// memory: a third less to fetch from L2 than two CTAs alone.  One thread
+// streams operand tiles of 64 steps into a ring of shared-memory stages by
+// bulk tensor copies, one issues the products (sums in tensor memory), four
+// warps read finished sums back and run the epilogue while the next tile's
+// products fill the other half of tensor memory.  With few rows the stages
+// hold as many rows of A as there are, so that the ring holds more of B,
+// whose stream from memory is then the time.
 
 #include <mutex>
 
@@ -50,20 +54,25 @@ struct KernelArgs {
     int32_t steps;       // 64-wide contraction steps per term
     int32_t terms;
     int32_t a_rows;      // rows of A a copy takes (all 128, or fewer where M is)
+    int32_t stages, stage;  // of the ring, and its bytes each
     int32_t m_tiles, n_tiles;
     int64_t tiles;
     int32_t vec;         // outputs, residual, bias and saved sums by 16- and 8-byte accesses
     uint32_t* err;
 };
 
-template <int BN, int KIND>
+constexpr int kMaxStages = 32;
+constexpr int kEpi = 4 * 32 * kPitch * 4;
+constexpr int kBarBytes = 16 * kMaxStages + 64;
+constexpr int kShared = 227 * 1024;  // all that a CTA may take
+constexpr int kRing = kShared - 1024 - kEpi - kBarBytes;
+
+template <int BN, bool PAIR>
 struct Shape {
-    static constexpr int kStageA = BM * BK * 2, kStageB = BN * BK * 2;
-    static constexpr int kStage = kStageA + kStageB;
-    static constexpr int kEpi = 4 * 32 * kPitch * 4;
-    static constexpr int kStages = (227 * 1024 - 1024 - 512 - kEpi) / kStage < 8 ? (227 * 1024 - 1024 - 512 - kEpi) / kStage : 8;
-    static constexpr int kBytes = 1024 + kStages * kStage + kEpi + 512;
-    static constexpr int kCols = BN == 256 ? 512 : 2 * BN;  // both halves of tensor memory in use
+    static constexpr int kTileM = PAIR ? 2 * BM : BM;
+    static constexpr int kRowsB = PAIR ? BN / 2 : BN;  // rows of B in this CTA
+    static constexpr int kStageA = BM * BK * 2, kStageB = kRowsB * BK * 2;
+    static constexpr int kCols = 2 * BN;  // both halves of tensor memory in use
 };
 
 // Tiles in order of groups of 16 tile rows, column by column within one: the
@@ -105,36 +114,25 @@ __device__ __forceinline__ void store_four(T* p, const float (&v)[4]) {
     }
 }
 
-// V sums of one row of C from column n on to what heddle_linear stores.
-template <class T, int V>
-__device__ __forceinline__ void finish_linear(const GemmArgs& g, int64_t m, int64_t n, float (&c)[V]) {
+// Four sums of one row of C from column n on to what heddle_linear stores.
+template <class T>
+__device__ __forceinline__ void finish_linear(const GemmArgs& g, int64_t m, int64_t n, float (&c)[4]) {
     if (g.bias) {
-        float b[V];
-        if constexpr (V == 4)
-            load_four<T>(g.bias, n, b);
-        else
-            b[0] = load_one<T>(g.bias, n);
+        float b[4];
+        load_four<T>(g.bias, n, b);
 #pragma unroll
-        for (int j = 0; j < V; ++j) c[j] += b[j];
+        for (int j = 0; j < 4; ++j) c[j] += b[j];
     }
-    if (g.pre[0]) {
-        if constexpr (V == 4)
-            store_four(g.pre[0] + m * g.ldp + n, c);
-        else
-            g.pre[0][m * g.ldp + n] = c[0];
-    }
+    if (g.pre[0]) store_four(g.pre[0] + m * g.ldp + n, c);
     if (g.act != HEDDLE_ACT_NONE) {
 #pragma unroll
-        for (int j = 0; j < V; ++j) c[j] = act_value(c[j], g.act);
+        for (int j = 0; j < 4; ++j) c[j] = act_value(c[j], g.act);
     }
     if (g.residual) {
-        float r[V];
-        if constexpr (V == 4)
-            load_four<T>(g.residual, m * g.ldr + n, r);
-        else
-            r[0] = load_one<T>(g.residual, m * g.ldr + n);
+        float r[4];
+        load_four<T>(g.residual, m * g.ldr + n, r);
 #pragma unroll
-        for (int j = 0; j < V; ++j) c[j] += r[j];
+        for (int j = 0; j < 4; ++j) c[j] += r[j];
     }
 }
 
@@ -155,15 +153,32 @@ __device__ __forceinline__ void store_block(const KernelArgs& p, TO* out, int64_
             if (m0 + row >= g.M) continue;
             const float4 f = *reinterpret_cast<const float4*>(t + row * kPitch + col);
             float c[4] = {f.x, f.y, f.z, f.w};
-            if (LINEAR) finish_linear<T, 4>(g, m0 + row, n0 + col, c);
+            if (LINEAR) finish_linear<T>(g, m0 + row, n0 + col, c);
             store_four(out + (m0 + row) * ld + n0 + col, c);
         }
     } else if (n0 + lane < g.N) {
         const int rows = (int)min((int64_t)32, g.M - m0);
-        for (int row = 0; row < rows; ++row) {
-            float c[1] = {t[row * kPitch + lane]};
-            if (LINEAR) finish_linear<T, 1>(g, m0 + row, n0 + lane, c);
-            out[(m0 + row) * ld + n0 + lane] = from_float<TO>(c[0]);
+        const int64_t n = n0 + lane;
+        const float bias = LINEAR && g.bias ? load_one<T>(g.bias, n) : 0.0f;
+        for (int r0 = 0; r0 < rows; r0 += 8) {  // eight rows' loads before their stores
+            float c[8], res[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                c[i] = t[(r0 + i) * kPitch + lane] + bias;
+                res[i] = LINEAR && g.residual && r0 + i < rows ? load_one<T>(g.residual, (m0 + r0 + i) * g.ldr + n)
+                                                               : 0.0f;
+            }
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                if (r0 + i >= rows) break;
+                const int64_t m = m0 + r0 + i;
+                if (LINEAR) {
+                    if (g.pre[0]) g.pre[0][m * g.ldp + n] = c[i];
+                    c[i] = act_value(c[i], g.act);
+                    if (g.residual) c[i] += res[i];
+                }
+                out[m * ld + n] = from_float<TO>(c[i]);
+            }
         }
     }
     __syncwarp();
@@ -175,40 +190,50 @@ __device__ __forceinline__ void put_row(float* t, const uint32_t (&v)[32], int l
         *reinterpret_cast<uint4*>(t + lane * kPitch + j) = make_uint4(v[j], v[j + 1], v[j + 2], v[j + 3]);
 }
 
-template <int BN, int KIND>
+template <int BN, int KIND, bool PAIR>
 __global__ void __launch_bounds__(kThreads, 1)
     gemm_kernel(const __grid_constant__ CUtensorMap a0, const __grid_constant__ CUtensorMap a1,
                 const __grid_constant__ CUtensorMap b0, const __grid_constant__ CUtensorMap b1,
                 const __grid_constant__ KernelArgs p) {
-    using S = Shape<BN, KIND>;
+    using S = Shape<BN, PAIR>;
     constexpr bool kAcrossA = KIND == kGemmPair, kAcrossB = KIND == kGemmPair || KIND == kGemmSum;
     constexpr int kOut = KIND == kGemmGated ? BN / 2 : BN;  // columns of C a tile covers
     extern __shared__ unsigned char raw[];
     unsigned char* base = raw + ((1024 - (smem_u32(raw) & 1023)) & 1023);
     unsigned char* stages = base;
-    float* epi = reinterpret_cast<float*>(base + S::kStages * S::kStage);
-    uint64_t* bars = reinterpret_cast<uint64_t*>(base + S::kStages * S::kStage + S::kEpi);
-    const uint32_t full = smem_u32(bars), empty = full + 8 * S::kStages, done = empty + 8 * S::kStages,
+    float* epi = reinterpret_cast<float*>(base + kRing);
+    uint64_t* bars = reinterpret_cast<uint64_t*>(base + kRing + kEpi);
+    const uint32_t full = smem_u32(bars), empty = full + 8 * kMaxStages, done = empty + 8 * kMaxStages,
                    freed = done + 16;
-    volatile uint32_t* gave_up = reinterpret_cast<uint32_t*>(bars + 2 * S::kStages + 4);
+    volatile uint32_t* gave_up = reinterpret_cast<uint32_t*>(bars + 2 * kMaxStages + 4);
     uint32_t* tmem_at = const_cast<uint32_t*>(gave_up) + 1;
 
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+    const uint32_t rank = PAIR ? cluster_rank() : 0;
+    const int64_t first = PAIR ? blockIdx.x / 2 : blockIdx.x, step = PAIR ? gridDim.x / 2 : gridDim.x;
     if (threadIdx.x == 0) {
-        for (int s = 0; s < S::kStages; ++s) {
+        for (int s = 0; s < p.stages; ++s) {
             mbar_init(full + 8 * s, 1);
             mbar_init(empty + 8 * s, 1);
         }
         for (int b = 0; b < 2; ++b) {
             mbar_init(done + 8 * b, 1);
-            mbar_init(freed + 8 * b, 4);
+            mbar_init(freed + 8 * b, PAIR ? 8 : 4);
         }
         *gave_up = 0;
         mbar_fence_init();
     }
-    if (warp == 2) tmem_alloc(smem_u32(tmem_at), S::kCols);
+    if (warp == 2) {
+        if (PAIR)
+            tmem_alloc_pair(smem_u32(tmem_at), S::kCols);
+        else
+            tmem_alloc(smem_u32(tmem_at), S::kCols);
+    }
     fence_before();
-    __syncthreads();
+    if (PAIR)
+        cluster_sync();
+    else
+        __syncthreads();
     fence_after();
     const uint32_t tmem = *tmem_at;
     const int per_tile = p.steps * p.terms;
@@ -219,75 +244,100 @@ __global__ void __launch_bounds__(kThreads, 1)
         int s = 0;
         uint32_t phase = 0;
         bool go = true;
-        const uint32_t bytes = (kAcrossA ? S::kStageA : p.a_rows * BK * 2) + S::kStageB;
-        for (int64_t t = blockIdx.x; go && t < p.tiles; t += gridDim.x) {
+        const int a_bytes = kAcrossA ? S::kStageA : p.a_rows * BK * 2;
+        auto load = [](uint32_t dst, const CUtensorMap* m, uint32_t bar, int x, int y) {
+            if (PAIR)
+                load_2d_pair(dst, m, bar, x, y);
+            else
+                load_2d(dst, m, bar, x, y);
+        };
+        for (int64_t t = first; go && t < p.tiles; t += step) {
             int z, tm, tn;
             tile_at(p, t, z, tm, tn);
+            const int m0 = tm * S::kTileM + (int)rank * BM;
             for (int it = 0; it < per_tile; ++it) {
                 if (!(go = mbar_wait(empty + 8 * s, phase ^ 1, gave_up))) break;
-                const uint32_t bar = full + 8 * s, sa = smem_u32(stages + s * S::kStage), sb = sa + S::kStageA;
+                const uint32_t own = full + 8 * s, bar = PAIR ? cluster_at(own, 0) : own;
+                const uint32_t sa = smem_u32(stages + s * p.stage), sb = sa + a_bytes;
                 const bool second = KIND == kGemmSum ? it >= p.steps : KIND == kGemmPair ? z : false;
                 const CUtensorMap* ma = second ? &a1 : &a0;
                 const CUtensorMap* mb = second ? &b1 : &b0;
                 const int k = (KIND == kGemmSum && second ? it - p.steps : it) * BK;
-                mbar_expect(bar, bytes);
+                if (rank == 0) mbar_expect(own, (PAIR ? 2 : 1) * (a_bytes + S::kStageB));
                 if (kAcrossA) {
 #pragma unroll
-                    for (int j = 0; j < BM / 64; ++j) load_2d(sa + j * 8192, ma, bar, tm * BM + j * 64, k);
+                    for (int j = 0; j < BM / 64; ++j) load(sa + j * 8192, ma, bar, m0 + j * 64, k);
                 } else {
-                    load_2d(sa, ma, bar, k, tm * BM);
+                    load(sa, ma, bar, k, m0);
                 }
                 if (KIND == kGemmGated) {
-                    load_2d(sb, &b0, bar, k, tn * kOut);
-                    load_2d(sb + kOut * BK * 2, &b1, bar, k, tn * kOut);
+                    if (PAIR) {  // the gate's columns come first, the first CTA's half
+                        load(sb, rank ? &b1 : &b0, bar, k, tn * kOut);
+                    } else {
+                        load(sb, &b0, bar, k, tn * kOut);
+                        load(sb + kOut * BK * 2, &b1, bar, k, tn * kOut);
+                    }
                 } else if (kAcrossB) {
+                    const int n0 = tn * BN + (int)rank * S::kRowsB;
 #pragma unroll
-                    for (int j = 0; j < BN / 64; ++j) load_2d(sb + j * 8192, mb, bar, tn * BN + j * 64, k);
+                    for (int j = 0; j < S::kRowsB / 64; ++j) load(sb + j * 8192, mb, bar, n0 + j * 64, k);
                 } else {
-                    load_2d(sb, mb, bar, k, tn * BN);
+                    load(sb, mb, bar, k, tn * BN + (int)rank * S::kRowsB);
                 }
-                if (++s == S::kStages) s = 0, phase ^= 1;
+                if (++s == p.stages) s = 0, phase ^= 1;
             }
         }
-    } else if (warp == 1 && per_tile && elect_one()) {  // issuer
-        const uint32_t idesc = instr_desc(p.g.dtype == HEDDLE_BF16, kAcrossA, kAcrossB, BN);
+    } else if (warp == 1 && rank == 0 && per_tile && elect_one()) {  // issuer
+        const uint32_t idesc = instr_desc(p.g.dtype == HEDDLE_BF16, kAcrossA, kAcrossB, BN, S::kTileM);
+        const int a_bytes = kAcrossA ? S::kStageA : p.a_rows * BK * 2;
         int s = 0, half = 0;
-        uint32_t phase = 0, round[2] = {0, 0};
+        uint32_t phase = 0, round = 0;
         bool go = true;
-        for (int64_t t = blockIdx.x; go && t < p.tiles; t += gridDim.x) {
-            if (!(go = mbar_wait(freed + 8 * half, round[half] ^ 1, gave_up))) break;
-            round[half] ^= 1;
+        for (int64_t t = first; go && t < p.tiles; t += step) {
+            if (!(go = mbar_wait(freed + 8 * half, round ^ 1, gave_up))) break;
             fence_after();
             for (int it = 0; it < per_tile; ++it) {
                 if (!(go = mbar_wait(full + 8 * s, phase, gave_up))) break;
                 fence_after();
-                const uint32_t sa = smem_u32(stages + s * S::kStage), sb = sa + S::kStageA;
+                const uint32_t sa = smem_u32(stages + s * p.stage), sb = sa + a_bytes;
                 const uint64_t da = smem_desc(sa, 8192), db = smem_desc(sb, 8192);
 #pragma unroll
-                for (int k = 0; k < BK / 16; ++k)
-                    mma_ss(tmem + half * BN, da + (kAcrossA ? 128 * k : 2 * k), db + (kAcrossB ? 128 * k : 2 * k),
-                           idesc, it | k);
-                commit(empty + 8 * s);
-                if (++s == S::kStages) s = 0, phase ^= 1;
+                for (int k = 0; k < BK / 16; ++k) {
+                    const uint64_t ka = da + (kAcrossA ? 128 * k : 2 * k), kb = db + (kAcrossB ? 128 * k : 2 * k);
+                    if (PAIR)
+                        mma_ss_pair(tmem + half * BN, ka, kb, idesc, it | k);
+                    else
+                        mma_ss(tmem + half * BN, ka, kb, idesc, it | k);
+                }
+                if (PAIR)
+                    commit_pair(empty + 8 * s);
+                else
+                    commit(empty + 8 * s);
+                if (++s == p.stages) s = 0, phase ^= 1;
             }
-            if (go) commit(done + 8 * half);
+            if (go) {
+                if (PAIR)
+                    commit_pair(done + 8 * half);
+                else
+                    commit(done + 8 * half);
+            }
             half ^= 1;
+            if (!half) round ^= 1;
         }
     } else if (warp >= 4) {  // epilogue
         const int w = warp - 4;
         float* t0 = epi + w * 32 * kPitch;
         int half = 0;
-        uint32_t round[2] = {0, 0};
-        for (int64_t t = blockIdx.x; t < p.tiles; t += gridDim.x) {
+        uint32_t round = 0;
+        for (int64_t t = first; t < p.tiles; t += step) {
             int z, tm, tn;
             tile_at(p, t, z, tm, tn);
             if (per_tile) {
-                if (!__all_sync(~0u, mbar_wait(done + 8 * half, round[half], gave_up))) break;
-                round[half] ^= 1;
+                if (!__all_sync(~0u, mbar_wait(done + 8 * half, round, gave_up))) break;
                 fence_after();
             }
             const uint32_t acc = tmem + half * BN + ((uint32_t)(w * 32) << 16);
-            const int64_t m0 = (int64_t)tm * BM + w * 32;
+            const int64_t m0 = (int64_t)tm * S::kTileM + rank * BM + w * 32;
             const bool rows = m0 < p.g.M;
 #pragma unroll 1
             for (int c = 0; c < kOut; c += 32) {
@@ -329,34 +379,55 @@ __global__ void __launch_bounds__(kThreads, 1)
                     store_block<__half, kLinear>(p, static_cast<__half*>(p.g.out[z]), p.g.ldo, m0, n0, t0);
             }
             fence_before();
-            if (lane == 0) mbar_arrive(freed + 8 * half);
+            if (lane == 0) {
+                if (PAIR)
+                    mbar_arrive_cluster(cluster_at(freed + 8 * half, 0));
+                else
+                    mbar_arrive(freed + 8 * half);
+            }
             half ^= 1;
+            if (!half) round ^= 1;
         }
     }
     __syncthreads();
     if (*gave_up) {
         if (threadIdx.x == 0) atomicOr(p.err, kErrOpWait);
         drain();
-        __syncthreads();
     }
-    if (warp == 2) tmem_free(tmem, S::kCols);
+    if (PAIR)
+        cluster_sync();  // the other CTA's products read this one's memory, and its warps' arrivals land here
+    else
+        __syncthreads();
+    if (warp == 2) {
+        if (PAIR)
+            tmem_free_pair(tmem, S::kCols);
+        else
+            tmem_free(tmem, S::kCols);
+    }
 }
 
 // ---------------------------------------------------------------- operands
 
-// Rows of `cols` 16-bit values to rows at a stride of whole 16-byte units.
-__global__ void __launch_bounds__(256) lay_out_kernel(const uint16_t* src, int64_t ld, int64_t rows, int64_t cols,
-                                                      uint16_t* dst, int64_t dld) {
-    const int64_t per = (cols + 7) / 8, total = rows * per;
+// Rows of `cols` 16-bit values to rows at a stride of whole 16-byte units, of
+// up to four operands in one launch.
+struct LayOut {
+    const uint16_t* src[4];
+    uint16_t* dst[4];
+    int64_t ld[4], dld[4], rows[4], cols[4];
+};
+__global__ void __launch_bounds__(256) lay_out_kernel(const __grid_constant__ LayOut l) {
+    const int o = blockIdx.y;
+    const int64_t per = (l.cols[o] + 7) / 8, total = l.rows[o] * per, cols = l.cols[o];
     for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
         const int64_t r = i / per, c = (i - r * per) * 8;
+        const uint16_t* src = l.src[o] + r * l.ld[o] + c;
         uint16_t v[8];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = c + j < cols ? src[r * ld + c + j] : 0;
+        for (int j = 0; j < 8; ++j) v[j] = c + j < cols ? src[j] : 0;
         uint4 u;
         u.x = v[0] | (uint32_t)v[1] << 16, u.y = v[2] | (uint32_t)v[3] << 16;
         u.z = v[4] | (uint32_t)v[5] << 16, u.w = v[6] | (uint32_t)v[7] << 16;
-        *reinterpret_cast<uint4*>(dst + r * dld + c) = u;
+        *reinterpret_cast<uint4*>(l.dst[o] + r * l.dld[o] + c) = u;
     }
 }
 
@@ -381,19 +452,18 @@ Plan plan_of(const GemmArgs& g) {
 }
 bool same(const GemmOperand& a, const GemmOperand& b) { return a.p == b.p && a.ld == b.ld; }
 
-cudaError_t lay_out(GemmOperand& o, int64_t rows, int64_t cols, unsigned char*& ws, const OpContext& x,
-                    cudaStream_t st) {
-    if (copies_as_is(o, rows)) {
-        if (rows == 1) o.ld = ceil_div(cols, 8) * 8;
-        return cudaSuccess;
-    }
+// Adds the operand to `l` where copies do not take it as it is.
+void lay_out(GemmOperand& o, int64_t rows, int64_t cols, unsigned char*& ws, LayOut& l, int& n) {
     const int64_t ld = ceil_div(cols, 8) * 8;
-    const int64_t units = rows * (ld / 8), most = (int64_t)x.num_sms * 32;
-    lay_out_kernel<<<(unsigned)(ceil_div(units, 256) < most ? ceil_div(units, 256) : most), 256, 0, st>>>(
-        static_cast<const uint16_t*>(o.p), o.ld, rows, cols, reinterpret_cast<uint16_t*>(ws), ld);
+    if (copies_as_is(o, rows)) {
+        if (rows == 1) o.ld = ld;
+        return;
+    }
+    l.src[n] = static_cast<const uint16_t*>(o.p), l.dst[n] = reinterpret_cast<uint16_t*>(ws);
+    l.ld[n] = o.ld, l.dld[n] = ld, l.rows[n] = rows, l.cols[n] = cols;
     o = {ws, ld};
     ws += align256((size_t)rows * ld * 2);
-    return cudaGetLastError();
+    ++n;
 }
 
 cudaError_t map_of(CUtensorMap* m, const GemmOperand& o, int dtype, int64_t rows, int64_t cols, int box_rows) {
@@ -406,29 +476,101 @@ bool unit16(const void* p, int64_t ld, int size, int unit) {
     return !p || ((uintptr_t)p % unit == 0 && ld * size % unit == 0);
 }
 
-template <int BN, int KIND>
+// Pairs of CTAs that run at a time; asked for once a kernel and device.
+template <class K>
+int resident_pairs(K* kernel, const cudaLaunchConfig_t& cfg, int device, std::atomic<int> (&known)[64]) {
+    if (device >= 0 && device < 64 && known[device].load(std::memory_order_relaxed) > 0)
+        return known[device].load(std::memory_order_relaxed);
+    int n = 0;
+    if (cudaOccupancyMaxActiveClusters(&n, kernel, &cfg) != cudaSuccess || n < 1) {
+        cudaGetLastError();
+        n = 1;
+    }
+    if (device >= 0 && device < 64) known[device].store(n, std::memory_order_relaxed);
+    return n;
+}
+
+template <int BN, int KIND, bool PAIR>
 cudaError_t run(const OpContext& x, const CUtensorMap (&a)[2], const CUtensorMap (&b)[2], KernelArgs& p,
                 cudaStream_t st) {
-    using S = Shape<BN, KIND>;
-    static_assert(S::kStages >= 3, "the ring needs room");
+    using S = Shape<BN, PAIR>;
     constexpr int kOut = KIND == kGemmGated ? BN / 2 : BN;
+    p.m_tiles = (int)ceil_div(p.g.M, S::kTileM);
     p.n_tiles = (int)ceil_div(p.g.N, kOut);
     p.tiles = (int64_t)p.m_tiles * p.n_tiles * (KIND == kGemmPair ? p.g.count : 1);
-    auto* k = gemm_kernel<BN, KIND>;
+    p.stage = (KIND == kGemmPair ? S::kStageA : p.a_rows * BK * 2) + S::kStageB;
+    // a product reads 128 rows of A wherever they start, so that many bytes lie after the last stage's
+    const int room = kRing - (S::kStageA + S::kStageB - p.stage);
+    p.stages = room / p.stage < kMaxStages ? room / p.stage : kMaxStages;
+    auto* k = gemm_kernel<BN, KIND, PAIR>;
     static std::atomic<uint64_t> asked{0};
-    const cudaError_t e = allow_shared(k, S::kBytes, x.device, asked);
+    const cudaError_t e = allow_shared(k, kShared, x.device, asked);
     if (e != cudaSuccess) return e;
-    const unsigned grid = (unsigned)(p.tiles < x.num_sms ? p.tiles : x.num_sms);
-    k<<<grid, kThreads, S::kBytes, st>>>(a[0], a[1], b[0], b[1], p);
-    return cudaGetLastError();
+    if constexpr (PAIR) {
+        cudaLaunchConfig_t cfg{};
+        cudaLaunchAttribute attr;
+        attr.id = cudaLaunchAttributeClusterDimension;
+        attr.val.clusterDim = {2, 1, 1};
+        cfg.gridDim = dim3(2 * (x.num_sms / 2));
+        cfg.blockDim = dim3(kThreads);
+        cfg.dynamicSmemBytes = kShared;
+        cfg.stream = st;
+        cfg.attrs = &attr;
+        cfg.numAttrs = 1;
+        static std::atomic<int> known[64];
+        const int pairs = resident_pairs(k, cfg, x.device, known);
+        cfg.gridDim = dim3(2 * (unsigned)(p.tiles < pairs ? p.tiles : pairs));
+        return cudaLaunchKernelEx(&cfg, k, a[0], a[1], b[0], b[1], p);
+    } else {
+        const unsigned grid = (unsigned)(p.tiles < x.num_sms ? p.tiles : x.num_sms);
+        k<<<grid, kThreads, kShared, st>>>(a[0], a[1], b[0], b[1], p);
+        return cudaGetLastError();
+    }
+}
+
+// Tile of a call: columns, and whether pairs of CTAs take 256 rows.
+struct Tile {
+    int bn;
+    bool pair;
+};
+
+// The tile that finishes first by the cycles a 64-wide step of its products
+// takes (measured on steps from L2: what is fetched bounds all but the pair)
+// and the rounds of tiles that the SMs run, plus the epilogue of the last one.
+Tile choose_tile(const OpContext& x, const GemmArgs& g) {
+    const int64_t batch = g.kind == kGemmPair ? g.count : 1;
+    const int64_t steps = ceil_div(g.K, BK) * (g.kind == kGemmSum ? g.count : 1);
+    const struct {
+        Tile t;
+        double cycles, end;
+    } all[] = {{{256, true}, 545, 5000}, {{256, false}, 660, 5000}, {{128, false}, 440, 3500}, {{64, false}, 340, 2800},
+               {{32, false}, 300, 2500}};
+    Tile best{256, false};
+    double least = 1e300;
+    for (const auto& c : all) {
+        if (c.t.bn < 64 && (g.kind != kGemmLinear || g.M > 64)) continue;  // 32 columns of C at least
+        if (c.t.pair && g.M <= BM) continue;
+        const int out = g.kind == kGemmGated ? c.t.bn / 2 : c.t.bn;
+        const int64_t tiles = ceil_div(g.M, c.t.pair ? 2 * BM : BM) * ceil_div(g.N, out) * batch;
+        const int64_t at_once = c.t.pair ? x.num_sms / 2 : x.num_sms;
+        // few rows: B streams from memory, a step as long as its bytes' share
+        double cycles = c.cycles;
+        if (g.M <= 64) cycles = c.t.bn * 2.2;
+        const double time = (double)ceil_div(tiles, at_once) * steps * cycles + c.end;
+        if (time < least) least = time, best = c.t;
+    }
+    return best;
 }
 
 template <int KIND>
-cudaError_t run_kind(const OpContext& x, int bn, const CUtensorMap (&a)[2], const CUtensorMap (&b)[2], KernelArgs& p,
+cudaError_t run_kind(const OpContext& x, Tile t, const CUtensorMap (&a)[2], const CUtensorMap (&b)[2], KernelArgs& p,
                      cudaStream_t st) {
-    if (bn == 256) return run<256, KIND>(x, a, b, p, st);
-    if (bn == 128) return run<128, KIND>(x, a, b, p, st);
-    return run<64, KIND>(x, a, b, p, st);
+    if (t.pair) return run<256, KIND, true>(x, a, b, p, st);
+    if (t.bn == 256) return run<256, KIND, false>(x, a, b, p, st);
+    if (t.bn == 128) return run<128, KIND, false>(x, a, b, p, st);
+    if constexpr (KIND == kGemmLinear)
+        if (t.bn == 32) return run<32, KIND, false>(x, a, b, p, st);
+    return run<64, KIND, false>(x, a, b, p, st);
 }
 
 }  // namespace
@@ -450,42 +592,44 @@ cudaError_t launch_gemm(const OpContext& x, const GemmArgs& args, unsigned char*
     const Plan pl = plan_of(g);
     p.steps = (int32_t)ceil_div(g.K, BK);
     p.terms = g.kind == kGemmSum ? g.count : 1;
-    p.m_tiles = (int32_t)ceil_div(g.M, BM);
     p.err = x.err;
     const int size = 2;
     p.vec = unit16(g.out[0], g.ldo, size, 8) && unit16(g.out[1], g.ldo, size, 8) &&
             unit16(g.residual, g.ldr, size, 8) && unit16(g.bias, 0, size, 8) && unit16(g.pre[0], g.ldp, 4, 16) &&
             unit16(g.pre[1], g.ldp, 4, 16);
 
-    // columns a tile: the widest whose tiles are enough for every SM
-    const int64_t batch = g.kind == kGemmPair ? g.count : 1;
-    int bn = 256;
-    while (bn > 64 && p.m_tiles * batch * ceil_div(g.N, g.kind == kGemmGated ? bn / 2 : bn) < x.num_sms) bn /= 2;
+    const Tile tile = choose_tile(x, g);
     const bool across_a = g.kind == kGemmPair, across_b = across_a || g.kind == kGemmSum;
     p.a_rows = across_a ? 64 : (int)(g.M < BM ? ceil_div(g.M, 8) * 8 : BM);
     CUtensorMap a[2] = {}, b[2] = {};
     if (g.K > 0) {
+        LayOut l{};
+        int n = 0;
+        const bool same_b = pl.b_count == 2 && same(g.b[0], g.b[1]);
+        for (int i = 0; i < pl.a_count; ++i) lay_out(g.a[i], pl.rows[0], pl.cols[0], ws, l, n);
+        for (int i = 0; i < (same_b ? 1 : pl.b_count); ++i) lay_out(g.b[i], pl.rows[1], pl.cols[1], ws, l, n);
+        if (same_b) g.b[1] = g.b[0];
         cudaError_t e = cudaSuccess;
-        for (int i = 0; e == cudaSuccess && i < pl.a_count; ++i) {
-            e = lay_out(g.a[i], pl.rows[0], pl.cols[0], ws, x, st);
-            if (e == cudaSuccess) e = map_of(&a[i], g.a[i], g.dtype, pl.rows[0], pl.cols[0], p.a_rows);
+        if (n) {
+            int64_t units = 0;
+            for (int i = 0; i < n; ++i) units = l.rows[i] * l.dld[i] / 8 > units ? l.rows[i] * l.dld[i] / 8 : units;
+            const int64_t most = (int64_t)x.num_sms * 32;
+            const dim3 grid((unsigned)(ceil_div(units, 256) < most ? ceil_div(units, 256) : most), n);
+            lay_out_kernel<<<grid, 256, 0, st>>>(l);
+            e = cudaGetLastError();
         }
-        const int b_box = across_b ? 64 : g.kind == kGemmGated ? bn / 2 : bn;
-        for (int i = 0; e == cudaSuccess && i < pl.b_count; ++i) {
-            if (i == 1 && same(args.b[0], args.b[1])) {
-                b[1] = b[0];
-                break;
-            }
-            e = lay_out(g.b[i], pl.rows[1], pl.cols[1], ws, x, st);
-            if (e == cudaSuccess) e = map_of(&b[i], g.b[i], g.dtype, pl.rows[1], pl.cols[1], b_box);
-        }
+        const int rows_b = tile.pair ? tile.bn / 2 : g.kind == kGemmGated ? tile.bn / 2 : tile.bn;
+        for (int i = 0; e == cudaSuccess && i < pl.a_count; ++i)
+            e = map_of(&a[i], g.a[i], g.dtype, pl.rows[0], pl.cols[0], p.a_rows);
+        for (int i = 0; e == cudaSuccess && i < pl.b_count; ++i)
+            e = map_of(&b[i], g.b[i], g.dtype, pl.rows[1], pl.cols[1], across_b ? 64 : rows_b);
         if (e != cudaSuccess) return e;
     }
     switch (g.kind) {
-        case kGemmLinear: return run_kind<kGemmLinear>(x, bn, a, b, p, st);
-        case kGemmGated: return run_kind<kGemmGated>(x, bn, a, b, p, st);
-        case kGemmSum: return run_kind<kGemmSum>(x, bn, a, b, p, st);
-        default: return run_kind<kGemmPair>(x, bn, a, b, p, st);
+        case kGemmLinear: return run_kind<kGemmLinear>(x, tile, a, b, p, st);
+        case kGemmGated: return run_kind<kGemmGated>(x, tile, a, b, p, st);
+        case kGemmSum: return run_kind<kGemmSum>(x, tile, a, b, p, st);
+        default: return run_kind<kGemmPair>(x, tile, a, b, p, st);
     }
 }
 

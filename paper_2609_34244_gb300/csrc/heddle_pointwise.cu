@@ -50,19 +50,29 @@ __global__ void __launch_bounds__(256) act_grad_kernel(ActGradArgs a, float* par
     const int64_t first = blockIdx.y * rows_per_chunk;
     const int64_t last = min(a.m, first + rows_per_chunk);
     float sum[V] = {};
+    constexpr int kDepth = V > 1 ? 2 : 4;  // rows in flight a warp
     if (n0 < a.n)
-        for (int64_t m = first + warp; m < last; m += kRowsPerBlock) {
-            float dy[V];
-            load_values<T, V>(static_cast<const T*>(a.dy) + m * a.lddy + n0, dy);
-            if (a.act != HEDDLE_ACT_NONE) {
-                float z[V];
-                load_floats<V>(a.pre + m * a.ldp + n0, z);
+        for (int64_t m = first + warp; m < last; m += kDepth * kRowsPerBlock) {
+            float dy[kDepth][V], z[kDepth][V];
 #pragma unroll
-                for (int i = 0; i < V; ++i) dy[i] *= act_slope(z[i], a.act);
+            for (int k = 0; k < kDepth; ++k) {
+                const int64_t r = m + k * kRowsPerBlock;
+                if (r >= last) break;
+                load_values<T, V>(static_cast<const T*>(a.dy) + r * a.lddy + n0, dy[k]);
+                if (a.act != HEDDLE_ACT_NONE) load_floats<V>(a.pre + r * a.ldp + n0, z[k]);
             }
-            if (a.dz) store_values<T, V>(static_cast<T*>(a.dz) + m * a.lddz + n0, dy);
 #pragma unroll
-            for (int i = 0; i < V; ++i) sum[i] += dy[i];
+            for (int k = 0; k < kDepth; ++k) {
+                const int64_t r = m + k * kRowsPerBlock;
+                if (r >= last) break;
+                if (a.act != HEDDLE_ACT_NONE) {
+#pragma unroll
+                    for (int i = 0; i < V; ++i) dy[k][i] *= act_slope(z[k][i], a.act);
+                }
+                if (a.dz) store_values<T, V>(static_cast<T*>(a.dz) + r * a.lddz + n0, dy[k]);
+#pragma unroll
+                for (int i = 0; i < V; ++i) sum[i] += dy[k][i];
+            }
         }
     if (!partial) return;
     __shared__ float s[kRowsPerBlock][32 * V];
@@ -84,6 +94,7 @@ __global__ void __launch_bounds__(256) column_sum_kernel(const float* partial, i
     const int64_t c = (int64_t)blockIdx.x * 256 + threadIdx.x;
     if (c >= n) return;
     float v = 0.0f;
+#pragma unroll 8
     for (int i = 0; i < chunks; ++i) v += partial[i * n + c];
     out[c] = from_float<T>(v);
 }
