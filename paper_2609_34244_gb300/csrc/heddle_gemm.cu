@@ -46,8 +46,10 @@ namespace {
 using namespace tc;
 
 constexpr int BM = 128, BK = 64;
-constexpr int kThreads = 256;  // producer, issuer, tensor-memory and spare warp, four epilogue warps
-constexpr int kPitch = 36;     // floats per row of an epilogue warp's 32 x 32 transposing tile
+constexpr int kEpiWarps = 8;   // two for every 32 rows of a tile, half of its columns each
+constexpr int kThreads = 128 + 32 * kEpiWarps;  // producer, issuer, tensor-memory and spare warp, epilogue
+constexpr int kCols = 16;      // columns that an epilogue warp takes at a time
+constexpr int kPitch = 20;     // floats per row of its 32 x 16 transposing tile
 
 struct KernelArgs {
     GemmArgs g;
@@ -62,7 +64,7 @@ struct KernelArgs {
 };
 
 constexpr int kMaxStages = 32;
-constexpr int kEpi = 4 * 32 * kPitch * 4;
+constexpr int kEpi = kEpiWarps * 32 * kPitch * 4;
 constexpr int kBarBytes = 16 * kMaxStages + 64;
 constexpr int kShared = 227 * 1024;  // all that a CTA may take
 constexpr int kRing = kShared - 1024 - kEpi - kBarBytes;
@@ -72,7 +74,7 @@ struct Shape {
     static constexpr int kTileM = PAIR ? 2 * BM : BM;
     static constexpr int kRowsB = PAIR ? BN / 2 : BN;  // rows of B in this CTA
     static constexpr int kStageA = BM * BK * 2, kStageB = kRowsB * BK * 2;
-    static constexpr int kCols = 2 * BN;  // both halves of tensor memory in use
+    static constexpr int kTmem = 2 * BN;  // both halves of tensor memory in use
 };
 
 // Tiles in order of groups of 16 tile rows, column by column within one: the
@@ -136,7 +138,7 @@ __device__ __forceinline__ void finish_linear(const GemmArgs& g, int64_t m, int6
     }
 }
 
-// A warp's 32 rows x 32 columns from its transposing tile to out: rows of
+// A warp's 32 rows x 16 columns from its transposing tile to out: rows of
 // memory are written by neighbouring lanes, four values each where the
 // alignment allows, else one.
 template <class T, bool LINEAR, class TO>
@@ -145,48 +147,46 @@ __device__ __forceinline__ void store_block(const KernelArgs& p, TO* out, int64_
     const GemmArgs& g = p.g;
     const int lane = threadIdx.x % 32;
     __syncwarp();
-    if (p.vec && n0 + 32 <= g.N) {
-        const int col = (lane % 8) * 4;
+    if (p.vec && n0 + kCols <= g.N) {
+        const int col = (lane % 4) * 4;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const int row = i * 4 + lane / 8;
+        for (int i = 0; i < 4; ++i) {
+            const int row = i * 8 + lane / 4;
             if (m0 + row >= g.M) continue;
             const float4 f = *reinterpret_cast<const float4*>(t + row * kPitch + col);
             float c[4] = {f.x, f.y, f.z, f.w};
             if (LINEAR) finish_linear<T>(g, m0 + row, n0 + col, c);
             store_four(out + (m0 + row) * ld + n0 + col, c);
         }
-    } else if (n0 + lane < g.N) {
-        const int rows = (int)min((int64_t)32, g.M - m0);
-        const int64_t n = n0 + lane;
+    } else if (n0 + lane % kCols < g.N) {
+        const int64_t n = n0 + lane % kCols;
+        const int64_t first = m0 + lane / kCols;  // every second row
         const float bias = LINEAR && g.bias ? load_one<T>(g.bias, n) : 0.0f;
-        for (int r0 = 0; r0 < rows; r0 += 8) {  // eight rows' loads before their stores
-            float c[8], res[8];
+        float c[16], res[16];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                c[i] = t[(r0 + i) * kPitch + lane] + bias;
-                res[i] = LINEAR && g.residual && r0 + i < rows ? load_one<T>(g.residual, (m0 + r0 + i) * g.ldr + n)
-                                                               : 0.0f;
-            }
+        for (int i = 0; i < 16; ++i) {  // all loads before the first store
+            c[i] = t[(2 * i + lane / kCols) * kPitch + lane % kCols] + bias;
+            res[i] = LINEAR && g.residual && first + 2 * i < g.M ? load_one<T>(g.residual, (first + 2 * i) * g.ldr + n)
+                                                                 : 0.0f;
+        }
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                if (r0 + i >= rows) break;
-                const int64_t m = m0 + r0 + i;
-                if (LINEAR) {
-                    if (g.pre[0]) g.pre[0][m * g.ldp + n] = c[i];
-                    c[i] = act_value(c[i], g.act);
-                    if (g.residual) c[i] += res[i];
-                }
-                out[m * ld + n] = from_float<TO>(c[i]);
+        for (int i = 0; i < 16; ++i) {
+            const int64_t m = first + 2 * i;
+            if (m >= g.M) break;
+            if (LINEAR) {
+                if (g.pre[0]) g.pre[0][m * g.ldp + n] = c[i];
+                c[i] = act_value(c[i], g.act);
+                if (g.residual) c[i] += res[i];
             }
+            out[m * ld + n] = from_float<TO>(c[i]);
         }
     }
     __syncwarp();
 }
 
-__device__ __forceinline__ void put_row(float* t, const uint32_t (&v)[32], int lane) {
+__device__ __forceinline__ void put_row(float* t, const uint32_t (&v)[kCols], int lane) {
 #pragma unroll
-    for (int j = 0; j < 32; j += 4)
+    for (int j = 0; j < kCols; j += 4)
         *reinterpret_cast<uint4*>(t + lane * kPitch + j) = make_uint4(v[j], v[j + 1], v[j + 2], v[j + 3]);
 }
 
@@ -218,16 +218,16 @@ __global__ void __launch_bounds__(kThreads, 1)
         }
         for (int b = 0; b < 2; ++b) {
             mbar_init(done + 8 * b, 1);
-            mbar_init(freed + 8 * b, PAIR ? 8 : 4);
+            mbar_init(freed + 8 * b, (PAIR ? 2 : 1) * kEpiWarps);
         }
         *gave_up = 0;
         mbar_fence_init();
     }
     if (warp == 2) {
         if (PAIR)
-            tmem_alloc_pair(smem_u32(tmem_at), S::kCols);
+            tmem_alloc_pair(smem_u32(tmem_at), S::kTmem);
         else
-            tmem_alloc(smem_u32(tmem_at), S::kCols);
+            tmem_alloc(smem_u32(tmem_at), S::kTmem);
     }
     fence_before();
     if (PAIR)
@@ -325,8 +325,9 @@ __global__ void __launch_bounds__(kThreads, 1)
             if (!half) round ^= 1;
         }
     } else if (warp >= 4) {  // epilogue
-        const int w = warp - 4;
-        float* t0 = epi + w * 32 * kPitch;
+        const int w = warp % 4;
+        const int from = (warp - 4) / 4 * (kOut / 2), to = from + kOut / 2;
+        float* t0 = epi + (warp - 4) * 32 * kPitch;
         int half = 0;
         uint32_t round = 0;
         for (int64_t t = first; t < p.tiles; t += step) {
@@ -340,26 +341,19 @@ __global__ void __launch_bounds__(kThreads, 1)
             const int64_t m0 = (int64_t)tm * S::kTileM + rank * BM + w * 32;
             const bool rows = m0 < p.g.M;
 #pragma unroll 1
-            for (int c = 0; c < kOut; c += 32) {
+            for (int c = from; c < to; c += kCols) {
                 const int64_t n0 = (int64_t)tn * kOut + c;
                 if (!rows || n0 >= p.g.N) break;
-                uint32_t v[32];
+                uint32_t v[kCols], u[kCols];
                 if (per_tile) {
-                    tmem_ld32(acc + c, v);
+                    tmem_ld16(acc + c, v);
+                    if (KIND == kGemmGated) tmem_ld16(acc + kOut + c, u);
                     wait_ld();
                 } else {
 #pragma unroll
-                    for (int j = 0; j < 32; ++j) v[j] = 0;  // a sum over nothing
+                    for (int j = 0; j < kCols; ++j) v[j] = u[j] = 0;  // a sum over nothing
                 }
                 if (KIND == kGemmGated) {
-                    uint32_t u[32];
-                    if (per_tile) {
-                        tmem_ld32(acc + kOut + c, u);
-                        wait_ld();
-                    } else {
-#pragma unroll
-                        for (int j = 0; j < 32; ++j) u[j] = 0;
-                    }
                     if (p.g.pre[0]) {
                         put_row(t0, v, lane);
                         store_block<float, false>(p, p.g.pre[0], p.g.ldp, m0, n0, t0);
@@ -367,7 +361,7 @@ __global__ void __launch_bounds__(kThreads, 1)
                         store_block<float, false>(p, p.g.pre[1], p.g.ldp, m0, n0, t0);
                     }
 #pragma unroll
-                    for (int j = 0; j < 32; ++j)
+                    for (int j = 0; j < kCols; ++j)
                         v[j] = __float_as_uint(act_value(__uint_as_float(v[j]), p.g.act) * __uint_as_float(u[j]));
                 }
                 put_row(t0, v, lane);
@@ -400,9 +394,9 @@ __global__ void __launch_bounds__(kThreads, 1)
         __syncthreads();
     if (warp == 2) {
         if (PAIR)
-            tmem_free_pair(tmem, S::kCols);
+            tmem_free_pair(tmem, S::kTmem);
         else
-            tmem_free(tmem, S::kCols);
+            tmem_free(tmem, S::kTmem);
     }
 }
 
