@@ -45,6 +45,38 @@ __device__ __forceinline__ uint32_t pack_two<__half>(float lo, float hi) {
     return r;
 }
 
+// Two floats at a time.
+__device__ __forceinline__ uint64_t two(float x, float y) {
+    uint64_t r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(x), "f"(y));
+    return r;
+}
+__device__ __forceinline__ uint64_t two(uint32_t x, uint32_t y) {
+    uint64_t r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "r"(x), "r"(y));
+    return r;
+}
+__device__ __forceinline__ float2 apart(uint64_t v) {
+    float2 r;
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(v));
+    return r;
+}
+__device__ __forceinline__ uint64_t fma_two(uint64_t a, uint64_t b, uint64_t c) {
+    uint64_t r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+__device__ __forceinline__ uint64_t add_two(uint64_t a, uint64_t b) {
+    uint64_t r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ uint64_t mul_two(uint64_t a, uint64_t b) {
+    uint64_t r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+
 struct Params {
     heddle_attention_args a;
     heddle_heads d_o, dq, dk, dv;
@@ -388,21 +420,22 @@ __global__ void __launch_bounds__(Forward<DP, NT>::kThreads, 1)
                 }
             }
             const float sub = top == -INFINITY ? 0.0f : top * c;
-            float s4[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+            const uint64_t c2 = two(c, c), sub2 = two(-sub, -sub);
+            uint64_t part[2] = {0, 0};
 #pragma unroll
             for (int x = 0; x < 2; ++x) {
                 uint32_t w[16];
 #pragma unroll
                 for (int y = 0; y < 32; y += 2) {
-                    const float lo = exp2_fast(fmaf(__uint_as_float(v[x][y]), c, -sub));
-                    const float hi = exp2_fast(fmaf(__uint_as_float(v[x][y + 1]), c, -sub));
-                    s4[y % 4] += lo;
-                    s4[y % 4 + 1] += hi;
+                    const float2 z = apart(fma_two(two(v[x][y], v[x][y + 1]), c2, sub2));
+                    const float lo = exp2_fast(z.x), hi = exp2_fast(z.y);
+                    part[y / 2 % 2] = add_two(part[y / 2 % 2], two(lo, hi));
                     w[y / 2] = pack_two<T>(lo, hi);
                 }
                 tmem_st16(ts + 64 * side + 16 * x, w);  // over scores that this warp itself has read
             }
-            sum += (s4[0] + s4[1]) + (s4[2] + s4[3]);
+            const float2 both = apart(add_two(part[0], part[1]));
+            sum += both.x + both.y;
             if (side == 0 && s.kl < p.a.kv_len && k0 + kTile > s.kl) {  // values past the sequence
                 const int iv = 2 * j + 1, sv = iv % F::kSlots;
                 if (!(go = __all_sync(~0u, mbar_wait(full + 8 * sv, iv / F::kSlots & 1, gave_up)))) break;
@@ -605,6 +638,7 @@ __global__ void __launch_bounds__(kGradThreads, 1)
         float lse = inside ? p.a.lse[r] : INFINITY;
         lse = lse == -INFINITY ? INFINITY : lse * kLog2e;  // weights of a row that sees nothing are zero
         const float delta = inside ? p.delta[r] : 0.0f, c = p.scale_log2;
+        const uint64_t c2 = two(c, c), lse2 = two(-lse, -lse), delta2 = two(-delta, -delta);
         bool go = true;
         for (int j = 0; j < n; ++j) {
             const int64_t k0 = (int64_t)keys.at(j) * kTile;
@@ -619,12 +653,16 @@ __global__ void __launch_bounds__(kGradThreads, 1)
             __syncwarp();
             if (lane == 0) mbar_arrive(bar.a_ready);
 #pragma unroll
-            for (int y = 0; y < 32; ++y)
-                v[y] = __float_as_uint(exp2_fast(fmaf(__uint_as_float(v[y]), c, -lse)));
+            for (int y = 0; y < 32; y += 2) {
+                const float2 z = apart(fma_two(two(v[y], v[y + 1]), c2, lse2));
+                v[y] = __float_as_uint(exp2_fast(z.x)), v[y + 1] = __float_as_uint(exp2_fast(z.y));
+            }
             if (whole) {
 #pragma unroll
-                for (int y = 0; y < 32; ++y)
-                    d[y] = __float_as_uint(__uint_as_float(v[y]) * (__uint_as_float(d[y]) - delta));
+                for (int y = 0; y < 32; y += 2) {
+                    const float2 z = apart(mul_two(two(v[y], v[y + 1]), add_two(two(d[y], d[y + 1]), delta2)));
+                    d[y] = __float_as_uint(z.x), d[y + 1] = __float_as_uint(z.y);
+                }
             } else {
                 // a product with what lies in hidden places must not count
 #pragma unroll
@@ -691,8 +729,9 @@ __global__ void __launch_bounds__(kGradThreads, 1)
     const GradBars bar(smem_u32(tail));
     volatile uint32_t* gave_up = reinterpret_cast<uint32_t*>(tail + kGradBarBytes);
     uint32_t* tmem_at = const_cast<uint32_t*>(gave_up) + 1;
-    float2* stat = reinterpret_cast<float2*>(tail + kGradBarBytes + 64);     // [3][128] lse, delta
-    int* pos = reinterpret_cast<int*>(stat + 3 * kTile);                     // [3][128] positions
+    float* stat_lse = reinterpret_cast<float*>(tail + kGradBarBytes + 64);  // [3][128] minus lse, in powers of two
+    float* stat_delta = stat_lse + 3 * kTile;                               // [3][128] minus delta
+    int* pos = reinterpret_cast<int*>(stat_delta + 3 * kTile);              // [3][128] positions
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
 
     // the first keys are seen by the most queries
@@ -789,24 +828,25 @@ __global__ void __launch_bounds__(kGradThreads, 1)
         const int side = (warp - 4) / 4, row = (warp % 4) * 32 + lane;  // which 32 of a tile's 128 queries
         const uint32_t lanes = (uint32_t)(warp % 4 * 32) << 16;
         const int64_t key = k0 + row;
-        const float c = p.scale_log2;
+        const uint64_t c2 = two(p.scale_log2, p.scale_log2);
 
-        // statistics of query tile j to buffer j % 3, by the first two sides:
-        // written a step ahead, while the slowest warp may still read those of
-        // the step before
+        // statistics of query tile j to buffer j % 3, a kind a side: written a
+        // step ahead, while the slowest warp may still read those of the step
+        // before
+        const int64_t i_row = (int64_t)first * p.tokens + row / p.group;
+        const int64_t r_row = ((int64_t)b * p.a.q_heads + hk * p.group + row % p.group) * p.a.q_len;
+        const bool in_tile = row < p.group * p.tokens;
         auto put_stats = [&](int j) {
-            const int64_t i = (int64_t)(first + j) * p.tokens + row / p.group;
-            const int64_t h = (int64_t)hk * p.group + row % p.group;
-            const int64_t r = ((int64_t)b * p.a.q_heads + h) * p.a.q_len + i;
-            const bool live = row < p.group * p.tokens && i < s.ql;
-            float2* to = stat + (j % 3) * kTile + row;
+            const int64_t i = i_row + (int64_t)j * p.tokens;
+            const bool live = in_tile && i < s.ql;
+            const int to = j % 3 * kTile + row;
             if (side == 0) {
-                const float l = live ? p.a.lse[r] : INFINITY;
-                to->x = l == -INFINITY ? -INFINITY : -l * kLog2e;
+                const float l = live ? p.a.lse[r_row + i] : INFINITY;
+                stat_lse[to] = l == -INFINITY ? -INFINITY : -l * kLog2e;
             } else if (side == 1) {
-                to->y = live ? p.delta[r] : 0.0f;
+                stat_delta[to] = live ? -p.delta[r_row + i] : 0.0f;
             } else if (side == 2) {
-                pos[(j % 3) * kTile + row] = live ? (int)max(s.off + i, (int64_t)-1) : -1;
+                pos[to] = live ? (int)max(s.off + i, (int64_t)-1) : -1;
             }
         };
         bool go = true;
@@ -823,7 +863,8 @@ __global__ void __launch_bounds__(kGradThreads, 1)
                 if (lane == 0) mbar_arrive(bar.stats);
             }
             const int64_t t0 = (int64_t)(first + j) * p.tokens, t1 = t0 + p.tokens;
-            const float4* st = reinterpret_cast<const float4*>(stat + (j % 3) * kTile + side * 32);
+            const float4* lses = reinterpret_cast<const float4*>(stat_lse + (j % 3) * kTile + side * 32);
+            const float4* deltas = reinterpret_cast<const float4*>(stat_delta + (j % 3) * kTile + side * 32);
             const bool whole = t1 <= s.ql && all_visible(p, s, t0, t1, k0);
             if (!(go = __all_sync(~0u, mbar_wait(bar.a_full, j & 1, gave_up)))) break;
             fence_after();
@@ -831,10 +872,12 @@ __global__ void __launch_bounds__(kGradThreads, 1)
             tmem_ld32(at_s + lanes + side * 32, v);
             wait_ld();
 #pragma unroll
-            for (int y = 0; y < 32; y += 2) {
-                const float4 f = st[y / 2];
-                v[y] = __float_as_uint(exp2_fast(fmaf(__uint_as_float(v[y]), c, f.x)));
-                v[y + 1] = __float_as_uint(exp2_fast(fmaf(__uint_as_float(v[y + 1]), c, f.z)));
+            for (int y = 0; y < 32; y += 4) {
+                const float4 f = lses[y / 4];
+                const float2 z0 = apart(fma_two(two(v[y], v[y + 1]), c2, two(f.x, f.y)));
+                const float2 z1 = apart(fma_two(two(v[y + 2], v[y + 3]), c2, two(f.z, f.w)));
+                v[y] = __float_as_uint(exp2_fast(z0.x)), v[y + 1] = __float_as_uint(exp2_fast(z0.y));
+                v[y + 2] = __float_as_uint(exp2_fast(z1.x)), v[y + 3] = __float_as_uint(exp2_fast(z1.y));
             }
             if (!whole) {
                 const int* at = pos + (j % 3) * kTile + side * 32;
@@ -864,10 +907,13 @@ __global__ void __launch_bounds__(kGradThreads, 1)
             tmem_ld32(at_dp + lanes + side * 32, d);
             wait_ld();
 #pragma unroll
-            for (int y = 0; y < 32; y += 2) {
-                const float4 f = st[y / 2];
-                d[y] = __float_as_uint(__uint_as_float(v[y]) * (__uint_as_float(d[y]) - f.y));
-                d[y + 1] = __float_as_uint(__uint_as_float(v[y + 1]) * (__uint_as_float(d[y + 1]) - f.w));
+            for (int y = 0; y < 32; y += 4) {
+                const float4 f = deltas[y / 4];
+                const float2 z0 = apart(mul_two(two(v[y], v[y + 1]), add_two(two(d[y], d[y + 1]), two(f.x, f.y))));
+                const float2 z1 =
+                    apart(mul_two(two(v[y + 2], v[y + 3]), add_two(two(d[y + 2], d[y + 3]), two(f.z, f.w))));
+                d[y] = __float_as_uint(z0.x), d[y + 1] = __float_as_uint(z0.y);
+                d[y + 2] = __float_as_uint(z1.x), d[y + 3] = __float_as_uint(z1.y);
             }
             if (!whole) {  // a product with what lies in hidden places must not count
 #pragma unroll

@@ -135,148 +135,144 @@ __global__ void __launch_bounds__(kWarps * 32) qk_norm_rope_kernel(heddle_qk_nor
     }
 }
 
-// V values of 16 bytes, at once or one by one.
+// Half of a lane's values: 8 bytes, at once or one by one.
 template <class T>
-__device__ __forceinline__ uint4 load_unit(const T* p, bool whole) {
-    if (whole) return *reinterpret_cast<const uint4*>(p);
-    uint4 u;
+__device__ __forceinline__ uint2 load_half(const T* p, bool whole) {
+    if (whole) return *reinterpret_cast<const uint2*>(p);
+    uint2 u;
     T* t = reinterpret_cast<T*>(&u);
 #pragma unroll
-    for (int i = 0; i < (int)(16 / sizeof(T)); ++i) t[i] = p[i];
+    for (int i = 0; i < (int)(8 / sizeof(T)); ++i) t[i] = p[i];
     return u;
 }
 template <class T>
-__device__ __forceinline__ void store_unit(T* p, const uint4& u, bool whole) {
+__device__ __forceinline__ void store_half(T* p, const uint2& u, bool whole) {
     if (whole) {
-        *reinterpret_cast<uint4*>(p) = u;
+        *reinterpret_cast<uint2*>(p) = u;
         return;
     }
     const T* t = reinterpret_cast<const T*>(&u);
 #pragma unroll
-    for (int i = 0; i < (int)(16 / sizeof(T)); ++i) p[i] = t[i];
+    for (int i = 0; i < (int)(8 / sizeof(T)); ++i) p[i] = t[i];
+}
+
+// 1 / sqrt(v), the approximation and one Newton step.
+__device__ __forceinline__ float inv_sqrt(float v) {
+    const float r = rsqrtf(v);
+    return v > 0.0f && v < INFINITY ? r * fmaf(-0.5f * v * r, r, 1.5f) : r;
 }
 
 // A head of whole 16-byte units in a group of GL lanes, V values a lane, the
-// last lanes idle where head_dim / V is not GL.  A group takes `chunk`
-// heads of one token at a time.
+// last lanes idle where head_dim / V is not GL.  A lane's values are two runs
+// of V / 2 that hold both values of every pair they turn: places i.. and
+// i + rot_dim / 2.., or 2i.., so that no value changes lanes.  A block takes
+// queries or keys alone (the first q_blocks queries); a group takes `chunk`
+// heads of one token at a time and keeps its angles.
 template <class T, int GL, bool GRAD>
-__global__ void __launch_bounds__(256) qk_norm_rope_wide_kernel(const __grid_constant__ heddle_qk_norm_rope_grad_args ga,
-                                                                float* partial, uint32_t* err, int chunk, bool whole) {
-    constexpr int V = 16 / sizeof(T), kGroups = 256 / GL, kDepth = GRAD ? 2 : 4;
+__global__ void __launch_bounds__(256, 3)
+    qk_norm_rope_wide_kernel(const __grid_constant__ heddle_qk_norm_rope_grad_args ga, float* partial, uint32_t* err,
+                             int q_blocks, int chunk, bool whole) {
+    constexpr int V = 16 / sizeof(T), H = V / 2, kGroups = 256 / GL, kDepth = GRAD ? 2 : 4;
     const heddle_qk_norm_rope_args& a = ga.fwd;
+    const bool is_q = blockIdx.x < q_blocks;
+    const int block = is_q ? blockIdx.x : blockIdx.x - q_blocks, blocks = is_q ? q_blocks : gridDim.x - q_blocks;
+    const int heads = is_q ? a.q_heads : a.k_heads, chunks = (heads + chunk - 1) / chunk;
+    const heddle_heads in = is_q ? a.q : a.k, out = is_q ? a.q_out : a.k_out, dst = is_q ? ga.dq : ga.dk;
     const int lane = threadIdx.x % GL, group = threadIdx.x / GL;
-    const int D = a.head_dim, rot = a.rot_dim, half = rot / 2, i0 = lane * V;
-    const int heads = a.q_heads + a.k_heads, chunks = (heads + chunk - 1) / chunk;
-    const int64_t units = a.tokens * chunks;
-    const bool live = i0 < D, turns = i0 < rot;
-    // the group's lanes, as a mask and where the pair's other half is
-    const uint32_t mask = GL == 32 ? ~0u : ((1u << GL) - 1) << (threadIdx.x % 32 / GL * GL);
-    const bool second = !a.interleaved && i0 >= half;
-    const int other = a.interleaved ? lane : turns ? (second ? lane - half / V : lane + half / V) : lane;
+    const int D = a.head_dim, rot = a.rot_dim;
+    const bool live = lane * V < D, turns = lane * V < rot, inter = a.interleaved;
+    // the lane's two runs; lanes past the turned part hold V values in a row
+    const int at0 = turns && !inter ? lane * H : lane * V, at1 = turns && !inter ? at0 + rot / 2 : at0 + H;
+    const uint32_t mask = GL == 32 ? ~0u : ((1u << (GL & 31)) - 1) << (threadIdx.x % 32 / GL * GL);
     const float inv_d = 1.0f / D;
-    float wq[V], wk[V];
+    float w[V], dw[V] = {};
+    {
+        const T* wt = static_cast<const T*>(is_q ? a.wq : a.wk);
 #pragma unroll
-    for (int v = 0; v < V; ++v) {
-        wq[v] = live && a.q_heads ? to_float(static_cast<const T*>(a.wq)[i0 + v]) : 0.0f;
-        wk[v] = live && a.k_heads ? to_float(static_cast<const T*>(a.wk)[i0 + v]) : 0.0f;
-    }
-    float dwq[V] = {}, dwk[V] = {};
-
-    // (p, q) -> turned by the lane's angles; back: by their negatives
-    auto turn = [&](float (&v)[V], const float (&cs)[V], const float (&sn)[V], float sign) {
-        if (a.interleaved) {
-            if (turns)
-#pragma unroll
-                for (int i = 0; i < V; i += 2) {
-                    const float p = v[i], q = v[i + 1], s = sign * sn[i / 2];
-                    v[i] = p * cs[i / 2] - q * s;
-                    v[i + 1] = q * cs[i / 2] + p * s;
-                }
-        } else {
-#pragma unroll
-            for (int i = 0; i < V; ++i) {
-                const float o = __shfl_sync(mask, v[i], other, GL);
-                const float s = second ? sign * sn[i] : -sign * sn[i];
-                if (turns) v[i] = v[i] * cs[i] + o * s;
-            }
+        for (int v = 0; v < H; ++v) {
+            w[v] = live ? to_float(wt[at0 + v]) : 0.0f;
+            w[H + v] = live ? to_float(wt[at1 + v]) : 0.0f;
         }
-    };
+    }
 
-    for (int64_t u = (int64_t)blockIdx.x * kGroups + group; u < units; u += (int64_t)gridDim.x * kGroups) {
+    const int64_t units = a.tokens * chunks;
+    for (int64_t u = (int64_t)block * kGroups + group; u < units; u += (int64_t)blocks * kGroups) {
         const int64_t t = u / chunks;
         const int h0 = (int)(u - t * chunks) * chunk, h1 = min(heads, h0 + chunk);
+        float cs[H], sn[H];
         bool bad = false;
-        float cs[V], sn[V];
         if (rot) {
             const int64_t p = a.positions[t];
             bad = p < 0 || p >= a.table_len;
             if (bad && lane == 0) atomicOr(err, kErrOpPosition);
-            if (turns) {
-                if (!bad) {
-                    const int64_t at = p * half + (a.interleaved ? i0 / 2 : second ? i0 - half : i0);
+            if (turns && !bad) {
+                const int64_t at = p * (rot / 2) + lane * H;
 #pragma unroll
-                    for (int v = 0; v < V; ++v)
-                        if (v < (a.interleaved ? V / 2 : V)) cs[v] = a.cos[at + v], sn[v] = a.sin[at + v];
-                }
+                for (int v = 0; v < H; ++v) cs[v] = a.cos[at + v], sn[v] = a.sin[at + v];
             }
         }
-        if (bad) {
+        // the lane's pairs turned by the angles, back by their negatives
+        auto turn = [&](float (&v)[V], bool back) {
+            if (!turns || bad) return;
 #pragma unroll
-            for (int v = 0; v < V; ++v) cs[v] = sn[v] = 0.0f;
-        }
+            for (int k = 0; k < H; ++k) {
+                const float s = back ? -sn[k] : sn[k];
+                if (inter) {
+                    const float x = v[2 * k], y = v[2 * k + 1];
+                    v[2 * k] = x * cs[k] - y * s;
+                    v[2 * k + 1] = y * cs[k] + x * s;
+                } else {
+                    const float x = v[k], y = v[H + k];
+                    v[k] = x * cs[k] - y * s;
+                    v[H + k] = y * cs[k] + x * s;
+                }
+            }
+        };
+        const T* x_at = static_cast<const T*>(in.data) + t * in.token_stride + h0 * in.head_stride;
+        const T* g_at = static_cast<const T*>(out.data) + t * out.token_stride + h0 * out.head_stride;
+        T* y_at = GRAD ? static_cast<T*>(dst.data) + t * dst.token_stride + h0 * dst.head_stride
+                       : static_cast<T*>(out.data) + t * out.token_stride + h0 * out.head_stride;
+        const int64_t y_step = GRAD ? dst.head_stride : out.head_stride;
         for (int h = h0; h < h1; h += kDepth) {
-            uint4 x[kDepth], g[kDepth];
+            uint2 x[kDepth][2], g[kDepth][2];
 #pragma unroll
-            for (int k = 0; k < kDepth; ++k) {
-                const int hh = min(h + k, h1 - 1);
-                const bool is_q = hh < a.q_heads;
-                const int at = is_q ? hh : hh - a.q_heads;
-                const heddle_heads& in = is_q ? a.q : a.k;
-                const heddle_heads& out = is_q ? a.q_out : a.k_out;
-                x[k] = g[k] = make_uint4(0, 0, 0, 0);
-                if (live) {
-                    x[k] = load_unit(static_cast<const T*>(in.data) + t * in.token_stride + at * in.head_stride + i0,
-                                     whole);
-                    if (GRAD)
-                        g[k] = load_unit(
-                            static_cast<const T*>(out.data) + t * out.token_stride + at * out.head_stride + i0, whole);
+            for (int k = 0; k < kDepth; ++k)
+                if (live && h + k < h1) {
+                    x[k][0] = load_half(x_at + k * in.head_stride + at0, whole);
+                    x[k][1] = load_half(x_at + k * in.head_stride + at1, whole);
+                    if (GRAD) {
+                        g[k][0] = load_half(g_at + k * out.head_stride + at0, whole);
+                        g[k][1] = load_half(g_at + k * out.head_stride + at1, whole);
+                    }
                 }
-            }
 #pragma unroll
             for (int k = 0; k < kDepth; ++k) {
-                const int hh = h + k;
-                if (hh >= h1) break;
-                const bool is_q = hh < a.q_heads;
-                const int at = is_q ? hh : hh - a.q_heads;
-                const heddle_heads& dst = GRAD ? (is_q ? ga.dq : ga.dk) : (is_q ? a.q_out : a.k_out);
-                const T* xt = reinterpret_cast<const T*>(&x[k]);
+                if (h + k >= h1) break;
                 float v[V], ss = 0.0f;
 #pragma unroll
                 for (int i = 0; i < V; ++i) {
-                    v[i] = to_float(xt[i]);
+                    v[i] = live ? to_float(reinterpret_cast<const T*>(&x[k][i / H])[i % H]) : 0.0f;
                     ss += v[i] * v[i];
                 }
 #pragma unroll
                 for (int o = GL / 2; o; o >>= 1) ss += __shfl_xor_sync(mask, ss, o, GL);
-                const float rstd = 1.0f / sqrtf(ss * inv_d + a.eps);
+                const float rstd = inv_sqrt(ss * inv_d + a.eps);
                 float r[V];
                 if (!GRAD) {
 #pragma unroll
-                    for (int i = 0; i < V; ++i) r[i] = v[i] * rstd * (is_q ? wq[i] : wk[i]);
-                    turn(r, cs, sn, 1.0f);
+                    for (int i = 0; i < V; ++i) r[i] = v[i] * rstd * w[i];
+                    turn(r, false);
                 } else {
-                    const T* gt = reinterpret_cast<const T*>(&g[k]);
                     float dot = 0.0f;
 #pragma unroll
-                    for (int i = 0; i < V; ++i) r[i] = to_float(gt[i]);
-                    turn(r, cs, sn, -1.0f);
+                    for (int i = 0; i < V; ++i)
+                        r[i] = live ? to_float(reinterpret_cast<const T*>(&g[k][i / H])[i % H]) : 0.0f;
+                    turn(r, true);
 #pragma unroll
                     for (int i = 0; i < V; ++i) {
                         v[i] *= rstd;
-                        const float dw = bad ? 0.0f : r[i] * v[i];
-                        dwq[i] += is_q ? dw : 0.0f;
-                        dwk[i] += is_q ? 0.0f : dw;
-                        r[i] *= is_q ? wq[i] : wk[i];
+                        if (!bad) dw[i] += r[i] * v[i];
+                        r[i] *= w[i];
                         dot += r[i] * v[i];
                     }
 #pragma unroll
@@ -286,42 +282,46 @@ __global__ void __launch_bounds__(256) qk_norm_rope_wide_kernel(const __grid_con
                     for (int i = 0; i < V; ++i) r[i] = rstd * (r[i] - v[i] * dot);
                 }
                 if (live) {
-                    uint4 y;
-                    T* yt = reinterpret_cast<T*>(&y);
+                    uint2 y[2];
 #pragma unroll
-                    for (int i = 0; i < V; ++i) yt[i] = from_float<T>(bad ? 0.0f : r[i]);
-                    store_unit(static_cast<T*>(dst.data) + t * dst.token_stride + at * dst.head_stride + i0, y, whole);
+                    for (int i = 0; i < V; ++i)
+                        reinterpret_cast<T*>(&y[i / H])[i % H] = from_float<T>(bad ? 0.0f : r[i]);
+                    store_half(y_at + k * y_step + at0, y[0], whole);
+                    store_half(y_at + k * y_step + at1, y[1], whole);
                 }
             }
+            x_at += kDepth * in.head_stride;
+            g_at += kDepth * out.head_stride;
+            y_at += kDepth * y_step;
         }
     }
     if (GRAD) {  // the block's groups, in order
         __shared__ float s[kGroups][GL * V];
-        for (int side = 0; side < 2; ++side) {
-            __syncthreads();
 #pragma unroll
-            for (int v = 0; v < V; ++v) s[group][i0 + v] = side ? dwk[v] : dwq[v];
-            __syncthreads();
-            for (int i = threadIdx.x; i < D; i += 256) {
-                float sum = 0.0f;
+        for (int v = 0; v < H; ++v)
+            if (live) s[group][at0 + v] = dw[v], s[group][at1 + v] = dw[H + v];
+        __syncthreads();
+        for (int i = threadIdx.x; i < D; i += 256) {
+            float sum = 0.0f;
 #pragma unroll
-                for (int k = 0; k < kGroups; ++k) sum += s[k][i];
-                partial[((int64_t)side * gridDim.x + blockIdx.x) * D + i] = sum;
-            }
+            for (int k = 0; k < kGroups; ++k) sum += s[k][i];
+            partial[(int64_t)blockIdx.x * D + i] = sum;
         }
     }
 }
 
-// Sums the blocks' partial weight gradients, one block per 32 columns of dwq or dwk.
-__global__ void __launch_bounds__(1024) weight_grad_kernel(const float* partial, int blocks, int D, float* dwq,
-                                                           float* dwk) {
+// Sums the blocks' partial weight gradients, one block per 32 columns of dwq
+// (the first q_blocks blocks) or dwk (the next k_blocks).
+__global__ void __launch_bounds__(1024) weight_grad_kernel(const float* partial, int q_blocks, int k_blocks, int D,
+                                                           float* dwq, float* dwk) {
     __shared__ float s[32][33];
     const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
     const int i = blockIdx.x * 32 + lane;
     float v = 0.0f;
+    const int first = blockIdx.y ? q_blocks : 0, blocks = blockIdx.y ? k_blocks : q_blocks;
     if (i < D)
 #pragma unroll 4
-        for (int b = warp; b < blocks; b += 32) v += partial[((int64_t)blockIdx.y * blocks + b) * D + i];
+        for (int b = warp; b < blocks; b += 32) v += partial[(int64_t)(first + b) * D + i];
     s[warp][lane] = v;
     __syncthreads();
     if (warp == 0 && i < D) {
@@ -332,60 +332,73 @@ __global__ void __launch_bounds__(1024) weight_grad_kernel(const float* partial,
 
 int elem_bytes(int32_t dtype) { return dtype == HEDDLE_FP32 ? 4 : 2; }
 
-bool units16(const heddle_heads& t, int heads, int size) {
-    return heads == 0 || ((uintptr_t)t.data % 16 == 0 && t.token_stride * size % 16 == 0 && t.head_stride * size % 16 == 0);
+bool units8(const heddle_heads& t, int heads, int size) {
+    return heads == 0 || ((uintptr_t)t.data % 8 == 0 && t.token_stride * size % 8 == 0 && t.head_stride * size % 8 == 0);
 }
 
-// Heads of whole 16-byte units in at most 32 lanes, pairs that lie in one
-// lane or in the same places of two: by sizes alone, so that results do not
-// depend on where the tensors lie.
+// Heads of whole 16-byte units in at most 32 lanes, whole lanes of turned
+// values: by sizes alone, so that results do not depend on where the tensors
+// lie.
 bool wide_takes(const heddle_qk_norm_rope_args& a) {
     const int V = 16 / elem_bytes(a.dtype);
-    return a.head_dim % V == 0 && a.head_dim / V <= 32 && a.rot_dim % (a.interleaved ? V : 2 * V) == 0;
+    return a.head_dim % V == 0 && a.head_dim / V <= 32 && a.rot_dim % V == 0;
 }
 bool whole_units(const heddle_qk_norm_rope_grad_args& g, bool grad) {
     const heddle_qk_norm_rope_args& a = g.fwd;
     const int size = elem_bytes(a.dtype);
-    return units16(a.q, a.q_heads, size) && units16(a.k, a.k_heads, size) && units16(a.q_out, a.q_heads, size) &&
-           units16(a.k_out, a.k_heads, size) &&
-           (!grad || (units16(g.dq, a.q_heads, size) && units16(g.dk, a.k_heads, size)));
+    return units8(a.q, a.q_heads, size) && units8(a.k, a.k_heads, size) && units8(a.q_out, a.q_heads, size) &&
+           units8(a.k_out, a.k_heads, size) &&
+           (!grad || (units8(g.dq, a.q_heads, size) && units8(g.dk, a.k_heads, size)));
 }
 
 struct Launch {
     bool wide, whole;
-    int lanes, chunk, blocks;
+    int lanes, chunk, q_blocks, k_blocks;
 };
 Launch plan_rows(const OpContext& x, const heddle_qk_norm_rope_grad_args& g, bool grad) {
     const heddle_qk_norm_rope_args& a = g.fwd;
-    Launch l{wide_takes(a), whole_units(g, grad), 32, 1, 1};
+    Launch l{wide_takes(a), whole_units(g, grad), 32, 1, 0, 0};
     const int64_t heads = (int64_t)a.q_heads + a.k_heads;
-    int64_t want;
-    if (l.wide) {
-        const int need = a.head_dim * elem_bytes(a.dtype) / 16;
-        l.lanes = need <= 8 ? 8 : need <= 16 ? 16 : 32;
-        const int groups = 256 / l.lanes;
-        // several heads a group once every SM has groups enough without
-        l.chunk = a.tokens * ceil_div(heads, 8) >= (int64_t)x.num_sms * groups * 4 ? 8 : 1;
-        want = ceil_div(a.tokens * ceil_div(heads, l.chunk), groups);
-    } else {
-        want = ceil_div(a.tokens * heads, kWarps);
+    if (!l.wide) {  // rows of queries and keys by turns: both sums over all blocks
+        const int64_t want = ceil_div(a.tokens * heads, kWarps), most = (int64_t)x.num_sms * 8;
+        l.q_blocks = l.k_blocks = (int)(want < 1 ? 1 : want < most ? want : most);
+        return l;
     }
-    const int64_t most = (int64_t)x.num_sms * 8;
-    l.blocks = (int)(want < 1 ? 1 : want < most ? want : most);
+    const int need = a.head_dim * elem_bytes(a.dtype) / 16;
+    l.lanes = need <= 8 ? 8 : need <= 16 ? 16 : 32;
+    const int groups = 256 / l.lanes;
+    // several heads a group once every SM has groups enough without
+    const int64_t each = ceil_div(a.q_heads, 8) + ceil_div(a.k_heads, 8);
+    l.chunk = a.tokens * each >= (int64_t)x.num_sms * groups * 3 ? 8 : 1;
+    const int64_t q_want = ceil_div(a.tokens * ceil_div(a.q_heads, l.chunk), groups),
+                  k_want = ceil_div(a.tokens * ceil_div(a.k_heads, l.chunk), groups);
+    const int64_t most = (int64_t)x.num_sms * 6;  // two rounds of three blocks an SM
+    if (q_want + k_want <= most) {
+        l.q_blocks = (int)q_want, l.k_blocks = (int)k_want;
+    } else {  // shared by heads, one block at least where there are any
+        int64_t kb = most * a.k_heads / heads;
+        kb = a.k_heads && kb < 1 ? 1 : kb;
+        const int64_t qb = a.q_heads ? (most - kb < 1 ? 1 : most - kb) : 0;
+        l.q_blocks = (int)(qb < q_want ? qb : q_want);
+        l.k_blocks = (int)(kb < k_want ? kb : k_want);
+    }
     return l;
 }
 
 template <class T, bool GRAD>
 void launch_typed(const Launch& l, const OpContext& x, const heddle_qk_norm_rope_grad_args& a, float* partial,
                   cudaStream_t st) {
+    const int blocks = l.q_blocks + l.k_blocks;
     if (!l.wide)
-        qk_norm_rope_kernel<T, GRAD><<<l.blocks, kWarps * 32, 0, st>>>(a, partial, x.err);
+        qk_norm_rope_kernel<T, GRAD><<<l.q_blocks, kWarps * 32, 0, st>>>(a, partial, x.err);
+    else if (blocks == 0)
+        return;
     else if (l.lanes == 8)
-        qk_norm_rope_wide_kernel<T, 8, GRAD><<<l.blocks, 256, 0, st>>>(a, partial, x.err, l.chunk, l.whole);
+        qk_norm_rope_wide_kernel<T, 8, GRAD><<<blocks, 256, 0, st>>>(a, partial, x.err, l.q_blocks, l.chunk, l.whole);
     else if (l.lanes == 16)
-        qk_norm_rope_wide_kernel<T, 16, GRAD><<<l.blocks, 256, 0, st>>>(a, partial, x.err, l.chunk, l.whole);
+        qk_norm_rope_wide_kernel<T, 16, GRAD><<<blocks, 256, 0, st>>>(a, partial, x.err, l.q_blocks, l.chunk, l.whole);
     else
-        qk_norm_rope_wide_kernel<T, 32, GRAD><<<l.blocks, 256, 0, st>>>(a, partial, x.err, l.chunk, l.whole);
+        qk_norm_rope_wide_kernel<T, 32, GRAD><<<blocks, 256, 0, st>>>(a, partial, x.err, l.q_blocks, l.chunk, l.whole);
 }
 
 template <bool GRAD>
@@ -409,7 +422,8 @@ cudaError_t launch_qk_norm_rope(const OpContext& x, const heddle_qk_norm_rope_ar
 }
 
 size_t qk_norm_rope_grad_scratch(const OpContext& x, const heddle_qk_norm_rope_grad_args& a) {
-    return align256(sizeof(float) * 2 * (size_t)plan_rows(x, a, true).blocks * a.fwd.head_dim);
+    const Launch l = plan_rows(x, a, true);
+    return align256(sizeof(float) * (size_t)(l.q_blocks + l.k_blocks) * a.fwd.head_dim);
 }
 
 cudaError_t launch_qk_norm_rope_grad(const OpContext& x, const heddle_qk_norm_rope_grad_args& a, unsigned char* ws,
@@ -418,7 +432,8 @@ cudaError_t launch_qk_norm_rope_grad(const OpContext& x, const heddle_qk_norm_ro
     const Launch l = plan_rows(x, a, true);
     launch_rows<true>(l, x, a, partial, st);
     const int D = a.fwd.head_dim;
-    weight_grad_kernel<<<dim3((unsigned)ceil_div(D, 32), 2), 1024, 0, st>>>(partial, l.blocks, D, a.dwq, a.dwk);
+    weight_grad_kernel<<<dim3((unsigned)ceil_div(D, 32), 2), 1024, 0, st>>>(partial, l.q_blocks, l.k_blocks, D, a.dwq,
+                                                                            a.dwk);
     return cudaGetLastError();
 }
 
