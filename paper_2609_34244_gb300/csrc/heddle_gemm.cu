@@ -57,6 +57,7 @@ struct KernelArgs {
     int32_t terms;
     int32_t a_rows;      // rows of A a copy takes (all 128, or fewer where M is)
     int32_t stages, stage;  // of the ring, and its bytes each
+    int32_t deep;           // 64-wide steps a stage holds: 1, or kDeep where rows are few
     int32_t m_tiles, n_tiles;
     int64_t tiles;
     int32_t vec;         // outputs, residual, bias and saved sums by 16- and 8-byte accesses
@@ -64,6 +65,9 @@ struct KernelArgs {
 };
 
 constexpr int kMaxStages = 32;
+// With few rows a step's products are short and its barriers are the time, so
+// a stage holds four, of one copy an operand where that gives the layout.
+constexpr int kDeep = 4;
 constexpr int kEpi = kEpiWarps * 32 * kPitch * 4;
 constexpr int kBarBytes = 16 * kMaxStages + 64;
 constexpr int kShared = 227 * 1024;  // all that a CTA may take
@@ -236,7 +240,9 @@ __global__ void __launch_bounds__(kThreads, 1)
         __syncthreads();
     fence_after();
     const uint32_t tmem = *tmem_at;
-    const int per_tile = p.steps * p.terms;
+    constexpr bool kMayBeDeep = !PAIR && BN <= 64 && (KIND == kGemmLinear || KIND == kGemmGated);
+    const int deep = kMayBeDeep ? p.deep : 1;
+    const int per_tile = (p.steps * p.terms + deep - 1) / deep;
 
     if (warp == 0 && per_tile && elect_one()) {  // producer
         prefetch_map(&a0);
@@ -258,7 +264,22 @@ __global__ void __launch_bounds__(kThreads, 1)
             for (int it = 0; it < per_tile; ++it) {
                 if (!(go = mbar_wait(empty + 8 * s, phase ^ 1, gave_up))) break;
                 const uint32_t own = full + 8 * s, bar = PAIR ? cluster_at(own, 0) : own;
-                const uint32_t sa = smem_u32(stages + s * p.stage), sb = sa + a_bytes;
+                const uint32_t sa = smem_u32(stages + s * p.stage), sb = sa + deep * a_bytes;
+                if (kMayBeDeep && deep > 1) {
+                    mbar_expect(own, p.stage);
+                    load_3d(sa, &a0, bar, 0, m0, it * deep);
+                    if (KIND == kGemmGated) {  // the two operands by turns
+#pragma unroll
+                        for (int d = 0; d < kDeep; ++d) {
+                            load_2d(sb + d * S::kStageB, &b0, bar, (it * kDeep + d) * BK, tn * kOut);
+                            load_2d(sb + d * S::kStageB + S::kStageB / 2, &b1, bar, (it * kDeep + d) * BK, tn * kOut);
+                        }
+                    } else {
+                        load_3d(sb, &b0, bar, 0, tn * kOut, it * deep);
+                    }
+                    if (++s == p.stages) s = 0, phase ^= 1;
+                    continue;
+                }
                 const bool second = KIND == kGemmSum ? it >= p.steps : KIND == kGemmPair ? z : false;
                 const CUtensorMap* ma = second ? &a1 : &a0;
                 const CUtensorMap* mb = second ? &b1 : &b0;
@@ -299,8 +320,19 @@ __global__ void __launch_bounds__(kThreads, 1)
             for (int it = 0; it < per_tile; ++it) {
                 if (!(go = mbar_wait(full + 8 * s, phase, gave_up))) break;
                 fence_after();
-                const uint32_t sa = smem_u32(stages + s * p.stage), sb = sa + a_bytes;
+                const uint32_t sa = smem_u32(stages + s * p.stage), sb = sa + deep * a_bytes;
                 const uint64_t da = smem_desc(sa, 8192), db = smem_desc(sb, 8192);
+                if (kMayBeDeep && deep > 1) {
+#pragma unroll
+                    for (int d = 0; d < kDeep; ++d)
+#pragma unroll
+                        for (int k = 0; k < BK / 16; ++k)
+                            mma_ss(tmem + half * BN, da + (d * a_bytes + 32 * k) / 16,
+                                   db + (d * S::kStageB + 32 * k) / 16, idesc, it | d | k);
+                    commit(empty + 8 * s);
+                    if (++s == p.stages) s = 0, phase ^= 1;
+                    continue;
+                }
 #pragma unroll
                 for (int k = 0; k < BK / 16; ++k) {
                     const uint64_t ka = da + (kAcrossA ? 128 * k : 2 * k), kb = db + (kAcrossB ? 128 * k : 2 * k);
@@ -409,21 +441,46 @@ struct LayOut {
     uint16_t* dst[4];
     int64_t ld[4], dld[4], rows[4], cols[4];
 };
+constexpr int kLayUnits = 4;  // units of eight values a thread moves at a time, loaded before any is stored
 __global__ void __launch_bounds__(256) lay_out_kernel(const __grid_constant__ LayOut l) {
     const int o = blockIdx.y;
-    const int64_t per = (l.cols[o] + 7) / 8, total = l.rows[o] * per, cols = l.cols[o];
-    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
-        const int64_t r = i / per, c = (i - r * per) * 8;
-        const uint16_t* src = l.src[o] + r * l.ld[o] + c;
-        uint16_t v[8];
+    const int64_t cols = l.cols[o], per = (cols + 7) / 8, total = l.rows[o] * per;
+    const int64_t threads = (int64_t)gridDim.x * 256;
+    for (int64_t i0 = (int64_t)blockIdx.x * 256 + threadIdx.x; i0 < total; i0 += kLayUnits * threads) {
+        uint32_t v[kLayUnits][5];
+        int odd[kLayUnits], left[kLayUnits];
+        uint16_t* dst[kLayUnits];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = c + j < cols ? src[j] : 0;
-        uint4 u;
-        u.x = v[0] | (uint32_t)v[1] << 16, u.y = v[2] | (uint32_t)v[3] << 16;
-        u.z = v[4] | (uint32_t)v[5] << 16, u.w = v[6] | (uint32_t)v[7] << 16;
-        *reinterpret_cast<uint4*>(l.dst[o] + r * l.dld[o] + c) = u;
+        for (int k = 0; k < kLayUnits; ++k) {
+            const int64_t i = i0 + k * threads;
+            left[k] = 0;
+            if (i >= total) continue;
+            const int64_t r = total <= UINT32_MAX ? (uint32_t)i / (uint32_t)per : i / per, c = (i - r * per) * 8;
+            // eight values out of the four or five 32-bit words that hold them
+            const uintptr_t at = reinterpret_cast<uintptr_t>(l.src[o] + r * l.ld[o] + c);
+            const uint32_t* word = reinterpret_cast<const uint32_t*>(at & ~(uintptr_t)3);
+            odd[k] = at >> 1 & 1, left[k] = (int)min((int64_t)8, cols - c);
+            dst[k] = l.dst[o] + r * l.dld[o] + c;
+#pragma unroll
+            for (int j = 0; j < 5; ++j) v[k][j] = 2 * j < left[k] + odd[k] ? word[j] : 0;
+        }
+#pragma unroll
+        for (int k = 0; k < kLayUnits; ++k) {
+            if (!left[k]) continue;
+            uint32_t u[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                u[j] = odd[k] ? __funnelshift_r(v[k][j], v[k][j + 1], 16) : v[k][j];
+                if (left[k] == 2 * j + 1) u[j] &= 0xffff;  // the word's other half is the next row's
+            }
+            *reinterpret_cast<uint4*>(dst[k]) = make_uint4(u[0], u[1], u[2], u[3]);
+        }
     }
 }
+
+// The row stride of what is laid out here: whole 128-byte lines, since copies
+// of 128 bytes a row that straddle lines took the products twice as long.
+int64_t laid_ld(int64_t cols) { return ceil_div(cols, 64) * 64; }
 
 // Whether bulk tensor copies read the operand as it is; a single row's
 // stride does not matter.
@@ -448,7 +505,7 @@ bool same(const GemmOperand& a, const GemmOperand& b) { return a.p == b.p && a.l
 
 // Adds the operand to `l` where copies do not take it as it is.
 void lay_out(GemmOperand& o, int64_t rows, int64_t cols, unsigned char*& ws, LayOut& l, int& n) {
-    const int64_t ld = ceil_div(cols, 8) * 8;
+    const int64_t ld = laid_ld(cols);
     if (copies_as_is(o, rows)) {
         if (rows == 1) o.ld = ld;
         return;
@@ -464,6 +521,13 @@ cudaError_t map_of(CUtensorMap* m, const GemmOperand& o, int dtype, int64_t rows
     const uint64_t dims[2] = {(uint64_t)cols, (uint64_t)rows}, strides[1] = {(uint64_t)o.ld * 2};
     const uint32_t box[2] = {64, (uint32_t)box_rows};
     return make_map(m, o.p, dtype, 2, dims, strides, box);
+}
+
+// The same operand as steps of 64 columns, several a copy.
+cudaError_t deep_map_of(CUtensorMap* m, const GemmOperand& o, int dtype, int64_t rows, int64_t cols, int box_rows) {
+    const uint64_t dims[3] = {64, (uint64_t)rows, (uint64_t)(cols / 64)}, strides[2] = {(uint64_t)o.ld * 2, 128};
+    const uint32_t box[3] = {64, (uint32_t)box_rows, kDeep};
+    return make_map(m, o.p, dtype, 3, dims, strides, box);
 }
 
 bool unit16(const void* p, int64_t ld, int size, int unit) {
@@ -492,9 +556,11 @@ cudaError_t run(const OpContext& x, const CUtensorMap (&a)[2], const CUtensorMap
     p.m_tiles = (int)ceil_div(p.g.M, S::kTileM);
     p.n_tiles = (int)ceil_div(p.g.N, kOut);
     p.tiles = (int64_t)p.m_tiles * p.n_tiles * (KIND == kGemmPair ? p.g.count : 1);
-    p.stage = (KIND == kGemmPair ? S::kStageA : p.a_rows * BK * 2) + S::kStageB;
-    // a product reads 128 rows of A wherever they start, so that many bytes lie after the last stage's
-    const int room = kRing - (S::kStageA + S::kStageB - p.stage);
+    const int a_bytes = KIND == kGemmPair ? S::kStageA : p.a_rows * BK * 2;
+    p.stage = p.deep * (a_bytes + S::kStageB);
+    // a product reads 128 rows of A wherever they start: they must end in the ring
+    const int past = (p.deep - 1) * a_bytes + S::kStageA - p.stage;
+    const int room = kRing - (past > 0 ? past : 0);
     p.stages = room / p.stage < kMaxStages ? room / p.stage : kMaxStages;
     auto* k = gemm_kernel<BN, KIND, PAIR>;
     static std::atomic<uint64_t> asked{0};
@@ -573,15 +639,17 @@ size_t gemm_scratch(const OpContext&, const GemmArgs& g) {
     const Plan pl = plan_of(g);
     size_t n = 0;
     for (int i = 0; i < pl.a_count; ++i)
-        if (!copies_as_is(g.a[i], pl.rows[0])) n += align256((size_t)pl.rows[0] * (ceil_div(pl.cols[0], 8) * 8) * 2);
+        if (!copies_as_is(g.a[i], pl.rows[0])) n += align256((size_t)pl.rows[0] * laid_ld(pl.cols[0]) * 2);
     for (int i = 0; i < pl.b_count; ++i)
-        if (!copies_as_is(g.b[i], pl.rows[1])) n += align256((size_t)pl.rows[1] * (ceil_div(pl.cols[1], 8) * 8) * 2);
+        if (!copies_as_is(g.b[i], pl.rows[1])) n += align256((size_t)pl.rows[1] * laid_ld(pl.cols[1]) * 2);
     return n;
 }
 
 cudaError_t launch_gemm(const OpContext& x, const GemmArgs& args, unsigned char* ws, cudaStream_t st) {
+    if (gemv_takes(args)) return launch_gemv(x, args, st);
     KernelArgs p{};
     p.g = args;
+    p.deep = 1;
     GemmArgs& g = p.g;
     const Plan pl = plan_of(g);
     p.steps = (int32_t)ceil_div(g.K, BK);
@@ -607,16 +675,20 @@ cudaError_t launch_gemm(const OpContext& x, const GemmArgs& args, unsigned char*
         if (n) {
             int64_t units = 0;
             for (int i = 0; i < n; ++i) units = l.rows[i] * l.dld[i] / 8 > units ? l.rows[i] * l.dld[i] / 8 : units;
-            const int64_t most = (int64_t)x.num_sms * 32;
-            const dim3 grid((unsigned)(ceil_div(units, 256) < most ? ceil_div(units, 256) : most), n);
+            const int64_t most = (int64_t)x.num_sms * 8, want = ceil_div(units, 256 * kLayUnits);
+            const dim3 grid((unsigned)(want < most ? want : most), n);
             lay_out_kernel<<<grid, 256, 0, st>>>(l);
             e = cudaGetLastError();
         }
+        // whole steps only: columns past the last would be the next row's
+        const bool few = g.M <= 64 && !tile.pair && tile.bn <= 64 && !across_b && g.K % BK == 0;
+        p.deep = few ? kDeep : 1;
+        auto map_a = few ? deep_map_of : map_of, map_b = few && g.kind == kGemmLinear ? deep_map_of : map_of;
         const int rows_b = tile.pair ? tile.bn / 2 : g.kind == kGemmGated ? tile.bn / 2 : tile.bn;
         for (int i = 0; e == cudaSuccess && i < pl.a_count; ++i)
-            e = map_of(&a[i], g.a[i], g.dtype, pl.rows[0], pl.cols[0], p.a_rows);
+            e = map_a(&a[i], g.a[i], g.dtype, pl.rows[0], pl.cols[0], p.a_rows);
         for (int i = 0; e == cudaSuccess && i < pl.b_count; ++i)
-            e = map_of(&b[i], g.b[i], g.dtype, pl.rows[1], pl.cols[1], across_b ? 64 : rows_b);
+            e = map_b(&b[i], g.b[i], g.dtype, pl.rows[1], pl.cols[1], across_b ? 64 : rows_b);
         if (e != cudaSuccess) return e;
     }
     switch (g.kind) {

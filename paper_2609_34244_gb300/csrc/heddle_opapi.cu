@@ -216,7 +216,7 @@ heddle_status heddle_linear_backward(heddle_ctx* ctx, const heddle_linear_grad_a
     ag.dy = a.dy, ag.lddy = a.lddy, ag.pre = a.pre, ag.ldp = a.ldp;
     ag.dbias = a.n ? a.dbias : nullptr;
     const bool own_dz = a.act != HEDDLE_ACT_NONE && (a.dx || a.dw);
-    ag.lddz = hd::ceil_div(a.n, 8) * 8;  // rows of whole 16-byte units for the products
+    ag.lddz = hd::ceil_div(a.n, 64) * 64;  // rows of whole 128-byte lines for the products
     const size_t dz_bytes = own_dz ? hd::align256((size_t)a.m * ag.lddz * 2) : 0;
 
     hd::GemmArgs gx{}, gw{};
@@ -301,7 +301,7 @@ heddle_status heddle_gated_ffn_backward(heddle_ctx* ctx, const heddle_gated_ffn_
     OpDeviceGuard guard(x->device);
     cudaStream_t st = (cudaStream_t)stream;
 
-    const int64_t ld = hd::ceil_div(a.n, 8) * 8;
+    const int64_t ld = hd::ceil_div(a.n, 64) * 64;  // rows of whole 128-byte lines for the products
     const size_t half = hd::align256((size_t)a.m * ld * 2);
     hd::GemmArgs gx{}, gw{};
     gx.M = a.m, gx.N = a.k, gx.K = a.n;

@@ -101,6 +101,12 @@ struct GemmArgs {
 size_t gemm_scratch(const OpContext& x, const GemmArgs& g);
 cudaError_t launch_gemm(const OpContext& x, const GemmArgs& g, unsigned char* ws, cudaStream_t st);
 
+// Forward products of up to kGemvRows rows in whole 16-byte units, without
+// the tensor cores (heddle_gemv.cu).
+constexpr int kGemvRows = 2;
+bool gemv_takes(const GemmArgs& g);
+cudaError_t launch_gemv(const OpContext& x, const GemmArgs& g, cudaStream_t st);
+
 // dz = dy act'(pre) (dz null: not written), partial column sums of it
 struct ActGradArgs {
     int64_t m, n;

@@ -162,16 +162,23 @@ __device__ __forceinline__ float inv_sqrt(float v) {
     return v > 0.0f && v < INFINITY ? r * fmaf(-0.5f * v * r, r, 1.5f) : r;
 }
 
+// What the kernel knows of a call beforehand.  kAny: nothing.  kHalves and
+// kPairs: every value is turned, in that layout, every lane of a group has
+// values, and all lies at whole units; two thirds of the instructions then
+// (16384 tokens of 72 heads of 128 bfloat16, forward: 186 us as kAny).
+enum RotaryCase { kAny, kHalves, kPairs };
+
 // A head of whole 16-byte units in a group of GL lanes, V values a lane, the
 // last lanes idle where head_dim / V is not GL.  A lane's values are two runs
 // of V / 2 that hold both values of every pair they turn: places i.. and
 // i + rot_dim / 2.., or 2i.., so that no value changes lanes.  A block takes
 // queries or keys alone (the first q_blocks queries); a group takes `chunk`
-// heads of one token at a time and keeps its angles.
-template <class T, int GL, bool GRAD>
+// heads of one token at a time and keeps its angles.  Sums and differences of
+// products are spelled out, so that every case rounds alike.
+template <class T, int GL, bool GRAD, RotaryCase CASE>
 __global__ void __launch_bounds__(256, 3)
     qk_norm_rope_wide_kernel(const __grid_constant__ heddle_qk_norm_rope_grad_args ga, float* partial, uint32_t* err,
-                             int q_blocks, int chunk, bool whole) {
+                             int q_blocks, int chunk, bool whole_units) {
     constexpr int V = 16 / sizeof(T), H = V / 2, kGroups = 256 / GL, kDepth = GRAD ? 2 : 4;
     const heddle_qk_norm_rope_args& a = ga.fwd;
     const bool is_q = blockIdx.x < q_blocks;
@@ -179,8 +186,9 @@ __global__ void __launch_bounds__(256, 3)
     const int heads = is_q ? a.q_heads : a.k_heads, chunks = (heads + chunk - 1) / chunk;
     const heddle_heads in = is_q ? a.q : a.k, out = is_q ? a.q_out : a.k_out, dst = is_q ? ga.dq : ga.dk;
     const int lane = threadIdx.x % GL, group = threadIdx.x / GL;
-    const int D = a.head_dim, rot = a.rot_dim;
-    const bool live = lane * V < D, turns = lane * V < rot, inter = a.interleaved;
+    const int D = CASE == kAny ? a.head_dim : GL * V, rot = CASE == kAny ? a.rot_dim : D;
+    const bool live = CASE != kAny || lane * V < D, turns = CASE != kAny || lane * V < rot;
+    const bool inter = CASE == kAny ? a.interleaved : CASE == kPairs, whole = CASE != kAny || whole_units;
     // the lane's two runs; lanes past the turned part hold V values in a row
     const int at0 = turns && !inter ? lane * H : lane * V, at1 = turns && !inter ? at0 + rot / 2 : at0 + H;
     const uint32_t mask = GL == 32 ? ~0u : ((1u << (GL & 31)) - 1) << (threadIdx.x % 32 / GL * GL);
@@ -198,65 +206,87 @@ __global__ void __launch_bounds__(256, 3)
     const int64_t units = a.tokens * chunks;
     for (int64_t u = (int64_t)block * kGroups + group; u < units; u += (int64_t)blocks * kGroups) {
         const int64_t t = u / chunks;
-        const int h0 = (int)(u - t * chunks) * chunk, h1 = min(heads, h0 + chunk);
+        const int h0 = (int)(u - t * chunks) * chunk, count = min(heads - h0, chunk);
         float cs[H], sn[H];
         bool bad = false;
         if (rot) {
             const int64_t p = a.positions[t];
             bad = p < 0 || p >= a.table_len;
-            if (bad && lane == 0) atomicOr(err, kErrOpPosition);
-            if (turns && !bad) {
-                const int64_t at = p * (rot / 2) + lane * H;
+            const int64_t at = (bad ? 0 : p) * (rot / 2) + lane * H;
+            if (bad) {
+                if (lane == 0) atomicOr(err, kErrOpPosition);
+            } else if (CASE != kAny) {
+#pragma unroll
+                for (int v = 0; v < H; v += 2) {
+                    const float2 c = *reinterpret_cast<const float2*>(a.cos + at + v),
+                                 s = *reinterpret_cast<const float2*>(a.sin + at + v);
+                    cs[v] = c.x, cs[v + 1] = c.y, sn[v] = s.x, sn[v + 1] = s.y;
+                }
+            } else if (turns) {
 #pragma unroll
                 for (int v = 0; v < H; ++v) cs[v] = a.cos[at + v], sn[v] = a.sin[at + v];
             }
         }
-        // the lane's pairs turned by the angles, back by their negatives
-        auto turn = [&](float (&v)[V], bool back) {
-            if (!turns || bad) return;
-#pragma unroll
-            for (int k = 0; k < H; ++k) {
-                const float s = back ? -sn[k] : sn[k];
-                if (inter) {
-                    const float x = v[2 * k], y = v[2 * k + 1];
-                    v[2 * k] = x * cs[k] - y * s;
-                    v[2 * k + 1] = y * cs[k] + x * s;
-                } else {
-                    const float x = v[k], y = v[H + k];
-                    v[k] = x * cs[k] - y * s;
-                    v[H + k] = y * cs[k] + x * s;
-                }
-            }
-        };
         const T* x_at = static_cast<const T*>(in.data) + t * in.token_stride + h0 * in.head_stride;
         const T* g_at = static_cast<const T*>(out.data) + t * out.token_stride + h0 * out.head_stride;
         T* y_at = GRAD ? static_cast<T*>(dst.data) + t * dst.token_stride + h0 * dst.head_stride
                        : static_cast<T*>(out.data) + t * out.token_stride + h0 * out.head_stride;
         const int64_t y_step = GRAD ? dst.head_stride : out.head_stride;
-        for (int h = h0; h < h1; h += kDepth) {
+        if (bad) {  // no such position: zeros
+            for (int h = 0; h < count; ++h)
+                if (live) {
+                    store_half(y_at + h * y_step + at0, make_uint2(0, 0), whole);
+                    store_half(y_at + h * y_step + at1, make_uint2(0, 0), whole);
+                }
+            continue;
+        }
+        // the lane's pairs turned by the angles, back by their negatives
+        auto turn = [&](float (&v)[V], bool back) {
+            if (!turns) return;
+            auto pair = [&](float& x, float& y, int k) {
+                const float s = back ? -sn[k] : sn[k], t = fmaf(x, cs[k], -__fmul_rn(y, s));
+                y = fmaf(y, cs[k], __fmul_rn(x, s));
+                x = t;
+            };
+            if (inter) {
+#pragma unroll
+                for (int k = 0; k < H; ++k) pair(v[2 * k], v[2 * k + 1], k);
+            } else {
+#pragma unroll
+                for (int k = 0; k < H; ++k) pair(v[k], v[H + k], k);
+            }
+        };
+        for (int h = 0; h < count; h += kDepth) {
+            // heads past the last are the last again, not stored
             uint2 x[kDepth][2], g[kDepth][2];
 #pragma unroll
-            for (int k = 0; k < kDepth; ++k)
-                if (live && h + k < h1) {
-                    x[k][0] = load_half(x_at + k * in.head_stride + at0, whole);
-                    x[k][1] = load_half(x_at + k * in.head_stride + at1, whole);
-                    if (GRAD) {
-                        g[k][0] = load_half(g_at + k * out.head_stride + at0, whole);
-                        g[k][1] = load_half(g_at + k * out.head_stride + at1, whole);
+            for (int k = 0; k < kDepth; ++k) {
+                const int at = min(k, count - 1 - h);
+                x[k][0] = x[k][1] = make_uint2(0, 0);
+                if (live) {
+                    x[k][0] = load_half(x_at + at * in.head_stride + at0, whole);
+                    x[k][1] = load_half(x_at + at * in.head_stride + at1, whole);
+                }
+                if (GRAD) {
+                    g[k][0] = g[k][1] = make_uint2(0, 0);
+                    if (live) {
+                        g[k][0] = load_half(g_at + at * out.head_stride + at0, whole);
+                        g[k][1] = load_half(g_at + at * out.head_stride + at1, whole);
                     }
                 }
+            }
 #pragma unroll
             for (int k = 0; k < kDepth; ++k) {
-                if (h + k >= h1) break;
+                const bool stored = h + k < count;
                 float v[V], ss = 0.0f;
 #pragma unroll
                 for (int i = 0; i < V; ++i) {
-                    v[i] = live ? to_float(reinterpret_cast<const T*>(&x[k][i / H])[i % H]) : 0.0f;
-                    ss += v[i] * v[i];
+                    v[i] = to_float(reinterpret_cast<const T*>(&x[k][i / H])[i % H]);
+                    ss = fmaf(v[i], v[i], ss);
                 }
 #pragma unroll
                 for (int o = GL / 2; o; o >>= 1) ss += __shfl_xor_sync(mask, ss, o, GL);
-                const float rstd = inv_sqrt(ss * inv_d + a.eps);
+                const float rstd = inv_sqrt(fmaf(ss, inv_d, a.eps));
                 float r[V];
                 if (!GRAD) {
 #pragma unroll
@@ -265,27 +295,26 @@ __global__ void __launch_bounds__(256, 3)
                 } else {
                     float dot = 0.0f;
 #pragma unroll
-                    for (int i = 0; i < V; ++i)
-                        r[i] = live ? to_float(reinterpret_cast<const T*>(&g[k][i / H])[i % H]) : 0.0f;
+                    for (int i = 0; i < V; ++i) r[i] = to_float(reinterpret_cast<const T*>(&g[k][i / H])[i % H]);
                     turn(r, true);
 #pragma unroll
                     for (int i = 0; i < V; ++i) {
+                        const float d = r[i];
                         v[i] *= rstd;
-                        if (!bad) dw[i] += r[i] * v[i];
-                        r[i] *= w[i];
-                        dot += r[i] * v[i];
+                        if (stored) dw[i] = fmaf(d, v[i], dw[i]);
+                        r[i] = d * w[i];
+                        dot = fmaf(r[i], v[i], dot);
                     }
 #pragma unroll
                     for (int o = GL / 2; o; o >>= 1) dot += __shfl_xor_sync(mask, dot, o, GL);
                     dot *= inv_d;
 #pragma unroll
-                    for (int i = 0; i < V; ++i) r[i] = rstd * (r[i] - v[i] * dot);
+                    for (int i = 0; i < V; ++i) r[i] = rstd * fmaf(-v[i], dot, r[i]);
                 }
-                if (live) {
+                if (live && stored) {
                     uint2 y[2];
 #pragma unroll
-                    for (int i = 0; i < V; ++i)
-                        reinterpret_cast<T*>(&y[i / H])[i % H] = from_float<T>(bad ? 0.0f : r[i]);
+                    for (int i = 0; i < V; ++i) reinterpret_cast<T*>(&y[i / H])[i % H] = from_float<T>(r[i]);
                     store_half(y_at + k * y_step + at0, y[0], whole);
                     store_half(y_at + k * y_step + at1, y[1], whole);
                 }
@@ -346,7 +375,7 @@ bool wide_takes(const heddle_qk_norm_rope_args& a) {
 bool whole_units(const heddle_qk_norm_rope_grad_args& g, bool grad) {
     const heddle_qk_norm_rope_args& a = g.fwd;
     const int size = elem_bytes(a.dtype);
-    return units8(a.q, a.q_heads, size) && units8(a.k, a.k_heads, size) && units8(a.q_out, a.q_heads, size) &&
+    return (uintptr_t)a.cos % 8 == 0 && (uintptr_t)a.sin % 8 == 0 && units8(a.q, a.q_heads, size) && units8(a.k, a.k_heads, size) && units8(a.q_out, a.q_heads, size) &&
            units8(a.k_out, a.k_heads, size) &&
            (!grad || (units8(g.dq, a.q_heads, size) && units8(g.dk, a.k_heads, size)));
 }
@@ -367,9 +396,11 @@ Launch plan_rows(const OpContext& x, const heddle_qk_norm_rope_grad_args& g, boo
     const int need = a.head_dim * elem_bytes(a.dtype) / 16;
     l.lanes = need <= 8 ? 8 : need <= 16 ? 16 : 32;
     const int groups = 256 / l.lanes;
-    // several heads a group once every SM has groups enough without
-    const int64_t each = ceil_div(a.q_heads, 8) + ceil_div(a.k_heads, 8);
-    l.chunk = a.tokens * each >= (int64_t)x.num_sms * groups * 3 ? 8 : 1;
+    // as many heads a group, up to eight, as leave every group that runs at a
+    // time four units of them
+    for (l.chunk = 8; l.chunk > 1; l.chunk /= 2)
+        if (a.tokens * (ceil_div(a.q_heads, l.chunk) + ceil_div(a.k_heads, l.chunk)) >= (int64_t)x.num_sms * groups * 12)
+            break;
     const int64_t q_want = ceil_div(a.tokens * ceil_div(a.q_heads, l.chunk), groups),
                   k_want = ceil_div(a.tokens * ceil_div(a.k_heads, l.chunk), groups);
     const int64_t most = (int64_t)x.num_sms * 6;  // two rounds of three blocks an SM
@@ -385,6 +416,23 @@ Launch plan_rows(const OpContext& x, const heddle_qk_norm_rope_grad_args& g, boo
     return l;
 }
 
+template <class T, int GL, bool GRAD>
+void launch_wide(const Launch& l, const OpContext& x, const heddle_qk_norm_rope_grad_args& a, float* partial,
+                 cudaStream_t st) {
+    const heddle_qk_norm_rope_args& f = a.fwd;
+    const int blocks = l.q_blocks + l.k_blocks;
+    const bool known = l.whole && f.rot_dim == f.head_dim && f.head_dim == GL * (int)(16 / sizeof(T));
+    if (!known)
+        qk_norm_rope_wide_kernel<T, GL, GRAD, kAny>
+            <<<blocks, 256, 0, st>>>(a, partial, x.err, l.q_blocks, l.chunk, l.whole);
+    else if (f.interleaved)
+        qk_norm_rope_wide_kernel<T, GL, GRAD, kPairs>
+            <<<blocks, 256, 0, st>>>(a, partial, x.err, l.q_blocks, l.chunk, l.whole);
+    else
+        qk_norm_rope_wide_kernel<T, GL, GRAD, kHalves>
+            <<<blocks, 256, 0, st>>>(a, partial, x.err, l.q_blocks, l.chunk, l.whole);
+}
+
 template <class T, bool GRAD>
 void launch_typed(const Launch& l, const OpContext& x, const heddle_qk_norm_rope_grad_args& a, float* partial,
                   cudaStream_t st) {
@@ -394,11 +442,11 @@ void launch_typed(const Launch& l, const OpContext& x, const heddle_qk_norm_rope
     else if (blocks == 0)
         return;
     else if (l.lanes == 8)
-        qk_norm_rope_wide_kernel<T, 8, GRAD><<<blocks, 256, 0, st>>>(a, partial, x.err, l.q_blocks, l.chunk, l.whole);
+        launch_wide<T, 8, GRAD>(l, x, a, partial, st);
     else if (l.lanes == 16)
-        qk_norm_rope_wide_kernel<T, 16, GRAD><<<blocks, 256, 0, st>>>(a, partial, x.err, l.q_blocks, l.chunk, l.whole);
+        launch_wide<T, 16, GRAD>(l, x, a, partial, st);
     else
-        qk_norm_rope_wide_kernel<T, 32, GRAD><<<blocks, 256, 0, st>>>(a, partial, x.err, l.q_blocks, l.chunk, l.whole);
+        launch_wide<T, 32, GRAD>(l, x, a, partial, st);
 }
 
 template <bool GRAD>

@@ -11,6 +11,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
 
 import numpy as np
 
@@ -133,6 +134,30 @@ class heddle_attention_args(C.Structure):
 class heddle_attention_grad_args(C.Structure):
     _fields_ = [("fwd", heddle_attention_args), ("d_o", heddle_heads), ("dq", heddle_heads), ("dk", heddle_heads),
                 ("dv", heddle_heads)]
+
+
+def _packer(cls):
+    """What packs a C struct's values, nested structs' in their place, into
+    bytes: a third of the time of filling the struct field by field."""
+    codes = {C.c_int64: "q", C.c_int32: "i", C.c_float: "f", C.c_void_p: "P"}
+
+    def flat(c):
+        return "".join(codes[t] if t in codes else flat(t) for _, t in c._fields_)
+
+    packed = struct.Struct("@" + flat(cls))
+    if packed.size != C.sizeof(cls):
+        raise TypeError("%s is not packed alike" % cls.__name__)
+    return packed.pack
+
+
+_pack_linear = _packer(heddle_linear_args)
+_pack_linear_grad = _packer(heddle_linear_grad_args)
+_pack_gated_ffn = _packer(heddle_gated_ffn_args)
+_pack_gated_ffn_grad = _packer(heddle_gated_ffn_grad_args)
+_pack_qk_norm_rope = _packer(heddle_qk_norm_rope_args)
+_pack_qk_norm_rope_grad = _packer(heddle_qk_norm_rope_grad_args)
+_pack_attention = _packer(heddle_attention_args)
+_pack_attention_grad = _packer(heddle_attention_grad_args)
 
 EXPORTS = ["heddle_create", "heddle_destroy", "heddle_last_error", "heddle_load_cluster",
            "heddle_load_model", "heddle_price_candidates", "heddle_topk_reset", "heddle_topk",
@@ -520,7 +545,7 @@ def _axes(what, t, axes):
 
 
 def _op_call(ctx, fn, args, device, stream):
-    st = fn(ctx, C.byref(args), _raw_stream(device) if stream is None else getattr(stream, "cuda_stream", stream))
+    st = fn(ctx, args, _raw_stream(device) if stream is None else getattr(stream, "cuda_stream", stream))
     if st:
         _check(ctx, st)
 
@@ -531,9 +556,9 @@ def _bad(what, t, shape, dtype):
 
 
 def _mat(what, t, shape, dtype, device):
-    """(address, row stride) of a [rows][cols] tensor; (None, 0) for None."""
+    """(address, row stride) of a [rows][cols] tensor; (0, 0) for None."""
     if t is None:
-        return None, 0
+        return 0, 0
     if t.dtype is not dtype or t.shape != shape or t.get_device() != device:
         _bad(what, t, shape, dtype)
     ld, inner = t.stride()
@@ -546,21 +571,21 @@ def _mat(what, t, shape, dtype, device):
 
 def _vec(what, t, n, dtype, device):
     if t is None:
-        return None
+        return 0
     if t.dtype is not dtype or t.shape != (n,) or t.get_device() != device or (n > 1 and t.stride(0) != 1):
         _bad(what, t, (n,), dtype)
     return t.data_ptr()
 
 
 def _heads(what, t, shape, dtype, device):
-    """heddle_heads of a [batch][tokens][heads][head_dim] tensor, or one
-    without the batch axis."""
+    """heddle_heads' values of a [batch][tokens][heads][head_dim] tensor, or
+    one without the batch axis."""
     if t.dtype is not dtype or t.shape != shape or t.get_device() != device:
         _bad(what, t, shape, dtype)
     st = t.stride()
     if st[-1] != 1 and shape[-1] > 1:
         _bad(what, t, shape, dtype)
-    return heddle_heads(t.data_ptr(), st[0] if len(st) == 4 else 0, st[-3], st[-2])
+    return t.data_ptr(), st[0] if len(st) == 4 else 0, st[-3], st[-2]
 
 
 def _same_stride(what, a, b):
@@ -574,7 +599,7 @@ def heddle_linear(ctx, x, w, y, bias=None, residual=None, act=ACT_NONE, pre=None
     (m, k), dt, code, dev = _first("x", x, 2)
     n = _axes("w", w, 2)[0]
     mn = (m, n)
-    a = heddle_linear_args(m, n, k, code, act, *_mat("x", x, (m, k), dt, dev), *_mat("w", w, (n, k), dt, dev),
+    a = _pack_linear(m, n, k, code, act, *_mat("x", x, (m, k), dt, dev), *_mat("w", w, (n, k), dt, dev),
                            _vec("bias", bias, n, dt, dev), *_mat("residual", residual, mn, dt, dev),
                            *_mat("y", y, mn, dt, dev), *_mat("pre", pre, mn, _torch.float32, dev))
     _op_call(ctx, load_library().heddle_linear, a, dev, stream)
@@ -585,7 +610,7 @@ def heddle_linear_backward(ctx, dy, x, w, act=ACT_NONE, pre=None, dx=None, dw=No
     (m, k), dt, code, dev = _first("x", x, 2)
     n = _axes("w", w, 2)[0]
     mn, mk, nk = (m, n), (m, k), (n, k)
-    a = heddle_linear_grad_args(m, n, k, code, act, *_mat("dy", dy, mn, dt, dev), *_mat("x", x, mk, dt, dev),
+    a = _pack_linear_grad(m, n, k, code, act, *_mat("dy", dy, mn, dt, dev), *_mat("x", x, mk, dt, dev),
                                 *_mat("w", w, nk, dt, dev), *_mat("pre", pre, mn, _torch.float32, dev),
                                 *_mat("dx", dx, mk, dt, dev), *_mat("dw", dw, nk, dt, dev),
                                 _vec("dbias", dbias, n, dt, dev))
@@ -598,7 +623,7 @@ def heddle_gated_ffn(ctx, x, w_gate, w_up, y, act=ACT_SILU, gate=None, up=None, 
     n = _axes("w_gate", w_gate, 2)[0]
     mn, nk, f32 = (m, n), (n, k), _torch.float32
     saved = _same_stride("gate and up", _mat("gate", gate, mn, f32, dev), _mat("up", up, mn, f32, dev))
-    a = heddle_gated_ffn_args(m, n, k, code, act, *_mat("x", x, (m, k), dt, dev),
+    a = _pack_gated_ffn(m, n, k, code, act, *_mat("x", x, (m, k), dt, dev),
                               *_mat("w_gate", w_gate, nk, dt, dev), *_mat("w_up", w_up, nk, dt, dev),
                               *_mat("y", y, mn, dt, dev), *saved)
     _op_call(ctx, load_library().heddle_gated_ffn, a, dev, stream)
@@ -613,7 +638,7 @@ def heddle_gated_ffn_backward(ctx, dy, x, w_gate, w_up, gate, up, act=ACT_SILU, 
     mn, mk, nk, f32 = (m, n), (m, k), (n, k), _torch.float32
     saved = _same_stride("gate and up", _mat("gate", gate, mn, f32, dev), _mat("up", up, mn, f32, dev))
     dw = _same_stride("dwg and dwu", _mat("dwg", dwg, nk, dt, dev), _mat("dwu", dwu, nk, dt, dev))
-    a = heddle_gated_ffn_grad_args(m, n, k, code, act, *_mat("dy", dy, mn, dt, dev), *_mat("x", x, mk, dt, dev),
+    a = _pack_gated_ffn_grad(m, n, k, code, act, *_mat("dy", dy, mn, dt, dev), *_mat("x", x, mk, dt, dev),
                                    *_mat("w_gate", w_gate, nk, dt, dev), *_mat("w_up", w_up, nk, dt, dev), *saved,
                                    *_mat("dx", dx, mk, dt, dev), *dw)
     _op_call(ctx, load_library().heddle_gated_ffn_backward, a, dev, stream)
@@ -624,7 +649,7 @@ def _norm_rope_args(q, k, wq, wk, q_out, k_out, positions, cos, sin, eps, interl
     t, hq, d = shape
     keys = (t, _axes("k", k, 3)[1], d)
     rot = table = 0
-    ptrs = (None, None, None)
+    ptrs = (0, 0, 0)
     if positions is not None:
         table, half = angles = _axes("cos", cos, 2)
         rot = 2 * half
@@ -632,10 +657,9 @@ def _norm_rope_args(q, k, wq, wk, q_out, k_out, positions, cos, sin, eps, interl
                 _mat("sin", sin, angles, _torch.float32, dev)[0])
         if not (cos.is_contiguous() and sin.is_contiguous()):
             raise HeddleError(E_ARG, "cos and sin are contiguous")
-    a = heddle_qk_norm_rope_args(t, table, hq, keys[1], d, rot, code, 1 if interleaved else 0, eps, 0,
-                                 _heads("q", q, shape, dt, dev), _heads("k", k, keys, dt, dev),
-                                 _vec("wq", wq, d, dt, dev), _vec("wk", wk, d, dt, dev), *ptrs,
-                                 _heads("q_out", q_out, shape, dt, dev), _heads("k_out", k_out, keys, dt, dev))
+    a = (t, table, hq, keys[1], d, rot, code, 1 if interleaved else 0, eps, 0, *_heads("q", q, shape, dt, dev),
+         *_heads("k", k, keys, dt, dev), _vec("wq", wq, d, dt, dev), _vec("wk", wk, d, dt, dev), *ptrs,
+         *_heads("q_out", q_out, shape, dt, dev), *_heads("k_out", k_out, keys, dt, dev))
     return a, shape, keys, dt, dev
 
 
@@ -644,7 +668,7 @@ def heddle_qk_norm_rope(ctx, q, k, wq, wk, q_out, k_out, positions=None, cos=Non
     """Norms and rotation of q and k ([tokens][heads][head_dim]); cos and sin
     are float32 [table_len][rot_dim / 2], no rotation without positions."""
     a, _, _, _, dev = _norm_rope_args(q, k, wq, wk, q_out, k_out, positions, cos, sin, eps, interleaved)
-    _op_call(ctx, load_library().heddle_qk_norm_rope, a, dev, stream)
+    _op_call(ctx, load_library().heddle_qk_norm_rope, _pack_qk_norm_rope(*a), dev, stream)
 
 
 def heddle_qk_norm_rope_backward(ctx, dq_out, dk_out, q, k, wq, wk, dq, dk, dwq, dwk, positions=None, cos=None,
@@ -653,8 +677,8 @@ def heddle_qk_norm_rope_backward(ctx, dq_out, dk_out, q, k, wq, wk, dq, dk, dwq,
     are float32 [head_dim]."""
     f, shape, keys, dt, dev = _norm_rope_args(q, k, wq, wk, dq_out, dk_out, positions, cos, sin, eps, interleaved)
     d, f32 = shape[2], _torch.float32
-    a = heddle_qk_norm_rope_grad_args(f, _heads("dq", dq, shape, dt, dev), _heads("dk", dk, keys, dt, dev),
-                                      _vec("dwq", dwq, d, f32, dev), _vec("dwk", dwk, d, f32, dev))
+    a = _pack_qk_norm_rope_grad(*f, *_heads("dq", dq, shape, dt, dev), *_heads("dk", dk, keys, dt, dev),
+                                _vec("dwq", dwq, d, f32, dev), _vec("dwk", dwk, d, f32, dev))
     _op_call(ctx, load_library().heddle_qk_norm_rope_backward, a, dev, stream)
 
 
@@ -667,11 +691,10 @@ def _attention_args(q, k, v, o, lse, q_lens, kv_lens, window, sinks, scale):
                             or not lse.is_contiguous()):
         _bad("lse", lse, (b, hq, tq), "float32")
     i32 = _torch.int32
-    a = heddle_attention_args(b, tq, tk, hq, hk, d, code, window, sinks, d ** -0.5 if scale is None else scale, 0,
-                              _heads("q", q, shape, dt, dev), _heads("k", k, keys, dt, dev),
-                              _heads("v", v, keys, dt, dev), _heads("o", o, shape, dt, dev),
-                              None if lse is None else lse.data_ptr(), _vec("q_lens", q_lens, b, i32, dev),
-                              _vec("kv_lens", kv_lens, b, i32, dev))
+    a = (b, tq, tk, hq, hk, d, code, window, sinks, d ** -0.5 if scale is None else scale, 0,
+         *_heads("q", q, shape, dt, dev), *_heads("k", k, keys, dt, dev), *_heads("v", v, keys, dt, dev),
+         *_heads("o", o, shape, dt, dev), 0 if lse is None else lse.data_ptr(), _vec("q_lens", q_lens, b, i32, dev),
+         _vec("kv_lens", kv_lens, b, i32, dev))
     return a, shape, keys, dt, dev
 
 
@@ -680,15 +703,15 @@ def heddle_attention(ctx, q, k, v, o, lse=None, q_lens=None, kv_lens=None, windo
     """Causal attention of q over k and v ([batch][tokens][heads][head_dim])
     with a sliding window (0: none) and sinks; scale None: head_dim ** -0.5."""
     a, _, _, _, dev = _attention_args(q, k, v, o, lse, q_lens, kv_lens, window, sinks, scale)
-    _op_call(ctx, load_library().heddle_attention, a, dev, stream)
+    _op_call(ctx, load_library().heddle_attention, _pack_attention(*a), dev, stream)
 
 
 def heddle_attention_backward(ctx, do, q, k, v, o, lse, dq, dk, dv, q_lens=None, kv_lens=None, window=0, sinks=0,
                               scale=None, stream=None):
     """Gradients of heddle_attention from ``do``, with its o and lse."""
     f, shape, keys, dt, dev = _attention_args(q, k, v, o, lse, q_lens, kv_lens, window, sinks, scale)
-    a = heddle_attention_grad_args(f, _heads("do", do, shape, dt, dev), _heads("dq", dq, shape, dt, dev),
-                                   _heads("dk", dk, keys, dt, dev), _heads("dv", dv, keys, dt, dev))
+    a = _pack_attention_grad(*f, *_heads("do", do, shape, dt, dev), *_heads("dq", dq, shape, dt, dev),
+                             *_heads("dk", dk, keys, dt, dev), *_heads("dv", dv, keys, dt, dev))
     _op_call(ctx, load_library().heddle_attention_backward, a, dev, stream)
 
 
