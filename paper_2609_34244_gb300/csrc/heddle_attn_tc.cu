@@ -91,8 +91,20 @@ struct Params {
     // the queries, the others in rest_parts; sums of parts as floats
     int32_t lead, lead_parts, rest_parts;
     float *part_dk, *part_dv;  // [slots][128][head_dim]
+    int32_t* sched;  // the next piece of work and the CTAs that are done, zero between launches
     uint32_t* err;
 };
+
+// Queries and keys of a sequence and how far positions are from query
+// indices, in 32 bits: lengths here are at most 2^30.
+struct Seq {
+    int ql, kl, off;
+};
+constexpr int64_t kMaxLength = 1 << 30;
+__device__ __forceinline__ Seq seq_of(const heddle_attention_args& a, int64_t b) {
+    const Span s = span_of(a, b);
+    return {(int)s.ql, (int)s.kl, (int)s.off};
+}
 
 // The key tiles that a range of queries sees: those of the first tokens ahead
 // of the window's, then the window's.
@@ -100,40 +112,38 @@ struct KeyTiles {
     int lead, first, count;  // lead tiles from 0, then from `first` on; count of both
     __device__ int at(int j) const { return j < lead ? j : first + j - lead; }
 };
-__device__ __forceinline__ KeyTiles key_tiles(const Params& p, const Span& s, int64_t i0, int64_t i1) {
+__device__ __forceinline__ KeyTiles key_tiles(const Params& p, const Seq& s, int i0, int i1) {
     KeyTiles k{0, 0, 0};
     i1 = min(i1, s.ql);
     if (i0 >= i1) return k;
-    const int64_t hi = min(s.off + i1 - 1, s.kl - 1);
+    const int hi = min(s.off + i1 - 1, s.kl - 1);
     if (hi < 0) return k;
-    int64_t lo = 0;
-    if (p.a.window) lo = max((int64_t)0, s.off + i0 - p.a.window + 1);
-    k.first = (int)(lo / kTile);
-    const int last = (int)(hi / kTile);
-    const int64_t sinks = min(p.a.sinks, hi + 1);
-    k.lead = min((int)((sinks + kTile - 1) / kTile), k.first);
-    k.count = k.lead + last - k.first + 1;
+    const int lo = p.a.window ? max(0, max(0, s.off + i0) - (int)p.a.window + 1) : 0;
+    k.first = lo / kTile;
+    const int sinks = min((int)p.a.sinks, hi + 1);
+    k.lead = min((sinks + kTile - 1) / kTile, k.first);
+    k.count = k.lead + hi / kTile - k.first + 1;
     return k;
 }
 
 // What the query at a position sees; positions below -1 see nothing either.
 struct RowMask {
     int pos, low, sinks;
-    __device__ RowMask(int64_t at, const heddle_attention_args& a)
-        : pos((int)max(at, (int64_t)-1)), low(a.window ? pos - (int)a.window + 1 : INT32_MIN), sinks((int)a.sinks) {}
+    __device__ RowMask(int at, const heddle_attention_args& a)
+        : pos(max(at, -1)), low(a.window ? pos - (int)a.window + 1 : INT32_MIN), sinks((int)a.sinks) {}
     __device__ bool sees(int key) const { return key <= pos && (key >= low || key < sinks); }
 };
 
 // Every query of tokens i0 .. i1 - 1 sees every key of the tile at k0.
-__device__ __forceinline__ bool all_visible(const Params& p, const Span& s, int64_t i0, int64_t i1, int64_t k0) {
-    return s.off + i0 >= k0 + kTile - 1 &&
-           (p.a.window == 0 || s.off + i1 - 1 - k0 < p.a.window || k0 + kTile <= p.a.sinks);
+__device__ __forceinline__ bool all_visible(const Params& p, const Seq& s, int i0, int i1, int k0) {
+    return s.off + i0 >= k0 + kTile - 1 && (p.a.window == 0 || s.off + i1 - 1 - k0 < (int)p.a.window ||
+                                            k0 + kTile <= (int)p.a.sinks);
 }
 
 // Rows [from, 128) of a tile in shared memory to zero, a row a thread; the
 // products read them after the next barrier.
 template <int DP>
-__device__ __forceinline__ void clear_rows(unsigned char* tile, int row, int64_t from) {
+__device__ __forceinline__ void clear_rows(unsigned char* tile, int row, int from) {
     if (row >= from)
 #pragma unroll
         for (int h = 0; h < DP / 64; ++h)
@@ -162,15 +172,15 @@ __device__ __forceinline__ void mma_rows(uint32_t d, uint32_t w, uint32_t b, uin
 
 template <int DP>
 __device__ __forceinline__ void load_q_tile(uint32_t dst, const CUtensorMap* m, uint32_t bar, const Params& p,
-                                            int64_t t0, int hk, int b) {
+                                            int t0, int hk, int b) {
 #pragma unroll
-    for (int h = 0; h < DP / 64; ++h) load_4d(dst + h * 16384, m, bar, h * 64, hk * p.group, (int)t0, b);
+    for (int h = 0; h < DP / 64; ++h) load_4d(dst + h * 16384, m, bar, h * 64, hk * p.group, t0, b);
 }
 template <int DP>
-__device__ __forceinline__ void load_kv_tile(uint32_t dst, const CUtensorMap* m, uint32_t bar, int64_t k0, int hk,
+__device__ __forceinline__ void load_kv_tile(uint32_t dst, const CUtensorMap* m, uint32_t bar, int k0, int hk,
                                              int b) {
 #pragma unroll
-    for (int h = 0; h < DP / 64; ++h) load_4d(dst + h * 16384, m, bar, h * 64, hk, (int)k0, b);
+    for (int h = 0; h < DP / 64; ++h) load_4d(dst + h * 16384, m, bar, h * 64, hk, k0, b);
 }
 
 // One row of DP sums times f from tensor memory to memory: 16 bytes at a time
@@ -241,6 +251,38 @@ struct Forward {
     static constexpr int kCols = NT * (kTile + DP) <= 256 ? 256 : 512;
 };
 
+// A piece of the forward pass: NT query tiles of a key head and the steps
+// j0 .. j0 + n - 1 of the key tiles they see, tile q those before to[q].
+template <int NT>
+struct ForwardPiece {
+    int hk, b, split, t0;
+    Seq s;
+    KeyTiles keys;
+    int j0, n, to[NT];
+    __device__ ForwardPiece(const Params& p, int id) {
+        split = id % p.splits;
+        id /= p.splits;
+        hk = id % p.a.kv_heads;
+        id /= p.a.kv_heads;
+        b = id % (int)p.a.batch;
+        // the last queries see the most keys: their tiles come first
+        t0 = ((p.q_tiles + NT - 1) / NT - 1 - id / (int)p.a.batch) * NT * p.tokens;
+        s = seq_of(p.a, b);
+        keys = key_tiles(p, s, t0, t0 + NT * p.tokens);
+        j0 = (int)((int64_t)keys.count * split / p.splits);
+        const int j1 = (int)((int64_t)keys.count * (split + 1) / p.splits);
+        n = 0;
+#pragma unroll
+        for (int q = 0; q < NT; ++q) {
+            const KeyTiles own = key_tiles(p, s, t0 + q * p.tokens, t0 + (q + 1) * p.tokens);
+            to[q] = j0;
+            // the last of its tiles in the common order; the first ones are common to all
+            if (own.count) to[q] = max(j0, min(j1, keys.lead + own.first + own.count - own.lead - keys.first));
+            n = max(n, to[q] - j0);
+        }
+    }
+};
+
 template <class T, int DP, int NT>
 __global__ void __launch_bounds__(Forward<DP, NT>::kThreads, 1)
     attn_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUtensorMap mk,
@@ -257,32 +299,11 @@ __global__ void __launch_bounds__(Forward<DP, NT>::kThreads, 1)
     float* highs = reinterpret_cast<float*>(reinterpret_cast<unsigned char*>(bars) + 512);  // [2][NT][2][128]
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
 
-    // the last queries see the most keys: their tiles start first
-    const int heads = p.a.kv_heads;
-    int64_t id = blockIdx.x;
-    const int split = (int)(id % p.splits);
-    id /= p.splits;
-    const int hk = (int)(id % heads);
-    id /= heads;
-    const int b = (int)(id % p.a.batch);
-    const int block = (int)((p.q_tiles + NT - 1) / NT - 1 - id / p.a.batch);
-    const Span s = span_of(p.a, b);
-    const int64_t t0 = (int64_t)block * NT * p.tokens;
-    const KeyTiles keys = key_tiles(p, s, t0, t0 + NT * p.tokens);
-    const int j0 = (int)((int64_t)keys.count * split / p.splits),
-              j1 = (int)((int64_t)keys.count * (split + 1) / p.splits);
-    // each tile's own first and last visible tile among them
-    int from[NT], to[NT];
-#pragma unroll
-    for (int q = 0; q < NT; ++q) {
-        const KeyTiles own = key_tiles(p, s, t0 + q * p.tokens, t0 + (q + 1) * p.tokens);
-        from[q] = to[q] = j0;
-        // the window's tiles of its own in the common order; leading tiles are common to both
-        if (own.count) {
-            const int last = keys.lead + own.first + own.count - own.lead - 1 - keys.first;
-            to[q] = max(j0, min(j1, last + 1));
-        }
-    }
+    const ForwardPiece<NT> w(p, blockIdx.x);
+    const Seq& s = w.s;
+    const KeyTiles& keys = w.keys;
+    const int (&to)[NT] = w.to;
+    const int j0 = w.j0, n = w.n, t0 = w.t0, hk = w.hk, b = w.b, split = w.split;
 
     if (threadIdx.x == 0) {
         for (int i = 0; i < F::kSlots; ++i) {
@@ -304,16 +325,11 @@ __global__ void __launch_bounds__(Forward<DP, NT>::kThreads, 1)
     __syncthreads();
     fence_after();
     const uint32_t tmem = *tmem_at;
-    int last_to = j0;
-#pragma unroll
-    for (int q = 0; q < NT; ++q) last_to = max(last_to, to[q]);
-    const int n = last_to - j0;
-
     if (warp == 0 && n > 0 && elect_one()) {
         const uint32_t q_bytes = p.group * p.tokens * DP * 2;
 #pragma unroll
         for (int q = 0; q < NT; ++q)
-            if (to[q] > from[q]) {
+            if (to[q] > j0) {
                 mbar_expect(q_full + 8 * q, q_bytes);
                 load_q_tile<DP>(smem_u32(base + q * F::kTileBytes), &mq, q_full + 8 * q, p, t0 + q * p.tokens, hk, b);
             }
@@ -322,7 +338,7 @@ __global__ void __launch_bounds__(Forward<DP, NT>::kThreads, 1)
             if (!mbar_wait(empty + 8 * slot, (i / F::kSlots & 1) ^ 1, gave_up)) break;
             mbar_expect(full + 8 * slot, F::kTileBytes);
             load_kv_tile<DP>(smem_u32(ring + slot * F::kTileBytes), i & 1 ? &mv : &mk, full + 8 * slot,
-                             (int64_t)keys.at(j0 + i / 2) * kTile, hk, b);
+                             keys.at(j0 + i / 2) * kTile, hk, b);
         }
     } else if (warp == 1 && n > 0 && elect_one()) {
         const uint32_t bf = p.a.dtype == HEDDLE_BF16;
@@ -359,9 +375,8 @@ __global__ void __launch_bounds__(Forward<DP, NT>::kThreads, 1)
         const uint32_t lanes = (uint32_t)(warp % 4 * 32) << 16;
         const uint32_t ts = tmem + lanes + q * kTile, to_acc = tmem + lanes + NT * kTile + q * DP;
         const uint32_t pair = met + 8 * (q * 4 + warp % 4);  // this warp and the one of the rows' other half
-        const int64_t i0 = t0 + (int64_t)q * p.tokens, i1 = i0 + p.tokens;
-        const int64_t i = i0 + row / p.group;
-        const int64_t h = (int64_t)hk * p.group + row % p.group;
+        const int i0 = t0 + q * p.tokens, i1 = i0 + p.tokens;
+        const int i = i0 + row / p.group, h = hk * p.group + row % p.group;
         const RowMask mask(s.off + i, p.a);
         const float c = p.scale_log2;
         float top = -INFINITY, sum = 0.0f;
@@ -516,6 +531,52 @@ __global__ void __launch_bounds__(256) attn_join_kernel(const __grid_constant__ 
 
 // ------------------------------------------------------------------ backward
 
+// A kernel's CTAs stay and take one piece of work after another, so that a
+// piece's first loads and products run under the end of the one before it.
+// The producer takes the next number from memory a piece ahead and hands it
+// to the other warps through two places in shared memory.
+struct Pieces {
+    uint32_t full, empty;  // two barriers each
+    volatile int* place;
+    __device__ void init(int readers) const {
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(full + 8 * i, 1);
+            mbar_init(empty + 8 * i, readers);
+        }
+    }
+    // the producer's: hands out piece `it`, the id-th, or -1 for the end
+    __device__ bool put(int it, int id, volatile uint32_t* gave_up) const {
+        if (!mbar_wait(empty + 8 * (it & 1), (it >> 1 & 1) ^ 1, gave_up)) return false;
+        place[it & 1] = id;
+        mbar_arrive(full + 8 * (it & 1));
+        return true;
+    }
+    // a single thread's
+    __device__ int get(int it, volatile uint32_t* gave_up) const {
+        if (!mbar_wait(full + 8 * (it & 1), it >> 1 & 1, gave_up)) return -1;
+        const int id = place[it & 1];
+        mbar_arrive(empty + 8 * (it & 1));
+        return id;
+    }
+    // a warp's
+    __device__ int get_warp(int it, volatile uint32_t* gave_up) const {
+        if (!__all_sync(~0u, mbar_wait(full + 8 * (it & 1), it >> 1 & 1, gave_up))) return -1;
+        const int id = place[it & 1];
+        __syncwarp();
+        if (threadIdx.x % 32 == 0) mbar_arrive(empty + 8 * (it & 1));
+        return id;
+    }
+};
+// The last CTA to end leaves the numbers as the next launch needs them.
+__device__ __forceinline__ void leave_pieces(int32_t* sched) {
+    __threadfence();
+    if (atomicAdd(sched + 1, 1) == (int)gridDim.x - 1) {
+        sched[0] = 0;
+        sched[1] = 0;
+        __threadfence();
+    }
+}
+
 // Sixteen warps turn scores into dS, four for every quarter of a tile's
 // columns: with eight, each scheduler's two warps left it idle two thirds of
 // the time.
@@ -523,12 +584,13 @@ constexpr int kGradWarps = 16, kGradThreads = 128 + 32 * kGradWarps;
 
 // Bars of a backward kernel, in the order that follows its tiles.
 struct GradBars {
-    uint32_t held, full, full2, empty, a_full, b_full, a_ready, b_ready, stats, done;
+    uint32_t held, full, full2, empty, a_full, b_full, a_ready, b_ready, stats, done, held_free, work;
     __device__ explicit GradBars(uint32_t at)
         : held(at), full(at + 8), full2(at + 24), empty(at + 40), a_full(at + 56), b_full(at + 64), a_ready(at + 72),
-          b_ready(at + 80), stats(at + 96), done(at + 104) {}
+          b_ready(at + 80), stats(at + 96), done(at + 104), held_free(at + 112), work(at + 120) {}
     __device__ void init() const {
         mbar_init(held, 1);
+        mbar_init(held_free, 1);
         for (int i = 0; i < 2; ++i) {
             mbar_init(full + 8 * i, 1);
             mbar_init(full2 + 8 * i, 1);
@@ -543,7 +605,7 @@ struct GradBars {
         mbar_init(done, 1);
     }
 };
-constexpr int kGradBarBytes = 128;
+constexpr int kGradBarBytes = 160;
 
 // dq of a query tile: dq = scale sum over key tiles of dS K with
 // S = Q K^T, dP = dO V^T, dS = P (dP - delta).  Q and dO stay in shared
@@ -560,29 +622,35 @@ template <class T, int DP>
 __global__ void __launch_bounds__(kGradThreads, 1)
     attn_dq_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUtensorMap mk,
                    const __grid_constant__ CUtensorMap mv, const __grid_constant__ CUtensorMap mdo,
-                   const __grid_constant__ Params p) {
+                   const __grid_constant__ Params p, const int pieces) {
     using G = GradShape<DP>;
     extern __shared__ unsigned char raw[];
     unsigned char* base = raw + ((1024 - (smem_u32(raw) & 1023)) & 1023);
     unsigned char *sq = base, *sdo = base + G::kTileBytes, *stage = base + 2 * G::kTileBytes;  // K, V, K, V
     unsigned char* tail = base + 6 * G::kTileBytes;
     const GradBars bar(smem_u32(tail));
-    volatile uint32_t* gave_up = reinterpret_cast<uint32_t*>(tail + kGradBarBytes);
+    const Pieces work{bar.work, bar.work + 16, reinterpret_cast<int*>(tail + kGradBarBytes)};
+    volatile uint32_t* gave_up = reinterpret_cast<uint32_t*>(tail + kGradBarBytes + 8);
     uint32_t* tmem_at = const_cast<uint32_t*>(gave_up) + 1;
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
 
-    int64_t id = blockIdx.x;
-    const int hk = (int)(id % p.a.kv_heads);
-    id /= p.a.kv_heads;
-    const int b = (int)(id % p.a.batch);
-    const int block = (int)(p.q_tiles - 1 - id / p.a.batch);
-    const Span s = span_of(p.a, b);
-    const int64_t t0 = (int64_t)block * p.tokens, t1 = min(t0 + p.tokens, s.ql);
-    const KeyTiles keys = key_tiles(p, s, t0, t0 + p.tokens);
-    const int n = keys.count;
-
+    struct Piece {
+        int hk, b, t0, t1;
+        Seq s;
+        KeyTiles keys;
+        __device__ Piece(const Params& p, int id) {
+            hk = id % p.a.kv_heads;
+            id /= p.a.kv_heads;
+            b = id % (int)p.a.batch;
+            t0 = (p.q_tiles - 1 - id / (int)p.a.batch) * p.tokens;
+            s = seq_of(p.a, b);
+            t1 = min(t0 + p.tokens, s.ql);
+            keys = key_tiles(p, s, t0, t0 + p.tokens);
+        }
+    };
     if (threadIdx.x == 0) {
         bar.init();
+        work.init(1 + kGradWarps);
         *gave_up = 0;
         mbar_fence_init();
     }
@@ -593,105 +661,145 @@ __global__ void __launch_bounds__(kGradThreads, 1)
     const uint32_t tmem = *tmem_at;
     const uint32_t at_s = tmem, at_dp = tmem + 128, at_dq = tmem + 256, at_ds = tmem + 256 + DP;  // two of 64 columns
 
-    if (warp == 0 && n > 0 && elect_one()) {
-        mbar_expect(bar.held, 2 * p.group * p.tokens * DP * 2);
-        load_q_tile<DP>(smem_u32(sq), &mq, bar.held, p, t0, hk, b);
-        load_q_tile<DP>(smem_u32(sdo), &mdo, bar.held, p, t0, hk, b);
-        for (int j = 0; j < n; ++j) {
-            const int st = j & 1;
-            if (!mbar_wait(bar.empty + 8 * st, (j / 2 & 1) ^ 1, gave_up)) break;
-            mbar_expect(bar.full + 8 * st, 2 * G::kTileBytes);
-            const int64_t k0 = (int64_t)keys.at(j) * kTile;
-            load_kv_tile<DP>(smem_u32(stage + 2 * st * G::kTileBytes), &mk, bar.full + 8 * st, k0, hk, b);
-            load_kv_tile<DP>(smem_u32(stage + (2 * st + 1) * G::kTileBytes), &mv, bar.full + 8 * st, k0, hk, b);
+    if (warp == 0 && elect_one()) {
+        int id = blockIdx.x;
+        uint32_t step = 0, held = 0;  // key tiles so far; query tiles so far
+        bool go = true;
+        for (int it = 0; go; ++it) {
+            if (!work.put(it, id < pieces ? id : -1, gave_up) || id >= pieces) break;
+            const Piece w(p, id);
+            id = (int)gridDim.x + atomicAdd(p.sched, 1);
+            if (!w.keys.count) continue;
+            if (!(go = mbar_wait(bar.held_free, (held & 1) ^ 1, gave_up))) break;
+            ++held;
+            mbar_expect(bar.held, 2 * p.group * p.tokens * DP * 2);
+            load_q_tile<DP>(smem_u32(sq), &mq, bar.held, p, w.t0, w.hk, w.b);
+            load_q_tile<DP>(smem_u32(sdo), &mdo, bar.held, p, w.t0, w.hk, w.b);
+            for (int j = 0; j < w.keys.count; ++j, ++step) {
+                const uint32_t st = step & 1;
+                if (!(go = mbar_wait(bar.empty + 8 * st, (step / 2 & 1) ^ 1, gave_up))) break;
+                mbar_expect(bar.full + 8 * st, 2 * G::kTileBytes);
+                const int k0 = w.keys.at(j) * kTile;
+                load_kv_tile<DP>(smem_u32(stage + 2 * st * G::kTileBytes), &mk, bar.full + 8 * st, k0, w.hk, w.b);
+                load_kv_tile<DP>(smem_u32(stage + (2 * st + 1) * G::kTileBytes), &mv, bar.full + 8 * st, k0, w.hk,
+                                 w.b);
+            }
         }
-    } else if (warp == 1 && n > 0 && elect_one()) {
+    } else if (warp == 1 && elect_one()) {
         const uint32_t bf = p.a.dtype == HEDDLE_BF16;
         const uint32_t id_s = instr_desc(bf, false, false, kTile), id_d = instr_desc(bf, false, true, DP);
-        bool go = mbar_wait(bar.held, 0, gave_up);
-        for (int j = -1; go && j < n; ++j) {
-            if (j + 1 < n) {
-                const int st = (j + 1) & 1;
-                if (!(go = mbar_wait(bar.full + 8 * st, (j + 1) / 2 & 1, gave_up))) break;
-                if (j >= 0 && !(go = mbar_wait(bar.a_ready, j & 1, gave_up))) break;  // scores of step j are read
-                fence_after();
-                mma_dims<DP>(at_s, smem_u32(sq), smem_u32(stage + 2 * st * G::kTileBytes), id_s);
-                mma_dims<DP>(at_dp, smem_u32(sdo), smem_u32(stage + (2 * st + 1) * G::kTileBytes), id_s);
-                commit(bar.a_full);
+        uint32_t step = 0, held = 0;
+        bool go = true;
+        for (int it = 0; go; ++it) {
+            const int id = work.get(it, gave_up);
+            if (id < 0) break;
+            const int n = Piece(p, id).keys.count;
+            if (!n) continue;
+            if (!(go = mbar_wait(bar.held, held & 1, gave_up))) break;
+            ++held;
+            for (int j = -1; go && j < n; ++j) {
+                const uint32_t g = step + j;  // this step among all; scores run one ahead
+                if (j + 1 < n) {
+                    const uint32_t st = (g + 1) & 1;
+                    if (!(go = mbar_wait(bar.full + 8 * st, (g + 1) / 2 & 1, gave_up))) break;
+                    if (g + 1 > 0 && !(go = mbar_wait(bar.a_ready, g & 1, gave_up))) break;  // the last scores are read
+                    fence_after();
+                    mma_dims<DP>(at_s, smem_u32(sq), smem_u32(stage + 2 * st * G::kTileBytes), id_s);
+                    mma_dims<DP>(at_dp, smem_u32(sdo), smem_u32(stage + (2 * st + 1) * G::kTileBytes), id_s);
+                    commit(bar.a_full);
+                    if (j + 2 == n) commit(bar.held_free);
+                }
+                if (j >= 0) {
+                    const uint32_t st = g & 1;
+                    if (!(go = mbar_wait(bar.b_ready + 8 * st, g / 2 & 1, gave_up))) break;
+                    fence_after();
+                    mma_rows<64, 64>(at_dq, at_ds + 64 * st, smem_u32(stage + 2 * st * G::kTileBytes), id_d, j > 0);
+                    commit(bar.empty + 8 * st);
+                }
             }
-            if (j >= 0) {
-                const int st = j & 1;
-                if (!(go = mbar_wait(bar.b_ready + 8 * st, j / 2 & 1, gave_up))) break;
-                fence_after();
-                mma_rows<64, 64>(at_dq, at_ds + 64 * st, smem_u32(stage + 2 * st * G::kTileBytes), id_d, j > 0);
-                commit(bar.empty + 8 * st);
-            }
+            if (go) commit(bar.done);
+            step += n;
         }
-        if (go) commit(bar.done);
     } else if (warp >= 4) {
         const int side = (warp - 4) / 4, row = (warp % 4) * 32 + lane;  // which 32 of a tile's 128 keys
         const uint32_t lanes = (uint32_t)(warp % 4 * 32) << 16;
-        const int64_t i = t0 + row / p.group, h = (int64_t)hk * p.group + row % p.group;
-        const bool inside = row < p.group * p.tokens && i < p.a.q_len;
-        const int64_t r = ((int64_t)b * p.a.q_heads + h) * p.a.q_len + i;
-        const RowMask mask(i < s.ql ? s.off + i : -1, p.a);
-        float lse = inside ? p.a.lse[r] : INFINITY;
-        lse = lse == -INFINITY ? INFINITY : lse * kLog2e;  // weights of a row that sees nothing are zero
-        const float delta = inside ? p.delta[r] : 0.0f, c = p.scale_log2;
-        const uint64_t c2 = two(c, c), lse2 = two(-lse, -lse), delta2 = two(-delta, -delta);
+        const int i_row = row / p.group, h_row = row % p.group;
+        const float c = p.scale_log2;
+        const uint64_t c2 = two(c, c);
+        uint32_t step = 0, held = 0;
         bool go = true;
-        for (int j = 0; j < n; ++j) {
-            const int64_t k0 = (int64_t)keys.at(j) * kTile;
-            const bool whole = t0 + p.tokens <= s.ql && all_visible(p, s, t0, t1, k0);
-            if (!(go = __all_sync(~0u, mbar_wait(bar.a_full, j & 1, gave_up)))) break;
-            fence_after();
-            uint32_t v[32], d[32], w[16];
-            tmem_ld32(at_s + lanes + side * 32, v);
-            tmem_ld32(at_dp + lanes + side * 32, d);
-            wait_ld();
-            fence_before();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(bar.a_ready);
-#pragma unroll
-            for (int y = 0; y < 32; y += 2) {
-                const float2 z = apart(fma_two(two(v[y], v[y + 1]), c2, lse2));
-                v[y] = __float_as_uint(exp2_fast(z.x)), v[y + 1] = __float_as_uint(exp2_fast(z.y));
-            }
-            if (whole) {
+        for (int it = 0; go; ++it) {
+            const int id = work.get_warp(it, gave_up);
+            if (id < 0) break;
+            const Piece w(p, id);
+            const Seq& s = w.s;
+            const int n = w.keys.count;
+            const int i = w.t0 + i_row, h = w.hk * p.group + h_row;
+            const bool inside = row < p.group * p.tokens && i < p.a.q_len;
+            const int64_t r = ((int64_t)w.b * p.a.q_heads + h) * p.a.q_len + i;
+            const RowMask mask(i < s.ql ? s.off + i : -1, p.a);
+            float lse = inside ? p.a.lse[r] : INFINITY;
+            lse = lse == -INFINITY ? INFINITY : lse * kLog2e;  // weights of a row that sees nothing are zero
+            const float delta = inside ? p.delta[r] : 0.0f;
+            const uint64_t lse2 = two(-lse, -lse), delta2 = two(-delta, -delta);
+            for (int j = 0; j < n; ++j, ++step) {
+                const uint32_t st = step & 1;
+                const int k0 = w.keys.at(j) * kTile;
+                const bool whole = w.t0 + p.tokens <= s.ql && all_visible(p, s, w.t0, w.t1, k0);
+                if (!(go = __all_sync(~0u, mbar_wait(bar.a_full, st, gave_up)))) break;
+                fence_after();
+                uint32_t v[32], d[32], u[16];
+                tmem_ld32(at_s + lanes + side * 32, v);
+                tmem_ld32(at_dp + lanes + side * 32, d);
+                wait_ld();
+                fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(bar.a_ready);
 #pragma unroll
                 for (int y = 0; y < 32; y += 2) {
-                    const float2 z = apart(mul_two(two(v[y], v[y + 1]), add_two(two(d[y], d[y + 1]), delta2)));
-                    d[y] = __float_as_uint(z.x), d[y + 1] = __float_as_uint(z.y);
+                    const float2 z = apart(fma_two(two(v[y], v[y + 1]), c2, lse2));
+                    v[y] = __float_as_uint(exp2_fast(z.x)), v[y + 1] = __float_as_uint(exp2_fast(z.y));
                 }
-            } else {
-                // a product with what lies in hidden places must not count
+                if (whole) {
 #pragma unroll
-                for (int y = 0; y < 32; ++y) {
-                    const float e = mask.sees((int)k0 + side * 32 + y) ? __uint_as_float(v[y]) : 0.0f;
-                    d[y] = __float_as_uint(e == 0.0f ? 0.0f : e * (__uint_as_float(d[y]) - delta));
+                    for (int y = 0; y < 32; y += 2) {
+                        const float2 z = apart(mul_two(two(v[y], v[y + 1]), add_two(two(d[y], d[y + 1]), delta2)));
+                        d[y] = __float_as_uint(z.x), d[y + 1] = __float_as_uint(z.y);
+                    }
+                } else {
+                    // a product with what lies in hidden places must not count
+#pragma unroll
+                    for (int y = 0; y < 32; ++y) {
+                        const float e = mask.sees(k0 + side * 32 + y) ? __uint_as_float(v[y]) : 0.0f;
+                        d[y] = __float_as_uint(e == 0.0f ? 0.0f : e * (__uint_as_float(d[y]) - delta));
+                    }
                 }
-            }
 #pragma unroll
-            for (int y = 0; y < 16; ++y)
-                w[y] = pack_two<T>(__uint_as_float(d[2 * y]), __uint_as_float(d[2 * y + 1]));
-            tmem_st16(at_ds + 64 * (j & 1) + lanes + side * 16, w);
-            if (side == 0 && s.kl < p.a.kv_len && k0 + kTile > s.kl) {  // keys past the sequence
-                clear_rows<DP>(stage + 2 * (j & 1) * G::kTileBytes, row, s.kl - k0);
-                fence_async_shared();
+                for (int y = 0; y < 16; ++y)
+                    u[y] = pack_two<T>(__uint_as_float(d[2 * y]), __uint_as_float(d[2 * y + 1]));
+                tmem_st16(at_ds + 64 * st + lanes + side * 16, u);
+                if (side == 0 && s.kl < p.a.kv_len && k0 + kTile > s.kl) {  // keys past the sequence
+                    clear_rows<DP>(stage + 2 * st * G::kTileBytes, row, s.kl - k0);
+                    fence_async_shared();
+                }
+                wait_st();
+                fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(bar.b_ready + 8 * st);  // a warp may be a step ahead of another
             }
-            wait_st();
-            fence_before();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(bar.b_ready + 8 * (j & 1));  // a warp may be a step ahead of another
-        }
-        if (go && n > 0) go = __all_sync(~0u, mbar_wait(bar.done, 0, gave_up));
-        fence_after();
-        if (go && side == 0) {
-            T* out = static_cast<T*>(p.dq.data) + b * p.dq.batch_stride + i * p.dq.token_stride + h * p.dq.head_stride;
-            if (n > 0)
-                store_row<T, DP>(at_dq + lanes, out, inside, p.a.head_dim, p.a.scale);
-            else if (inside)
-                zero_row(out, p.a.head_dim);
+            if (go && n > 0) {
+                go = __all_sync(~0u, mbar_wait(bar.done, held & 1, gave_up));
+                ++held;
+            }
+            fence_after();
+            if (go && side == 0) {  // the other sides start on the next piece
+                T* out = static_cast<T*>(p.dq.data) + w.b * p.dq.batch_stride + i * p.dq.token_stride +
+                         h * p.dq.head_stride;
+                if (n > 0)
+                    store_row<T, DP>(at_dq + lanes, out, inside, p.a.head_dim, p.a.scale);
+                else if (inside)
+                    zero_row(out, p.a.head_dim);
+            }
         }
     }
     fence_before();
@@ -701,6 +809,7 @@ __global__ void __launch_bounds__(kGradThreads, 1)
         drain();
         __syncthreads();
     }
+    if (threadIdx.x == 0) leave_pieces(p.sched);
     if (warp == 2) tmem_free(tmem, 512);
 }
 
@@ -743,18 +852,18 @@ __global__ void __launch_bounds__(kGradThreads, 1)
     id /= parts;
     const int hb = (int)(id % heads), hk = hb % p.a.kv_heads, b = hb / p.a.kv_heads;
     const int tile = (int)(id / heads);
-    const int64_t k0 = (int64_t)(lead ? tile : p.lead + tile) * kTile;
+    const int k0 = (lead ? tile : p.lead + tile) * kTile;
     const int64_t slot = dkv_slot(p, lead, tile, hb, part);
-    const Span s = span_of(p.a, b);
+    const Seq s = seq_of(p.a, b);
     // query tiles that see a key of the tile
     int first = 0, n = 0;
     if (k0 < s.kl) {
-        const int64_t lo = max((int64_t)0, k0 - s.off);
-        int64_t hi = s.ql;
-        if (p.a.window && k0 >= p.a.sinks) hi = min(hi, k0 + kTile - 1 + p.a.window - s.off);
+        const int lo = max(0, k0 - s.off);
+        int hi = s.ql;
+        if (p.a.window && k0 >= p.a.sinks) hi = (int)min((int64_t)hi, k0 + kTile - 1 + p.a.window - s.off);
         if (lo < hi) {
-            first = (int)(lo / p.tokens);
-            n = (int)((hi - 1) / p.tokens) - first + 1;
+            first = lo / p.tokens;
+            n = (hi - 1) / p.tokens - first + 1;
             const int from = (int)((int64_t)n * part / parts);
             n = (int)((int64_t)n * (part + 1) / parts) - from;
             first += from;
@@ -786,7 +895,7 @@ __global__ void __launch_bounds__(kGradThreads, 1)
         for (int j = 0; j < n; ++j) {
             const int st = j & 1;
             if (!mbar_wait(bar.empty + 8 * st, (j / 2 & 1) ^ 1, gave_up)) break;
-            const int64_t t = (int64_t)(first + j) * p.tokens;
+            const int t = (first + j) * p.tokens;
             mbar_expect(bar.full + 8 * st, bytes);
             load_q_tile<DP>(smem_u32(stage + 2 * st * G::kTileBytes), &mq, bar.full + 8 * st, p, t, hk, b);
             mbar_expect(bar.full2 + 8 * st, bytes);
@@ -827,17 +936,17 @@ __global__ void __launch_bounds__(kGradThreads, 1)
     } else if (warp >= 4) {
         const int side = (warp - 4) / 4, row = (warp % 4) * 32 + lane;  // which 32 of a tile's 128 queries
         const uint32_t lanes = (uint32_t)(warp % 4 * 32) << 16;
-        const int64_t key = k0 + row;
+        const int key = k0 + row;
         const uint64_t c2 = two(p.scale_log2, p.scale_log2);
 
         // statistics of query tile j to buffer j % 3, a kind a side: written a
         // step ahead, while the slowest warp may still read those of the step
         // before
-        const int64_t i_row = (int64_t)first * p.tokens + row / p.group;
+        const int i_row = first * p.tokens + row / p.group;
         const int64_t r_row = ((int64_t)b * p.a.q_heads + hk * p.group + row % p.group) * p.a.q_len;
         const bool in_tile = row < p.group * p.tokens;
         auto put_stats = [&](int j) {
-            const int64_t i = i_row + (int64_t)j * p.tokens;
+            const int i = i_row + j * p.tokens;
             const bool live = in_tile && i < s.ql;
             const int to = j % 3 * kTile + row;
             if (side == 0) {
@@ -846,7 +955,7 @@ __global__ void __launch_bounds__(kGradThreads, 1)
             } else if (side == 1) {
                 stat_delta[to] = live ? -p.delta[r_row + i] : 0.0f;
             } else if (side == 2) {
-                pos[to] = live ? (int)max(s.off + i, (int64_t)-1) : -1;
+                pos[to] = live ? max(s.off + i, -1) : -1;
             }
         };
         bool go = true;
@@ -862,7 +971,7 @@ __global__ void __launch_bounds__(kGradThreads, 1)
                 __syncwarp();
                 if (lane == 0) mbar_arrive(bar.stats);
             }
-            const int64_t t0 = (int64_t)(first + j) * p.tokens, t1 = t0 + p.tokens;
+            const int t0 = (first + j) * p.tokens, t1 = t0 + p.tokens;
             const float4* lses = reinterpret_cast<const float4*>(stat_lse + (j % 3) * kTile + side * 32);
             const float4* deltas = reinterpret_cast<const float4*>(stat_delta + (j % 3) * kTile + side * 32);
             const bool whole = t1 <= s.ql && all_visible(p, s, t0, t1, k0);
@@ -883,7 +992,7 @@ __global__ void __launch_bounds__(kGradThreads, 1)
                 const int* at = pos + (j % 3) * kTile + side * 32;
 #pragma unroll
                 for (int y = 0; y < 32; ++y)
-                    if (!RowMask(at[y], p.a).sees((int)key)) v[y] = 0;
+                    if (!RowMask(at[y], p.a).sees(key)) v[y] = 0;
             }
 #pragma unroll
             for (int y = 0; y < 16; ++y)
@@ -931,20 +1040,25 @@ __global__ void __launch_bounds__(kGradThreads, 1)
         }
         if (go && n > 0) go = __all_sync(~0u, mbar_wait(bar.done, 0, gave_up));
         fence_after();
-        if (go && side < 2) {
-            const heddle_heads& t = side ? p.dk : p.dv;
-            T* out = static_cast<T*>(t.data) + b * t.batch_stride + key * t.token_stride + hk * t.head_stride;
+        if (go) {  // two sides for dv, two for dk, half of the columns each
+            const bool is_dk = side & 1;
+            const int d0 = side / 2 * (DP / 2), D = p.a.head_dim - d0;
+            const uint32_t from = (is_dk ? at_dk : at_dv) + lanes + d0;
+            const float f = is_dk ? p.a.scale : 1.0f;
+            const heddle_heads& t = is_dk ? p.dk : p.dv;
+            T* out = static_cast<T*>(t.data) + b * t.batch_stride + key * t.token_stride + hk * t.head_stride + d0;
             const bool inside = key < p.a.kv_len;
             if (parts > 1) {
-                float* to = (side ? p.part_dk : p.part_dv) + (slot * kTile + row) * p.a.head_dim;
+                float* to = (is_dk ? p.part_dk : p.part_dv) + (slot * kTile + row) * p.a.head_dim + d0;
                 if (n > 0)
-                    store_floats<DP>((side ? at_dk : at_dv) + lanes, to, true, p.a.head_dim, side ? p.a.scale : 1.0f);
+                    store_floats<DP / 2>(from, to, true, D, f);
                 else
-                    for (int x = 0; x < p.a.head_dim; ++x) to[x] = 0.0f;
-            } else if (n > 0)
-                store_row<T, DP>((side ? at_dk : at_dv) + lanes, out, inside, p.a.head_dim, side ? p.a.scale : 1.0f);
-            else if (inside)
-                zero_row(out, p.a.head_dim);
+                    for (int x = 0; x < min(D, DP / 2); ++x) to[x] = 0.0f;
+            } else if (n > 0) {
+                store_row<T, DP / 2>(from, out, inside, D, f);
+            } else if (inside) {
+                zero_row(out, min(D, DP / 2));
+            }
         }
     }
     fence_before();
@@ -1017,6 +1131,7 @@ Params params_of(const OpContext& x, const heddle_attention_args& a) {
     p.kv_tiles = (int32_t)ceil_div(a.kv_len, kTile);
     p.scale_log2 = a.scale * kLog2e;
     p.err = x.err;
+    p.sched = x.sched;
     // Parts along the keys where the query tiles are too few for the SMs: at
     // least two key tiles each, at most 32 (the join holds one a lane).
     const int nt = tiles_per_block(a);
@@ -1062,8 +1177,8 @@ cudaError_t forward(int device, const Params& p, const CUtensorMap& q, const CUt
     static std::atomic<uint64_t> asked{0};
     const cudaError_t e = allow_shared(f, F::kBytes, device, asked);
     if (e != cudaSuccess) return e;
-    const int64_t grid = ceil_div(p.q_tiles, NT) * p.a.batch * p.a.kv_heads * p.splits;
-    f<<<(unsigned)grid, F::kThreads, F::kBytes, st>>>(q, k, v, p);
+    const int64_t pieces = ceil_div(p.q_tiles, NT) * p.a.batch * p.a.kv_heads * p.splits;
+    f<<<(unsigned)pieces, F::kThreads, F::kBytes, st>>>(q, k, v, p);
     if (p.splits > 1) {
         const int64_t rows = p.a.batch * p.a.q_heads * p.a.q_len;
         attn_join_kernel<T><<<(unsigned)ceil_div(rows, 8), 256, 0, st>>>(p);
@@ -1072,7 +1187,7 @@ cudaError_t forward(int device, const Params& p, const CUtensorMap& q, const CUt
 }
 
 template <class T, int DP>
-cudaError_t backward(int device, const Params& p, const CUtensorMap& q, const CUtensorMap& k, const CUtensorMap& v,
+cudaError_t backward(int device, int sms, const Params& p, const CUtensorMap& q, const CUtensorMap& k, const CUtensorMap& v,
                      const CUtensorMap& d_o, cudaStream_t st) {
     using G = GradShape<DP>;
     static std::atomic<uint64_t> asked_q{0}, asked_kv{0};
@@ -1086,7 +1201,8 @@ cudaError_t backward(int device, const Params& p, const CUtensorMap& q, const CU
         attn_dkv_join_kernel<T><<<(unsigned)(heads * p.lead * 16), 256, 0, st>>>(p, 1);
     if (p.rest_parts > 1 && p.kv_tiles > p.lead)
         attn_dkv_join_kernel<T><<<(unsigned)(heads * (p.kv_tiles - p.lead) * 16), 256, 0, st>>>(p, 0);
-    attn_dq_kernel<T, DP><<<(unsigned)(p.q_tiles * heads), kGradThreads, G::kBytes, st>>>(q, k, v, d_o, p);
+    const int64_t pieces = p.q_tiles * heads, grid = pieces < sms ? pieces : sms;
+    attn_dq_kernel<T, DP><<<(unsigned)grid, kGradThreads, G::kBytes, st>>>(q, k, v, d_o, p, (int)pieces);
     return cudaGetLastError();
 }
 
@@ -1111,7 +1227,7 @@ cudaError_t input_maps(const Params& p, CUtensorMap* q, CUtensorMap* k, CUtensor
 // head_dim in whole 16-byte units, at most 128, and bases and strides that
 // bulk tensor copies take; a scale whose sign keeps the order of scores.
 bool attn_tc_takes(const heddle_attention_args& a) {
-    return a.head_dim % 8 == 0 && a.head_dim <= 128 && a.q_heads / a.kv_heads <= kTile && a.scale > 0.0f &&
+    return a.q_len <= kMaxLength && a.kv_len <= kMaxLength && a.head_dim % 8 == 0 && a.head_dim <= 128 && a.q_heads / a.kv_heads <= kTile && a.scale > 0.0f &&
            a.q_len > 0 && a.kv_len > 0 && copies(a.q, a.batch, a.q_len, a.q_heads) &&
            copies(a.k, a.batch, a.kv_len, a.kv_heads) && copies(a.v, a.batch, a.kv_len, a.kv_heads);
 }
@@ -1157,8 +1273,8 @@ cudaError_t launch_attn_tc_grad(const OpContext& x, const heddle_attention_grad_
     if (e != cudaSuccess) return e;
     const bool narrow = a.head_dim <= 64;
     if (a.dtype == HEDDLE_BF16)
-        return narrow ? backward<__nv_bfloat16, 64>(x.device, p, q, k, v, d_o, st) : backward<__nv_bfloat16, 128>(x.device, p, q, k, v, d_o, st);
-    return narrow ? backward<__half, 64>(x.device, p, q, k, v, d_o, st) : backward<__half, 128>(x.device, p, q, k, v, d_o, st);
+        return narrow ? backward<__nv_bfloat16, 64>(x.device, x.num_sms, p, q, k, v, d_o, st) : backward<__nv_bfloat16, 128>(x.device, x.num_sms, p, q, k, v, d_o, st);
+    return narrow ? backward<__half, 64>(x.device, x.num_sms, p, q, k, v, d_o, st) : backward<__half, 128>(x.device, x.num_sms, p, q, k, v, d_o, st);
 }
 
 }  // namespace hd

@@ -500,6 +500,8 @@ heddle_status heddle_create(heddle_ctx** out, int32_t device) {
     if (e == cudaSuccess) e = cudaMalloc(&x->d_meet, meet);
     if (e == cudaSuccess) e = cudaMemset(x->d_meet, 0, meet);
 
+    if (e == cudaSuccess) e = cudaMalloc(&x->op.sched, 2 * sizeof(int32_t));
+    if (e == cudaSuccess) e = cudaMemset(x->op.sched, 0, 2 * sizeof(int32_t));
     x->op.device = device;
     x->op.num_sms = x->num_sms;
     x->op.err = x->d_flags + 1;
@@ -559,6 +561,7 @@ void heddle_destroy(heddle_ctx* x) {
         cudaFree(x->lv_bounds[i]);
     }
     cudaFree(x->op.ws);
+    cudaFree(x->op.sched);
     cudaFree(x->d_timg);
     cudaFree(x->d_node_type);
     cudaFree(x->d_node_gpus);

@@ -22,6 +22,7 @@ struct OpContext {
     int device = 0;
     int num_sms = 0;
     uint32_t* err = nullptr;  // device error flags
+    int32_t* sched = nullptr;  // two counters of kernels that hand out work, zero between launches
     unsigned char* ws = nullptr;
     size_t ws_cap = 0;
     char* msg = nullptr;
