@@ -83,10 +83,10 @@ struct Params {
     const float* delta;
     int32_t group, tokens;  // G, tokens of a tile
     int32_t q_tiles, kv_tiles;
-    int32_t splits;
+    int32_t splits, twins, parts;  // pieces along the keys; twins in each; both together
     float scale_log2;
-    float* part_o;    // [splits][batch * q_heads * q_len][head_dim]
-    float* part_lse;  // [splits][batch * q_heads * q_len]
+    float* part_o;    // [parts][batch * q_heads * q_len][head_dim]
+    float* part_lse;  // [parts][batch * q_heads * q_len]
     // backward over keys: the first `lead` key tiles in lead_parts parts along
     // the queries, the others in rest_parts; sums of parts as floats
     int32_t lead, lead_parts, rest_parts;
@@ -126,12 +126,22 @@ __device__ __forceinline__ KeyTiles key_tiles(const Params& p, const Seq& s, int
     return k;
 }
 
+// Bits lo .. hi of 32, as far as they are among them.
+__device__ __forceinline__ uint32_t bits_between(int lo, int hi) {
+    const uint32_t up = hi < 0 ? 0u : hi >= 31 ? ~0u : (2u << hi) - 1;
+    const uint32_t below = lo <= 0 ? 0u : lo >= 32 ? ~0u : (1u << lo) - 1;
+    return up & ~below;
+}
+
 // What the query at a position sees; positions below -1 see nothing either.
 struct RowMask {
     int pos, low, sinks;
     __device__ RowMask(int at, const heddle_attention_args& a)
-        : pos(max(at, -1)), low(a.window ? pos - (int)a.window + 1 : INT32_MIN), sinks((int)a.sinks) {}
-    __device__ bool sees(int key) const { return key <= pos && (key >= low || key < sinks); }
+        : pos(max(at, -1)), low(a.window ? max(pos - (int)a.window + 1, 0) : 0), sinks((int)a.sinks) {}
+    // bit y: whether it sees key + y
+    __device__ uint32_t sees32(int key) const {
+        return bits_between(low - key, pos - key) | bits_between(0, min(sinks - 1, pos) - key);
+    }
 };
 
 // Every query of tokens i0 .. i1 - 1 sees every key of the tile at k0.
@@ -251,39 +261,54 @@ struct Forward {
     static constexpr int kCols = NT * (kTile + DP) <= 256 ? 256 : 512;
 };
 
-// A piece of the forward pass: NT query tiles of a key head and the steps
-// j0 .. j0 + n - 1 of the key tiles they see, tile q those before to[q].
-template <int NT>
+// A piece of the forward pass: NT query tiles of a key head and the key tiles
+// they see; tile q takes count[q] of them from from[q] on.  Twins are one
+// query tile twice, each with half of its key tiles.
+template <int NT, bool TWINS>
 struct ForwardPiece {
     int hk, b, split, t0;
     Seq s;
     KeyTiles keys;
-    int j0, n, to[NT];
+    int n, from[NT], count[NT];
     __device__ ForwardPiece(const Params& p, int id) {
         split = id % p.splits;
         id /= p.splits;
         hk = id % p.a.kv_heads;
         id /= p.a.kv_heads;
         b = id % (int)p.a.batch;
-        // the last queries see the most keys: their tiles come first
-        t0 = ((p.q_tiles + NT - 1) / NT - 1 - id / (int)p.a.batch) * NT * p.tokens;
         s = seq_of(p.a, b);
-        keys = key_tiles(p, s, t0, t0 + NT * p.tokens);
-        j0 = (int)((int64_t)keys.count * split / p.splits);
-        const int j1 = (int)((int64_t)keys.count * (split + 1) / p.splits);
+        constexpr int kTiles = TWINS ? 1 : NT;
+        // the last queries see the most keys: their tiles come first
+        t0 = ((p.q_tiles + kTiles - 1) / kTiles - 1 - id / (int)p.a.batch) * kTiles * p.tokens;
+        keys = key_tiles(p, s, t0, t0 + kTiles * p.tokens);
+        const int j0 = (int)((int64_t)keys.count * split / p.splits),
+                  j1 = (int)((int64_t)keys.count * (split + 1) / p.splits);
         n = 0;
 #pragma unroll
         for (int q = 0; q < NT; ++q) {
-            const KeyTiles own = key_tiles(p, s, t0 + q * p.tokens, t0 + (q + 1) * p.tokens);
-            to[q] = j0;
-            // the last of its tiles in the common order; the first ones are common to all
-            if (own.count) to[q] = max(j0, min(j1, keys.lead + own.first + own.count - own.lead - keys.first));
-            n = max(n, to[q] - j0);
+            from[q] = j0;
+            if (TWINS) {
+                const int half = (j1 - j0 + 1) / 2;
+                from[q] = j0 + q * half;
+                count[q] = q ? j1 - j0 - half : half;
+            } else {
+                const KeyTiles own = key_tiles(p, s, t0 + q * p.tokens, t0 + (q + 1) * p.tokens);
+                count[q] = 0;
+                // up to the last of its tiles in the common order; the first ones are common to all
+                if (own.count)
+                    count[q] = max(0, min(j1, keys.lead + own.first + own.count - own.lead - keys.first) - j0);
+            }
+            n = max(n, count[q]);
         }
     }
+    // Places in the order of loading.  Tiles share keys and values: K and V by
+    // turns.  Twins: both K of a step, then both V, one of each in a last
+    // step of the first twin alone.
+    __device__ int k_at(int q, int j) const { return TWINS ? 4 * j + q : 2 * j; }
+    __device__ int v_at(int q, int j) const { return TWINS ? 4 * j + q + (j < count[NT - 1] ? 2 : 1) : 2 * j + 1; }
 };
 
-template <class T, int DP, int NT>
+template <class T, int DP, int NT, bool TWINS>
 __global__ void __launch_bounds__(Forward<DP, NT>::kThreads, 1)
     attn_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUtensorMap mk,
                 const __grid_constant__ CUtensorMap mv, const __grid_constant__ Params p) {
@@ -299,11 +324,10 @@ __global__ void __launch_bounds__(Forward<DP, NT>::kThreads, 1)
     float* highs = reinterpret_cast<float*>(reinterpret_cast<unsigned char*>(bars) + 512);  // [2][NT][2][128]
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
 
-    const ForwardPiece<NT> w(p, blockIdx.x);
+    const ForwardPiece<NT, TWINS> w(p, blockIdx.x);
     const Seq& s = w.s;
     const KeyTiles& keys = w.keys;
-    const int (&to)[NT] = w.to;
-    const int j0 = w.j0, n = w.n, t0 = w.t0, hk = w.hk, b = w.b, split = w.split;
+    const int n = w.n, t0 = w.t0, hk = w.hk, b = w.b, split = w.split;
 
     if (threadIdx.x == 0) {
         for (int i = 0; i < F::kSlots; ++i) {
@@ -328,59 +352,68 @@ __global__ void __launch_bounds__(Forward<DP, NT>::kThreads, 1)
     if (warp == 0 && n > 0 && elect_one()) {
         const uint32_t q_bytes = p.group * p.tokens * DP * 2;
 #pragma unroll
-        for (int q = 0; q < NT; ++q)
-            if (to[q] > j0) {
+        for (int q = 0; q < (TWINS ? 1 : NT); ++q)
+            if (w.count[q] > 0) {
                 mbar_expect(q_full + 8 * q, q_bytes);
                 load_q_tile<DP>(smem_u32(base + q * F::kTileBytes), &mq, q_full + 8 * q, p, t0 + q * p.tokens, hk, b);
             }
-        for (int i = 0; i < 2 * n; ++i) {
+        int i = 0;
+        bool go = true;
+        auto load = [&](const CUtensorMap* m, int tile) {
             const int slot = i % F::kSlots;
-            if (!mbar_wait(empty + 8 * slot, (i / F::kSlots & 1) ^ 1, gave_up)) break;
+            if (!(go = go && mbar_wait(empty + 8 * slot, (i / F::kSlots & 1) ^ 1, gave_up))) return;
             mbar_expect(full + 8 * slot, F::kTileBytes);
-            load_kv_tile<DP>(smem_u32(ring + slot * F::kTileBytes), i & 1 ? &mv : &mk, full + 8 * slot,
-                             keys.at(j0 + i / 2) * kTile, hk, b);
+            load_kv_tile<DP>(smem_u32(ring + slot * F::kTileBytes), m, full + 8 * slot, keys.at(tile) * kTile, hk, b);
+            ++i;
+        };
+        for (int j = 0; go && j < n; ++j) {
+            load(&mk, w.from[0] + j);
+            if (TWINS && j < w.count[NT - 1]) load(&mk, w.from[NT - 1] + j);
+            load(&mv, w.from[0] + j);
+            if (TWINS && j < w.count[NT - 1]) load(&mv, w.from[NT - 1] + j);
         }
     } else if (warp == 1 && n > 0 && elect_one()) {
         const uint32_t bf = p.a.dtype == HEDDLE_BF16;
         const uint32_t id_s = instr_desc(bf, false, false, kTile), id_o = instr_desc(bf, false, true, DP);
         bool go = true;
         for (int j = -1; go && j < n; ++j) {
-            const int iv = 2 * j + 1, ik = 2 * j + 2;  // V of step j, K of step j + 1
-            const int sv = iv % F::kSlots, sk = ik % F::kSlots;
-            if (j + 1 < n) go = mbar_wait(full + 8 * sk, ik / F::kSlots & 1, gave_up);
-            if (go && j >= 0) go = mbar_wait(full + 8 * sv, iv / F::kSlots & 1, gave_up);
-            if (!go) break;
-            fence_after();
 #pragma unroll
             for (int q = 0; q < NT; ++q) {
                 const uint32_t ts = tmem + q * kTile, to_acc = tmem + NT * kTile + q * DP;
-                if (j >= 0 && j0 + j < to[q]) {
+                const int iv = w.v_at(q, j), ik = w.k_at(q, j + 1), sv = iv % F::kSlots, sk = ik % F::kSlots;
+                const bool last = TWINS || q == NT - 1;  // of those that read the step's keys and values
+                if (j >= 0 && j < w.count[q]) {
+                    if (!(go = mbar_wait(full + 8 * sv, iv / F::kSlots & 1, gave_up))) break;
                     if (!(go = mbar_wait(p_ready + 8 * q, j & 1, gave_up))) break;
                     fence_after();
                     mma_rows<32, 64>(to_acc, ts, smem_u32(ring + sv * F::kTileBytes), id_o, j > 0);
-                    if (j0 + j + 1 == to[q]) commit(o_done + 8 * q);
+                    if (j + 1 == w.count[q]) commit(o_done + 8 * q);
                 }
-                if (j0 + j + 1 < to[q]) {
-                    if (j < 0 && !(go = mbar_wait(q_full + 8 * q, 0, gave_up))) break;
-                    mma_dims<DP>(ts, smem_u32(base + q * F::kTileBytes), smem_u32(ring + sk * F::kTileBytes), id_s);
+                if (last && j >= 0 && (TWINS ? j < w.count[q] : true)) commit(empty + 8 * sv);
+                if (j + 1 < w.count[q]) {
+                    if (!(go = mbar_wait(full + 8 * sk, ik / F::kSlots & 1, gave_up))) break;
+                    if (j < 0 && !(go = mbar_wait(q_full + (TWINS ? 0 : 8 * q), 0, gave_up))) break;
+                    fence_after();
+                    mma_dims<DP>(ts, smem_u32(base + (TWINS ? 0 : q) * F::kTileBytes),
+                                 smem_u32(ring + sk * F::kTileBytes), id_s);
                     commit(s_full + 8 * q);
                 }
+                if (last && (TWINS ? j + 1 < w.count[q] : j + 1 < n)) commit(empty + 8 * sk);
             }
-            if (!go) break;
-            if (j >= 0) commit(empty + 8 * sv);
-            if (j + 1 < n) commit(empty + 8 * sk);
         }
     } else if (warp >= 4) {
         const int q = (warp - 4) / 8, side = (warp - 4) / 4 % 2, row = (warp % 4) * 32 + lane;
         const uint32_t lanes = (uint32_t)(warp % 4 * 32) << 16;
         const uint32_t ts = tmem + lanes + q * kTile, to_acc = tmem + lanes + NT * kTile + q * DP;
         const uint32_t pair = met + 8 * (q * 4 + warp % 4);  // this warp and the one of the rows' other half
-        const int i0 = t0 + q * p.tokens, i1 = i0 + p.tokens;
+        const int i0 = t0 + (TWINS ? 0 : q * p.tokens), i1 = i0 + p.tokens;
         const int i = i0 + row / p.group, h = hk * p.group + row % p.group;
         const RowMask mask(s.off + i, p.a);
         const float c = p.scale_log2;
         float top = -INFINITY, sum = 0.0f;
-        const int mine = to[q] - j0;
+        const int mine = w.count[q];
+        // a warp whose rows no query fills only keeps step
+        const bool idle = (min(i1, s.ql) - i0) * p.group <= warp % 4 * 32;
         bool go = true;
         // the other half's value for the row, and this one's for it
         auto swap = [&](int turn, float v) {
@@ -392,67 +425,71 @@ __global__ void __launch_bounds__(Forward<DP, NT>::kThreads, 1)
             return at[(side ^ 1) * kTile];
         };
         for (int j = 0; j < mine; ++j) {
-            const int k0 = keys.at(j0 + j) * kTile;
+            const int k0 = keys.at(w.from[q] + j) * kTile;
             const bool whole = all_visible(p, s, i0, min(i1, s.ql), k0);
             if (!(go = __all_sync(~0u, mbar_wait(s_full + 8 * q, j & 1, gave_up)))) break;
             fence_after();
-            uint32_t v[2][32];
+            if (!idle) {
+                uint32_t v[2][32];
 #pragma unroll
-            for (int x = 0; x < 2; ++x) tmem_ld32(ts + 64 * side + 32 * x, v[x]);
-            wait_ld();
-            if (!whole) {
+                for (int x = 0; x < 2; ++x) tmem_ld32(ts + 64 * side + 32 * x, v[x]);
+                wait_ld();
+                if (!whole) {
+#pragma unroll
+                    for (int x = 0; x < 2; ++x) {
+                        const uint32_t seen = mask.sees32(k0 + 64 * side + 32 * x);
+#pragma unroll
+                        for (int y = 0; y < 32; ++y)
+                            if (!(seen >> y & 1)) v[x][y] = 0xff800000u;  // -infinity
+                    }
+                }
+                float m4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
 #pragma unroll
                 for (int x = 0; x < 2; ++x)
 #pragma unroll
-                    for (int y = 0; y < 32; ++y)
-                        if (!mask.sees(k0 + 64 * side + 32 * x + y)) v[x][y] = 0xff800000u;  // -infinity
-            }
-            float m4[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
-#pragma unroll
-            for (int x = 0; x < 2; ++x)
-#pragma unroll
-                for (int y = 0; y < 32; ++y) m4[y % 4] = fmaxf(m4[y % 4], __uint_as_float(v[x][y]));
-            float high = fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3]));
-            high = fmaxf(high, swap(j, high));
-            if (!go) break;
-            float keep = 1.0f;
-            if (high > top && (top == -INFINITY || (high - top) * c > kSlack)) {
-                keep = top == -INFINITY ? 0.0f : exp2_fast((top - high) * c);
-                top = high;
-                sum *= keep;
-            }
-            if (j > 0 && __any_sync(~0u, keep != 1.0f)) {
-                // the product of the step before has completed: the scores'
-                // barrier was committed after it
+                    for (int y = 0; y < 32; ++y) m4[y % 4] = fmaxf(m4[y % 4], __uint_as_float(v[x][y]));
+                float high = fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3]));
+                high = fmaxf(high, swap(j, high));
+                if (!go) break;
+                float keep = 1.0f;
+                if (high > top && (top == -INFINITY || (high - top) * c > kSlack)) {
+                    keep = top == -INFINITY ? 0.0f : exp2_fast((top - high) * c);
+                    top = high;
+                    sum *= keep;
+                }
+                if (j > 0 && __any_sync(~0u, keep != 1.0f)) {
+                    // the product of the step before has completed: the scores'
+                    // barrier was committed after it
 #pragma unroll 1
-                for (int x = 0; x < DP / 2; x += 16) {
-                    uint32_t o[16];
-                    tmem_ld16(to_acc + side * (DP / 2) + x, o);
-                    wait_ld();
+                    for (int x = 0; x < DP / 2; x += 16) {
+                        uint32_t o[16];
+                        tmem_ld16(to_acc + side * (DP / 2) + x, o);
+                        wait_ld();
 #pragma unroll
-                    for (int y = 0; y < 16; ++y) o[y] = __float_as_uint(__uint_as_float(o[y]) * keep);
-                    tmem_st16(to_acc + side * (DP / 2) + x, o);
+                        for (int y = 0; y < 16; ++y) o[y] = __float_as_uint(__uint_as_float(o[y]) * keep);
+                        tmem_st16(to_acc + side * (DP / 2) + x, o);
+                    }
                 }
-            }
-            const float sub = top == -INFINITY ? 0.0f : top * c;
-            const uint64_t c2 = two(c, c), sub2 = two(-sub, -sub);
-            uint64_t part[2] = {0, 0};
+                const float sub = top == -INFINITY ? 0.0f : top * c;
+                const uint64_t c2 = two(c, c), sub2 = two(-sub, -sub);
+                uint64_t part[2] = {0, 0};
 #pragma unroll
-            for (int x = 0; x < 2; ++x) {
-                uint32_t w[16];
+                for (int x = 0; x < 2; ++x) {
+                    uint32_t w[16];
 #pragma unroll
-                for (int y = 0; y < 32; y += 2) {
-                    const float2 z = apart(fma_two(two(v[x][y], v[x][y + 1]), c2, sub2));
-                    const float lo = exp2_fast(z.x), hi = exp2_fast(z.y);
-                    part[y / 2 % 2] = add_two(part[y / 2 % 2], two(lo, hi));
-                    w[y / 2] = pack_two<T>(lo, hi);
+                    for (int y = 0; y < 32; y += 2) {
+                        const float2 z = apart(fma_two(two(v[x][y], v[x][y + 1]), c2, sub2));
+                        const float lo = exp2_fast(z.x), hi = exp2_fast(z.y);
+                        part[y / 2 % 2] = add_two(part[y / 2 % 2], two(lo, hi));
+                        w[y / 2] = pack_two<T>(lo, hi);
+                    }
+                    tmem_st16(ts + 64 * side + 16 * x, w);  // over scores that this warp itself has read
                 }
-                tmem_st16(ts + 64 * side + 16 * x, w);  // over scores that this warp itself has read
+                const float2 both = apart(add_two(part[0], part[1]));
+                sum += both.x + both.y;
             }
-            const float2 both = apart(add_two(part[0], part[1]));
-            sum += both.x + both.y;
             if (side == 0 && s.kl < p.a.kv_len && k0 + kTile > s.kl) {  // values past the sequence
-                const int iv = 2 * j + 1, sv = iv % F::kSlots;
+                const int iv = w.v_at(q, j), sv = iv % F::kSlots;
                 if (!(go = __all_sync(~0u, mbar_wait(full + 8 * sv, iv / F::kSlots & 1, gave_up)))) break;
                 clear_rows<DP>(ring + sv * F::kTileBytes, row, s.kl - k0);
                 fence_async_shared();
@@ -463,7 +500,7 @@ __global__ void __launch_bounds__(Forward<DP, NT>::kThreads, 1)
             if (lane == 0) mbar_arrive(p_ready + 8 * q);
         }
         if (go && mine > 0) {
-            sum += swap(mine, sum);
+            if (!idle) sum += swap(mine, sum);
             if (go) go = __all_sync(~0u, mbar_wait(o_done + 8 * q, 0, gave_up));
         }
         fence_after();
@@ -474,8 +511,9 @@ __global__ void __launch_bounds__(Forward<DP, NT>::kThreads, 1)
             const float lse = some ? (top * c + log2f(sum)) * kLn2 : -INFINITY;
             const int64_t r = ((int64_t)b * p.a.q_heads + h) * p.a.q_len + i;
             const int D = p.a.head_dim, d0 = side * (DP / 2);
-            if (p.splits > 1) {
-                const int64_t at = (int64_t)split * p.a.batch * p.a.q_heads * p.a.q_len + r;
+            if (p.parts > 1) {
+                const int part = TWINS ? 2 * split + q : split;
+                const int64_t at = (int64_t)part * p.a.batch * p.a.q_heads * p.a.q_len + r;
                 if (inside && side == 0) p.part_lse[at] = lse;
                 // a part of no weight is not read
                 if (mine > 0) store_floats<DP / 2>(to_acc + d0, p.part_o + at * D + d0, inside && some, D - d0, f);
@@ -505,7 +543,7 @@ __global__ void __launch_bounds__(256) attn_join_kernel(const __grid_constant__ 
     const int64_t rows = p.a.batch * p.a.q_heads * p.a.q_len;
     const int64_t r = (int64_t)blockIdx.x * 8 + threadIdx.x / 32;
     if (r >= rows) return;
-    const float mine = lane < p.splits ? p.part_lse[lane * rows + r] : -INFINITY;
+    const float mine = lane < p.parts ? p.part_lse[lane * rows + r] : -INFINITY;
     float top = mine;
 #pragma unroll
     for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, o));
@@ -513,7 +551,7 @@ __global__ void __launch_bounds__(256) attn_join_kernel(const __grid_constant__ 
     const float total = warp_sum(e);
     const float w = total > 0.0f ? e / total : 0.0f;
     float acc[4] = {};
-    for (int x = 0; x < p.splits; ++x) {
+    for (int x = 0; x < p.parts; ++x) {
         const float f = __shfl_sync(~0u, w, x);
         if (f == 0.0f) continue;
         const float* o = p.part_o + ((int64_t)x * rows + r) * D;
@@ -614,7 +652,7 @@ constexpr int kGradBarBytes = 160;
 template <int DP>
 struct GradShape {
     static constexpr int kTileBytes = kTile * DP * 2;
-    static constexpr int kStats = 3 * kTile * 12;
+    static constexpr int kStats = 3 * kTile * 8;
     static constexpr int kBytes = 1024 + 6 * kTileBytes + kGradBarBytes + 64 + kStats;
 };
 
@@ -768,9 +806,10 @@ __global__ void __launch_bounds__(kGradThreads, 1)
                     }
                 } else {
                     // a product with what lies in hidden places must not count
+                    const uint32_t seen = mask.sees32(k0 + side * 32);
 #pragma unroll
                     for (int y = 0; y < 32; ++y) {
-                        const float e = mask.sees(k0 + side * 32 + y) ? __uint_as_float(v[y]) : 0.0f;
+                        const float e = seen >> y & 1 ? __uint_as_float(v[y]) : 0.0f;
                         d[y] = __float_as_uint(e == 0.0f ? 0.0f : e * (__uint_as_float(d[y]) - delta));
                     }
                 }
@@ -840,7 +879,6 @@ __global__ void __launch_bounds__(kGradThreads, 1)
     uint32_t* tmem_at = const_cast<uint32_t*>(gave_up) + 1;
     float* stat_lse = reinterpret_cast<float*>(tail + kGradBarBytes + 64);  // [3][128] minus lse, in powers of two
     float* stat_delta = stat_lse + 3 * kTile;                               // [3][128] minus delta
-    int* pos = reinterpret_cast<int*>(stat_delta + 3 * kTile);              // [3][128] positions
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
 
     // the first keys are seen by the most queries
@@ -939,7 +977,7 @@ __global__ void __launch_bounds__(kGradThreads, 1)
         const int key = k0 + row;
         const uint64_t c2 = two(p.scale_log2, p.scale_log2);
 
-        // statistics of query tile j to buffer j % 3, a kind a side: written a
+        // statistics of query tile j to buffer j % 3, by two of the sides: written a
         // step ahead, while the slowest warp may still read those of the step
         // before
         const int i_row = first * p.tokens + row / p.group;
@@ -954,9 +992,15 @@ __global__ void __launch_bounds__(kGradThreads, 1)
                 stat_lse[to] = l == -INFINITY ? -INFINITY : -l * kLog2e;
             } else if (side == 1) {
                 stat_delta[to] = live ? -p.delta[r_row + i] : 0.0f;
-            } else if (side == 2) {
-                pos[to] = live ? max(s.off + i, -1) : -1;
             }
+        };
+        // the tile's columns that see the key: query heads of consecutive tokens
+        auto seen_by = [&](int t0) {
+            const int last = p.a.window && key >= (int)p.a.sinks
+                                 ? (int)min((int64_t)s.ql - 1, key + p.a.window - 1 - s.off)
+                                 : s.ql - 1;
+            const int lo = max(0, min(key - s.off - t0, p.tokens)), hi = max(0, min(last - t0 + 1, p.tokens));
+            return bits_between(lo * p.group - side * 32, hi * p.group - 1 - side * 32);
         };
         bool go = true;
         if (n > 0) {
@@ -989,10 +1033,10 @@ __global__ void __launch_bounds__(kGradThreads, 1)
                 v[y + 2] = __float_as_uint(exp2_fast(z1.x)), v[y + 3] = __float_as_uint(exp2_fast(z1.y));
             }
             if (!whole) {
-                const int* at = pos + (j % 3) * kTile + side * 32;
+                const uint32_t seen = seen_by(t0);
 #pragma unroll
                 for (int y = 0; y < 32; ++y)
-                    if (!RowMask(at[y], p.a).sees(key)) v[y] = 0;
+                    if (!(seen >> y & 1)) v[y] = 0;
             }
 #pragma unroll
             for (int y = 0; y < 16; ++y)
@@ -1133,7 +1177,7 @@ Params params_of(const OpContext& x, const heddle_attention_args& a) {
     p.err = x.err;
     p.sched = x.sched;
     // Parts along the keys where the query tiles are too few for the SMs: at
-    // least two key tiles each, at most 32 (the join holds one a lane).
+    // least two key tiles each, at most 32 with twins (the join holds one a lane).
     const int nt = tiles_per_block(a);
     const int64_t blocks = ceil_div(p.q_tiles, nt) * a.kv_heads * a.batch;
     int64_t keys = a.kv_len;
@@ -1144,7 +1188,11 @@ Params params_of(const OpContext& x, const heddle_attention_args& a) {
     int64_t parts = x.num_sms / blocks;
     const int64_t most = keys / (2 * kTile);
     parts = parts < most ? parts : most;
-    p.splits = (int32_t)(parts < 1 ? 1 : parts > 32 ? 32 : parts);
+    parts = parts < 1 ? 1 : parts > 16 ? 16 : parts;
+    p.splits = (int32_t)parts;
+    // a single query tile leaves half of a CTA idle: it takes the tile twice
+    p.twins = nt == 1 && keys >= 4 * kTile * parts;
+    p.parts = p.splits * (p.twins ? 2 : 1);
     // Backward over keys: blocks enough for the SMs, of four query tiles at
     // least; the tiles of the first tokens, which every query sees, in parts
     // of about the query tiles that a window's key tile has.
@@ -1168,18 +1216,18 @@ int64_t dkv_slots(const Params& p) {
                     (p.rest_parts > 1 ? (int64_t)(p.kv_tiles - p.lead) * p.rest_parts : 0));
 }
 
-template <class T, int DP, int NT>
+template <class T, int DP, int NT, bool TWINS>
 cudaError_t forward(int device, const Params& p, const CUtensorMap& q, const CUtensorMap& k, const CUtensorMap& v,
                     cudaStream_t st) {
     using F = Forward<DP, NT>;
     static_assert(F::kSlots >= 4, "two steps of K and V");
-    auto* f = attn_kernel<T, DP, NT>;
+    auto* f = attn_kernel<T, DP, NT, TWINS>;
     static std::atomic<uint64_t> asked{0};
     const cudaError_t e = allow_shared(f, F::kBytes, device, asked);
     if (e != cudaSuccess) return e;
-    const int64_t pieces = ceil_div(p.q_tiles, NT) * p.a.batch * p.a.kv_heads * p.splits;
+    const int64_t pieces = ceil_div(p.q_tiles, TWINS ? 1 : NT) * p.a.batch * p.a.kv_heads * p.splits;
     f<<<(unsigned)pieces, F::kThreads, F::kBytes, st>>>(q, k, v, p);
-    if (p.splits > 1) {
+    if (p.parts > 1) {
         const int64_t rows = p.a.batch * p.a.q_heads * p.a.q_len;
         attn_join_kernel<T><<<(unsigned)ceil_div(rows, 8), 256, 0, st>>>(p);
     }
@@ -1210,8 +1258,13 @@ template <class T>
 cudaError_t forward_of(int device, const Params& p, const CUtensorMap& q, const CUtensorMap& k, const CUtensorMap& v,
                        cudaStream_t st) {
     const bool two = tiles_per_block(p.a) == 2;
-    if (p.a.head_dim <= 64) return two ? forward<T, 64, 2>(device, p, q, k, v, st) : forward<T, 64, 1>(device, p, q, k, v, st);
-    return two ? forward<T, 128, 2>(device, p, q, k, v, st) : forward<T, 128, 1>(device, p, q, k, v, st);
+    if (p.a.head_dim <= 64)
+        return two       ? forward<T, 64, 2, false>(device, p, q, k, v, st)
+               : p.twins ? forward<T, 64, 2, true>(device, p, q, k, v, st)
+                         : forward<T, 64, 1, false>(device, p, q, k, v, st);
+    return two       ? forward<T, 128, 2, false>(device, p, q, k, v, st)
+           : p.twins ? forward<T, 128, 2, true>(device, p, q, k, v, st)
+                     : forward<T, 128, 1, false>(device, p, q, k, v, st);
 }
 
 cudaError_t input_maps(const Params& p, CUtensorMap* q, CUtensorMap* k, CUtensorMap* v) {
@@ -1237,15 +1290,15 @@ bool attn_tc_takes_grad(const heddle_attention_grad_args& g) {
 
 size_t attn_tc_scratch(const OpContext& x, const heddle_attention_args& a) {
     const Params p = params_of(x, a);
-    if (p.splits == 1) return 0;
-    const size_t rows = (size_t)(a.batch * a.q_heads * a.q_len) * p.splits;
+    if (p.parts == 1) return 0;
+    const size_t rows = (size_t)(a.batch * a.q_heads * a.q_len) * p.parts;
     return align256(rows * a.head_dim * 4) + align256(rows * 4);
 }
 
 cudaError_t launch_attn_tc(const OpContext& x, const heddle_attention_args& a, unsigned char* ws, cudaStream_t st) {
     Params p = params_of(x, a);
-    if (p.splits > 1) {
-        const size_t rows = (size_t)(a.batch * a.q_heads * a.q_len) * p.splits;
+    if (p.parts > 1) {
+        const size_t rows = (size_t)(a.batch * a.q_heads * a.q_len) * p.parts;
         p.part_o = reinterpret_cast<float*>(ws);
         p.part_lse = reinterpret_cast<float*>(ws + align256(rows * a.head_dim * 4));
     }
