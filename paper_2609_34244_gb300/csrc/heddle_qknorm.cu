@@ -163,9 +163,9 @@ __device__ __forceinline__ float inv_sqrt(float v) {
 }
 
 // What the kernel knows of a call beforehand.  kAny: nothing.  kHalves and
-// kPairs: every value is turned, in that layout, every lane of a group has
-// values, and all lies at whole units; two thirds of the instructions then
-// (16384 tokens of 72 heads of 128 bfloat16, forward: 186 us as kAny).
+// kPairs: the layout of the pairs, and that all lies at whole units; two
+// thirds of the instructions then (16384 tokens of 72 heads of 128 bfloat16,
+// forward: 186 us as kAny).
 enum RotaryCase { kAny, kHalves, kPairs };
 
 // A head of whole 16-byte units in a group of GL lanes, V values a lane, the
@@ -186,11 +186,13 @@ __global__ void __launch_bounds__(256, 3)
     const int heads = is_q ? a.q_heads : a.k_heads, chunks = (heads + chunk - 1) / chunk;
     const heddle_heads in = is_q ? a.q : a.k, out = is_q ? a.q_out : a.k_out, dst = is_q ? ga.dq : ga.dk;
     const int lane = threadIdx.x % GL, group = threadIdx.x / GL;
-    const int D = CASE == kAny ? a.head_dim : GL * V, rot = CASE == kAny ? a.rot_dim : D;
-    const bool live = CASE != kAny || lane * V < D, turns = CASE != kAny || lane * V < rot;
+    const int D = a.head_dim, rot = a.rot_dim;
+    const bool live = lane * V < D, turns = lane * V < rot;
     const bool inter = CASE == kAny ? a.interleaved : CASE == kPairs, whole = CASE != kAny || whole_units;
-    // the lane's two runs; lanes past the turned part hold V values in a row
-    const int at0 = turns && !inter ? lane * H : lane * V, at1 = turns && !inter ? at0 + rot / 2 : at0 + H;
+    // the lane's two runs; lanes past the turned part hold V values in a row,
+    // those past the head read its first ones and count for nothing
+    const int at0 = !live ? 0 : turns && !inter ? lane * H : lane * V;
+    const int at1 = turns && !inter ? at0 + rot / 2 : at0 + H;
     const uint32_t mask = GL == 32 ? ~0u : ((1u << (GL & 31)) - 1) << (threadIdx.x % 32 / GL * GL);
     const float inv_d = 1.0f / D;
     float w[V], dw[V] = {};
@@ -198,8 +200,8 @@ __global__ void __launch_bounds__(256, 3)
         const T* wt = static_cast<const T*>(is_q ? a.wq : a.wk);
 #pragma unroll
         for (int v = 0; v < H; ++v) {
-            w[v] = live ? to_float(wt[at0 + v]) : 0.0f;
-            w[H + v] = live ? to_float(wt[at1 + v]) : 0.0f;
+            w[v] = to_float(wt[at0 + v]);
+            w[H + v] = to_float(wt[at1 + v]);
         }
     }
 
@@ -212,7 +214,7 @@ __global__ void __launch_bounds__(256, 3)
         if (rot) {
             const int64_t p = a.positions[t];
             bad = p < 0 || p >= a.table_len;
-            const int64_t at = (bad ? 0 : p) * (rot / 2) + lane * H;
+            const int64_t at = (bad ? 0 : p) * (rot / 2) + (turns ? lane * H : 0);
             if (bad) {
                 if (lane == 0) atomicOr(err, kErrOpPosition);
             } else if (CASE != kAny) {
@@ -222,7 +224,7 @@ __global__ void __launch_bounds__(256, 3)
                                  s = *reinterpret_cast<const float2*>(a.sin + at + v);
                     cs[v] = c.x, cs[v + 1] = c.y, sn[v] = s.x, sn[v + 1] = s.y;
                 }
-            } else if (turns) {
+            } else {
 #pragma unroll
                 for (int v = 0; v < H; ++v) cs[v] = a.cos[at + v], sn[v] = a.sin[at + v];
             }
@@ -242,11 +244,12 @@ __global__ void __launch_bounds__(256, 3)
         }
         // the lane's pairs turned by the angles, back by their negatives
         auto turn = [&](float (&v)[V], bool back) {
-            if (!turns) return;
+            if (!rot) return;
             auto pair = [&](float& x, float& y, int k) {
-                const float s = back ? -sn[k] : sn[k], t = fmaf(x, cs[k], -__fmul_rn(y, s));
-                y = fmaf(y, cs[k], __fmul_rn(x, s));
-                x = t;
+                const float s = back ? -sn[k] : sn[k];
+                const float tx = fmaf(x, cs[k], -__fmul_rn(y, s)), ty = fmaf(y, cs[k], __fmul_rn(x, s));
+                x = turns ? tx : x;
+                y = turns ? ty : y;
             };
             if (inter) {
 #pragma unroll
@@ -262,17 +265,11 @@ __global__ void __launch_bounds__(256, 3)
 #pragma unroll
             for (int k = 0; k < kDepth; ++k) {
                 const int at = min(k, count - 1 - h);
-                x[k][0] = x[k][1] = make_uint2(0, 0);
-                if (live) {
-                    x[k][0] = load_half(x_at + at * in.head_stride + at0, whole);
-                    x[k][1] = load_half(x_at + at * in.head_stride + at1, whole);
-                }
+                x[k][0] = load_half(x_at + at * in.head_stride + at0, whole);
+                x[k][1] = load_half(x_at + at * in.head_stride + at1, whole);
                 if (GRAD) {
-                    g[k][0] = g[k][1] = make_uint2(0, 0);
-                    if (live) {
-                        g[k][0] = load_half(g_at + at * out.head_stride + at0, whole);
-                        g[k][1] = load_half(g_at + at * out.head_stride + at1, whole);
-                    }
+                    g[k][0] = load_half(g_at + at * out.head_stride + at0, whole);
+                    g[k][1] = load_half(g_at + at * out.head_stride + at1, whole);
                 }
             }
 #pragma unroll
@@ -284,6 +281,7 @@ __global__ void __launch_bounds__(256, 3)
                     v[i] = to_float(reinterpret_cast<const T*>(&x[k][i / H])[i % H]);
                     ss = fmaf(v[i], v[i], ss);
                 }
+                ss = live ? ss : 0.0f;
 #pragma unroll
                 for (int o = GL / 2; o; o >>= 1) ss += __shfl_xor_sync(mask, ss, o, GL);
                 const float rstd = inv_sqrt(fmaf(ss, inv_d, a.eps));
@@ -305,6 +303,7 @@ __global__ void __launch_bounds__(256, 3)
                         r[i] = d * w[i];
                         dot = fmaf(r[i], v[i], dot);
                     }
+                    dot = live ? dot : 0.0f;
 #pragma unroll
                     for (int o = GL / 2; o; o >>= 1) dot += __shfl_xor_sync(mask, dot, o, GL);
                     dot *= inv_d;
@@ -419,13 +418,11 @@ Launch plan_rows(const OpContext& x, const heddle_qk_norm_rope_grad_args& g, boo
 template <class T, int GL, bool GRAD>
 void launch_wide(const Launch& l, const OpContext& x, const heddle_qk_norm_rope_grad_args& a, float* partial,
                  cudaStream_t st) {
-    const heddle_qk_norm_rope_args& f = a.fwd;
     const int blocks = l.q_blocks + l.k_blocks;
-    const bool known = l.whole && f.rot_dim == f.head_dim && f.head_dim == GL * (int)(16 / sizeof(T));
-    if (!known)
+    if (!l.whole)
         qk_norm_rope_wide_kernel<T, GL, GRAD, kAny>
             <<<blocks, 256, 0, st>>>(a, partial, x.err, l.q_blocks, l.chunk, l.whole);
-    else if (f.interleaved)
+    else if (a.fwd.interleaved)
         qk_norm_rope_wide_kernel<T, GL, GRAD, kPairs>
             <<<blocks, 256, 0, st>>>(a, partial, x.err, l.q_blocks, l.chunk, l.whole);
     else
