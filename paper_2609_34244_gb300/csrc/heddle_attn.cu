@@ -66,73 +66,83 @@ __global__ void __launch_bounds__(kWarps * 32) attn_row_kernel(heddle_attention_
     }
 }
 
-// Queries that see at most this many keys take delta from the weights
-// themselves: o is rounded to the element type, which is as large an error of
-// dS there as the rounding of dS itself, and fades with more keys.
-constexpr int kFewKeys = 16;
-
-// delta_i = do_i . o_i, or sum_j P_ij (do_i . v_j) where the keys are few, for
-// heads of whole 16-byte units: GL lanes a row, 16 bytes a lane or 16 / GL
-// keys a lane, rows in the order of memory.
+// delta_i = do_i . o_i for heads of whole 16-byte units: GL lanes a row, 16
+// bytes a lane, rows in the order of memory.
 template <class T, int GL>
 __global__ void __launch_bounds__(256) attn_delta_wide_kernel(const __grid_constant__ heddle_attention_grad_args g,
-                                                              float* delta, bool few_exact) {
+                                                              float* delta) {
     const heddle_attention_args& a = g.fwd;
-    const int lane = threadIdx.x % GL, D = a.head_dim;
+    const int lane = threadIdx.x % GL;
     const uint32_t r = blockIdx.x * (256 / GL) + threadIdx.x / GL;  // (b, i, h)
     const uint32_t heads = a.q_heads, n = (uint32_t)a.q_len;
     if (r >= a.batch * heads * n) return;
     const uint32_t h = r % heads, bi = r / heads, i = bi % n, b = bi / n;
-    const int64_t at_row = ((int64_t)b * heads + h) * n + i;
-    const Span sp = span_of(a, b);
-    const int64_t pos = i < sp.ql ? sp.off + i : -1;
-    const int64_t low = a.window && pos + 1 > a.window ? pos + 1 - a.window : 0;
-    const int64_t first = min(a.sinks, low), keys = pos < 0 ? 0 : first + pos + 1 - low;
-    const uint32_t mask = ((1ull << GL) - 1) << (threadIdx.x % 32 / GL * GL);
-    const T* d_o = at<T>(g.d_o, b, i, h);
     float s = 0.0f;
-    if (few_exact && keys > 0 && keys <= kFewKeys) {
-        const int64_t hk = h / (heads / a.kv_heads);
-        const T* q = at<T>(a.q, b, i, h);
-        const float lse = a.lse[at_row];
-        float total = 0.0f;
-        for (int e = lane; e < keys; e += GL) {
-            const int64_t key = e < first ? e : low + e - first;
-            const T *k = at<T>(a.k, b, key, hk), *v = at<T>(a.v, b, key, hk);
-            float qk = 0.0f, dv = 0.0f;
-            for (int c = 0; c < D; c += 8) {
-                const uint4 uq = *reinterpret_cast<const uint4*>(q + c), uk = *reinterpret_cast<const uint4*>(k + c);
-                const uint4 ud = *reinterpret_cast<const uint4*>(d_o + c), uv = *reinterpret_cast<const uint4*>(v + c);
-                const T *tq = reinterpret_cast<const T*>(&uq), *tk = reinterpret_cast<const T*>(&uk);
-                const T *td = reinterpret_cast<const T*>(&ud), *tv = reinterpret_cast<const T*>(&uv);
+    if (lane * 8 < a.head_dim) {
+        const uint4 u = *reinterpret_cast<const uint4*>(at<T>(a.o, b, i, h) + lane * 8);
+        const uint4 w = *reinterpret_cast<const uint4*>(at<T>(g.d_o, b, i, h) + lane * 8);
+        const T *x = reinterpret_cast<const T*>(&u), *y = reinterpret_cast<const T*>(&w);
 #pragma unroll
-                for (int x = 0; x < 8; ++x) {
-                    qk += to_float(tq[x]) * to_float(tk[x]);
-                    dv += to_float(td[x]) * to_float(tv[x]);
-                }
-            }
-            const float w = expf(qk * a.scale - lse);
-            total += w;
-            s += w * dv;
-        }
-#pragma unroll
-        for (int o = GL / 2; o; o >>= 1) {
-            s += __shfl_xor_sync(mask, s, o, GL);
-            total += __shfl_xor_sync(mask, total, o, GL);
-        }
-        s /= total;
-    } else {
-        if (lane * 8 < D) {
-            const uint4 u = *reinterpret_cast<const uint4*>(at<T>(a.o, b, i, h) + lane * 8);
-            const uint4 w = *reinterpret_cast<const uint4*>(d_o + lane * 8);
-            const T *x = reinterpret_cast<const T*>(&u), *y = reinterpret_cast<const T*>(&w);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) s += to_float(x[j]) * to_float(y[j]);
-        }
-#pragma unroll
-        for (int o = GL / 2; o; o >>= 1) s += __shfl_xor_sync(mask, s, o, GL);
+        for (int j = 0; j < 8; ++j) s += to_float(x[j]) * to_float(y[j]);
     }
-    if (lane == 0) delta[at_row] = s;
+    const uint32_t mask = ((1ull << GL) - 1) << (threadIdx.x % 32 / GL * GL);
+#pragma unroll
+    for (int o = GL / 2; o; o >>= 1) s += __shfl_xor_sync(mask, s, o, GL);
+    if (lane == 0) delta[((int64_t)b * heads + h) * n + i] = s;
+}
+
+// Queries that see at most this many keys take delta from the weights
+// instead, sum_j P_ij (do_i . v_j): o is rounded to the element type, which is
+// as large an error of dS there as the rounding of dS itself, and fades with
+// more keys.  They are the first kFewKeys positions of a sequence, or every
+// query of a call whose window and sinks together are no more.
+constexpr int kFewKeys = 16;
+
+// 16 lanes a row, a key each; `per` rows a head: the queries of the first
+// `per` positions, or (all) the first `per` queries.
+template <class T>
+__global__ void __launch_bounds__(256) attn_few_delta_kernel(const __grid_constant__ heddle_attention_grad_args g,
+                                                             float* delta, int64_t per, bool all) {
+    const heddle_attention_args& a = g.fwd;
+    const int lane = threadIdx.x % kFewKeys, D = a.head_dim;
+    const int64_t r = (int64_t)blockIdx.x * (256 / kFewKeys) + threadIdx.x / kFewKeys;  // (b, h, e)
+    if (r >= a.batch * a.q_heads * per) return;
+    const int64_t e = r % per, h = r / per % a.q_heads, b = r / (per * a.q_heads);
+    const Span sp = span_of(a, b);
+    const int64_t i = all ? e : e - sp.off, pos = sp.off + i;
+    if (i < 0 || i >= sp.ql || pos < 0) return;
+    const int64_t low = a.window && pos + 1 > a.window ? pos + 1 - a.window : 0;
+    const int64_t first = min(a.sinks, low), keys = first + pos + 1 - low;
+    if (keys > kFewKeys) return;
+    const int64_t hk = h / (a.q_heads / a.kv_heads), row = (b * a.q_heads + h) * a.q_len + i;
+    const uint32_t mask = 0xffffu << (threadIdx.x % 32 / kFewKeys * kFewKeys);
+    float s = 0.0f, total = 0.0f;
+    if (lane < keys) {
+        const int64_t key = lane < first ? lane : low + lane - first;
+        const T *q = at<T>(a.q, b, i, h), *d_o = at<T>(g.d_o, b, i, h);
+        const T *k = at<T>(a.k, b, key, hk), *v = at<T>(a.v, b, key, hk);
+        float qk = 0.0f, dv = 0.0f;
+#pragma unroll 4
+        for (int c = 0; c < D; c += 8) {
+            const uint4 uq = *reinterpret_cast<const uint4*>(q + c), uk = *reinterpret_cast<const uint4*>(k + c);
+            const uint4 ud = *reinterpret_cast<const uint4*>(d_o + c), uv = *reinterpret_cast<const uint4*>(v + c);
+            const T *tq = reinterpret_cast<const T*>(&uq), *tk = reinterpret_cast<const T*>(&uk);
+            const T *td = reinterpret_cast<const T*>(&ud), *tv = reinterpret_cast<const T*>(&uv);
+#pragma unroll
+            for (int x = 0; x < 8; ++x) {
+                qk += to_float(tq[x]) * to_float(tk[x]);
+                dv += to_float(td[x]) * to_float(tv[x]);
+            }
+        }
+        total = expf(qk * a.scale - a.lse[row]);
+        s = total * dv;
+    }
+#pragma unroll
+    for (int o = kFewKeys / 2; o; o >>= 1) {
+        s += __shfl_xor_sync(mask, s, o, kFewKeys);
+        total += __shfl_xor_sync(mask, total, o, kFewKeys);
+    }
+    if (lane == 0) delta[row] = s / total;
 }
 
 bool units16(const heddle_heads& t) {
@@ -230,13 +240,17 @@ cudaError_t attention_grad(const OpContext& x, const heddle_attention_grad_args&
     const bool tc = attn_tc_takes_grad(g);
     if (rows && a.head_dim % 8 == 0 && a.head_dim <= 128 && units16(a.o) && units16(g.d_o)) {
         if (a.head_dim <= 64)
-            attn_delta_wide_kernel<T, 8><<<(unsigned)ceil_div(rows, 32), 256, 0, st>>>(g, delta, tc);
+            attn_delta_wide_kernel<T, 8><<<(unsigned)ceil_div(rows, 32), 256, 0, st>>>(g, delta);
         else
-            attn_delta_wide_kernel<T, 16><<<(unsigned)ceil_div(rows, 16), 256, 0, st>>>(g, delta, tc);
+            attn_delta_wide_kernel<T, 16><<<(unsigned)ceil_div(rows, 16), 256, 0, st>>>(g, delta);
     } else if (rows) {
         attn_delta_kernel<T><<<row_blocks(x, rows), kWarps * 32, 0, st>>>(g, delta);
     }
     if (tc) {
+        const bool all = a.window && a.window + a.sinks <= kFewKeys;
+        const int64_t per = all || a.q_len < kFewKeys ? a.q_len : kFewKeys;
+        attn_few_delta_kernel<T><<<(unsigned)ceil_div(a.batch * a.q_heads * per, 256 / kFewKeys), 256, 0, st>>>(
+            g, delta, per, all || a.q_len < kFewKeys);
         const cudaError_t e = cudaGetLastError();
         return e == cudaSuccess ? launch_attn_tc_grad(x, g, delta, rest, st) : e;
     }

@@ -56,6 +56,7 @@ PRODUCTS = [
     # m, n, k
     (1, 1, 1), (1, 17, 1), (5, 3, 7), (64, 64, 64), (1, 256, 512), (3, 130, 1000), (128, 256, 64), (129, 257, 65),
     (255, 511, 200), (300, 40, 1031), (33, 1200, 4096), (513, 72, 9), (2, 100, 20000),
+    (640, 1300, 520), (1025, 2304, 264), (64, 2600, 128), (17, 4500, 320),
 ]
 
 
@@ -382,6 +383,8 @@ ATTENTION = [
     (2, 100, 40, 2, 1, 64, 0, 0, None), (1, 40, 600, 7, 1, 80, 200, 0, None), (2, 5, 0, 2, 1, 64, 0, 0, None),
     (2, 60, 300, 2, 1, 128, 33, 2, "short"), (1, 90, 90, 2, 1, 160, 20, 1, None), (2, 64, 64, 4, 2, 33, 0, 0, "both"),
     (1, 500, 500, 16, 1, 64, 77, 5, None), (1, 260, 1100, 1, 1, 128, 300, 150, None),
+    (2, 1100, 1100, 8, 2, 64, 257, 130, "both"), (1, 1500, 1500, 4, 4, 128, 0, 0, None),
+    (1, 3, 3000, 9, 3, 128, 0, 0, None), (2, 130, 130, 4, 1, 64, 3, 2, None), (1, 70, 70, 128, 1, 64, 0, 0, None),
 ]
 
 
@@ -510,6 +513,67 @@ def test_attention_repeats(lib):
         h.heddle_attention_backward(ctx, do, q, k, v, o, lse, *d, window=100)
         got.append((o, lse, *d))
     assert all(torch.equal(a, b) for a, b in zip(*got))
+
+
+def test_offsets_past_32_bits(lib):
+    """Rows and tokens that lie more than 2^31 elements apart."""
+    h, ctx = lib
+    g = gen(51)
+    far = 1 << 30  # elements: the third row and the third head start past 2^31
+    room = torch.empty(2 * far + (1 << 20), dtype=torch.bfloat16, device="cuda")
+    x = room.as_strided((3, 72), (far, 1))
+    x.copy_(rand(g, 3, 72, dt=x.dtype))
+    w = rand(g, 40, 72, dt=x.dtype, std=0.1)
+    y = room[4096:].as_strided((3, 40), (far, 1))
+    h.heddle_linear(ctx, x, w, y)
+    _, _, want, ey = R.linear(x, w, None, None, "none")
+    R.close(y, want, ey, "y")
+    step = (2 * far) // 199 // 8 * 8
+    k, v = (room[8192 + 512 * i:].as_strided((1, 200, 1, 64), (0, step, 64, 1)) for i in range(2))
+    for t in (k, v):
+        t.copy_(rand(g, 1, 200, 1, 64, dt=x.dtype))
+    q, do = rand(g, 1, 200, 2, 64, dt=x.dtype), rand(g, 1, 200, 2, 64, dt=x.dtype)
+    o, lse = torch.empty_like(q), torch.empty(1, 2, 200, device="cuda")
+    h.heddle_attention(ctx, q, k, v, o, lse)
+    dq = torch.empty_like(q)
+    dk, dv = (room[16384 + 512 * i:].as_strided((1, 200, 1, 64), (0, step, 64, 1)) for i in range(2))
+    h.heddle_attention_backward(ctx, do, q, k, v, o, lse, dq, dk, dv)
+    both = [R.attention(q[0, :, j], k[0, :, 0], v[0, :, 0], 200, 200, 0, 0, 0.125, do[0, :, j]) for j in range(2)]
+    for j in range(2):
+        R.close(o[0, :, j], *both[j]["o"], "o")
+        R.close(dq[0, :, j], *both[j]["dq"], "dq")
+    for got, n in ((dk, "dk"), (dv, "dv")):
+        value = both[0][n][0] + both[1][n][0]
+        bound = both[0][n][1] + both[1][n][1] + 2.0 ** -22 * (both[0][n][0].abs() + both[1][n][0].abs())
+        R.close(got[0, :, 0], value, bound, n)
+
+
+def test_captured_calls_repeat(lib):
+    """A graph of calls whose scratch exists takes new inputs in place."""
+    h, ctx = lib
+    g = gen(61)
+    x, w = rand(g, 100, 136, dt=torch.bfloat16), rand(g, 72, 136, dt=torch.bfloat16, std=0.1)
+    q, k = rand(g, 1, 100, 2, 64, dt=torch.bfloat16), rand(g, 1, 100, 1, 64, dt=torch.bfloat16)
+    y, o = torch.empty(100, 72, dtype=x.dtype, device="cuda"), torch.empty_like(q)
+    lse = torch.empty(1, 2, 100, device="cuda")
+    grads = [torch.empty_like(t) for t in (q, k, k)]
+
+    def calls():
+        h.heddle_linear(ctx, x, w, y, act=h.ACT_SILU)
+        h.heddle_attention(ctx, q, k, k, o, lse, window=30)
+        h.heddle_attention_backward(ctx, q, q, k, k, o, lse, *grads, window=30)
+
+    calls()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        calls()
+    x.mul_(0.5)
+    q.mul_(2)
+    graph.replay()
+    got = [t.clone() for t in (y, o, *grads)]
+    calls()
+    assert all(torch.equal(a, b) for a, b in zip(got, (y, o, *grads)))
 
 
 # -------------------------------------------------------------------- refusals
