@@ -78,7 +78,7 @@ struct Shape {
     static constexpr int kTileM = PAIR ? 2 * BM : BM;
     static constexpr int kRowsB = PAIR ? BN / 2 : BN;  // rows of B in this CTA
     static constexpr int kStageA = BM * BK * 2, kStageB = kRowsB * BK * 2;
-    static constexpr int kTmem = 2 * BN;  // both halves of tensor memory in use
+    static constexpr int kTmem = BN > 128 ? 512 : 2 * BN;  // both halves of tensor memory in use
 };
 
 // Tiles in order of groups of 16 tile rows, column by column within one: the
@@ -434,7 +434,7 @@ __global__ void __launch_bounds__(kThreads, 1)
 
 // ---------------------------------------------------------------- operands
 
-// Rows of `cols` 16-bit values to rows at a stride of whole 16-byte units, of
+// Rows of `cols` 16-bit values to rows at a stride of whole 128-byte lines, of
 // up to four operands in one launch.
 struct LayOut {
     const uint16_t* src[4];
@@ -501,15 +501,19 @@ Plan plan_of(const GemmArgs& g) {
     p.b_count = g.kind == kGemmGated ? 2 : p.a_count;
     return p;
 }
-bool same(const GemmOperand& a, const GemmOperand& b) { return a.p == b.p && a.ld == b.ld; }
-
-// Adds the operand to `l` where copies do not take it as it is.
+// Adds the operand to `l` where copies do not take it as it is, once if it is
+// there already.
 void lay_out(GemmOperand& o, int64_t rows, int64_t cols, unsigned char*& ws, LayOut& l, int& n) {
     const int64_t ld = laid_ld(cols);
     if (copies_as_is(o, rows)) {
         if (rows == 1) o.ld = ld;
         return;
     }
+    for (int i = 0; i < n; ++i)
+        if (l.src[i] == o.p && l.ld[i] == o.ld && l.rows[i] == rows && l.cols[i] == cols) {
+            o = {l.dst[i], ld};
+            return;
+        }
     l.src[n] = static_cast<const uint16_t*>(o.p), l.dst[n] = reinterpret_cast<uint16_t*>(ws);
     l.ld[n] = o.ld, l.dld[n] = ld, l.rows[n] = rows, l.cols[n] = cols;
     o = {ws, ld};
@@ -595,28 +599,30 @@ struct Tile {
 };
 
 // The tile that finishes first by the cycles a 64-wide step of its products
-// takes (measured on steps from L2: what is fetched bounds all but the pair)
-// and the rounds of tiles that the SMs run, plus the epilogue of the last one.
+// takes (measured on steps from L2: what is fetched bounds all but the pair),
+// the rounds of tiles that the SMs run, and the last one's epilogue, about 60
+// cycles a column.
 Tile choose_tile(const OpContext& x, const GemmArgs& g) {
     const int64_t batch = g.kind == kGemmPair ? g.count : 1;
     const int64_t steps = ceil_div(g.K, BK) * (g.kind == kGemmSum ? g.count : 1);
     const struct {
         Tile t;
-        double cycles, end;
-    } all[] = {{{256, true}, 545, 5000}, {{256, false}, 660, 5000}, {{128, false}, 440, 3500}, {{64, false}, 340, 2800},
-               {{32, false}, 300, 2500}};
+        double cycles;
+    } all[] = {{{256, true}, 545}, {{224, true}, 485}, {{192, true}, 425}, {{256, false}, 660},
+               {{128, false}, 440}, {{64, false}, 340}, {{32, false}, 300}};
     Tile best{256, false};
     double least = 1e300;
     for (const auto& c : all) {
         if (c.t.bn < 64 && (g.kind != kGemmLinear || g.M > 64)) continue;  // 32 columns of C at least
         if (c.t.pair && g.M <= BM) continue;
+        if (c.t.pair && c.t.bn < 256 && g.kind != kGemmLinear) continue;  // B's halves in whole copies
         const int out = g.kind == kGemmGated ? c.t.bn / 2 : c.t.bn;
         const int64_t tiles = ceil_div(g.M, c.t.pair ? 2 * BM : BM) * ceil_div(g.N, out) * batch;
         const int64_t at_once = c.t.pair ? x.num_sms / 2 : x.num_sms;
         // few rows: B streams from memory, a step as long as its bytes' share
         double cycles = c.cycles;
         if (g.M <= 64) cycles = c.t.bn * 2.2;
-        const double time = (double)ceil_div(tiles, at_once) * steps * cycles + c.end;
+        const double time = (double)ceil_div(tiles, at_once) * steps * cycles + 60.0 * c.t.bn;
         if (time < least) least = time, best = c.t;
     }
     return best;
@@ -625,6 +631,10 @@ Tile choose_tile(const OpContext& x, const GemmArgs& g) {
 template <int KIND>
 cudaError_t run_kind(const OpContext& x, Tile t, const CUtensorMap (&a)[2], const CUtensorMap (&b)[2], KernelArgs& p,
                      cudaStream_t st) {
+    if constexpr (KIND == kGemmLinear) {
+        if (t.pair && t.bn == 224) return run<224, KIND, true>(x, a, b, p, st);
+        if (t.pair && t.bn == 192) return run<192, KIND, true>(x, a, b, p, st);
+    }
     if (t.pair) return run<256, KIND, true>(x, a, b, p, st);
     if (t.bn == 256) return run<256, KIND, false>(x, a, b, p, st);
     if (t.bn == 128) return run<128, KIND, false>(x, a, b, p, st);
@@ -643,6 +653,25 @@ size_t gemm_scratch(const OpContext&, const GemmArgs& g) {
     for (int i = 0; i < pl.b_count; ++i)
         if (!copies_as_is(g.b[i], pl.rows[1])) n += align256((size_t)pl.rows[1] * laid_ld(pl.cols[1]) * 2);
     return n;
+}
+
+cudaError_t lay_out_operands(const OpContext& x, GemmArgs* const* list, int count, unsigned char* ws,
+                             cudaStream_t st) {
+    LayOut l{};
+    int n = 0;
+    for (int c = 0; c < count; ++c) {
+        GemmArgs& g = *list[c];
+        const Plan pl = plan_of(g);
+        for (int i = 0; i < pl.a_count; ++i) lay_out(g.a[i], pl.rows[0], pl.cols[0], ws, l, n);
+        for (int i = 0; i < pl.b_count; ++i) lay_out(g.b[i], pl.rows[1], pl.cols[1], ws, l, n);
+    }
+    if (!n) return cudaSuccess;
+    int64_t units = 0;
+    for (int i = 0; i < n; ++i) units = l.rows[i] * l.dld[i] / 8 > units ? l.rows[i] * l.dld[i] / 8 : units;
+    const int64_t most = (int64_t)x.num_sms * 8, want = ceil_div(units, 256 * kLayUnits);
+    const dim3 grid((unsigned)(want < most ? want : most), n);
+    lay_out_kernel<<<grid, 256, 0, st>>>(l);
+    return cudaGetLastError();
 }
 
 cudaError_t launch_gemm(const OpContext& x, const GemmArgs& args, unsigned char* ws, cudaStream_t st) {
@@ -665,21 +694,9 @@ cudaError_t launch_gemm(const OpContext& x, const GemmArgs& args, unsigned char*
     p.a_rows = across_a ? 64 : (int)(g.M < BM ? ceil_div(g.M, 8) * 8 : BM);
     CUtensorMap a[2] = {}, b[2] = {};
     if (g.K > 0) {
-        LayOut l{};
-        int n = 0;
-        const bool same_b = pl.b_count == 2 && same(g.b[0], g.b[1]);
-        for (int i = 0; i < pl.a_count; ++i) lay_out(g.a[i], pl.rows[0], pl.cols[0], ws, l, n);
-        for (int i = 0; i < (same_b ? 1 : pl.b_count); ++i) lay_out(g.b[i], pl.rows[1], pl.cols[1], ws, l, n);
-        if (same_b) g.b[1] = g.b[0];
-        cudaError_t e = cudaSuccess;
-        if (n) {
-            int64_t units = 0;
-            for (int i = 0; i < n; ++i) units = l.rows[i] * l.dld[i] / 8 > units ? l.rows[i] * l.dld[i] / 8 : units;
-            const int64_t most = (int64_t)x.num_sms * 8, want = ceil_div(units, 256 * kLayUnits);
-            const dim3 grid((unsigned)(want < most ? want : most), n);
-            lay_out_kernel<<<grid, 256, 0, st>>>(l);
-            e = cudaGetLastError();
-        }
+        GemmArgs* one = &g;
+        cudaError_t e = lay_out_operands(x, &one, 1, ws, st);
+        if (e != cudaSuccess) return e;
         // whole steps only: columns past the last would be the next row's
         const bool few = g.M <= 64 && !tile.pair && tile.bn <= 64 && !across_b && g.K % BK == 0;
         p.deep = few ? kDeep : 1;

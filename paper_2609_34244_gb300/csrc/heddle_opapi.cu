@@ -231,9 +231,8 @@ heddle_status heddle_linear_backward(heddle_ctx* ctx, const heddle_linear_grad_a
     const bool want_x = a.dx && a.m && a.k, want_w = a.dw && a.n && a.k;
     // with dz in the scratch its stride counts, whatever its base will be
     gx.a[0] = gw.a[0] = own_dz ? hd::GemmOperand{nullptr, ag.lddz} : hd::GemmOperand{a.dy, a.lddy};
-    size_t need = hd::act_grad_scratch(*x, ag);
-    if (want_x) need = need > hd::gemm_scratch(*x, gx) ? need : hd::gemm_scratch(*x, gx);
-    if (want_w) need = need > hd::gemm_scratch(*x, gw) ? need : hd::gemm_scratch(*x, gw);
+    size_t need = (want_x ? hd::gemm_scratch(*x, gx) : 0) + (want_w ? hd::gemm_scratch(*x, gw) : 0);
+    if (need < hd::act_grad_scratch(*x, ag)) need = hd::act_grad_scratch(*x, ag);
     CHECK(reserve(x, dz_bytes + need));
     unsigned char* rest = x->ws + dz_bytes;
     if (own_dz) {
@@ -242,6 +241,11 @@ heddle_status heddle_linear_backward(heddle_ctx* ctx, const heddle_linear_grad_a
     }
     cudaError_t e = cudaSuccess;
     if (ag.dz || ag.dbias) e = hd::launch_act_grad(*x, ag, rest, st);
+    hd::GemmArgs* both[2];
+    int count = 0;
+    if (want_x) both[count++] = &gx;
+    if (want_w) both[count++] = &gw;
+    if (e == cudaSuccess && a.m && a.n && a.k) e = hd::lay_out_operands(*x, both, count, rest, st);
     if (e == cudaSuccess && want_x) e = hd::launch_gemm(*x, gx, rest, st);
     if (e == cudaSuccess && want_w) e = hd::launch_gemm(*x, gw, rest, st);
     return done(x, e, "heddle_linear_backward");
@@ -315,9 +319,7 @@ heddle_status heddle_gated_ffn_backward(heddle_ctx* ctx, const heddle_gated_ffn_
     gw.out[0] = a.dw_gate, gw.out[1] = a.dw_up, gw.ldo = a.lddw;
     // dg and du in the scratch: their stride counts, whatever the base will be
     gx.a[0] = gx.a[1] = gw.a[0] = gw.a[1] = {nullptr, ld};
-    size_t need = 0;
-    if (want_x) need = hd::gemm_scratch(*x, gx);
-    if (want_w) need = need > hd::gemm_scratch(*x, gw) ? need : hd::gemm_scratch(*x, gw);
+    const size_t need = (want_x ? hd::gemm_scratch(*x, gx) : 0) + (want_w ? hd::gemm_scratch(*x, gw) : 0);
     CHECK(reserve(x, 2 * half + need));
     unsigned char* rest = x->ws + 2 * half;
     gx.a[0] = gw.a[0] = {x->ws, ld};
@@ -328,6 +330,11 @@ heddle_status heddle_gated_ffn_backward(heddle_ctx* ctx, const heddle_gated_ffn_
     gg.dy = a.dy, gg.lddy = a.lddy, gg.gate = a.gate, gg.up = a.up, gg.lds = a.lds;
     gg.dg = x->ws, gg.du = x->ws + half, gg.ldo = ld;
     cudaError_t e = a.m && a.n ? hd::launch_gate_grad(*x, gg, st) : cudaSuccess;
+    hd::GemmArgs* both[2];
+    int count = 0;
+    if (want_x) both[count++] = &gx;
+    if (want_w) both[count++] = &gw;
+    if (e == cudaSuccess && a.m && a.n && a.k) e = hd::lay_out_operands(*x, both, count, rest, st);
     if (e == cudaSuccess && want_x) e = hd::launch_gemm(*x, gx, rest, st);
     if (e == cudaSuccess && want_w) e = hd::launch_gemm(*x, gw, rest, st);
     return done(x, e, "heddle_gated_ffn_backward");

@@ -100,6 +100,9 @@ struct GemmArgs {
     int64_t ldp;
 };
 size_t gemm_scratch(const OpContext& x, const GemmArgs& g);
+// Lays out in `ws`, in one launch, what bulk tensor copies do not take as it
+// is of several products' operands (at most four), which then name the copies.
+cudaError_t lay_out_operands(const OpContext& x, GemmArgs* const* list, int count, unsigned char* ws, cudaStream_t st);
 cudaError_t launch_gemm(const OpContext& x, const GemmArgs& g, unsigned char* ws, cudaStream_t st);
 
 // Forward products of up to kGemvRows rows in whole 16-byte units, without
