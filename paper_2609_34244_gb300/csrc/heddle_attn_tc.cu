@@ -83,10 +83,10 @@ struct Params {
     const float* delta;
     int32_t group, tokens;  // G, tokens of a tile
     int32_t q_tiles, kv_tiles;
-    int32_t splits, twins, parts;  // pieces along the keys; twins in each; both together
+    int32_t splits, twins;  // pieces along the keys; whether they are twins
     float scale_log2;
-    float* part_o;    // [parts][batch * q_heads * q_len][head_dim]
-    float* part_lse;  // [parts][batch * q_heads * q_len]
+    float* part_o;    // [splits][batch * q_heads * q_len][head_dim]
+    float* part_lse;  // [splits][batch * q_heads * q_len]
     // backward over keys: the first `lead` key tiles in lead_parts parts along
     // the queries, the others in rest_parts; sums of parts as floats
     int32_t lead, lead_parts, rest_parts;
@@ -193,10 +193,27 @@ __device__ __forceinline__ void load_kv_tile(uint32_t dst, const CUtensorMap* m,
     for (int h = 0; h < DP / 64; ++h) load_4d(dst + h * 16384, m, bar, h * 64, hk, k0, b);
 }
 
-// One row of DP sums times f from tensor memory to memory: 16 bytes at a time
-// where the row allows.
+// Sums times f, and those of a second place times f1 added.
+__device__ __forceinline__ void scale_sums(uint32_t (&v)[32], float f, uint32_t second, float f1) {
+#pragma unroll
+    for (int j = 0; j < 32; ++j) v[j] = __float_as_uint(__uint_as_float(v[j]) * f);
+    if (!second) return;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        uint32_t u[16];
+        tmem_ld16(second + 16 * h, u);
+        wait_ld();
+#pragma unroll
+        for (int j = 0; j < 16; ++j)
+            v[16 * h + j] = __float_as_uint(__uint_as_float(v[16 * h + j]) + __uint_as_float(u[j]) * f1);
+    }
+}
+
+// One row of DP sums times f (and a second place's times f1) from tensor
+// memory to memory: 16 bytes at a time where the row allows.
 template <class T, int DP>
-__device__ __forceinline__ void store_row(uint32_t tmem, T* out, bool live, int D, float f) {
+__device__ __forceinline__ void store_row(uint32_t tmem, T* out, bool live, int D, float f, uint32_t second = 0,
+                                          float f1 = 0.0f) {
     const bool wide = ((uintptr_t)out & 15) == 0;
 #pragma unroll 1
     for (int c = 0; c < DP; c += 32) {
@@ -204,39 +221,40 @@ __device__ __forceinline__ void store_row(uint32_t tmem, T* out, bool live, int 
         uint32_t v[32];
         tmem_ld32(tmem + c, v);
         wait_ld();
+        scale_sums(v, f, second ? second + c : 0u, f1);
         if (!live) continue;
         if (wide && c + 32 <= D) {
 #pragma unroll
             for (int j = 0; j < 32; j += 8) {
                 uint4 u;
-                u.x = pack_two<T>(__uint_as_float(v[j]) * f, __uint_as_float(v[j + 1]) * f);
-                u.y = pack_two<T>(__uint_as_float(v[j + 2]) * f, __uint_as_float(v[j + 3]) * f);
-                u.z = pack_two<T>(__uint_as_float(v[j + 4]) * f, __uint_as_float(v[j + 5]) * f);
-                u.w = pack_two<T>(__uint_as_float(v[j + 6]) * f, __uint_as_float(v[j + 7]) * f);
+                u.x = pack_two<T>(__uint_as_float(v[j]), __uint_as_float(v[j + 1]));
+                u.y = pack_two<T>(__uint_as_float(v[j + 2]), __uint_as_float(v[j + 3]));
+                u.z = pack_two<T>(__uint_as_float(v[j + 4]), __uint_as_float(v[j + 5]));
+                u.w = pack_two<T>(__uint_as_float(v[j + 6]), __uint_as_float(v[j + 7]));
                 *reinterpret_cast<uint4*>(out + c + j) = u;
             }
         } else {
 #pragma unroll
             for (int j = 0; j < 32; ++j)
-                if (c + j < D) out[c + j] = from_float<T>(__uint_as_float(v[j]) * f);
+                if (c + j < D) out[c + j] = from_float<T>(__uint_as_float(v[j]));
         }
     }
 }
 template <int COLS>
-__device__ __forceinline__ void store_floats(uint32_t tmem, float* out, bool live, int D, float f) {
+__device__ __forceinline__ void store_floats(uint32_t tmem, float* out, bool live, int D, float f,
+                                             uint32_t second = 0, float f1 = 0.0f) {
 #pragma unroll 1
     for (int c = 0; c < COLS; c += 32) {
         __syncwarp();
         uint32_t v[32];
         tmem_ld32(tmem + c, v);
         wait_ld();
+        scale_sums(v, f, second ? second + c : 0u, f1);
         if (!live) continue;
 #pragma unroll
         for (int j = 0; j < 32; j += 4)
             if (c + j < D)  // whole units of four: head_dim is a multiple of eight
-                *reinterpret_cast<float4*>(out + c + j) =
-                    make_float4(__uint_as_float(v[j]) * f, __uint_as_float(v[j + 1]) * f, __uint_as_float(v[j + 2]) * f,
-                                __uint_as_float(v[j + 3]) * f);
+                *reinterpret_cast<uint4*>(out + c + j) = make_uint4(v[j], v[j + 1], v[j + 2], v[j + 3]);
     }
 }
 template <class T>
@@ -253,7 +271,7 @@ __device__ __forceinline__ void zero_row(T* out, int D) {
 template <int DP, int NT>
 struct Forward {
     static constexpr int kTileBytes = kTile * DP * 2;
-    static constexpr int kHigh = 2 * NT * 2 * kTile * 4;  // the halves' maxima, by turns
+    static constexpr int kHigh = (2 * NT + 1) * 2 * kTile * 4;  // the halves' maxima, by turns; a twin's statistics
     static constexpr int kRoom = 227 * 1024 - 1024 - 512 - kHigh - NT * kTileBytes;
     static constexpr int kSlots = kRoom / kTileBytes < 8 ? kRoom / kTileBytes : 8;  // K and V tiles by turns
     static constexpr int kBytes = 1024 + (NT + kSlots) * kTileBytes + 512 + kHigh;
@@ -318,8 +336,9 @@ __global__ void __launch_bounds__(Forward<DP, NT>::kThreads, 1)
     unsigned char* ring = base + NT * F::kTileBytes;
     uint64_t* bars = reinterpret_cast<uint64_t*>(ring + F::kSlots * F::kTileBytes);
     const uint32_t full = smem_u32(bars), empty = full + 8 * F::kSlots, q_full = empty + 8 * F::kSlots,
-                   s_full = q_full + 16, p_ready = s_full + 16, o_done = p_ready + 16, met = o_done + 16;
-    volatile uint32_t* gave_up = reinterpret_cast<uint32_t*>(bars + 2 * F::kSlots + 16);
+                   s_full = q_full + 16, p_ready = s_full + 16, o_done = p_ready + 16, met = o_done + 16,
+                   told = met + 64;
+    volatile uint32_t* gave_up = reinterpret_cast<uint32_t*>(bars + 2 * F::kSlots + 18);
     uint32_t* tmem_at = const_cast<uint32_t*>(gave_up) + 1;
     float* highs = reinterpret_cast<float*>(reinterpret_cast<unsigned char*>(bars) + 512);  // [2][NT][2][128]
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
@@ -341,6 +360,7 @@ __global__ void __launch_bounds__(Forward<DP, NT>::kThreads, 1)
             mbar_init(o_done + 8 * q, 1);
         }
         for (int q = 0; q < 8; ++q) mbar_init(met + 8 * q, 2);
+        mbar_init(told, 4);
         *gave_up = 0;
         mbar_fence_init();
     }
@@ -505,24 +525,54 @@ __global__ void __launch_bounds__(Forward<DP, NT>::kThreads, 1)
         }
         fence_after();
         if (go) {
+            // twins: the second tells the first what it has, and the first adds
+            // up both tiles' sums, which lie in the same lanes
+            float f_mine = 1.0f, f_other = 0.0f;
+            bool other = false;
+            float* told_at = highs + 2 * NT * 2 * kTile + row;
+            if (TWINS && q == 1 && side == 0) {
+                told_at[0] = mine > 0 ? top : -INFINITY;
+                told_at[kTile] = mine > 0 ? sum : 0.0f;
+                __syncwarp();
+                if (lane == 0) mbar_arrive(told);
+            }
+            if (TWINS && q == 0) {
+                go = __all_sync(~0u, mbar_wait(told, 0, gave_up));
+                other = w.count[NT - 1] > 0;
+                if (go && other) go = __all_sync(~0u, mbar_wait(o_done + 8, 0, gave_up));
+                fence_after();
+                const float top1 = told_at[0], sum1 = told_at[kTile], both = fmaxf(top, top1);
+                if (both > -INFINITY) {
+                    const float e0 = exp2_fast((top - both) * c), e1 = exp2_fast((top1 - both) * c);
+                    sum = sum * e0 + sum1 * e1;
+                    f_other = e1, top = both;
+                    f_mine = e0;
+                }
+            }
             const bool inside = row < p.group * p.tokens && i < p.a.q_len;
             const bool some = mine > 0 && i < s.ql && !(sum == 0.0f);
             const float f = some ? 1.0f / sum : 0.0f;
             const float lse = some ? (top * c + log2f(sum)) * kLn2 : -INFINITY;
             const int64_t r = ((int64_t)b * p.a.q_heads + h) * p.a.q_len + i;
             const int D = p.a.head_dim, d0 = side * (DP / 2);
-            if (p.parts > 1) {
-                const int part = TWINS ? 2 * split + q : split;
-                const int64_t at = (int64_t)part * p.a.batch * p.a.q_heads * p.a.q_len + r;
-                if (inside && side == 0) p.part_lse[at] = lse;
-                // a part of no weight is not read
-                if (mine > 0) store_floats<DP / 2>(to_acc + d0, p.part_o + at * D + d0, inside && some, D - d0, f);
-            } else {
-                T* out = static_cast<T*>(p.a.o.data) + b * p.a.o.batch_stride + i * p.a.o.token_stride +
-                         h * p.a.o.head_stride + d0;
-                if (mine > 0) store_row<T, DP / 2>(to_acc + d0, out, inside && some, D - d0, f);
-                if (inside && !some) zero_row(out, min(D - d0, DP / 2));
-                if (inside && side == 0 && p.a.lse) p.a.lse[r] = lse;
+            if (go && !(TWINS && q == 1)) {
+                const uint32_t second = to_acc + DP + d0;  // the twin's
+                const float f0 = f * f_mine, f1 = f * f_other;
+                if (p.splits > 1) {
+                    const int64_t at = (int64_t)split * p.a.batch * p.a.q_heads * p.a.q_len + r;
+                    if (inside && side == 0) p.part_lse[at] = lse;
+                    // a part of no weight is not read
+                    if (mine > 0)
+                        store_floats<DP / 2>(to_acc + d0, p.part_o + at * D + d0, inside && some, D - d0, f0,
+                                             other ? second : 0u, f1);
+                } else {
+                    T* out = static_cast<T*>(p.a.o.data) + b * p.a.o.batch_stride + i * p.a.o.token_stride +
+                             h * p.a.o.head_stride + d0;
+                    if (mine > 0)
+                        store_row<T, DP / 2>(to_acc + d0, out, inside && some, D - d0, f0, other ? second : 0u, f1);
+                    if (inside && !some) zero_row(out, min(D - d0, DP / 2));
+                    if (inside && side == 0 && p.a.lse) p.a.lse[r] = lse;
+                }
             }
         }
     }
@@ -543,7 +593,7 @@ __global__ void __launch_bounds__(256) attn_join_kernel(const __grid_constant__ 
     const int64_t rows = p.a.batch * p.a.q_heads * p.a.q_len;
     const int64_t r = (int64_t)blockIdx.x * 8 + threadIdx.x / 32;
     if (r >= rows) return;
-    const float mine = lane < p.parts ? p.part_lse[lane * rows + r] : -INFINITY;
+    const float mine = lane < p.splits ? p.part_lse[lane * rows + r] : -INFINITY;
     float top = mine;
 #pragma unroll
     for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, o));
@@ -551,7 +601,7 @@ __global__ void __launch_bounds__(256) attn_join_kernel(const __grid_constant__ 
     const float total = warp_sum(e);
     const float w = total > 0.0f ? e / total : 0.0f;
     float acc[4] = {};
-    for (int x = 0; x < p.parts; ++x) {
+    for (int x = 0; x < p.splits; ++x) {
         const float f = __shfl_sync(~0u, w, x);
         if (f == 0.0f) continue;
         const float* o = p.part_o + ((int64_t)x * rows + r) * D;
@@ -1177,7 +1227,7 @@ Params params_of(const OpContext& x, const heddle_attention_args& a) {
     p.err = x.err;
     p.sched = x.sched;
     // Parts along the keys where the query tiles are too few for the SMs: at
-    // least two key tiles each, at most 32 with twins (the join holds one a lane).
+    // least two key tiles each, at most 32 (the join holds one a lane).
     const int nt = tiles_per_block(a);
     const int64_t blocks = ceil_div(p.q_tiles, nt) * a.kv_heads * a.batch;
     int64_t keys = a.kv_len;
@@ -1188,11 +1238,10 @@ Params params_of(const OpContext& x, const heddle_attention_args& a) {
     int64_t parts = x.num_sms / blocks;
     const int64_t most = keys / (2 * kTile);
     parts = parts < most ? parts : most;
-    parts = parts < 1 ? 1 : parts > 16 ? 16 : parts;
+    parts = parts < 1 ? 1 : parts > 32 ? 32 : parts;
     p.splits = (int32_t)parts;
     // a single query tile leaves half of a CTA idle: it takes the tile twice
     p.twins = nt == 1 && keys >= 4 * kTile * parts;
-    p.parts = p.splits * (p.twins ? 2 : 1);
     // Backward over keys: blocks enough for the SMs, of four query tiles at
     // least; the tiles of the first tokens, which every query sees, in parts
     // of about the query tiles that a window's key tile has.
@@ -1227,7 +1276,7 @@ cudaError_t forward(int device, const Params& p, const CUtensorMap& q, const CUt
     if (e != cudaSuccess) return e;
     const int64_t pieces = ceil_div(p.q_tiles, TWINS ? 1 : NT) * p.a.batch * p.a.kv_heads * p.splits;
     f<<<(unsigned)pieces, F::kThreads, F::kBytes, st>>>(q, k, v, p);
-    if (p.parts > 1) {
+    if (p.splits > 1) {
         const int64_t rows = p.a.batch * p.a.q_heads * p.a.q_len;
         attn_join_kernel<T><<<(unsigned)ceil_div(rows, 8), 256, 0, st>>>(p);
     }
@@ -1290,15 +1339,15 @@ bool attn_tc_takes_grad(const heddle_attention_grad_args& g) {
 
 size_t attn_tc_scratch(const OpContext& x, const heddle_attention_args& a) {
     const Params p = params_of(x, a);
-    if (p.parts == 1) return 0;
-    const size_t rows = (size_t)(a.batch * a.q_heads * a.q_len) * p.parts;
+    if (p.splits == 1) return 0;
+    const size_t rows = (size_t)(a.batch * a.q_heads * a.q_len) * p.splits;
     return align256(rows * a.head_dim * 4) + align256(rows * 4);
 }
 
 cudaError_t launch_attn_tc(const OpContext& x, const heddle_attention_args& a, unsigned char* ws, cudaStream_t st) {
     Params p = params_of(x, a);
-    if (p.parts > 1) {
-        const size_t rows = (size_t)(a.batch * a.q_heads * a.q_len) * p.parts;
+    if (p.splits > 1) {
+        const size_t rows = (size_t)(a.batch * a.q_heads * a.q_len) * p.splits;
         p.part_o = reinterpret_cast<float*>(ws);
         p.part_lse = reinterpret_cast<float*>(ws + align256(rows * a.head_dim * 4));
     }
