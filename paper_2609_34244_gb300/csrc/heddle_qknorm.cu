@@ -165,8 +165,9 @@ __device__ __forceinline__ float inv_sqrt(float v) {
 // What the kernel knows of a call beforehand.  kAny: nothing.  kHalves and
 // kPairs: the layout of the pairs, and that all lies at whole units; two
 // thirds of the instructions then (16384 tokens of 72 heads of 128 bfloat16,
-// forward: 186 us as kAny).
-enum RotaryCase { kAny, kHalves, kPairs };
+// forward: 186 us as kAny, 114 us).  kAllHalves and kAllPairs: also that every
+// lane has values and turns them, as most models' heads do (108 us).
+enum RotaryCase { kAny, kHalves, kPairs, kAllHalves, kAllPairs };
 
 // A head of whole 16-byte units in a group of GL lanes, V values a lane, the
 // last lanes idle where head_dim / V is not GL.  A lane's values are two runs
@@ -186,9 +187,10 @@ __global__ void __launch_bounds__(256, 3)
     const int heads = is_q ? a.q_heads : a.k_heads, chunks = (heads + chunk - 1) / chunk;
     const heddle_heads in = is_q ? a.q : a.k, out = is_q ? a.q_out : a.k_out, dst = is_q ? ga.dq : ga.dk;
     const int lane = threadIdx.x % GL, group = threadIdx.x / GL;
-    const int D = a.head_dim, rot = a.rot_dim;
-    const bool live = lane * V < D, turns = lane * V < rot;
-    const bool inter = CASE == kAny ? a.interleaved : CASE == kPairs, whole = CASE != kAny || whole_units;
+    constexpr bool kAll = CASE == kAllHalves || CASE == kAllPairs;
+    const int D = kAll ? GL * V : a.head_dim, rot = kAll ? D : a.rot_dim;
+    const bool live = kAll || lane * V < D, turns = kAll || lane * V < rot;
+    const bool inter = CASE == kAny ? a.interleaved : CASE == kPairs || CASE == kAllPairs, whole = CASE != kAny || whole_units;
     // the lane's two runs; lanes past the turned part hold V values in a row,
     // those past the head read its first ones and count for nothing
     const int at0 = !live ? 0 : turns && !inter ? lane * H : lane * V;
@@ -419,15 +421,13 @@ template <class T, int GL, bool GRAD>
 void launch_wide(const Launch& l, const OpContext& x, const heddle_qk_norm_rope_grad_args& a, float* partial,
                  cudaStream_t st) {
     const int blocks = l.q_blocks + l.k_blocks;
-    if (!l.whole)
-        qk_norm_rope_wide_kernel<T, GL, GRAD, kAny>
-            <<<blocks, 256, 0, st>>>(a, partial, x.err, l.q_blocks, l.chunk, l.whole);
-    else if (a.fwd.interleaved)
-        qk_norm_rope_wide_kernel<T, GL, GRAD, kPairs>
-            <<<blocks, 256, 0, st>>>(a, partial, x.err, l.q_blocks, l.chunk, l.whole);
-    else
-        qk_norm_rope_wide_kernel<T, GL, GRAD, kHalves>
-            <<<blocks, 256, 0, st>>>(a, partial, x.err, l.q_blocks, l.chunk, l.whole);
+    const bool all = a.fwd.rot_dim == a.fwd.head_dim && a.fwd.head_dim == GL * (int)(16 / sizeof(T));
+    auto* kernel = !l.whole            ? qk_norm_rope_wide_kernel<T, GL, GRAD, kAny>
+                   : a.fwd.interleaved ? (all ? qk_norm_rope_wide_kernel<T, GL, GRAD, kAllPairs>
+                                              : qk_norm_rope_wide_kernel<T, GL, GRAD, kPairs>)
+                                       : (all ? qk_norm_rope_wide_kernel<T, GL, GRAD, kAllHalves>
+                                              : qk_norm_rope_wide_kernel<T, GL, GRAD, kHalves>);
+    kernel<<<blocks, 256, 0, st>>>(a, partial, x.err, l.q_blocks, l.chunk, l.whole);
 }
 
 template <class T, bool GRAD>
