@@ -67,7 +67,8 @@ __global__ void __launch_bounds__(kWarps * 32) attn_row_kernel(heddle_attention_
 }
 
 // delta_i = do_i . o_i for heads of whole 16-byte units: GL lanes a row, 16
-// bytes a lane, rows in the order of memory.
+// bytes a lane, rows in the order of memory.  Bound by memory: 67 MB in 14 us
+// with its launch (4096 tokens of 32 heads of 128; a warp a row took 33).
 template <class T, int GL>
 __global__ void __launch_bounds__(256) attn_delta_wide_kernel(const __grid_constant__ heddle_attention_grad_args g,
                                                               float* delta) {

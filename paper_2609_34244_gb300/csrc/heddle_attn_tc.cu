@@ -268,6 +268,14 @@ __device__ __forceinline__ void zero_row(T* out, int D) {
 // warps each: two threads a row, half of the columns each (one warp a row
 // left its scheduler idle most of the time).  While one tile's warps turn
 // scores into weights the tensor cores run the other's products.
+//
+// A step of 128 x 128 scores is 2 x 512 cycles of the tensor cores and as long
+// a chain of trips to tensor memory (some 600 cycles each), barriers and 128
+// exponentials a thread; the two tiles hide each other's.  Bound by that chain
+// where sequences are short, with the prologue and epilogue of a CTA: two
+// causal sequences of 2048, 32 heads over 8 of 128, 84 us (8.2e14 operations a
+// second); by the tensor cores and the exponentials together where they are
+// long: one of 8192 takes 433 us (1.27e15).
 template <int DP, int NT>
 struct Forward {
     static constexpr int kTileBytes = kTile * DP * 2;
@@ -586,7 +594,10 @@ __global__ void __launch_bounds__(Forward<DP, NT>::kThreads, 1)
     if (warp == 2) tmem_free(tmem, F::kCols);
 }
 
-// Joins the parts of rows split along the keys, one warp a row.
+// Joins the parts of rows split along the keys, one warp a row: a call of few
+// query tiles takes the keys in parts, enough for every SM.  Single tokens read
+// the cache once: 16 histories of up to 8192 with a window of 4096, 8 key heads
+// of 128, 269 MB in 51 us both kernels (5.2e12 bytes a second).
 template <class T>
 __global__ void __launch_bounds__(256) attn_join_kernel(const __grid_constant__ Params p) {
     const int lane = threadIdx.x % 32, D = p.a.head_dim;
@@ -698,7 +709,10 @@ constexpr int kGradBarBytes = 160;
 // dq of a query tile: dq = scale sum over key tiles of dS K with
 // S = Q K^T, dP = dO V^T, dS = P (dP - delta).  Q and dO stay in shared
 // memory, K and V tiles come in two stages.  Scores of the next tile are
-// computed while this one's are turned into dS (two buffers).
+// computed while this one's are turned into dS (two buffers).  CTAs take one
+// query tile after another, the longest first (a grid of one tile each: 137 us
+// against 119).  Bound by the chain from scores to dS as the forward is:
+// 114 us for two causal sequences of 2048 (32 heads over 8 of 128).
 template <int DP>
 struct GradShape {
     static constexpr int kTileBytes = kTile * DP * 2;
@@ -911,9 +925,14 @@ __device__ __forceinline__ int64_t dkv_slot(const Params& p, bool lead, int tile
 
 // dk and dv of a key tile, over every query tile that sees it (or a part of
 // them: the first tokens of a windowed call are seen by every query, and few
-// key tiles alone would leave SMs idle), the group's heads among its rows.  The scores are computed transposed, keys along the
-// lanes, so that P^T and dS^T are left operands in tensor memory as they come:
-// S^T = K Q^T, dP^T = V dO^T, dv += P^T dO, dk += dS^T Q.
+// key tiles alone would leave SMs idle), the group's heads among its rows, so
+// that no two CTAs add to one result and sums come in one order.  The scores
+// are computed transposed, keys along the lanes, so that P^T and dS^T are left
+// operands in tensor memory as they come: S^T = K Q^T, dP^T = V dO^T,
+// dv += P^T dO, dk += dS^T Q.  The tensor cores are busy half of the time,
+// bound by the chain as above: 101 us for two causal sequences of 2048 (32
+// heads over 8 of 128).  Tiles of 64 queries in two groups of warps by turns
+// took 117: products of 64 columns read their left operand twice as often.
 template <class T, int DP>
 __global__ void __launch_bounds__(kGradThreads, 1)
     attn_dkv_kernel(const __grid_constant__ CUtensorMap mq, const __grid_constant__ CUtensorMap mk,
@@ -1165,7 +1184,8 @@ __global__ void __launch_bounds__(kGradThreads, 1)
     if (warp == 2) tmem_free(tmem, 512);
 }
 
-// Adds up the parts of key tiles, in order: a block for 8 rows of one.
+// Adds up the parts of key tiles, in order: a block for 8 rows of one.  5 us
+// for the windowed call of 4095 tokens whose first tiles come in parts.
 template <class T>
 __global__ void __launch_bounds__(256) attn_dkv_join_kernel(const __grid_constant__ Params p, int is_lead) {
     const int lane = threadIdx.x % 32, D = p.a.head_dim;
@@ -1205,7 +1225,8 @@ cudaError_t heads_map(CUtensorMap* m, const heddle_heads& t, const heddle_attent
                       int box_heads, int box_tokens) {
     const uint64_t row = (uint64_t)(a.head_dim + 7) / 8 * 16;  // where an axis has one entry
     const uint64_t dims[4] = {(uint64_t)a.head_dim, (uint64_t)h, (uint64_t)n, (uint64_t)a.batch};
-    const uint64_t strides[3] = {h == 1 ? row : (uint64_t)t.head_stride * 2, n == 1 ? row : (uint64_t)t.token_stride * 2,
+    const uint64_t strides[3] = {h == 1 ? row : (uint64_t)t.head_stride * 2,
+                                 n == 1 ? row : (uint64_t)t.token_stride * 2,
                                  a.batch == 1 ? row : (uint64_t)t.batch_stride * 2};
     const uint32_t box[4] = {64, (uint32_t)box_heads, (uint32_t)box_tokens, 1};
     return make_map(m, t.data, a.dtype, 4, dims, strides, box);
@@ -1284,7 +1305,8 @@ cudaError_t forward(int device, const Params& p, const CUtensorMap& q, const CUt
 }
 
 template <class T, int DP>
-cudaError_t backward(int device, int sms, const Params& p, const CUtensorMap& q, const CUtensorMap& k, const CUtensorMap& v,
+cudaError_t backward(int device, int sms, const Params& p, const CUtensorMap& q, const CUtensorMap& k,
+                     const CUtensorMap& v,
                      const CUtensorMap& d_o, cudaStream_t st) {
     using G = GradShape<DP>;
     static std::atomic<uint64_t> asked_q{0}, asked_kv{0};
@@ -1329,7 +1351,8 @@ cudaError_t input_maps(const Params& p, CUtensorMap* q, CUtensorMap* k, CUtensor
 // head_dim in whole 16-byte units, at most 128, and bases and strides that
 // bulk tensor copies take; a scale whose sign keeps the order of scores.
 bool attn_tc_takes(const heddle_attention_args& a) {
-    return a.q_len <= kMaxLength && a.kv_len <= kMaxLength && a.head_dim % 8 == 0 && a.head_dim <= 128 && a.q_heads / a.kv_heads <= kTile && a.scale > 0.0f &&
+    return a.q_len <= kMaxLength && a.kv_len <= kMaxLength && a.head_dim % 8 == 0 && a.head_dim <= 128 &&
+           a.q_heads / a.kv_heads <= kTile && a.scale > 0.0f &&
            a.q_len > 0 && a.kv_len > 0 && copies(a.q, a.batch, a.q_len, a.q_heads) &&
            copies(a.k, a.batch, a.kv_len, a.kv_heads) && copies(a.v, a.batch, a.kv_len, a.kv_heads);
 }
@@ -1354,7 +1377,8 @@ cudaError_t launch_attn_tc(const OpContext& x, const heddle_attention_args& a, u
     CUtensorMap q, k, v;
     const cudaError_t e = input_maps(p, &q, &k, &v);
     if (e != cudaSuccess) return e;
-    return a.dtype == HEDDLE_BF16 ? forward_of<__nv_bfloat16>(x.device, p, q, k, v, st) : forward_of<__half>(x.device, p, q, k, v, st);
+    return a.dtype == HEDDLE_BF16 ? forward_of<__nv_bfloat16>(x.device, p, q, k, v, st)
+                                  : forward_of<__half>(x.device, p, q, k, v, st);
 }
 
 size_t attn_tc_grad_scratch(const OpContext& x, const heddle_attention_args& a) {
@@ -1375,8 +1399,10 @@ cudaError_t launch_attn_tc_grad(const OpContext& x, const heddle_attention_grad_
     if (e != cudaSuccess) return e;
     const bool narrow = a.head_dim <= 64;
     if (a.dtype == HEDDLE_BF16)
-        return narrow ? backward<__nv_bfloat16, 64>(x.device, x.num_sms, p, q, k, v, d_o, st) : backward<__nv_bfloat16, 128>(x.device, x.num_sms, p, q, k, v, d_o, st);
-    return narrow ? backward<__half, 64>(x.device, x.num_sms, p, q, k, v, d_o, st) : backward<__half, 128>(x.device, x.num_sms, p, q, k, v, d_o, st);
+        return narrow ? backward<__nv_bfloat16, 64>(x.device, x.num_sms, p, q, k, v, d_o, st)
+                      : backward<__nv_bfloat16, 128>(x.device, x.num_sms, p, q, k, v, d_o, st);
+    return narrow ? backward<__half, 64>(x.device, x.num_sms, p, q, k, v, d_o, st)
+                  : backward<__half, 128>(x.device, x.num_sms, p, q, k, v, d_o, st);
 }
 
 }  // namespace hd

@@ -5,7 +5,10 @@
 // the gated block); every warp an eighth of the contraction, 16 bytes a lane
 // and row, so that a block's whole stream is in flight at once.  Products
 // are summed in 32 bits per lane, across the lanes, then across the warps in
-// order.
+// order.  One row of 4096 x 4096 bfloat16 weights: 7.7 us with its launch,
+// 5.7 us of the kernel alone (5.9e12 bytes a second); the tensor cores' kernel
+// takes 12.9.  From four rows on that one is as fast (11.3 us both), at eight
+// twice as fast, since every row costs this one as many multiply-adds again.
 
 #include "heddle_ops.cuh"
 

