@@ -3,16 +3,21 @@
 Each ``csrc/*.cu`` translation unit compiles in parallel to an object file
 under ``_build/``; the objects link into ``paper_2609_34244_gb300/libheddle.so``
 (CUDA runtime linked statically).  Rebuilds only when a source or header is
-newer than the library.  Works without a GPU (cross-compilation).
+newer than the library.  Works without a GPU (cross-compilation).  The layer
+operators' marshalling of torch tensors, ``csrc/heddle_ops_py.cpp``, becomes
+the Python module ``_heddle_ops.so`` beside it (g++ with the headers of Python
+and of the installed torch).
 """
 
 from __future__ import annotations
 
 import concurrent.futures as cf
 import glob
+import importlib.util
 import os
 import shutil
 import subprocess
+import sysconfig
 
 PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
@@ -20,6 +25,8 @@ CSRC = os.path.join(PKG, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 BUILD = os.path.join(ROOT, "_build")
 LIB = os.path.join(PKG, "libheddle.so")
+BINDING_SOURCE = os.path.join(CSRC, "heddle_ops_py.cpp")
+BINDING = os.path.join(PKG, "_heddle_ops.so")
 
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 NVCC_FLAGS = ["-O3", "-std=c++17", "-lineinfo", "-Xcompiler", "-fPIC", "-Xcompiler", "-O2",
@@ -69,12 +76,43 @@ def stale(variant: str | None = None) -> bool:
     return any(os.path.getmtime(p) > t for p in _deps())
 
 
+def build_binding(force: bool = False) -> str | None:
+    """Compile the operators' marshalling; returns the module's path (None
+    without torch: pricing needs neither)."""
+    spec = importlib.util.find_spec("torch")
+    if spec is None:
+        return None
+    torch = spec.submodule_search_locations[0]
+    deps = [BINDING_SOURCE, os.path.join(INCLUDE, "heddle.h"), os.path.abspath(__file__),
+            os.path.join(torch, "version.py")]
+    if not force and os.path.exists(BINDING) and all(os.path.getmtime(BINDING) >= os.path.getmtime(p) for p in deps):
+        return BINDING
+    tmp = BINDING + ".tmp%d" % os.getpid()
+    cmd = [os.environ.get("CXX") or "g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-I", INCLUDE,
+           "-I", os.path.join(torch, "include"), "-I", os.path.join(torch, "include", "torch", "csrc", "api", "include"),
+           "-I", sysconfig.get_paths()["include"], BINDING_SOURCE, "-o", tmp,
+           "-L", os.path.join(torch, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10"]
+    p = subprocess.run(cmd, capture_output=True, text=True)
+    if p.returncode != 0:
+        raise RuntimeError("compiling the binding failed:\n%s\n%s" % (" ".join(cmd), p.stderr))
+    os.replace(tmp, BINDING)
+    return BINDING
+
+
 def build(force: bool = False, verbose: bool = False, extra: list | None = None, variant: str | None = None) -> str:
     """Compile and link; returns the library path (``variant``: one of
     VARIANTS, built beside the product library)."""
     target = lib_path(variant)
-    if not force and not stale(variant):
-        return target
+    with cf.ThreadPoolExecutor(max_workers=1) as ex:  # beside the library
+        binding = None if variant else ex.submit(build_binding, force)
+        if force or stale(variant):
+            _build_library(target, verbose, extra, variant)
+        if binding:
+            binding.result()
+    return target
+
+
+def _build_library(target, verbose, extra, variant):
     objdir = BUILD if not variant else os.path.join(BUILD, variant)
     os.makedirs(objdir, exist_ok=True)
     cc = nvcc()
@@ -101,7 +139,6 @@ def build(force: bool = False, verbose: bool = False, extra: list | None = None,
     if p.returncode != 0:
         raise RuntimeError("link failed:\n%s\n%s" % (" ".join(cmd), p.stderr))
     os.replace(tmp, target)
-    return target
 
 
 if __name__ == "__main__":

@@ -1,4 +1,6 @@
-"""Thin ctypes binding of ``libheddle.so`` (``include/heddle.h``).
+"""Thin binding of ``libheddle.so`` (``include/heddle.h``): ctypes for pricing,
+compiled marshalling (``csrc/heddle_ops_py.cpp``) for the layer operators,
+whose calls are a few microseconds.
 
 Argument marshalling only: every function has the C name, packs Python /
 numpy / torch arguments into the C structs and raises ``HeddleError`` on a
@@ -11,7 +13,6 @@ from __future__ import annotations
 
 import ctypes as C
 import os
-import struct
 
 import numpy as np
 
@@ -136,33 +137,11 @@ class heddle_attention_grad_args(C.Structure):
                 ("dv", heddle_heads)]
 
 
-def _packer(cls):
-    """What packs a C struct's values, nested structs' in their place, into
-    bytes: a third of the time of filling the struct field by field."""
-    codes = {C.c_int64: "q", C.c_int32: "i", C.c_float: "f", C.c_void_p: "P"}
-
-    def flat(c):
-        return "".join(codes[t] if t in codes else flat(t) for _, t in c._fields_)
-
-    packed = struct.Struct("@" + flat(cls))
-    if packed.size != C.sizeof(cls):
-        raise TypeError("%s is not packed alike" % cls.__name__)
-    return packed.pack
-
-
-_pack_linear = _packer(heddle_linear_args)
-_pack_linear_grad = _packer(heddle_linear_grad_args)
-_pack_gated_ffn = _packer(heddle_gated_ffn_args)
-_pack_gated_ffn_grad = _packer(heddle_gated_ffn_grad_args)
-_pack_qk_norm_rope = _packer(heddle_qk_norm_rope_args)
-_pack_qk_norm_rope_grad = _packer(heddle_qk_norm_rope_grad_args)
-_pack_attention = _packer(heddle_attention_args)
-_pack_attention_grad = _packer(heddle_attention_grad_args)
-
 EXPORTS = ["heddle_create", "heddle_destroy", "heddle_last_error", "heddle_load_cluster",
            "heddle_load_model", "heddle_price_candidates", "heddle_topk_reset", "heddle_topk",
            "heddle_price_topk_host", "heddle_get_tables", "heddle_device_errors",
-           "heddle_count_next", "heddle_work_counters", "heddle_set_search", "heddle_get_search", "heddle_set_thread_search_min",
+           "heddle_count_next", "heddle_work_counters", "heddle_set_search", "heddle_get_search",
+           "heddle_set_thread_search_min",
            "heddle_price_topk", "heddle_topk_noalloc", "heddle_time_phases", "heddle_phase_times",
            "heddle_load_mbs", "heddle_price_mbs", "heddle_price_plans", "heddle_load_experts",
            "heddle_price_tiled", "heddle_set_chunk",
@@ -503,216 +482,97 @@ def heddle_get_search(ctx) -> int:
 #
 # Tensors are torch CUDA tensors of one element type (named outputs and saved
 # values float32), their last axis contiguous; every output is given by the
-# caller.  Shapes and types are checked here, since the C structs carry only
-# one set of sizes; everything else is checked by the library.
+# caller.  The marshalling is compiled (csrc/heddle_ops_py.cpp): it checks
+# shapes and types, since the C structs carry only one set of sizes;
+# everything else is checked by the library.
 
-_torch = None
-_OP_TYPES = {}
-_raw_stream = None
+_ops = None
+_OP_NAMES = ("heddle_linear", "heddle_linear_backward", "heddle_gated_ffn", "heddle_gated_ffn_backward",
+             "heddle_qk_norm_rope", "heddle_qk_norm_rope_backward", "heddle_attention", "heddle_attention_backward")
 
 
 def _op_setup():
-    """What the operators need of torch, looked up once: a call of a few
-    microseconds on the GPU notices every one on the host."""
-    global _torch, _raw_stream
+    """The compiled marshalling, bound to the loaded library once."""
+    global _ops
     import torch
-    _OP_TYPES.update({torch.bfloat16: BF16, torch.float16: FP16, torch.float32: FP32})
-    _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or \
+    try:
+        from . import _heddle_ops
+    except ImportError as e:
+        raise RuntimeError("_heddle_ops.so is not built (%s); run __graft_entry__.build()" % e) from e
+    L = load_library()
+    stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or \
         (lambda device: torch.cuda.current_stream(device).cuda_stream)
-    _torch = torch
-
-
-def _first(what, t, axes):
-    """(shape, element type, its code, device index) of a call's first tensor."""
-    if _torch is None:
-        _op_setup()
-    code = _OP_TYPES.get(t.dtype)
-    if code is None:
-        raise HeddleError(E_ARG, "unsupported element type %s of %s" % (t.dtype, what))
-    shape = t.shape
-    device = t.get_device()
-    if len(shape) != axes or device < 0:
-        raise HeddleError(E_ARG, "%s: expected a CUDA tensor of %d axes, got %s on %s"
-                          % (what, axes, tuple(shape), t.device))
-    return shape, t.dtype, code, device
-
-
-def _axes(what, t, axes):
-    shape = t.shape
-    if len(shape) != axes:
-        raise HeddleError(E_ARG, "%s: expected %d axes, got %s" % (what, axes, tuple(shape)))
-    return shape
-
-
-def _op_call(ctx, fn, args, device, stream):
-    st = fn(ctx, args, _raw_stream(device) if stream is None else getattr(stream, "cuda_stream", stream))
-    if st:
-        _check(ctx, st)
-
-
-def _bad(what, t, shape, dtype):
-    raise HeddleError(E_ARG, "%s: expected a CUDA tensor %s of %s with a contiguous last axis, got %s of %s on %s"
-                      % (what, tuple(shape), dtype, tuple(t.shape), t.dtype, t.device))
-
-
-def _mat(what, t, shape, dtype, device):
-    """(address, row stride) of a [rows][cols] tensor; (0, 0) for None."""
-    if t is None:
-        return 0, 0
-    if t.dtype is not dtype or t.shape != shape or t.get_device() != device:
-        _bad(what, t, shape, dtype)
-    ld, inner = t.stride()
-    if inner != 1 and shape[1] > 1:
-        _bad(what, t, shape, dtype)
-    if ld < shape[1] and shape[0] <= 1:
-        ld = shape[1]
-    return t.data_ptr(), ld
-
-
-def _vec(what, t, n, dtype, device):
-    if t is None:
-        return 0
-    if t.dtype is not dtype or t.shape != (n,) or t.get_device() != device or (n > 1 and t.stride(0) != 1):
-        _bad(what, t, (n,), dtype)
-    return t.data_ptr()
-
-
-def _heads(what, t, shape, dtype, device):
-    """heddle_heads' values of a [batch][tokens][heads][head_dim] tensor, or
-    one without the batch axis."""
-    if t.dtype is not dtype or t.shape != shape or t.get_device() != device:
-        _bad(what, t, shape, dtype)
-    st = t.stride()
-    if st[-1] != 1 and shape[-1] > 1:
-        _bad(what, t, shape, dtype)
-    return t.data_ptr(), st[0] if len(st) == 4 else 0, st[-3], st[-2]
-
-
-def _same_stride(what, a, b):
-    if a[1] != b[1]:
-        raise HeddleError(E_ARG, "%s have different row strides" % what)
-    return a[0], b[0], a[1]
+    _heddle_ops.bind({n: C.cast(getattr(L, n), C.c_void_p).value for n in _OP_NAMES}, HeddleError, stream)
+    _ops = _heddle_ops
+    return _ops
 
 
 def heddle_linear(ctx, x, w, y, bias=None, residual=None, act=ACT_NONE, pre=None, stream=None):
     """y = act(x w^T + bias) + residual; ``pre`` receives the sum before act."""
-    (m, k), dt, code, dev = _first("x", x, 2)
-    n = _axes("w", w, 2)[0]
-    mn = (m, n)
-    a = _pack_linear(m, n, k, code, act, *_mat("x", x, (m, k), dt, dev), *_mat("w", w, (n, k), dt, dev),
-                     _vec("bias", bias, n, dt, dev), *_mat("residual", residual, mn, dt, dev),
-                     *_mat("y", y, mn, dt, dev), *_mat("pre", pre, mn, _torch.float32, dev))
-    _op_call(ctx, load_library().heddle_linear, a, dev, stream)
+    st = (_ops or _op_setup()).linear(ctx, x, w, y, bias, residual, act, pre, stream)
+    if st:
+        _check(ctx, st)
 
 
 def heddle_linear_backward(ctx, dy, x, w, act=ACT_NONE, pre=None, dx=None, dw=None, dbias=None, stream=None):
     """Gradients of heddle_linear; an output that is None is not computed."""
-    (m, k), dt, code, dev = _first("x", x, 2)
-    n = _axes("w", w, 2)[0]
-    mn, mk, nk = (m, n), (m, k), (n, k)
-    a = _pack_linear_grad(m, n, k, code, act, *_mat("dy", dy, mn, dt, dev), *_mat("x", x, mk, dt, dev),
-                          *_mat("w", w, nk, dt, dev), *_mat("pre", pre, mn, _torch.float32, dev),
-                          *_mat("dx", dx, mk, dt, dev), *_mat("dw", dw, nk, dt, dev),
-                          _vec("dbias", dbias, n, dt, dev))
-    _op_call(ctx, load_library().heddle_linear_backward, a, dev, stream)
+    st = (_ops or _op_setup()).linear_backward(ctx, dy, x, w, act, pre, dx, dw, dbias, stream)
+    if st:
+        _check(ctx, st)
 
 
 def heddle_gated_ffn(ctx, x, w_gate, w_up, y, act=ACT_SILU, gate=None, up=None, stream=None):
     """y = act(x w_gate^T) * (x w_up^T); ``gate`` and ``up`` receive the products."""
-    (m, k), dt, code, dev = _first("x", x, 2)
-    n = _axes("w_gate", w_gate, 2)[0]
-    mn, nk, f32 = (m, n), (n, k), _torch.float32
-    saved = _same_stride("gate and up", _mat("gate", gate, mn, f32, dev), _mat("up", up, mn, f32, dev))
-    a = _pack_gated_ffn(m, n, k, code, act, *_mat("x", x, (m, k), dt, dev),
-                        *_mat("w_gate", w_gate, nk, dt, dev), *_mat("w_up", w_up, nk, dt, dev),
-                        *_mat("y", y, mn, dt, dev), *saved)
-    _op_call(ctx, load_library().heddle_gated_ffn, a, dev, stream)
+    st = (_ops or _op_setup()).gated_ffn(ctx, x, w_gate, w_up, y, act, gate, up, stream)
+    if st:
+        _check(ctx, st)
 
 
 def heddle_gated_ffn_backward(ctx, dy, x, w_gate, w_up, gate, up, act=ACT_SILU, dx=None, dwg=None, dwu=None,
                               stream=None):
     """Gradients of heddle_gated_ffn; dx, or dwg and dwu (those of w_gate and
     w_up) together, are not computed where they are None."""
-    (m, k), dt, code, dev = _first("x", x, 2)
-    n = _axes("w_gate", w_gate, 2)[0]
-    mn, mk, nk, f32 = (m, n), (m, k), (n, k), _torch.float32
-    saved = _same_stride("gate and up", _mat("gate", gate, mn, f32, dev), _mat("up", up, mn, f32, dev))
-    dw = _same_stride("dwg and dwu", _mat("dwg", dwg, nk, dt, dev), _mat("dwu", dwu, nk, dt, dev))
-    a = _pack_gated_ffn_grad(m, n, k, code, act, *_mat("dy", dy, mn, dt, dev), *_mat("x", x, mk, dt, dev),
-                             *_mat("w_gate", w_gate, nk, dt, dev), *_mat("w_up", w_up, nk, dt, dev), *saved,
-                             *_mat("dx", dx, mk, dt, dev), *dw)
-    _op_call(ctx, load_library().heddle_gated_ffn_backward, a, dev, stream)
-
-
-def _norm_rope_args(q, k, wq, wk, q_out, k_out, positions, cos, sin, eps, interleaved):
-    shape, dt, code, dev = _first("q", q, 3)
-    t, hq, d = shape
-    keys = (t, _axes("k", k, 3)[1], d)
-    rot = table = 0
-    ptrs = (0, 0, 0)
-    if positions is not None:
-        table, half = angles = _axes("cos", cos, 2)
-        rot = 2 * half
-        ptrs = (_vec("positions", positions, t, _torch.int32, dev), _mat("cos", cos, angles, _torch.float32, dev)[0],
-                _mat("sin", sin, angles, _torch.float32, dev)[0])
-        if not (cos.is_contiguous() and sin.is_contiguous()):
-            raise HeddleError(E_ARG, "cos and sin are contiguous")
-    a = (t, table, hq, keys[1], d, rot, code, 1 if interleaved else 0, eps, 0, *_heads("q", q, shape, dt, dev),
-         *_heads("k", k, keys, dt, dev), _vec("wq", wq, d, dt, dev), _vec("wk", wk, d, dt, dev), *ptrs,
-         *_heads("q_out", q_out, shape, dt, dev), *_heads("k_out", k_out, keys, dt, dev))
-    return a, shape, keys, dt, dev
+    st = (_ops or _op_setup()).gated_ffn_backward(ctx, dy, x, w_gate, w_up, gate, up, act, dx, dwg, dwu, stream)
+    if st:
+        _check(ctx, st)
 
 
 def heddle_qk_norm_rope(ctx, q, k, wq, wk, q_out, k_out, positions=None, cos=None, sin=None, eps=1e-6,
                         interleaved=False, stream=None):
     """Norms and rotation of q and k ([tokens][heads][head_dim]); cos and sin
     are float32 [table_len][rot_dim / 2], no rotation without positions."""
-    a, _, _, _, dev = _norm_rope_args(q, k, wq, wk, q_out, k_out, positions, cos, sin, eps, interleaved)
-    _op_call(ctx, load_library().heddle_qk_norm_rope, _pack_qk_norm_rope(*a), dev, stream)
+    st = (_ops or _op_setup()).qk_norm_rope(ctx, q, k, wq, wk, q_out, k_out, positions, cos, sin, eps, interleaved,
+                                            stream)
+    if st:
+        _check(ctx, st)
 
 
 def heddle_qk_norm_rope_backward(ctx, dq_out, dk_out, q, k, wq, wk, dq, dk, dwq, dwk, positions=None, cos=None,
                                  sin=None, eps=1e-6, interleaved=False, stream=None):
     """Gradients of heddle_qk_norm_rope from those of its outputs; dwq and dwk
     are float32 [head_dim]."""
-    f, shape, keys, dt, dev = _norm_rope_args(q, k, wq, wk, dq_out, dk_out, positions, cos, sin, eps, interleaved)
-    d, f32 = shape[2], _torch.float32
-    a = _pack_qk_norm_rope_grad(*f, *_heads("dq", dq, shape, dt, dev), *_heads("dk", dk, keys, dt, dev),
-                                _vec("dwq", dwq, d, f32, dev), _vec("dwk", dwk, d, f32, dev))
-    _op_call(ctx, load_library().heddle_qk_norm_rope_backward, a, dev, stream)
-
-
-def _attention_args(q, k, v, o, lse, q_lens, kv_lens, window, sinks, scale):
-    shape, dt, code, dev = _first("q", q, 4)
-    b, tq, hq, d = shape
-    _, tk, hk, _ = _axes("k", k, 4)
-    keys = (b, tk, hk, d)
-    if lse is not None and (lse.dtype is not _torch.float32 or lse.shape != (b, hq, tq) or lse.get_device() != dev
-                            or not lse.is_contiguous()):
-        _bad("lse", lse, (b, hq, tq), "float32")
-    i32 = _torch.int32
-    a = (b, tq, tk, hq, hk, d, code, window, sinks, d ** -0.5 if scale is None else scale, 0,
-         *_heads("q", q, shape, dt, dev), *_heads("k", k, keys, dt, dev), *_heads("v", v, keys, dt, dev),
-         *_heads("o", o, shape, dt, dev), 0 if lse is None else lse.data_ptr(), _vec("q_lens", q_lens, b, i32, dev),
-         _vec("kv_lens", kv_lens, b, i32, dev))
-    return a, shape, keys, dt, dev
+    st = (_ops or _op_setup()).qk_norm_rope_backward(ctx, q, k, wq, wk, dq_out, dk_out, positions, cos, sin, eps,
+                                                     interleaved, dq, dk, dwq, dwk, stream)
+    if st:
+        _check(ctx, st)
 
 
 def heddle_attention(ctx, q, k, v, o, lse=None, q_lens=None, kv_lens=None, window=0, sinks=0, scale=None,
                      stream=None):
     """Causal attention of q over k and v ([batch][tokens][heads][head_dim])
     with a sliding window (0: none) and sinks; scale None: head_dim ** -0.5."""
-    a, _, _, _, dev = _attention_args(q, k, v, o, lse, q_lens, kv_lens, window, sinks, scale)
-    _op_call(ctx, load_library().heddle_attention, _pack_attention(*a), dev, stream)
+    st = (_ops or _op_setup()).attention(ctx, q, k, v, o, lse, q_lens, kv_lens, window, sinks, scale, stream)
+    if st:
+        _check(ctx, st)
 
 
 def heddle_attention_backward(ctx, do, q, k, v, o, lse, dq, dk, dv, q_lens=None, kv_lens=None, window=0, sinks=0,
                               scale=None, stream=None):
     """Gradients of heddle_attention from ``do``, with its o and lse."""
-    f, shape, keys, dt, dev = _attention_args(q, k, v, o, lse, q_lens, kv_lens, window, sinks, scale)
-    a = _pack_attention_grad(*f, *_heads("do", do, shape, dt, dev), *_heads("dq", dq, shape, dt, dev),
-                             *_heads("dk", dk, keys, dt, dev), *_heads("dv", dv, keys, dt, dev))
-    _op_call(ctx, load_library().heddle_attention_backward, a, dev, stream)
+    st = (_ops or _op_setup()).attention_backward(ctx, q, k, v, o, lse, q_lens, kv_lens, window, sinks, scale, do,
+                                                  dq, dk, dv, stream)
+    if st:
+        _check(ctx, st)
 
 
 # ------------------------------------------------------------- marshalling helpers
