@@ -107,13 +107,6 @@ template <class T>
 __device__ __forceinline__ float load_one(const void* p, int64_t i) {
     return to_float(static_cast<const T*>(p)[i]);
 }
-template <class T>
-__device__ __forceinline__ void load_four(const void* p, int64_t i, float (&v)[4]) {
-    const uint2 u = *reinterpret_cast<const uint2*>(static_cast<const T*>(p) + i);
-    const T* t = reinterpret_cast<const T*>(&u);
-#pragma unroll
-    for (int j = 0; j < 4; ++j) v[j] = to_float(t[j]);
-}
 
 template <class T>
 __device__ __forceinline__ void store_four(T* p, const float (&v)[4]) {
@@ -128,72 +121,132 @@ __device__ __forceinline__ void store_four(T* p, const float (&v)[4]) {
     }
 }
 
-// Four sums of one row of C from column n on to what heddle_linear stores.
-template <class T>
-__device__ __forceinline__ void finish_linear(const GemmArgs& g, int64_t m, int64_t n, float (&c)[4]) {
-    if (g.bias) {
-        float b[4];
-        load_four<T>(g.bias, n, b);
-#pragma unroll
-        for (int j = 0; j < 4; ++j) c[j] += b[j];
+// How a warp goes over a block of 32 rows x 16 columns: neighbouring lanes on
+// a row of memory, four values each where the alignment allows, else one.
+struct Walk {
+    int row, col;  // a lane's first; the others lie `step` rows apart
+    bool four;
+    __device__ Walk(const KernelArgs& p, int64_t n0) {
+        const int lane = threadIdx.x % 32;
+        four = p.vec && n0 + kCols <= p.g.N;
+        row = four ? lane / 4 : lane / kCols;
+        col = four ? lane % 4 * 4 : lane % kCols;
     }
-    if (g.pre[0]) store_four(g.pre[0] + m * g.ldp + n, c);
-    if (g.act != HEDDLE_ACT_NONE) {
-#pragma unroll
-        for (int j = 0; j < 4; ++j) c[j] = act_value(c[j], g.act);
+    // of a lane's 4 or 16 rows, those that lie in C
+    __device__ int rows(const KernelArgs& p, int64_t m0, int64_t n0) const {
+        const int64_t left = p.g.M - m0 - row;
+        if (left <= 0 || n0 + col >= p.g.N) return 0;
+        return four ? (int)min((left + 7) / 8, (int64_t)4) : (int)min((left + 1) / 2, (int64_t)16);
     }
-    if (g.residual) {
-        float r[4];
-        load_four<T>(g.residual, m * g.ldr + n, r);
+};
+
+// The block's residual, fetched before the sums are waited for: it is added
+// last, and a load behind the stores of another row would wait for memory.
+__device__ __forceinline__ void fetch_residual(const KernelArgs& p, int64_t m0, int64_t n0, uint32_t (&r)[kCols]) {
+    const Walk w(p, n0);
+    const int n = w.rows(p, m0, n0);
+    const uint16_t* at = static_cast<const uint16_t*>(p.g.residual) + (m0 + w.row) * p.g.ldr + n0 + w.col;
+    if (w.four) {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) c[j] += r[j];
+        for (int i = 0; i < 4; ++i) {
+            const uint2 u = i < n ? *reinterpret_cast<const uint2*>(at + i * 8 * p.g.ldr) : make_uint2(0, 0);
+            r[2 * i] = u.x, r[2 * i + 1] = u.y;
+        }
+    } else {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) r[i] = i < n ? at[i * 2 * p.g.ldr] : 0;
     }
 }
 
-// A warp's 32 rows x 16 columns from its transposing tile to out: rows of
-// memory are written by neighbouring lanes, four values each where the
-// alignment allows, else one.
-template <class T, bool LINEAR, class TO>
-__device__ __forceinline__ void store_block(const KernelArgs& p, TO* out, int64_t ld, int64_t m0, int64_t n0,
-                                            const float* t) {
+// heddle_linear's bias, saved sums and activation on a block in its
+// transposing tile.  A loop, not unrolled: sixteen copies of an activation
+// waited for their instructions (1023 x 2047 x 4099 with gelu: 42 us).
+template <class T>
+__device__ __forceinline__ void activate_block(const KernelArgs& p, int64_t m0, int64_t n0, float* t) {
     const GemmArgs& g = p.g;
-    const int lane = threadIdx.x % 32;
-    __syncwarp();
-    if (p.vec && n0 + kCols <= g.N) {
-        const int col = (lane % 4) * 4;
+    const Walk w(p, n0);
+    const int n = w.rows(p, m0, n0);
+    t += w.row * kPitch + w.col;
+    float* pre = g.pre[0] ? g.pre[0] + (m0 + w.row) * g.ldp + n0 + w.col : nullptr;
+    if (w.four) {
+        float b[4] = {};
+        if (g.bias) {
+            const uint2 u = *reinterpret_cast<const uint2*>(static_cast<const T*>(g.bias) + n0 + w.col);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) b[j] = to_float(reinterpret_cast<const T*>(&u)[j]);
+        }
+#pragma unroll 1
+        for (int i = 0; i < n; ++i, t += 8 * kPitch) {
+            float4 f = *reinterpret_cast<const float4*>(t);
+            float c[4] = {f.x + b[0], f.y + b[1], f.z + b[2], f.w + b[3]};
+            if (pre) store_four(pre + i * 8 * g.ldp, c);
+            if (g.act != HEDDLE_ACT_NONE) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) c[j] = act_value(c[j], g.act);
+            }
+            *reinterpret_cast<float4*>(t) = make_float4(c[0], c[1], c[2], c[3]);
+        }
+    } else if (n) {
+        const float b = g.bias ? load_one<T>(g.bias, n0 + w.col) : 0.0f;
+#pragma unroll 1
+        for (int i = 0; i < n; i += 4) {
+            float c[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                c[j] = t[(i + j) * 2 * kPitch] + b;
+                if (pre && i + j < n) pre[(i + j) * 2 * g.ldp] = c[j];
+            }
+#pragma unroll
+            for (int j = 0; j < 4; ++j) t[(i + j) * 2 * kPitch] = act_value(c[j], g.act);
+        }
+    }
+}
+
+// A block from its transposing tile to out, the residual added.
+template <class T, bool RESIDUAL, class TO>
+__device__ __forceinline__ void store_block(const KernelArgs& p, TO* out, int64_t ld, int64_t m0, int64_t n0,
+                                            const float* t, const uint32_t (&r)[kCols]) {
+    const Walk w(p, n0);
+    const int n = w.rows(p, m0, n0);
+    t += w.row * kPitch + w.col;
+    out += (m0 + w.row) * ld + n0 + w.col;
+    if (w.four) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const int row = i * 8 + lane / 4;
-            if (m0 + row >= g.M) continue;
-            const float4 f = *reinterpret_cast<const float4*>(t + row * kPitch + col);
+            const float4 f = *reinterpret_cast<const float4*>(t + i * 8 * kPitch);
             float c[4] = {f.x, f.y, f.z, f.w};
-            if (LINEAR) finish_linear<T>(g, m0 + row, n0 + col, c);
-            store_four(out + (m0 + row) * ld + n0 + col, c);
-        }
-    } else if (n0 + lane % kCols < g.N) {
-        const int64_t n = n0 + lane % kCols;
-        const int64_t first = m0 + lane / kCols;  // every second row
-        const float bias = LINEAR && g.bias ? load_one<T>(g.bias, n) : 0.0f;
-        float c[16], res[16];
+            if (RESIDUAL) {
+                const uint32_t two[2] = {r[2 * i], r[2 * i + 1]};
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {  // all loads before the first store
-            c[i] = t[(2 * i + lane / kCols) * kPitch + lane % kCols] + bias;
-            res[i] = LINEAR && g.residual && first + 2 * i < g.M ? load_one<T>(g.residual, (first + 2 * i) * g.ldr + n)
-                                                                 : 0.0f;
+                for (int j = 0; j < 4; ++j) c[j] += to_float(reinterpret_cast<const T*>(two)[j]);
+            }
+            if (i < n) store_four(out + i * 8 * ld, c);
         }
+    } else {
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
-            const int64_t m = first + 2 * i;
-            if (m >= g.M) break;
-            if (LINEAR) {
-                if (g.pre[0]) g.pre[0][m * g.ldp + n] = c[i];
-                c[i] = act_value(c[i], g.act);
-                if (g.residual) c[i] += res[i];
+            float c = t[i * 2 * kPitch];
+            if (RESIDUAL) {
+                const uint16_t bits = (uint16_t)r[i];
+                c += to_float(*reinterpret_cast<const T*>(&bits));
             }
-            out[m * ld + n] = from_float<TO>(c[i]);
+            if (i < n) out[i * 2 * ld] = from_float<TO>(c);
         }
     }
     __syncwarp();
+}
+
+// What a finished block of 16-bit results goes through.
+template <class T, bool LINEAR>
+__device__ __forceinline__ void finish_block(const KernelArgs& p, void* to, int64_t m0, int64_t n0, float* t,
+                                             const uint32_t (&r)[kCols]) {
+    const GemmArgs& g = p.g;
+    T* out = static_cast<T*>(to);
+    if (LINEAR && (g.bias || g.pre[0] || g.act != HEDDLE_ACT_NONE)) activate_block<T>(p, m0, n0, t);
+    if (LINEAR && g.residual)
+        store_block<T, true>(p, out, g.ldo, m0, n0, t, r);
+    else
+        store_block<T, false>(p, out, g.ldo, m0, n0, t, r);
 }
 
 __device__ __forceinline__ void put_row(float* t, const uint32_t (&v)[kCols], int lane) {
@@ -215,6 +268,8 @@ __global__ void __launch_bounds__(kThreads, 1)
     using S = Shape<BN, PAIR>;
     constexpr bool kAcrossA = KIND == kGemmPair, kAcrossB = KIND == kGemmPair || KIND == kGemmSum;
     constexpr int kOut = KIND == kGemmGated ? BN / 2 : BN;  // columns of C a tile covers
+    // blocks of sums an epilogue warp reads back at a time
+    constexpr int kAhead = KIND == kGemmGated || kOut / 2 < 2 * kCols ? 1 : 2;
     extern __shared__ unsigned char raw[];
     unsigned char* base = raw + ((1024 - (smem_u32(raw) & 1023)) & 1023);
     unsigned char* stages = base;
@@ -386,36 +441,48 @@ __global__ void __launch_bounds__(kThreads, 1)
             const int64_t m0 = (int64_t)tm * S::kTileM + rank * BM + w * 32;
             const bool rows = m0 < p.g.M;
 #pragma unroll 1
-            for (int c = from; c < to; c += kCols) {
+            for (int c = from; c < to; c += kAhead * kCols) {
                 const int64_t n0 = (int64_t)tn * kOut + c;
                 if (!rows || n0 >= p.g.N) break;
-                uint32_t v[kCols], u[kCols];
+                uint32_t v[kAhead][kCols], u[kCols], r[kAhead][kCols];
+                if (KIND == kGemmLinear && p.g.residual) {
+#pragma unroll
+                    for (int h = 0; h < kAhead; ++h) fetch_residual(p, m0, n0 + h * kCols, r[h]);
+                }
                 if (per_tile) {
-                    tmem_ld16(acc + c, v);
+#pragma unroll
+                    for (int h = 0; h < kAhead; ++h) tmem_ld16(acc + c + h * kCols, v[h]);
                     if (KIND == kGemmGated) tmem_ld16(acc + kOut + c, u);
                     wait_ld();
                 } else {
 #pragma unroll
-                    for (int j = 0; j < kCols; ++j) v[j] = u[j] = 0;  // a sum over nothing
+                    for (int j = 0; j < kAhead * kCols; ++j) v[j / kCols][j % kCols] = u[j % kCols] = 0;  // a sum over nothing
                 }
                 if (KIND == kGemmGated) {
                     if (p.g.pre[0]) {
-                        put_row(t0, v, lane);
-                        store_block<float, false>(p, p.g.pre[0], p.g.ldp, m0, n0, t0);
+                        put_row(t0, v[0], lane);
+                        __syncwarp();
+                        store_block<float, false>(p, p.g.pre[0], p.g.ldp, m0, n0, t0, u);
                         put_row(t0, u, lane);
-                        store_block<float, false>(p, p.g.pre[1], p.g.ldp, m0, n0, t0);
+                        __syncwarp();
+                        store_block<float, false>(p, p.g.pre[1], p.g.ldp, m0, n0, t0, u);
                     }
 #pragma unroll
                     for (int j = 0; j < kCols; ++j)
-                        v[j] = __float_as_uint(act_value(__uint_as_float(v[j]), p.g.act) * __uint_as_float(u[j]));
+                        v[0][j] =
+                            __float_as_uint(act_value(__uint_as_float(v[0][j]), p.g.act) * __uint_as_float(u[j]));
                 }
-                put_row(t0, v, lane);
                 constexpr bool kLinear = KIND == kGemmLinear;
-                if (p.g.dtype == HEDDLE_BF16)
-                    store_block<__nv_bfloat16, kLinear>(p, static_cast<__nv_bfloat16*>(p.g.out[z]), p.g.ldo, m0, n0,
-                                                        t0);
-                else
-                    store_block<__half, kLinear>(p, static_cast<__half*>(p.g.out[z]), p.g.ldo, m0, n0, t0);
+#pragma unroll
+                for (int h = 0; h < kAhead; ++h) {
+                    if (h && (c + h * kCols >= to || n0 + h * kCols >= p.g.N)) break;
+                    put_row(t0, v[h], lane);
+                    __syncwarp();
+                    if (p.g.dtype == HEDDLE_BF16)
+                        finish_block<__nv_bfloat16, kLinear>(p, p.g.out[z], m0, n0 + h * kCols, t0, r[h]);
+                    else
+                        finish_block<__half, kLinear>(p, p.g.out[z], m0, n0 + h * kCols, t0, r[h]);
+                }
             }
             fence_before();
             if (lane == 0) {
