@@ -691,14 +691,14 @@ Tile choose_tile(const OpContext& x, const GemmArgs& g) {
     const struct {
         Tile t;
         double cycles;
-    } all[] = {{{256, true}, 545}, {{224, true}, 485}, {{192, true}, 425}, {{256, false}, 660},
-               {{128, false}, 440}, {{64, false}, 340}, {{32, false}, 300}};
+    } all[] = {{{256, true}, 545}, {{224, true}, 485}, {{192, true}, 425}, {{128, true}, 340},
+               {{256, false}, 660},               {{128, false}, 440}, {{64, false}, 340}, {{32, false}, 300}};
     Tile best{256, false};
     double least = 1e300;
     for (const auto& c : all) {
         if (c.t.bn < 64 && (g.kind != kGemmLinear || g.M > 64)) continue;  // 32 columns of C at least
         if (c.t.pair && g.M <= BM) continue;
-        if (c.t.pair && c.t.bn < 256 && g.kind != kGemmLinear) continue;  // B's halves in whole copies
+        if (c.t.pair && c.t.bn % 128 && g.kind != kGemmLinear) continue;  // B's halves in whole copies
         const int out = g.kind == kGemmGated ? c.t.bn / 2 : c.t.bn;
         const int64_t tiles = ceil_div(g.M, c.t.pair ? 2 * BM : BM) * ceil_div(g.N, out) * batch;
         const int64_t at_once = c.t.pair ? x.num_sms / 2 : x.num_sms;
@@ -718,6 +718,7 @@ cudaError_t run_kind(const OpContext& x, Tile t, const CUtensorMap (&a)[2], cons
         if (t.pair && t.bn == 224) return run<224, KIND, true>(x, a, b, p, st);
         if (t.pair && t.bn == 192) return run<192, KIND, true>(x, a, b, p, st);
     }
+    if (t.pair && t.bn == 128) return run<128, KIND, true>(x, a, b, p, st);
     if (t.pair) return run<256, KIND, true>(x, a, b, p, st);
     if (t.bn == 256) return run<256, KIND, false>(x, a, b, p, st);
     if (t.bn == 128) return run<128, KIND, false>(x, a, b, p, st);
