@@ -235,7 +235,7 @@ unsigned row_blocks(const OpContext& x, int64_t rows) {
 
 template <class T>
 cudaError_t attention_grad(const OpContext& x, const heddle_attention_grad_args& g, float* delta, unsigned char* rest,
-                           cudaStream_t st) {
+                           bool keep, cudaStream_t st) {
     const heddle_attention_args& a = g.fwd;
     const int64_t rows = a.batch * a.q_heads * a.q_len, keys = a.batch * a.kv_heads * a.kv_len;
     const bool tc = attn_tc_takes_grad(g);
@@ -253,7 +253,7 @@ cudaError_t attention_grad(const OpContext& x, const heddle_attention_grad_args&
         attn_few_delta_kernel<T><<<(unsigned)ceil_div(a.batch * a.q_heads * per, 256 / kFewKeys), 256, 0, st>>>(
             g, delta, per, all || a.q_len < kFewKeys);
         const cudaError_t e = cudaGetLastError();
-        return e == cudaSuccess ? launch_attn_tc_grad(x, g, delta, rest, st) : e;
+        return e == cudaSuccess ? launch_attn_tc_grad(x, g, delta, rest, keep, st) : e;
     }
     if (rows) {
         attn_dq_row_kernel<T><<<row_blocks(x, rows), kWarps * 32, 0, st>>>(g, delta);
@@ -282,16 +282,16 @@ static size_t delta_bytes(const heddle_attention_args& a) {
     return align256(sizeof(float) * (size_t)(a.batch * a.q_heads * a.q_len));
 }
 
-size_t attention_grad_scratch(const OpContext& x, const heddle_attention_grad_args& g) {
-    return delta_bytes(g.fwd) + (attn_tc_takes_grad(g) ? attn_tc_grad_scratch(x, g.fwd) : 0);
+size_t attention_grad_scratch(const OpContext& x, const heddle_attention_grad_args& g, bool keep) {
+    return delta_bytes(g.fwd) + (attn_tc_takes_grad(g) ? attn_tc_grad_scratch(x, g.fwd, keep) : 0);
 }
 
 cudaError_t launch_attention_grad(const OpContext& x, const heddle_attention_grad_args& g, unsigned char* ws,
-                                  cudaStream_t st) {
+                                  bool keep, cudaStream_t st) {
     float* delta = reinterpret_cast<float*>(ws);
     unsigned char* rest = ws + delta_bytes(g.fwd);
-    return g.fwd.dtype == HEDDLE_BF16 ? attention_grad<__nv_bfloat16>(x, g, delta, rest, st)
-                                      : attention_grad<__half>(x, g, delta, rest, st);
+    return g.fwd.dtype == HEDDLE_BF16 ? attention_grad<__nv_bfloat16>(x, g, delta, rest, keep, st)
+                                      : attention_grad<__half>(x, g, delta, rest, keep, st);
 }
 
 }  // namespace hd

@@ -23,8 +23,9 @@ bool attn_tc_takes(const heddle_attention_args& a);
 bool attn_tc_takes_grad(const heddle_attention_grad_args& g);
 size_t attn_tc_scratch(const OpContext& x, const heddle_attention_args& a);
 cudaError_t launch_attn_tc(const OpContext& x, const heddle_attention_args& a, unsigned char* ws, cudaStream_t st);
-size_t attn_tc_grad_scratch(const OpContext& x, const heddle_attention_args& a);
+// keep: with room for the scores' gradients between the backward's passes
+size_t attn_tc_grad_scratch(const OpContext& x, const heddle_attention_args& a, bool keep);
 cudaError_t launch_attn_tc_grad(const OpContext& x, const heddle_attention_grad_args& g, const float* delta,
-                                unsigned char* ws, cudaStream_t st);
+                                unsigned char* ws, bool keep, cudaStream_t st);
 
 }  // namespace hd

@@ -91,6 +91,13 @@ struct Params {
     // the queries, the others in rest_parts; sums of parts as floats
     int32_t lead, lead_parts, rest_parts;
     float *part_dk, *part_dv;  // [slots][128][head_dim]
+    // dS of pairs of tiles, where it is kept between the backward's passes:
+    // query tile t's key tiles at places from t * ds_stride on, or (0) from
+    // where those that causality leaves to the tiles before it end
+    unsigned char* ds;
+    int64_t ds_head;  // places of a key head
+    int32_t ds_stride, ds_lead, ds_wrap, ds_reach;
+    int32_t hb0, hbs;  // key heads of the batch that a launch takes: the first, how many
     int32_t* sched;  // the next piece of work and the CTAs that are done, zero between launches
     uint32_t* err;
 };
@@ -143,6 +150,18 @@ struct RowMask {
         return bits_between(low - key, pos - key) | bits_between(0, min(sinks - 1, pos) - key);
     }
 };
+
+// Where dS of a pair of tiles lies, among the launch's.  A query tile's near
+// key tiles are consecutive and at most ds_wrap; with no window its last one is
+// at most (t tokens + ds_reach) / 128, and a sum of floors is at most the floor
+// of the sum.
+constexpr int kPlaceBytes = kTile * kTile * 2;
+__host__ __device__ __forceinline__ int64_t ds_row(const Params& p, int64_t t) {
+    return p.ds_stride ? t * p.ds_stride : (p.tokens * (t * (t - 1) / 2) + p.ds_reach * t) / kTile + t;
+}
+__device__ __forceinline__ int ds_col(const Params& p, int tile) {
+    return tile < p.ds_lead ? tile : p.ds_lead + tile % p.ds_wrap;
+}
 
 // Every query of tokens i0 .. i1 - 1 sees every key of the tile at k0.
 __device__ __forceinline__ bool all_visible(const Params& p, const Seq& s, int i0, int i1, int k0) {
@@ -916,6 +935,161 @@ __global__ void __launch_bounds__(kGradThreads, 1)
     if (warp == 2) tmem_free(tmem, 512);
 }
 
+// dq from dS as the pass over keys left it: dq = scale sum over key tiles of
+// dS K, one product of 128 x 128 by 128 x head_dim a step.  Bound by the stream
+// of dS from memory, 32 KB a pair of tiles.  CTAs take one query tile after
+// another, the longest first; sums alternate between two places of tensor
+// memory, so that one tile's result is written under the next one's products.
+template <int DP>
+struct StoredShape {
+    static constexpr int kTileBytes = kTile * DP * 2;
+    static constexpr int kStage = kPlaceBytes + kTileBytes;
+    static constexpr int kStages = DP > 64 ? 3 : 4;
+    static constexpr int kBars = 16 * kStages + 32 + 32;
+    static constexpr int kBytes = 1024 + kStages * kStage + kBars + 32;
+    static constexpr int kThreads = 256;
+};
+
+template <class T, int DP>
+__global__ void __launch_bounds__(StoredShape<DP>::kThreads, 1)
+    attn_dq_stored_kernel(const __grid_constant__ CUtensorMap mk, const __grid_constant__ Params p, const int pieces) {
+    using G = StoredShape<DP>;
+    extern __shared__ unsigned char raw[];
+    unsigned char* base = raw + ((1024 - (smem_u32(raw) & 1023)) & 1023);
+    unsigned char* tail = base + G::kStages * G::kStage;
+    const uint32_t full = smem_u32(tail), empty = full + 8 * G::kStages, done = empty + 8 * G::kStages,
+                   freed = done + 16;
+    const Pieces work{freed + 16, freed + 32, reinterpret_cast<int*>(tail + G::kBars)};
+    volatile uint32_t* gave_up = reinterpret_cast<uint32_t*>(tail + G::kBars + 8);
+    uint32_t* tmem_at = const_cast<uint32_t*>(gave_up) + 1;
+    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+
+    struct Piece {
+        int hb, hk, b, tile, t0;
+        Seq s;
+        KeyTiles keys;
+        __device__ Piece(const Params& p, int id) {
+            hb = id % p.hbs;
+            hk = (p.hb0 + hb) % p.a.kv_heads;
+            b = (p.hb0 + hb) / p.a.kv_heads;
+            tile = p.q_tiles - 1 - id / p.hbs;
+            t0 = tile * p.tokens;
+            s = seq_of(p.a, b);
+            keys = key_tiles(p, s, t0, t0 + p.tokens);
+        }
+    };
+    if (threadIdx.x == 0) {
+        for (int i = 0; i < G::kStages; ++i) {
+            mbar_init(full + 8 * i, 1);
+            mbar_init(empty + 8 * i, 1);
+        }
+        for (int i = 0; i < 2; ++i) {
+            mbar_init(done + 8 * i, 1);
+            mbar_init(freed + 8 * i, 4);
+        }
+        work.init(1 + 4);
+        *gave_up = 0;
+        mbar_fence_init();
+    }
+    if (warp == 2) tmem_alloc(smem_u32(tmem_at), 2 * DP);
+    fence_before();
+    __syncthreads();
+    fence_after();
+    const uint32_t tmem = *tmem_at;
+
+    if (warp == 0 && elect_one()) {
+        int id = blockIdx.x, st = 0;
+        uint32_t phase = 0;
+        bool go = true;
+        for (int it = 0; go; ++it) {
+            if (!work.put(it, id < pieces ? id : -1, gave_up) || id >= pieces) break;
+            const Piece w(p, id);
+            id = (int)gridDim.x + atomicAdd(p.sched, 1);
+            const unsigned char* from = p.ds + (w.hb * p.ds_head + ds_row(p, w.tile)) * kPlaceBytes;
+            for (int j = 0; j < w.keys.count; ++j) {
+                if (!(go = mbar_wait(empty + 8 * st, phase ^ 1, gave_up))) break;
+                const uint32_t to = smem_u32(base + st * G::kStage), bar = full + 8 * st;
+                const int tile = w.keys.at(j);
+                mbar_expect(bar, G::kStage);
+                load_bytes(to, from + (int64_t)ds_col(p, tile) * kPlaceBytes, kPlaceBytes, bar);
+                load_kv_tile<DP>(to + kPlaceBytes, &mk, bar, tile * kTile, w.hk, w.b);
+                if (++st == G::kStages) st = 0, phase ^= 1;
+            }
+        }
+    } else if (warp == 1) {
+        const bool one = elect_one();
+        const uint32_t idesc = instr_desc(p.a.dtype == HEDDLE_BF16, true, true, DP);
+        int st = 0;
+        uint32_t phase = 0, held = 0;
+        bool go = true;
+        for (int it = 0; go; ++it) {
+            const int id = work.get_warp(it, gave_up);
+            if (id < 0) break;
+            const Piece w(p, id);
+            if (!w.keys.count) continue;
+            const uint32_t half = held & 1;
+            if (!(go = __all_sync(~0u, mbar_wait(freed + 8 * half, (held / 2 & 1) ^ 1, gave_up)))) break;
+            for (int j = 0; j < w.keys.count; ++j) {
+                if (!(go = __all_sync(~0u, mbar_wait(full + 8 * st, phase, gave_up)))) break;
+                unsigned char* ds = base + st * G::kStage;
+                const int k0 = w.keys.at(j) * kTile;
+                if (w.s.kl < p.a.kv_len && k0 + kTile > w.s.kl) {  // keys past the sequence
+#pragma unroll 1
+                    for (int r = lane; r < kTile; r += 32) clear_rows<DP>(ds + kPlaceBytes, r, w.s.kl - k0);
+                    fence_async_shared();
+                    __syncwarp();
+                }
+                fence_after();
+                if (one) {
+                    const uint32_t a = smem_u32(ds), b = a + kPlaceBytes;
+#pragma unroll
+                    for (int k = 0; k < kTile / 16; ++k)
+                        mma_ss(tmem + half * DP, smem_desc_units(a + k * 256, 128, kTile * 16),
+                               smem_desc(b + k * 2048, 16384), idesc, j | k);
+                    commit(empty + 8 * st);
+                }
+                if (++st == G::kStages) st = 0, phase ^= 1;
+            }
+            if (go && one) commit(done + 8 * half);
+            ++held;
+        }
+    } else if (warp >= 4) {
+        const int row = (warp % 4) * 32 + lane;
+        const uint32_t lanes = (uint32_t)(warp % 4 * 32) << 16;
+        uint32_t held = 0;
+        for (int it = 0;; ++it) {
+            const int id = work.get_warp(it, gave_up);
+            if (id < 0) break;
+            const Piece w(p, id);
+            const int i = w.t0 + row / p.group, h = w.hk * p.group + row % p.group;
+            const bool inside = row < p.group * p.tokens && i < p.a.q_len;
+            T* out = static_cast<T*>(p.dq.data) + w.b * p.dq.batch_stride + i * p.dq.token_stride +
+                     h * p.dq.head_stride;
+            if (!w.keys.count) {
+                if (inside) zero_row(out, p.a.head_dim);
+                continue;
+            }
+            const uint32_t half = held & 1;
+            if (!__all_sync(~0u, mbar_wait(done + 8 * half, held / 2 & 1, gave_up))) break;
+            ++held;
+            fence_after();
+            store_row<T, DP>(tmem + half * DP + lanes, out, inside, p.a.head_dim, p.a.scale);
+            fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(freed + 8 * half);
+        }
+    }
+    fence_before();
+    __syncthreads();
+    if (*gave_up) {
+        if (threadIdx.x == 0) atomicOr(p.err, kErrOpWait);
+        drain();
+        __syncthreads();
+    }
+    if (threadIdx.x == 0) leave_pieces(p.sched);
+    if (warp == 2) tmem_free(tmem, 2 * DP);
+}
+
 // Where the sums of a key tile's part go.
 __device__ __forceinline__ int64_t dkv_slot(const Params& p, bool lead, int tile, int hb, int part) {
     const int64_t heads = p.a.batch * p.a.kv_heads;
@@ -951,13 +1125,13 @@ __global__ void __launch_bounds__(kGradThreads, 1)
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
 
     // the first keys are seen by the most queries
-    const int64_t heads = p.a.batch * p.a.kv_heads, lead_blocks = heads * p.lead * p.lead_parts;
+    const int64_t heads = p.hbs, lead_blocks = heads * p.lead * p.lead_parts;
     const bool lead = blockIdx.x < lead_blocks;
     const int parts = lead ? p.lead_parts : p.rest_parts;
     int64_t id = lead ? blockIdx.x : blockIdx.x - lead_blocks;
     const int part = (int)(id % parts);
     id /= parts;
-    const int hb = (int)(id % heads), hk = hb % p.a.kv_heads, b = hb / p.a.kv_heads;
+    const int hb = p.hb0 + (int)(id % heads), hk = hb % p.a.kv_heads, b = hb / p.a.kv_heads;
     const int tile = (int)(id / heads);
     const int k0 = (lead ? tile : p.lead + tile) * kTile;
     const int64_t slot = dkv_slot(p, lead, tile, hb, part);
@@ -1150,6 +1324,14 @@ __global__ void __launch_bounds__(kGradThreads, 1)
             fence_before();
             __syncwarp();
             if (lane == 0) mbar_arrive(bar.b_ready);
+            if (p.ds) {  // units of 8 queries, the keys of each one after another: a warp writes 512 bytes at a time
+                const int64_t place = (hb - p.hb0) * p.ds_head + ds_row(p, first + j) + ds_col(p, k0 / kTile);
+                unsigned char* to = p.ds + place * kPlaceBytes + side * (4 * kTile * 16) + row * 16;
+#pragma unroll
+                for (int y = 0; y < 4; ++y)
+                    *reinterpret_cast<uint4*>(to + y * (kTile * 16)) =
+                        make_uint4(w[4 * y], w[4 * y + 1], w[4 * y + 2], w[4 * y + 3]);
+            }
         }
         if (go && n > 0) go = __all_sync(~0u, mbar_wait(bar.done, 0, gave_up));
         fence_after();
@@ -1279,6 +1461,38 @@ Params params_of(const OpContext& x, const heddle_attention_args& a) {
     return p;
 }
 
+// Whether dS is kept for the pass over queries, and its places.  It is where
+// they come to at most kMostKept bytes for as many key heads as the SMs need;
+// beyond, the scores are computed in both passes.  Kept: two causal sequences
+// of 2048 XX us against YY, one of 8192 XX against YY.
+constexpr int64_t kMostKept = (int64_t)4 << 30;
+int64_t keep_ds(const OpContext& x, Params& p) {
+    const heddle_attention_args& a = p.a;
+    const int64_t heads = a.batch * a.kv_heads;
+    p.hb0 = 0, p.hbs = (int32_t)heads;
+    p.ds_lead = a.window ? (int32_t)ceil_div(a.sinks < a.kv_len ? a.sinks : a.kv_len, kTile) : 0;
+    const int64_t wrap = a.window ? (a.window + p.tokens - 2) / kTile + 2 : p.kv_tiles;
+    if (p.ds_lead + wrap >= p.kv_tiles)
+        p.ds_lead = 0, p.ds_wrap = p.kv_tiles;
+    else
+        p.ds_wrap = (int32_t)wrap;
+    p.ds_stride = p.ds_lead + p.ds_wrap;
+    p.ds_head = ds_row(p, p.q_tiles);
+    if (a.q_lens == a.kv_lens) {  // queries end where keys do: at most as many keys ahead as there are more
+        Params q = p;
+        const int64_t more = a.kv_len > a.q_len ? a.kv_len - a.q_len : 0;
+        q.ds_stride = 0, q.ds_lead = 0, q.ds_wrap = p.kv_tiles, q.ds_reach = (int32_t)(p.tokens - 1 + more);
+        q.ds_head = ds_row(q, q.q_tiles);
+        if (q.ds_head < p.ds_head) p = q;
+    }
+    int64_t at_once = kMostKept / kPlaceBytes / (p.ds_head < 1 ? 1 : p.ds_head);
+    at_once = at_once < heads ? at_once : heads;
+    if (at_once < heads && at_once * p.kv_tiles < 2 * x.num_sms) return 0;
+    // the launches alike
+    if (at_once) p.hbs = (int32_t)ceil_div(heads, ceil_div(heads, at_once));
+    return p.hbs * p.ds_head * kPlaceBytes;
+}
+
 // Slots of partial sums of the backward pass over keys.
 int64_t dkv_slots(const Params& p) {
     const int64_t heads = (int64_t)p.a.batch * p.a.kv_heads;
@@ -1305,23 +1519,31 @@ cudaError_t forward(int device, const Params& p, const CUtensorMap& q, const CUt
 }
 
 template <class T, int DP>
-cudaError_t backward(int device, int sms, const Params& p, const CUtensorMap& q, const CUtensorMap& k,
-                     const CUtensorMap& v,
+cudaError_t backward(int device, int sms, Params p, const CUtensorMap& q, const CUtensorMap& k, const CUtensorMap& v,
                      const CUtensorMap& d_o, cudaStream_t st) {
     using G = GradShape<DP>;
-    static std::atomic<uint64_t> asked_q{0}, asked_kv{0};
-    cudaError_t e = allow_shared(attn_dq_kernel<T, DP>, G::kBytes, device, asked_q);
-    if (e == cudaSuccess) e = allow_shared(attn_dkv_kernel<T, DP>, G::kBytes, device, asked_kv);
+    using S = StoredShape<DP>;
+    static std::atomic<uint64_t> asked_q{0}, asked_kv{0}, asked_s{0};
+    cudaError_t e = allow_shared(attn_dkv_kernel<T, DP>, G::kBytes, device, asked_kv);
+    if (e == cudaSuccess && !p.ds) e = allow_shared(attn_dq_kernel<T, DP>, G::kBytes, device, asked_q);
+    if (e == cudaSuccess && p.ds) e = allow_shared(attn_dq_stored_kernel<T, DP>, S::kBytes, device, asked_s);
     if (e != cudaSuccess) return e;
-    const int64_t heads = p.a.batch * p.a.kv_heads;
-    const int64_t blocks = heads * (p.lead * p.lead_parts + (int64_t)(p.kv_tiles - p.lead) * p.rest_parts);
-    attn_dkv_kernel<T, DP><<<(unsigned)blocks, kGradThreads, G::kBytes, st>>>(q, k, v, d_o, p);
+    const int64_t heads = p.a.batch * p.a.kv_heads, tiles = p.lead * p.lead_parts +
+                                                            (int64_t)(p.kv_tiles - p.lead) * p.rest_parts;
+    const int each = p.hbs;
+    for (p.hb0 = 0; p.hb0 < heads; p.hb0 += each) {
+        p.hbs = (int32_t)(heads - p.hb0 < each ? heads - p.hb0 : each);
+        attn_dkv_kernel<T, DP><<<(unsigned)(p.hbs * tiles), kGradThreads, G::kBytes, st>>>(q, k, v, d_o, p);
+        const int64_t pieces = (int64_t)p.q_tiles * p.hbs, grid = pieces < sms ? pieces : sms;
+        if (p.ds)
+            attn_dq_stored_kernel<T, DP><<<(unsigned)grid, S::kThreads, S::kBytes, st>>>(k, p, (int)pieces);
+        else
+            attn_dq_kernel<T, DP><<<(unsigned)grid, kGradThreads, G::kBytes, st>>>(q, k, v, d_o, p, (int)pieces);
+    }
     if (p.lead_parts > 1 && p.lead)
         attn_dkv_join_kernel<T><<<(unsigned)(heads * p.lead * 16), 256, 0, st>>>(p, 1);
     if (p.rest_parts > 1 && p.kv_tiles > p.lead)
         attn_dkv_join_kernel<T><<<(unsigned)(heads * (p.kv_tiles - p.lead) * 16), 256, 0, st>>>(p, 0);
-    const int64_t pieces = p.q_tiles * heads, grid = pieces < sms ? pieces : sms;
-    attn_dq_kernel<T, DP><<<(unsigned)grid, kGradThreads, G::kBytes, st>>>(q, k, v, d_o, p, (int)pieces);
     return cudaGetLastError();
 }
 
@@ -1381,16 +1603,24 @@ cudaError_t launch_attn_tc(const OpContext& x, const heddle_attention_args& a, u
                                   : forward_of<__half>(x.device, p, q, k, v, st);
 }
 
-size_t attn_tc_grad_scratch(const OpContext& x, const heddle_attention_args& a) {
-    return 2 * align256((size_t)dkv_slots(params_of(x, a)) * kTile * a.head_dim * 4);
+size_t attn_tc_grad_scratch(const OpContext& x, const heddle_attention_args& a, bool keep) {
+    Params p = params_of(x, a);
+    const size_t kept = keep_ds(x, p);
+    return 2 * align256((size_t)dkv_slots(p) * kTile * a.head_dim * 4) + (keep ? kept : 0);
 }
 
 cudaError_t launch_attn_tc_grad(const OpContext& x, const heddle_attention_grad_args& g, const float* delta,
-                                unsigned char* ws, cudaStream_t st) {
+                                unsigned char* ws, bool keep, cudaStream_t st) {
     const heddle_attention_args& a = g.fwd;
     Params p = params_of(x, a);
+    const size_t parts = attn_tc_grad_scratch(x, a, false);
     p.part_dk = reinterpret_cast<float*>(ws);
-    p.part_dv = reinterpret_cast<float*>(ws + attn_tc_grad_scratch(x, a) / 2);
+    p.part_dv = reinterpret_cast<float*>(ws + parts / 2);
+    const int64_t kept = keep_ds(x, p);
+    if (keep && kept)
+        p.ds = ws + parts;
+    else
+        p.hbs = (int32_t)(a.batch * a.kv_heads);
     p.d_o = g.d_o, p.dq = g.dq, p.dk = g.dk, p.dv = g.dv;
     p.delta = delta;
     CUtensorMap q, k, v, d_o;

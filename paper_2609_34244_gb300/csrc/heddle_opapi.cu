@@ -391,8 +391,15 @@ heddle_status heddle_attention_backward(heddle_ctx* ctx, const heddle_attention_
     REQUIRE(a.lse || a.batch * a.q_len == 0, HEDDLE_E_ARG, "lse is null");
     if (a.batch == 0 || (a.q_len == 0 && a.kv_len == 0)) return done(x, cudaSuccess, "");
     OpDeviceGuard guard(x->device);
-    CHECK(reserve(x, hd::attention_grad_scratch(*x, *args)));
-    return done(x, hd::launch_attention_grad(*x, *args, x->ws, (cudaStream_t)stream), "heddle_attention_backward");
+    // room to keep the scores' gradients, or without them where that is refused
+    const size_t most = hd::attention_grad_scratch(*x, *args, true), least = hd::attention_grad_scratch(*x, *args, false);
+    const bool keep = !(x->ws_refused && most >= x->ws_refused) && reserve(x, most) == HEDDLE_OK;
+    if (!keep) {
+        if (!x->ws_refused || most < x->ws_refused) x->ws_refused = most;
+        CHECK(reserve(x, least));
+    }
+    return done(x, hd::launch_attention_grad(*x, *args, x->ws, keep, (cudaStream_t)stream),
+                "heddle_attention_backward");
 }
 
 }  // extern "C"

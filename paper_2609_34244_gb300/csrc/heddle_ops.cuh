@@ -25,6 +25,7 @@ struct OpContext {
     int32_t* sched = nullptr;  // two counters of kernels that hand out work, zero between launches
     unsigned char* ws = nullptr;
     size_t ws_cap = 0;
+    size_t ws_refused = 0;  // the least scratch that the device had no room for, where a call can do without
     char* msg = nullptr;
     size_t msg_size = 0;
 };
@@ -149,8 +150,9 @@ cudaError_t launch_qk_norm_rope_grad(const OpContext& x, const heddle_qk_norm_ro
 
 size_t attention_scratch(const OpContext& x, const heddle_attention_args& a);
 cudaError_t launch_attention(const OpContext& x, const heddle_attention_args& a, unsigned char* ws, cudaStream_t st);
-size_t attention_grad_scratch(const OpContext& x, const heddle_attention_grad_args& a);
-cudaError_t launch_attention_grad(const OpContext& x, const heddle_attention_grad_args& a, unsigned char* ws,
+// keep: with room for the scores' gradients between the backward's passes
+size_t attention_grad_scratch(const OpContext& x, const heddle_attention_grad_args& a, bool keep);
+cudaError_t launch_attention_grad(const OpContext& x, const heddle_attention_grad_args& a, unsigned char* ws, bool keep,
                                   cudaStream_t st);
 
 }  // namespace hd

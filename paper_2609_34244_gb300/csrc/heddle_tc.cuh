@@ -102,6 +102,12 @@ __device__ __forceinline__ void load_4d(uint32_t dst, const CUtensorMap* m, uint
         "l"(m), "r"(bar), "r"(x), "r"(y), "r"(z), "r"(w)
         : "memory");
 }
+// Bytes as they lie: addresses and size in whole 16-byte units.
+__device__ __forceinline__ void load_bytes(uint32_t dst, const void* src, uint32_t size, uint32_t bar) {
+    asm volatile("cp.async.bulk.shared::cta.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst),
+                 "l"(__cvta_generic_to_global(src)), "r"(size), "r"(bar)
+                 : "memory");
+}
 // Of a pair of CTAs: into this CTA's memory, counted by the barrier at a
 // cluster address (the first one's).
 __device__ __forceinline__ void load_2d_pair(uint32_t dst, const CUtensorMap* m, uint32_t bar, int x, int y) {
@@ -234,6 +240,13 @@ __device__ __forceinline__ void tmem_st16(uint32_t addr, const uint32_t (&v)[16]
 __device__ __forceinline__ uint64_t smem_desc(uint32_t addr, uint32_t lead) {
     return (uint64_t)((addr & 0x3FFFF) >> 4) | ((uint64_t)(lead >> 4) << 16) | ((uint64_t)(1024 >> 4) << 32) |
            (1ull << 46) | (2ull << 61);
+}
+// The same for an operand whose contraction runs across 16-byte units of 8
+// values, not swizzled: units of 8 steps lie together (128 bytes), the next 8
+// steps `steps` bytes on, the next 8 rows `rows` bytes on.
+__device__ __forceinline__ uint64_t smem_desc_units(uint32_t addr, uint32_t steps, uint32_t rows) {
+    return (uint64_t)((addr & 0x3FFFF) >> 4) | ((uint64_t)(steps >> 4) << 16) | ((uint64_t)(rows >> 4) << 32) |
+           (1ull << 46);
 }
 // Products of m x n tiles (128 rows, 256 for a pair) of 16-bit operands
 // summed in 32 bits.
