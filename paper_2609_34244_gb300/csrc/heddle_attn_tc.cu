@@ -735,7 +735,7 @@ constexpr int kGradBarBytes = 160;
 template <int DP>
 struct GradShape {
     static constexpr int kTileBytes = kTile * DP * 2;
-    static constexpr int kStats = 3 * kTile * 8;
+    static constexpr int kStats = 3 * kTile * 8 + 16;
     static constexpr int kBytes = 1024 + 6 * kTileBytes + kGradBarBytes + 64 + kStats;
 };
 
@@ -1122,6 +1122,7 @@ __global__ void __launch_bounds__(kGradThreads, 1)
     uint32_t* tmem_at = const_cast<uint32_t*>(gave_up) + 1;
     float* stat_lse = reinterpret_cast<float*>(tail + kGradBarBytes + 64);  // [3][128] minus lse, in powers of two
     float* stat_delta = stat_lse + 3 * kTile;                               // [3][128] minus delta
+    uint32_t* stat_place = reinterpret_cast<uint32_t*>(stat_delta + 3 * kTile);  // [3] the query tile's places
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
 
     // the first keys are seen by the most queries
@@ -1220,8 +1221,12 @@ __global__ void __launch_bounds__(kGradThreads, 1)
         const int key = k0 + row;
         const uint64_t c2 = two(p.scale_log2, p.scale_log2);
 
-        // statistics of query tile j to buffer j % 3, by two of the sides: written a
-        // step ahead, while the slowest warp may still read those of the step
+        // where dS goes, less the query tile's part: all of it is below 2^32 bytes
+        const uint32_t ds_at =
+            p.ds ? (uint32_t)((hb - p.hb0) * p.ds_head + ds_col(p, k0 / kTile)) * kPlaceBytes + side * (4 * kTile * 16) + row * 16 : 0;
+
+        // statistics of query tile j to buffer j % 3, by three of the sides: written
+        // a step ahead, while the slowest warp may still read those of the step
         // before
         const int i_row = first * p.tokens + row / p.group;
         const int64_t r_row = ((int64_t)b * p.a.q_heads + hk * p.group + row % p.group) * p.a.q_len;
@@ -1235,6 +1240,8 @@ __global__ void __launch_bounds__(kGradThreads, 1)
                 stat_lse[to] = l == -INFINITY ? -INFINITY : -l * kLog2e;
             } else if (side == 1) {
                 stat_delta[to] = live ? -p.delta[r_row + i] : 0.0f;
+            } else if (side == 2 && row == 0 && p.ds) {
+                stat_place[j % 3] = (uint32_t)ds_row(p, first + j) * kPlaceBytes;
             }
         };
         // the tile's columns that see the key: query heads of consecutive tokens
@@ -1325,8 +1332,7 @@ __global__ void __launch_bounds__(kGradThreads, 1)
             __syncwarp();
             if (lane == 0) mbar_arrive(bar.b_ready);
             if (p.ds) {  // units of 8 queries, the keys of each one after another: a warp writes 512 bytes at a time
-                const int64_t place = (hb - p.hb0) * p.ds_head + ds_row(p, first + j) + ds_col(p, k0 / kTile);
-                unsigned char* to = p.ds + place * kPlaceBytes + side * (4 * kTile * 16) + row * 16;
+                unsigned char* to = p.ds + (ds_at + stat_place[j % 3]);
 #pragma unroll
                 for (int y = 0; y < 4; ++y)
                     *reinterpret_cast<uint4*>(to + y * (kTile * 16)) =
