@@ -302,7 +302,7 @@ struct Forward {
     static constexpr int kRoom = 227 * 1024 - 1024 - 512 - kHigh - NT * kTileBytes;
     static constexpr int kSlots = kRoom / kTileBytes < 8 ? kRoom / kTileBytes : 8;  // K and V tiles by turns
     static constexpr int kBytes = 1024 + (NT + kSlots) * kTileBytes + 512 + kHigh;
-    static constexpr int kThreads = 128 + NT * 256;
+    static constexpr int kThreads = 64 + NT * 256;
     static constexpr int kCols = NT * (kTile + DP) <= 256 ? 256 : 512;
 };
 
@@ -448,8 +448,8 @@ __global__ void __launch_bounds__(Forward<DP, NT>::kThreads, 1)
                 if (last && (TWINS ? j + 1 < w.count[q] : j + 1 < n)) commit(empty + 8 * sk);
             }
         }
-    } else if (warp >= 4) {
-        const int q = (warp - 4) / 8, side = (warp - 4) / 4 % 2, row = (warp % 4) * 32 + lane;
+    } else if (warp >= 2) {
+        const int q = (warp - 2) / 8, side = (warp - 2) / 4 % 2, row = (warp % 4) * 32 + lane;
         const uint32_t lanes = (uint32_t)(warp % 4 * 32) << 16;
         const uint32_t ts = tmem + lanes + q * kTile, to_acc = tmem + lanes + NT * kTile + q * DP;
         const uint32_t pair = met + 8 * (q * 4 + warp % 4);  // this warp and the one of the rows' other half
@@ -698,7 +698,7 @@ __device__ __forceinline__ void leave_pieces(int32_t* sched) {
 // Sixteen warps turn scores into dS, four for every quarter of a tile's
 // columns: with eight, each scheduler's two warps left it idle two thirds of
 // the time.
-constexpr int kGradWarps = 16, kGradThreads = 128 + 32 * kGradWarps;
+constexpr int kGradWarps = 16, kGradThreads = 64 + 32 * kGradWarps;
 
 // Bars of a backward kernel, in the order that follows its tiles.
 struct GradBars {
@@ -841,8 +841,8 @@ __global__ void __launch_bounds__(kGradThreads, 1)
             if (go) commit(bar.done);
             step += n;
         }
-    } else if (warp >= 4) {
-        const int side = (warp - 4) / 4, row = (warp % 4) * 32 + lane;  // which 32 of a tile's 128 keys
+    } else if (warp >= 2) {
+        const int side = (warp - 2) / 4, row = (warp % 4) * 32 + lane;  // which 32 of a tile's 128 keys
         const uint32_t lanes = (uint32_t)(warp % 4 * 32) << 16;
         const int i_row = row / p.group, h_row = row % p.group;
         const float c = p.scale_log2;
@@ -1158,9 +1158,9 @@ __global__ void __launch_bounds__(kGradThreads, 1)
         mbar_fence_init();
     }
     if (warp == 2) tmem_alloc(smem_u32(tmem_at), 512);
-    if (warp >= 4) {  // rows that no copy writes are zero throughout
-        const int row = threadIdx.x & 127, rows = p.group * p.tokens;
-        clear_rows<DP>(stage + (threadIdx.x - 128) / 128 * G::kTileBytes, row, rows);
+    if (warp >= 2) {  // rows that no copy writes are zero throughout
+        const int row = (threadIdx.x - 64) & 127, rows = p.group * p.tokens;
+        clear_rows<DP>(stage + (threadIdx.x - 64) / 128 * G::kTileBytes, row, rows);
         fence_async_shared();
     }
     fence_before();
@@ -1215,8 +1215,8 @@ __global__ void __launch_bounds__(kGradThreads, 1)
             }
         }
         if (go) commit(bar.done);
-    } else if (warp >= 4) {
-        const int side = (warp - 4) / 4, row = (warp % 4) * 32 + lane;  // which 32 of a tile's 128 queries
+    } else if (warp >= 2) {
+        const int side = (warp - 2) / 4, row = (warp % 4) * 32 + lane;  // which 32 of a tile's 128 queries
         const uint32_t lanes = (uint32_t)(warp % 4 * 32) << 16;
         const int key = k0 + row;
         const uint64_t c2 = two(p.scale_log2, p.scale_log2);
