@@ -390,6 +390,18 @@ __global__ void __launch_bounds__(Forward<DP, NT>::kThreads, 1)
         mbar_init(told, 4);
         *gave_up = 0;
         mbar_fence_init();
+        if (n > 0) {  // the first loads run while the CTA gathers
+            const uint32_t q_bytes = p.group * p.tokens * DP * 2;
+#pragma unroll
+            for (int q = 0; q < (TWINS ? 1 : NT); ++q)
+                if (w.count[q] > 0) {
+                    mbar_expect(q_full + 8 * q, q_bytes);
+                    load_q_tile<DP>(smem_u32(base + q * F::kTileBytes), &mq, q_full + 8 * q, p, t0 + q * p.tokens, hk,
+                                    b);
+                }
+            mbar_expect(full, F::kTileBytes);
+            load_kv_tile<DP>(smem_u32(ring), &mk, full, keys.at(w.from[0]) * kTile, hk, b);
+        }
     }
     if (warp == 2) tmem_alloc(smem_u32(tmem_at), F::kCols);
     fence_before();
@@ -397,14 +409,7 @@ __global__ void __launch_bounds__(Forward<DP, NT>::kThreads, 1)
     fence_after();
     const uint32_t tmem = *tmem_at;
     if (warp == 0 && n > 0 && elect_one()) {
-        const uint32_t q_bytes = p.group * p.tokens * DP * 2;
-#pragma unroll
-        for (int q = 0; q < (TWINS ? 1 : NT); ++q)
-            if (w.count[q] > 0) {
-                mbar_expect(q_full + 8 * q, q_bytes);
-                load_q_tile<DP>(smem_u32(base + q * F::kTileBytes), &mq, q_full + 8 * q, p, t0 + q * p.tokens, hk, b);
-            }
-        int i = 0;
+        int i = 1;
         bool go = true;
         auto load = [&](const CUtensorMap* m, int tile) {
             const int slot = i % F::kSlots;
@@ -414,7 +419,7 @@ __global__ void __launch_bounds__(Forward<DP, NT>::kThreads, 1)
             ++i;
         };
         for (int j = 0; go && j < n; ++j) {
-            load(&mk, w.from[0] + j);
+            if (j > 0) load(&mk, w.from[0] + j);
             if (TWINS && j < w.count[NT - 1]) load(&mk, w.from[NT - 1] + j);
             load(&mv, w.from[0] + j);
             if (TWINS && j < w.count[NT - 1]) load(&mv, w.from[NT - 1] + j);
@@ -1152,10 +1157,24 @@ __global__ void __launch_bounds__(kGradThreads, 1)
         }
     }
 
+    auto load_tile = [&](int j, const CUtensorMap* m, int second, uint32_t on) {
+        mbar_expect(on + 8 * (j & 1), p.group * p.tokens * DP * 2);
+        load_q_tile<DP>(smem_u32(stage + (2 * (j & 1) + second) * G::kTileBytes), m, on + 8 * (j & 1), p,
+                        (first + j) * p.tokens, hk, b);
+    };
+    auto load_q = [&](int j) { load_tile(j, &mq, 0, bar.full); };
+    auto load_do = [&](int j) { load_tile(j, &mdo, 1, bar.full2); };
     if (threadIdx.x == 0) {
         bar.init();
         *gave_up = 0;
         mbar_fence_init();
+        if (n > 0) {  // the first loads run while the CTA gathers
+            mbar_expect(bar.held, 2 * G::kTileBytes);
+            load_kv_tile<DP>(smem_u32(sk), &mk, bar.held, k0, hk, b);
+            load_q(0);
+            load_kv_tile<DP>(smem_u32(sv), &mv, bar.held, k0, hk, b);
+            load_do(0);
+        }
     }
     if (warp == 2) tmem_alloc(smem_u32(tmem_at), 512);
     if (warp >= 2) {  // rows that no copy writes are zero throughout
@@ -1170,18 +1189,10 @@ __global__ void __launch_bounds__(kGradThreads, 1)
     const uint32_t at_s = tmem, at_dp = tmem + 128, at_dv = tmem + 256, at_dk = tmem + 256 + DP;
 
     if (warp == 0 && n > 0 && elect_one()) {
-        mbar_expect(bar.held, 2 * G::kTileBytes);
-        load_kv_tile<DP>(smem_u32(sk), &mk, bar.held, k0, hk, b);
-        load_kv_tile<DP>(smem_u32(sv), &mv, bar.held, k0, hk, b);
-        const uint32_t bytes = p.group * p.tokens * DP * 2;
-        for (int j = 0; j < n; ++j) {
-            const int st = j & 1;
-            if (!mbar_wait(bar.empty + 8 * st, (j / 2 & 1) ^ 1, gave_up)) break;
-            const int t = (first + j) * p.tokens;
-            mbar_expect(bar.full + 8 * st, bytes);
-            load_q_tile<DP>(smem_u32(stage + 2 * st * G::kTileBytes), &mq, bar.full + 8 * st, p, t, hk, b);
-            mbar_expect(bar.full2 + 8 * st, bytes);
-            load_q_tile<DP>(smem_u32(stage + (2 * st + 1) * G::kTileBytes), &mdo, bar.full2 + 8 * st, p, t, hk, b);
+        for (int j = 1; j < n; ++j) {
+            if (!mbar_wait(bar.empty + 8 * (j & 1), (j / 2 & 1) ^ 1, gave_up)) break;
+            load_q(j);
+            load_do(j);
         }
     } else if (warp == 1 && n > 0 && elect_one()) {
         const uint32_t bf = p.a.dtype == HEDDLE_BF16;
