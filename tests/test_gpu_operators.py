@@ -515,6 +515,32 @@ def test_attention_repeats(lib):
     assert all(torch.equal(a, b) for a, b in zip(*got))
 
 
+@pytest.mark.parametrize("t,hq,hk,d,groups", [
+    (6000, 120, 12, 16, (0, 5, 6, 11)),  # the scores' gradients of six key heads at a time fit between the passes
+    (5800, 128, 1, 8, (0,)),             # those of a single key head do not
+])
+def test_attention_backward_beyond_its_room(lib, t, hq, hk, d, groups):
+    h, ctx = lib
+    g = gen(t)
+    q, k, v, do = (rand(g, 1, t, n, d, dt=torch.bfloat16) for n in (hq, hk, hk, hq))
+    o, lse = torch.empty_like(q), torch.empty(1, hq, t, device="cuda")
+    h.heddle_attention(ctx, q, k, v, o, lse)
+    dq, dk, dv = (torch.full_like(x, CANARY) for x in (q, k, v))
+    h.heddle_attention_backward(ctx, do, q, k, v, o, lse, dq, dk, dv)
+    n = hq // hk
+    for kv in groups:
+        sums = {x: [torch.zeros(t, d, dtype=torch.float64, device="cuda") for _ in range(2)] for x in ("dk", "dv")}
+        for j in range(kv * n, kv * n + n):
+            w = R.attention(q[0, :, j], k[0, :, kv], v[0, :, kv], t, t, 0, 0, d ** -0.5, do[0, :, j])
+            R.close(o[0, :, j], *w["o"], "o")
+            R.close(dq[0, :, j], *w["dq"], "dq")
+            for x in sums:
+                sums[x][0] += w[x][0]
+                sums[x][1] += w[x][1] + n * 2.0 ** -23 * w[x][0].abs()
+        R.close(dk[0, :, kv], *sums["dk"], "dk")
+        R.close(dv[0, :, kv], *sums["dv"], "dv")
+
+
 def test_offsets_past_32_bits(lib):
     """Rows and tokens that lie more than 2^31 elements apart."""
     h, ctx = lib
