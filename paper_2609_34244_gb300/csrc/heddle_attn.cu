@@ -72,6 +72,8 @@ __global__ void __launch_bounds__(kWarps * 32) attn_row_kernel(heddle_attention_
 template <class T, int GL>
 __global__ void __launch_bounds__(256) attn_delta_wide_kernel(const __grid_constant__ heddle_attention_grad_args g,
                                                               float* delta) {
+    allow_dependents();
+    await_previous();
     const heddle_attention_args& a = g.fwd;
     const int lane = threadIdx.x % GL;
     const uint32_t r = blockIdx.x * (256 / GL) + threadIdx.x / GL;  // (b, i, h)
@@ -100,21 +102,20 @@ __global__ void __launch_bounds__(256) attn_delta_wide_kernel(const __grid_const
 constexpr int kFewKeys = 16;
 
 // 16 lanes a row, a key each; `per` rows a head: the queries of the first
-// `per` positions, or (all) the first `per` queries.
+// `per` positions, or (all) the first `per` queries.  The row, or -1.
 template <class T>
-__global__ void __launch_bounds__(256) attn_few_delta_kernel(const __grid_constant__ heddle_attention_grad_args g,
-                                                             float* delta, int64_t per, bool all) {
+__device__ __forceinline__ int64_t few_delta(const heddle_attention_grad_args& g, int64_t per, bool all, float* value) {
     const heddle_attention_args& a = g.fwd;
     const int lane = threadIdx.x % kFewKeys, D = a.head_dim;
     const int64_t r = (int64_t)blockIdx.x * (256 / kFewKeys) + threadIdx.x / kFewKeys;  // (b, h, e)
-    if (r >= a.batch * a.q_heads * per) return;
+    if (r >= a.batch * a.q_heads * per) return -1;
     const int64_t e = r % per, h = r / per % a.q_heads, b = r / (per * a.q_heads);
     const Span sp = span_of(a, b);
     const int64_t i = all ? e : e - sp.off, pos = sp.off + i;
-    if (i < 0 || i >= sp.ql || pos < 0) return;
+    if (i < 0 || i >= sp.ql || pos < 0) return -1;
     const int64_t low = a.window && pos + 1 > a.window ? pos + 1 - a.window : 0;
     const int64_t first = min(a.sinks, low), keys = first + pos + 1 - low;
-    if (keys > kFewKeys) return;
+    if (keys > kFewKeys) return -1;
     const int64_t hk = h / (a.q_heads / a.kv_heads), row = (b * a.q_heads + h) * a.q_len + i;
     const uint32_t mask = 0xffffu << (threadIdx.x % 32 / kFewKeys * kFewKeys);
     float s = 0.0f, total = 0.0f;
@@ -143,7 +144,17 @@ __global__ void __launch_bounds__(256) attn_few_delta_kernel(const __grid_consta
         s += __shfl_xor_sync(mask, s, o, kFewKeys);
         total += __shfl_xor_sync(mask, total, o, kFewKeys);
     }
-    if (lane == 0) delta[row] = s / total;
+    *value = s / total;
+    return row;
+}
+template <class T>
+__global__ void __launch_bounds__(256) attn_few_delta_kernel(const __grid_constant__ heddle_attention_grad_args g,
+                                                             float* delta, int64_t per, bool all) {
+    allow_dependents();
+    float value = 0.0f;
+    const int64_t row = few_delta<T>(g, per, all, &value);
+    await_previous();  // which writes these rows as well
+    if (row >= 0 && threadIdx.x % kFewKeys == 0) delta[row] = value;
 }
 
 bool units16(const heddle_heads& t) {
@@ -153,6 +164,8 @@ bool units16(const heddle_heads& t) {
 // delta_i = do_i . o_i
 template <class T>
 __global__ void __launch_bounds__(kWarps * 32) attn_delta_kernel(heddle_attention_grad_args g, float* delta) {
+    allow_dependents();
+    await_previous();
     const heddle_attention_args& a = g.fwd;
     const int lane = threadIdx.x % 32, D = a.head_dim;
     const int64_t rows = a.batch * a.q_heads * a.q_len;
@@ -241,17 +254,17 @@ cudaError_t attention_grad(const OpContext& x, const heddle_attention_grad_args&
     const bool tc = attn_tc_takes_grad(g);
     if (rows && a.head_dim % 8 == 0 && a.head_dim <= 128 && units16(a.o) && units16(g.d_o)) {
         if (a.head_dim <= 64)
-            attn_delta_wide_kernel<T, 8><<<(unsigned)ceil_div(rows, 32), 256, 0, st>>>(g, delta);
+            launch(x, attn_delta_wide_kernel<T, 8>, dim3((unsigned)ceil_div(rows, 32)), 256, 0, st, g, delta);
         else
-            attn_delta_wide_kernel<T, 16><<<(unsigned)ceil_div(rows, 16), 256, 0, st>>>(g, delta);
+            launch(x, attn_delta_wide_kernel<T, 16>, dim3((unsigned)ceil_div(rows, 16)), 256, 0, st, g, delta);
     } else if (rows) {
-        attn_delta_kernel<T><<<row_blocks(x, rows), kWarps * 32, 0, st>>>(g, delta);
+        launch(x, attn_delta_kernel<T>, dim3(row_blocks(x, rows)), kWarps * 32, 0, st, g, delta);
     }
     if (tc) {
         const bool all = a.window && a.window + a.sinks <= kFewKeys;
         const int64_t per = all || a.q_len < kFewKeys ? a.q_len : kFewKeys;
-        attn_few_delta_kernel<T><<<(unsigned)ceil_div(a.batch * a.q_heads * per, 256 / kFewKeys), 256, 0, st>>>(
-            g, delta, per, all || a.q_len < kFewKeys);
+        launch(x, attn_few_delta_kernel<T>, dim3((unsigned)ceil_div(a.batch * a.q_heads * per, 256 / kFewKeys)), 256, 0, st,
+               g, delta, per, all || a.q_len < kFewKeys);
         const cudaError_t e = cudaGetLastError();
         return e == cudaSuccess ? launch_attn_tc_grad(x, g, delta, rest, keep, st) : e;
     }

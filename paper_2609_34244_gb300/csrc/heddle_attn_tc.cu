@@ -370,6 +370,8 @@ __global__ void __launch_bounds__(Forward<DP, NT>::kThreads, 1)
     float* highs = reinterpret_cast<float*>(reinterpret_cast<unsigned char*>(bars) + 512);  // [2][NT][2][128]
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
 
+    allow_dependents();
+    await_previous();
     const ForwardPiece<NT, TWINS> w(p, blockIdx.x);
     const Seq& s = w.s;
     const KeyTiles& keys = w.keys;
@@ -624,6 +626,8 @@ __global__ void __launch_bounds__(Forward<DP, NT>::kThreads, 1)
 // of 128, 269 MB in 51 us both kernels (5.2e12 bytes a second).
 template <class T>
 __global__ void __launch_bounds__(256) attn_join_kernel(const __grid_constant__ Params p) {
+    allow_dependents();
+    await_previous();
     const int lane = threadIdx.x % 32, D = p.a.head_dim;
     const int64_t rows = p.a.batch * p.a.q_heads * p.a.q_len;
     const int64_t r = (int64_t)blockIdx.x * 8 + threadIdx.x / 32;
@@ -760,6 +764,7 @@ __global__ void __launch_bounds__(kGradThreads, 1)
     uint32_t* tmem_at = const_cast<uint32_t*>(gave_up) + 1;
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
 
+    allow_dependents();
     struct Piece {
         int hk, b, t0, t1;
         Seq s;
@@ -784,6 +789,7 @@ __global__ void __launch_bounds__(kGradThreads, 1)
     fence_before();
     __syncthreads();
     fence_after();
+    await_previous();
     const uint32_t tmem = *tmem_at;
     const uint32_t at_s = tmem, at_dp = tmem + 128, at_dq = tmem + 256, at_ds = tmem + 256 + DP;  // two of 64 columns
 
@@ -969,6 +975,7 @@ __global__ void __launch_bounds__(StoredShape<DP>::kThreads, 1)
     uint32_t* tmem_at = const_cast<uint32_t*>(gave_up) + 1;
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
 
+    allow_dependents();
     struct Piece {
         int hb, hk, b, tile, t0;
         Seq s;
@@ -1000,6 +1007,7 @@ __global__ void __launch_bounds__(StoredShape<DP>::kThreads, 1)
     fence_before();
     __syncthreads();
     fence_after();
+    await_previous();
     const uint32_t tmem = *tmem_at;
 
     if (warp == 0 && elect_one()) {
@@ -1130,6 +1138,7 @@ __global__ void __launch_bounds__(kGradThreads, 1)
     uint32_t* stat_place = reinterpret_cast<uint32_t*>(stat_delta + 3 * kTile);  // [3] the query tile's places
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
 
+    allow_dependents();
     // the first keys are seen by the most queries
     const int64_t heads = p.hbs, lead_blocks = heads * p.lead * p.lead_parts;
     const bool lead = blockIdx.x < lead_blocks;
@@ -1227,6 +1236,7 @@ __global__ void __launch_bounds__(kGradThreads, 1)
         }
         if (go) commit(bar.done);
     } else if (warp >= 2) {
+        await_previous();  // for delta; everything read before is the caller's
         const int side = (warp - 2) / 4, row = (warp % 4) * 32 + lane;  // which 32 of a tile's 128 queries
         const uint32_t lanes = (uint32_t)(warp % 4 * 32) << 16;
         const int key = k0 + row;
@@ -1387,6 +1397,8 @@ __global__ void __launch_bounds__(kGradThreads, 1)
 // for the windowed call of 4095 tokens whose first tiles come in parts.
 template <class T>
 __global__ void __launch_bounds__(256) attn_dkv_join_kernel(const __grid_constant__ Params p, int is_lead) {
+    allow_dependents();
+    await_previous();
     const int lane = threadIdx.x % 32, D = p.a.head_dim;
     const int parts = is_lead ? p.lead_parts : p.rest_parts;
     const int64_t heads = p.a.batch * p.a.kv_heads, unit = blockIdx.x / 16;
@@ -1518,63 +1530,64 @@ int64_t dkv_slots(const Params& p) {
 }
 
 template <class T, int DP, int NT, bool TWINS>
-cudaError_t forward(int device, const Params& p, const CUtensorMap& q, const CUtensorMap& k, const CUtensorMap& v,
+cudaError_t forward(const OpContext& x, const Params& p, const CUtensorMap& q, const CUtensorMap& k, const CUtensorMap& v,
                     cudaStream_t st) {
     using F = Forward<DP, NT>;
     static_assert(F::kSlots >= 4, "two steps of K and V");
     auto* f = attn_kernel<T, DP, NT, TWINS>;
     static std::atomic<uint64_t> asked{0};
-    const cudaError_t e = allow_shared(f, F::kBytes, device, asked);
+    const cudaError_t e = allow_shared(f, F::kBytes, x.device, asked);
     if (e != cudaSuccess) return e;
     const int64_t pieces = ceil_div(p.q_tiles, TWINS ? 1 : NT) * p.a.batch * p.a.kv_heads * p.splits;
-    f<<<(unsigned)pieces, F::kThreads, F::kBytes, st>>>(q, k, v, p);
+    launch(x, f, dim3((unsigned)pieces), F::kThreads, F::kBytes, st, q, k, v, p);
     if (p.splits > 1) {
         const int64_t rows = p.a.batch * p.a.q_heads * p.a.q_len;
-        attn_join_kernel<T><<<(unsigned)ceil_div(rows, 8), 256, 0, st>>>(p);
+        launch(x, attn_join_kernel<T>, dim3((unsigned)ceil_div(rows, 8)), 256, 0, st, p);
     }
     return cudaGetLastError();
 }
 
 template <class T, int DP>
-cudaError_t backward(int device, int sms, Params p, const CUtensorMap& q, const CUtensorMap& k, const CUtensorMap& v,
+cudaError_t backward(const OpContext& x, Params p, const CUtensorMap& q, const CUtensorMap& k, const CUtensorMap& v,
                      const CUtensorMap& d_o, cudaStream_t st) {
     using G = GradShape<DP>;
     using S = StoredShape<DP>;
     static std::atomic<uint64_t> asked_q{0}, asked_kv{0}, asked_s{0};
-    cudaError_t e = allow_shared(attn_dkv_kernel<T, DP>, G::kBytes, device, asked_kv);
-    if (e == cudaSuccess && !p.ds) e = allow_shared(attn_dq_kernel<T, DP>, G::kBytes, device, asked_q);
-    if (e == cudaSuccess && p.ds) e = allow_shared(attn_dq_stored_kernel<T, DP>, S::kBytes, device, asked_s);
+    cudaError_t e = allow_shared(attn_dkv_kernel<T, DP>, G::kBytes, x.device, asked_kv);
+    if (e == cudaSuccess && !p.ds) e = allow_shared(attn_dq_kernel<T, DP>, G::kBytes, x.device, asked_q);
+    if (e == cudaSuccess && p.ds) e = allow_shared(attn_dq_stored_kernel<T, DP>, S::kBytes, x.device, asked_s);
     if (e != cudaSuccess) return e;
     const int64_t heads = p.a.batch * p.a.kv_heads, tiles = p.lead * p.lead_parts +
                                                             (int64_t)(p.kv_tiles - p.lead) * p.rest_parts;
     const int each = p.hbs;
     for (p.hb0 = 0; p.hb0 < heads; p.hb0 += each) {
         p.hbs = (int32_t)(heads - p.hb0 < each ? heads - p.hb0 : each);
-        attn_dkv_kernel<T, DP><<<(unsigned)(p.hbs * tiles), kGradThreads, G::kBytes, st>>>(q, k, v, d_o, p);
-        const int64_t pieces = (int64_t)p.q_tiles * p.hbs, grid = pieces < sms ? pieces : sms;
+        launch(x, attn_dkv_kernel<T, DP>, dim3((unsigned)(p.hbs * tiles)), kGradThreads, G::kBytes, st, q, k, v, d_o, p);
+        const int64_t pieces = (int64_t)p.q_tiles * p.hbs, grid = pieces < x.num_sms ? pieces : x.num_sms;
         if (p.ds)
-            attn_dq_stored_kernel<T, DP><<<(unsigned)grid, S::kThreads, S::kBytes, st>>>(k, p, (int)pieces);
+            launch(x, attn_dq_stored_kernel<T, DP>, dim3((unsigned)grid), S::kThreads, S::kBytes, st, k, p, (int)pieces);
         else
-            attn_dq_kernel<T, DP><<<(unsigned)grid, kGradThreads, G::kBytes, st>>>(q, k, v, d_o, p, (int)pieces);
+            launch(x, attn_dq_kernel<T, DP>, dim3((unsigned)grid), kGradThreads, G::kBytes, st, q, k, v, d_o, p,
+                   (int)pieces);
     }
     if (p.lead_parts > 1 && p.lead)
-        attn_dkv_join_kernel<T><<<(unsigned)(heads * p.lead * 16), 256, 0, st>>>(p, 1);
+        launch(x, attn_dkv_join_kernel<T>, dim3((unsigned)(heads * p.lead * 16)), 256, 0, st, p, 1);
     if (p.rest_parts > 1 && p.kv_tiles > p.lead)
-        attn_dkv_join_kernel<T><<<(unsigned)(heads * (p.kv_tiles - p.lead) * 16), 256, 0, st>>>(p, 0);
+        launch(x, attn_dkv_join_kernel<T>, dim3((unsigned)(heads * (p.kv_tiles - p.lead) * 16)), 256, 0, st, p, 0);
     return cudaGetLastError();
 }
 
 template <class T>
-cudaError_t forward_of(int device, const Params& p, const CUtensorMap& q, const CUtensorMap& k, const CUtensorMap& v,
+cudaError_t forward_of(const OpContext& x, const Params& p, const CUtensorMap& q, const CUtensorMap& k, const CUtensorMap& v,
                        cudaStream_t st) {
     const bool two = tiles_per_block(p.a) == 2;
     if (p.a.head_dim <= 64)
-        return two       ? forward<T, 64, 2, false>(device, p, q, k, v, st)
-               : p.twins ? forward<T, 64, 2, true>(device, p, q, k, v, st)
-                         : forward<T, 64, 1, false>(device, p, q, k, v, st);
-    return two       ? forward<T, 128, 2, false>(device, p, q, k, v, st)
-           : p.twins ? forward<T, 128, 2, true>(device, p, q, k, v, st)
-                     : forward<T, 128, 1, false>(device, p, q, k, v, st);
+        return two       ? forward<T, 64, 2, false>(x, p, q, k, v, st)
+               : p.twins ? forward<T, 64, 2, true>(x, p, q, k, v, st)
+                         : forward<T, 64, 1, false>(x, p, q, k, v, st);
+    return two       ? forward<T, 128, 2, false>(x, p, q, k, v, st)
+           : p.twins ? forward<T, 128, 2, true>(x, p, q, k, v, st)
+                     : forward<T, 128, 1, false>(x, p, q, k, v, st);
 }
 
 cudaError_t input_maps(const Params& p, CUtensorMap* q, CUtensorMap* k, CUtensorMap* v) {
@@ -1616,8 +1629,8 @@ cudaError_t launch_attn_tc(const OpContext& x, const heddle_attention_args& a, u
     CUtensorMap q, k, v;
     const cudaError_t e = input_maps(p, &q, &k, &v);
     if (e != cudaSuccess) return e;
-    return a.dtype == HEDDLE_BF16 ? forward_of<__nv_bfloat16>(x.device, p, q, k, v, st)
-                                  : forward_of<__half>(x.device, p, q, k, v, st);
+    return a.dtype == HEDDLE_BF16 ? forward_of<__nv_bfloat16>(x, p, q, k, v, st)
+                                  : forward_of<__half>(x, p, q, k, v, st);
 }
 
 size_t attn_tc_grad_scratch(const OpContext& x, const heddle_attention_args& a, bool keep) {
@@ -1646,10 +1659,10 @@ cudaError_t launch_attn_tc_grad(const OpContext& x, const heddle_attention_grad_
     if (e != cudaSuccess) return e;
     const bool narrow = a.head_dim <= 64;
     if (a.dtype == HEDDLE_BF16)
-        return narrow ? backward<__nv_bfloat16, 64>(x.device, x.num_sms, p, q, k, v, d_o, st)
-                      : backward<__nv_bfloat16, 128>(x.device, x.num_sms, p, q, k, v, d_o, st);
-    return narrow ? backward<__half, 64>(x.device, x.num_sms, p, q, k, v, d_o, st)
-                  : backward<__half, 128>(x.device, x.num_sms, p, q, k, v, d_o, st);
+        return narrow ? backward<__nv_bfloat16, 64>(x, p, q, k, v, d_o, st)
+                      : backward<__nv_bfloat16, 128>(x, p, q, k, v, d_o, st);
+    return narrow ? backward<__half, 64>(x, p, q, k, v, d_o, st)
+                  : backward<__half, 128>(x, p, q, k, v, d_o, st);
 }
 
 }  // namespace hd

@@ -280,6 +280,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     volatile uint32_t* gave_up = reinterpret_cast<uint32_t*>(bars + 2 * kMaxStages + 4);
     uint32_t* tmem_at = const_cast<uint32_t*>(gave_up) + 1;
 
+    allow_dependents();
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
     const uint32_t rank = PAIR ? cluster_rank() : 0;
     const int64_t first = PAIR ? blockIdx.x / 2 : blockIdx.x, step = PAIR ? gridDim.x / 2 : gridDim.x;
@@ -307,6 +308,7 @@ __global__ void __launch_bounds__(kThreads, 1)
     else
         __syncthreads();
     fence_after();
+    await_previous();
     const uint32_t tmem = *tmem_at;
     constexpr bool kMayBeDeep = !PAIR && BN <= 64 && (KIND == kGemmLinear || KIND == kGemmGated);
     const int deep = kMayBeDeep ? p.deep : 1;
@@ -526,6 +528,7 @@ struct LayOut {
 };
 constexpr int kLayUnits = 4;  // units of eight values a thread moves at a time, loaded before any is stored
 __global__ void __launch_bounds__(256) lay_out_kernel(const __grid_constant__ LayOut l) {
+    allow_dependents();
     const int o = blockIdx.y;
     const int64_t cols = l.cols[o], per = (cols + 7) / 8, total = l.rows[o] * per;
     const int64_t threads = (int64_t)gridDim.x * 256;
@@ -559,6 +562,7 @@ __global__ void __launch_bounds__(256) lay_out_kernel(const __grid_constant__ La
             *reinterpret_cast<uint4*>(dst[k]) = make_uint4(u[0], u[1], u[2], u[3]);
         }
     }
+    await_previous();  // operands are the caller's, and no kernel before has to do with their places
 }
 
 // The row stride of what is laid out here: whole 128-byte lines, since copies
@@ -655,23 +659,26 @@ cudaError_t run(const OpContext& x, const CUtensorMap (&a)[2], const CUtensorMap
     if (e != cudaSuccess) return e;
     if constexpr (PAIR) {
         cudaLaunchConfig_t cfg{};
-        cudaLaunchAttribute attr;
-        attr.id = cudaLaunchAttributeClusterDimension;
-        attr.val.clusterDim = {2, 1, 1};
+        cudaLaunchAttribute attr[2] = {};
+        attr[0].id = cudaLaunchAttributeClusterDimension;
+        attr[0].val.clusterDim = {2, 1, 1};
+        attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        attr[1].val.programmaticStreamSerializationAllowed = 1;
         cfg.gridDim = dim3(2 * (x.num_sms / 2));
         cfg.blockDim = dim3(kThreads);
         cfg.dynamicSmemBytes = kShared;
         cfg.stream = st;
-        cfg.attrs = &attr;
+        cfg.attrs = attr;
         cfg.numAttrs = 1;
         static std::atomic<int> known[64];
         const int pairs = resident_pairs(k, cfg, x.device, known);
         cfg.gridDim = dim3(2 * (unsigned)(p.tiles < pairs ? p.tiles : pairs));
+        cfg.numAttrs = x.chained ? 2 : 1;
+        x.chained = true;
         return cudaLaunchKernelEx(&cfg, k, a[0], a[1], b[0], b[1], p);
     } else {
         const unsigned grid = (unsigned)(p.tiles < x.num_sms ? p.tiles : x.num_sms);
-        k<<<grid, kThreads, kShared, st>>>(a[0], a[1], b[0], b[1], p);
-        return cudaGetLastError();
+        return launch(x, k, grid, kThreads, kShared, st, a[0], a[1], b[0], b[1], p);
     }
 }
 
@@ -754,8 +761,7 @@ cudaError_t lay_out_operands(const OpContext& x, GemmArgs* const* list, int coun
     for (int i = 0; i < n; ++i) units = l.rows[i] * l.dld[i] / 8 > units ? l.rows[i] * l.dld[i] / 8 : units;
     const int64_t most = (int64_t)x.num_sms * 8, want = ceil_div(units, 256 * kLayUnits);
     const dim3 grid((unsigned)(want < most ? want : most), n);
-    lay_out_kernel<<<grid, 256, 0, st>>>(l);
-    return cudaGetLastError();
+    return launch(x, lay_out_kernel, grid, 256, 0, st, l);
 }
 
 cudaError_t launch_gemm(const OpContext& x, const GemmArgs& args, unsigned char* ws, cudaStream_t st) {

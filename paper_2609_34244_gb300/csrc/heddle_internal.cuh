@@ -8,6 +8,7 @@
 #include <utility>
 
 #include "heddle.h"
+#include "heddle_launch.cuh"
 
 namespace hd {
 
@@ -163,17 +164,9 @@ cudaError_t launch_tables(const TableArgs& a, cudaStream_t st);
 // which a small pricing call would otherwise pay on every launch.
 cudaError_t resident_blocks(const void* func, int block, size_t smem, int* per_sm);
 
-// Programmatic dependent launch: a kernel launched by launch_after may start
-// while the previous kernel of its stream still runs, once every CTA of that
-// one has called allow_dependents (or exited); await_previous returns when
-// the previous kernel has completed and its writes are visible (at once when
-// the kernel was launched the ordinary way).  What the previous kernels write
-// is read by ordinary loads only: the wait does not order the read-only path
-// (__ldg).  A call of one chunk chains its
-// kernels so: with a thousand candidates each runs for little longer than a
-// launch takes.
-__device__ __forceinline__ void allow_dependents() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
-__device__ __forceinline__ void await_previous() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+// Programmatic dependent launch (heddle_launch.cuh).  A call of one chunk
+// chains its kernels so: with a thousand candidates each runs for little longer
+// than a launch takes.
 
 template <class... P, class... A>
 cudaError_t launch_after(bool chained, void (*kernel)(P...), int grid, int block, size_t smem, cudaStream_t st,

@@ -23,9 +23,10 @@ heddle_status fail(OpContext* x, heddle_status st, const char* fmt, ...) {
 // Makes the context's device current for the duration of a call.
 struct OpDeviceGuard {
     int prev = -1;
-    explicit OpDeviceGuard(int dev) {
+    explicit OpDeviceGuard(OpContext* x) {
+        x->chained = false;
         if (cudaGetDevice(&prev) != cudaSuccess) prev = -1;
-        if (prev != dev) cudaSetDevice(dev);
+        if (prev != x->device) cudaSetDevice(x->device);
         else prev = -1;
     }
     ~OpDeviceGuard() {
@@ -177,7 +178,7 @@ heddle_status heddle_linear(heddle_ctx* ctx, const heddle_linear_args* args, voi
     REQUIRE(aligned_to(a.bias, 2), HEDDLE_E_ARG, "bias is not aligned to its element");
     if (a.pre) CHECK(check_matrix(x, "pre", a.pre, a.ldp, a.m, a.n, 4));
     if (a.m == 0 || a.n == 0) return done(x, cudaSuccess, "");
-    OpDeviceGuard guard(x->device);
+    OpDeviceGuard guard(x);
     hd::GemmArgs g{};
     g.M = a.m, g.N = a.n, g.K = a.k;
     g.kind = hd::kGemmLinear, g.dtype = a.dtype, g.act = a.act, g.count = 1;
@@ -208,7 +209,7 @@ heddle_status heddle_linear_backward(heddle_ctx* ctx, const heddle_linear_grad_a
     }
     REQUIRE(aligned_to(a.dbias, 2), HEDDLE_E_ARG, "dbias is not aligned to its element");
     if (a.act != HEDDLE_ACT_NONE) CHECK(check_matrix(x, "pre", a.pre, a.ldp, a.m, a.n, 4));
-    OpDeviceGuard guard(x->device);
+    OpDeviceGuard guard(x);
     cudaStream_t st = (cudaStream_t)stream;
 
     hd::ActGradArgs ag{};
@@ -231,16 +232,17 @@ heddle_status heddle_linear_backward(heddle_ctx* ctx, const heddle_linear_grad_a
     const bool want_x = a.dx && a.m && a.k, want_w = a.dw && a.n && a.k;
     // with dz in the scratch its stride counts, whatever its base will be
     gx.a[0] = gw.a[0] = own_dz ? hd::GemmOperand{nullptr, ag.lddz} : hd::GemmOperand{a.dy, a.lddy};
-    size_t need = (want_x ? hd::gemm_scratch(*x, gx) : 0) + (want_w ? hd::gemm_scratch(*x, gw) : 0);
-    if (need < hd::act_grad_scratch(*x, ag)) need = hd::act_grad_scratch(*x, ag);
-    CHECK(reserve(x, dz_bytes + need));
-    unsigned char* rest = x->ws + dz_bytes;
+    // places of their own: operands are laid out while the activation's gradient is at work
+    const size_t need = (want_x ? hd::gemm_scratch(*x, gx) : 0) + (want_w ? hd::gemm_scratch(*x, gw) : 0);
+    const size_t sums_bytes = hd::act_grad_scratch(*x, ag);
+    CHECK(reserve(x, dz_bytes + sums_bytes + need));
+    unsigned char *sums = x->ws + dz_bytes, *rest = sums + sums_bytes;
     if (own_dz) {
         ag.dz = x->ws;
         gx.a[0] = gw.a[0] = {ag.dz, ag.lddz};
     }
     cudaError_t e = cudaSuccess;
-    if (ag.dz || ag.dbias) e = hd::launch_act_grad(*x, ag, rest, st);
+    if (ag.dz || ag.dbias) e = hd::launch_act_grad(*x, ag, sums, st);
     hd::GemmArgs* both[2];
     int count = 0;
     if (want_x) both[count++] = &gx;
@@ -267,7 +269,7 @@ heddle_status heddle_gated_ffn(heddle_ctx* ctx, const heddle_gated_ffn_args* arg
         CHECK(check_matrix(x, "up", a.up, a.lds, a.m, a.n, 4));
     }
     if (a.m == 0 || a.n == 0) return done(x, cudaSuccess, "");
-    OpDeviceGuard guard(x->device);
+    OpDeviceGuard guard(x);
     hd::GemmArgs g{};
     g.M = a.m, g.N = a.n, g.K = a.k;
     g.kind = hd::kGemmGated, g.dtype = a.dtype, g.act = a.act, g.count = 1;
@@ -302,7 +304,7 @@ heddle_status heddle_gated_ffn_backward(heddle_ctx* ctx, const heddle_gated_ffn_
     }
     const bool want_x = a.dx && a.m && a.k, want_w = a.dw_gate && a.n && a.k;
     if (!want_x && !want_w) return done(x, cudaSuccess, "");
-    OpDeviceGuard guard(x->device);
+    OpDeviceGuard guard(x);
     cudaStream_t st = (cudaStream_t)stream;
 
     const int64_t ld = hd::ceil_div(a.n, 64) * 64;  // rows of whole 128-byte lines for the products
@@ -346,7 +348,7 @@ heddle_status heddle_qk_norm_rope(heddle_ctx* ctx, const heddle_qk_norm_rope_arg
     REQUIRE(args, HEDDLE_E_ARG, "args is null");
     CHECK(check_norm_rope(x, *args, true));
     if (args->tokens == 0 || args->q_heads + args->k_heads == 0) return done(x, cudaSuccess, "");
-    OpDeviceGuard guard(x->device);
+    OpDeviceGuard guard(x);
     return done(x, hd::launch_qk_norm_rope(*x, *args, (cudaStream_t)stream), "heddle_qk_norm_rope");
 }
 
@@ -361,7 +363,7 @@ heddle_status heddle_qk_norm_rope_backward(heddle_ctx* ctx, const heddle_qk_norm
     CHECK(check_heads(x, "dk", args->dk, 1, a.tokens, a.k_heads, a.head_dim, size, true));
     REQUIRE(args->dwq && args->dwk, HEDDLE_E_ARG, "dwq or dwk is null");
     REQUIRE(aligned_to(args->dwq, 4) && aligned_to(args->dwk, 4), HEDDLE_E_ARG, "dwq or dwk is not aligned");
-    OpDeviceGuard guard(x->device);
+    OpDeviceGuard guard(x);
     CHECK(reserve(x, hd::qk_norm_rope_grad_scratch(*x, *args)));
     return done(x, hd::launch_qk_norm_rope_grad(*x, *args, x->ws, (cudaStream_t)stream),
                 "heddle_qk_norm_rope_backward");
@@ -373,7 +375,7 @@ heddle_status heddle_attention(heddle_ctx* ctx, const heddle_attention_args* arg
     REQUIRE(args, HEDDLE_E_ARG, "args is null");
     CHECK(check_attention(x, *args, true));
     if (args->batch == 0 || args->q_len == 0) return done(x, cudaSuccess, "");
-    OpDeviceGuard guard(x->device);
+    OpDeviceGuard guard(x);
     CHECK(reserve(x, hd::attention_scratch(*x, *args)));
     return done(x, hd::launch_attention(*x, *args, x->ws, (cudaStream_t)stream), "heddle_attention");
 }
@@ -390,7 +392,7 @@ heddle_status heddle_attention_backward(heddle_ctx* ctx, const heddle_attention_
     CHECK(check_heads(x, "dv", args->dv, a.batch, a.kv_len, a.kv_heads, a.head_dim, 2, true));
     REQUIRE(a.lse || a.batch * a.q_len == 0, HEDDLE_E_ARG, "lse is null");
     if (a.batch == 0 || (a.q_len == 0 && a.kv_len == 0)) return done(x, cudaSuccess, "");
-    OpDeviceGuard guard(x->device);
+    OpDeviceGuard guard(x);
     // room to keep the scores' gradients, or without them where that is refused
     const size_t most = hd::attention_grad_scratch(*x, *args, true), least = hd::attention_grad_scratch(*x, *args, false);
     const bool keep = !(x->ws_refused && most >= x->ws_refused) && reserve(x, most) == HEDDLE_OK;

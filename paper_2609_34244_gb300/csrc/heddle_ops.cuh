@@ -9,7 +9,10 @@
 #include <math.h>
 #include <stdint.h>
 
+#include <utility>
+
 #include "heddle.h"
+#include "heddle_launch.cuh"
 
 namespace hd {
 
@@ -28,7 +31,30 @@ struct OpContext {
     size_t ws_refused = 0;  // the least scratch that the device had no room for, where a call can do without
     char* msg = nullptr;
     size_t msg_size = 0;
+    mutable bool chained = false;  // the call has launched a kernel already
 };
+
+// A kernel of a call.  All but the first start under the end of the one before
+// (their launch, barriers and tensor memory cost a few microseconds): every
+// kernel allows that at its start, and waits in some thread of every block,
+// whatever its share of the work, before it reads what the call's kernels
+// wrote and before it writes.  The caller's own tensors may be read earlier.
+template <class... P, class... A>
+cudaError_t launch(const OpContext& x, void (*kernel)(P...), dim3 grid, int block, size_t smem, cudaStream_t st,
+                   A&&... args) {
+    cudaLaunchAttribute attr{};
+    attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr.val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchConfig_t cfg{};
+    cfg.gridDim = grid;
+    cfg.blockDim = dim3((unsigned)block);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cfg.attrs = &attr;
+    cfg.numAttrs = x.chained ? 1 : 0;
+    x.chained = true;
+    return cudaLaunchKernelEx(&cfg, kernel, std::forward<A>(args)...);
+}
 
 inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 inline size_t align256(size_t v) { return (v + 255) & ~(size_t)255; }

@@ -51,6 +51,8 @@ constexpr int kRowsPerBlock = 8;  // rows in flight, one per warp
 // of them; the chunk's column sums go to partial[chunk][n].
 template <class T, int V>
 __global__ void __launch_bounds__(256) act_grad_kernel(ActGradArgs a, float* partial, int64_t rows_per_chunk) {
+    allow_dependents();
+    await_previous();
     const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
     const int64_t n0 = ((int64_t)blockIdx.x * 32 + lane) * V;
     const int64_t first = blockIdx.y * rows_per_chunk;
@@ -97,6 +99,8 @@ __global__ void __launch_bounds__(256) act_grad_kernel(ActGradArgs a, float* par
 
 template <class T>
 __global__ void __launch_bounds__(256) column_sum_kernel(const float* partial, int chunks, int64_t n, T* out) {
+    allow_dependents();
+    await_previous();
     const int64_t c = (int64_t)blockIdx.x * 256 + threadIdx.x;
     if (c >= n) return;
     float v = 0.0f;
@@ -107,6 +111,8 @@ __global__ void __launch_bounds__(256) column_sum_kernel(const float* partial, i
 
 template <class T, int V>
 __global__ void __launch_bounds__(256) gate_grad_kernel(GateGradArgs a) {
+    allow_dependents();
+    await_previous();
     const int64_t per_row = (a.n + V - 1) / V;
     const int64_t total = a.m * per_row;
     for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < total; i += (int64_t)gridDim.x * 256) {
@@ -148,13 +154,13 @@ cudaError_t act_grad(const OpContext& x, const ActGradArgs& a, unsigned char* ws
     if (chunks) {
         const dim3 grid((unsigned)bx, (unsigned)chunks);
         if (wide)
-            act_grad_kernel<T, 8><<<grid, 256, 0, st>>>(a, partial, rows);
+            launch(x, act_grad_kernel<T, 8>, grid, 256, 0, st, a, partial, rows);
         else
-            act_grad_kernel<T, 1><<<grid, 256, 0, st>>>(a, partial, rows);
+            launch(x, act_grad_kernel<T, 1>, grid, 256, 0, st, a, partial, rows);
     }
     if (partial)
-        column_sum_kernel<T><<<(unsigned)ceil_div(a.n, 256), 256, 0, st>>>(partial, (int)chunks, a.n,
-                                                                           static_cast<T*>(a.dbias));
+        launch(x, column_sum_kernel<T>, dim3((unsigned)ceil_div(a.n, 256)), 256, 0, st, partial, (int)chunks, a.n,
+               static_cast<T*>(a.dbias));
     return cudaGetLastError();
 }
 
@@ -166,9 +172,9 @@ cudaError_t gate_grad(const OpContext& x, const GateGradArgs& a, cudaStream_t st
     const int64_t most = (int64_t)x.num_sms * 32;
     const unsigned grid = (unsigned)(ceil_div(total, 256) < most ? ceil_div(total, 256) : most);
     if (wide)
-        gate_grad_kernel<T, 8><<<grid, 256, 0, st>>>(a);
+        launch(x, gate_grad_kernel<T, 8>, grid, 256, 0, st, a);
     else
-        gate_grad_kernel<T, 1><<<grid, 256, 0, st>>>(a);
+        launch(x, gate_grad_kernel<T, 1>, grid, 256, 0, st, a);
     return cudaGetLastError();
 }
 

@@ -27,6 +27,8 @@ template <class T, bool GRAD>
 __global__ void __launch_bounds__(kWarps * 32) qk_norm_rope_kernel(heddle_qk_norm_rope_grad_args ga, float* partial,
                                                                   uint32_t* err) {
     const heddle_qk_norm_rope_args& a = ga.fwd;
+    allow_dependents();
+    await_previous();
     __shared__ float row[kWarps][kMaxDim];
     __shared__ float grad[kWarps][kMaxDim];
     const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
@@ -182,6 +184,8 @@ template <class T, int GL, bool GRAD, RotaryCase CASE>
 __global__ void __launch_bounds__(256, 3)
     qk_norm_rope_wide_kernel(const __grid_constant__ heddle_qk_norm_rope_grad_args ga, float* partial, uint32_t* err,
                              int q_blocks, int chunk, bool whole_units) {
+    allow_dependents();
+    await_previous();
     constexpr int V = 16 / sizeof(T), H = V / 2, kGroups = 256 / GL, kDepth = GRAD ? 2 : 4;
     const heddle_qk_norm_rope_args& a = ga.fwd;
     const bool is_q = blockIdx.x < q_blocks;
@@ -347,6 +351,8 @@ __global__ void __launch_bounds__(256, 3)
 // (the first q_blocks blocks) or dwk (the next k_blocks).
 __global__ void __launch_bounds__(1024) weight_grad_kernel(const float* partial, int q_blocks, int k_blocks, int D,
                                                            float* dwq, float* dwk) {
+    allow_dependents();
+    await_previous();
     __shared__ float s[32][33];
     const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
     const int i = blockIdx.x * 32 + lane;
@@ -431,7 +437,7 @@ void launch_wide(const Launch& l, const OpContext& x, const heddle_qk_norm_rope_
                                               : qk_norm_rope_wide_kernel<T, GL, GRAD, kPairs>)
                                        : (all ? qk_norm_rope_wide_kernel<T, GL, GRAD, kAllHalves>
                                               : qk_norm_rope_wide_kernel<T, GL, GRAD, kHalves>);
-    kernel<<<blocks, 256, 0, st>>>(a, partial, x.err, l.q_blocks, l.chunk, l.whole);
+    launch(x, kernel, dim3(blocks), 256, 0, st, a, partial, x.err, l.q_blocks, l.chunk, l.whole);
 }
 
 template <class T, bool GRAD>
@@ -439,7 +445,7 @@ void launch_typed(const Launch& l, const OpContext& x, const heddle_qk_norm_rope
                   cudaStream_t st) {
     const int blocks = l.q_blocks + l.k_blocks;
     if (!l.wide)
-        qk_norm_rope_kernel<T, GRAD><<<l.q_blocks, kWarps * 32, 0, st>>>(a, partial, x.err);
+        launch(x, qk_norm_rope_kernel<T, GRAD>, dim3(l.q_blocks), kWarps * 32, 0, st, a, partial, x.err);
     else if (blocks == 0)
         return;
     else if (l.lanes == 8)
@@ -481,8 +487,8 @@ cudaError_t launch_qk_norm_rope_grad(const OpContext& x, const heddle_qk_norm_ro
     const Launch l = plan_rows(x, a, true);
     launch_rows<true>(l, x, a, partial, st);
     const int D = a.fwd.head_dim;
-    weight_grad_kernel<<<dim3((unsigned)ceil_div(D, 32), 2), 1024, 0, st>>>(partial, l.q_blocks, l.k_blocks, D, a.dwq,
-                                                                            a.dwk);
+    launch(x, weight_grad_kernel, dim3((unsigned)ceil_div(D, 32), 2), 1024, 0, st, partial, l.q_blocks, l.k_blocks, D,
+           a.dwq, a.dwk);
     return cudaGetLastError();
 }
 
