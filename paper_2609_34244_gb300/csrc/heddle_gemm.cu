@@ -69,6 +69,7 @@ struct KernelArgs {
     int32_t m_tiles, n_tiles;
     int64_t tiles;
     int32_t vec;         // outputs, residual, bias and saved sums by 16- and 8-byte accesses
+    int32_t direct;      // outputs, residual and saved sums by 32-byte accesses, a row a lane
     uint32_t* err;
 };
 
@@ -119,6 +120,41 @@ __device__ __forceinline__ void store_four(T* p, const float (&v)[4]) {
         for (int j = 0; j < 4; ++j) t[j] = from_float<T>(v[j]);
         *reinterpret_cast<uint2*>(p) = u;
     }
+}
+
+// Sixteen columns of a row as they come from tensor memory, a row a lane: the
+// 32 bytes that memory is written by.  Through shared memory a warp's rows came
+// out side by side, but one block waited for the next: weights' gradients of 17
+// rows, all output, at 1.7e12 bytes a second.
+__device__ __forceinline__ void store_32(void* p, const uint32_t* v) {
+    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(__cvta_generic_to_global(p)),
+                 "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7])
+                 : "memory");
+}
+__device__ __forceinline__ void load_32(const void* p, uint32_t* v) {
+    const uint4 a = *static_cast<const uint4*>(p), b = *(static_cast<const uint4*>(p) + 1);
+    v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w, v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
+}
+template <class T>
+__device__ __forceinline__ void finish_row(const KernelArgs& p, void* out, int64_t m, int64_t n0, bool live,
+                                           uint32_t (&v)[kCols], const uint32_t (&r)[kCols], bool linear) {
+    const GemmArgs& g = p.g;
+    if (linear && g.bias) {
+        uint32_t b[8];
+        load_32(static_cast<const T*>(g.bias) + n0, b);
+#pragma unroll
+        for (int j = 0; j < kCols; ++j)
+            v[j] = __float_as_uint(__uint_as_float(v[j]) + to_float(reinterpret_cast<const T*>(b)[j]));
+    }
+    if (linear && g.residual) {
+#pragma unroll
+        for (int j = 0; j < kCols; ++j)
+            v[j] = __float_as_uint(__uint_as_float(v[j]) + to_float(reinterpret_cast<const T*>(r)[j]));
+    }
+    uint32_t w[8];
+#pragma unroll
+    for (int j = 0; j < kCols; ++j) reinterpret_cast<T*>(w)[j] = from_float<T>(__uint_as_float(v[j]));
+    if (live) store_32(static_cast<T*>(out) + m * g.ldo + n0, w);
 }
 
 // How a warp goes over a block of 32 rows x 16 columns: neighbouring lanes on
@@ -447,9 +483,16 @@ __global__ void __launch_bounds__(kThreads, 1)
                 const int64_t n0 = (int64_t)tn * kOut + c;
                 if (!rows || n0 >= p.g.N) break;
                 uint32_t v[kAhead][kCols], u[kCols], r[kAhead][kCols];
+                const int64_t row = m0 + lane;
+                const bool direct = p.direct && n0 + kAhead * kCols <= p.g.N;
                 if (KIND == kGemmLinear && p.g.residual) {
 #pragma unroll
-                    for (int h = 0; h < kAhead; ++h) fetch_residual(p, m0, n0 + h * kCols, r[h]);
+                    for (int h = 0; h < kAhead; ++h) {
+                        if (!direct)
+                            fetch_residual(p, m0, n0 + h * kCols, r[h]);
+                        else if (row < p.g.M)
+                            load_32(static_cast<const uint16_t*>(p.g.residual) + row * p.g.ldr + n0 + h * kCols, r[h]);
+                    }
                 }
                 if (per_tile) {
 #pragma unroll
@@ -461,7 +504,13 @@ __global__ void __launch_bounds__(kThreads, 1)
                     for (int j = 0; j < kAhead * kCols; ++j) v[j / kCols][j % kCols] = u[j % kCols] = 0;  // a sum over nothing
                 }
                 if (KIND == kGemmGated) {
-                    if (p.g.pre[0]) {
+                    if (p.g.pre[0] && direct) {
+                        if (row < p.g.M) {
+                            float *pg = p.g.pre[0] + row * p.g.ldp + n0, *pu = p.g.pre[1] + row * p.g.ldp + n0;
+                            store_32(pg, v[0]), store_32(pg + 8, v[0] + 8);
+                            store_32(pu, u), store_32(pu + 8, u + 8);
+                        }
+                    } else if (p.g.pre[0]) {
                         put_row(t0, v[0], lane);
                         __syncwarp();
                         store_block<float, false>(p, p.g.pre[0], p.g.ldp, m0, n0, t0, u);
@@ -478,6 +527,14 @@ __global__ void __launch_bounds__(kThreads, 1)
 #pragma unroll
                 for (int h = 0; h < kAhead; ++h) {
                     if (h && (c + h * kCols >= to || n0 + h * kCols >= p.g.N)) break;
+                    if (direct) {
+                        if (p.g.dtype == HEDDLE_BF16)
+                            finish_row<__nv_bfloat16>(p, p.g.out[z], row, n0 + h * kCols, row < p.g.M, v[h], r[h],
+                                                      kLinear);
+                        else
+                            finish_row<__half>(p, p.g.out[z], row, n0 + h * kCols, row < p.g.M, v[h], r[h], kLinear);
+                        continue;
+                    }
                     put_row(t0, v[h], lane);
                     __syncwarp();
                     if (p.g.dtype == HEDDLE_BF16)
@@ -778,6 +835,13 @@ cudaError_t launch_gemm(const OpContext& x, const GemmArgs& args, unsigned char*
     p.vec = unit16(g.out[0], g.ldo, size, 8) && unit16(g.out[1], g.ldo, size, 8) &&
             unit16(g.residual, g.ldr, size, 8) && unit16(g.bias, 0, size, 8) && unit16(g.pre[0], g.ldp, 4, 16) &&
             unit16(g.pre[1], g.ldp, 4, 16);
+
+    // an activation goes over a block in shared memory
+    p.direct = (g.kind != kGemmLinear || g.act == HEDDLE_ACT_NONE) && unit16(g.out[0], g.ldo, size, 32) &&
+               unit16(g.out[1], g.ldo, size, 32) && unit16(g.residual, g.ldr, size, 32) &&
+               unit16(g.bias, 0, size, 16) &&
+               (g.kind == kGemmLinear ? !g.pre[0]
+                                      : unit16(g.pre[0], g.ldp, 4, 32) && unit16(g.pre[1], g.ldp, 4, 32));
 
     const Tile tile = choose_tile(x, g);
     const bool across_a = g.kind == kGemmPair, across_b = across_a || g.kind == kGemmSum;
