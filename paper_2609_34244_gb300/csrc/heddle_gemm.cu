@@ -747,16 +747,18 @@ struct Tile {
 
 // The tile that finishes first by the cycles a 64-wide step of its products
 // takes (measured on steps from L2: what is fetched bounds all but the pair),
-// the rounds of tiles that the SMs run, and the last one's epilogue, about 60
-// cycles a column.
-Tile choose_tile(const OpContext& x, const GemmArgs& g) {
+// those of its epilogue, which the next tile's products hide or not, the rounds
+// of tiles that the SMs run, and the start of a pair.  Weights' gradients of 17
+// rows, 4544 x 13376: 31 us on single 256-wide tiles, 43 on pairs, 58 on pairs
+// of 128; 1024 x 4096 x 4096: 25.5 and 27.3, 2048 x 4096 x 14336 the pair's.
+Tile choose_tile(const OpContext& x, const GemmArgs& g, bool direct) {
     const int64_t batch = g.kind == kGemmPair ? g.count : 1;
     const int64_t steps = ceil_div(g.K, BK) * (g.kind == kGemmSum ? g.count : 1);
     const struct {
         Tile t;
         double cycles;
     } all[] = {{{256, true}, 545}, {{224, true}, 485}, {{192, true}, 425}, {{128, true}, 340},
-               {{256, false}, 660},               {{128, false}, 440}, {{64, false}, 340}, {{32, false}, 300}};
+               {{256, false}, 660}, {{128, false}, 440}, {{64, false}, 340}, {{32, false}, 300}};
     Tile best{256, false};
     double least = 1e300;
     for (const auto& c : all) {
@@ -765,11 +767,13 @@ Tile choose_tile(const OpContext& x, const GemmArgs& g) {
         if (c.t.pair && c.t.bn % 128 && g.kind != kGemmLinear) continue;  // B's halves in whole copies
         const int out = g.kind == kGemmGated ? c.t.bn / 2 : c.t.bn;
         const int64_t tiles = ceil_div(g.M, c.t.pair ? 2 * BM : BM) * ceil_div(g.N, out) * batch;
-        const int64_t at_once = c.t.pair ? x.num_sms / 2 : x.num_sms;
-        // few rows: B streams from memory, a step as long as its bytes' share
+        const int64_t rounds = ceil_div(tiles, c.t.pair ? x.num_sms / 2 : x.num_sms);
+        // few rows: B streams from memory, a step as long as its bytes' share,
+        // or as its barriers where a stage holds one
         double cycles = c.cycles;
-        if (g.M <= 64) cycles = c.t.bn * 2.2;
-        const double time = (double)ceil_div(tiles, at_once) * steps * cycles + 60.0 * c.t.bn;
+        if (g.M <= 64) cycles = c.t.bn * 2.2 < 250 && g.kind == kGemmSum ? 250 : c.t.bn * 2.2;
+        const double sums = steps * cycles, end = (c.t.pair ? 2450 : 900) + (direct ? 15.0 : 45.0) * out;
+        const double time = (c.t.pair ? 6000 : 0) + (rounds - 1) * (sums < end ? end : sums) + sums + end;
         if (time < least) least = time, best = c.t;
     }
     return best;
@@ -843,7 +847,7 @@ cudaError_t launch_gemm(const OpContext& x, const GemmArgs& args, unsigned char*
                (g.kind == kGemmLinear ? !g.pre[0]
                                       : unit16(g.pre[0], g.ldp, 4, 32) && unit16(g.pre[1], g.ldp, 4, 32));
 
-    const Tile tile = choose_tile(x, g);
+    const Tile tile = choose_tile(x, g, p.direct);
     const bool across_a = g.kind == kGemmPair, across_b = across_a || g.kind == kGemmSum;
     p.a_rows = across_a ? 64 : (int)(g.M < BM ? ceil_div(g.M, 8) * 8 : BM);
     CUtensorMap a[2] = {}, b[2] = {};
