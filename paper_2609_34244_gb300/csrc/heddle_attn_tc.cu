@@ -276,9 +276,17 @@ __device__ __forceinline__ void store_floats(uint32_t tmem, float* out, bool liv
                 *reinterpret_cast<uint4*>(out + c + j) = make_uint4(v[j], v[j + 1], v[j + 2], v[j + 3]);
     }
 }
+// A row of zeros: whole units of eight values, as a head has, where they lie
+// so (value by value a tile past its sequence's end took longer than three
+// tiles of keys).
 template <class T>
 __device__ __forceinline__ void zero_row(T* out, int D) {
-    for (int c = 0; c < D; ++c) out[c] = from_float<T>(0.0f);
+    constexpr int kUnit = 16 / sizeof(T);
+    if (((uintptr_t)out & 15) == 0) {
+        for (int c = 0; c < D; c += kUnit) *reinterpret_cast<uint4*>(out + c) = make_uint4(0, 0, 0, 0);
+    } else {
+        for (int c = 0; c < D; ++c) out[c] = from_float<T>(0.0f);
+    }
 }
 
 // ------------------------------------------------------------------- forward
@@ -1375,7 +1383,7 @@ __global__ void __launch_bounds__(kGradThreads, 1)
                 if (n > 0)
                     store_floats<DP / 2>(from, to, true, D, f);
                 else
-                    for (int x = 0; x < min(D, DP / 2); ++x) to[x] = 0.0f;
+                    zero_row(to, min(D, DP / 2));
             } else if (n > 0) {
                 store_row<T, DP / 2>(from, out, inside, D, f);
             } else if (inside) {
