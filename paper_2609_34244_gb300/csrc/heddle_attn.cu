@@ -263,8 +263,8 @@ cudaError_t attention_grad(const OpContext& x, const heddle_attention_grad_args&
     if (tc) {
         const bool all = a.window && a.window + a.sinks <= kFewKeys;
         const int64_t per = all || a.q_len < kFewKeys ? a.q_len : kFewKeys;
-        launch(x, attn_few_delta_kernel<T>, dim3((unsigned)ceil_div(a.batch * a.q_heads * per, 256 / kFewKeys)), 256, 0, st,
-               g, delta, per, all || a.q_len < kFewKeys);
+        const unsigned blocks = (unsigned)ceil_div(a.batch * a.q_heads * per, 256 / kFewKeys);
+        launch(x, attn_few_delta_kernel<T>, dim3(blocks), 256, 0, st, g, delta, per, all || a.q_len < kFewKeys);
         const cudaError_t e = cudaGetLastError();
         return e == cudaSuccess ? launch_attn_tc_grad(x, g, delta, rest, keep, st) : e;
     }

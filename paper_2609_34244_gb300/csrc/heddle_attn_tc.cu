@@ -300,9 +300,9 @@ __device__ __forceinline__ void zero_row(T* out, int D) {
 // a chain of trips to tensor memory (some 600 cycles each), barriers and 128
 // exponentials a thread; the two tiles hide each other's.  Bound by that chain
 // where sequences are short, with the prologue and epilogue of a CTA: two
-// causal sequences of 2048, 32 heads over 8 of 128, 84 us (8.2e14 operations a
-// second); by the tensor cores and the exponentials together where they are
-// long: one of 8192 takes 433 us (1.27e15).
+// causal sequences of 2048, 32 heads over 8 of 128, 82 us (8.3e14 operations a
+// second); one of 8192 takes 422 us (1.3e15).  Not by the exponentials: an
+// eighth of them as polynomials took 428, a quarter 487.
 template <int DP, int NT>
 struct Forward {
     static constexpr int kTileBytes = kTile * DP * 2;
@@ -631,7 +631,7 @@ __global__ void __launch_bounds__(Forward<DP, NT>::kThreads, 1)
 // Joins the parts of rows split along the keys, one warp a row: a call of few
 // query tiles takes the keys in parts, enough for every SM.  Single tokens read
 // the cache once: 16 histories of up to 8192 with a window of 4096, 8 key heads
-// of 128, 269 MB in 51 us both kernels (5.2e12 bytes a second).
+// of 128, 269 MB in 52 us both kernels (5.2e12 bytes a second).
 template <class T>
 __global__ void __launch_bounds__(256) attn_join_kernel(const __grid_constant__ Params p) {
     allow_dependents();
@@ -742,9 +742,9 @@ struct GradBars {
 };
 constexpr int kGradBarBytes = 160;
 
-// dq of a query tile: dq = scale sum over key tiles of dS K with
-// S = Q K^T, dP = dO V^T, dS = P (dP - delta).  Q and dO stay in shared
-// memory, K and V tiles come in two stages.  Scores of the next tile are
+// dq of a query tile where dS is not kept: dq = scale sum over key tiles of
+// dS K with S = Q K^T, dP = dO V^T, dS = P (dP - delta).  Q and dO stay in
+// shared memory, K and V tiles come in two stages.  Scores of the next tile are
 // computed while this one's are turned into dS (two buffers).  CTAs take one
 // query tile after another, the longest first (a grid of one tile each: 137 us
 // against 119).  Bound by the chain from scores to dS as the forward is:
@@ -956,7 +956,8 @@ __global__ void __launch_bounds__(kGradThreads, 1)
 
 // dq from dS as the pass over keys left it: dq = scale sum over key tiles of
 // dS K, one product of 128 x 128 by 128 x head_dim a step.  Bound by the stream
-// of dS from memory, 32 KB a pair of tiles.  CTAs take one query tile after
+// of dS from memory, 32 KB a pair of tiles: 54 us for two causal sequences of
+// 2048 (32 heads over 8 of 128; 114 with the scores computed again).  CTAs take one query tile after
 // another, the longest first; sums alternate between two places of tensor
 // memory, so that one tile's result is written under the next one's products.
 template <int DP>
@@ -1125,8 +1126,8 @@ __device__ __forceinline__ int64_t dkv_slot(const Params& p, bool lead, int tile
 // are computed transposed, keys along the lanes, so that P^T and dS^T are left
 // operands in tensor memory as they come: S^T = K Q^T, dP^T = V dO^T,
 // dv += P^T dO, dk += dS^T Q.  The tensor cores are busy half of the time,
-// bound by the chain as above: 101 us for two causal sequences of 2048 (32
-// heads over 8 of 128).  Tiles of 64 queries in two groups of warps by turns
+// bound by the chain as above: 120 us for two causal sequences of 2048 (32
+// heads over 8 of 128), 101 where dS is not kept.  Tiles of 64 queries in two groups of warps by turns
 // took 117: products of 64 columns read their left operand twice as often.
 template <class T, int DP>
 __global__ void __launch_bounds__(kGradThreads, 1)
@@ -1251,8 +1252,9 @@ __global__ void __launch_bounds__(kGradThreads, 1)
         const uint64_t c2 = two(p.scale_log2, p.scale_log2);
 
         // where dS goes, less the query tile's part: all of it is below 2^32 bytes
-        const uint32_t ds_at =
-            p.ds ? (uint32_t)((hb - p.hb0) * p.ds_head + ds_col(p, k0 / kTile)) * kPlaceBytes + side * (4 * kTile * 16) + row * 16 : 0;
+        const uint32_t ds_at = !p.ds ? 0
+                                     : (uint32_t)((hb - p.hb0) * p.ds_head + ds_col(p, k0 / kTile)) * kPlaceBytes +
+                                           side * (4 * kTile * 16) + row * 16;
 
         // statistics of query tile j to buffer j % 3, by three of the sides: written
         // a step ahead, while the slowest warp may still read those of the step
@@ -1501,7 +1503,8 @@ Params params_of(const OpContext& x, const heddle_attention_args& a) {
 // Whether dS is kept for the pass over queries, and its places.  It is where
 // they come to at most kMostKept bytes for as many key heads as the SMs need;
 // beyond, the scores are computed in both passes.  Kept: two causal sequences
-// of 2048 XX us against YY, one of 8192 XX against YY.
+// of 2048 took 175 us in these two kernels, 215 computed twice; one of 8192 the
+// whole backward 1230 and 1380.
 constexpr int64_t kMostKept = (int64_t)4 << 30;
 int64_t keep_ds(const OpContext& x, Params& p) {
     const heddle_attention_args& a = p.a;
@@ -1538,7 +1541,8 @@ int64_t dkv_slots(const Params& p) {
 }
 
 template <class T, int DP, int NT, bool TWINS>
-cudaError_t forward(const OpContext& x, const Params& p, const CUtensorMap& q, const CUtensorMap& k, const CUtensorMap& v,
+cudaError_t forward(const OpContext& x, const Params& p, const CUtensorMap& q, const CUtensorMap& k,
+                    const CUtensorMap& v,
                     cudaStream_t st) {
     using F = Forward<DP, NT>;
     static_assert(F::kSlots >= 4, "two steps of K and V");
@@ -1570,10 +1574,12 @@ cudaError_t backward(const OpContext& x, Params p, const CUtensorMap& q, const C
     const int each = p.hbs;
     for (p.hb0 = 0; p.hb0 < heads; p.hb0 += each) {
         p.hbs = (int32_t)(heads - p.hb0 < each ? heads - p.hb0 : each);
-        launch(x, attn_dkv_kernel<T, DP>, dim3((unsigned)(p.hbs * tiles)), kGradThreads, G::kBytes, st, q, k, v, d_o, p);
+        launch(x, attn_dkv_kernel<T, DP>, dim3((unsigned)(p.hbs * tiles)), kGradThreads, G::kBytes, st, q, k, v, d_o,
+               p);
         const int64_t pieces = (int64_t)p.q_tiles * p.hbs, grid = pieces < x.num_sms ? pieces : x.num_sms;
         if (p.ds)
-            launch(x, attn_dq_stored_kernel<T, DP>, dim3((unsigned)grid), S::kThreads, S::kBytes, st, k, p, (int)pieces);
+            launch(x, attn_dq_stored_kernel<T, DP>, dim3((unsigned)grid), S::kThreads, S::kBytes, st, k, p,
+                   (int)pieces);
         else
             launch(x, attn_dq_kernel<T, DP>, dim3((unsigned)grid), kGradThreads, G::kBytes, st, q, k, v, d_o, p,
                    (int)pieces);
@@ -1586,7 +1592,8 @@ cudaError_t backward(const OpContext& x, Params p, const CUtensorMap& q, const C
 }
 
 template <class T>
-cudaError_t forward_of(const OpContext& x, const Params& p, const CUtensorMap& q, const CUtensorMap& k, const CUtensorMap& v,
+cudaError_t forward_of(const OpContext& x, const Params& p, const CUtensorMap& q, const CUtensorMap& k,
+                       const CUtensorMap& v,
                        cudaStream_t st) {
     const bool two = tiles_per_block(p.a) == 2;
     if (p.a.head_dim <= 64)

@@ -12,12 +12,13 @@
 // whose stream from memory is then the time.
 //
 // Bound by the tensor cores where rows are many: 2048 x 4096 x 14336 in
-// bfloat16 with the residual 139 us (1.73e15 operations a second), its
-// gradients 125 us each (1.92e15); the gated block's 4096 x 14336 x 4096
-// 505 us forward with both sums saved in 32 bits, 542 us for dx, 482 us for
-// the weights' gradients (2e15: single CTAs of 128 x 256 reached 1.4e15, the
-// copies from L2 being their time).  With 16 rows of the gated block the
-// weights' stream takes 40 us (5.9e12 bytes a second).
+// bfloat16 with the residual 130 us (1.85e15 operations a second), its
+// gradients 124 us each (1.94e15); the gated block's 4096 x 14336 x 4096
+// 515 us forward with both sums saved in 32 bits (1.87e15), 550 us for dx,
+// 490 us for the weights' gradients (1.96e15: single CTAs of 128 x 256 reached
+// 1.4e15, the copies from L2 being their time).  With 16 rows of the gated
+// block the weights' stream takes 40 us (5.9e12 bytes a second).  Bound by
+// their epilogue where the contraction is short (choose_tile).
 
 #include <mutex>
 
@@ -123,9 +124,10 @@ __device__ __forceinline__ void store_four(T* p, const float (&v)[4]) {
 }
 
 // Sixteen columns of a row as they come from tensor memory, a row a lane: the
-// 32 bytes that memory is written by.  Through shared memory a warp's rows came
-// out side by side, but one block waited for the next: weights' gradients of 17
-// rows, all output, at 1.7e12 bytes a second.
+// 32 bytes that memory is written by.  Through shared memory a warp's rows come
+// out side by side, but each block waits for the one before: weights' gradients
+// of 17 rows, 243 MB and all of it output, 140 us, this way 106, and 116 with
+// rows of 128 bytes gathered in shared memory.
 __device__ __forceinline__ void store_32(void* p, const uint32_t* v) {
     asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(__cvta_generic_to_global(p)),
                  "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]), "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7])
@@ -501,7 +503,8 @@ __global__ void __launch_bounds__(kThreads, 1)
                     wait_ld();
                 } else {
 #pragma unroll
-                    for (int j = 0; j < kAhead * kCols; ++j) v[j / kCols][j % kCols] = u[j % kCols] = 0;  // a sum over nothing
+                    for (int j = 0; j < kAhead * kCols; ++j)
+                        v[j / kCols][j % kCols] = u[j % kCols] = 0;  // a sum over nothing
                 }
                 if (KIND == kGemmGated) {
                     if (p.g.pre[0] && direct) {

@@ -394,7 +394,8 @@ heddle_status heddle_attention_backward(heddle_ctx* ctx, const heddle_attention_
     if (a.batch == 0 || (a.q_len == 0 && a.kv_len == 0)) return done(x, cudaSuccess, "");
     OpDeviceGuard guard(x);
     // room to keep the scores' gradients, or without them where that is refused
-    const size_t most = hd::attention_grad_scratch(*x, *args, true), least = hd::attention_grad_scratch(*x, *args, false);
+    const size_t most = hd::attention_grad_scratch(*x, *args, true);
+    const size_t least = hd::attention_grad_scratch(*x, *args, false);
     const bool keep = !(x->ws_refused && most >= x->ws_refused) && reserve(x, most) == HEDDLE_OK;
     if (!keep) {
         if (!x->ws_refused || most < x->ws_refused) x->ws_refused = most;

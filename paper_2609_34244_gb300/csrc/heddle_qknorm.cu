@@ -359,7 +359,7 @@ __global__ void __launch_bounds__(1024) weight_grad_kernel(const float* partial,
     float v = 0.0f;
     const int first = blockIdx.y ? q_blocks : 0, blocks = blockIdx.y ? k_blocks : q_blocks;
     if (i < D)
-#pragma unroll 4
+#pragma unroll 8
         for (int b = warp; b < blocks; b += 32) v += partial[(int64_t)(first + b) * D + i];
     s[warp][lane] = v;
     __syncthreads();
@@ -372,7 +372,8 @@ __global__ void __launch_bounds__(1024) weight_grad_kernel(const float* partial,
 int elem_bytes(int32_t dtype) { return dtype == HEDDLE_FP32 ? 4 : 2; }
 
 bool units8(const heddle_heads& t, int heads, int size) {
-    return heads == 0 || ((uintptr_t)t.data % 8 == 0 && t.token_stride * size % 8 == 0 && t.head_stride * size % 8 == 0);
+    return heads == 0 ||
+           ((uintptr_t)t.data % 8 == 0 && t.token_stride * size % 8 == 0 && t.head_stride * size % 8 == 0);
 }
 
 // Heads of whole 16-byte units in at most 32 lanes, whole lanes of turned
@@ -410,7 +411,8 @@ Launch plan_rows(const OpContext& x, const heddle_qk_norm_rope_grad_args& g, boo
     // as many heads a group, up to eight, as leave every group that runs at a
     // time four units of them
     for (l.chunk = 8; l.chunk > 1; l.chunk /= 2)
-        if (a.tokens * (ceil_div(a.q_heads, l.chunk) + ceil_div(a.k_heads, l.chunk)) >= (int64_t)x.num_sms * groups * 12)
+        if (a.tokens * (ceil_div(a.q_heads, l.chunk) + ceil_div(a.k_heads, l.chunk)) >=
+            (int64_t)x.num_sms * groups * 12)
             break;
     const int64_t q_want = ceil_div(a.tokens * ceil_div(a.q_heads, l.chunk), groups),
                   k_want = ceil_div(a.tokens * ceil_div(a.k_heads, l.chunk), groups);
