@@ -829,7 +829,7 @@ cudaError_t lay_out_operands(const OpContext& x, GemmArgs* const* list, int coun
 }
 
 cudaError_t launch_gemm(const OpContext& x, const GemmArgs& args, unsigned char* ws, cudaStream_t st) {
-    if (gemv_takes(args)) return launch_gemv(x, args, st);
+    if (gemv_takes(x, args)) return launch_gemv(x, args, st);
     KernelArgs p{};
     p.g = args;
     p.deep = 1;

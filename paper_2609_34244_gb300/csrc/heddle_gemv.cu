@@ -1,5 +1,5 @@
-// heddle_gemv.cu -- the forward products of one or two rows: the weights'
-// stream from memory is the time.
+// heddle_gemv.cu -- the forward products of one or two rows, and of up to eight
+// with few weights: the weights' stream from memory is the time.
 //
 // A block of eight warps takes four rows of weights (two of each matrix of
 // the gated block); every warp an eighth of the contraction, 16 bytes a lane
@@ -7,8 +7,7 @@
 // are summed in 32 bits per lane, across the lanes, then across the warps in
 // order.  One row of 4096 x 4096 bfloat16 weights: 7.7 us with its launch,
 // 5.7 us of the kernel alone (5.9e12 bytes a second); the tensor cores' kernel
-// takes 12.9.  From four rows on that one is as fast (11.3 us both), at eight
-// twice as fast, since every row costs this one as many multiply-adds again.
+// takes 12.9.  Every row costs as many multiply-adds again (gemv_takes).
 
 #include "heddle_ops.cuh"
 
@@ -39,7 +38,7 @@ __global__ void __launch_bounds__(256) gemv_kernel(const __grid_constant__ GemmA
             w[r] = static_cast<const T*>(b.p) + n * b.ld;
         }
         float acc[kRows][M] = {};
-#pragma unroll 2
+#pragma unroll(M <= 2 ? 2 : 1)
         for (int64_t u = warp * 32 + lane; u < units; u += kWarps * 32) {
             uint4 wv[kRows], xv[M];
 #pragma unroll
@@ -47,7 +46,7 @@ __global__ void __launch_bounds__(256) gemv_kernel(const __grid_constant__ GemmA
 #pragma unroll
             for (int m = 0; m < M; ++m)
                 xv[m] = *reinterpret_cast<const uint4*>(static_cast<const T*>(g.a[0].p) +
-                                                        m * g.a[0].ld + u * 8);
+                                                        (M <= 2 ? m : min((int64_t)m, g.M - 1)) * g.a[0].ld + u * 8);
             float wf[kRows][8];
 #pragma unroll
             for (int r = 0; r < kRows; ++r) to_floats<T>(wv[r], wf[r]);
@@ -70,7 +69,7 @@ __global__ void __launch_bounds__(256) gemv_kernel(const __grid_constant__ GemmA
             }
         __syncthreads();
         const int m = threadIdx.x % M, c = threadIdx.x / M;
-        if (c < kOut && n0 + c < g.N) {
+        if (c < kOut && n0 + c < g.N && m < g.M) {
             float s[2] = {0.0f, 0.0f};
 #pragma unroll
             for (int k = 0; k < kWarps; ++k) {
@@ -109,8 +108,12 @@ template <class T>
 cudaError_t launch_rows(const OpContext& x, const GemmArgs& g, cudaStream_t st) {
     if (g.M == 1)
         launch<T, 1>(x, g, st);
-    else
+    else if (g.M == 2)
         launch<T, 2>(x, g, st);
+    else if (g.M <= 4)
+        launch<T, 4>(x, g, st);
+    else
+        launch<T, 8>(x, g, st);
     return cudaGetLastError();
 }
 
@@ -118,13 +121,17 @@ bool units16(const GemmOperand& o, int64_t rows) { return (uintptr_t)o.p % 16 ==
 
 }  // namespace
 
-// One or two rows: at 4096 x 4096 5.7 and 8.6 us against 12.9 on the tensor
-// cores; a third row costs as much as it saves (11.3 us for four, 36 against
-// 32 at 14336 columns).
-bool gemv_takes(const GemmArgs& g) {
+// One or two rows always: at 4096 x 4096 5.7 and 8.6 us against 12.9 on the
+// tensor cores.  Up to four or eight where the rows of weights are so few that
+// tiles of them leave most SMs idle, each with the whole contraction to itself:
+// four rows of 8192 by 64, 2048 and 4096 columns 4.7, 9.1 and 14.3 us against
+// 16.6, 16.8 and 16.9; eight 6.6, 14.5 and 24.1.  More weights than that cost
+// this kernel their multiply-adds: 14336 x 4096 with four rows 33 against 26.
+bool gemv_takes(const OpContext& x, const GemmArgs& g) {
     if (g.kind != kGemmLinear && g.kind != kGemmGated) return false;
-    return g.M <= kGemvRows && g.K > 0 && g.K % 8 == 0 && units16(g.a[0], g.M) && units16(g.b[0], g.N) &&
-           (g.kind == kGemmLinear || units16(g.b[1], g.N));
+    const int64_t weights = g.kind == kGemmGated ? 2 * g.N : g.N, rows = g.M <= 4 ? 4 : 8;
+    return (g.M <= 2 || (g.M <= 8 && weights * rows <= 108ll * x.num_sms)) && g.K > 0 && g.K % 8 == 0 &&
+           units16(g.a[0], g.M) && units16(g.b[0], g.N) && (g.kind == kGemmLinear || units16(g.b[1], g.N));
 }
 
 cudaError_t launch_gemv(const OpContext& x, const GemmArgs& g, cudaStream_t st) {

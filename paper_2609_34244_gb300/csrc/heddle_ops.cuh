@@ -132,10 +132,9 @@ size_t gemm_scratch(const OpContext& x, const GemmArgs& g);
 cudaError_t lay_out_operands(const OpContext& x, GemmArgs* const* list, int count, unsigned char* ws, cudaStream_t st);
 cudaError_t launch_gemm(const OpContext& x, const GemmArgs& g, unsigned char* ws, cudaStream_t st);
 
-// Forward products of up to kGemvRows rows in whole 16-byte units, without
-// the tensor cores (heddle_gemv.cu).
-constexpr int kGemvRows = 2;
-bool gemv_takes(const GemmArgs& g);
+// Forward products of few rows in whole 16-byte units, without the tensor
+// cores (heddle_gemv.cu).
+bool gemv_takes(const OpContext& x, const GemmArgs& g);
 cudaError_t launch_gemv(const OpContext& x, const GemmArgs& g, cudaStream_t st);
 
 // dz = dy act'(pre) (dz null: not written), partial column sums of it

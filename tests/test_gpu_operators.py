@@ -168,6 +168,14 @@ def test_gated_ffn(lib, m, n, k, dt):
             frame_kept(v, buf, "gated grads")
 
 
+@pytest.mark.parametrize("dt", ["bf16", "fp16"])
+@pytest.mark.parametrize("m,n,k", [(3, 64, 4104), (4, 1000, 264), (5, 70, 520), (8, 900, 2048), (8, 31, 8),
+                                   (6, 4000, 64), (9, 64, 1000)])
+def test_few_rows(lib, m, n, k, dt):
+    test_linear(lib, m, n, k, dt)
+    test_gated_ffn(lib, m, n, k, dt)
+
+
 def test_products_without_rows_or_steps(lib):
     h, ctx = lib
     dt = torch.bfloat16
