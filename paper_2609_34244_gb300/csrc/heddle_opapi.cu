@@ -216,7 +216,7 @@ heddle_status heddle_linear_backward(heddle_ctx* ctx, const heddle_linear_grad_a
     ag.m = a.m, ag.n = a.n, ag.dtype = a.dtype, ag.act = a.act;
     ag.dy = a.dy, ag.lddy = a.lddy, ag.pre = a.pre, ag.ldp = a.ldp;
     ag.dbias = a.n ? a.dbias : nullptr;
-    const bool own_dz = a.act != HEDDLE_ACT_NONE && (a.dx || a.dw);
+    const bool own_dz = a.act != HEDDLE_ACT_NONE && (a.dx || a.dw) && a.m && a.n;
     ag.lddz = hd::ceil_div(a.n, 64) * 64;  // rows of whole 128-byte lines for the products
     const size_t dz_bytes = own_dz ? hd::align256((size_t)a.m * ag.lddz * 2) : 0;
 
