@@ -158,7 +158,7 @@ cudaError_t act_grad(const OpContext& x, const ActGradArgs& a, unsigned char* ws
         else
             launch(x, act_grad_kernel<T, 1>, grid, 256, 0, st, a, partial, rows);
     }
-    if (partial)
+    if (a.dbias)  // without rows the sums are zero, and nothing is read
         launch(x, column_sum_kernel<T>, dim3((unsigned)ceil_div(a.n, 256)), 256, 0, st, partial, (int)chunks, a.n,
                static_cast<T*>(a.dbias));
     return cudaGetLastError();
