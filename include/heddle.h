@@ -723,7 +723,8 @@ heddle_status heddle_qk_norm_rope_backward(heddle_ctx* ctx, const heddle_qk_norm
  * [batch][q_heads][q_len], nullable).  A query that sees nothing, and rows
  * past a sequence's queries, get o = 0 and lse = -infinity.  Keys and values
  * past kv_lens are not used, whatever they hold; those within must be
- * finite.  P is rounded to the element type for its product with v, its sum
+ * finite.  A query with a score of NaN or +infinity gets NaN, scores of
+ * -infinity weigh nothing.  P is rounded to the element type for its product with v, its sum
  * is not.  One query against many keys is split along the keys.
  * dtype BF16 or FP16; 1 <= head_dim <= 256; kv_heads divides q_heads;
  * batch * q_heads * q_len and batch * kv_heads * kv_len below 2^31. */

@@ -55,14 +55,14 @@ __global__ void __launch_bounds__(kWarps * 32) attn_row_kernel(heddle_attention_
             load_row(at<T>(a.v, b, j, hk), D, lane, v);
             const float sc = dot_rows(q, k) * a.scale;
             const float top = fmaxf(m, sc);
-            const float keep = m == -INFINITY ? 0.0f : expf(m - top), w = expf(sc - top);
+            const float keep = m == -INFINITY ? 0.0f : expf(m - top), w = sc == -INFINITY ? 0.0f : expf(sc - top);
             l = l * keep + w;
 #pragma unroll
             for (int x = 0; x < kVals; ++x) o[x] = o[x] * keep + w * v[x];
             m = top;
         }
-        store_row(out_at<T>(a.o, b, i, h), D, lane, o, l > 0.0f ? 1.0f / l : 0.0f);
-        if (a.lse && lane == 0) a.lse[r] = l > 0.0f ? m + logf(l) : -INFINITY;
+        store_row(out_at<T>(a.o, b, i, h), D, lane, o, l == 0.0f ? 0.0f : 1.0f / l);
+        if (a.lse && lane == 0) a.lse[r] = l == 0.0f ? -INFINITY : m + logf(l);
     }
 }
 

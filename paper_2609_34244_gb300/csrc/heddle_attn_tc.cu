@@ -589,6 +589,8 @@ __global__ void __launch_bounds__(Forward<DP, NT>::kThreads, 1)
                     sum = sum * e0 + sum1 * e1;
                     f_other = e1, top = both;
                     f_mine = e0;
+                } else {  // zeros, or NaN from scores that are
+                    sum += sum1;
                 }
             }
             const bool inside = row < p.group * p.tokens && i < p.a.q_len;
@@ -644,9 +646,10 @@ __global__ void __launch_bounds__(256) attn_join_kernel(const __grid_constant__ 
     float top = mine;
 #pragma unroll
     for (int o = 16; o; o >>= 1) top = fmaxf(top, __shfl_xor_sync(~0u, top, o));
-    const float e = top == -INFINITY ? 0.0f : expf(mine - top);
+    // a part without weights has no logarithm; one of NaN makes the row NaN
+    const float e = mine == -INFINITY ? 0.0f : expf(mine - top);
     const float total = warp_sum(e);
-    const float w = total > 0.0f ? e / total : 0.0f;
+    const float w = e == 0.0f ? 0.0f : e / total;
     float acc[4] = {};
     for (int x = 0; x < p.splits; ++x) {
         const float f = __shfl_sync(~0u, w, x);
@@ -661,7 +664,7 @@ __global__ void __launch_bounds__(256) attn_join_kernel(const __grid_constant__ 
 #pragma unroll
     for (int j = 0; j < 4; ++j)
         if (lane + 32 * j < D) out[lane + 32 * j] = from_float<T>(acc[j]);
-    if (p.a.lse && lane == 0) p.a.lse[r] = total > 0.0f ? top + logf(total) : -INFINITY;
+    if (p.a.lse && lane == 0) p.a.lse[r] = total == 0.0f ? -INFINITY : top + logf(total);
 }
 
 // ------------------------------------------------------------------ backward

@@ -57,3 +57,50 @@ def test_gradients_over_no_rows(heddle_lib, name, scratch):
         assert (db == 0).all()
     finally:
         h.heddle_destroy(ctx)
+
+
+# Attention calls by the kernel that they run on this GPU: keys in parts, a
+# tile taken twice (alone and in parts), neither, one warp a row.
+FORMS = [
+    # batch, q_len, kv_len, q heads, kv heads, head_dim, window, sinks
+    (1, 1, 3000, 2, 1, 64, 0, 0), (2, 3, 2000, 4, 2, 128, 0, 0), (16, 1, 1100, 16, 8, 128, 0, 0),
+    (20, 60, 700, 8, 4, 64, 250, 0), (9, 1, 1300, 16, 8, 64, 0, 0), (2, 300, 300, 4, 2, 64, 100, 3),
+    (10, 128, 1024, 8, 8, 64, 128, 0),  # the last query sees keys of its tile's second half alone
+    (1, 5, 40, 2, 1, 160, 0, 0), (1, 9, 9, 1, 1, 33, 0, 0),
+]
+
+
+@pytest.mark.parametrize("dt", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("b,tq,tk,hq,hk,d,window,sinks", FORMS)
+def test_queries_that_are_not_finite(lib, b, tq, tk, hq, hk, d, window, sinks, dt):
+    """A NaN query gives NaN whichever kernels take it, and so does a score of
+    +infinity; scores of -infinity weigh nothing.  Zeros and a logarithm of
+    -infinity stay those of a query with no weights at all, and other queries
+    keep their values."""
+    h, ctx = lib
+    g = gen(b + tq + tk + d)
+    q, k, v = rand(g, b, tq, hq, d, dt=dt), rand(g, b, tk, hk, d, dt=dt), rand(g, b, tk, hk, d, dt=dt)
+    k[..., 0] = k[..., 0].abs() + 0.5  # the sign of an infinite score is that of the query's first value
+    rest = dict(window=window, sinks=sinks, scale=0.1)
+
+    def run(q):
+        o, lse = torch.full_like(q, CANARY), torch.full((b, hq, tq), CANARY, device="cuda")
+        h.heddle_attention(ctx, q, k, v, o, lse, **rest)
+        return o, lse
+
+    want, want_lse = run(q)
+    at = [(b - 1, tq - 1, hq - 1), (0, 0, 0)]
+    for value in (math.nan, math.inf, -math.inf):
+        p, other = q.clone(), torch.ones(b, tq, hq, dtype=torch.bool, device="cuda")
+        for i, t, j in at:
+            p[i, t, j] = math.nan if math.isnan(value) else 0.0
+            p[i, t, j, 0] = value
+            other[i, t, j] = False
+        o, lse = run(p)
+        for i, t, j in at:
+            if value == -math.inf:
+                assert (o[i, t, j] == 0).all() and lse[i, j, t] == -math.inf
+            else:
+                assert torch.isnan(o[i, t, j]).all() and (torch.isnan(lse[i, j, t]) or lse[i, j, t] == math.inf)
+        assert torch.equal(o[other], want[other])
+        assert torch.equal(lse.transpose(1, 2)[other], want_lse.transpose(1, 2)[other])
