@@ -745,13 +745,16 @@ struct GradBars {
 };
 constexpr int kGradBarBytes = 160;
 
-// dq of a query tile where dS is not kept: dq = scale sum over key tiles of
-// dS K with S = Q K^T, dP = dO V^T, dS = P (dP - delta).  Q and dO stay in
-// shared memory, K and V tiles come in two stages.  Scores of the next tile are
-// computed while this one's are turned into dS (two buffers).  CTAs take one
-// query tile after another, the longest first (a grid of one tile each: 137 us
-// against 119).  Bound by the chain from scores to dS as the forward is:
-// 114 us for two causal sequences of 2048 (32 heads over 8 of 128).
+// dq of a query tile where dS is not kept: dq = sum over key tiles of dS K with
+// S = Q K^T, dP = dO V^T, dS = scale P (dP - delta).  dS is rounded to the
+// element type with the scale in it, so that float16 has to hold what the
+// gradients of Q K^T are: under a loss scale P (dP - delta) passes 65504 before
+// they do.  Q and dO stay in shared memory, K and V tiles come in two stages.
+// Scores of the next tile are computed while this one's are turned into dS (two
+// buffers).  CTAs take one query tile after another, the longest first (a grid
+// of one tile each: 137 us against 119).  Bound by the chain from scores to dS
+// as the forward is: 114 us for two causal sequences of 2048 (32 heads over 8 of
+// 128).
 template <int DP>
 struct GradShape {
     static constexpr int kTileBytes = kTile * DP * 2;
@@ -868,7 +871,7 @@ __global__ void __launch_bounds__(kGradThreads, 1)
         const uint32_t lanes = (uint32_t)(warp % 4 * 32) << 16;
         const int i_row = row / p.group, h_row = row % p.group;
         const float c = p.scale_log2;
-        const uint64_t c2 = two(c, c);
+        const uint64_t c2 = two(c, c), scale2 = two(p.a.scale, p.a.scale);
         uint32_t step = 0, held = 0;
         bool go = true;
         for (int it = 0; go; ++it) {
@@ -883,7 +886,7 @@ __global__ void __launch_bounds__(kGradThreads, 1)
             const RowMask mask(i < s.ql ? s.off + i : -1, p.a);
             float lse = inside ? p.a.lse[r] : INFINITY;
             lse = lse == -INFINITY ? INFINITY : lse * kLog2e;  // weights of a row that sees nothing are zero
-            const float delta = inside ? p.delta[r] : 0.0f;
+            const float delta = inside ? p.delta[r] * p.a.scale : 0.0f;
             const uint64_t lse2 = two(-lse, -lse), delta2 = two(-delta, -delta);
             for (int j = 0; j < n; ++j, ++step) {
                 const uint32_t st = step & 1;
@@ -906,7 +909,7 @@ __global__ void __launch_bounds__(kGradThreads, 1)
                 if (whole) {
 #pragma unroll
                     for (int y = 0; y < 32; y += 2) {
-                        const float2 z = apart(mul_two(two(v[y], v[y + 1]), add_two(two(d[y], d[y + 1]), delta2)));
+                        const float2 z = apart(mul_two(two(v[y], v[y + 1]), fma_two(two(d[y], d[y + 1]), scale2, delta2)));
                         d[y] = __float_as_uint(z.x), d[y + 1] = __float_as_uint(z.y);
                     }
                 } else {
@@ -915,7 +918,7 @@ __global__ void __launch_bounds__(kGradThreads, 1)
 #pragma unroll
                     for (int y = 0; y < 32; ++y) {
                         const float e = seen >> y & 1 ? __uint_as_float(v[y]) : 0.0f;
-                        d[y] = __float_as_uint(e == 0.0f ? 0.0f : e * (__uint_as_float(d[y]) - delta));
+                        d[y] = __float_as_uint(e == 0.0f ? 0.0f : e * fmaf(__uint_as_float(d[y]), p.a.scale, -delta));
                     }
                 }
 #pragma unroll
@@ -940,7 +943,7 @@ __global__ void __launch_bounds__(kGradThreads, 1)
                 T* out = static_cast<T*>(p.dq.data) + w.b * p.dq.batch_stride + i * p.dq.token_stride +
                          h * p.dq.head_stride;
                 if (n > 0)
-                    store_row<T, DP>(at_dq + lanes, out, inside, p.a.head_dim, p.a.scale);
+                    store_row<T, DP>(at_dq + lanes, out, inside, p.a.head_dim, 1.0f);
                 else if (inside)
                     zero_row(out, p.a.head_dim);
             }
@@ -957,12 +960,13 @@ __global__ void __launch_bounds__(kGradThreads, 1)
     if (warp == 2) tmem_free(tmem, 512);
 }
 
-// dq from dS as the pass over keys left it: dq = scale sum over key tiles of
-// dS K, one product of 128 x 128 by 128 x head_dim a step.  Bound by the stream
-// of dS from memory, 32 KB a pair of tiles: 54 us for two causal sequences of
-// 2048 (32 heads over 8 of 128; 114 with the scores computed again).  CTAs take one query tile after
-// another, the longest first; sums alternate between two places of tensor
-// memory, so that one tile's result is written under the next one's products.
+// dq from dS as the pass over keys left it: dq = sum over key tiles of dS K,
+// one product of 128 x 128 by 128 x head_dim a step.  Bound by the stream of dS
+// from memory, 32 KB a pair of tiles: 54 us for two causal sequences of 2048
+// (32 heads over 8 of 128; 114 with the scores computed again).  CTAs take one
+// query tile after another, the longest first; sums alternate between two
+// places of tensor memory, so that one tile's result is written under the next
+// one's products.
 template <int DP>
 struct StoredShape {
     static constexpr int kTileBytes = kTile * DP * 2;
@@ -1098,7 +1102,7 @@ __global__ void __launch_bounds__(StoredShape<DP>::kThreads, 1)
             if (!__all_sync(~0u, mbar_wait(done + 8 * half, held / 2 & 1, gave_up))) break;
             ++held;
             fence_after();
-            store_row<T, DP>(tmem + half * DP + lanes, out, inside, p.a.head_dim, p.a.scale);
+            store_row<T, DP>(tmem + half * DP + lanes, out, inside, p.a.head_dim, 1.0f);
             fence_before();
             __syncwarp();
             if (lane == 0) mbar_arrive(freed + 8 * half);
@@ -1146,7 +1150,7 @@ __global__ void __launch_bounds__(kGradThreads, 1)
     volatile uint32_t* gave_up = reinterpret_cast<uint32_t*>(tail + kGradBarBytes);
     uint32_t* tmem_at = const_cast<uint32_t*>(gave_up) + 1;
     float* stat_lse = reinterpret_cast<float*>(tail + kGradBarBytes + 64);  // [3][128] minus lse, in powers of two
-    float* stat_delta = stat_lse + 3 * kTile;                               // [3][128] minus delta
+    float* stat_delta = stat_lse + 3 * kTile;                               // [3][128] minus scale delta
     uint32_t* stat_place = reinterpret_cast<uint32_t*>(stat_delta + 3 * kTile);  // [3] the query tile's places
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
 
@@ -1252,7 +1256,7 @@ __global__ void __launch_bounds__(kGradThreads, 1)
         const int side = (warp - 2) / 4, row = (warp % 4) * 32 + lane;  // which 32 of a tile's 128 queries
         const uint32_t lanes = (uint32_t)(warp % 4 * 32) << 16;
         const int key = k0 + row;
-        const uint64_t c2 = two(p.scale_log2, p.scale_log2);
+        const uint64_t c2 = two(p.scale_log2, p.scale_log2), scale2 = two(p.a.scale, p.a.scale);
 
         // where dS goes, less the query tile's part: all of it is below 2^32 bytes
         const uint32_t ds_at = !p.ds ? 0
@@ -1273,7 +1277,7 @@ __global__ void __launch_bounds__(kGradThreads, 1)
                 const float l = live ? p.a.lse[r_row + i] : INFINITY;
                 stat_lse[to] = l == -INFINITY ? -INFINITY : -l * kLog2e;
             } else if (side == 1) {
-                stat_delta[to] = live ? -p.delta[r_row + i] : 0.0f;
+                stat_delta[to] = live ? -p.delta[r_row + i] * p.a.scale : 0.0f;
             } else if (side == 2 && row == 0 && p.ds) {
                 stat_place[j % 3] = (uint32_t)ds_row(p, first + j) * kPlaceBytes;
             }
@@ -1346,9 +1350,10 @@ __global__ void __launch_bounds__(kGradThreads, 1)
 #pragma unroll
             for (int y = 0; y < 32; y += 4) {
                 const float4 f = deltas[y / 4];
-                const float2 z0 = apart(mul_two(two(v[y], v[y + 1]), add_two(two(d[y], d[y + 1]), two(f.x, f.y))));
+                const float2 z0 =
+                    apart(mul_two(two(v[y], v[y + 1]), fma_two(two(d[y], d[y + 1]), scale2, two(f.x, f.y))));
                 const float2 z1 =
-                    apart(mul_two(two(v[y + 2], v[y + 3]), add_two(two(d[y + 2], d[y + 3]), two(f.z, f.w))));
+                    apart(mul_two(two(v[y + 2], v[y + 3]), fma_two(two(d[y + 2], d[y + 3]), scale2, two(f.z, f.w))));
                 d[y] = __float_as_uint(z0.x), d[y + 1] = __float_as_uint(z0.y);
                 d[y + 2] = __float_as_uint(z1.x), d[y + 3] = __float_as_uint(z1.y);
             }
@@ -1379,18 +1384,17 @@ __global__ void __launch_bounds__(kGradThreads, 1)
             const bool is_dk = side & 1;
             const int d0 = side / 2 * (DP / 2), D = p.a.head_dim - d0;
             const uint32_t from = (is_dk ? at_dk : at_dv) + lanes + d0;
-            const float f = is_dk ? p.a.scale : 1.0f;
             const heddle_heads& t = is_dk ? p.dk : p.dv;
             T* out = static_cast<T*>(t.data) + b * t.batch_stride + key * t.token_stride + hk * t.head_stride + d0;
             const bool inside = key < p.a.kv_len;
             if (parts > 1) {
                 float* to = (is_dk ? p.part_dk : p.part_dv) + (slot * kTile + row) * p.a.head_dim + d0;
                 if (n > 0)
-                    store_floats<DP / 2>(from, to, true, D, f);
+                    store_floats<DP / 2>(from, to, true, D, 1.0f);
                 else
                     zero_row(to, min(D, DP / 2));
             } else if (n > 0) {
-                store_row<T, DP / 2>(from, out, inside, D, f);
+                store_row<T, DP / 2>(from, out, inside, D, 1.0f);
             } else if (inside) {
                 zero_row(out, min(D, DP / 2));
             }

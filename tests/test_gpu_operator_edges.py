@@ -104,3 +104,46 @@ def test_queries_that_are_not_finite(lib, b, tq, tk, hq, hk, d, window, sinks, d
                 assert torch.isnan(o[i, t, j]).all() and (torch.isnan(lse[i, j, t]) or lse[i, j, t] == math.inf)
         assert torch.equal(o[other], want[other])
         assert torch.equal(lse.transpose(1, 2)[other], want_lse.transpose(1, 2)[other])
+
+
+@pytest.mark.parametrize("b,t,hq,hk,d", [
+    (1, 24, 2, 1, 64), (1, 200, 4, 2, 128),  # the scores' gradients are kept between the passes
+    (80, 440, 128, 1, 64),                   # those of all heads do not fit, and are computed twice
+])
+def test_scores_gradients_near_the_end_of_float16(lib, b, t, hq, hk, d):
+    """Gradients whose P (dP - delta) passes 65504 while the scores' gradients,
+    which are `scale` of it, do not: as a loss scale brings about."""
+    h, ctx = lib
+    g, dt = gen(t), torch.float16
+    q, k = rand(g, b, t, hq, d, dt=dt, std=0.1), rand(g, b, t, hk, d, dt=dt, std=0.1)
+    v = rand(g, b, t, hk, d, dt=dt, std=4.0)
+    do = (torch.randn(b, t, hq, d, generator=g, device="cuda") * (8000 if t < 100 else 4000)).clamp(-30000, 30000)
+    do[:, 16:] *= 0.01  # the first queries' weights are large enough, and a key's sum stays in range
+    do[:, :, 2:] *= 0.01
+    do = do.to(dt)
+    lens = [torch.full((b,), t, dtype=torch.int32, device="cuda") for _ in range(2)]
+    o, lse = torch.empty_like(q), torch.empty(b, hq, t, device="cuda")
+    rest = dict(q_lens=lens[0], kv_lens=lens[1])
+    h.heddle_attention(ctx, q, k, v, o, lse, **rest)
+    dq, dk, dv = (torch.full_like(x, CANARY) for x in (q, k, v))
+    h.heddle_attention_backward(ctx, do, q, k, v, o, lse, dq, dk, dv, **rest)
+    scale, n, beyond = d ** -0.5, hq // hk, 0.0
+    for i in sorted({0, b - 1}):
+        for kv in range(hk):
+            sums = {x: [torch.zeros(t, d, dtype=torch.float64, device="cuda") for _ in range(2)] for x in ("dk", "dv")}
+            for j in range(kv * n, kv * n + n):
+                w = R.attention(q[i, :, j], k[i, :, kv], v[i, :, kv], t, t, 0, 0, scale, do[i, :, j])
+                R.close(dq[i, :, j], *w["dq"], "dq")
+                for x in sums:
+                    sums[x][0] += w[x][0]
+                    sums[x][1] += w[x][1] + n * 2.0 ** -23 * w[x][0].abs()
+                s = (q[i, :, j].double() @ k[i, :, kv].double().T * scale).masked_fill(
+                    ~R.visible(t, t, t, t, 0, 0, "cuda"), -math.inf)
+                p, dp = s.softmax(1), do[i, :, j].double() @ v[i, :, kv].double().T
+                ds = p * (dp - (p * dp).sum(1, keepdim=True))
+                beyond = max(beyond, ds.abs().max().item())
+                assert ds.abs().max().item() * scale < 60000
+            assert all(x[0].abs().max().item() < 60000 for x in sums.values())
+            R.close(dk[i, :, kv], *sums["dk"], "dk")
+            R.close(dv[i, :, kv], *sums["dv"], "dv")
+    assert beyond > 65504
