@@ -118,7 +118,9 @@ heddle_heads heads(const char* what, PyObject* o, at::IntArrayRef shape, const F
     return {t.data_ptr(), n == 4 ? s[0] : 0, s[n - 3], s[n - 2]};
 }
 
-int64_t same_stride(const char* what, const Mat& a, const Mat& b) {
+// The stride of two tensors of so many rows; a single row's means nothing.
+int64_t same_stride(const char* what, const Mat& a, const Mat& b, int64_t rows) {
+    if (rows <= 1) return a.ld < b.ld ? b.ld : a.ld;
     if (a.ld != b.ld) throw Refused(std::string(what) + " have different row strides");
     return a.ld;
 }
@@ -256,7 +258,7 @@ PyObject* gated_ffn(PyObject*, PyObject* const* v, Py_ssize_t count) {
         a.m = x[0], a.n = axes_of("w_gate", v[2], 2)[0], a.k = x[1];
         a.dtype = x.code, a.act = integer32(v[5]);
         const Mat gate("gate", v[6], a.m, a.n, at::kFloat, x.device), up("up", v[7], a.m, a.n, at::kFloat, x.device);
-        a.lds = same_stride("gate and up", gate, up);
+        a.lds = same_stride("gate and up", gate, up, a.m);
         a.gate = static_cast<float*>(gate.p), a.up = static_cast<float*>(up.p);
         const Mat mx("x", v[1], a.m, a.k, x.type, x.device), wg("w_gate", v[2], a.n, a.k, x.type, x.device),
             wu("w_up", v[3], a.n, a.k, x.type, x.device), y("y", v[4], a.m, a.n, x.type, x.device);
@@ -274,10 +276,10 @@ PyObject* gated_ffn_backward(PyObject*, PyObject* const* v, Py_ssize_t count) {
         a.m = x[0], a.n = axes_of("w_gate", v[3], 2)[0], a.k = x[1];
         a.dtype = x.code, a.act = integer32(v[7]);
         const Mat gate("gate", v[5], a.m, a.n, at::kFloat, x.device), up("up", v[6], a.m, a.n, at::kFloat, x.device);
-        a.lds = same_stride("gate and up", gate, up);
+        a.lds = same_stride("gate and up", gate, up, a.m);
         a.gate = static_cast<float*>(gate.p), a.up = static_cast<float*>(up.p);
         const Mat dwg("dwg", v[9], a.n, a.k, x.type, x.device), dwu("dwu", v[10], a.n, a.k, x.type, x.device);
-        a.lddw = same_stride("dwg and dwu", dwg, dwu);
+        a.lddw = same_stride("dwg and dwu", dwg, dwu, a.n);
         a.dw_gate = dwg.p, a.dw_up = dwu.p;
         const Mat dy("dy", v[1], a.m, a.n, x.type, x.device), mx("x", v[2], a.m, a.k, x.type, x.device),
             wg("w_gate", v[3], a.n, a.k, x.type, x.device), wu("w_up", v[4], a.n, a.k, x.type, x.device),

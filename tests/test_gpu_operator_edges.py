@@ -147,3 +147,33 @@ def test_scores_gradients_near_the_end_of_float16(lib, b, t, hq, hk, d):
             R.close(dk[i, :, kv], *sums["dk"], "dk")
             R.close(dv[i, :, kv], *sums["dv"], "dv")
     assert beyond > 65504
+
+
+def test_single_rows_at_any_stride(lib):
+    """The stride of a single row means nothing, so two of them need not share it."""
+    h, ctx = lib
+    g, dt = gen(3), torch.bfloat16
+    x, wg, wu = rand(g, 1, 40, dt=dt), rand(g, 24, 40, dt=dt), rand(g, 24, 40, dt=dt)
+    y, want = (torch.empty(1, 24, dtype=dt, device="cuda") for _ in range(2))
+    gates = [torch.empty(1, 24, device="cuda") for _ in range(2)]
+    h.heddle_gated_ffn(ctx, x, wg, wu, want, gate=gates[0], up=gates[1])
+    wide = torch.full((2, 100), CANARY, device="cuda")
+    up = wide[:1, 8:32]
+    gate = torch.empty(1, 24, device="cuda")
+    h.heddle_gated_ffn(ctx, x, wg, wu, y, gate=gate, up=up)
+    assert torch.equal(y, want) and torch.equal(gate, gates[0]) and torch.equal(up, gates[1])
+    assert (wide[1] == CANARY).all() and (wide[0, :8] == CANARY).all() and (wide[0, 32:] == CANARY).all()
+    dy = rand(g, 1, 24, dt=dt)
+    first = [torch.empty_like(t) for t in (x, wg, wu)]
+    h.heddle_gated_ffn_backward(ctx, dy, x, wg, wu, gates[0], gates[1], dx=first[0], dwg=first[1], dwu=first[2])
+    again = [torch.empty_like(t) for t in (x, wg, wu)]
+    h.heddle_gated_ffn_backward(ctx, dy, x, wg, wu, gate, up, dx=again[0], dwg=again[1], dwu=again[2])
+    assert all(torch.equal(a, b) for a, b in zip(first, again))
+    # one output: its two weights' gradients
+    dwg, dwu = torch.empty(1, 40, dtype=dt, device="cuda"), torch.empty(3, 72, dtype=dt, device="cuda")[1:2, :40]
+    h.heddle_gated_ffn_backward(ctx, dy[:, :1], x, wg[:1], wu[:1], gate[:, :1], up[:, :1], dwg=dwg, dwu=dwu)
+    assert torch.equal(dwg, first[1][:1]) and torch.equal(dwu, first[2][:1])
+    refused(h, h.E_ARG, h.heddle_gated_ffn, ctx, x, wg, wu, y, gate=gate)
+    two = torch.empty(2, 24, device="cuda")
+    refused(h, h.E_ARG, h.heddle_gated_ffn, ctx, x.expand(2, 40).clone(), wg, wu, y.expand(2, 24).clone(), gate=two,
+            up=wide[:, 8:32])
