@@ -76,6 +76,10 @@ void heddle_destroy(heddle_ctx* ctx);
  * The buffer belongs to ctx and is overwritten by the next call. */
 const char* heddle_last_error(const heddle_ctx* ctx);
 
+/* The device that ctx was created for: all buffers of its calls lie there.
+ * -1 for NULL. */
+int32_t heddle_device(const heddle_ctx* ctx);
+
 /* ------------------------------------------------------------- cluster */
 
 /* One GPU type (§5.1 "normalized hardware attributes"): peak dense TFLOPS,

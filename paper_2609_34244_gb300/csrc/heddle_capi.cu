@@ -576,6 +576,8 @@ void heddle_destroy(heddle_ctx* x) {
 
 const char* heddle_last_error(const heddle_ctx* x) { return x ? x->msg : "null context"; }
 
+int32_t heddle_device(const heddle_ctx* x) { return x ? x->device : -1; }
+
 heddle_status heddle_load_cluster(heddle_ctx* x, const heddle_gpu_type* types, int32_t n_types,
                                   const heddle_node* nodes, int32_t n_nodes) {
     if (!x) return HEDDLE_E_ARG;

@@ -33,6 +33,7 @@ const char* const kNames[kEntries] = {"heddle_linear",       "heddle_linear_back
                                       "heddle_qk_norm_rope", "heddle_qk_norm_rope_backward",
                                       "heddle_attention",    "heddle_attention_backward"};
 void* functions[kEntries];
+int32_t (*device_of)(const heddle_ctx*) = nullptr;
 
 std::string text(at::IntArrayRef s) {
     std::string r = "(";
@@ -173,6 +174,9 @@ template <class Args>
 PyObject* call(Entry entry, PyObject* ctx, const Args& a, int device, PyObject* stream) {
     if (!functions[entry]) throw Refused("the library's functions are not bound");
     heddle_ctx* c = static_cast<heddle_ctx*>(address(ctx, name_value));
+    if (c && device_of(c) != device)  // kernels would run there on this device's addresses
+        throw Refused("the context is of cuda:" + std::to_string(device_of(c)) + ", the tensors are on cuda:" +
+                      std::to_string(device));
     void* st;
     if (stream == Py_None) {
         PyObject* index = PyLong_FromLong(device);
@@ -389,15 +393,16 @@ PyObject* attention_backward(PyObject*, PyObject* const* v, Py_ssize_t count) {
 // (the functions' addresses by name, HeddleError, device index -> current stream)
 PyObject* bind(PyObject*, PyObject* const* v, Py_ssize_t count) {
     return guarded<3>(count, [&] {
-        void* found[kEntries];
-        for (int i = 0; i < kEntries; ++i) {
-            PyObject* p = PyMapping_GetItemString(v[0], kNames[i]);
+        void* found[kEntries + 1];
+        for (int i = 0; i <= kEntries; ++i) {
+            PyObject* p = PyMapping_GetItemString(v[0], i < kEntries ? kNames[i] : "heddle_device");
             if (!p) throw PythonError();
             found[i] = PyLong_AsVoidPtr(p);
             Py_DECREF(p);
             if (PyErr_Occurred()) throw PythonError();
         }
         for (int i = 0; i < kEntries; ++i) functions[i] = found[i];
+        device_of = reinterpret_cast<int32_t (*)(const heddle_ctx*)>(found[kEntries]);
         Py_INCREF(v[1]), Py_INCREF(v[2]);
         Py_XSETREF(error_class, v[1]);
         Py_XSETREF(current_stream, v[2]);

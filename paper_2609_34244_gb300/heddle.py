@@ -137,7 +137,7 @@ class heddle_attention_grad_args(C.Structure):
                 ("dv", heddle_heads)]
 
 
-EXPORTS = ["heddle_create", "heddle_destroy", "heddle_last_error", "heddle_load_cluster",
+EXPORTS = ["heddle_create", "heddle_destroy", "heddle_last_error", "heddle_device", "heddle_load_cluster",
            "heddle_load_model", "heddle_price_candidates", "heddle_topk_reset", "heddle_topk",
            "heddle_price_topk_host", "heddle_get_tables", "heddle_device_errors",
            "heddle_count_next", "heddle_work_counters", "heddle_set_search", "heddle_get_search",
@@ -168,6 +168,7 @@ def load_library(path: str = LIB_PATH):
         "heddle_create": (i32, [C.POINTER(C.c_void_p), i32]),
         "heddle_destroy": (None, [p]),
         "heddle_last_error": (C.c_char_p, [p]),
+        "heddle_device": (i32, [p]),
         "heddle_load_cluster": (i32, [p, p, i32, p, i32]),
         "heddle_load_model": (i32, [p, p, i32, i64, i32, p]),
         "heddle_price_candidates": (i32, [p, p, p, p]),
@@ -250,6 +251,10 @@ def heddle_destroy(ctx):
 
 def heddle_last_error(ctx) -> str:
     return (load_library().heddle_last_error(ctx) or b"").decode()
+
+
+def heddle_device(ctx) -> int:
+    return int(load_library().heddle_device(ctx))
 
 
 def heddle_load_cluster(ctx, cluster: dict):
@@ -481,10 +486,11 @@ def heddle_get_search(ctx) -> int:
 # ------------------------------------------------------- layer operators
 #
 # Tensors are torch CUDA tensors of one element type (named outputs and saved
-# values float32), their last axis contiguous; every output is given by the
-# caller.  The marshalling is compiled (csrc/heddle_ops_py.cpp): it checks
-# shapes and types, since the C structs carry only one set of sizes;
-# everything else is checked by the library.
+# values float32) on the context's device, their last axis contiguous; every
+# output is given by the caller.  The marshalling is compiled
+# (csrc/heddle_ops_py.cpp): it checks shapes, types and the device, since the C
+# structs carry only one set of sizes; everything else is checked by the
+# library.
 
 _ops = None
 _OP_NAMES = ("heddle_linear", "heddle_linear_backward", "heddle_gated_ffn", "heddle_gated_ffn_backward",
@@ -502,7 +508,8 @@ def _op_setup():
     L = load_library()
     stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or \
         (lambda device: torch.cuda.current_stream(device).cuda_stream)
-    _heddle_ops.bind({n: C.cast(getattr(L, n), C.c_void_p).value for n in _OP_NAMES}, HeddleError, stream)
+    _heddle_ops.bind({n: C.cast(getattr(L, n), C.c_void_p).value for n in _OP_NAMES + ("heddle_device",)},
+                     HeddleError, stream)
     _ops = _heddle_ops
     return _ops
 

@@ -177,3 +177,49 @@ def test_single_rows_at_any_stride(lib):
     two = torch.empty(2, 24, device="cuda")
     refused(h, h.E_ARG, h.heddle_gated_ffn, ctx, x.expand(2, 40).clone(), wg, wu, y.expand(2, 24).clone(), gate=two,
             up=wide[:, 8:32])
+
+
+def test_tensors_of_another_device_are_refused(lib):
+    """The context's device as a stand-in reports it is not the tensors': no
+    operator's function may be entered."""
+    import ctypes
+    h, ctx = lib
+    native = h._op_setup()
+    entered = []
+
+    @ctypes.CFUNCTYPE(ctypes.c_int32, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p)
+    def operator(c, a, s):
+        entered.append(c)
+        return 0
+
+    @ctypes.CFUNCTYPE(ctypes.c_int32, ctypes.c_void_p)
+    def device(c):
+        return where
+
+    address = lambda f: ctypes.cast(f, ctypes.c_void_p).value
+    names = dict.fromkeys(h._OP_NAMES, address(operator))
+    names["heddle_device"] = address(device)
+    dt = dict(dtype=torch.bfloat16, device="cuda")
+    x, p = torch.zeros(4, 8, **dt), torch.zeros(4, 4, device="cuda")
+    q3, q4, f8, lse = x.view(1, 2, 16), x.view(1, 1, 2, 16), torch.zeros(16, device="cuda"), torch.zeros(1, 2, 1, device="cuda")
+    w16 = torch.zeros(16, **dt)
+    calls = [(h.heddle_linear, (x, x, x[:, :4])), (h.heddle_linear_backward, (x[:, :4], x, x)),
+             (h.heddle_gated_ffn, (x, x, x, x[:, :4])), (h.heddle_gated_ffn_backward, (x[:, :4], x, x, x, p, p)),
+             (h.heddle_qk_norm_rope, (q3, q3, w16, w16, q3, q3)),
+             (h.heddle_qk_norm_rope_backward, (q3, q3, q3, q3, w16, w16, q3, q3, f8, f8)),
+             (h.heddle_attention, (q4, q4, q4, q4)),
+             (h.heddle_attention_backward, (q4, q4, q4, q4, q4, lse, q4, q4, q4))]
+    assert len(calls) == len(h._OP_NAMES)
+    try:
+        native.bind(names, h.HeddleError, lambda index: 0)
+        for where in (0, 1):
+            for f, args in calls:
+                entered.clear()
+                if where == torch.cuda.current_device():
+                    f(ctx, *args)
+                    assert len(entered) == 1
+                else:
+                    refused(h, h.E_ARG, f, ctx, *args)
+                    assert not entered
+    finally:
+        h._op_setup()
