@@ -555,9 +555,11 @@ heddle_status heddle_phase_times(heddle_ctx* ctx, double ms[HEDDLE_N_PHASES],
  * row stride is no multiple of 16 bytes.  An output must not overlap an
  * input unless named.  All calls are asynchronous on `stream`, results do not
  * depend on the launch configuration of other calls and repeat bit for bit.
- * Scratch belongs to the context and grows on first use of a larger size
- * (E_NOMEM if that fails): before a stream capture, make the call once.
- * Calls on one context must not overlap on the GPU.
+ * Scratch belongs to the context, grows on first use of a larger size (E_NOMEM
+ * if that fails) and is held until the context is destroyed; what a captured
+ * call was given is held beside the larger blocks that follow it, so that its
+ * graph can be replayed as long as the context lives.  Calls on one context,
+ * and replays of graphs of them, must not overlap on the GPU.
  * Errors of all: E_ARG (a null pointer, a negative size, a bad stride, type
  * or activation), E_LIMIT (a size beyond the limits named), E_CUDA, E_NOMEM;
  * nothing is launched then.  A call whose outputs are empty is a no-op; a

@@ -560,7 +560,7 @@ void heddle_destroy(heddle_ctx* x) {
         cudaFree(x->lv_status[i]);
         cudaFree(x->lv_bounds[i]);
     }
-    cudaFree(x->op.ws);
+    x->op.scratch.release_all();
     cudaFree(x->op.sched);
     cudaFree(x->d_timg);
     cudaFree(x->d_node_type);

@@ -34,20 +34,19 @@ struct OpDeviceGuard {
     }
 };
 
-// At least `need` bytes of scratch.  Freeing the old one waits for the work
-// that may still use it.
-heddle_status reserve(OpContext* x, size_t need) {
-    if (x->ws_cap >= need) return HEDDLE_OK;
-    cudaFree(x->ws);
-    x->ws = nullptr;
-    x->ws_cap = 0;
-    if (cudaMalloc((void**)&x->ws, need) != cudaSuccess) {
-        x->ws = nullptr;
-        cudaGetLastError();
-        return fail(x, HEDDLE_E_NOMEM, "%zu bytes of operator scratch", need);
-    }
-    x->ws_cap = need;
-    return HEDDLE_OK;
+// Whether a graph is being captured of the stream, or of one that it may not
+// run beside.
+bool capturing(cudaStream_t st) {
+    cudaStreamCaptureStatus status;
+    if (cudaStreamIsCapturing(st, &status) == cudaSuccess) return status != cudaStreamCaptureStatusNone;
+    cudaGetLastError();
+    return true;
+}
+
+// At least `need` bytes of scratch.
+heddle_status reserve(OpContext* x, size_t need, cudaStream_t st) {
+    if (need == 0 || x->scratch.reserve(need, capturing(st))) return HEDDLE_OK;
+    return fail(x, HEDDLE_E_NOMEM, "%zu bytes of operator scratch", need);
 }
 
 heddle_status done(OpContext* x, cudaError_t e, const char* what) {
@@ -188,8 +187,8 @@ heddle_status heddle_linear(heddle_ctx* ctx, const heddle_linear_args* args, voi
     g.bias = a.bias;
     g.residual = a.residual, g.ldr = a.ldr;
     g.pre[0] = a.pre, g.ldp = a.ldp;
-    CHECK(reserve(x, hd::gemm_scratch(*x, g)));
-    return done(x, hd::launch_gemm(*x, g, x->ws, (cudaStream_t)stream), "heddle_linear");
+    CHECK(reserve(x, hd::gemm_scratch(*x, g), (cudaStream_t)stream));
+    return done(x, hd::launch_gemm(*x, g, x->scratch.get(), (cudaStream_t)stream), "heddle_linear");
 }
 
 heddle_status heddle_linear_backward(heddle_ctx* ctx, const heddle_linear_grad_args* args, void* stream) {
@@ -235,10 +234,10 @@ heddle_status heddle_linear_backward(heddle_ctx* ctx, const heddle_linear_grad_a
     // places of their own: operands are laid out while the activation's gradient is at work
     const size_t need = (want_x ? hd::gemm_scratch(*x, gx) : 0) + (want_w ? hd::gemm_scratch(*x, gw) : 0);
     const size_t sums_bytes = hd::act_grad_scratch(*x, ag);
-    CHECK(reserve(x, dz_bytes + sums_bytes + need));
-    unsigned char *sums = x->ws + dz_bytes, *rest = sums + sums_bytes;
+    CHECK(reserve(x, dz_bytes + sums_bytes + need, st));
+    unsigned char *ws = x->scratch.get(), *sums = ws + dz_bytes, *rest = sums + sums_bytes;
     if (own_dz) {
-        ag.dz = x->ws;
+        ag.dz = ws;
         gx.a[0] = gw.a[0] = {ag.dz, ag.lddz};
     }
     cudaError_t e = cudaSuccess;
@@ -278,8 +277,8 @@ heddle_status heddle_gated_ffn(heddle_ctx* ctx, const heddle_gated_ffn_args* arg
     g.b[1] = {a.w_up, a.ldu};
     g.out[0] = a.y, g.ldo = a.ldy;
     g.pre[0] = a.gate, g.pre[1] = a.up, g.ldp = a.lds;
-    CHECK(reserve(x, hd::gemm_scratch(*x, g)));
-    return done(x, hd::launch_gemm(*x, g, x->ws, (cudaStream_t)stream), "heddle_gated_ffn");
+    CHECK(reserve(x, hd::gemm_scratch(*x, g), (cudaStream_t)stream));
+    return done(x, hd::launch_gemm(*x, g, x->scratch.get(), (cudaStream_t)stream), "heddle_gated_ffn");
 }
 
 heddle_status heddle_gated_ffn_backward(heddle_ctx* ctx, const heddle_gated_ffn_grad_args* args, void* stream) {
@@ -322,15 +321,15 @@ heddle_status heddle_gated_ffn_backward(heddle_ctx* ctx, const heddle_gated_ffn_
     // dg and du in the scratch: their stride counts, whatever the base will be
     gx.a[0] = gx.a[1] = gw.a[0] = gw.a[1] = {nullptr, ld};
     const size_t need = (want_x ? hd::gemm_scratch(*x, gx) : 0) + (want_w ? hd::gemm_scratch(*x, gw) : 0);
-    CHECK(reserve(x, 2 * half + need));
-    unsigned char* rest = x->ws + 2 * half;
-    gx.a[0] = gw.a[0] = {x->ws, ld};
-    gx.a[1] = gw.a[1] = {x->ws + half, ld};
+    CHECK(reserve(x, 2 * half + need, st));
+    unsigned char *ws = x->scratch.get(), *rest = ws + 2 * half;
+    gx.a[0] = gw.a[0] = {ws, ld};
+    gx.a[1] = gw.a[1] = {ws + half, ld};
 
     hd::GateGradArgs gg{};
     gg.m = a.m, gg.n = a.n, gg.dtype = a.dtype, gg.act = a.act;
     gg.dy = a.dy, gg.lddy = a.lddy, gg.gate = a.gate, gg.up = a.up, gg.lds = a.lds;
-    gg.dg = x->ws, gg.du = x->ws + half, gg.ldo = ld;
+    gg.dg = ws, gg.du = ws + half, gg.ldo = ld;
     cudaError_t e = a.m && a.n ? hd::launch_gate_grad(*x, gg, st) : cudaSuccess;
     hd::GemmArgs* both[2];
     int count = 0;
@@ -364,8 +363,8 @@ heddle_status heddle_qk_norm_rope_backward(heddle_ctx* ctx, const heddle_qk_norm
     REQUIRE(args->dwq && args->dwk, HEDDLE_E_ARG, "dwq or dwk is null");
     REQUIRE(aligned_to(args->dwq, 4) && aligned_to(args->dwk, 4), HEDDLE_E_ARG, "dwq or dwk is not aligned");
     OpDeviceGuard guard(x);
-    CHECK(reserve(x, hd::qk_norm_rope_grad_scratch(*x, *args)));
-    return done(x, hd::launch_qk_norm_rope_grad(*x, *args, x->ws, (cudaStream_t)stream),
+    CHECK(reserve(x, hd::qk_norm_rope_grad_scratch(*x, *args), (cudaStream_t)stream));
+    return done(x, hd::launch_qk_norm_rope_grad(*x, *args, x->scratch.get(), (cudaStream_t)stream),
                 "heddle_qk_norm_rope_backward");
 }
 
@@ -376,8 +375,8 @@ heddle_status heddle_attention(heddle_ctx* ctx, const heddle_attention_args* arg
     CHECK(check_attention(x, *args, true));
     if (args->batch == 0 || args->q_len == 0) return done(x, cudaSuccess, "");
     OpDeviceGuard guard(x);
-    CHECK(reserve(x, hd::attention_scratch(*x, *args)));
-    return done(x, hd::launch_attention(*x, *args, x->ws, (cudaStream_t)stream), "heddle_attention");
+    CHECK(reserve(x, hd::attention_scratch(*x, *args), (cudaStream_t)stream));
+    return done(x, hd::launch_attention(*x, *args, x->scratch.get(), (cudaStream_t)stream), "heddle_attention");
 }
 
 heddle_status heddle_attention_backward(heddle_ctx* ctx, const heddle_attention_grad_args* args, void* stream) {
@@ -396,12 +395,13 @@ heddle_status heddle_attention_backward(heddle_ctx* ctx, const heddle_attention_
     // room to keep the scores' gradients, or without them where that is refused
     const size_t most = hd::attention_grad_scratch(*x, *args, true);
     const size_t least = hd::attention_grad_scratch(*x, *args, false);
-    const bool keep = !(x->ws_refused && most >= x->ws_refused) && reserve(x, most) == HEDDLE_OK;
+    const bool keep = !(x->ws_refused && most >= x->ws_refused) &&
+                      (most == 0 || x->scratch.reserve(most, capturing((cudaStream_t)stream), most > least));
     if (!keep) {
         if (!x->ws_refused || most < x->ws_refused) x->ws_refused = most;
-        CHECK(reserve(x, least));
+        CHECK(reserve(x, least, (cudaStream_t)stream));
     }
-    return done(x, hd::launch_attention_grad(*x, *args, x->ws, keep, (cudaStream_t)stream),
+    return done(x, hd::launch_attention_grad(*x, *args, x->scratch.get(), keep, (cudaStream_t)stream),
                 "heddle_attention_backward");
 }
 

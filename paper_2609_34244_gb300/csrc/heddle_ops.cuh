@@ -13,6 +13,7 @@
 
 #include "heddle.h"
 #include "heddle_launch.cuh"
+#include "heddle_scratch.cuh"
 
 namespace hd {
 
@@ -20,14 +21,28 @@ namespace hd {
 constexpr uint32_t kErrOpWait = 16u;      // a wait inside an operator ran out
 constexpr uint32_t kErrOpPosition = 32u;  // a position outside its rotation table
 
+struct DeviceMemory {
+    static void* allocate(size_t size) {
+        // allowed during a capture, and no part of the graph
+        cudaStreamCaptureMode mode = cudaStreamCaptureModeRelaxed;
+        cudaThreadExchangeStreamCaptureMode(&mode);
+        void* p = nullptr;
+        const cudaError_t e = cudaMalloc(&p, size);
+        cudaThreadExchangeStreamCaptureMode(&mode);
+        if (e == cudaSuccess) return p;
+        cudaGetLastError();
+        return nullptr;
+    }
+    static void release(void* p) { cudaFree(p); }
+};
+
 // What an operator call uses of its context.
 struct OpContext {
     int device = 0;
     int num_sms = 0;
     uint32_t* err = nullptr;  // device error flags
     int32_t* sched = nullptr;  // two counters of kernels that hand out work, zero between launches
-    unsigned char* ws = nullptr;
-    size_t ws_cap = 0;
+    Scratch<DeviceMemory> scratch;
     size_t ws_refused = 0;  // the least scratch that the device had no room for, where a call can do without
     char* msg = nullptr;
     size_t msg_size = 0;

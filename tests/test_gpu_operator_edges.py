@@ -223,3 +223,56 @@ def test_tensors_of_another_device_are_refused(lib):
                     assert not entered
     finally:
         h._op_setup()
+
+
+def _step(h, ctx, g, t):
+    """A linear at odd rows and an attention, with their gradients: tensors, and
+    the calls on them."""
+    dt = torch.bfloat16
+    x, w = rand(g, t, 137, dt=dt), rand(g, 71, 137, dt=dt, std=0.1)
+    dy, pre = rand(g, t, 71, dt=dt), torch.empty(t, 71, device="cuda")
+    q, k = rand(g, 1, t, 4, 64, dt=dt), rand(g, 1, t, 2, 64, dt=dt)
+    y, dx, dw, o, dq, dk, dv = (torch.empty_like(v) for v in (dy, x, w, q, q, k, k))
+    db, lse = torch.empty(71, dtype=dt, device="cuda"), torch.empty(1, 4, t, device="cuda")
+
+    def calls():
+        h.heddle_linear(ctx, x, w, y, act=h.ACT_SILU, pre=pre)
+        h.heddle_linear_backward(ctx, dy, x, w, act=h.ACT_SILU, pre=pre, dx=dx, dw=dw, dbias=db)
+        h.heddle_attention(ctx, q, k, k, o, lse)
+        h.heddle_attention_backward(ctx, q, q, k, k, o, lse, dq, dk, dv)
+
+    return (x, dy, q), (y, dx, dw, db, o, lse, dq, dk, dv), calls
+
+
+@pytest.mark.parametrize("warm", [True, False])
+def test_graphs_outlive_larger_calls(heddle_lib, warm):
+    """A captured call's scratch stays, whatever later calls need, and a
+    capture may be the first to need it."""
+    h = heddle_lib
+    ctx = h.heddle_create(0)
+    try:
+        inputs, outputs, calls = _step(h, ctx, gen(71), 150)
+        if warm:
+            calls()
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            calls()
+        _, _, larger = _step(h, ctx, gen(72), 3000)
+        larger()
+        larger()
+        others = [torch.full((1 << 22,), CANARY, device="cuda") for _ in range(64)]  # what was given back is taken again
+        for v in inputs:
+            v.mul_(0.5)
+        for v in outputs:
+            v.fill_(CANARY)
+        graph.replay()
+        got = [v.clone() for v in outputs]
+        assert all((v == CANARY).all() for v in others)
+        calls()
+        assert all(torch.equal(a, b) for a, b in zip(got, outputs))
+        del graph
+        torch.cuda.synchronize()
+        assert h.heddle_device_errors(ctx) == 0
+    finally:
+        h.heddle_destroy(ctx)

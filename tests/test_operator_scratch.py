@@ -1,0 +1,114 @@
+"""The layer operators' scratch (csrc/heddle_scratch.cuh) with memory of its
+own that records what is released and when (no GPU): a block whose address a
+captured graph holds outlives every growth."""
+
+import os
+import subprocess
+
+import pytest
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+CSRC = os.path.join(ROOT, "paper_2609_34244_gb300", "csrc")
+
+HEAD = r'''
+#include <cstdio>
+#include <cstdlib>
+#include <set>
+#include "heddle_scratch.cuh"
+
+#define CHECK(c) do { if (!(c)) { std::printf("line %d: %s\n", __LINE__, #c); return 1; } } while (0)
+
+static size_t room = 0;  // bytes left
+static std::set<void*> live;
+static bool in_capture = false, released_in_capture = false;
+struct Memory {  // the size is held ahead of the block
+    static void* allocate(size_t n) {
+        if (n > room) return nullptr;
+        size_t* p = static_cast<size_t*>(std::malloc(16 + n));
+        p[0] = n;
+        room -= n;
+        live.insert(p + 2);
+        return p + 2;
+    }
+    static void release(void* v) {
+        if (in_capture) released_in_capture = true;
+        if (!live.erase(v)) { std::printf("released twice\n"); std::exit(2); }
+        size_t* p = static_cast<size_t*>(v) - 2;
+        room += p[0];
+        std::free(p);
+    }
+};
+static bool take(hd::Scratch<Memory>& s, size_t n, bool captured, bool or_keep = false) {
+    in_capture = captured;
+    const bool ok = s.reserve(n, captured, or_keep);
+    in_capture = false;
+    return ok;
+}
+int main() {
+    hd::Scratch<Memory> s;
+'''
+
+CASES = {
+    "grows and gives back what no graph holds": r'''
+    room = 1000;
+    CHECK(take(s, 100, false));
+    void* a = s.get();
+    CHECK(take(s, 60, false) && s.get() == a && s.size() == 100);
+    CHECK(take(s, 300, false) && s.size() == 300 && live.size() == 1 && room == 700);
+''',
+    "keeps what a graph holds": r'''
+    room = 1000;
+    CHECK(take(s, 100, true));
+    void* a = s.get();
+    CHECK(take(s, 200, false) && s.get() != a && live.count(a));
+    CHECK(take(s, 400, false) && live.count(a) && live.size() == 2 && room == 500);
+''',
+    "keeps what a graph holds that grew before": r'''
+    room = 1000;
+    CHECK(take(s, 100, false));
+    CHECK(take(s, 50, true));  // captured in the block that was there
+    void* a = s.get();
+    CHECK(take(s, 200, true));
+    void* b = s.get();
+    CHECK(take(s, 300, false) && live.count(a) && live.count(b) && live.size() == 3);
+''',
+    "releases nothing during a capture, and later what no graph holds": r'''
+    room = 1000;
+    CHECK(take(s, 100, false));
+    CHECK(take(s, 200, true) && live.size() == 2 && !released_in_capture);
+    void* b = s.get();
+    CHECK(take(s, 300, false) && live.count(b) && live.size() == 2);
+''',
+    "without room the old block is given up for the new one, unless it is kept": r'''
+    room = 1000;
+    CHECK(take(s, 600, false));
+    void* a = s.get();
+    CHECK(!take(s, 900, false, true) && s.get() == a && s.size() == 600);
+    CHECK(take(s, 900, false) && s.size() == 900 && live.size() == 1);
+    CHECK(!take(s, 2000, false) && !s.get() && s.size() == 0 && live.empty());
+    CHECK(take(s, 10, false) && s.size() == 10);
+''',
+    "without room a captured block stays": r'''
+    room = 1000;
+    CHECK(take(s, 600, true));
+    void* a = s.get();
+    CHECK(!take(s, 700, false) && s.get() == a && live.count(a) && s.size() == 600);
+    CHECK(!take(s, 700, true) && s.get() == a && live.count(a));
+    CHECK(take(s, 500, false) && s.get() == a);
+''',
+}
+
+
+@pytest.mark.parametrize("name", CASES)
+def test_scratch(name, tmp_path):
+    src, exe = tmp_path / "scratch.cpp", tmp_path / "scratch"
+    src.write_text(HEAD + CASES[name] + r'''
+    s.release_all();
+    CHECK(live.empty() && !s.get() && !released_in_capture);
+    return 0;
+}
+''')
+    subprocess.check_call(["g++", "-std=c++17", "-Wall", "-Wextra", "-Werror", "-fsanitize=address,undefined", "-I", CSRC,
+                           str(src), "-o", str(exe)])
+    p = subprocess.run([str(exe)], capture_output=True, text=True)
+    assert p.returncode == 0, p.stdout + p.stderr
