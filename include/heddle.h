@@ -755,7 +755,8 @@ heddle_status heddle_attention(heddle_ctx* ctx, const heddle_attention_args* arg
  * the context's scratch between its passes, 2 bytes a visible pair and query
  * head in tiles of 128 x 128, as many key heads at a time as 4 GiB hold; longer
  * sequences, and a device without that room, have them computed twice (dq may
- * then differ in its last bits). */
+ * then differ in its last bits); room once refused is asked for again by later
+ * calls. */
 typedef struct {
     heddle_attention_args fwd;
     heddle_heads d_o, dq, dk, dv;

@@ -395,12 +395,12 @@ heddle_status heddle_attention_backward(heddle_ctx* ctx, const heddle_attention_
     // room to keep the scores' gradients, or without them where that is refused
     const size_t most = hd::attention_grad_scratch(*x, *args, true);
     const size_t least = hd::attention_grad_scratch(*x, *args, false);
-    const bool keep = !(x->ws_refused && most >= x->ws_refused) &&
-                      (most == 0 || x->scratch.reserve(most, capturing((cudaStream_t)stream), most > least));
-    if (!keep) {
-        if (!x->ws_refused || most < x->ws_refused) x->ws_refused = most;
-        CHECK(reserve(x, least, (cudaStream_t)stream));
+    bool keep = most <= x->scratch.size();
+    if (!keep && most > least && x->refusal.worth_asking(most)) {
+        keep = x->scratch.reserve(most, capturing((cudaStream_t)stream), true);
+        keep ? x->refusal.granted(most) : x->refusal.refused(most);
     }
+    CHECK(reserve(x, keep ? most : least, (cudaStream_t)stream));
     return done(x, hd::launch_attention_grad(*x, *args, x->scratch.get(), keep, (cudaStream_t)stream),
                 "heddle_attention_backward");
 }

@@ -43,7 +43,7 @@ struct OpContext {
     uint32_t* err = nullptr;  // device error flags
     int32_t* sched = nullptr;  // two counters of kernels that hand out work, zero between launches
     Scratch<DeviceMemory> scratch;
-    size_t ws_refused = 0;  // the least scratch that the device had no room for, where a call can do without
+    Refusal refusal;  // of scratch that a call can do without
     char* msg = nullptr;
     size_t msg_size = 0;
     mutable bool chained = false;  // the call has launched a kernel already

@@ -86,4 +86,27 @@ class Scratch {
     Kept* kept = nullptr;
 };
 
+// Room that a call can do without, once it was refused: asked for again by
+// every kAgain-th call alone, since the device's refusal takes its time.
+class Refusal {
+  public:
+    static constexpr int kAgain = 16;
+    bool worth_asking(size_t need) {
+        if (!least || need < least) return true;
+        return ++passed % kAgain == 0;
+    }
+    void refused(size_t need) {
+        if (least && least <= need) return;
+        least = need;
+        passed = 0;
+    }
+    void granted(size_t need) {
+        if (need >= least) least = 0;
+    }
+
+  private:
+    size_t least = 0;  // of the sizes refused
+    unsigned passed = 0;
+};
+
 }  // namespace hd

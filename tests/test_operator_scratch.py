@@ -99,6 +99,42 @@ CASES = {
 }
 
 
+REFUSALS = {
+    "is asked for again after some calls": r'''
+    CHECK(r.worth_asking(100));
+    r.refused(100);
+    int asked = 0;
+    for (int i = 0; i < 10 * hd::Refusal::kAgain; ++i) asked += r.worth_asking(i % 2 ? 100 : 200);
+    CHECK(asked == 10);
+''',
+    "less than what was refused is asked for at once": r'''
+    r.refused(100);
+    CHECK(r.worth_asking(99) && !r.worth_asking(100));
+    r.refused(50);
+    CHECK(!r.worth_asking(99) && r.worth_asking(49));
+    r.refused(80);
+    CHECK(!r.worth_asking(50));
+''',
+    "is forgotten once granted": r'''
+    r.refused(100);
+    r.granted(60);  // less than was refused says nothing of it
+    CHECK(!r.worth_asking(100));
+    r.granted(100);
+    CHECK(r.worth_asking(100) && r.worth_asking(200));
+''',
+}
+
+
+@pytest.mark.parametrize("name", REFUSALS)
+def test_refusal(name, tmp_path):
+    src, exe = tmp_path / "refusal.cpp", tmp_path / "refusal"
+    src.write_text(HEAD.split("static size_t room")[0] + "int main() {\n    hd::Refusal r;\n" + REFUSALS[name]
+                   + "    return 0;\n}\n")
+    subprocess.check_call(["g++", "-std=c++17", "-Wall", "-Wextra", "-Werror", "-I", CSRC, str(src), "-o", str(exe)])
+    p = subprocess.run([str(exe)], capture_output=True, text=True)
+    assert p.returncode == 0, p.stdout + p.stderr
+
+
 @pytest.mark.parametrize("name", CASES)
 def test_scratch(name, tmp_path):
     src, exe = tmp_path / "scratch.cpp", tmp_path / "scratch"
