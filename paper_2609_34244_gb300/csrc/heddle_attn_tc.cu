@@ -1502,7 +1502,13 @@ Params params_of(const OpContext& x, const heddle_attention_args& a) {
     p.rest_parts = (int32_t)(rest < 1 ? 1 : rest > 32 ? 32 : rest);
     const int64_t sinks = a.sinks < a.kv_len ? a.sinks : a.kv_len;
     p.lead = a.window ? (int32_t)ceil_div(sinks, kTile) : 0;
-    const int64_t lead = p.rest_parts * p.q_tiles / (each < 8 ? 8 : each);
+    // at most 64 parts, and no more than make eight CTAs an SM: their sums are
+    // 128 KB a part at heads of 128, 0.3 GB in all, however many tokens stay
+    // visible (8192 tokens with 2048 first ones, window 256, 32 heads over 8 of
+    // 128: 788 us, and 949 in twice the parts)
+    int64_t lead = p.rest_parts * p.q_tiles / (each < 8 ? 8 : each);
+    const int64_t enough = p.lead ? ceil_div(8 * (int64_t)x.num_sms, heads * p.lead) : 1;
+    lead = lead < enough ? lead : enough;
     p.lead_parts = (int32_t)(lead < p.rest_parts ? p.rest_parts : lead > 64 ? 64 : lead);
     return p;
 }

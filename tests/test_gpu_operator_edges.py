@@ -10,6 +10,7 @@ torch = pytest.importorskip("torch")
 
 import op_reference as R  # noqa: E402
 from test_gpu_operators import CANARY, gen, lib, rand, refused  # noqa: E402, F401
+from test_gpu_operators import test_attention as attention_test  # noqa: E402
 
 pytestmark = pytest.mark.gpu
 
@@ -276,3 +277,12 @@ def test_graphs_outlive_larger_calls(heddle_lib, warm):
         assert h.heddle_device_errors(ctx) == 0
     finally:
         h.heddle_destroy(ctx)
+
+
+@pytest.mark.parametrize("b,t,hq,hk,d,window,sinks,kind", [
+    (1, 1100, 4, 2, 64, 50, 400, None), (2, 2100, 4, 4, 128, 30, 900, "both"), (1, 1500, 8, 1, 96, 1, 1400, None),
+])
+def test_first_tokens_of_several_tiles(lib, b, t, hq, hk, d, window, sinks, kind):
+    """Many tokens that stay visible, whose gradients come in parts."""
+    for dt in ("bf16", "fp16"):
+        attention_test(lib, b, t, t, hq, hk, d, window, sinks, kind, dt)

@@ -8,7 +8,8 @@ import subprocess
 import pytest
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
-CSRC = os.path.join(ROOT, "paper_2609_34244_gb300", "csrc")
+PKG = os.path.join(ROOT, "paper_2609_34244_gb300")
+CSRC = os.path.join(PKG, "csrc")
 
 HEAD = r'''
 #include <cstdio>
@@ -148,3 +149,40 @@ def test_scratch(name, tmp_path):
                            str(src), "-o", str(exe)])
     p = subprocess.run([str(exe)], capture_output=True, text=True)
     assert p.returncode == 0, p.stdout + p.stderr
+
+
+def test_scratch_of_tokens_that_stay_visible(heddle_lib, tmp_path):
+    """Sums of parts of the gradients' key tiles stay within 0.35 GB (two of 128
+    x 128 floats a part, 16 parts an SM at most, where a ceiling doubles eight)
+    beside delta and dS, whatever the first tokens and lengths are."""
+    from paper_2609_34244_gb300 import _build
+    src, exe = tmp_path / "sizes.cu", tmp_path / "sizes"
+    src.write_text(r"""
+#include <cstdio>
+#include "heddle_attn.cuh"
+int main() {
+    hd::OpContext x;
+    x.num_sms = 152;
+    const long long lengths[] = {1, 100, 4095, 8192, 32768, 131072};
+    for (long long t : lengths)
+        for (long long window : {0ll, 1ll, 256ll, 5000ll})
+            for (long long sinks : {0ll, 4ll, 300ll, 4096ll, 16384ll, 100000ll})
+                for (int group : {1, 4, 128})
+                    for (int heads : {1, 8})
+                        for (int batch : {1, 16}) {
+                            heddle_attention_args a{};
+                            a.batch = batch, a.q_len = a.kv_len = t;
+                            a.q_heads = group * heads, a.kv_heads = heads, a.head_dim = 128;
+                            a.window = window, a.sinks = sinks, a.scale = 0.1f;
+                            std::printf("%lld %lld %lld %d %d %d %zu\n", t, window, sinks, group, heads, batch,
+                                        hd::attn_tc_grad_scratch(x, a, false));
+                        }
+    return 0;
+}
+""")
+    subprocess.check_call([_build.nvcc(), *_build.ARCH, "-std=c++17", "-I", _build.INCLUDE, "-I", CSRC, str(src), "-o",
+                           str(exe), "-L", PKG, "-lheddle", "-Xlinker", "-rpath", "-Xlinker", PKG])
+    sizes = [tuple(map(int, line.split())) for line in subprocess.check_output([str(exe)], text=True).splitlines()]
+    assert len(sizes) == 6 * 4 * 6 * 3 * 2 * 2
+    assert max(s[-1] for s in sizes) <= 0.35e9, max(sizes, key=lambda s: s[-1])
+    assert any(s[-1] > 1e6 for s in sizes)
