@@ -558,8 +558,11 @@ heddle_status heddle_phase_times(heddle_ctx* ctx, double ms[HEDDLE_N_PHASES],
  * Scratch belongs to the context, grows on first use of a larger size (E_NOMEM
  * if that fails) and is held until the context is destroyed; what a captured
  * call was given is held beside the larger blocks that follow it, so that its
- * graph can be replayed as long as the context lives.  Calls on one context,
- * and replays of graphs of them, must not overlap on the GPU.
+ * graph can be replayed as long as the context lives.  A context is one host
+ * thread's at a time.  Its calls may come on any streams: one that takes scratch
+ * waits on its stream for the last that did.  Replays of graphs are not waited
+ * for and do not wait: they must not overlap the context's other calls, nor one
+ * another.
  * Errors of all: E_ARG (a null pointer, a negative size, a bad stride, type
  * or activation), E_LIMIT (a size beyond the limits named), E_CUDA, E_NOMEM;
  * nothing is launched then.  A call whose outputs are empty is a no-op; a

@@ -502,6 +502,7 @@ heddle_status heddle_create(heddle_ctx** out, int32_t device) {
 
     if (e == cudaSuccess) e = cudaMalloc(&x->op.sched, 2 * sizeof(int32_t));
     if (e == cudaSuccess) e = cudaMemset(x->op.sched, 0, 2 * sizeof(int32_t));
+    if (e == cudaSuccess) e = cudaEventCreateWithFlags(&x->op.last, cudaEventDisableTiming);
     x->op.device = device;
     x->op.num_sms = x->num_sms;
     x->op.err = x->d_flags + 1;
@@ -561,6 +562,7 @@ void heddle_destroy(heddle_ctx* x) {
         cudaFree(x->lv_bounds[i]);
     }
     x->op.scratch.release_all();
+    if (x->op.last) cudaEventDestroy(x->op.last);
     cudaFree(x->op.sched);
     cudaFree(x->d_timg);
     cudaFree(x->d_node_type);

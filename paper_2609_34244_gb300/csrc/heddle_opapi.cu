@@ -25,6 +25,7 @@ struct OpDeviceGuard {
     int prev = -1;
     explicit OpDeviceGuard(OpContext* x) {
         x->chained = false;
+        x->takes_scratch = false;
         if (cudaGetDevice(&prev) != cudaSuccess) prev = -1;
         if (prev != x->device) cudaSetDevice(x->device);
         else prev = -1;
@@ -43,17 +44,42 @@ bool capturing(cudaStream_t st) {
     return true;
 }
 
-// At least `need` bytes of scratch.
+// At least `need` bytes of scratch, which the last call that took some may
+// still be using on another stream: the call waits for its end there.
 heddle_status reserve(OpContext* x, size_t need, cudaStream_t st) {
-    if (need == 0 || x->scratch.reserve(need, capturing(st))) return HEDDLE_OK;
-    return fail(x, HEDDLE_E_NOMEM, "%zu bytes of operator scratch", need);
+    if (need == 0) return HEDDLE_OK;
+    const bool captured = capturing(st);
+    if (!x->scratch.reserve(need, captured)) return fail(x, HEDDLE_E_NOMEM, "%zu bytes of operator scratch", need);
+    if (captured) return HEDDLE_OK;
+    unsigned long long id = 0;
+    cudaError_t e = cudaStreamGetId(st, &id);
+    if (e == cudaSuccess && x->any_last && id != x->last_stream) e = cudaStreamWaitEvent(st, x->last, 0);
+    if (e != cudaSuccess) {
+        cudaGetLastError();
+        return fail(x, HEDDLE_E_CUDA, "the call's stream: %s", cudaGetErrorString(e));
+    }
+    x->last_stream = id;
+    x->takes_scratch = true;
+    return HEDDLE_OK;
 }
 
-heddle_status done(OpContext* x, cudaError_t e, const char* what) {
+// The end of a call that may have launched kernels on the stream.
+heddle_status done(OpContext* x, cudaError_t e, const char* what, cudaStream_t st) {
+    if (x->takes_scratch) {
+        const cudaError_t r = cudaEventRecord(x->last, st);
+        if (e == cudaSuccess) e = r;
+        x->any_last = true;
+    }
     if (e != cudaSuccess) {
         cudaGetLastError();
         return fail(x, HEDDLE_E_CUDA, "%s: %s", what, cudaGetErrorString(e));
     }
+    x->msg[0] = 0;
+    return HEDDLE_OK;
+}
+
+// A call without outputs.
+heddle_status nothing(OpContext* x) {
     x->msg[0] = 0;
     return HEDDLE_OK;
 }
@@ -176,8 +202,9 @@ heddle_status heddle_linear(heddle_ctx* ctx, const heddle_linear_args* args, voi
     if (a.residual) CHECK(check_matrix(x, "residual", a.residual, a.ldr, a.m, a.n, 2));
     REQUIRE(aligned_to(a.bias, 2), HEDDLE_E_ARG, "bias is not aligned to its element");
     if (a.pre) CHECK(check_matrix(x, "pre", a.pre, a.ldp, a.m, a.n, 4));
-    if (a.m == 0 || a.n == 0) return done(x, cudaSuccess, "");
+    if (a.m == 0 || a.n == 0) return nothing(x);
     OpDeviceGuard guard(x);
+    cudaStream_t st = (cudaStream_t)stream;
     hd::GemmArgs g{};
     g.M = a.m, g.N = a.n, g.K = a.k;
     g.kind = hd::kGemmLinear, g.dtype = a.dtype, g.act = a.act, g.count = 1;
@@ -187,8 +214,8 @@ heddle_status heddle_linear(heddle_ctx* ctx, const heddle_linear_args* args, voi
     g.bias = a.bias;
     g.residual = a.residual, g.ldr = a.ldr;
     g.pre[0] = a.pre, g.ldp = a.ldp;
-    CHECK(reserve(x, hd::gemm_scratch(*x, g), (cudaStream_t)stream));
-    return done(x, hd::launch_gemm(*x, g, x->scratch.get(), (cudaStream_t)stream), "heddle_linear");
+    CHECK(reserve(x, hd::gemm_scratch(*x, g), st));
+    return done(x, hd::launch_gemm(*x, g, x->scratch.get(), st), "heddle_linear", st);
 }
 
 heddle_status heddle_linear_backward(heddle_ctx* ctx, const heddle_linear_grad_args* args, void* stream) {
@@ -249,7 +276,7 @@ heddle_status heddle_linear_backward(heddle_ctx* ctx, const heddle_linear_grad_a
     if (e == cudaSuccess && a.m && a.n && a.k) e = hd::lay_out_operands(*x, both, count, rest, st);
     if (e == cudaSuccess && want_x) e = hd::launch_gemm(*x, gx, rest, st);
     if (e == cudaSuccess && want_w) e = hd::launch_gemm(*x, gw, rest, st);
-    return done(x, e, "heddle_linear_backward");
+    return done(x, e, "heddle_linear_backward", st);
 }
 
 heddle_status heddle_gated_ffn(heddle_ctx* ctx, const heddle_gated_ffn_args* args, void* stream) {
@@ -267,8 +294,9 @@ heddle_status heddle_gated_ffn(heddle_ctx* ctx, const heddle_gated_ffn_args* arg
         CHECK(check_matrix(x, "gate", a.gate, a.lds, a.m, a.n, 4));
         CHECK(check_matrix(x, "up", a.up, a.lds, a.m, a.n, 4));
     }
-    if (a.m == 0 || a.n == 0) return done(x, cudaSuccess, "");
+    if (a.m == 0 || a.n == 0) return nothing(x);
     OpDeviceGuard guard(x);
+    cudaStream_t st = (cudaStream_t)stream;
     hd::GemmArgs g{};
     g.M = a.m, g.N = a.n, g.K = a.k;
     g.kind = hd::kGemmGated, g.dtype = a.dtype, g.act = a.act, g.count = 1;
@@ -277,8 +305,8 @@ heddle_status heddle_gated_ffn(heddle_ctx* ctx, const heddle_gated_ffn_args* arg
     g.b[1] = {a.w_up, a.ldu};
     g.out[0] = a.y, g.ldo = a.ldy;
     g.pre[0] = a.gate, g.pre[1] = a.up, g.ldp = a.lds;
-    CHECK(reserve(x, hd::gemm_scratch(*x, g), (cudaStream_t)stream));
-    return done(x, hd::launch_gemm(*x, g, x->scratch.get(), (cudaStream_t)stream), "heddle_gated_ffn");
+    CHECK(reserve(x, hd::gemm_scratch(*x, g), st));
+    return done(x, hd::launch_gemm(*x, g, x->scratch.get(), st), "heddle_gated_ffn", st);
 }
 
 heddle_status heddle_gated_ffn_backward(heddle_ctx* ctx, const heddle_gated_ffn_grad_args* args, void* stream) {
@@ -302,7 +330,7 @@ heddle_status heddle_gated_ffn_backward(heddle_ctx* ctx, const heddle_gated_ffn_
         CHECK(check_matrix(x, "dx", a.dx, a.lddx, a.m, a.k, 2));
     }
     const bool want_x = a.dx && a.m && a.k, want_w = a.dw_gate && a.n && a.k;
-    if (!want_x && !want_w) return done(x, cudaSuccess, "");
+    if (!want_x && !want_w) return nothing(x);
     OpDeviceGuard guard(x);
     cudaStream_t st = (cudaStream_t)stream;
 
@@ -338,7 +366,7 @@ heddle_status heddle_gated_ffn_backward(heddle_ctx* ctx, const heddle_gated_ffn_
     if (e == cudaSuccess && a.m && a.n && a.k) e = hd::lay_out_operands(*x, both, count, rest, st);
     if (e == cudaSuccess && want_x) e = hd::launch_gemm(*x, gx, rest, st);
     if (e == cudaSuccess && want_w) e = hd::launch_gemm(*x, gw, rest, st);
-    return done(x, e, "heddle_gated_ffn_backward");
+    return done(x, e, "heddle_gated_ffn_backward", st);
 }
 
 heddle_status heddle_qk_norm_rope(heddle_ctx* ctx, const heddle_qk_norm_rope_args* args, void* stream) {
@@ -346,9 +374,10 @@ heddle_status heddle_qk_norm_rope(heddle_ctx* ctx, const heddle_qk_norm_rope_arg
     OpContext* x = heddle_op_context(ctx);
     REQUIRE(args, HEDDLE_E_ARG, "args is null");
     CHECK(check_norm_rope(x, *args, true));
-    if (args->tokens == 0 || args->q_heads + args->k_heads == 0) return done(x, cudaSuccess, "");
+    if (args->tokens == 0 || args->q_heads + args->k_heads == 0) return nothing(x);
     OpDeviceGuard guard(x);
-    return done(x, hd::launch_qk_norm_rope(*x, *args, (cudaStream_t)stream), "heddle_qk_norm_rope");
+    cudaStream_t st = (cudaStream_t)stream;
+    return done(x, hd::launch_qk_norm_rope(*x, *args, st), "heddle_qk_norm_rope", st);
 }
 
 heddle_status heddle_qk_norm_rope_backward(heddle_ctx* ctx, const heddle_qk_norm_rope_grad_args* args, void* stream) {
@@ -363,9 +392,10 @@ heddle_status heddle_qk_norm_rope_backward(heddle_ctx* ctx, const heddle_qk_norm
     REQUIRE(args->dwq && args->dwk, HEDDLE_E_ARG, "dwq or dwk is null");
     REQUIRE(aligned_to(args->dwq, 4) && aligned_to(args->dwk, 4), HEDDLE_E_ARG, "dwq or dwk is not aligned");
     OpDeviceGuard guard(x);
-    CHECK(reserve(x, hd::qk_norm_rope_grad_scratch(*x, *args), (cudaStream_t)stream));
-    return done(x, hd::launch_qk_norm_rope_grad(*x, *args, x->scratch.get(), (cudaStream_t)stream),
-                "heddle_qk_norm_rope_backward");
+    cudaStream_t st = (cudaStream_t)stream;
+    CHECK(reserve(x, hd::qk_norm_rope_grad_scratch(*x, *args), st));
+    return done(x, hd::launch_qk_norm_rope_grad(*x, *args, x->scratch.get(), st),
+                "heddle_qk_norm_rope_backward", st);
 }
 
 heddle_status heddle_attention(heddle_ctx* ctx, const heddle_attention_args* args, void* stream) {
@@ -373,10 +403,11 @@ heddle_status heddle_attention(heddle_ctx* ctx, const heddle_attention_args* arg
     OpContext* x = heddle_op_context(ctx);
     REQUIRE(args, HEDDLE_E_ARG, "args is null");
     CHECK(check_attention(x, *args, true));
-    if (args->batch == 0 || args->q_len == 0) return done(x, cudaSuccess, "");
+    if (args->batch == 0 || args->q_len == 0) return nothing(x);
     OpDeviceGuard guard(x);
-    CHECK(reserve(x, hd::attention_scratch(*x, *args), (cudaStream_t)stream));
-    return done(x, hd::launch_attention(*x, *args, x->scratch.get(), (cudaStream_t)stream), "heddle_attention");
+    cudaStream_t st = (cudaStream_t)stream;
+    CHECK(reserve(x, hd::attention_scratch(*x, *args), st));
+    return done(x, hd::launch_attention(*x, *args, x->scratch.get(), st), "heddle_attention", st);
 }
 
 heddle_status heddle_attention_backward(heddle_ctx* ctx, const heddle_attention_grad_args* args, void* stream) {
@@ -390,19 +421,20 @@ heddle_status heddle_attention_backward(heddle_ctx* ctx, const heddle_attention_
     CHECK(check_heads(x, "dk", args->dk, a.batch, a.kv_len, a.kv_heads, a.head_dim, 2, true));
     CHECK(check_heads(x, "dv", args->dv, a.batch, a.kv_len, a.kv_heads, a.head_dim, 2, true));
     REQUIRE(a.lse || a.batch * a.q_len == 0, HEDDLE_E_ARG, "lse is null");
-    if (a.batch == 0 || (a.q_len == 0 && a.kv_len == 0)) return done(x, cudaSuccess, "");
+    if (a.batch == 0 || (a.q_len == 0 && a.kv_len == 0)) return nothing(x);
     OpDeviceGuard guard(x);
+    cudaStream_t st = (cudaStream_t)stream;
     // room to keep the scores' gradients, or without them where that is refused
     const size_t most = hd::attention_grad_scratch(*x, *args, true);
     const size_t least = hd::attention_grad_scratch(*x, *args, false);
     bool keep = most <= x->scratch.size();
     if (!keep && most > least && x->refusal.worth_asking(most)) {
-        keep = x->scratch.reserve(most, capturing((cudaStream_t)stream), true);
+        keep = x->scratch.reserve(most, capturing(st), true);
         keep ? x->refusal.granted(most) : x->refusal.refused(most);
     }
-    CHECK(reserve(x, keep ? most : least, (cudaStream_t)stream));
-    return done(x, hd::launch_attention_grad(*x, *args, x->scratch.get(), keep, (cudaStream_t)stream),
-                "heddle_attention_backward");
+    CHECK(reserve(x, keep ? most : least, st));
+    return done(x, hd::launch_attention_grad(*x, *args, x->scratch.get(), keep, st),
+                "heddle_attention_backward", st);
 }
 
 }  // extern "C"

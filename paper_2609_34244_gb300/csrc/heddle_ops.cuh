@@ -44,6 +44,10 @@ struct OpContext {
     int32_t* sched = nullptr;  // two counters of kernels that hand out work, zero between launches
     Scratch<DeviceMemory> scratch;
     Refusal refusal;  // of scratch that a call can do without
+    // the end of the last call that took scratch, on the stream of that id; none in graphs
+    cudaEvent_t last = nullptr;
+    unsigned long long last_stream = 0;
+    bool any_last = false, takes_scratch = false;  // takes_scratch: the call at hand does
     char* msg = nullptr;
     size_t msg_size = 0;
     mutable bool chained = false;  // the call has launched a kernel already

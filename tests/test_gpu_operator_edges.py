@@ -286,3 +286,33 @@ def test_first_tokens_of_several_tiles(lib, b, t, hq, hk, d, window, sinks, kind
     """Many tokens that stay visible, whose gradients come in parts."""
     for dt in ("bf16", "fp16"):
         attention_test(lib, b, t, t, hq, hk, d, window, sinks, kind, dt)
+
+
+def test_calls_on_several_streams_take_turns_at_scratch(heddle_lib):
+    """Calls of one context on streams that nothing orders give what they give
+    one after another."""
+    h = heddle_lib
+    ctx = h.heddle_create(0)
+    try:
+        sizes = (1500, 130, 700, 40, 1100, 257)
+        steps = [_step(h, ctx, gen(80 + i), t) for i, t in enumerate(sizes)]
+        want = []
+        for _, outputs, calls in steps:
+            calls()
+            torch.cuda.synchronize()
+            want.append([v.clone() for v in outputs])
+        streams = [torch.cuda.Stream() for _ in range(3)]
+        for turn in range(8):
+            for _, outputs, _ in steps:
+                for v in outputs:
+                    v.fill_(CANARY)
+            torch.cuda.synchronize()
+            for i, (_, _, calls) in enumerate(steps):
+                with torch.cuda.stream(streams[(i + turn) % 3]):
+                    calls()
+            torch.cuda.synchronize()
+            for (_, outputs, _), values in zip(steps, want):
+                assert all(torch.equal(a, b) for a, b in zip(outputs, values))
+        assert h.heddle_device_errors(ctx) == 0
+    finally:
+        h.heddle_destroy(ctx)
