@@ -66,14 +66,22 @@ __global__ void __launch_bounds__(kWarps * 32) attn_row_kernel(heddle_attention_
     }
 }
 
+// The counters of kernels that hand out work, zero at the start of every call's
+// gradients: whatever calls that overlapped against the rule left in them would
+// make all later ones leave out query tiles.
+__device__ __forceinline__ void start_pieces(int32_t* sched) {
+    if (blockIdx.x == 0 && threadIdx.x < 2) sched[threadIdx.x] = 0;
+}
+
 // delta_i = do_i . o_i for heads of whole 16-byte units: GL lanes a row, 16
 // bytes a lane, rows in the order of memory.  Bound by memory: 67 MB in 14 us
 // with its launch (4096 tokens of 32 heads of 128; a warp a row took 33).
 template <class T, int GL>
 __global__ void __launch_bounds__(256) attn_delta_wide_kernel(const __grid_constant__ heddle_attention_grad_args g,
-                                                              float* delta) {
+                                                              float* delta, int32_t* sched) {
     allow_dependents();
     await_previous();
+    start_pieces(sched);
     const heddle_attention_args& a = g.fwd;
     const int lane = threadIdx.x % GL;
     const uint32_t r = blockIdx.x * (256 / GL) + threadIdx.x / GL;  // (b, i, h)
@@ -163,9 +171,11 @@ bool units16(const heddle_heads& t) {
 
 // delta_i = do_i . o_i
 template <class T>
-__global__ void __launch_bounds__(kWarps * 32) attn_delta_kernel(heddle_attention_grad_args g, float* delta) {
+__global__ void __launch_bounds__(kWarps * 32) attn_delta_kernel(heddle_attention_grad_args g, float* delta,
+                                                                 int32_t* sched) {
     allow_dependents();
     await_previous();
+    start_pieces(sched);
     const heddle_attention_args& a = g.fwd;
     const int lane = threadIdx.x % 32, D = a.head_dim;
     const int64_t rows = a.batch * a.q_heads * a.q_len;
@@ -254,11 +264,13 @@ cudaError_t attention_grad(const OpContext& x, const heddle_attention_grad_args&
     const bool tc = attn_tc_takes_grad(g);
     if (rows && a.head_dim % 8 == 0 && a.head_dim <= 128 && units16(a.o) && units16(g.d_o)) {
         if (a.head_dim <= 64)
-            launch(x, attn_delta_wide_kernel<T, 8>, dim3((unsigned)ceil_div(rows, 32)), 256, 0, st, g, delta);
+            launch(x, attn_delta_wide_kernel<T, 8>, dim3((unsigned)ceil_div(rows, 32)), 256, 0, st, g, delta,
+                   x.sched);
         else
-            launch(x, attn_delta_wide_kernel<T, 16>, dim3((unsigned)ceil_div(rows, 16)), 256, 0, st, g, delta);
+            launch(x, attn_delta_wide_kernel<T, 16>, dim3((unsigned)ceil_div(rows, 16)), 256, 0, st, g, delta,
+                   x.sched);
     } else if (rows) {
-        launch(x, attn_delta_kernel<T>, dim3(row_blocks(x, rows)), kWarps * 32, 0, st, g, delta);
+        launch(x, attn_delta_kernel<T>, dim3(row_blocks(x, rows)), kWarps * 32, 0, st, g, delta, x.sched);
     }
     if (tc) {
         const bool all = a.window && a.window + a.sinks <= kFewKeys;

@@ -316,3 +316,46 @@ def test_calls_on_several_streams_take_turns_at_scratch(heddle_lib):
         assert h.heddle_device_errors(ctx) == 0
     finally:
         h.heddle_destroy(ctx)
+
+
+def test_counters_left_by_calls_that_overlapped(heddle_lib, tmp_path):
+    """What replays that overlap against the rule may leave in the context's
+    work counters does not reach later calls."""
+    import ctypes
+    import os
+    import subprocess
+    from paper_2609_34244_gb300 import _build
+    h = heddle_lib
+    src, so = tmp_path / "counters.cu", tmp_path / "counters.so"
+    src.write_text('#include "heddle_ops.cuh"\n'
+                   'extern "C" int leave(heddle_ctx* c, int a, int b) {\n'
+                   '    const int32_t v[2] = {a, b};\n'
+                   '    return cudaMemcpy(heddle_op_context(c)->sched, v, sizeof v, cudaMemcpyHostToDevice);\n'
+                   '}\n')
+    pkg = os.path.dirname(h.LIB_PATH)
+    subprocess.check_call([_build.nvcc(), *_build.ARCH, "-std=c++17", "-shared", "-Xcompiler", "-fPIC", "-I",
+                           _build.INCLUDE, "-I", _build.CSRC, str(src), "-o", str(so), "-L", pkg, "-lheddle", "-Xlinker",
+                           "-rpath", "-Xlinker", pkg])
+    leave = ctypes.CDLL(str(so)).leave
+    leave.argtypes = [ctypes.c_void_p, ctypes.c_int, ctypes.c_int]
+    ctx = h.heddle_create(0)
+    try:
+        for heads, t in ((8, 1000), (4, 33)):
+            g, dt = gen(t), torch.bfloat16
+            q, k, v, do = (rand(g, 4, t, n, 64, dt=dt) for n in (heads, 2, 2, heads))
+            o, lse = torch.empty_like(q), torch.empty(4, heads, t, device="cuda")
+            h.heddle_attention(ctx, q, k, v, o, lse)
+
+            def grads():
+                d = [torch.full_like(x, CANARY) for x in (q, k, v)]
+                h.heddle_attention_backward(ctx, do, q, k, v, o, lse, *d)
+                torch.cuda.synchronize()
+                return d
+
+            want = grads()
+            for left in ((3, 0), (1 << 20, 5), (0, 1 << 20)):
+                assert leave(ctx, *left) == 0
+                for _ in range(2):
+                    assert all(torch.equal(a, b) for a, b in zip(grads(), want))
+    finally:
+        h.heddle_destroy(ctx)
