@@ -468,13 +468,15 @@ __global__ void __launch_bounds__(kThreads, 1)
         const int w = warp % 4;
         const int from = (warp - 4) / 4 * (kOut / 2), to = from + kOut / 2;
         float* t0 = epi + (warp - 4) * 32 * kPitch;
+        // a tile's sums are waited for as a whole: at most 4096 cycles a step more
+        const long long limit = kWaitCycles + 4096ll * per_tile;
         int half = 0;
         uint32_t round = 0;
         for (int64_t t = first; t < p.tiles; t += step) {
             int z, tm, tn;
             tile_at(p, t, z, tm, tn);
             if (per_tile) {
-                if (!__all_sync(~0u, mbar_wait(done + 8 * half, round, gave_up))) break;
+                if (!__all_sync(~0u, mbar_wait(done + 8 * half, round, gave_up, limit))) break;
                 fence_after();
             }
             const uint32_t acc = tmem + half * BN + ((uint32_t)(w * 32) << 16);

@@ -49,20 +49,23 @@ __device__ __forceinline__ bool mbar_try(uint32_t bar, uint32_t parity) {
 }
 
 // Cycles a wait lasts at most: two seconds at 2 GHz, thousands of times the
-// longest wait of a launch that runs as it should.
+// longest wait of a launch that runs as it should.  A wait for work of any
+// length has a `limit` of its own; it ends early all the same where a wait of
+// those at that work runs out.
 constexpr long long kWaitCycles = 4ll << 30;
 
 // Waits for the phase of the given parity.  False where the wait ran out, or
 // another one of the CTA did (`gave_up`, shared): the caller then stops
 // issuing work and leaves for the CTA's common end.
-__device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatile uint32_t* gave_up) {
+__device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatile uint32_t* gave_up,
+                                          long long limit = kWaitCycles) {
     if (mbar_try(bar, parity)) return true;
     const long long start = clock64();
     for (;;) {
         for (int i = 0; i < 32; ++i)
             if (mbar_try(bar, parity)) return true;
         if (*gave_up) return false;
-        if (clock64() - start > kWaitCycles) {
+        if (clock64() - start > limit) {
             *gave_up = 1;
             return false;
         }

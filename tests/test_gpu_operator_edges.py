@@ -359,3 +359,29 @@ def test_counters_left_by_calls_that_overlapped(heddle_lib, tmp_path):
                     assert all(torch.equal(a, b) for a, b in zip(grads(), want))
     finally:
         h.heddle_destroy(ctx)
+
+
+@pytest.mark.parametrize("m,n,k", [(1, 1, 2 ** 31 - 1), (9, 4, 1_000_000_000)])
+def test_contractions_that_take_seconds(lib, m, n, k):
+    """The longest contractions: a tile's one takes longer than any other wait
+    lasts.  Products of +-1, whose sums are whole numbers in any order."""
+    h, ctx = lib
+    g, dt = gen(k % 1000), torch.bfloat16
+
+    def signs(rows):
+        t = torch.empty(rows, k, dtype=dt, device="cuda")
+        for r in range(rows):
+            for at in range(0, k, 1 << 28):
+                part = t[r, at:at + (1 << 28)]
+                part.copy_(torch.randint(0, 2, part.shape, generator=g, device="cuda", dtype=torch.int8).mul_(2).sub_(1))
+        return t
+
+    x, w = signs(m), signs(n)
+    y, pre = torch.empty(m, n, dtype=dt, device="cuda"), torch.empty(m, n, device="cuda")
+    h.heddle_linear(ctx, x, w, y, pre=pre)
+    want = torch.zeros(m, n, dtype=torch.float64, device="cuda")
+    for at in range(0, k, 1 << 24):
+        want += x[:, at:at + (1 << 24)].float() @ w[:, at:at + (1 << 24)].float().T  # below 2^24: exact
+    assert want.abs().max().item() < 2 ** 24
+    assert torch.equal(pre.double(), want) and torch.equal(y, want.to(dt))
+    assert h.heddle_device_errors(ctx) == 0
