@@ -1,6 +1,6 @@
 """Calls at the edges of the layer operators' contract: empty sizes, values
-that are not finite, the ends of the element types' ranges, single rows,
-other devices."""
+that are not finite, the ends of the element types' ranges, single rows, other
+devices, graphs and streams that share a context, contractions of seconds."""
 
 import math
 
@@ -202,8 +202,8 @@ def test_tensors_of_another_device_are_refused(lib):
     names["heddle_device"] = address(device)
     dt = dict(dtype=torch.bfloat16, device="cuda")
     x, p = torch.zeros(4, 8, **dt), torch.zeros(4, 4, device="cuda")
-    q3, q4, f8, lse = x.view(1, 2, 16), x.view(1, 1, 2, 16), torch.zeros(16, device="cuda"), torch.zeros(1, 2, 1, device="cuda")
-    w16 = torch.zeros(16, **dt)
+    q3, q4 = x.view(1, 2, 16), x.view(1, 1, 2, 16)
+    f8, lse, w16 = torch.zeros(16, device="cuda"), torch.zeros(1, 2, 1, device="cuda"), torch.zeros(16, **dt)
     calls = [(h.heddle_linear, (x, x, x[:, :4])), (h.heddle_linear_backward, (x[:, :4], x, x)),
              (h.heddle_gated_ffn, (x, x, x, x[:, :4])), (h.heddle_gated_ffn_backward, (x[:, :4], x, x, x, p, p)),
              (h.heddle_qk_norm_rope, (q3, q3, w16, w16, q3, q3)),
@@ -262,7 +262,8 @@ def test_graphs_outlive_larger_calls(heddle_lib, warm):
         _, _, larger = _step(h, ctx, gen(72), 3000)
         larger()
         larger()
-        others = [torch.full((1 << 22,), CANARY, device="cuda") for _ in range(64)]  # what was given back is taken again
+        # what was given back is taken again
+        others = [torch.full((1 << 22,), CANARY, device="cuda") for _ in range(64)]
         for v in inputs:
             v.mul_(0.5)
         for v in outputs:
@@ -373,7 +374,8 @@ def test_contractions_that_take_seconds(lib, m, n, k):
         for r in range(rows):
             for at in range(0, k, 1 << 28):
                 part = t[r, at:at + (1 << 28)]
-                part.copy_(torch.randint(0, 2, part.shape, generator=g, device="cuda", dtype=torch.int8).mul_(2).sub_(1))
+                bits = torch.randint(0, 2, part.shape, generator=g, device="cuda", dtype=torch.int8)
+                part.copy_(bits.mul_(2).sub_(1))
         return t
 
     x, w = signs(m), signs(n)

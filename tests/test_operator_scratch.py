@@ -1,6 +1,6 @@
 """The layer operators' scratch (csrc/heddle_scratch.cuh) with memory of its
 own that records what is released and when (no GPU): a block whose address a
-captured graph holds outlives every growth."""
+captured graph holds outlives every growth.  And how much attention asks for."""
 
 import os
 import subprocess
@@ -145,8 +145,8 @@ def test_scratch(name, tmp_path):
     return 0;
 }
 ''')
-    subprocess.check_call(["g++", "-std=c++17", "-Wall", "-Wextra", "-Werror", "-fsanitize=address,undefined", "-I", CSRC,
-                           str(src), "-o", str(exe)])
+    subprocess.check_call(["g++", "-std=c++17", "-Wall", "-Wextra", "-Werror", "-fsanitize=address,undefined", "-I",
+                           CSRC, str(src), "-o", str(exe)])
     p = subprocess.run([str(exe)], capture_output=True, text=True)
     assert p.returncode == 0, p.stdout + p.stderr
 
