@@ -744,6 +744,11 @@ struct GradBars {
     }
 };
 constexpr int kGradBarBytes = 160;
+// Chained kernels that hold tensor memory take more than half of an SM's shared
+// memory, so that no two of their CTAs share an SM: one that holds it while it
+// waits for the end of the kernel before could hold what that kernel's CTA
+// waits for, and that wait has no limit.
+constexpr int kAlone = 114 * 1024;
 
 // dq of a query tile where dS is not kept: dq = sum over key tiles of dS K with
 // S = Q K^T, dP = dO V^T, dS = scale P (dP - delta).  dS is rounded to the
@@ -759,7 +764,8 @@ template <int DP>
 struct GradShape {
     static constexpr int kTileBytes = kTile * DP * 2;
     static constexpr int kStats = 3 * kTile * 8 + 16;
-    static constexpr int kBytes = 1024 + 6 * kTileBytes + kGradBarBytes + 64 + kStats;
+    static constexpr int kUsed = 1024 + 6 * kTileBytes + kGradBarBytes + 64 + kStats;
+    static constexpr int kBytes = kUsed > kAlone ? kUsed : kAlone;
 };
 
 template <class T, int DP>
@@ -974,6 +980,7 @@ struct StoredShape {
     static constexpr int kStages = DP > 64 ? 3 : 4;
     static constexpr int kBars = 16 * kStages + 32 + 32;
     static constexpr int kBytes = 1024 + kStages * kStage + kBars + 32;
+    static_assert(kBytes >= kAlone, "see kAlone");
     static constexpr int kThreads = 256;
 };
 
@@ -1559,6 +1566,7 @@ cudaError_t forward(const OpContext& x, const Params& p, const CUtensorMap& q, c
                     cudaStream_t st) {
     using F = Forward<DP, NT>;
     static_assert(F::kSlots >= 4, "two steps of K and V");
+    static_assert(F::kBytes >= kAlone, "see kAlone");
     auto* f = attn_kernel<T, DP, NT, TWINS>;
     static std::atomic<uint64_t> asked{0};
     const cudaError_t e = allow_shared(f, F::kBytes, x.device, asked);
