@@ -1,13 +1,15 @@
 // heddle_gemv.cu -- the forward products of one or two rows, and of up to eight
-// with few weights: the weights' stream from memory is the time.
+// with few weights: the weights' stream, and the latency of its start and end,
+// are the time.
 //
 // A block of eight warps takes four rows of weights (two of each matrix of
 // the gated block); every warp an eighth of the contraction, 16 bytes a lane
 // and row, so that a block's whole stream is in flight at once.  Products
 // are summed in 32 bits per lane, across the lanes, then across the warps in
-// order.  One row of 4096 x 4096 bfloat16 weights: 7.7 us with its launch,
-// 5.7 us of the kernel alone (5.9e12 bytes a second); the tensor cores' kernel
-// takes 12.9.  Every row costs as many multiply-adds again (gemv_takes).
+// order.  One row of 4096 x 4096 bfloat16 weights, a call in a graph of them:
+// 7.5 us where the weights come from memory (4.4e12 bytes a second), 4.9 where
+// L2 holds them; the tensor cores' kernel takes 11.5 and 10.1.  Every row costs
+// as many multiply-adds again (gemv_takes).
 
 #include "heddle_ops.cuh"
 
@@ -121,11 +123,12 @@ bool units16(const GemmOperand& o, int64_t rows) { return (uintptr_t)o.p % 16 ==
 
 }  // namespace
 
-// One or two rows always: at 4096 x 4096 5.7 and 8.6 us against 12.9 on the
-// tensor cores.  Up to four or eight where the rows of weights are so few that
-// tiles of them leave most SMs idle, each with the whole contraction to itself:
-// four rows of 8192 by 64, 2048 and 4096 columns 4.7, 9.1 and 14.3 us against
-// 16.6, 16.8 and 16.9; eight 6.6, 14.5 and 24.1.  More weights than that cost
+// All times with the weights from memory.  One or two rows always: at 4096 x
+// 4096 7.5 and 11.4 us against 11.5 and 11.9 on the tensor cores.  Up to four or
+// eight where the rows of weights are so few that tiles of them leave most SMs
+// idle, each with the whole contraction to itself: four rows of 8192 by 64, 2048
+// and 4096 columns 6.2, 12.6 and 18.6 us against 17.0, 17.5 and 18.7; eight by
+// 64 and 2048 8.1 and 17.0 against 17.0 and 17.5.  More weights than that cost
 // this kernel their multiply-adds: 14336 x 4096 with four rows 33 against 26.
 bool gemv_takes(const OpContext& x, const GemmArgs& g) {
     if (g.kind != kGemmLinear && g.kind != kGemmGated) return false;

@@ -12,6 +12,12 @@ the degree -- and its forward and backward passes are timed together:
   f = act(y w_gate^T) (y w_up^T)    heddle_gated_ffn
   z = f w_down^T + y                heddle_linear
 
+The norms of the hidden state that models have ahead of attention and of the
+feed-forward block are not part of it, nor are experts: the entries are those
+of the products, attention and norms per head of a dense layer, and too small
+by two passes over the hidden state in either direction.  The backward pass
+adds the two residual gradients with torch.
+
 ``python -m paper_2609_34244_gb300.layer_profile`` measures a layer, loads the
 profile beside a cluster of this GPU and slower types, and prices candidates.
 """
