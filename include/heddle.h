@@ -753,13 +753,14 @@ heddle_status heddle_attention(heddle_ctx* ctx, const heddle_attention_args* arg
 /* Gradients of heddle_attention: fwd as in the forward call with its o and
  * lse (both required, read), d_o = dL/do.  dq, dk, dv are all written (the
  * shared heads' sums included; zeros where a row sees nothing or is past its
- * sequence).  Sums run in a fixed order; the scores' gradients, scale
- * included, are rounded to the element type for their products.  Keeps them in
- * the context's scratch between its passes, 2 bytes a visible pair and query
- * head in tiles of 128 x 128, as many key heads at a time as 4 GiB hold; longer
- * sequences, and a device without that room, have them computed twice (dq may
- * then differ in its last bits); room once refused is asked for again by later
- * calls. */
+ * sequence).  Sums run in a fixed order; the scores' gradients are
+ * rounded to the element type for their products, in float16 at a power of two
+ * that the largest rows of d_o and v give, so that none overflows and small ones
+ * keep their digits.  Keeps them in the context's scratch between its passes, 2
+ * bytes a visible pair and query head in tiles of 128 x 128, as many key heads
+ * at a time as 4 GiB hold; longer sequences, and a device without that room,
+ * have them computed twice (dq may then differ in its last bits); room once
+ * refused is asked for again by later calls. */
 typedef struct {
     heddle_attention_args fwd;
     heddle_heads d_o, dq, dk, dv;

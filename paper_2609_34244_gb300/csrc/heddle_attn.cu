@@ -1,6 +1,8 @@
 // heddle_attn.cu -- attention with a sliding window and first tokens that
 // stay visible, one warp per row: any head_dim, stride and alignment.
 
+#include <type_traits>
+
 #include "heddle_attn.cuh"
 
 namespace hd {
@@ -68,9 +70,9 @@ __global__ void __launch_bounds__(kWarps * 32) attn_row_kernel(heddle_attention_
 
 // The counters of kernels that hand out work, zero at the start of every call's
 // gradients: whatever calls that overlapped against the rule left in them would
-// make all later ones leave out query tiles.
+// make all later ones leave out query tiles.  The maxima start from zero too.
 __device__ __forceinline__ void start_pieces(int32_t* sched) {
-    if (blockIdx.x == 0 && threadIdx.x < 2) sched[threadIdx.x] = 0;
+    if (blockIdx.x == 0 && threadIdx.x < kSched) sched[threadIdx.x] = 0;
 }
 
 // delta_i = do_i . o_i for heads of whole 16-byte units: GL lanes a row, 16
@@ -155,10 +157,69 @@ __device__ __forceinline__ int64_t few_delta(const heddle_attention_grad_args& g
     *value = s / total;
     return row;
 }
-template <class T>
+
+// The largest square of a gradient's row (which 0) or of a value's (1), of those
+// that count and are finite, GL lanes a row: what dS of float16 is kept in range
+// by (ds_factor).  `block` of `blocks`; to sched[2 + which], the same in any
+// order.
+template <class T, int GL>
+__device__ __forceinline__ void row_squares(const heddle_attention_grad_args& g, int which, int block, int blocks,
+                                            int32_t* sched) {
+    const heddle_attention_args& a = g.fwd;
+    constexpr int kAhead = 4;
+    const int lane = threadIdx.x % GL;
+    const int64_t step = (int64_t)blocks * (256 / GL);
+    const uint32_t mask = ((1ull << GL) - 1) << (threadIdx.x % 32 / GL * GL);
+    const heddle_heads& t = which ? a.v : g.d_o;
+    const uint32_t n = (uint32_t)(which ? a.kv_len : a.q_len), heads = which ? a.kv_heads : a.q_heads;
+    const int64_t rows = a.batch * heads * n;
+    float most = 0.0f;
+    for (int64_t r0 = (int64_t)block * (256 / GL) + threadIdx.x / GL; r0 < rows; r0 += kAhead * step) {
+        uint4 u[kAhead];
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) {
+            u[k] = make_uint4(0, 0, 0, 0);
+            if (r0 + k * step >= rows || lane * 8 >= a.head_dim) continue;
+            const uint32_t r = (uint32_t)(r0 + k * step), h = r % heads, bi = r / heads, i = bi % n, b = bi / n;
+            const Span s = span_of(a, b);
+            if (i < (which ? s.kl : s.ql)) u[k] = *reinterpret_cast<const uint4*>(at<T>(t, b, i, h) + lane * 8);
+        }
+#pragma unroll
+        for (int k = 0; k < kAhead; ++k) {
+            const T* x = reinterpret_cast<const T*>(&u[k]);
+            float s = 0.0f;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) s += to_float(x[j]) * to_float(x[j]);
+#pragma unroll
+            for (int o = GL / 2; o; o >>= 1) s += __shfl_xor_sync(mask, s, o, GL);
+            if (s < INFINITY) most = fmaxf(most, s);
+        }
+    }
+    __shared__ float parts[8];
+#pragma unroll
+    for (int o = 16; o; o >>= 1) most = fmaxf(most, __shfl_xor_sync(~0u, most, o));
+    if (threadIdx.x % 32 == 0) parts[threadIdx.x / 32] = most;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        for (int k = 1; k < 8; ++k) most = fmaxf(most, parts[k]);
+        await_previous();  // which sets it to zero
+        if (most > 0.0f) atomicMax(sched + 2 + which, __float_as_int(most));
+    }
+}
+
+// Blocks from `few` on, of float16 alone: row_squares, `squares` of them of the
+// gradients' rows and the others of the values'.
+template <class T, int GL>
 __global__ void __launch_bounds__(256) attn_few_delta_kernel(const __grid_constant__ heddle_attention_grad_args g,
-                                                             float* delta, int64_t per, bool all) {
+                                                             float* delta, int64_t per, bool all, int few,
+                                                             int squares, int32_t* sched) {
     allow_dependents();
+    if (std::is_same<T, __half>::value && (int)blockIdx.x >= few) {
+        const int block = (int)blockIdx.x - few, others = (int)gridDim.x - few - squares;
+        const int which = block >= squares;
+        row_squares<T, GL>(g, which, which ? block - squares : block, which ? others : squares, sched);
+        return;
+    }
     float value = 0.0f;
     const int64_t row = few_delta<T>(g, per, all, &value);
     await_previous();  // which writes these rows as well
@@ -275,8 +336,16 @@ cudaError_t attention_grad(const OpContext& x, const heddle_attention_grad_args&
     if (tc) {
         const bool all = a.window && a.window + a.sinks <= kFewKeys;
         const int64_t per = all || a.q_len < kFewKeys ? a.q_len : kFewKeys;
-        const unsigned blocks = (unsigned)ceil_div(a.batch * a.q_heads * per, 256 / kFewKeys);
-        launch(x, attn_few_delta_kernel<T>, dim3(blocks), 256, 0, st, g, delta, per, all || a.q_len < kFewKeys);
+        const int64_t few = ceil_div(a.batch * a.q_heads * per, 256 / kFewKeys);
+        const int group = a.head_dim <= 64 ? 8 : 16;
+        auto blocks_of = [&](int64_t n) {
+            const int64_t want = ceil_div(n, 4 * 256 / group), most = 4 * (int64_t)x.num_sms;
+            return !std::is_same<T, __half>::value ? 0 : want < most ? want : most;
+        };
+        const int64_t squares = blocks_of(rows), others = blocks_of(keys);
+        launch(x, group == 8 ? attn_few_delta_kernel<T, 8> : attn_few_delta_kernel<T, 16>,
+               dim3((unsigned)(few + squares + others)), 256, 0, st, g, delta, per, all || a.q_len < kFewKeys, (int)few,
+               (int)squares, x.sched);
         const cudaError_t e = cudaGetLastError();
         return e == cudaSuccess ? launch_attn_tc_grad(x, g, delta, rest, keep, st) : e;
     }

@@ -8,6 +8,8 @@
 // are written back over the scores as the 16-bit left operand of the next
 // product.
 
+#include <type_traits>
+
 #include "heddle_attn.cuh"
 #include "heddle_tc.cuh"
 
@@ -98,7 +100,9 @@ struct Params {
     int64_t ds_head;  // places of a key head
     int32_t ds_stride, ds_lead, ds_wrap, ds_reach;
     int32_t hb0, hbs;  // key heads of the batch that a launch takes: the first, how many
-    int32_t* sched;  // the next piece of work and the CTAs that are done, zero between launches
+    // the next piece of work and the CTAs that are done, zero between launches;
+    // the largest squares of dO's and V's rows
+    int32_t* sched;
     uint32_t* err;
 };
 
@@ -715,6 +719,23 @@ __device__ __forceinline__ void leave_pieces(int32_t* sched) {
     }
 }
 
+// What dS is multiplied by before it is rounded, and its products divided by: a
+// power of two that takes the largest dS that the call can have, 2 scale times
+// the largest gradient's row and value's row by their norms, to 2^15, so that in
+// float16 no gradient that is itself in range is lost at either end.  bfloat16
+// has the range of the sums.  Finding the maxima takes 4 us of the 241 of the
+// windowed step of two sequences of 4095 (16 heads over 4 of 64).
+template <class T>
+__device__ __forceinline__ float ds_factor(const Params& p) {
+    if (std::is_same<T, __nv_bfloat16>::value) return 1.0f;
+    const float squares[2] = {__int_as_float(p.sched[2]), __int_as_float(p.sched[3])};
+    const float most = 2.0f * p.a.scale * sqrtf(squares[0]) * sqrtf(squares[1]);
+    if (!(most > 0.0f && most < INFINITY)) return 1.0f;
+    int e;
+    frexpf(most, &e);
+    return ldexpf(1.0f, min(15 - e, 100));
+}
+
 // Sixteen warps turn scores into dS, four for every quarter of a tile's
 // columns: with eight, each scheduler's two warps left it idle two thirds of
 // the time.
@@ -751,12 +772,10 @@ constexpr int kGradBarBytes = 160;
 constexpr int kAlone = 114 * 1024;
 
 // dq of a query tile where dS is not kept: dq = sum over key tiles of dS K with
-// S = Q K^T, dP = dO V^T, dS = scale P (dP - delta).  dS is rounded to the
-// element type with the scale in it, so that float16 has to hold what the
-// gradients of Q K^T are: under a loss scale P (dP - delta) passes 65504 before
-// they do.  Q and dO stay in shared memory, K and V tiles come in two stages.
-// Scores of the next tile are computed while this one's are turned into dS (two
-// buffers).  CTAs take one query tile after another, the longest first (a grid
+// S = Q K^T, dP = dO V^T, dS = scale P (dP - delta), rounded to the element type
+// in a range of its own (ds_factor).  Q and dO stay in shared memory, K and V
+// tiles come in two stages.  Scores of the next tile are computed while this
+// one's are turned into dS (two buffers).  CTAs take one query tile after another, the longest first (a grid
 // of one tile each: 137 us against 119).  Bound by the chain from scores to dS
 // as the forward is: 114 us for two causal sequences of 2048 (32 heads over 8 of
 // 128).
@@ -877,7 +896,8 @@ __global__ void __launch_bounds__(kGradThreads, 1)
         const uint32_t lanes = (uint32_t)(warp % 4 * 32) << 16;
         const int i_row = row / p.group, h_row = row % p.group;
         const float c = p.scale_log2;
-        const uint64_t c2 = two(c, c), scale2 = two(p.a.scale, p.a.scale);
+        const float factor = ds_factor<T>(p), scale = p.a.scale * factor;
+        const uint64_t c2 = two(c, c), scale2 = two(scale, scale);
         uint32_t step = 0, held = 0;
         bool go = true;
         for (int it = 0; go; ++it) {
@@ -892,7 +912,7 @@ __global__ void __launch_bounds__(kGradThreads, 1)
             const RowMask mask(i < s.ql ? s.off + i : -1, p.a);
             float lse = inside ? p.a.lse[r] : INFINITY;
             lse = lse == -INFINITY ? INFINITY : lse * kLog2e;  // weights of a row that sees nothing are zero
-            const float delta = inside ? p.delta[r] * p.a.scale : 0.0f;
+            const float delta = inside ? p.delta[r] * scale : 0.0f;
             const uint64_t lse2 = two(-lse, -lse), delta2 = two(-delta, -delta);
             for (int j = 0; j < n; ++j, ++step) {
                 const uint32_t st = step & 1;
@@ -924,7 +944,7 @@ __global__ void __launch_bounds__(kGradThreads, 1)
 #pragma unroll
                     for (int y = 0; y < 32; ++y) {
                         const float e = seen >> y & 1 ? __uint_as_float(v[y]) : 0.0f;
-                        d[y] = __float_as_uint(e == 0.0f ? 0.0f : e * fmaf(__uint_as_float(d[y]), p.a.scale, -delta));
+                        d[y] = __float_as_uint(e == 0.0f ? 0.0f : e * fmaf(__uint_as_float(d[y]), scale, -delta));
                     }
                 }
 #pragma unroll
@@ -949,7 +969,7 @@ __global__ void __launch_bounds__(kGradThreads, 1)
                 T* out = static_cast<T*>(p.dq.data) + w.b * p.dq.batch_stride + i * p.dq.token_stride +
                          h * p.dq.head_stride;
                 if (n > 0)
-                    store_row<T, DP>(at_dq + lanes, out, inside, p.a.head_dim, 1.0f);
+                    store_row<T, DP>(at_dq + lanes, out, inside, p.a.head_dim, 1.0f / factor);
                 else if (inside)
                     zero_row(out, p.a.head_dim);
             }
@@ -1092,6 +1112,7 @@ __global__ void __launch_bounds__(StoredShape<DP>::kThreads, 1)
     } else if (warp >= 4) {
         const int row = (warp % 4) * 32 + lane;
         const uint32_t lanes = (uint32_t)(warp % 4 * 32) << 16;
+        const float f = 1.0f / ds_factor<T>(p);
         uint32_t held = 0;
         for (int it = 0;; ++it) {
             const int id = work.get_warp(it, gave_up);
@@ -1109,7 +1130,7 @@ __global__ void __launch_bounds__(StoredShape<DP>::kThreads, 1)
             if (!__all_sync(~0u, mbar_wait(done + 8 * half, held / 2 & 1, gave_up))) break;
             ++held;
             fence_after();
-            store_row<T, DP>(tmem + half * DP + lanes, out, inside, p.a.head_dim, 1.0f);
+            store_row<T, DP>(tmem + half * DP + lanes, out, inside, p.a.head_dim, f);
             fence_before();
             __syncwarp();
             if (lane == 0) mbar_arrive(freed + 8 * half);
@@ -1259,11 +1280,12 @@ __global__ void __launch_bounds__(kGradThreads, 1)
         }
         if (go) commit(bar.done);
     } else if (warp >= 2) {
-        await_previous();  // for delta; everything read before is the caller's
+        await_previous();  // for delta and the maxima; everything read before is the caller's
         const int side = (warp - 2) / 4, row = (warp % 4) * 32 + lane;  // which 32 of a tile's 128 queries
         const uint32_t lanes = (uint32_t)(warp % 4 * 32) << 16;
         const int key = k0 + row;
-        const uint64_t c2 = two(p.scale_log2, p.scale_log2), scale2 = two(p.a.scale, p.a.scale);
+        const float factor = ds_factor<T>(p), scale = p.a.scale * factor;
+        const uint64_t c2 = two(p.scale_log2, p.scale_log2), scale2 = two(scale, scale);
 
         // where dS goes, less the query tile's part: all of it is below 2^32 bytes
         const uint32_t ds_at = !p.ds ? 0
@@ -1284,7 +1306,7 @@ __global__ void __launch_bounds__(kGradThreads, 1)
                 const float l = live ? p.a.lse[r_row + i] : INFINITY;
                 stat_lse[to] = l == -INFINITY ? -INFINITY : -l * kLog2e;
             } else if (side == 1) {
-                stat_delta[to] = live ? -p.delta[r_row + i] * p.a.scale : 0.0f;
+                stat_delta[to] = live ? -p.delta[r_row + i] * scale : 0.0f;
             } else if (side == 2 && row == 0 && p.ds) {
                 stat_place[j % 3] = (uint32_t)ds_row(p, first + j) * kPlaceBytes;
             }
@@ -1391,17 +1413,18 @@ __global__ void __launch_bounds__(kGradThreads, 1)
             const bool is_dk = side & 1;
             const int d0 = side / 2 * (DP / 2), D = p.a.head_dim - d0;
             const uint32_t from = (is_dk ? at_dk : at_dv) + lanes + d0;
+            const float f = is_dk ? 1.0f / factor : 1.0f;
             const heddle_heads& t = is_dk ? p.dk : p.dv;
             T* out = static_cast<T*>(t.data) + b * t.batch_stride + key * t.token_stride + hk * t.head_stride + d0;
             const bool inside = key < p.a.kv_len;
             if (parts > 1) {
                 float* to = (is_dk ? p.part_dk : p.part_dv) + (slot * kTile + row) * p.a.head_dim + d0;
                 if (n > 0)
-                    store_floats<DP / 2>(from, to, true, D, 1.0f);
+                    store_floats<DP / 2>(from, to, true, D, f);
                 else
                     zero_row(to, min(D, DP / 2));
             } else if (n > 0) {
-                store_row<T, DP / 2>(from, out, inside, D, 1.0f);
+                store_row<T, DP / 2>(from, out, inside, D, f);
             } else if (inside) {
                 zero_row(out, min(D, DP / 2));
             }

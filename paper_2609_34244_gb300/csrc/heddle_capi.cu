@@ -500,8 +500,8 @@ heddle_status heddle_create(heddle_ctx** out, int32_t device) {
     if (e == cudaSuccess) e = cudaMalloc(&x->d_meet, meet);
     if (e == cudaSuccess) e = cudaMemset(x->d_meet, 0, meet);
 
-    if (e == cudaSuccess) e = cudaMalloc(&x->op.sched, 2 * sizeof(int32_t));
-    if (e == cudaSuccess) e = cudaMemset(x->op.sched, 0, 2 * sizeof(int32_t));
+    if (e == cudaSuccess) e = cudaMalloc(&x->op.sched, hd::kSched * sizeof(int32_t));
+    if (e == cudaSuccess) e = cudaMemset(x->op.sched, 0, hd::kSched * sizeof(int32_t));
     if (e == cudaSuccess) e = cudaEventCreateWithFlags(&x->op.last, cudaEventDisableTiming);
     x->op.device = device;
     x->op.num_sms = x->num_sms;

@@ -21,6 +21,8 @@ namespace hd {
 constexpr uint32_t kErrOpWait = 16u;      // a wait inside an operator ran out
 constexpr uint32_t kErrOpPosition = 32u;  // a position outside its rotation table
 
+constexpr int kSched = 4;
+
 struct DeviceMemory {
     static void* allocate(size_t size) {
         // allowed during a capture, and no part of the graph
@@ -41,7 +43,9 @@ struct OpContext {
     int device = 0;
     int num_sms = 0;
     uint32_t* err = nullptr;  // device error flags
-    int32_t* sched = nullptr;  // two counters of kernels that hand out work, zero between launches
+    // two counters of kernels that hand out work, zero between launches, and two
+    // maxima as floats' bits (attention's gradients)
+    int32_t* sched = nullptr;
     Scratch<DeviceMemory> scratch;
     Refusal refusal;  // of scratch that a call can do without
     // the end of the last call that took scratch, on the stream of that id; none in graphs

@@ -387,3 +387,60 @@ def test_contractions_that_take_seconds(lib, m, n, k):
     assert want.abs().max().item() < 2 ** 24
     assert torch.equal(pre.double(), want) and torch.equal(y, want.to(dt))
     assert h.heddle_device_errors(ctx) == 0
+
+
+@pytest.mark.parametrize("b,t,hq,hk,d,kind", [(1, 2000, 2, 1, 64, None), (2, 600, 4, 2, 128, "both"),
+                                              (80, 440, 128, 1, 64, "both")])
+@pytest.mark.parametrize("power", [12, 16])
+def test_small_gradients_in_float16(lib, b, t, hq, hk, d, kind, power):
+    """Gradients are linear in the outputs': small ones have the bounds of
+    2^power times larger ones, at that scale, and their results' own rounding."""
+    h, ctx = lib
+    g, dt = gen(t + power), torch.float16
+    q, k, v = rand(g, b, t, hq, d, dt=dt), rand(g, b, t, hk, d, dt=dt), rand(g, b, t, hk, d, dt=dt)
+    do = rand(g, b, t, hq, d, dt=dt, std=2.0 ** -power)
+    lens = [torch.tensor([t - 7 * i % 50 for i in range(b)], dtype=torch.int32, device="cuda") for _ in range(2)]
+    ql, kl = lens if kind else (None, None)
+    if kind:  # what lies past a sequence gives no range
+        for i in range(b):
+            do[i, int(ql[i]):], v[i, int(kl[i]):] = 60000.0, 60000.0
+    o, lse = torch.empty_like(q), torch.empty(b, hq, t, device="cuda")
+    h.heddle_attention(ctx, q, k, v, o, lse, q_lens=ql, kv_lens=kl)
+    dq, dk, dv = (torch.full_like(x, CANARY) for x in (q, k, v))
+    h.heddle_attention_backward(ctx, do, q, k, v, o, lse, dq, dk, dv, q_lens=ql, kv_lens=kl)
+    n, small = hq // hk, 2.0 ** -power
+    for i in sorted({0, b - 1}):
+        nq, nk = (t, t) if ql is None else (int(ql[i]), int(kl[i]))
+        for kv in range(hk):
+            sums = {x: [torch.zeros(t, d, dtype=torch.float64, device="cuda") for _ in range(2)] for x in ("dk", "dv")}
+            for j in range(kv * n, kv * n + n):
+                large = do[i, :, j].double() / small
+                w = R.attention(q[i, :, j], k[i, :, kv], v[i, :, kv], nq, nk, 0, 0, d ** -0.5, large)
+                R.close(dq[i, :, j], w["dq"][0] * small, w["dq"][1] * small, "dq")
+                for x in sums:
+                    sums[x][0] += w[x][0] * small
+                    sums[x][1] += (w[x][1] + n * 2.0 ** -23 * w[x][0].abs()) * small
+            R.close(dk[i, :, kv], *sums["dk"], "dk")
+            R.close(dv[i, :, kv], *sums["dv"], "dv")
+
+
+def test_scores_gradients_beyond_float16_with_small_keys(lib):
+    """Scores' gradients past 65504 whose products with small keys and queries
+    are finite."""
+    h, ctx = lib
+    g, dt, t, d = gen(5), torch.float16, 24, 64
+    q, k = (rand(g, 1, t, 1, d, dt=dt, std=0.002) for _ in range(2))
+    v = rand(g, 1, t, 1, d, dt=dt, std=60.0)
+    do = (torch.randn(1, t, 1, d, generator=g, device="cuda") * 6000).clamp(-20000, 20000).to(dt)
+    o, lse = torch.empty_like(q), torch.empty(1, 1, t, device="cuda")
+    h.heddle_attention(ctx, q, k, v, o, lse)
+    dq, dk, dv = (torch.full_like(x, CANARY) for x in (q, k, v))
+    h.heddle_attention_backward(ctx, do, q, k, v, o, lse, dq, dk, dv)
+    w = R.attention(q[0, :, 0], k[0, :, 0], v[0, :, 0], t, t, 0, 0, d ** -0.5, do[0, :, 0])
+    s = (q[0, :, 0].double() @ k[0, :, 0].double().T * d ** -0.5).masked_fill(
+        ~R.visible(t, t, t, t, 0, 0, "cuda"), -math.inf)
+    p, dp = s.softmax(1), do[0, :, 0].double() @ v[0, :, 0].double().T
+    assert (p * (dp - (p * dp).sum(1, keepdim=True))).abs().max().item() * d ** -0.5 > 65504
+    assert all(w[x][0].abs().max().item() < 60000 for x in ("dq", "dk", "dv"))
+    for got, x in ((dq, "dq"), (dk, "dk"), (dv, "dv")):
+        R.close(got[0, :, 0], *w[x], x)
