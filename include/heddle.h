@@ -648,7 +648,8 @@ heddle_status heddle_gated_ffn(heddle_ctx* ctx, const heddle_gated_ffn_args* arg
  * du = dy act(gate),  dx = dg w_gate + du w_up,  dw_gate = dg^T x,
  * dw_up = du^T x.  dx is nullable, dw_gate and dw_up are together; x is read
  * for the weights' gradients, the weights for dx.  dg and du are rounded to
- * the element type for the products. */
+ * the element type for the products: in float16 one past 65504 is infinite, and
+ * one below 6e-5 loses digits. */
 typedef struct {
     int64_t m, n, k;
     int32_t dtype, act;
