@@ -734,8 +734,8 @@ heddle_status heddle_qk_norm_rope_backward(heddle_ctx* ctx, const heddle_qk_norm
  * past a sequence's queries, get o = 0 and lse = -infinity.  Keys and values
  * past kv_lens are not used, whatever they hold; those within must be
  * finite.  A query with a score of NaN or +infinity gets NaN, scores of
- * -infinity weigh nothing.  P is rounded to the element type for its product with v, its sum
- * is not.  One query against many keys is split along the keys.
+ * -infinity weigh nothing.  P is rounded to the element type for its product
+ * with v, its sum is not.  One query against many keys is split along the keys.
  * dtype BF16 or FP16; 1 <= head_dim <= 256; kv_heads divides q_heads;
  * batch * q_heads * q_len and batch * kv_heads * kv_len below 2^31. */
 typedef struct {
@@ -754,9 +754,9 @@ heddle_status heddle_attention(heddle_ctx* ctx, const heddle_attention_args* arg
 /* Gradients of heddle_attention: fwd as in the forward call with its o and
  * lse (both required, read), d_o = dL/do.  dq, dk, dv are all written (the
  * shared heads' sums included; zeros where a row sees nothing or is past its
- * sequence).  Sums run in a fixed order; the scores' gradients are
- * rounded to the element type for their products, in float16 at a power of two
- * that the largest rows of d_o and v give, so that none overflows and small ones
+ * sequence).  Sums run in a fixed order; the scores' gradients are rounded to
+ * the element type for their products, in float16 at a power of two that the
+ * largest rows of d_o and v give, so that none overflows and small ones
  * keep their digits.  Keeps them in the context's scratch between its passes, 2
  * bytes a visible pair and query head in tiles of 128 x 128, as many key heads
  * at a time as 4 GiB hold; longer sequences, and a device without that room,
