@@ -454,7 +454,7 @@ heddle_status heddle_get_tables(heddle_ctx* ctx, int64_t* q, int64_t* p2p);
  * consistency check failed, bit 3 (bounds-checked builds only) an index
  * test failed and the access was skipped, bit 4 a wait inside a layer
  * operator ran out (its outputs are not valid), bit 5 a position outside its
- * rotation table.  0 in normal operation. */
+ * rotation table, bit 6 a token past the vocabulary.  0 in normal operation. */
 heddle_status heddle_device_errors(heddle_ctx* ctx, uint32_t* flags);
 
 /* PartitionLayers search.  AUTO (default) uses the equal-layer closed form
@@ -767,6 +767,164 @@ typedef struct {
     heddle_heads d_o, dq, dk, dv;
 } heddle_attention_grad_args;
 heddle_status heddle_attention_backward(heddle_ctx* ctx, const heddle_attention_grad_args* args, void* stream);
+
+/* ------------------------------------- the hidden state between the products
+ *
+ * Element types of these four operators: HEDDLE_BF16, HEDDLE_FP16, HEDDLE_FP32. */
+
+/* Layer norm of every row of x ([rows][cols]):
+ *   mean = sum x / cols,  rstd = 1 / sqrt(sum (x - mean)^2 / cols + eps),
+ *   y = (x - mean) rstd weight + bias
+ * weight, bias: [cols], of the same type, each nullable (1 and 0).  mean, rstd
+ * (float [rows], nullable together): receive the statistics for the backward
+ * pass.  Deviations from the mean are squared, not values: a large mean costs
+ * no digits.  y may be x itself (same stride).  A row with a value that is not
+ * finite gets NaN. */
+typedef struct {
+    int64_t rows, cols;
+    int32_t dtype;
+    float eps;
+    const void* x;
+    int64_t ldx;
+    const void* weight;
+    const void* bias;
+    void* y;
+    int64_t ldy;
+    float* mean;
+    float* rstd;
+} heddle_layer_norm_args;
+heddle_status heddle_layer_norm(heddle_ctx* ctx, const heddle_layer_norm_args* args, void* stream);
+
+/* Gradients of heddle_layer_norm from dy, with its x, mean and rstd: with
+ * n = (x - mean) rstd and t = dy weight,
+ *   dx = rstd (t - sum t / cols - n sum(t n) / cols) + dres
+ *   dw = sum over rows of dy n,  dbias = sum over rows of dy  (float [cols])
+ * dres (nullable): the gradient that reaches x along the residual path, added
+ * before dx is rounded.  dx, dw and dbias are each nullable: not computed.
+ * dx may be dy or dres itself (same stride).  The sums over rows run in a
+ * fixed order. */
+typedef struct {
+    int64_t rows, cols;
+    int32_t dtype, reserved;
+    const void* dy;
+    int64_t lddy;
+    const void* x;
+    int64_t ldx;
+    const void* weight;
+    const float* mean;
+    const float* rstd;
+    const void* dres;
+    int64_t ldr;
+    void* dx;
+    int64_t lddx;
+    float* dw;
+    float* dbias;
+} heddle_layer_norm_grad_args;
+heddle_status heddle_layer_norm_backward(heddle_ctx* ctx, const heddle_layer_norm_grad_args* args, void* stream);
+
+/* Dropout, its result added to the residual stream:
+ *   y = (u < D ? 0 : x s) + residual,  D = p 2^32 rounded,  s = 2^32 / (2^32 - D)
+ * The number u of element i = row * cols + col (whatever the strides) is word
+ * i % 4 of Philox4x32-10 with the key `seed` (low word first) and the counter
+ * (i / 4, offset + *step), 64 bits each, low words first: the mask is never
+ * stored, and the same seed, offset and sizes give it again.  step (nullable
+ * device int64 [1]) is read when the call runs, so that the replays of a graph
+ * can differ.  0 <= p < 1; with p = 0 nothing is dropped.  A dropped value
+ * counts for nothing, whatever it is.  residual: nullable.  y may be x or
+ * residual itself (same stride). */
+typedef struct {
+    int64_t rows, cols;
+    int32_t dtype, reserved;
+    double p;
+    uint64_t seed, offset;
+    const int64_t* step;
+    const void* x;
+    int64_t ldx;
+    const void* residual;
+    int64_t ldr;
+    void* y;
+    int64_t ldy;
+} heddle_dropout_args;
+heddle_status heddle_dropout(heddle_ctx* ctx, const heddle_dropout_args* args, void* stream);
+
+/* The gradient of heddle_dropout's x from y's (the residual's is y's own): x
+ * holds dy and y receives dx = (u < D ? 0 : dy s), with p, seed, offset and
+ * step (its value at that call) as in the forward call; residual is null. */
+heddle_status heddle_dropout_backward(heddle_ctx* ctx, const heddle_dropout_args* args, void* stream);
+
+/* Embedding: row t of y ([tokens][cols]) is scale times the row of token t in
+ * a table of the tokens first .. first + table_rows - 1: the whole vocabulary,
+ * or one shard of it.  Tokens of other shards and negative ones (padding) give
+ * rows of zeros, so that the shards' results add up.  vocab: the vocabulary's
+ * size (at least first + table_rows); a token that is not below it raises
+ * bit 6 of heddle_device_errors and gives zeros.  token: [tokens], int32, or
+ * int64 with wide_tokens.  */
+typedef struct {
+    int64_t tokens, cols, table_rows, first, vocab;
+    int32_t dtype, wide_tokens;
+    float scale;
+    int32_t reserved;
+    const void* token;
+    const void* table;
+    int64_t ldt;
+    void* y;
+    int64_t ldy;
+} heddle_embedding_args;
+heddle_status heddle_embedding(heddle_ctx* ctx, const heddle_embedding_args* args, void* stream);
+
+/* The gradient of heddle_embedding's table: fwd as in the forward call, except
+ * that y holds the gradient of the output and table and ldt are those of the
+ * gradient, which is written:
+ *   dtable[v] = scale * (sum of dy[t] over the t whose token is first + v)
+ * in full, or, with `accumulate`, added to what it holds (rows without tokens
+ * are then not touched).  grad_dtype: the gradient's type, dtype or
+ * HEDDLE_FP32.  Tokens are sorted and each row's terms are added in an order
+ * that the tokens alone fix, in 32 bits; one rounding at the end. */
+typedef struct {
+    heddle_embedding_args fwd;
+    int32_t grad_dtype, accumulate;
+} heddle_embedding_grad_args;
+heddle_status heddle_embedding_backward(heddle_ctx* ctx, const heddle_embedding_grad_args* args, void* stream);
+
+/* Router of an expert layer: of every token's logits ([tokens][experts])
+ *   p = softmax(logits);  expert[t][j], j < top_k: the experts of the largest
+ *   logits, largest first, equal ones by index;  weight[t][j] = p of it, with
+ *   `normalize` over the sum of the token's chosen ones (float)
+ *   count[e]: choices of expert e,  count[experts] = n: the tokens that chose
+ *   loss = experts * sum over e of count[e] / (top_k n) * (sum over t of p[t][e]) / n
+ * loss: float [1], nullable.  valid: uint8 [tokens], nullable; a token whose
+ * entry is 0 (padding) takes no part: expert -1, weight 0.  The same holds for
+ * a token whose logits are all -infinity; an expert of logit -infinity is not
+ * chosen (expert -1, weight 0 where fewer than top_k are left).  A token with a
+ * logit of NaN or +infinity counts in n, has expert -1 and weight NaN, and the
+ * loss is NaN.  Sums run in a fixed order.
+ * experts <= 1024, top_k <= 32 and at most experts. */
+typedef struct {
+    int64_t tokens;
+    int32_t experts, top_k, dtype, normalize;
+    const void* logits;
+    int64_t ldl;
+    const uint8_t* valid;
+    int32_t* expert;
+    float* weight;
+    int32_t* count;
+    float* loss;
+} heddle_router_args;
+heddle_status heddle_router(heddle_ctx* ctx, const heddle_router_args* args, void* stream);
+
+/* The gradient of heddle_router's logits: fwd as in the forward call with its
+ * expert, weight and count (read; loss is not).  d_weight (float
+ * [tokens][top_k]) and d_loss (device float [1]): gradients of the weights and
+ * of the loss, each nullable (zeros).  The counts have no gradient.  dlogits:
+ * rows of zeros for tokens that took no part; may be the logits themselves. */
+typedef struct {
+    heddle_router_args fwd;
+    const float* d_weight;
+    const float* d_loss;
+    void* dlogits;
+    int64_t ldd;
+} heddle_router_grad_args;
+heddle_status heddle_router_backward(heddle_ctx* ctx, const heddle_router_grad_args* args, void* stream);
 
 #ifdef __cplusplus
 }

@@ -186,6 +186,57 @@ heddle_status check_attention(OpContext* x, const heddle_attention_args& a, bool
     return HEDDLE_OK;
 }
 
+// Sizes and types of the hidden state's operators.
+heddle_status check_rows(OpContext* x, int64_t rows, int64_t cols, int32_t dtype) {
+    REQUIRE(rows >= 0 && cols >= 0, HEDDLE_E_ARG, "negative size");
+    REQUIRE(rows <= kMaxSize && cols <= kMaxSize, HEDDLE_E_LIMIT, "a size exceeds 2^31 - 1");
+    REQUIRE(dtype >= HEDDLE_BF16 && dtype <= HEDDLE_FP32, HEDDLE_E_ARG, "unknown dtype %d", dtype);
+    return HEDDLE_OK;
+}
+
+heddle_status check_dropout(OpContext* x, const heddle_dropout_args& a) {
+    CHECK(check_rows(x, a.rows, a.cols, a.dtype));
+    REQUIRE(a.p >= 0.0 && a.p < 1.0, HEDDLE_E_ARG, "p %g: at least 0 and below 1", a.p);
+    const int size = elem_size(a.dtype);
+    CHECK(check_matrix(x, "x", a.x, a.ldx, a.rows, a.cols, size));
+    CHECK(check_matrix(x, "y", a.y, a.ldy, a.rows, a.cols, size));
+    if (a.residual) CHECK(check_matrix(x, "residual", a.residual, a.ldr, a.rows, a.cols, size));
+    REQUIRE(aligned_to(a.step, 8), HEDDLE_E_ARG, "step is not aligned");
+    return HEDDLE_OK;
+}
+
+// table_type: the element type of the table, or of its gradient
+heddle_status check_embedding(OpContext* x, const heddle_embedding_args& a, int32_t table_type) {
+    CHECK(check_rows(x, a.tokens, a.cols, a.dtype));
+    REQUIRE(a.cols <= (int64_t)1 << 22, HEDDLE_E_LIMIT, "a row of more than 2^22 values");
+    REQUIRE(a.table_rows >= 0 && a.first >= 0, HEDDLE_E_ARG, "negative size");
+    REQUIRE(a.table_rows <= kMaxSize, HEDDLE_E_LIMIT, "a size exceeds 2^31 - 1");
+    REQUIRE(a.first <= INT64_MAX - a.table_rows && a.vocab >= a.first + a.table_rows, HEDDLE_E_ARG,
+            "a vocabulary of %lld, and rows from %lld on: %lld", (long long)a.vocab, (long long)a.first,
+            (long long)a.table_rows);
+    REQUIRE(isfinite(a.scale), HEDDLE_E_ARG, "scale is not finite");
+    const int size = elem_size(a.dtype);
+    CHECK(check_matrix(x, "table", a.table, a.ldt, a.table_rows, a.cols, elem_size(table_type)));
+    CHECK(check_matrix(x, "y", a.y, a.ldy, a.tokens, a.cols, size));
+    REQUIRE(a.tokens == 0 || a.cols == 0 || a.token, HEDDLE_E_ARG, "token is null");
+    REQUIRE(aligned_to(a.token, a.wide_tokens ? 8 : 4), HEDDLE_E_ARG, "token is not aligned");
+    return HEDDLE_OK;
+}
+
+heddle_status check_router(OpContext* x, const heddle_router_args& a) {
+    CHECK(check_rows(x, a.tokens, a.experts, a.dtype));
+    REQUIRE(a.experts >= 1 && a.top_k >= 1 && a.top_k <= a.experts, HEDDLE_E_ARG, "%d of %d experts", a.top_k,
+            a.experts);
+    REQUIRE(a.experts <= 1024 && a.top_k <= 32, HEDDLE_E_LIMIT, "%d of %d experts: 32 of 1024 at most", a.top_k,
+            a.experts);
+    CHECK(check_matrix(x, "logits", a.logits, a.ldl, a.tokens, a.experts, elem_size(a.dtype)));
+    REQUIRE(a.tokens == 0 || (a.expert && a.weight), HEDDLE_E_ARG, "expert or weight is null");
+    REQUIRE(a.count, HEDDLE_E_ARG, "count is null");
+    REQUIRE(aligned_to(a.expert, 4) && aligned_to(a.weight, 4) && aligned_to(a.count, 4) && aligned_to(a.loss, 4),
+            HEDDLE_E_ARG, "expert, weight, count or loss is not aligned");
+    return HEDDLE_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -435,6 +486,123 @@ heddle_status heddle_attention_backward(heddle_ctx* ctx, const heddle_attention_
     CHECK(reserve(x, keep ? most : least, st));
     return done(x, hd::launch_attention_grad(*x, *args, x->scratch.get(), keep, st),
                 "heddle_attention_backward", st);
+}
+
+heddle_status heddle_layer_norm(heddle_ctx* ctx, const heddle_layer_norm_args* args, void* stream) {
+    if (!ctx) return HEDDLE_E_ARG;
+    OpContext* x = heddle_op_context(ctx);
+    REQUIRE(args, HEDDLE_E_ARG, "args is null");
+    const heddle_layer_norm_args& a = *args;
+    CHECK(check_rows(x, a.rows, a.cols, a.dtype));
+    REQUIRE(a.eps >= 0.0f && isfinite(a.eps), HEDDLE_E_ARG, "eps is negative or not finite");
+    const int size = elem_size(a.dtype);
+    CHECK(check_matrix(x, "x", a.x, a.ldx, a.rows, a.cols, size));
+    CHECK(check_matrix(x, "y", a.y, a.ldy, a.rows, a.cols, size));
+    REQUIRE(aligned_to(a.weight, size) && aligned_to(a.bias, size), HEDDLE_E_ARG,
+            "weight or bias is not aligned to its element");
+    REQUIRE(!a.mean == !a.rstd, HEDDLE_E_ARG, "mean and rstd are given together");
+    REQUIRE(aligned_to(a.mean, 4) && aligned_to(a.rstd, 4), HEDDLE_E_ARG, "mean or rstd is not aligned");
+    if (a.rows == 0 || a.cols == 0) return nothing(x);
+    OpDeviceGuard guard(x);
+    cudaStream_t st = (cudaStream_t)stream;
+    return done(x, hd::launch_layer_norm(*x, a, st), "heddle_layer_norm", st);
+}
+
+heddle_status heddle_layer_norm_backward(heddle_ctx* ctx, const heddle_layer_norm_grad_args* args, void* stream) {
+    if (!ctx) return HEDDLE_E_ARG;
+    OpContext* x = heddle_op_context(ctx);
+    REQUIRE(args, HEDDLE_E_ARG, "args is null");
+    const heddle_layer_norm_grad_args& a = *args;
+    CHECK(check_rows(x, a.rows, a.cols, a.dtype));
+    const int size = elem_size(a.dtype);
+    CHECK(check_matrix(x, "dy", a.dy, a.lddy, a.rows, a.cols, size));
+    CHECK(check_matrix(x, "x", a.x, a.ldx, a.rows, a.cols, size));
+    if (a.dx) CHECK(check_matrix(x, "dx", a.dx, a.lddx, a.rows, a.cols, size));
+    if (a.dres) CHECK(check_matrix(x, "dres", a.dres, a.ldr, a.rows, a.cols, size));
+    REQUIRE(aligned_to(a.weight, size), HEDDLE_E_ARG, "weight is not aligned to its element");
+    REQUIRE(a.rows == 0 || a.cols == 0 || (a.mean && a.rstd), HEDDLE_E_ARG, "mean or rstd is null");
+    REQUIRE(aligned_to(a.mean, 4) && aligned_to(a.rstd, 4) && aligned_to(a.dw, 4) && aligned_to(a.dbias, 4),
+            HEDDLE_E_ARG, "mean, rstd, dw or dbias is not aligned");
+    if (a.cols == 0 || (!a.dw && !a.dbias && (!a.dx || a.rows == 0))) return nothing(x);
+    OpDeviceGuard guard(x);
+    cudaStream_t st = (cudaStream_t)stream;
+    CHECK(reserve(x, hd::layer_norm_grad_scratch(*x, a), st));
+    return done(x, hd::launch_layer_norm_grad(*x, a, x->scratch.get(), st), "heddle_layer_norm_backward", st);
+}
+
+heddle_status heddle_dropout(heddle_ctx* ctx, const heddle_dropout_args* args, void* stream) {
+    if (!ctx) return HEDDLE_E_ARG;
+    OpContext* x = heddle_op_context(ctx);
+    REQUIRE(args, HEDDLE_E_ARG, "args is null");
+    CHECK(check_dropout(x, *args));
+    if (args->rows == 0 || args->cols == 0) return nothing(x);
+    OpDeviceGuard guard(x);
+    cudaStream_t st = (cudaStream_t)stream;
+    return done(x, hd::launch_dropout(*x, *args, st), "heddle_dropout", st);
+}
+
+heddle_status heddle_dropout_backward(heddle_ctx* ctx, const heddle_dropout_args* args, void* stream) {
+    if (!ctx) return HEDDLE_E_ARG;
+    OpContext* x = heddle_op_context(ctx);
+    REQUIRE(args, HEDDLE_E_ARG, "args is null");
+    REQUIRE(!args->residual, HEDDLE_E_ARG, "the gradient takes no residual");
+    CHECK(check_dropout(x, *args));
+    if (args->rows == 0 || args->cols == 0) return nothing(x);
+    OpDeviceGuard guard(x);
+    cudaStream_t st = (cudaStream_t)stream;
+    return done(x, hd::launch_dropout(*x, *args, st), "heddle_dropout_backward", st);
+}
+
+heddle_status heddle_embedding(heddle_ctx* ctx, const heddle_embedding_args* args, void* stream) {
+    if (!ctx) return HEDDLE_E_ARG;
+    OpContext* x = heddle_op_context(ctx);
+    REQUIRE(args, HEDDLE_E_ARG, "args is null");
+    CHECK(check_embedding(x, *args, args->dtype));
+    if (args->tokens == 0 || args->cols == 0) return nothing(x);
+    OpDeviceGuard guard(x);
+    cudaStream_t st = (cudaStream_t)stream;
+    return done(x, hd::launch_embedding(*x, *args, st), "heddle_embedding", st);
+}
+
+heddle_status heddle_embedding_backward(heddle_ctx* ctx, const heddle_embedding_grad_args* args, void* stream) {
+    if (!ctx) return HEDDLE_E_ARG;
+    OpContext* x = heddle_op_context(ctx);
+    REQUIRE(args, HEDDLE_E_ARG, "args is null");
+    const heddle_embedding_args& a = args->fwd;
+    REQUIRE(args->grad_dtype == a.dtype || args->grad_dtype == HEDDLE_FP32, HEDDLE_E_ARG,
+            "grad_dtype %d: the element type or FP32", args->grad_dtype);
+    CHECK(check_embedding(x, a, args->grad_dtype));
+    if (a.table_rows == 0 || a.cols == 0 || (a.tokens == 0 && args->accumulate)) return nothing(x);
+    OpDeviceGuard guard(x);
+    cudaStream_t st = (cudaStream_t)stream;
+    CHECK(reserve(x, hd::embedding_grad_scratch(*x, *args), st));
+    return done(x, hd::launch_embedding_grad(*x, *args, x->scratch.get(), st), "heddle_embedding_backward", st);
+}
+
+heddle_status heddle_router(heddle_ctx* ctx, const heddle_router_args* args, void* stream) {
+    if (!ctx) return HEDDLE_E_ARG;
+    OpContext* x = heddle_op_context(ctx);
+    REQUIRE(args, HEDDLE_E_ARG, "args is null");
+    CHECK(check_router(x, *args));
+    OpDeviceGuard guard(x);
+    cudaStream_t st = (cudaStream_t)stream;
+    CHECK(reserve(x, hd::router_scratch(*x, *args), st));
+    return done(x, hd::launch_router(*x, *args, x->scratch.get(), st), "heddle_router", st);
+}
+
+heddle_status heddle_router_backward(heddle_ctx* ctx, const heddle_router_grad_args* args, void* stream) {
+    if (!ctx) return HEDDLE_E_ARG;
+    OpContext* x = heddle_op_context(ctx);
+    REQUIRE(args, HEDDLE_E_ARG, "args is null");
+    const heddle_router_args& a = args->fwd;
+    CHECK(check_router(x, a));
+    CHECK(check_matrix(x, "dlogits", args->dlogits, args->ldd, a.tokens, a.experts, elem_size(a.dtype)));
+    REQUIRE(aligned_to(args->d_weight, 4) && aligned_to(args->d_loss, 4), HEDDLE_E_ARG,
+            "d_weight or d_loss is not aligned");
+    if (a.tokens == 0) return nothing(x);
+    OpDeviceGuard guard(x);
+    cudaStream_t st = (cudaStream_t)stream;
+    return done(x, hd::launch_router_grad(*x, *args, st), "heddle_router_backward", st);
 }
 
 }  // extern "C"

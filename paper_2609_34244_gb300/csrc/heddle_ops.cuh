@@ -20,6 +20,7 @@ namespace hd {
 // Device error flags of the operators (heddle_device_errors).
 constexpr uint32_t kErrOpWait = 16u;      // a wait inside an operator ran out
 constexpr uint32_t kErrOpPosition = 32u;  // a position outside its rotation table
+constexpr uint32_t kErrOpToken = 64u;     // a token past the vocabulary
 
 constexpr int kSched = 4;
 
@@ -79,7 +80,7 @@ cudaError_t launch(const OpContext& x, void (*kernel)(P...), dim3 grid, int bloc
     return cudaLaunchKernelEx(&cfg, kernel, std::forward<A>(args)...);
 }
 
-inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+__host__ __device__ inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 inline size_t align256(size_t v) { return (v + 255) & ~(size_t)255; }
 
 template <class T>
@@ -202,6 +203,24 @@ cudaError_t launch_attention(const OpContext& x, const heddle_attention_args& a,
 size_t attention_grad_scratch(const OpContext& x, const heddle_attention_grad_args& a, bool keep);
 cudaError_t launch_attention_grad(const OpContext& x, const heddle_attention_grad_args& a, unsigned char* ws, bool keep,
                                   cudaStream_t st);
+
+// ------------------------------------ the hidden state between the products
+
+cudaError_t launch_layer_norm(const OpContext& x, const heddle_layer_norm_args& a, cudaStream_t st);
+size_t layer_norm_grad_scratch(const OpContext& x, const heddle_layer_norm_grad_args& a);
+cudaError_t launch_layer_norm_grad(const OpContext& x, const heddle_layer_norm_grad_args& a, unsigned char* ws,
+                                   cudaStream_t st);
+
+cudaError_t launch_dropout(const OpContext& x, const heddle_dropout_args& a, cudaStream_t st);
+
+cudaError_t launch_embedding(const OpContext& x, const heddle_embedding_args& a, cudaStream_t st);
+size_t embedding_grad_scratch(const OpContext& x, const heddle_embedding_grad_args& g);
+cudaError_t launch_embedding_grad(const OpContext& x, const heddle_embedding_grad_args& g, unsigned char* ws,
+                                  cudaStream_t st);
+
+size_t router_scratch(const OpContext& x, const heddle_router_args& a);
+cudaError_t launch_router(const OpContext& x, const heddle_router_args& a, unsigned char* ws, cudaStream_t st);
+cudaError_t launch_router_grad(const OpContext& x, const heddle_router_grad_args& g, cudaStream_t st);
 
 }  // namespace hd
 

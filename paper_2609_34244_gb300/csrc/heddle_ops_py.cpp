@@ -27,11 +27,18 @@ struct PythonError {};  // one is set
 
 PyObject *error_class = nullptr, *current_stream = nullptr;  // HeddleError; device index -> address
 PyObject *name_value = nullptr, *name_stream = nullptr;
-enum Entry { kLinear, kLinearGrad, kFfn, kFfnGrad, kNorm, kNormGrad, kAttention, kAttentionGrad, kEntries };
+enum Entry {
+    kLinear, kLinearGrad, kFfn, kFfnGrad, kNorm, kNormGrad, kAttention, kAttentionGrad, kLayerNorm, kLayerNormGrad,
+    kDropout, kDropoutGrad, kEmbedding, kEmbeddingGrad, kRouter, kRouterGrad, kEntries
+};
 const char* const kNames[kEntries] = {"heddle_linear",       "heddle_linear_backward",
                                       "heddle_gated_ffn",    "heddle_gated_ffn_backward",
                                       "heddle_qk_norm_rope", "heddle_qk_norm_rope_backward",
-                                      "heddle_attention",    "heddle_attention_backward"};
+                                      "heddle_attention",    "heddle_attention_backward",
+                                      "heddle_layer_norm",   "heddle_layer_norm_backward",
+                                      "heddle_dropout",      "heddle_dropout_backward",
+                                      "heddle_embedding",    "heddle_embedding_backward",
+                                      "heddle_router",       "heddle_router_backward"};
 void* functions[kEntries];
 int32_t (*device_of)(const heddle_ctx*) = nullptr;
 
@@ -139,10 +146,16 @@ int32_t integer32(PyObject* o) {
     }
     return (int32_t)v;
 }
-float real(PyObject* o) {
+double real64(PyObject* o) {
     const double v = PyFloat_AsDouble(o);
     if (v == -1.0 && PyErr_Occurred()) throw PythonError();
-    return (float)v;
+    return v;
+}
+float real(PyObject* o) { return (float)real64(o); }
+uint64_t natural(PyObject* o) {
+    const unsigned long long v = PyLong_AsUnsignedLongLong(o);
+    if (v == (unsigned long long)-1 && PyErr_Occurred()) throw PythonError();
+    return v;
 }
 bool truth(PyObject* o) {
     const int v = PyObject_IsTrue(o);
@@ -390,6 +403,146 @@ PyObject* attention_backward(PyObject*, PyObject* const* v, Py_ssize_t count) {
     });
 }
 
+// (ctx, x, weight, bias, y, mean, rstd, eps, stream)
+PyObject* layer_norm(PyObject*, PyObject* const* v, Py_ssize_t count) {
+    return guarded<9>(count, [&] {
+        const First x("x", v[1], 2);
+        heddle_layer_norm_args a{};
+        a.rows = x[0], a.cols = x[1], a.dtype = x.code, a.eps = real(v[7]);
+        const Mat mx("x", v[1], a.rows, a.cols, x.type, x.device), y("y", v[4], a.rows, a.cols, x.type, x.device);
+        a.x = mx.p, a.ldx = mx.ld, a.y = y.p, a.ldy = y.ld;
+        a.weight = vec("weight", v[2], a.cols, x.type, x.device);
+        a.bias = vec("bias", v[3], a.cols, x.type, x.device);
+        a.mean = static_cast<float*>(vec("mean", v[5], a.rows, at::kFloat, x.device));
+        a.rstd = static_cast<float*>(vec("rstd", v[6], a.rows, at::kFloat, x.device));
+        return call(kLayerNorm, v[0], a, x.device, v[8]);
+    });
+}
+
+// (ctx, dy, x, weight, mean, rstd, dx, dw, dbias, dres, stream)
+PyObject* layer_norm_backward(PyObject*, PyObject* const* v, Py_ssize_t count) {
+    return guarded<11>(count, [&] {
+        const First x("x", v[2], 2);
+        heddle_layer_norm_grad_args a{};
+        a.rows = x[0], a.cols = x[1], a.dtype = x.code;
+        const Mat dy("dy", v[1], a.rows, a.cols, x.type, x.device), mx("x", v[2], a.rows, a.cols, x.type, x.device),
+            dx("dx", v[6], a.rows, a.cols, x.type, x.device), dres("dres", v[9], a.rows, a.cols, x.type, x.device);
+        a.dy = dy.p, a.lddy = dy.ld, a.x = mx.p, a.ldx = mx.ld, a.dx = dx.p, a.lddx = dx.ld;
+        a.dres = dres.p, a.ldr = dres.ld;
+        a.weight = vec("weight", v[3], a.cols, x.type, x.device);
+        a.mean = static_cast<float*>(vec("mean", v[4], a.rows, at::kFloat, x.device));
+        a.rstd = static_cast<float*>(vec("rstd", v[5], a.rows, at::kFloat, x.device));
+        a.dw = static_cast<float*>(vec("dw", v[7], a.cols, at::kFloat, x.device));
+        a.dbias = static_cast<float*>(vec("dbias", v[8], a.cols, at::kFloat, x.device));
+        return call(kLayerNormGrad, v[0], a, x.device, v[10]);
+    });
+}
+
+// v: x, y, p, seed, offset, step, and the residual or null
+PyObject* dropout_call(Entry entry, PyObject* ctx, PyObject* const* v, PyObject* residual, PyObject* stream,
+                       const char* in, const char* out) {
+    const First x(in, v[0], 2);
+    heddle_dropout_args a{};
+    a.rows = x[0], a.cols = x[1], a.dtype = x.code;
+    a.p = real64(v[2]), a.seed = natural(v[3]), a.offset = natural(v[4]);
+    a.step = static_cast<const int64_t*>(vec("step", v[5], 1, at::kLong, x.device));
+    const Mat mx(in, v[0], a.rows, a.cols, x.type, x.device), y(out, v[1], a.rows, a.cols, x.type, x.device),
+        r("residual", residual, a.rows, a.cols, x.type, x.device);
+    a.x = mx.p, a.ldx = mx.ld, a.y = y.p, a.ldy = y.ld, a.residual = r.p, a.ldr = r.ld;
+    return call(entry, ctx, a, x.device, stream);
+}
+
+// (ctx, x, y, p, seed, offset, step, residual, stream)
+PyObject* dropout(PyObject*, PyObject* const* v, Py_ssize_t count) {
+    return guarded<9>(count, [&] { return dropout_call(kDropout, v[0], v + 1, v[7], v[8], "x", "y"); });
+}
+
+// (ctx, dy, dx, p, seed, offset, step, stream)
+PyObject* dropout_backward(PyObject*, PyObject* const* v, Py_ssize_t count) {
+    return guarded<8>(count, [&] { return dropout_call(kDropoutGrad, v[0], v + 1, Py_None, v[7], "dy", "dx"); });
+}
+
+// v: tokens, the table or its gradient, y or its gradient, scale, first, vocab
+void embedding_args(heddle_embedding_args& a, const First& y, PyObject* const* v, at::ScalarType table_type) {
+    const at::Tensor& t = tensor("tokens", v[0]);
+    const at::IntArrayRef table = axes_of("table", v[1], 2);
+    a.tokens = y[0], a.cols = y[1], a.table_rows = table[0], a.dtype = y.code;
+    a.scale = real(v[3]), a.first = integer(v[4]);
+    a.vocab = v[5] != Py_None ? integer(v[5]) : a.first > INT64_MAX - a.table_rows ? INT64_MAX : a.first + a.table_rows;
+    a.wide_tokens = t.scalar_type() == at::kLong;
+    a.token = vec("tokens", v[0], a.tokens, a.wide_tokens ? at::kLong : at::kInt, y.device);
+    const Mat m("table", v[1], a.table_rows, a.cols, table_type, y.device),
+        out("y", v[2], a.tokens, a.cols, y.type, y.device);
+    a.table = m.p, a.ldt = m.ld, a.y = out.p, a.ldy = out.ld;
+}
+
+// (ctx, tokens, table, y, scale, first, vocab, stream)
+PyObject* embedding(PyObject*, PyObject* const* v, Py_ssize_t count) {
+    return guarded<8>(count, [&] {
+        const First y("y", v[3], 2);
+        heddle_embedding_args a{};
+        embedding_args(a, y, v + 1, y.type);
+        return call(kEmbedding, v[0], a, y.device, v[7]);
+    });
+}
+
+// (ctx, tokens, dtable, dy, scale, first, vocab, accumulate, stream)
+PyObject* embedding_backward(PyObject*, PyObject* const* v, Py_ssize_t count) {
+    return guarded<9>(count, [&] {
+        const First dy("dy", v[3], 2);
+        heddle_embedding_grad_args a{};
+        const bool wide = tensor("dtable", v[2]).scalar_type() == at::kFloat;
+        embedding_args(a.fwd, dy, v + 1, wide ? at::kFloat : dy.type);
+        a.grad_dtype = wide ? HEDDLE_FP32 : dy.code, a.accumulate = truth(v[7]);
+        return call(kEmbeddingGrad, v[0], a, dy.device, v[8]);
+    });
+}
+
+// v: logits, experts, weights, counts, valid, normalize
+void router_args(heddle_router_args& a, const First& l, PyObject* const* v) {
+    const int64_t k = axes_of("experts", v[1], 2)[1];
+    if (l[1] > INT32_MAX - 1 || k > INT32_MAX) throw Refused("experts do not fit into 32 bits");
+    a.tokens = l[0], a.experts = (int32_t)l[1], a.top_k = (int32_t)k, a.dtype = l.code, a.normalize = truth(v[5]);
+    const Mat logits("logits", v[0], l[0], l[1], l.type, l.device), e("experts", v[1], l[0], k, at::kInt, l.device),
+        w("weights", v[2], l[0], k, at::kFloat, l.device);
+    if (v[1] == Py_None || v[2] == Py_None || !tensor("experts", v[1]).is_contiguous() ||
+        !tensor("weights", v[2]).is_contiguous())
+        throw Refused("experts and weights are contiguous");
+    a.logits = logits.p, a.ldl = logits.ld;
+    a.expert = static_cast<int32_t*>(e.p), a.weight = static_cast<float*>(w.p);
+    a.count = static_cast<int32_t*>(vec("counts", v[3], l[1] + 1, at::kInt, l.device));
+    if (v[4] != Py_None) {
+        const bool bytes = tensor("valid", v[4]).scalar_type() == at::kByte;
+        a.valid = static_cast<const uint8_t*>(vec("valid", v[4], l[0], bytes ? at::kByte : at::kBool, l.device));
+    }
+}
+
+// (ctx, logits, experts, weights, counts, valid, normalize, loss, stream)
+PyObject* router(PyObject*, PyObject* const* v, Py_ssize_t count) {
+    return guarded<9>(count, [&] {
+        const First l("logits", v[1], 2);
+        heddle_router_args a{};
+        router_args(a, l, v + 1);
+        a.loss = static_cast<float*>(vec("loss", v[7], 1, at::kFloat, l.device));
+        return call(kRouter, v[0], a, l.device, v[8]);
+    });
+}
+
+// (ctx, logits, experts, weights, counts, valid, normalize, dlogits, dweights, dloss, stream)
+PyObject* router_backward(PyObject*, PyObject* const* v, Py_ssize_t count) {
+    return guarded<11>(count, [&] {
+        const First l("logits", v[1], 2);
+        heddle_router_grad_args a{};
+        router_args(a.fwd, l, v + 1);
+        const int64_t k = a.fwd.top_k;
+        const Mat d("dlogits", v[7], l[0], l[1], l.type, l.device), w("dweights", v[8], l[0], k, at::kFloat, l.device);
+        if (v[8] != Py_None && !tensor("dweights", v[8]).is_contiguous()) throw Refused("dweights is contiguous");
+        a.dlogits = d.p, a.ldd = d.ld, a.d_weight = static_cast<const float*>(w.p);
+        a.d_loss = static_cast<const float*>(vec("dloss", v[9], 1, at::kFloat, l.device));
+        return call(kRouterGrad, v[0], a, l.device, v[10]);
+    });
+}
+
 // (the functions' addresses by name, HeddleError, device index -> current stream)
 PyObject* bind(PyObject*, PyObject* const* v, Py_ssize_t count) {
     return guarded<3>(count, [&] {
@@ -421,6 +574,14 @@ PyMethodDef methods[] = {METHOD(bind),
                          METHOD(qk_norm_rope_backward),
                          METHOD(attention),
                          METHOD(attention_backward),
+                         METHOD(layer_norm),
+                         METHOD(layer_norm_backward),
+                         METHOD(dropout),
+                         METHOD(dropout_backward),
+                         METHOD(embedding),
+                         METHOD(embedding_backward),
+                         METHOD(router),
+                         METHOD(router_backward),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_heddle_ops", "Marshalling of the layer operators' calls.", -1, methods,
                       nullptr, nullptr, nullptr, nullptr};

@@ -85,7 +85,7 @@ ACTIVATIONS = {"none": ACT_NONE, "relu": ACT_RELU, "silu": ACT_SILU, "gelu": ACT
 
 
 def _fields(spec):
-    kinds = {"q": C.c_int64, "i": C.c_int32, "f": C.c_float, "p": C.c_void_p}
+    kinds = {"q": C.c_int64, "u": C.c_uint64, "i": C.c_int32, "f": C.c_float, "d": C.c_double, "p": C.c_void_p}
     return [(name, kinds[kind] if isinstance(kind, str) else kind)
             for kind, names in spec for name in names.split()]
 
@@ -137,6 +137,40 @@ class heddle_attention_grad_args(C.Structure):
                 ("dv", heddle_heads)]
 
 
+class heddle_layer_norm_args(C.Structure):
+    _fields_ = _fields([("q", "rows cols"), ("i", "dtype"), ("f", "eps"), ("p", "x"), ("q", "ldx"),
+                        ("p", "weight bias y"), ("q", "ldy"), ("p", "mean rstd")])
+
+
+class heddle_layer_norm_grad_args(C.Structure):
+    _fields_ = _fields([("q", "rows cols"), ("i", "dtype reserved"), ("p", "dy"), ("q", "lddy"), ("p", "x"),
+                        ("q", "ldx"), ("p", "weight mean rstd dres"), ("q", "ldr"), ("p", "dx"), ("q", "lddx"), ("p", "dw dbias")])
+
+
+class heddle_dropout_args(C.Structure):
+    _fields_ = _fields([("q", "rows cols"), ("i", "dtype reserved"), ("d", "p"), ("u", "seed offset"), ("p", "step x"),
+                        ("q", "ldx"), ("p", "residual"), ("q", "ldr"), ("p", "y"), ("q", "ldy")])
+
+
+class heddle_embedding_args(C.Structure):
+    _fields_ = _fields([("q", "tokens cols table_rows first vocab"), ("i", "dtype wide_tokens"), ("f", "scale"),
+                        ("i", "reserved"), ("p", "token table"), ("q", "ldt"), ("p", "y"), ("q", "ldy")])
+
+
+class heddle_embedding_grad_args(C.Structure):
+    _fields_ = [("fwd", heddle_embedding_args), ("grad_dtype", C.c_int32), ("accumulate", C.c_int32)]
+
+
+class heddle_router_args(C.Structure):
+    _fields_ = _fields([("q", "tokens"), ("i", "experts top_k dtype normalize"), ("p", "logits"), ("q", "ldl"),
+                        ("p", "valid expert weight count loss")])
+
+
+class heddle_router_grad_args(C.Structure):
+    _fields_ = [("fwd", heddle_router_args), ("d_weight", C.c_void_p), ("d_loss", C.c_void_p),
+                ("dlogits", C.c_void_p), ("ldd", C.c_int64)]
+
+
 EXPORTS = ["heddle_create", "heddle_destroy", "heddle_last_error", "heddle_device", "heddle_load_cluster",
            "heddle_load_model", "heddle_price_candidates", "heddle_topk_reset", "heddle_topk",
            "heddle_price_topk_host", "heddle_get_tables", "heddle_device_errors",
@@ -146,7 +180,9 @@ EXPORTS = ["heddle_create", "heddle_destroy", "heddle_last_error", "heddle_devic
            "heddle_load_mbs", "heddle_price_mbs", "heddle_price_plans", "heddle_load_experts",
            "heddle_price_tiled", "heddle_set_chunk",
            "heddle_linear", "heddle_linear_backward", "heddle_gated_ffn", "heddle_gated_ffn_backward",
-           "heddle_qk_norm_rope", "heddle_qk_norm_rope_backward", "heddle_attention", "heddle_attention_backward"]
+           "heddle_qk_norm_rope", "heddle_qk_norm_rope_backward", "heddle_attention", "heddle_attention_backward",
+           "heddle_layer_norm", "heddle_layer_norm_backward", "heddle_dropout", "heddle_dropout_backward",
+           "heddle_embedding", "heddle_embedding_backward", "heddle_router", "heddle_router_backward"]
 MAX_MBS_LEVELS = 4
 PHASES = ("screen", "search", "topk")
 TOPK_NOALLOC_MAX_N = 4194304
@@ -200,6 +236,14 @@ def load_library(path: str = LIB_PATH):
         "heddle_qk_norm_rope_backward": (i32, [p, p, p]),
         "heddle_attention": (i32, [p, p, p]),
         "heddle_attention_backward": (i32, [p, p, p]),
+        "heddle_layer_norm": (i32, [p, p, p]),
+        "heddle_layer_norm_backward": (i32, [p, p, p]),
+        "heddle_dropout": (i32, [p, p, p]),
+        "heddle_dropout_backward": (i32, [p, p, p]),
+        "heddle_embedding": (i32, [p, p, p]),
+        "heddle_embedding_backward": (i32, [p, p, p]),
+        "heddle_router": (i32, [p, p, p]),
+        "heddle_router_backward": (i32, [p, p, p]),
     }
     for name, (res, args) in sig.items():
         f = getattr(L, name)
@@ -494,7 +538,9 @@ def heddle_get_search(ctx) -> int:
 
 _ops = None
 _OP_NAMES = ("heddle_linear", "heddle_linear_backward", "heddle_gated_ffn", "heddle_gated_ffn_backward",
-             "heddle_qk_norm_rope", "heddle_qk_norm_rope_backward", "heddle_attention", "heddle_attention_backward")
+             "heddle_qk_norm_rope", "heddle_qk_norm_rope_backward", "heddle_attention", "heddle_attention_backward",
+             "heddle_layer_norm", "heddle_layer_norm_backward", "heddle_dropout", "heddle_dropout_backward",
+             "heddle_embedding", "heddle_embedding_backward", "heddle_router", "heddle_router_backward")
 
 
 def _op_setup():
@@ -578,6 +624,75 @@ def heddle_attention_backward(ctx, do, q, k, v, o, lse, dq, dk, dv, q_lens=None,
     """Gradients of heddle_attention from ``do``, with its o and lse."""
     st = (_ops or _op_setup()).attention_backward(ctx, q, k, v, o, lse, q_lens, kv_lens, window, sinks, scale, do,
                                                   dq, dk, dv, stream)
+    if st:
+        _check(ctx, st)
+
+
+# The hidden state between the products: float32 tensors are taken too.
+
+def heddle_layer_norm(ctx, x, weight, bias, y, mean=None, rstd=None, eps=1e-5, stream=None):
+    """y = (x - mean) rstd weight + bias for every row of x ([rows][cols]);
+    weight and bias may be None, float32 mean and rstd receive the statistics."""
+    st = (_ops or _op_setup()).layer_norm(ctx, x, weight, bias, y, mean, rstd, eps, stream)
+    if st:
+        _check(ctx, st)
+
+
+def heddle_layer_norm_backward(ctx, dy, x, weight, mean, rstd, dx=None, dw=None, dbias=None, dres=None, stream=None):
+    """Gradients of heddle_layer_norm, those of weight and bias in float32; an
+    output that is None is not computed.  ``dres`` is added to dx."""
+    st = (_ops or _op_setup()).layer_norm_backward(ctx, dy, x, weight, mean, rstd, dx, dw, dbias, dres, stream)
+    if st:
+        _check(ctx, st)
+
+
+def heddle_dropout(ctx, x, y, p, seed, offset=0, residual=None, step=None, stream=None):
+    """y = residual + (x / (1 - p) or 0, by random numbers of seed and offset);
+    ``step`` (an int64 CUDA tensor of one element) is added to offset when the
+    call runs."""
+    st = (_ops or _op_setup()).dropout(ctx, x, y, p, seed, offset, step, residual, stream)
+    if st:
+        _check(ctx, st)
+
+
+def heddle_dropout_backward(ctx, dy, dx, p, seed, offset=0, step=None, stream=None):
+    """The gradient of heddle_dropout's x, by the same p, seed, offset and step."""
+    st = (_ops or _op_setup()).dropout_backward(ctx, dy, dx, p, seed, offset, step, stream)
+    if st:
+        _check(ctx, st)
+
+
+def heddle_embedding(ctx, tokens, table, y, scale=1.0, first=0, vocab=None, stream=None):
+    """y[t] = scale table[tokens[t] - first], zeros for tokens outside the table
+    (a shard of ``vocab`` tokens; None: it ends with the table)."""
+    st = (_ops or _op_setup()).embedding(ctx, tokens, table, y, scale, first, vocab, stream)
+    if st:
+        _check(ctx, st)
+
+
+def heddle_embedding_backward(ctx, tokens, dy, dtable, scale=1.0, first=0, vocab=None, accumulate=False, stream=None):
+    """The gradient of heddle_embedding's table, of dy's type or float32;
+    ``accumulate`` adds it to what dtable holds."""
+    st = (_ops or _op_setup()).embedding_backward(ctx, tokens, dtable, dy, scale, first, vocab, accumulate, stream)
+    if st:
+        _check(ctx, st)
+
+
+def heddle_router(ctx, logits, experts, weights, counts, loss=None, valid=None, normalize=True, stream=None):
+    """The chosen experts (int32 [tokens][top_k]) and their weights (float32) of
+    logits ([tokens][experts]), counts (int32 [experts + 1], the last of the
+    tokens) and the balance loss (float32 [1]); ``valid``: bool [tokens]."""
+    st = (_ops or _op_setup()).router(ctx, logits, experts, weights, counts, valid, normalize, loss, stream)
+    if st:
+        _check(ctx, st)
+
+
+def heddle_router_backward(ctx, logits, experts, weights, counts, dlogits, dweights=None, dloss=None, valid=None,
+                           normalize=True, stream=None):
+    """The gradient of heddle_router's logits from its results and the gradients
+    of weights and loss."""
+    st = (_ops or _op_setup()).router_backward(ctx, logits, experts, weights, counts, valid, normalize, dlogits,
+                                               dweights, dloss, stream)
     if st:
         _check(ctx, st)
 
