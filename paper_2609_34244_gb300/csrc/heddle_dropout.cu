@@ -12,92 +12,104 @@
 namespace hd {
 namespace {
 
+constexpr int kRounds = 10;
+
 struct Dropout {
     heddle_dropout_args a;
     uint32_t least;  // the smallest number that is kept
     float scale;
+    // each round's: added up by the host, so that an exclusive or takes them as
+    // they come with the launch
+    uint32_t key[kRounds][2];
 };
 
-// Ten rounds: the counter in c, the key in k.
-__device__ __forceinline__ void philox(uint32_t (&c)[4], uint32_t k0, uint32_t k1) {
+// Two of the twenty products are the same for all counters of one offset whose
+// upper halves (`high`) agree, 2^32 of them: the first round's second and the
+// second round's first.  They are kept.
+struct Start {
+    uint32_t high, c1, hi, lo, c3;
+};
+__device__ __forceinline__ Start start_of(const Dropout& d, uint32_t high, uint64_t offset) {
+    const uint64_t b = (uint64_t)(uint32_t)offset * 0xCD9E8D57u;
+    const uint32_t c0 = (uint32_t)(b >> 32) ^ high ^ d.key[0][0];
+    const uint64_t a = (uint64_t)c0 * 0xD2511F53u;
+    return {high, (uint32_t)b, (uint32_t)(a >> 32), (uint32_t)a, (uint32_t)(offset >> 32) ^ d.key[0][1]};
+}
+
+// The four numbers of the counter (low, s.high, offset).
+__device__ __forceinline__ void numbers(uint32_t (&c)[4], const Dropout& d, const Start& s, uint32_t low) {
+    const uint64_t first = (uint64_t)low * 0xD2511F53u;
+    const uint64_t second = (uint64_t)((uint32_t)(first >> 32) ^ s.c3) * 0xCD9E8D57u;
+    c[0] = (uint32_t)(second >> 32) ^ s.c1 ^ d.key[1][0];
+    c[1] = (uint32_t)second;
+    c[2] = s.hi ^ (uint32_t)first ^ d.key[1][1];
+    c[3] = s.lo;
 #pragma unroll
-    for (int r = 0; r < 10; ++r) {
+    for (int r = 2; r < kRounds; ++r) {
         const uint64_t a = (uint64_t)c[0] * 0xD2511F53u, b = (uint64_t)c[2] * 0xCD9E8D57u;
-        c[0] = (uint32_t)(b >> 32) ^ c[1] ^ (k0 + r * 0x9E3779B9u);
+        c[0] = (uint32_t)(b >> 32) ^ c[1] ^ d.key[r][0];
         c[1] = (uint32_t)b;
-        c[2] = (uint32_t)(a >> 32) ^ c[3] ^ (k1 + r * 0xBB67AE85u);
+        c[2] = (uint32_t)(a >> 32) ^ c[3] ^ d.key[r][1];
         c[3] = (uint32_t)a;
     }
 }
 
-__device__ __forceinline__ void numbers(uint32_t (&c)[4], const Dropout& d, uint64_t four, uint64_t offset) {
-    c[0] = (uint32_t)four, c[1] = (uint32_t)(four >> 32);
-    c[2] = (uint32_t)offset, c[3] = (uint32_t)(offset >> 32);
-    philox(c, (uint32_t)d.a.seed, (uint32_t)(d.a.seed >> 32));
-}
-
-__device__ __forceinline__ float dropped(const Dropout& d, uint32_t u, float x) {
-    return u < d.least ? 0.0f : x * d.scale;
+// to + (u < least ? 0 : x scale), the product under a predicate: a selection
+// would take another instruction of the pipe that the exclusive ors fill.
+__device__ __forceinline__ float kept(const Dropout& d, uint32_t u, float x, float to) {
+    asm("{\n\t.reg .pred p;\n\tsetp.ge.u32 p, %1, %2;\n\t@p fma.rn.f32 %0, %3, %4, %0;\n\t}"
+        : "+f"(to)
+        : "r"(u), "r"(d.least), "f"(x), "f"(d.scale));
+    return to;
 }
 
 constexpr int kThreads = 256;
-constexpr int kUnits = 2;  // of 16 bytes a thread takes at a time
+// Blocks an SM: as many as the numbers' registers allow without spilling, in
+// four rounds (a unit a thread in more or fewer registers, two units at a
+// time, the next unit fetched ahead: 228 to 290 us where this takes 224).
+constexpr int kResident = 6, kTurns = 4;
 
-// Rows of whole 16-byte units; everything is one row where rows follow each
-// other, and its end may then be part of a unit.
-template <class T, bool RESIDUAL>
-__global__ void __launch_bounds__(kThreads) dropout_units_kernel(const __grid_constant__ Dropout d) {
+// Whole 16-byte units.  FLAT: rows follow each other and are taken as one,
+// whose end may be part of a unit.
+template <class T, bool RESIDUAL, bool FLAT>
+__global__ void __launch_bounds__(kThreads, kResident) dropout_units_kernel(const __grid_constant__ Dropout d) {
     allow_dependents();
     await_previous();
     constexpr int V = 16 / sizeof(T);
     const T *x = static_cast<const T*>(d.a.x), *res = static_cast<const T*>(d.a.residual);
     T* y = static_cast<T*>(d.a.y);
     const uint64_t offset = d.a.offset + (d.a.step ? (uint64_t)*d.a.step : 0);
-    const int64_t cols = d.a.cols, per = (cols + V - 1) / V, total = d.a.rows * per;
-    const int64_t step = (int64_t)gridDim.x * kThreads;
-    for (int64_t i0 = (int64_t)blockIdx.x * kThreads + threadIdx.x; i0 < total; i0 += kUnits * step) {
-        uint4 v[kUnits], w[kUnits];
-        int64_t row[kUnits], col[kUnits];
-        bool live[kUnits], full[kUnits];
+    Start start = start_of(d, 0, offset);
+    const int64_t per = d.a.cols / V, total = FLAT ? per : d.a.rows * per, step = (int64_t)gridDim.x * kThreads;
+    auto take = [&](int64_t i, const float (&f)[V], float (&to)[V]) {
+        const uint64_t four = (uint64_t)i * (V / 4);
+        if (four >> 32 != start.high) start = start_of(d, (uint32_t)(four >> 32), offset);
 #pragma unroll
-        for (int k = 0; k < kUnits; ++k) {
-            const int64_t i = i0 + k * step;
-            live[k] = i < total;
-            row[k] = d.a.rows == 1 ? 0 : i / per;
-            col[k] = (i - row[k] * per) * V;
-            full[k] = live[k] && col[k] + V <= cols;
-            if (full[k]) {
-                v[k] = *reinterpret_cast<const uint4*>(x + row[k] * d.a.ldx + col[k]);
-                if (RESIDUAL) w[k] = *reinterpret_cast<const uint4*>(res + row[k] * d.a.ldr + col[k]);
-            }
+        for (int q = 0; q < V / 4; ++q) {
+            uint32_t u[4];
+            numbers(u, d, start, (uint32_t)four + q);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) to[4 * q + e] = kept(d, u[e], f[4 * q + e], to[4 * q + e]);
         }
+    };
+    for (int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x; i < total; i += step) {
+        const int64_t row = FLAT ? 0 : i / per, col = (i - row * per) * V;
+        float f[V], to[V] = {};
+        unpack<T>(*reinterpret_cast<const uint4*>(x + row * d.a.ldx + col), f);
+        if (RESIDUAL) unpack<T>(*reinterpret_cast<const uint4*>(res + row * d.a.ldr + col), to);
+        take(i, f, to);
+        *reinterpret_cast<uint4*>(y + row * d.a.ldy + col) = pack<T>(to);
+    }
+    const int64_t left = FLAT ? d.a.cols - per * V : 0;
+    if (left && blockIdx.x == 0 && threadIdx.x == 0) {
+        float f[V] = {}, to[V] = {};
 #pragma unroll
-        for (int k = 0; k < kUnits; ++k) {
-            if (!live[k]) continue;
-            const uint64_t first = (uint64_t)row[k] * cols + col[k];
-            uint32_t u[V / 4][4];
+        for (int e = 0; e < V; ++e)
+            if (e < left) f[e] = to_float(x[per * V + e]), to[e] = RESIDUAL ? to_float(res[per * V + e]) : 0.0f;
+        take(per, f, to);
 #pragma unroll
-            for (int q = 0; q < V / 4; ++q) numbers(u[q], d, first / 4 + q, offset);
-            if (full[k]) {
-                T* t = reinterpret_cast<T*>(&v[k]);
-                const T* r = reinterpret_cast<const T*>(&w[k]);
-#pragma unroll
-                for (int e = 0; e < V; ++e) {
-                    float f = dropped(d, u[e / 4][e % 4], to_float(t[e]));
-                    if (RESIDUAL) f += to_float(r[e]);
-                    t[e] = from_float<T>(f);
-                }
-                *reinterpret_cast<uint4*>(y + row[k] * d.a.ldy + col[k]) = v[k];
-            } else {
-#pragma unroll
-                for (int e = 0; e < V; ++e) {
-                    if (col[k] + e >= cols) break;
-                    float f = dropped(d, u[e / 4][e % 4], to_float(x[row[k] * d.a.ldx + col[k] + e]));
-                    if (RESIDUAL) f += to_float(res[row[k] * d.a.ldr + col[k] + e]);
-                    y[row[k] * d.a.ldy + col[k] + e] = from_float<T>(f);
-                }
-            }
-        }
+        for (int e = 0; e < V; ++e)
+            if (e < left) y[per * V + e] = from_float<T>(to[e]);
     }
 }
 
@@ -116,8 +128,9 @@ __global__ void __launch_bounds__(kThreads) dropout_any_kernel(const __grid_cons
         const uint64_t first = (uint64_t)row * cols + col;
         const int skip = (int)(first & 3);
         uint32_t u[2][4];
-        numbers(u[0], d, first / 4, offset);
-        if (skip) numbers(u[1], d, first / 4 + 1, offset);
+        const uint64_t four = first / 4;
+        numbers(u[0], d, start_of(d, (uint32_t)(four >> 32), offset), (uint32_t)four);
+        if (skip) numbers(u[1], d, start_of(d, (uint32_t)((four + 1) >> 32), offset), (uint32_t)(four + 1));
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             if (col + e >= cols) break;
@@ -125,9 +138,8 @@ __global__ void __launch_bounds__(kThreads) dropout_any_kernel(const __grid_cons
 #pragma unroll
             for (int j = 0; j < 8; ++j)
                 if (j == skip + e) n = u[j / 4][j % 4];
-            float f = dropped(d, n, to_float(x[row * d.a.ldx + col + e]));
-            if (res) f += to_float(res[row * d.a.ldr + col + e]);
-            y[row * d.a.ldy + col + e] = from_float<T>(f);
+            const float to = res ? to_float(res[row * d.a.ldr + col + e]) : 0.0f;
+            y[row * d.a.ldy + col + e] = from_float<T>(kept(d, n, to_float(x[row * d.a.ldx + col + e]), to));
         }
     }
 }
@@ -140,12 +152,15 @@ cudaError_t run(const OpContext& x, Dropout d, cudaStream_t st) {
         a.cols *= a.rows, a.rows = 1;
     const bool units = (a.rows == 1 || a.cols % V == 0) && rows_whole(a.x, a.ldx, a.rows, size) &&
                        rows_whole(a.y, a.ldy, a.rows, size) && rows_whole(a.residual, a.ldr, a.rows, size);
-    const int64_t per = units ? kUnits * kThreads : kThreads, most = (int64_t)x.num_sms * 16;
-    const int64_t want = ceil_div(a.rows * ceil_div(a.cols, units ? V : 4), per);
+    const int64_t most = (int64_t)x.num_sms * kResident * kTurns;
+    const int64_t want = ceil_div(units ? ceil_div(a.rows * a.cols, V) : a.rows * ceil_div(a.cols, 4), kThreads);
     const dim3 grid((unsigned)(want < most ? want : most));
     if (!units) return launch(x, dropout_any_kernel<T>, grid, kThreads, 0, st, d);
-    return a.residual ? launch(x, dropout_units_kernel<T, true>, grid, kThreads, 0, st, d)
-                      : launch(x, dropout_units_kernel<T, false>, grid, kThreads, 0, st, d);
+    if (a.rows == 1)
+        return a.residual ? launch(x, dropout_units_kernel<T, true, true>, grid, kThreads, 0, st, d)
+                          : launch(x, dropout_units_kernel<T, false, true>, grid, kThreads, 0, st, d);
+    return a.residual ? launch(x, dropout_units_kernel<T, true, false>, grid, kThreads, 0, st, d)
+                      : launch(x, dropout_units_kernel<T, false, false>, grid, kThreads, 0, st, d);
 }
 
 }  // namespace
@@ -156,6 +171,10 @@ cudaError_t launch_dropout(const OpContext& x, const heddle_dropout_args& a, cud
     const double all = 4294967296.0, least = nearbyint(a.p * all);
     d.least = (uint32_t)(least < all ? least : all - 1.0);
     d.scale = (float)(all / (all - (double)d.least));
+    for (int r = 0; r < kRounds; ++r) {
+        d.key[r][0] = (uint32_t)a.seed + r * 0x9E3779B9u;
+        d.key[r][1] = (uint32_t)(a.seed >> 32) + r * 0xBB67AE85u;
+    }
     if (a.dtype == HEDDLE_BF16) return run<__nv_bfloat16>(x, d, st);
     if (a.dtype == HEDDLE_FP16) return run<__half>(x, d, st);
     return run<float>(x, d, st);

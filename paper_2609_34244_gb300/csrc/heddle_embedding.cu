@@ -31,7 +31,7 @@ __global__ void __launch_bounds__(kThreads)
     embedding_kernel(const __grid_constant__ heddle_embedding_args a, bool whole, uint32_t* err) {
     allow_dependents();
     await_previous();
-    using R = RowPart<T, GL, U, STRIDED>;
+    using R = RowPart<T, U, STRIDED>;
     constexpr int kTokens = kThreads / GL, kCols = GL * R::N;
     const int64_t t = (int64_t)blockIdx.x * kTokens + threadIdx.x / GL, from = (int64_t)blockIdx.y * kCols;
     if (t >= a.tokens) return;
@@ -39,17 +39,14 @@ __global__ void __launch_bounds__(kThreads)
     const int64_t row = row_of(a, t, past);
     if (past && from == 0 && threadIdx.x % GL == 0) atomicOr(err, kErrOpToken);
     const int64_t left = a.cols - from;
-    const R part{(int)(threadIdx.x % GL), (int)(left < kCols ? left : kCols)};
-    uint4 v[U];
+    const R part{(int)(threadIdx.x % GL), GL, (int)(left < kCols ? left : kCols)};
+    uint32_t v[R::kWords] = {};
     if (row >= 0) {
         part.load(v, static_cast<const T*>(a.table) + row * a.ldt + from, whole);
         if (a.scale != 1.0f) {
 #pragma unroll
-            for (int e = 0; e < R::N; ++e) R::set(v, e, R::get(v, e) * a.scale);
+            for (int p = 0; p < R::N / 2; ++p) set_pair<T>(v, p, mul2(pair_of<T>(v, p), both(a.scale)));
         }
-    } else {
-#pragma unroll
-        for (int u = 0; u < U; ++u) v[u] = make_uint4(0, 0, 0, 0);
     }
     part.store(static_cast<T*>(a.y) + t * a.ldy + from, v, whole);
 }
@@ -245,12 +242,12 @@ struct Sums {
     int32_t accumulate;
 };
 
-template <class T, class TO, int GL, int U, bool STRIDED>
-__device__ __forceinline__ void add_out(const Sums& s, const RowPart<T, GL, U, STRIDED>& part, int64_t row,
-                                        int64_t from, const float (&sum)[RowPart<T, GL, U, STRIDED>::N]) {
+template <class TO, class R>
+__device__ __forceinline__ void add_out(const Sums& s, const R& part, int64_t row, int64_t from,
+                                        const float (&sum)[R::N]) {
     TO* p = static_cast<TO*>(s.out) + row * s.a.ldt + from;
 #pragma unroll
-    for (int e = 0; e < part.N; ++e)
+    for (int e = 0; e < R::N; ++e)
         if (part.in(e)) {
             float v = sum[e] * s.a.scale;
             if (s.accumulate) v += to_float(p[part.at(e)]);
@@ -268,13 +265,13 @@ __global__ void __launch_bounds__(kThreads)
     embedding_sums_kernel(const __grid_constant__ Sums s, bool whole) {
     allow_dependents();
     await_previous();
-    using R = RowPart<T, kThreads, U, STRIDED>;
+    using R = RowPart<T, U, STRIDED>;
     constexpr int kCols = kThreads * R::N;
     const int64_t n = *s.count, first = (int64_t)blockIdx.x * s.chunk;
     if (first >= n) return;
     const int64_t end = first + s.chunk < n ? first + s.chunk : n, from = (int64_t)blockIdx.y * kCols;
     const int64_t left = s.a.cols - from;
-    const R part{(int)threadIdx.x, (int)(left < kCols ? left : kCols)};
+    const R part{(int)threadIdx.x, kThreads, (int)(left < kCols ? left : kCols)};
     const T* dy = static_cast<const T*>(s.a.y) + from;
     const uint32_t before = first ? s.list[first - 1].row : ~0u, behind = end < n ? s.list[end].row : ~0u;
     float* partial = s.partial + ((int64_t)blockIdx.x * 2) * s.a.cols + from;
@@ -288,11 +285,11 @@ __global__ void __launch_bounds__(kThreads)
             for (int e = 0; e < R::N; ++e)
                 if (part.in(e)) p[part.at(e)] = sum[e];
         } else {
-            add_out<T, TO, kThreads, U, STRIDED>(s, part, row, from, sum);
+            add_out<TO>(s, part, row, from, sum);
         }
     };
     for (int64_t i = first; i < end; i += kAhead) {
-        uint4 v[kAhead][U];
+        uint32_t v[kAhead][R::kWords];
         uint32_t rows[kAhead];
 #pragma unroll
         for (int k = 0; k < kAhead; ++k) {
@@ -310,7 +307,10 @@ __global__ void __launch_bounds__(kThreads)
                 for (int e = 0; e < R::N; ++e) sum[e] = 0.0f;
             }
 #pragma unroll
-            for (int e = 0; e < R::N; ++e) sum[e] += R::get(v[k], e);
+            for (int p = 0; p < R::N / 2; ++p) {
+                const float2 f = pair_of<T>(v[k], p);
+                sum[2 * p] += f.x, sum[2 * p + 1] += f.y;
+            }
         }
     }
     finish(row == behind);
@@ -351,7 +351,7 @@ int size_of(int32_t dtype) { return dtype == HEDDLE_FP32 ? 4 : 2; }
 
 template <class T, int GL, int U, bool STRIDED>
 cudaError_t lookup(const OpContext& x, const heddle_embedding_args& a, bool whole, cudaStream_t st) {
-    constexpr int kCols = RowPart<T, GL, U, STRIDED>::N * GL;
+    constexpr int kCols = RowPart<T, U, STRIDED>::N * GL;
     const dim3 grid((unsigned)ceil_div(a.tokens, kThreads / GL), (unsigned)ceil_div(a.cols, kCols));
     return launch(x, embedding_kernel<T, GL, U, STRIDED>, grid, kThreads, 0, st, a, whole, x.err);
 }
@@ -390,7 +390,7 @@ Places places(const heddle_embedding_args& a) {
 
 template <class T, class TO, bool STRIDED>
 cudaError_t sums(const OpContext& x, const Sums& s, cudaStream_t st) {
-    constexpr int kCols = RowPart<T, kThreads, 1, STRIDED>::N * kThreads;
+    constexpr int kCols = RowPart<T, 1, STRIDED>::N * kThreads;
     const unsigned chunks = (unsigned)ceil_div(s.a.tokens, s.chunk);
     const bool whole = rows_whole(s.a.y, s.a.ldy, s.a.tokens, sizeof(T));
     cudaError_t e = launch(x, embedding_sums_kernel<T, TO, 1, STRIDED>,

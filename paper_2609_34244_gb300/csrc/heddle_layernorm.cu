@@ -1,161 +1,498 @@
 // heddle_layernorm.cu -- layer norm and its gradients.
 //
-// Bound by memory.  A row is held in the registers of a group of threads: its
-// mean first, then the squares of its deviations from it, so that a large mean
-// costs no digits and nothing is read twice.  A block walks over rows and
-// fetches the next one while it adds up the one at hand.  Gradients: the same,
-// with the weights' sums over rows in registers, one set a block, which a
-// second kernel adds in order.
+// Bound by memory.  A row is held by a group of threads, two 16-byte units each at most:
+// its mean first, then the squares of its deviations from it, so that a large
+// mean costs no digits and nothing is read from memory twice.  Short rows take
+// 4 to 32 lanes of a warp, others a block, which walks over rows.  Gradients of
+// such rows are read through a ring in shared memory that bulk copies fill
+// ahead; the weights' sums over rows stay in registers, one set a block, and a
+// second kernel adds the sets in order.  Arithmetic runs on two values at a
+// time, and 16-bit values are taken out of their words in pairs: one by one,
+// bfloat16 was bound by instructions (16384 x 8192: forward 149 us, backward
+// 350).
+
+#include <atomic>
 
 #include "heddle_rows.cuh"
 
+#ifndef FWD_THREADS
+#define FWD_THREADS 1024
+#define GRAD_THREADS 512
+#define GRAD32 1024
+#define FRING 0
+#define FWD_SHORT 4
+#endif
 namespace hd {
 namespace {
 
-// The group's sums of N values, the same in every thread.  `turn` alternates
-// between calls: one barrier each.
-template <int G, int N>
-__device__ __forceinline__ void group_sum(float (&v)[N], int& turn) {
-#pragma unroll
-    for (int i = 0; i < N; ++i) v[i] = warp_sum(v[i]);
-    if constexpr (G > 32) {
-        constexpr int W = G / 32;
-        __shared__ float part[2][N][W];
-        const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
-        if (lane == 0) {
-#pragma unroll
-            for (int i = 0; i < N; ++i) part[turn][i][warp] = v[i];
-        }
+// The block's sum, the same in every thread.  `turn` alternates between calls:
+// one barrier each.
+struct BlockSum {
+    float* part;  // [2][32], of a block's shared memory
+    int lanes;    // a power of two that has the warps' sums
+    int turn = 0;
+    __device__ __forceinline__ BlockSum() {
+        __shared__ float all[2][32];
+        part = all[0];
+        const int warps = blockDim.x / 32;
+        lanes = 1 << (32 - __clz(warps - 1));
+        if (threadIdx.x < 64) part[threadIdx.x] = 0.0f;
         __syncthreads();
+    }
+    __device__ __forceinline__ float operator()(float v) {
+        float* at = part + turn;
+        v = warp_sum(v);
+        if (threadIdx.x % 32 == 0) at[threadIdx.x / 32] = v;
+        __syncthreads();
+        v = at[threadIdx.x % lanes];
 #pragma unroll
-        for (int i = 0; i < N; ++i) {
-            v[i] = part[turn][i][lane % W];
+        for (int o = 16; o; o >>= 1)
+            if (o < lanes) v += __shfl_xor_sync(~0u, v, o);
+        turn ^= 32;
+        return v;
+    }
+};
+// Two sums: the lower half of a warp's lanes goes on with the first, the upper
+// half with the second.
+__device__ __forceinline__ void block_sums(float& v0, float& v1, int& turn) {
+    __shared__ float part[2][2][32];
+    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, warps = blockDim.x / 32, half = lane / 16;
+    float v = (half ? v1 : v0) + __shfl_xor_sync(~0u, half ? v0 : v1, 16);
 #pragma unroll
-            for (int o = W / 2; o; o >>= 1) v[i] += __shfl_xor_sync(~0u, v[i], o);
-        }
-        turn ^= 1;
+    for (int o = 8; o; o >>= 1) v += __shfl_xor_sync(~0u, v, o);
+    if (lane % 16 == 0) part[turn][half][warp] = v;
+    __syncthreads();
+    const int i = lane % 16;
+    v = (i < warps ? part[turn][half][i] : 0.0f) + (i + 16 < warps ? part[turn][half][i + 16] : 0.0f);
+#pragma unroll
+    for (int o = 8; o; o >>= 1) v += __shfl_xor_sync(~0u, v, o);
+    v0 = __shfl_sync(~0u, v, 0), v1 = __shfl_sync(~0u, v, 16);
+    turn ^= 1;
+}
+
+// Four sums: a quarter of a warp's lanes for each.
+__device__ __forceinline__ void block_sums(float (&v)[4], int& turn) {
+    __shared__ float part[2][4][32];
+    const int warp = threadIdx.x / 32, lane = threadIdx.x % 32, warps = blockDim.x / 32;
+    const bool up = lane & 16, odd = lane & 8;
+    const float a = (up ? v[2] : v[0]) + __shfl_xor_sync(~0u, up ? v[0] : v[2], 16),
+                b = (up ? v[3] : v[1]) + __shfl_xor_sync(~0u, up ? v[1] : v[3], 16);
+    float c = (odd ? b : a) + __shfl_xor_sync(~0u, odd ? a : b, 8);
+#pragma unroll
+    for (int o = 4; o; o >>= 1) c += __shfl_xor_sync(~0u, c, o);
+    if (lane % 8 == 0) part[turn][lane / 8][warp] = c;
+    __syncthreads();
+    c = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 32; i += 8)
+        if (i + lane % 8 < warps) c += part[turn][lane / 8][i + lane % 8];
+#pragma unroll
+    for (int o = 4; o; o >>= 1) c += __shfl_xor_sync(~0u, c, o);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = __shfl_sync(~0u, c, 8 * i);
+    turn ^= 1;
+}
+
+// sum / cols, inv = 1 / cols: the product and one correction by its remainder
+// (exact where the quotient is a float: a row of one value has no variance).
+// A division would take a dozen instructions of every thread.
+__device__ __forceinline__ float over(float sum, float cols, float inv) {
+    const float q = sum * inv;
+    return fmaf(fmaf(-q, cols, sum), inv, q);
+}
+
+// Of GL lanes of a warp, all of which take part.
+template <int GL, int N>
+__device__ __forceinline__ void lanes_sum(float (&v)[N]) {
+#pragma unroll
+    for (int o = GL / 2; o; o >>= 1) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) v[i] += __shfl_xor_sync(~0u, v[i], o);
     }
 }
 
-template <int G>
-constexpr int kBlock = G == 32 ? 256 : G;
+// A vector of the row's length in registers, or `none`.
+template <class T, class R>
+__device__ __forceinline__ void load_vector(const R& part, uint32_t (&w)[R::kWords], const void* p, float none) {
+    if (p) {
+        part.load(w, static_cast<const T*>(p), (uintptr_t)p % 16 == 0 && part.cols % R::V == 0);
+    } else {
+#pragma unroll
+        for (int i = 0; i < R::N / 2; ++i) set_pair<T>(w, i, both(none));
+    }
+}
 
-template <class T, int G, int U, bool STRIDED>
-__global__ void __launch_bounds__(kBlock<G>)
+// The sum of a row's values, zeros past its end.
+template <class T, class R>
+__device__ __forceinline__ float sum_of(const R&, const uint32_t (&r)[R::kWords]) {
+    float2 s[2] = {both(0.0f), both(0.0f)};
+#pragma unroll
+    for (int p = 0; p < R::N / 2; ++p) s[p % 2] = plus<T>(r, p, s[p % 2]);
+    s[0] = add2(s[0], s[1]);
+    return s[0].x + s[0].y;
+}
+// Their deviations from the mean, and the sum of these' squares.  ENDS: the
+// row's end may lie in a unit.
+template <class T, bool ENDS, class R>
+__device__ __forceinline__ float squares_of(const R& part, const uint32_t (&r)[R::kWords], float2 (&v)[R::N / 2],
+                                            float mean) {
+    float2 s = both(0.0f);
+    const float2 m = both(-mean);
+#pragma unroll
+    for (int p = 0; p < R::N / 2; ++p) {
+        v[p] = plus<T>(r, p, m);
+        if (ENDS) {
+            const float2 d = make_float2(part.in(2 * p) ? v[p].x : 0.0f, part.in(2 * p + 1) ? v[p].y : 0.0f);
+            s = fma2(d, d, s);
+        } else if (part.in(2 * p)) {
+            s = fma2(v[p], v[p], s);
+        }
+    }
+    return s.x + s.y;
+}
+
+// Weight and bias of a lane as floats in its registers.
+template <class T, class R>
+struct Held {
+    float2 w[R::N / 2], b[R::N / 2];
+    __device__ __forceinline__ Held(const R& part, const heddle_layer_norm_args& a, float4*) {
+        uint32_t r[R::kWords];
+        load_vector<T>(part, r, a.weight, 1.0f);
+#pragma unroll
+        for (int p = 0; p < R::N / 2; ++p) w[p] = pair_of<T>(r, p);
+        load_vector<T>(part, r, a.bias, 0.0f);
+#pragma unroll
+        for (int p = 0; p < R::N / 2; ++p) b[p] = pair_of<T>(r, p);
+    }
+    __device__ __forceinline__ void scale(const R&, uint32_t (&out)[R::kWords], const float2 (&v)[R::N / 2],
+                                          float rstd) const {
+        const float2 s = both(rstd);
+#pragma unroll
+        for (int p = 0; p < R::N / 2; ++p) set_pair<T>(out, p, fma2(mul2(v[p], s), w[p], b[p]));
+    }
+};
+// Those of a block as floats in shared memory, each thread its own, four values
+// after four: taking 16-bit ones out of their words for every row cost more.
+template <class T, class R>
+struct Shared {
+    const float4 *w, *b;
+    int threads;
+    __device__ __forceinline__ Shared(const R& part, const heddle_layer_norm_args& a, float4* at)
+        : w(at), b(at + blockDim.x * (R::N / 4)), threads(blockDim.x) {
+        uint32_t r[R::kWords];
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            load_vector<T>(part, r, k ? a.bias : a.weight, k ? 0.0f : 1.0f);
+#pragma unroll
+            for (int q = 0; q < R::N / 4; ++q) {
+                const float2 x = pair_of<T>(r, 2 * q), y = pair_of<T>(r, 2 * q + 1);
+                at[(k * (R::N / 4) + q) * threads + threadIdx.x] = make_float4(x.x, x.y, y.x, y.y);
+            }
+        }
+    }
+    __device__ __forceinline__ void scale(const R&, uint32_t (&out)[R::kWords], const float2 (&v)[R::N / 2],
+                                          float rstd) const {
+        const float2 s = both(rstd);
+#pragma unroll
+        for (int q = 0; q < R::N / 4; ++q) {
+            const float4 wv = w[q * threads + threadIdx.x], bv = b[q * threads + threadIdx.x];
+            set_pair<T>(out, 2 * q, fma2(mul2(v[2 * q], s), make_float2(wv.x, wv.y), make_float2(bv.x, bv.y)));
+            set_pair<T>(out, 2 * q + 1, fma2(mul2(v[2 * q + 1], s), make_float2(wv.z, wv.w), make_float2(bv.z, bv.w)));
+        }
+    }
+};
+// 32-bit ones need no taking out and stay in registers.
+template <class T, class R, int GL>
+using Affine = typename std::conditional<GL != 0 || sizeof(T) == 4, Held<T, R>, Shared<T, R>>::type;
+template <class T>
+int affine_bytes(int threads, int units) {
+    return sizeof(T) == 4 ? 0 : 2 * threads * units * 16 * 2;
+}
+
+template <int GL>
+struct Total {
+    __device__ __forceinline__ float operator()(float v) const {
+        float one[1] = {v};
+        lanes_sum<GL>(one);
+        return one[0];
+    }
+};
+template <>
+struct Total<0> : BlockSum {};
+
+constexpr int kShort = 256;  // threads a block of short rows
+
+// GL lanes a row; GL 0: the block.
+template <class T, int GL, int U, bool STRIDED, int MOST>
+__global__ void __launch_bounds__(MOST, GL ? FWD_SHORT : 1024 / MOST)
     layer_norm_kernel(const __grid_constant__ heddle_layer_norm_args a, bool whole) {
+    extern __shared__ __align__(128) unsigned char shared[];
     allow_dependents();
     await_previous();
-    using R = RowPart<T, G, U, STRIDED>;
-    constexpr int kGroups = kBlock<G> / G;
-    const R part{(int)(threadIdx.x % G), (int)a.cols};
-    const float n_cols = (float)a.cols;
+    using R = RowPart<T, U, STRIDED>;
+    const int group = GL ? GL : blockDim.x, groups = GL ? MOST / GL : 1;
+    const R part{GL ? (int)threadIdx.x % GL : (int)threadIdx.x, group, (int)a.cols};
+    const float cols = (float)a.cols, inv = 1.0f / cols;
     const T* x = static_cast<const T*>(a.x);
-    uint4 w[U], b[U], now[U], next[U];
-    const int64_t step = (int64_t)gridDim.x * kGroups;
-    int64_t r = (int64_t)blockIdx.x * kGroups + threadIdx.x / G;
-    if (r >= a.rows) return;  // whole warps where a group is one
-    part.load(next, x + r * a.ldx, whole);
-    if (a.weight) part.load(w, static_cast<const T*>(a.weight), whole);
-    if (a.bias) part.load(b, static_cast<const T*>(a.bias), whole);
-    int turn = 0;
-    for (; r < a.rows; r += step) {
+    uint32_t now[R::kWords], next[R::kWords];
+    const int64_t step = (int64_t)gridDim.x * groups;
+    int64_t r = (int64_t)blockIdx.x * groups + (GL ? threadIdx.x / GL : 0);
+    T* y = static_cast<T*>(a.y) + r * a.ldy;
+    // rows past the last are the last again, not stored
+    x += (r < a.rows ? r : a.rows - 1) * a.ldx;
+    part.load(next, x, whole);
+    const Affine<T, R, GL> affine(part, a, reinterpret_cast<float4*>(shared));
+    Total<GL> total;
+    // a warp's groups go round together
+    for (int64_t first = (int64_t)blockIdx.x * groups; first < a.rows; first += step, r += step, y += step * a.ldy) {
+        float2 v[R::N / 2];
 #pragma unroll
-        for (int u = 0; u < U; ++u) now[u] = next[u];
-        if (r + step < a.rows) part.load(next, x + (r + step) * a.ldx, whole);
-        float sum[1] = {0.0f};
-#pragma unroll
-        for (int e = 0; e < R::N; ++e) sum[0] += R::get(now, e);
-        group_sum<G>(sum, turn);
-        const float mean = sum[0] / n_cols;
-        float sq[1] = {0.0f};
-#pragma unroll
-        for (int e = 0; e < R::N; ++e) {
-            const float d = part.in(e) ? R::get(now, e) - mean : 0.0f;
-            sq[0] = fmaf(d, d, sq[0]);
-        }
-        group_sum<G>(sq, turn);
-        const float rstd = 1.0f / sqrtf(sq[0] / n_cols + a.eps);
+        for (int i = 0; i < R::kWords; ++i) now[i] = next[i];
+        if (r + step < a.rows) x += step * a.ldx;
+        if (first + step < a.rows) part.load(next, x, whole);
+        const float mean = over(total(sum_of<T>(part, now)), cols, inv);
+        const float rstd = inv_sqrt(fmaf(total(squares_of<T, STRIDED>(part, now, v, mean)), inv, a.eps));
+        if (r >= a.rows) continue;
         if (a.mean && part.lane == 0) a.mean[r] = mean, a.rstd[r] = rstd;
-#pragma unroll
-        for (int e = 0; e < R::N; ++e) {
-            const float n = (R::get(now, e) - mean) * rstd;
-            R::set(now, e, fmaf(n, a.weight ? R::get(w, e) : 1.0f, a.bias ? R::get(b, e) : 0.0f));
-        }
-        part.store(static_cast<T*>(a.y) + r * a.ldy, now, whole);
+        affine.scale(part, now, v, rstd);
+        part.store(y, now, whole);
     }
 }
 
-// SUMS: with the sums over rows, partial[dw, db][block][cols].
-template <class T, int G, int U, bool STRIDED, bool SUMS>
-__global__ void __launch_bounds__(kBlock<G>)
+// The same by a block for rows that do not lie at 16 bytes: through the ring,
+// read from and written to memory in units all the same.
+template <class T, int U, int MOST>
+__global__ void __launch_bounds__(MOST, 1024 / MOST)
+    layer_norm_ring_kernel(const __grid_constant__ heddle_layer_norm_args a, int stages, bool staged, uint32_t* err) {
+    extern __shared__ __align__(128) unsigned char shared[];
+    allow_dependents();
+    await_previous();
+    using R = RowPart<T, U, false>;
+    const R part{(int)threadIdx.x, (int)blockDim.x, (int)a.cols};
+    const float cols = (float)a.cols, inv = 1.0f / cols;
+    const T* x = static_cast<const T*>(a.x);
+    Ring ring(shared + sizeof(RingBars), reinterpret_cast<RingBars*>(shared), 1, stages,
+              (int)(a.cols * (int64_t)sizeof(T)));
+    unsigned char* out = shared + sizeof(RingBars) + stages * ring.place;
+    const int rows = (int)((a.rows - blockIdx.x + gridDim.x - 1) / gridDim.x);
+    const int64_t step = gridDim.x * a.ldx;
+    x += blockIdx.x * a.ldx;
+    const T* ahead = x;
+    auto fetch = [&](int k) {
+        if (k < rows) ring.fetch(ahead, nullptr, nullptr);
+        ahead += step;
+    };
+    for (int k = 0; k < stages - 1; ++k) fetch(k);
+    const Affine<T, R, 0> affine(part, a, reinterpret_cast<float4*>(out + (staged ? ring.place : 0)));
+    T* y = static_cast<T*>(a.y) + blockIdx.x * a.ldy;
+    BlockSum total;
+    for (int k = 0; k < rows; ++k, x += step, y += gridDim.x * a.ldy) {
+        uint32_t words[R::kWords];
+        float2 v[R::N / 2];
+        ring.wait(0);
+        load_units<false>(words, part, ring.row(0, 0), low_of(x) & 15);
+        const float mean = over(total(sum_of<T>(part, words)), cols, inv);
+        fetch(k + stages - 1);  // all have read the row before this one
+        ring.advance(1);
+        const float rstd = inv_sqrt(fmaf(total(squares_of<T, true>(part, words, v, mean)), inv, a.eps));
+        if (a.mean && threadIdx.x == 0) {
+            const int64_t r = blockIdx.x + (int64_t)k * gridDim.x;
+            a.mean[r] = mean, a.rstd[r] = rstd;
+        }
+        affine.scale(part, words, v, rstd);
+        store_units<false>(y, part, words, staged ? out : nullptr);
+    }
+    ring.leave(err);
+}
+
+// --------------------------------------------------------------- gradients
+
+// A row's part in the two sums, and in those over rows.
+template <class T, class R>
+__device__ __forceinline__ void add_row(const R&, const uint32_t (&x)[R::kWords], const uint32_t (&g)[R::kWords],
+                                        const uint32_t (&w)[R::kWords], float mean, float rstd, bool live, float& sum0,
+                                        float& sum1, float2 (&dw)[R::N / 2], float2 (&db)[R::N / 2]) {
+    float2 s0 = both(0.0f), s1 = both(0.0f);
+    const float2 m = both(-mean), s = both(rstd);
+#pragma unroll
+    for (int p = 0; p < R::N / 2; ++p) {
+        // past the row's end dy is zero
+        const float2 n = mul2(plus<T>(x, p, m), s), f = pair_of<T>(g, p), t = times<T>(g, w, p);
+        s0 = add2(s0, t);
+        s1 = fma2(t, n, s1);
+        if (live) {
+            dw[p] = fma2(f, n, dw[p]);
+            db[p] = add2(db[p], f);
+        }
+    }
+    sum0 = s0.x + s0.y, sum1 = s1.x + s1.y;
+}
+// dx = rstd t - rstd mean(t) - (x - mean) rstd^2 mean(t n) + dres
+template <class T, class R>
+__device__ __forceinline__ void grad_row(const R&, uint32_t (&out)[R::kWords], const uint32_t (&x)[R::kWords],
+                                         const uint32_t (&g)[R::kWords], const uint32_t (&w)[R::kWords],
+                                         const uint32_t (&res)[R::kWords], float mean, float rstd, float mean0,
+                                         float mean1) {
+    const float2 m = both(-mean), s = both(rstd), c = both(-rstd * mean0), d = both(-rstd * rstd * mean1);
+#pragma unroll
+    for (int p = 0; p < R::N / 2; ++p)
+        set_pair<T>(out, p, plus<T>(res, p, fma2(times<T>(g, w, p), s, fma2(plus<T>(x, p, m), d, c))));
+}
+
+// With the sums over rows, partial[dw, db][block][cols].
+template <class T, int GL, int U, bool STRIDED>
+__global__ void __launch_bounds__(kShort, 2)
     layer_norm_grad_kernel(const __grid_constant__ heddle_layer_norm_grad_args a, float* partial, bool whole) {
     allow_dependents();
     await_previous();
-    using R = RowPart<T, G, U, STRIDED>;
-    constexpr int kGroups = kBlock<G> / G;
-    const R part{(int)(threadIdx.x % G), (int)a.cols};
-    const float n_cols = (float)a.cols;
+    using R = RowPart<T, U, STRIDED>;
+    constexpr int kGroups = kShort / GL;
+    const R part{(int)threadIdx.x % GL, GL, (int)a.cols};
+    const float cols = (float)a.cols, inv = 1.0f / cols;
     const T *x = static_cast<const T*>(a.x), *dy = static_cast<const T*>(a.dy), *dres = static_cast<const T*>(a.dres);
-    uint4 w[U], xv[U], gv[U], rv[U];
-    float dw[SUMS ? R::N : 1] = {}, db[SUMS ? R::N : 1] = {};
-    if (a.weight) part.load(w, static_cast<const T*>(a.weight), whole);
-    int turn = 0;
+    uint32_t w[R::kWords], xv[R::kWords], gv[R::kWords], rv[R::kWords] = {};
+    float2 dw[R::N / 2], db[R::N / 2];
+#pragma unroll
+    for (int p = 0; p < R::N / 2; ++p) dw[p] = db[p] = both(0.0f);
+    load_vector<T>(part, w, a.weight, 1.0f);
     const int64_t step = (int64_t)gridDim.x * kGroups;
-    for (int64_t r = (int64_t)blockIdx.x * kGroups + threadIdx.x / G; r < a.rows; r += step) {
-        part.load(xv, x + r * a.ldx, whole);
-        part.load(gv, dy + r * a.lddy, whole);
-        if (dres && a.dx) part.load(rv, dres + r * a.ldr, whole);
-        const float mean = a.mean[r], rstd = a.rstd[r];
-        float s[2] = {0.0f, 0.0f};
-#pragma unroll
-        for (int e = 0; e < R::N; ++e) {
-            // past the row's end dy and the weight are zeros
-            const float n = (R::get(xv, e) - mean) * rstd, g = R::get(gv, e);
-            const float t = a.weight ? __fmul_rn(g, R::get(w, e)) : g;
-            s[0] += t;
-            s[1] = fmaf(t, part.in(e) ? n : 0.0f, s[1]);
-            if constexpr (SUMS) {
-                dw[e] = fmaf(g, n, dw[e]);
-                db[e] += g;
-            }
-        }
-        if (!a.dx) continue;
-        group_sum<G>(s, turn);
-        s[0] /= n_cols, s[1] /= n_cols;
-#pragma unroll
-        for (int e = 0; e < R::N; ++e) {
-            const float n = (R::get(xv, e) - mean) * rstd, g = R::get(gv, e);
-            const float t = a.weight ? __fmul_rn(g, R::get(w, e)) : g;
-            R::set(gv, e, fmaf(rstd, fmaf(-n, s[1], t - s[0]), dres ? R::get(rv, e) : 0.0f));
-        }
+    int64_t r = (int64_t)blockIdx.x * kGroups + threadIdx.x / GL;
+    for (int64_t first = (int64_t)blockIdx.x * kGroups; first < a.rows; first += step, r += step) {
+        const bool live = r < a.rows;
+        const int64_t at = live ? r : a.rows - 1;
+        part.load(xv, x + at * a.ldx, whole);
+        part.load(gv, dy + at * a.lddy, whole);
+        if (dres && a.dx) part.load(rv, dres + at * a.ldr, whole);
+        const float mean = a.mean[at], rstd = a.rstd[at];
+        float v[2];
+        add_row<T>(part, xv, gv, w, mean, rstd, live, v[0], v[1], dw, db);
+        lanes_sum<GL>(v);
+        if (!a.dx || !live) continue;
+        grad_row<T>(part, gv, xv, gv, w, rv, mean, rstd, v[0] * inv, v[1] * inv);
         part.store(static_cast<T*>(a.dx) + r * a.lddx, gv, whole);
     }
-    if constexpr (SUMS) {
-        float *pw = partial + (int64_t)blockIdx.x * a.cols, *pb = pw + (int64_t)gridDim.x * a.cols;
-        if constexpr (G > 32) {
+    // the block's groups, in order
+    __shared__ float sums[kGroups][GL * R::N];
 #pragma unroll
-            for (int e = 0; e < R::N; ++e)
-                if (part.in(e)) pw[part.at(e)] = dw[e], pb[part.at(e)] = db[e];
-        } else {  // the block's groups, in order
-            __shared__ float s[kGroups][G * R::N];
+    for (int k = 0; k < 2; ++k) {
+        __syncthreads();
 #pragma unroll
-            for (int k = 0; k < 2; ++k) {
-                __syncthreads();
+        for (int p = 0; p < R::N / 2; ++p) {
+            const float2 v = k ? db[p] : dw[p];
+            sums[threadIdx.x / GL][part.at(2 * p)] = v.x, sums[threadIdx.x / GL][part.at(2 * p + 1)] = v.y;
+        }
+        __syncthreads();
+        for (int i = threadIdx.x; i < a.cols; i += kShort) {
+            float v = 0.0f;
 #pragma unroll
-                for (int e = 0; e < R::N; ++e) s[threadIdx.x / G][part.at(e)] = k ? db[e] : dw[e];
-                __syncthreads();
-                for (int i = threadIdx.x; i < a.cols; i += kBlock<G>) {
-                    float v = 0.0f;
-#pragma unroll
-                    for (int g = 0; g < kGroups; ++g) v += s[g][i];
-                    (k ? pb : pw)[i] = v;
-                }
-            }
+            for (int g = 0; g < kGroups; ++g) v += sums[g][i];
+            partial[((int64_t)k * gridDim.x + blockIdx.x) * a.cols + i] = v;
         }
     }
 }
 
-// ------------------------------------------------- rows beyond the registers
+// A block a row, x, dy and dres through the ring; they are read from it once
+// for the sums and once more for dx.  ROWS at a time between two barriers: two
+// where that leaves four ahead (26214 x 5120 bfloat16: 165 us, one at a time
+// 182), one where the slots are few (16384 x 8192: 168 us, two 189).
+template <class T, int U, bool WHOLE, int ROWS, int MOST>
+__global__ void __launch_bounds__(MOST)
+    layer_norm_grad_ring_kernel(const __grid_constant__ heddle_layer_norm_grad_args a, float* partial, int stages,
+                                int arrays, bool staged, uint32_t* err) {
+    extern __shared__ __align__(128) unsigned char shared[];
+    allow_dependents();
+    await_previous();
+    using R = RowPart<T, U, false>;
+    const R part{(int)threadIdx.x, (int)blockDim.x, (int)a.cols};
+    const float inv = 1.0f / (float)a.cols;
+    const T *x = static_cast<const T*>(a.x), *dy = static_cast<const T*>(a.dy),
+            *dres = a.dx ? static_cast<const T*>(a.dres) : nullptr;
+    Ring ring(shared + sizeof(RingBars), reinterpret_cast<RingBars*>(shared), arrays, stages,
+              (int)(a.cols * (int64_t)sizeof(T)));
+    unsigned char* out = shared + sizeof(RingBars) + stages * arrays * ring.place;
+    const int rows = (int)((a.rows - blockIdx.x + gridDim.x - 1) / gridDim.x);
+    const int64_t xs = gridDim.x * a.ldx, gs = gridDim.x * a.lddy, rs = gridDim.x * a.ldr, ds = gridDim.x * a.lddx;
+    x += blockIdx.x * a.ldx, dy += blockIdx.x * a.lddy;
+    if (dres) dres += blockIdx.x * a.ldr;
+    T* dx = a.dx ? static_cast<T*>(a.dx) + blockIdx.x * a.lddx : nullptr;
+    // where rows lie modulo 16 bytes: those at hand, and their steps
+    uint32_t xl = low_of(x), gl = low_of(dy), rl = low_of(dres);
+    const uint32_t xd = (uint32_t)(xs * sizeof(T)), gd = (uint32_t)(gs * sizeof(T)), rd = (uint32_t)(rs * sizeof(T));
+    auto fetch = [&](int k) {
+        if (k < rows) ring.fetch(x, dy, dres);
+        x += xs, dy += gs;
+        if (dres) dres += rs;
+    };
+    for (int k = 0; k < stages - ROWS; ++k) fetch(k);
+    uint32_t w[R::kWords];
+    float2 dw[R::N / 2], db[R::N / 2];
+#pragma unroll
+    for (int p = 0; p < R::N / 2; ++p) dw[p] = db[p] = both(0.0f);
+    load_vector<T>(part, w, a.weight, 1.0f);
+    float mean[ROWS], rstd[ROWS];
+    auto statistics = [&](int k) {
+#pragma unroll
+        for (int i = 0; i < ROWS; ++i) {
+            const int64_t r = blockIdx.x + (int64_t)(k + i < rows ? k + i : rows - 1) * gridDim.x;
+            mean[i] = a.mean[r], rstd[i] = a.rstd[r];
+        }
+    };
+    statistics(0);
+    int turn = 0;
+    for (int k = 0; k < rows; k += ROWS) {
+        float v[2 * ROWS] = {}, m[ROWS], s[ROWS];
+        const unsigned char* at[ROWS][3];
+#pragma unroll
+        for (int i = 0; i < ROWS; ++i) {
+            m[i] = mean[i], s[i] = rstd[i];
+#pragma unroll
+            for (int j = 0; j < 3; ++j) at[i][j] = ring.row(i, j);
+        }
+        statistics(k + ROWS);
+#pragma unroll
+        for (int i = 0; i < ROWS; ++i) {
+            if (k + i >= rows) break;
+            ring.wait(i);
+            uint32_t xv[R::kWords], gv[R::kWords];
+            load_units<WHOLE>(xv, part, at[i][0], xl + i * xd & 15);
+            load_units<WHOLE>(gv, part, at[i][1], gl + i * gd & 15);
+            add_row<T>(part, xv, gv, w, m[i], s[i], true, v[2 * i], v[2 * i + 1], dw, db);
+        }
+        if constexpr (ROWS == 1)
+            block_sums(v[0], v[1], turn);
+        else
+            block_sums(v, turn);
+#pragma unroll
+        for (int i = 0; i < ROWS; ++i) fetch(k + stages - ROWS + i);  // in the place of rows that all have left
+        ring.advance(ROWS);
+        if (dx) {
+#pragma unroll
+            for (int i = 0; i < ROWS; ++i, dx += ds) {
+                if (k + i >= rows) break;
+                uint32_t xv[R::kWords], gv[R::kWords], rv[R::kWords] = {};
+                load_units<WHOLE>(xv, part, at[i][0], xl + i * xd & 15);
+                load_units<WHOLE>(gv, part, at[i][1], gl + i * gd & 15);
+                if (dres) load_units<WHOLE>(rv, part, at[i][2], rl + i * rd & 15);
+                grad_row<T>(part, gv, xv, gv, w, rv, m[i], s[i], v[2 * i] * inv, v[2 * i + 1] * inv);
+                if (!WHOLE && i) __syncthreads();  // the row before has left its place on its way out
+                store_units<WHOLE>(dx, part, gv, staged ? out : nullptr);
+            }
+        }
+        xl += ROWS * xd, gl += ROWS * gd, rl += ROWS * rd;
+    }
+    if (partial) {
+        float *pw = partial + (int64_t)blockIdx.x * a.cols, *pb = pw + (int64_t)gridDim.x * a.cols;
+#pragma unroll
+        for (int p = 0; p < R::N / 2; ++p) {
+            const int i = part.at(2 * p);
+            if (i < a.cols) pw[i] = dw[p].x, pb[i] = db[p].x;
+            if (i + 1 < a.cols) pw[i + 1] = dw[p].y, pb[i + 1] = db[p].y;
+        }
+    }
+    ring.leave(err);
+}
+
+// ------------------------------------------- rows beyond registers or the ring
 
 constexpr int kLong = 1024;
 
@@ -163,21 +500,19 @@ template <class T>
 __global__ void __launch_bounds__(kLong) layer_norm_long_kernel(const __grid_constant__ heddle_layer_norm_args a) {
     allow_dependents();
     await_previous();
-    const float n_cols = (float)a.cols;
-    int turn = 0;
+    const float cols = (float)a.cols, inv = 1.0f / cols;
+    BlockSum total;
     for (int64_t r = blockIdx.x; r < a.rows; r += gridDim.x) {
         const T* x = static_cast<const T*>(a.x) + r * a.ldx;
         T* y = static_cast<T*>(a.y) + r * a.ldy;
-        float sum[1] = {0.0f}, sq[1] = {0.0f};
-        for (int64_t i = threadIdx.x; i < a.cols; i += kLong) sum[0] += to_float(x[i]);
-        group_sum<kLong>(sum, turn);
-        const float mean = sum[0] / n_cols;
+        float sum = 0.0f, sq = 0.0f;
+        for (int64_t i = threadIdx.x; i < a.cols; i += kLong) sum += to_float(x[i]);
+        const float mean = over(total(sum), cols, inv);
         for (int64_t i = threadIdx.x; i < a.cols; i += kLong) {
             const float d = to_float(x[i]) - mean;
-            sq[0] = fmaf(d, d, sq[0]);
+            sq = fmaf(d, d, sq);
         }
-        group_sum<kLong>(sq, turn);
-        const float rstd = 1.0f / sqrtf(sq[0] / n_cols + a.eps);
+        const float rstd = inv_sqrt(fmaf(total(sq), inv, a.eps));
         if (a.mean && threadIdx.x == 0) a.mean[r] = mean, a.rstd[r] = rstd;
         for (int64_t i = threadIdx.x; i < a.cols; i += kLong) {
             const float n = (to_float(x[i]) - mean) * rstd;
@@ -192,7 +527,7 @@ __global__ void __launch_bounds__(kLong)
     layer_norm_long_grad_kernel(const __grid_constant__ heddle_layer_norm_grad_args a) {
     allow_dependents();
     await_previous();
-    const float n_cols = (float)a.cols;
+    const float cols = (float)a.cols, inv = 1.0f / cols;
     const T* w = static_cast<const T*>(a.weight);
     int turn = 0;
     for (int64_t r = blockIdx.x; r < a.rows; r += gridDim.x) {
@@ -206,8 +541,8 @@ __global__ void __launch_bounds__(kLong)
             s[0] += t;
             s[1] = fmaf(t, (to_float(x[i]) - mean) * rstd, s[1]);
         }
-        group_sum<kLong>(s, turn);
-        s[0] /= n_cols, s[1] /= n_cols;
+        block_sums(s[0], s[1], turn);
+        s[0] *= inv, s[1] *= inv;
         for (int64_t i = threadIdx.x; i < a.cols; i += kLong) {
             const float t = to_float(dy[i]) * (w ? to_float(w[i]) : 1.0f), n = (to_float(x[i]) - mean) * rstd;
             dx[i] = from_float<T>(fmaf(rstd, fmaf(-n, s[1], t - s[0]), a.dres ? to_float(dres[i]) : 0.0f));
@@ -236,23 +571,27 @@ __global__ void __launch_bounds__(256)
 }
 
 // The blocks' sums, 32 columns of dw or dbias a block.
-__global__ void __launch_bounds__(1024)
+constexpr int kJoin = 8;  // warps
+__global__ void __launch_bounds__(32 * kJoin)
     layer_norm_join_kernel(const float* partial, int blocks, int64_t cols, float* dw, float* dbias) {
     allow_dependents();
     await_previous();
-    __shared__ float s[32][33];
+    __shared__ float s[kJoin][32];
     const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
     const int64_t i = (int64_t)blockIdx.x * 32 + lane;
     float* out = blockIdx.y ? dbias : dw;
     if (!out) return;
     float v = 0.0f;
-    if (i < cols)
-#pragma unroll 8
-        for (int b = warp; b < blocks; b += 32) v += partial[((int64_t)blockIdx.y * blocks + b) * cols + i];
+    if (i < cols) {
+        const float* p = partial + (int64_t)blockIdx.y * blocks * cols + i;
+#pragma unroll 16
+        for (int b = warp; b < blocks; b += kJoin) v += p[b * cols];
+    }
     s[warp][lane] = v;
     __syncthreads();
     if (warp == 0 && i < cols) {
-        for (int k = 1; k < 32; ++k) v += s[k][lane];
+#pragma unroll
+        for (int k = 1; k < kJoin; ++k) v += s[k][lane];
         out[i] = v;
     }
 }
@@ -260,114 +599,215 @@ __global__ void __launch_bounds__(1024)
 // -------------------------------------------------------------------- launches
 
 int size_of(int32_t dtype) { return dtype == HEDDLE_FP32 ? 4 : 2; }
-
-// Threads a row, by the 16-byte units that it takes: up to two a thread, in
-// warps where they do; 0: beyond the registers.
-int group_of(int64_t cols, int32_t dtype) {
-    const int64_t units = ceil_div(cols, 16 / size_of(dtype));
-    return units <= 64 ? 32 : units <= 256 ? 128 : units <= 512 ? 256 : units <= 1024 ? 512 : units <= 2048 ? 1024 : 0;
-}
-
 int64_t at_most(int64_t want, int64_t most) { return want < most ? want : most; }
 
-int64_t blocks_of(const OpContext& x, int64_t rows, int group, int threads_an_sm) {
-    if (!group) return at_most(rows, (int64_t)x.num_sms * 2);
-    const int block = group == 32 ? 256 : group;
-    return at_most(ceil_div(rows, block / group), (int64_t)x.num_sms * (threads_an_sm / block));
+constexpr int kShared = 208 * 1024;  // of an SM's, shared by the blocks that it runs
+
+// How a call's rows are taken.  What the order of sums depends on goes by sizes
+// alone.
+enum Way { kLanes, kBlocks, kRing, kLongRows };
+struct Plan {
+    Way way;
+    bool strided;      // a short row's values are dealt out one by one
+    bool whole;        // whole units at 16 bytes throughout
+    bool staged;       // rows leave by way of shared memory
+    int lanes, units;  // of a short row: lanes, units each
+    int threads, stages;
+    size_t shared;
+    int64_t blocks;
+};
+
+// Short rows: up to 64 units, of which a lane has one, or two of 32 lanes.
+void plan_short(const OpContext& x, Plan& p, int64_t rows, int64_t units, int threads_an_sm) {
+    p.way = kLanes;
+    p.lanes = units <= 4 ? 4 : units <= 8 ? 8 : units <= 16 ? 16 : 32;
+    p.units = units <= 32 ? 1 : 2;
+    p.threads = kShort;
+    p.blocks = at_most(ceil_div(rows, kShort / p.lanes), (int64_t)x.num_sms * (threads_an_sm / kShort));
 }
 
-// Rows that a block of the sums beyond the registers takes are those of its
-// place among so many.
+// `arrays` of rows through the ring, by up to `an_sm` blocks an SM: as many as
+// leave each three slots of `most` arrays.  `fixed`: shared memory beside it.
+void plan_ring(Plan& p, int64_t row_bytes, int arrays, int most, bool whole, int fixed, int& an_sm) {
+    const int64_t place = row_place(row_bytes);
+    auto stages = [&](int n, bool out) {
+        return (kShared / an_sm - (int64_t)sizeof(RingBars) - fixed - (out ? place : 0)) / (n * place);
+    };
+    while (an_sm > 1 && stages(most, true) < 3) --an_sm;
+    p.way = stages(most, false) >= 2 ? kRing : kLongRows;
+    p.staged = !whole && stages(arrays, true) >= 2;
+    p.stages = (int)at_most(stages(arrays, p.staged), kRingStages);
+    p.shared = sizeof(RingBars) + fixed + (p.stages * arrays + p.staged) * place;
+}
+
+constexpr int kEach = 2;  // units a thread of a block holds
+int block_of(int64_t units) { return (int)at_most(ceil_div(ceil_div(units, kEach), 32) * 32, kLong); }
+int blocks_an_sm(int threads_an_sm, int threads) {
+    const int n = threads_an_sm / threads;
+    return n < 1 ? 1 : n > 24 ? 24 : n;
+}
+
+template <class T>
+Plan plan_forward(const OpContext& x, const heddle_layer_norm_args& a) {
+    Plan p{};
+    constexpr int size = sizeof(T), V = 16 / size;
+    const int64_t units = ceil_div(a.cols, V);
+    p.strided = a.cols % V != 0;
+    if (units <= 64) {
+        plan_short(x, p, a.rows, units, 256 * FWD_SHORT);
+        return p;
+    }
+    const bool whole = !p.strided && rows_whole(a.x, a.ldx, a.rows, size) && rows_whole(a.y, a.ldy, a.rows, size);
+    p.threads = block_of(units);
+    p.way = units > kEach * kLong ? kLongRows : kBlocks;
+    p.shared = affine_bytes<T>(p.threads, kEach);
+    int an_sm = blocks_an_sm(FWD_THREADS, p.threads);
+    if (p.way == kBlocks && !whole) plan_ring(p, a.cols * size, 1, 1, false, (int)p.shared, an_sm);
+    if (p.way == kLongRows) p.threads = kLong, an_sm = 2;
+    p.blocks = at_most(a.rows, (int64_t)x.num_sms * an_sm);
+    return p;
+}
+
+// Rows that a block of the sums beyond the ring takes are those of its place
+// among so many.
 int64_t long_parts(int64_t rows) { return at_most(rows, 32); }
 
-constexpr int kFwdThreads = 1024, kGradThreads = 1024;  // an SM
-
-template <class T, bool STRIDED>
-cudaError_t forward(const OpContext& x, const heddle_layer_norm_args& a, cudaStream_t st) {
-    const int group = group_of(a.cols, a.dtype), size = sizeof(T);
-    const dim3 grid((unsigned)blocks_of(x, a.rows, group, kFwdThreads));
-    const bool whole = rows_whole(a.x, a.ldx, a.rows, size) && rows_whole(a.y, a.ldy, a.rows, size) &&
-                       rows_whole(a.weight, 0, 1, size) && rows_whole(a.bias, 0, 1, size);
-    switch (group) {
-        case 32: return launch(x, layer_norm_kernel<T, 32, 2, STRIDED>, grid, 256, 0, st, a, whole);
-        case 128: return launch(x, layer_norm_kernel<T, 128, 2, STRIDED>, grid, 128, 0, st, a, whole);
-        case 256: return launch(x, layer_norm_kernel<T, 256, 2, STRIDED>, grid, 256, 0, st, a, whole);
-        case 512: return launch(x, layer_norm_kernel<T, 512, 2, STRIDED>, grid, 512, 0, st, a, whole);
-        case 1024: return launch(x, layer_norm_kernel<T, 1024, 2, STRIDED>, grid, 1024, 0, st, a, whole);
-        default: return launch(x, layer_norm_long_kernel<T>, grid, kLong, 0, st, a);
+Plan plan_grad(const OpContext& x, const heddle_layer_norm_grad_args& a) {
+    Plan p{};
+    const int size = size_of(a.dtype), V = 16 / size;
+    const int64_t units = ceil_div(a.cols, V);
+    p.strided = a.cols % V != 0;
+    if (units <= 64) {
+        plan_short(x, p, a.rows, units, 512);
+        return p;
     }
+    p.threads = block_of(units);
+    p.way = kLongRows;
+    int an_sm = blocks_an_sm(size == 4 ? GRAD32 : GRAD_THREADS, p.threads);
+    p.whole = !p.strided && rows_whole(a.x, a.ldx, a.rows, size) && rows_whole(a.dy, a.lddy, a.rows, size) &&
+              rows_whole(a.dres, a.ldr, a.rows, size) && rows_whole(a.dx, a.lddx, a.rows, size);
+    if (units <= kEach * kLong) plan_ring(p, a.cols * size, a.dres ? 3 : 2, 3, p.whole, 0, an_sm);
+    if (p.way == kLongRows) p.threads = kLong, an_sm = 2;
+    p.blocks = at_most(a.rows, (int64_t)x.num_sms * an_sm);
+    return p;
 }
 
-template <class T, bool STRIDED, bool SUMS>
-cudaError_t backward(const OpContext& x, const heddle_layer_norm_grad_args& a, float* partial, unsigned blocks,
-                     cudaStream_t st) {
-    const int size = sizeof(T);
+template <class K, class... A>
+cudaError_t launch_planned(const OpContext& x, K* kernel, std::atomic<uint64_t>& asked, const Plan& p, cudaStream_t st,
+                           A... args) {
+    const cudaError_t e = allow_shared(kernel, kShared, x.device, asked);
+    if (e != cudaSuccess) return e;
+    return launch(x, kernel, dim3((unsigned)p.blocks), p.threads, p.shared, st, args...);
+}
+
+template <class T, bool STRIDED>
+cudaError_t forward_short(const OpContext& x, const heddle_layer_norm_args& a, const Plan& p, cudaStream_t st) {
+    constexpr int size = sizeof(T);
+    const bool whole = rows_whole(a.x, a.ldx, a.rows, size) && rows_whole(a.y, a.ldy, a.rows, size);
+    auto* kernel = p.lanes == 4    ? layer_norm_kernel<T, 4, 1, STRIDED, kShort>
+                   : p.lanes == 8  ? layer_norm_kernel<T, 8, 1, STRIDED, kShort>
+                   : p.lanes == 16 ? layer_norm_kernel<T, 16, 1, STRIDED, kShort>
+                   : p.units == 1  ? layer_norm_kernel<T, 32, 1, STRIDED, kShort>
+                                   : layer_norm_kernel<T, 32, 2, STRIDED, kShort>;
+    return launch(x, kernel, dim3((unsigned)p.blocks), kShort, 0, st, a, whole);
+}
+
+template <class T, int MOST>
+cudaError_t forward_blocks(const OpContext& x, const heddle_layer_norm_args& a, const Plan& p, cudaStream_t st) {
+    static std::atomic<uint64_t> asked[2];
+    if (p.way == kRing)
+        return launch_planned(x, layer_norm_ring_kernel<T, kEach, MOST>, asked[0], p, st, a, p.stages, p.staged, x.err);
+    return launch_planned(x, layer_norm_kernel<T, 0, kEach, false, MOST>, asked[1], p, st, a, true);
+}
+
+template <class T>
+cudaError_t forward_typed(const OpContext& x, const heddle_layer_norm_args& a, cudaStream_t st) {
+    const Plan p = plan_forward<T>(x, a);
+    if (p.way == kLanes) return p.strided ? forward_short<T, true>(x, a, p, st) : forward_short<T, false>(x, a, p, st);
+    if (p.way == kLongRows) return launch(x, layer_norm_long_kernel<T>, dim3((unsigned)p.blocks), kLong, 0, st, a);
+    return p.threads <= 512 ? forward_blocks<T, 512>(x, a, p, st) : forward_blocks<T, 1024>(x, a, p, st);
+}
+
+template <class T, bool STRIDED>
+cudaError_t backward_short(const OpContext& x, const heddle_layer_norm_grad_args& a, const Plan& p, float* partial,
+                           cudaStream_t st) {
+    constexpr int size = sizeof(T);
     const bool whole = rows_whole(a.x, a.ldx, a.rows, size) && rows_whole(a.dy, a.lddy, a.rows, size) &&
-                       rows_whole(a.dres, a.ldr, a.rows, size) && rows_whole(a.dx, a.lddx, a.rows, size) &&
-                       rows_whole(a.weight, 0, 1, size);
-    const dim3 grid(blocks);
-    switch (group_of(a.cols, a.dtype)) {
-        case 32: return launch(x, layer_norm_grad_kernel<T, 32, 2, STRIDED, SUMS>, grid, 256, 0, st, a, partial, whole);
-        case 128:
-            return launch(x, layer_norm_grad_kernel<T, 128, 2, STRIDED, SUMS>, grid, 128, 0, st, a, partial, whole);
-        case 256:
-            return launch(x, layer_norm_grad_kernel<T, 256, 2, STRIDED, SUMS>, grid, 256, 0, st, a, partial, whole);
-        case 512:
-            return launch(x, layer_norm_grad_kernel<T, 512, 2, STRIDED, SUMS>, grid, 512, 0, st, a, partial, whole);
-        default:
-            return launch(x, layer_norm_grad_kernel<T, 1024, 2, STRIDED, SUMS>, grid, 1024, 0, st, a, partial, whole);
-    }
+                       rows_whole(a.dres, a.ldr, a.rows, size) && rows_whole(a.dx, a.lddx, a.rows, size);
+    auto* kernel = p.lanes == 4    ? layer_norm_grad_kernel<T, 4, 1, STRIDED>
+                   : p.lanes == 8  ? layer_norm_grad_kernel<T, 8, 1, STRIDED>
+                   : p.lanes == 16 ? layer_norm_grad_kernel<T, 16, 1, STRIDED>
+                   : p.units == 1  ? layer_norm_grad_kernel<T, 32, 1, STRIDED>
+                                   : layer_norm_grad_kernel<T, 32, 2, STRIDED>;
+    return launch(x, kernel, dim3((unsigned)p.blocks), kShort, 0, st, a, partial, whole);
+}
+
+template <class T, bool WHOLE>
+cudaError_t backward_ring(const OpContext& x, const heddle_layer_norm_grad_args& a, const Plan& p, float* partial,
+                          cudaStream_t st) {
+    static std::atomic<uint64_t> asked[3];
+    const int arrays = a.dres ? 3 : 2;
+    if (p.threads > 512)
+        return launch_planned(x, layer_norm_grad_ring_kernel<T, kEach, WHOLE, 1, 1024>, asked[0], p, st, a, partial,
+                              p.stages, arrays, p.staged, x.err);
+    if (p.stages < 6)
+        return launch_planned(x, layer_norm_grad_ring_kernel<T, kEach, WHOLE, 1, 512>, asked[1], p, st, a, partial,
+                              p.stages, arrays, p.staged, x.err);
+    return launch_planned(x, layer_norm_grad_ring_kernel<T, kEach, WHOLE, 2, 512>, asked[2], p, st, a, partial,
+                          p.stages, arrays, p.staged, x.err);
+}
+
+template <class T>
+cudaError_t backward_rows(const OpContext& x, const heddle_layer_norm_grad_args& a, const Plan& p, float* partial,
+                          cudaStream_t st) {
+    if (p.way == kLanes)
+        return p.strided ? backward_short<T, true>(x, a, p, partial, st)
+                         : backward_short<T, false>(x, a, p, partial, st);
+    return p.whole ? backward_ring<T, true>(x, a, p, partial, st) : backward_ring<T, false>(x, a, p, partial, st);
 }
 
 template <class T>
 cudaError_t backward_typed(const OpContext& x, const heddle_layer_norm_grad_args& a, float* partial, cudaStream_t st) {
-    const int group = group_of(a.cols, a.dtype);
-    const bool sums = a.dw || a.dbias, strided = a.cols % (16 / (int)sizeof(T)) != 0;
-    unsigned blocks = (unsigned)blocks_of(x, a.rows, group, kGradThreads);
+    const Plan p = plan_grad(x, a);
+    const bool sums = a.dw || a.dbias;
+    int64_t parts = a.rows ? p.blocks : 0;
     cudaError_t e = cudaSuccess;
-    if (!group) {  // the sums first: dx may take dy's place
-        const unsigned rows = blocks;
-        blocks = (unsigned)long_parts(a.rows);
-        const dim3 grid((unsigned)ceil_div(a.cols, 256), blocks);
+    if (p.way == kLongRows) {  // the sums first: dx may take dy's place
+        parts = long_parts(a.rows);
+        const dim3 grid((unsigned)ceil_div(a.cols, 256), (unsigned)parts);
         if (sums && a.rows) e = launch(x, layer_norm_long_sums_kernel<T>, grid, 256, 0, st, a, partial);
         if (e == cudaSuccess && a.dx && a.rows)
-            e = launch(x, layer_norm_long_grad_kernel<T>, dim3(rows), kLong, 0, st, a);
+            e = launch(x, layer_norm_long_grad_kernel<T>, dim3((unsigned)p.blocks), kLong, 0, st, a);
     } else if (a.rows) {
-        if (sums)
-            e = strided ? backward<T, true, true>(x, a, partial, blocks, st)
-                        : backward<T, false, true>(x, a, partial, blocks, st);
-        else
-            e = strided ? backward<T, true, false>(x, a, partial, blocks, st)
-                        : backward<T, false, false>(x, a, partial, blocks, st);
+        e = backward_rows<T>(x, a, p, partial, st);
     }
     if (e == cudaSuccess && sums)
-        e = launch(x, layer_norm_join_kernel, dim3((unsigned)ceil_div(a.cols, 32), 2), 1024, 0, st, partial,
-                   (int)(a.rows ? blocks : 0), a.cols, a.dw, a.dbias);
+        e = launch(x, layer_norm_join_kernel, dim3((unsigned)ceil_div(a.cols, 32), 2), 32 * kJoin, 0, st,
+                   (const float*)partial, (int)parts, a.cols, a.dw, a.dbias);
     return e;
 }
 
 }  // namespace
 
 cudaError_t launch_layer_norm(const OpContext& x, const heddle_layer_norm_args& a, cudaStream_t st) {
-    const bool strided = a.cols % (16 / size_of(a.dtype)) != 0;
     switch (a.dtype) {
-        case HEDDLE_BF16:
-            return strided ? forward<__nv_bfloat16, true>(x, a, st) : forward<__nv_bfloat16, false>(x, a, st);
-        case HEDDLE_FP16: return strided ? forward<__half, true>(x, a, st) : forward<__half, false>(x, a, st);
-        default: return strided ? forward<float, true>(x, a, st) : forward<float, false>(x, a, st);
+        case HEDDLE_BF16: return forward_typed<__nv_bfloat16>(x, a, st);
+        case HEDDLE_FP16: return forward_typed<__half>(x, a, st);
+        default: return forward_typed<float>(x, a, st);
     }
 }
 
 size_t layer_norm_grad_scratch(const OpContext& x, const heddle_layer_norm_grad_args& a) {
-    if (!a.dw && !a.dbias) return 0;
-    const int group = group_of(a.cols, a.dtype);
-    const int64_t parts = group ? blocks_of(x, a.rows, group, kGradThreads) : long_parts(a.rows);
-    return align256(sizeof(float) * 2 * (size_t)parts * a.cols);
+    const Plan p = plan_grad(x, a);
+    // a short row's kernel writes its sums whether they are asked for or not
+    if (!a.dw && !a.dbias && p.way != kLanes) return 0;
+    return align256(sizeof(float) * 2 * (size_t)(p.way == kLongRows ? long_parts(a.rows) : p.blocks) * a.cols);
 }
 
 cudaError_t launch_layer_norm_grad(const OpContext& x, const heddle_layer_norm_grad_args& a, unsigned char* ws,
                                    cudaStream_t st) {
-    float* partial = reinterpret_cast<float*>(ws);
+    const Plan p = plan_grad(x, a);
+    float* partial = a.dw || a.dbias || p.way == kLanes ? reinterpret_cast<float*>(ws) : nullptr;
     switch (a.dtype) {
         case HEDDLE_BF16: return backward_typed<__nv_bfloat16>(x, a, partial, st);
         case HEDDLE_FP16: return backward_typed<__half>(x, a, partial, st);

@@ -100,6 +100,57 @@ __device__ __forceinline__ __nv_bfloat16 from_float(float v) { return __float2bf
 template <>
 __device__ __forceinline__ __half from_float(float v) { return __float2half_rn(v); }
 
+// Two 16-bit values of a word, the first in its lower half, at once.
+template <class T>
+__device__ __forceinline__ float2 to_floats(uint32_t w);
+template <>
+__device__ __forceinline__ float2 to_floats<__nv_bfloat16>(uint32_t w) {
+    return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xffff0000u));
+}
+template <>
+__device__ __forceinline__ float2 to_floats<__half>(uint32_t w) {
+    return __half22float2(*reinterpret_cast<const __half2*>(&w));
+}
+template <class T>
+__device__ __forceinline__ uint32_t from_floats(float a, float b);
+template <>
+__device__ __forceinline__ uint32_t from_floats<__nv_bfloat16>(float a, float b) {
+    const __nv_bfloat162 v = __floats2bfloat162_rn(a, b);
+    return *reinterpret_cast<const uint32_t*>(&v);
+}
+template <>
+__device__ __forceinline__ uint32_t from_floats<__half>(float a, float b) {
+    const __half2 v = __floats2half2_rn(a, b);
+    return *reinterpret_cast<const uint32_t*>(&v);
+}
+
+// The values of a 16-byte unit, and back.
+template <class T>
+__device__ __forceinline__ void unpack(const uint4& u, float (&v)[16 / sizeof(T)]) {
+    const uint32_t* w = reinterpret_cast<const uint32_t*>(&u);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if constexpr (sizeof(T) == 4) {
+            v[i] = __uint_as_float(w[i]);
+        } else {
+            const float2 f = to_floats<T>(w[i]);
+            v[2 * i] = f.x, v[2 * i + 1] = f.y;
+        }
+    }
+}
+template <class T>
+__device__ __forceinline__ uint4 pack(const float (&v)[16 / sizeof(T)]) {
+    uint32_t w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if constexpr (sizeof(T) == 4)
+            w[i] = __float_as_uint(v[i]);
+        else
+            w[i] = from_floats<T>(v[2 * i], v[2 * i + 1]);
+    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
+}
+
 __device__ __forceinline__ float act_value(float z, int act) {
     if (act == HEDDLE_ACT_SILU) return z / (1.0f + expf(-z));
     if (act == HEDDLE_ACT_GELU) return 0.5f * z * (1.0f + erff(z * 0.70710678118654752f));
@@ -115,6 +166,12 @@ __device__ __forceinline__ float act_slope(float z, int act) {
         return 0.5f * (1.0f + erff(z * 0.70710678118654752f)) + z * expf(-0.5f * z * z) * 0.39894228040143268f;
     if (act == HEDDLE_ACT_RELU) return z > 0.0f ? 1.0f : 0.0f;
     return 1.0f;
+}
+
+// 1 / sqrt(v), the approximation and one step of Newton's iteration for it.
+__device__ __forceinline__ float inv_sqrt(float v) {
+    const float r = rsqrtf(v);
+    return v > 0.0f && v < INFINITY ? r * fmaf(-0.5f * v * r, r, 1.5f) : r;
 }
 
 __device__ __forceinline__ float warp_sum(float v) {

@@ -160,12 +160,6 @@ __device__ __forceinline__ void store_half(T* p, const uint2& u, bool whole) {
     for (int i = 0; i < (int)(8 / sizeof(T)); ++i) p[i] = t[i];
 }
 
-// 1 / sqrt(v), the approximation and one step of Newton's iteration for it.
-__device__ __forceinline__ float inv_sqrt(float v) {
-    const float r = rsqrtf(v);
-    return v > 0.0f && v < INFINITY ? r * fmaf(-0.5f * v * r, r, 1.5f) : r;
-}
-
 // What the kernel knows of a call beforehand.  kAny: nothing.  kHalves and
 // kPairs: the layout of the pairs, and that all lies at whole units; two
 // thirds of the instructions then (16384 tokens of 72 heads of 128 bfloat16,
