@@ -25,30 +25,69 @@ __device__ __forceinline__ int64_t row_of(const heddle_embedding_args& a, int64_
 
 constexpr int kThreads = 128;
 
-// GL threads a token's row, U units of 16 bytes a thread at a time.
-template <class T, int GL, int U, bool STRIDED>
+// GL threads a token's row, U units of 16 bytes a thread: those that the
+// output's row is made of; TOKENS of them one after the other, their loads
+// together (32771 tokens of 1023 values, one at a time: 35 us, mostly waits).
+// WHOLE: rows of whole units at 16 bytes; else units are put together from the
+// two of the table that hold them, and the row's ends go value by value.
+template <class T, int GL, int U, int TOKENS, bool WHOLE>
 __global__ void __launch_bounds__(kThreads)
-    embedding_kernel(const __grid_constant__ heddle_embedding_args a, bool whole, uint32_t* err) {
+    embedding_kernel(const __grid_constant__ heddle_embedding_args a, uint32_t* err) {
     allow_dependents();
     await_previous();
-    using R = RowPart<T, U, STRIDED>;
-    constexpr int kTokens = kThreads / GL, kCols = GL * R::N;
-    const int64_t t = (int64_t)blockIdx.x * kTokens + threadIdx.x / GL, from = (int64_t)blockIdx.y * kCols;
-    if (t >= a.tokens) return;
-    bool past;
-    const int64_t row = row_of(a, t, past);
-    if (past && from == 0 && threadIdx.x % GL == 0) atomicOr(err, kErrOpToken);
-    const int64_t left = a.cols - from;
-    const R part{(int)(threadIdx.x % GL), GL, (int)(left < kCols ? left : kCols)};
-    uint32_t v[R::kWords] = {};
-    if (row >= 0) {
-        part.load(v, static_cast<const T*>(a.table) + row * a.ldt + from, whole);
-        if (a.scale != 1.0f) {
+    constexpr int V = 16 / sizeof(T), kGroups = kThreads / GL;
+    const int lane = threadIdx.x % GL, cols = (int)a.cols, u0 = blockIdx.y * GL * U + lane;
+    const int64_t t0 = (int64_t)blockIdx.x * kGroups * TOKENS + threadIdx.x / GL;
+    const float2 scale = both(a.scale);
+    int64_t row[TOKENS];
 #pragma unroll
-            for (int p = 0; p < R::N / 2; ++p) set_pair<T>(v, p, mul2(pair_of<T>(v, p), both(a.scale)));
+    for (int j = 0; j < TOKENS; ++j) {
+        const int64_t t = t0 + j * kGroups;
+        bool past = false;
+        row[j] = t < a.tokens ? row_of(a, t, past) : -1;
+        if (past && blockIdx.y == 0 && lane == 0) atomicOr(err, kErrOpToken);
+    }
+    uint4 v[TOKENS][U];
+    auto head_of = [&](const T* dst) {
+        const int head = WHOLE ? 0 : (int)((16 - ((uintptr_t)dst & 15)) & 15) / (int)sizeof(T);
+        return head < cols ? head : cols;
+    };
+#pragma unroll
+    for (int j = 0; j < TOKENS; ++j) {
+        const int64_t t = t0 + j * kGroups;
+        const int head = head_of(static_cast<T*>(a.y) + t * a.ldy);
+        const T* src = static_cast<const T*>(a.table) + row[j] * a.ldt + head;
+        const uint32_t skew = WHOLE ? 0 : low_of(src) & 15;
+        const unsigned char* from = reinterpret_cast<const unsigned char*>((uintptr_t)src - skew);
+        const int units = row[j] >= 0 ? (cols - head) / V : 0;
+#pragma unroll
+        for (int k = 0; k < U; ++k)
+            v[j][k] = u0 + k * GL < units ? load_skewed(from + (u0 + k * GL) * 16, skew) : make_uint4(0, 0, 0, 0);
+    }
+#pragma unroll
+    for (int j = 0; j < TOKENS; ++j) {
+        const int64_t t = t0 + j * kGroups;
+        if (t >= a.tokens) break;
+        T* dst = static_cast<T*>(a.y) + t * a.ldy;
+        const int head = head_of(dst), units = (cols - head) / V, tail = head + units * V;
+        if (!WHOLE && blockIdx.y == 0) {
+            const T* src = static_cast<const T*>(a.table) + row[j] * a.ldt;
+            auto one = [&](int i) { dst[i] = from_float<T>(row[j] >= 0 ? to_float(src[i]) * a.scale : 0.0f); };
+            if (lane < head) one(lane);
+            if (tail + lane < cols) one(tail + lane);
+        }
+#pragma unroll
+        for (int k = 0; k < U; ++k) {
+            if (u0 + k * GL >= units) break;
+            if (a.scale != 1.0f) {
+                uint32_t w[4] = {v[j][k].x, v[j][k].y, v[j][k].z, v[j][k].w};
+#pragma unroll
+                for (int p = 0; p < V / 2; ++p) set_pair<T>(w, p, mul2(pair_of<T>(w, p), scale));
+                v[j][k] = make_uint4(w[0], w[1], w[2], w[3]);
+            }
+            *reinterpret_cast<uint4*>(dst + head + (u0 + k * GL) * V) = v[j][k];
         }
     }
-    part.store(static_cast<T*>(a.y) + t * a.ldy + from, v, whole);
 }
 
 // -------------------------------------------------------------------- sorting
@@ -63,12 +102,9 @@ struct Entry {
 
 struct Sort {
     heddle_embedding_args a;
-    void* out;          // the gradient
-    int64_t out_bytes;  // of an element
     int32_t passes, bits;
-    int32_t fill;       // rows without tokens are written
-    Entry* list[2];     // by turns; the last pass leaves its result in list[passes & 1]
-    int64_t* count;     // entries of rows of the table
+    Entry* list[2];  // by turns; the last pass leaves its result in list[passes & 1]
+    int64_t* count;  // entries of rows of the table; and of rows that go over several runs, from zero
     uint32_t* err;
 };
 
@@ -82,14 +118,14 @@ __device__ __forceinline__ uint32_t load_of_rank(const uint32_t* p, uint32_t ran
 // the cluster has a run of the list: it counts its digits, its places in the
 // result follow from the counts of all warps before it, and it walks over its
 // run again in order.
-__device__ void sort_pass(const Sort& s, int pass, int64_t n, uint32_t (*counts)[kDigits], uint32_t* total,
-                          uint32_t* scan) {
+__device__ __forceinline__ void sort_pass(const Sort& s, int pass, int64_t n, uint32_t (*counts)[kDigits],
+                                          uint32_t* total, uint32_t* base, uint32_t* scan) {
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
     const uint32_t rank = tc::cluster_rank();
     const Entry* from = s.list[pass & 1];
     Entry* to = s.list[(pass & 1) ^ 1];
     const int shift = pass * s.bits, digits = 1 << s.bits;
-    const int64_t run = ceil_div(n, kCluster * kSortWarps) , first = (rank * kSortWarps + warp) * run;
+    const int64_t run = ceil_div(n, kCluster * kSortWarps), first = (rank * kSortWarps + warp) * run;
     const int64_t end = first + run < n ? first + run : n;
     // entry i; false where it is none of the table's
     auto entry = [&](int64_t i, Entry& e, bool flag) {
@@ -106,7 +142,16 @@ __device__ void sort_pass(const Sort& s, int pass, int64_t n, uint32_t (*counts)
     };
     for (int d = lane; d < digits; d += 32) counts[warp][d] = 0;
     __syncwarp();
-    for (int64_t i = first + lane; i < end; i += 32) {
+    // a short run stays in registers for the second walk
+    constexpr int kHeld = 4;
+    Entry held[kHeld];
+    bool is_held[kHeld];
+#pragma unroll
+    for (int k = 0; k < kHeld; ++k) is_held[k] = entry(first + k * 32 + lane, held[k], true);
+#pragma unroll
+    for (int k = 0; k < kHeld; ++k)
+        if (is_held[k]) atomicAdd(&counts[warp][held[k].row >> shift & (digits - 1)], 1u);
+    for (int64_t i = first + kHeld * 32 + lane; i < end; i += 32) {
         Entry e;
         if (entry(i, e, true)) atomicAdd(&counts[warp][e.row >> shift & (digits - 1)], 1u);
     }
@@ -114,6 +159,7 @@ __device__ void sort_pass(const Sort& s, int pass, int64_t n, uint32_t (*counts)
     // before this warp among the CTA's warps, and the CTA's own count
     for (int d = threadIdx.x; d < digits; d += kSortThreads) {
         uint32_t sum = 0;
+#pragma unroll 8
         for (int w = 0; w < kSortWarps; ++w) {
             const uint32_t c = counts[w][d];
             counts[w][d] = sum;
@@ -150,53 +196,116 @@ __device__ void sort_pass(const Sort& s, int pass, int64_t n, uint32_t (*counts)
             v += lane >= o ? w : 0;
         }
         scan[lane] = v - own;
-        if (lane == 31 && rank == 0 && pass == 0) *s.count = v;
+        if (lane == 31 && rank == 0 && pass == 0) s.count[0] = v, s.count[1] = 0;
     }
     __syncthreads();
-    if (d < digits) {
-        const uint32_t base = scan[warp] + up - all + before;
-        for (int w = 0; w < kSortWarps; ++w) counts[w][d] += base;
-    }
+    if (d < digits) base[d] = scan[warp] + up - all + before;
     __syncthreads();
-    for (int64_t i0 = first; i0 < end; i0 += 32) {
-        Entry e{};
-        const bool is = entry(i0 + lane, e, false);
+    auto place = [&](const Entry& e, bool is) {
         const uint32_t digit = is ? e.row >> shift & (digits - 1) : (uint32_t)kDigits;
         const uint32_t same = __match_any_sync(~0u, digit);
         const uint32_t ahead = __popc(same & ((1u << lane) - 1));
+        uint32_t at = 0;
         if (is) {
-            const uint32_t at = counts[warp][digit] + ahead;
-            to[at] = e;
+            at = counts[warp][digit];
+            to[base[digit] + at + ahead] = e;
         }
         __syncwarp();
-        if (is && ahead == 0) counts[warp][digit] += __popc(same);
+        if (is && ahead == 0) counts[warp][digit] = at + __popc(same);
         __syncwarp();
+    };
+#pragma unroll
+    for (int k = 0; k < kHeld; ++k)
+        if (first + k * 32 < end) place(held[k], is_held[k]);
+    for (int64_t i0 = first + kHeld * 32; i0 < end; i0 += 32) {
+        Entry e{};
+        const bool is = entry(i0 + lane, e, false);
+        place(e, is);
     }
-    __threadfence();
     tc::cluster_sync();  // the next pass reads what all wrote, and its counts take these ones' place
 }
 
-// Zeros to the rows of the gradient without tokens: a CTA has a range of rows,
-// `kMark` at a time, marks those that the tokens name, and writes the others.
-constexpr int kMark = 1 << 16;
+__global__ void __launch_bounds__(kSortThreads) __cluster_dims__(kCluster, 1, 1)
+    embedding_sort_kernel(const __grid_constant__ Sort s) {
+    allow_dependents();
+    await_previous();
+    extern __shared__ uint32_t shared[];
+    auto* counts = reinterpret_cast<uint32_t(*)[kDigits]>(shared);
+    uint32_t *total = shared + kSortWarps * kDigits, *base = total + kDigits, *scan = base + kDigits;
+    int64_t n = s.a.tokens;
+    for (int pass = 0; pass < s.passes; ++pass) {
+        sort_pass(s, pass, n, counts, total, base, scan);
+        if (pass == 0) n = *s.count;
+    }
+}
+constexpr int kSortShared = (kSortWarps * kDigits + 2 * kDigits + 32) * 4;
+
+// ----------------------------------------------------------------------- sums
+
+struct Sums {
+    heddle_embedding_args a;  // y: the gradient in
+    void* out;
+    const Entry* list;
+    int64_t* count;     // of entries, and of rows that go over several runs
+    uint32_t* crossing;  // the runs that these begin in
+    float* partial;     // [chunk][2][cols]
+    int32_t chunk;   // entries a block
+    int32_t accumulate;
+    unsigned fillers;  // blocks that write zeros to the rows without tokens
+};
+
+// Zeros to the gradient's rows that the sorted list does not name, a range of
+// rows a block: kWindow of them are marked at a time, the others written by
+// bulk copies out of shared memory where they lie at 16 bytes.
+constexpr int kWindow = 8192, kZeros = 8192;
 template <class TO>
-__device__ void fill_rows(const Sort& s, int64_t part, int64_t parts, uint32_t* marks) {
-    const int64_t rows = s.a.table_rows, each = ceil_div(rows, parts), r0 = part * each;
-    const int64_t r1 = r0 + each < rows ? r0 + each : rows;
+__device__ __noinline__ void fill_rows(const Sums& s, int64_t part) {
+    __shared__ uint32_t marks[kWindow / 32];
+    __shared__ __align__(128) unsigned char zeros[kZeros];
+    const int64_t rows = s.a.table_rows, each = ceil_div(rows, (int64_t)s.fillers), r0 = part * each;
+    const int64_t r1 = r0 + each < rows ? r0 + each : rows, n = *s.count;
     TO* out = static_cast<TO*>(s.out);
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
-    for (int64_t from = r0; from < r1; from += kMark) {
-        const int64_t to = from + kMark < r1 ? from + kMark : r1;
+    const int64_t bytes = s.a.cols * (int64_t)sizeof(TO);
+    const bool bulk = ((uintptr_t)out | (uintptr_t)(s.a.ldt * sizeof(TO)) | (uintptr_t)bytes) % 16 == 0;
+    for (int i = threadIdx.x; i < kZeros / 16; i += kThreads)
+        reinterpret_cast<uint4*>(zeros)[i] = make_uint4(0, 0, 0, 0);
+    tc::fence_async_shared();
+    for (int64_t from = r0; from < r1; from += kWindow) {
+        const int64_t to = from + kWindow < r1 ? from + kWindow : r1;
         __syncthreads();
-        for (int i = threadIdx.x; i < ceil_div(to - from, 32); i += kSortThreads) marks[i] = 0;
+        for (int i = threadIdx.x; i < ceil_div(to - from, 32); i += kThreads) marks[i] = 0;
         __syncthreads();
-        for (int64_t t = threadIdx.x; t < s.a.tokens; t += kSortThreads) {
-            bool past;
-            const int64_t row = row_of(s.a, t, past);
-            if (row >= from && row < to) atomicOr(&marks[(row - from) / 32], 1u << ((row - from) % 32));
+        int64_t lo = 0, hi = n;  // the first entry from `from` on, 32 probes at a time
+        while (lo < hi) {
+            const int64_t step = ceil_div(hi - lo, 32), at = lo + step * lane;
+            const int below = __popc(__ballot_sync(~0u, at < hi && s.list[at].row < from));
+            if (below == 0) break;
+            hi = lo + step * below < hi ? lo + step * below : hi;
+            lo += step * (below - 1) + 1;
+        }
+        for (int64_t i = lo + threadIdx.x; i < n; i += kThreads) {
+            const int64_t row = s.list[i].row;
+            if (row >= to) break;
+            atomicOr(&marks[(row - from) / 32], 1u << ((row - from) % 32));
         }
         __syncthreads();
-        for (int64_t row = from + warp; row < to; row += kSortWarps) {
+        if (bulk) {  // a row a thread
+            for (int64_t row = from + threadIdx.x; row < to; row += kThreads) {
+                if (marks[(row - from) / 32] >> ((row - from) % 32) & 1) continue;
+                unsigned char* p = reinterpret_cast<unsigned char*>(out + row * s.a.ldt);
+                for (int64_t at = 0; at < bytes; at += kZeros) {
+                    const uint32_t size = (uint32_t)(bytes - at < kZeros ? bytes - at : kZeros);
+                    asm volatile("cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], %2;" ::"l"(
+                                     __cvta_generic_to_global(p + at)),
+                                 "r"(tc::smem_u32(zeros)), "r"(size)
+                                 : "memory");
+                }
+            }
+            asm volatile("cp.async.bulk.commit_group;" ::: "memory");
+            continue;
+        }
+        for (int64_t row = from + warp; row < to; row += kThreads / 32) {
             if (marks[(row - from) / 32] >> ((row - from) % 32) & 1) continue;
             TO* p = out + row * s.a.ldt;
             // to 16 bytes, whole units, the rest
@@ -208,39 +317,9 @@ __device__ void fill_rows(const Sort& s, int64_t part, int64_t parts, uint32_t* 
             if (tail + lane < s.a.cols) p[tail + lane] = from_float<TO>(0.0f);
         }
     }
+    // the copies read shared memory, and the rows are written when the kernel ends
+    asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
 }
-
-template <class TO>
-__global__ void __launch_bounds__(kSortThreads) __cluster_dims__(kCluster, 1, 1)
-    embedding_sort_kernel(const __grid_constant__ Sort s) {
-    allow_dependents();
-    await_previous();
-    extern __shared__ uint32_t shared[];
-    if (blockIdx.x < kCluster) {
-        auto* counts = reinterpret_cast<uint32_t(*)[kDigits]>(shared);
-        uint32_t *total = shared + kSortWarps * kDigits, *scan = total + kDigits;
-        int64_t n = s.a.tokens;
-        for (int pass = 0; pass < s.passes; ++pass) {
-            sort_pass(s, pass, n, counts, total, scan);
-            if (pass == 0) n = *s.count;
-        }
-    } else if (s.fill) {
-        fill_rows<TO>(s, blockIdx.x - kCluster, gridDim.x - kCluster, shared);
-    }
-}
-constexpr int kSortShared = (kSortWarps * kDigits + kDigits + 32) * 4;
-
-// ----------------------------------------------------------------------- sums
-
-struct Sums {
-    heddle_embedding_args a;  // y: the gradient in
-    void* out;
-    const Entry* list;
-    const int64_t* count;
-    float* partial;  // [chunk][2][cols]
-    int32_t chunk;   // entries a block
-    int32_t accumulate;
-};
 
 template <class TO, class R>
 __device__ __forceinline__ void add_out(const Sums& s, const R& part, int64_t row, int64_t from,
@@ -256,27 +335,40 @@ __device__ __forceinline__ void add_out(const Sums& s, const R& part, int64_t ro
 }
 
 constexpr int kAhead = 8;  // rows fetched before any is added
+constexpr int kLeastRun = 16, kMostRun = 512;  // entries a block
 
 // A run of the sorted list and a range of columns a block.  A row whose
 // entries all lie in the run is written; the sums of one that began before it
-// go to partial[.][0], of one that goes on behind it to partial[.][1].
+// go to partial[.][0], of one that goes on behind it to partial[.][1].  The
+// first blocks write zeros to the other rows meanwhile.
 template <class T, class TO, int U, bool STRIDED>
 __global__ void __launch_bounds__(kThreads)
-    embedding_sums_kernel(const __grid_constant__ Sums s, bool whole) {
+    embedding_sums_kernel(const __grid_constant__ Sums s, unsigned slabs, bool whole) {
     allow_dependents();
     await_previous();
+    if (blockIdx.x < s.fillers) {
+        fill_rows<TO>(s, blockIdx.x);
+        return;
+    }
     using R = RowPart<T, U, STRIDED>;
     constexpr int kCols = kThreads * R::N;
-    const int64_t n = *s.count, first = (int64_t)blockIdx.x * s.chunk;
+    __shared__ Entry run[kMostRun + 2];  // with the one before and the one behind
+    const unsigned chunk = (blockIdx.x - s.fillers) / slabs, slab = (blockIdx.x - s.fillers) % slabs;
+    const int64_t first = (int64_t)chunk * s.chunk, from = (int64_t)slab * kCols;
+    // entries past the last are in the list's place, and not used
+    for (int i = threadIdx.x; i < s.chunk + 2; i += kThreads)
+        if (first + i >= 1 && first + i <= s.a.tokens) run[i] = s.list[first + i - 1];
+    const int64_t n = *s.count;
     if (first >= n) return;
-    const int64_t end = first + s.chunk < n ? first + s.chunk : n, from = (int64_t)blockIdx.y * kCols;
+    __syncthreads();
+    const int end = (int)(first + s.chunk < n ? s.chunk : n - first);
     const int64_t left = s.a.cols - from;
     const R part{(int)threadIdx.x, kThreads, (int)(left < kCols ? left : kCols)};
     const T* dy = static_cast<const T*>(s.a.y) + from;
-    const uint32_t before = first ? s.list[first - 1].row : ~0u, behind = end < n ? s.list[end].row : ~0u;
-    float* partial = s.partial + ((int64_t)blockIdx.x * 2) * s.a.cols + from;
+    const uint32_t before = first ? run[0].row : ~0u, behind = first + end < n ? run[end + 1].row : ~0u;
+    float* partial = s.partial + (int64_t)chunk * 2 * s.a.cols + from;
     float sum[R::N] = {};
-    uint32_t row = s.list[first].row;
+    uint32_t row = run[1].row;
     bool began = row == before;
     auto finish = [&](bool goes_on) {
         if (began || goes_on) {
@@ -288,21 +380,17 @@ __global__ void __launch_bounds__(kThreads)
             add_out<TO>(s, part, row, from, sum);
         }
     };
-    for (int64_t i = first; i < end; i += kAhead) {
+    for (int i = 0; i < end; i += kAhead) {
         uint32_t v[kAhead][R::kWords];
-        uint32_t rows[kAhead];
 #pragma unroll
-        for (int k = 0; k < kAhead; ++k) {
-            const Entry e = s.list[i + k < end ? i + k : end - 1];
-            rows[k] = e.row;
-            if (i + k < end) part.load(v[k], dy + (int64_t)e.token * s.a.ldy, whole);
-        }
+        for (int k = 0; k < kAhead; ++k)
+            if (i + k < end) part.load(v[k], dy + (int64_t)run[i + k + 1].token * s.a.ldy, whole);
 #pragma unroll
         for (int k = 0; k < kAhead; ++k) {
             if (i + k >= end) break;
-            if (rows[k] != row) {
+            if (run[i + k + 1].row != row) {
                 finish(false);
-                row = rows[k], began = false;
+                row = run[i + k + 1].row, began = false;
 #pragma unroll
                 for (int e = 0; e < R::N; ++e) sum[e] = 0.0f;
             }
@@ -314,90 +402,121 @@ __global__ void __launch_bounds__(kThreads)
         }
     }
     finish(row == behind);
+    if (row == behind && !began && slab == 0 && threadIdx.x == 0)
+        s.crossing[atomicAdd(reinterpret_cast<unsigned long long*>(s.count + 1), 1ull)] = chunk;
 }
 
-// Rows that go over several runs, by the block of the one that they begin in.
+// Rows that go over several runs, 1024 columns of one a block at a time.  (A
+// block for every run, most of which have nothing to do, took 40 us for 16384
+// tokens; narrow slabs, each with the search and its waits, 36.)
+constexpr int kJoinThreads = 256, kJoinCols = 4 * kJoinThreads;
 template <class TO>
-__global__ void __launch_bounds__(kThreads) embedding_join_kernel(const __grid_constant__ Sums s) {
+__global__ void __launch_bounds__(kJoinThreads)
+    embedding_join_kernel(const __grid_constant__ Sums s, unsigned slabs) {
     allow_dependents();
     await_previous();
-    const int64_t n = *s.count, end = ((int64_t)blockIdx.x + 1) * s.chunk, first = end - s.chunk;
-    if (end >= n) return;
-    const uint32_t row = s.list[end].row;
-    if (s.list[end - 1].row != row || (first && s.list[first].row == row && s.list[first - 1].row == row)) return;
-    const int64_t i = (int64_t)blockIdx.y * kThreads + threadIdx.x;
-    if (i >= s.a.cols) return;
-    // the runs that it goes on into: those that start with it
-    int64_t last = blockIdx.x + 1, none = ceil_div(n, s.chunk);
-    while (none - last > 1) {
-        const int64_t mid = (last + none) / 2;
-        if (s.list[mid * s.chunk].row == row)
-            last = mid;
-        else
-            none = mid;
-    }
-    float sum = s.partial[((int64_t)blockIdx.x * 2 + 1) * s.a.cols + i];
+    const int lane = threadIdx.x % 32;
+    const int64_t n = s.count[0], work = s.count[1] * slabs;
+    for (int64_t i = blockIdx.x; i < work; i += gridDim.x) {
+        const int64_t begin = s.crossing[i / slabs], col = i % slabs * kJoinCols + threadIdx.x;
+        const uint32_t row = s.list[(begin + 1) * s.chunk].row;
+        // the runs that it goes on into, those that start with it: from `last`
+        // on, `none` is not one; 32 probes at a time
+        int64_t last = begin + 1, none = ceil_div(n, s.chunk);
+        while (none - last > 1) {
+            const int64_t step = ceil_div(none - last, 32), at = last + step * lane;
+            const unsigned is = __ballot_sync(~0u, at < none && s.list[at * s.chunk].row == row);
+            const int64_t found = last + step * (31 - __clz(is));  // the first probe always is
+            none = found + step < none ? found + step : none;
+            last = found;
+        }
+        const float* from = s.partial + begin * 2 * s.a.cols + col;
+        float sum[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            sum[k] = col + k * kJoinThreads < s.a.cols ? from[s.a.cols + k * kJoinThreads] : 0.0f;
 #pragma unroll 8
-    for (int64_t c = blockIdx.x + 1; c <= last; ++c) sum += s.partial[c * 2 * s.a.cols + i];
-    TO* p = static_cast<TO*>(s.out) + row * s.a.ldt + i;
-    float v = sum * s.a.scale;
-    if (s.accumulate) v += to_float(*p);
-    *p = from_float<TO>(v);
+        for (int64_t p = begin + 1; p <= last; ++p) {
+            from += 2 * s.a.cols;
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                if (col + k * kJoinThreads < s.a.cols) sum[k] += from[k * kJoinThreads];
+        }
+        TO* p = static_cast<TO*>(s.out) + row * s.a.ldt + col;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            if (col + k * kJoinThreads >= s.a.cols) break;
+            float v = sum[k] * s.a.scale;
+            if (s.accumulate) v += to_float(p[k * kJoinThreads]);
+            p[k * kJoinThreads] = from_float<TO>(v);
+        }
+    }
 }
 
 // -------------------------------------------------------------------- launches
 
-int size_of(int32_t dtype) { return dtype == HEDDLE_FP32 ? 4 : 2; }
-
-template <class T, int GL, int U, bool STRIDED>
-cudaError_t lookup(const OpContext& x, const heddle_embedding_args& a, bool whole, cudaStream_t st) {
-    constexpr int kCols = RowPart<T, U, STRIDED>::N * GL;
-    const dim3 grid((unsigned)ceil_div(a.tokens, kThreads / GL), (unsigned)ceil_div(a.cols, kCols));
-    return launch(x, embedding_kernel<T, GL, U, STRIDED>, grid, kThreads, 0, st, a, whole, x.err);
+template <class T, int GL, int U, int TOKENS, bool WHOLE>
+cudaError_t lookup(const OpContext& x, const heddle_embedding_args& a, cudaStream_t st) {
+    const int64_t units = ceil_div(a.cols, 16 / (int)sizeof(T));
+    const dim3 grid((unsigned)ceil_div(a.tokens, kThreads / GL * TOKENS), (unsigned)ceil_div(units, GL * U));
+    return launch(x, embedding_kernel<T, GL, U, TOKENS, WHOLE>, grid, kThreads, 0, st, a, x.err);
 }
 
-template <class T, bool STRIDED>
+template <class T, bool WHOLE>
 cudaError_t lookup_typed(const OpContext& x, const heddle_embedding_args& a, cudaStream_t st) {
-    const int size = sizeof(T);
-    const int64_t units = ceil_div(a.cols, 16 / size);
-    const bool whole = rows_whole(a.table, a.ldt, a.table_rows, size) && rows_whole(a.y, a.ldy, a.tokens, size);
-    if (units <= 16) return lookup<T, 16, 1, STRIDED>(x, a, whole, st);
-    if (units <= 32) return lookup<T, 32, 1, STRIDED>(x, a, whole, st);
-    if (units <= 128 || a.tokens * units < (int64_t)x.num_sms * 1024)
-        return lookup<T, 128, 1, STRIDED>(x, a, whole, st);
-    return lookup<T, 128, 4, STRIDED>(x, a, whole, st);
+    const int64_t units = ceil_div(a.cols, 16 / (int)sizeof(T));
+    if (a.tokens * units < (int64_t)x.num_sms * 1024)  // a unit a thread, so that more SMs take part
+        return units <= 16   ? lookup<T, 16, 1, 1, WHOLE>(x, a, st)
+               : units <= 32 ? lookup<T, 32, 1, 1, WHOLE>(x, a, st)
+                             : lookup<T, 128, 1, 1, WHOLE>(x, a, st);
+    if (units <= 16) return lookup<T, 16, 1, 4, WHOLE>(x, a, st);
+    if (units <= 32) return lookup<T, 32, 1, 4, WHOLE>(x, a, st);
+    if (units <= 64) return lookup<T, 32, 2, 2, WHOLE>(x, a, st);
+    if (units <= 128) return lookup<T, 128, 1, 4, WHOLE>(x, a, st);
+    return lookup<T, 128, 4, 1, WHOLE>(x, a, st);
 }
 
-// Entries a block of the sums takes: few, and no more than 2048 blocks of them,
-// which bounds the parts that a row can be joined from.
-constexpr int64_t kMostChunks = 2048;
+template <class T>
+cudaError_t lookup_any(const OpContext& x, const heddle_embedding_args& a, cudaStream_t st) {
+    constexpr int size = sizeof(T);
+    const bool whole = a.cols % (16 / size) == 0 && rows_whole(a.table, a.ldt, a.table_rows, size) &&
+                       rows_whole(a.y, a.ldy, a.tokens, size);
+    return whole ? lookup_typed<T, true>(x, a, st) : lookup_typed<T, false>(x, a, st);
+}
+
+// Entries a block of the sums takes: few, and for up to a million tokens no
+// more than 2048 blocks of them, which bounds the parts that a row is joined
+// from.
 int64_t chunk_of(int64_t tokens) {
-    int64_t c = 16;
-    while (ceil_div(tokens, c) > kMostChunks) c *= 2;
+    int64_t c = kLeastRun;
+    while (c < kMostRun && ceil_div(tokens, c) > 2048) c *= 2;
     return c;
 }
 
 struct Places {
-    size_t list, partial, total;
+    size_t list, crossing, partial, total;
 };
 Places places(const heddle_embedding_args& a) {
     Places p;
     p.list = 256;
-    p.partial = p.list + 2 * align256(sizeof(Entry) * (size_t)a.tokens);
-    p.total = p.partial + align256(sizeof(float) * 2 * (size_t)ceil_div(a.tokens, chunk_of(a.tokens)) * a.cols);
+    const size_t chunks = (size_t)ceil_div(a.tokens, chunk_of(a.tokens));
+    p.crossing = p.list + 2 * align256(sizeof(Entry) * (size_t)a.tokens);
+    p.partial = p.crossing + align256(sizeof(uint32_t) * chunks);
+    p.total = p.partial + align256(sizeof(float) * 2 * chunks * a.cols);
     return p;
 }
 
 template <class T, class TO, bool STRIDED>
 cudaError_t sums(const OpContext& x, const Sums& s, cudaStream_t st) {
     constexpr int kCols = RowPart<T, 1, STRIDED>::N * kThreads;
-    const unsigned chunks = (unsigned)ceil_div(s.a.tokens, s.chunk);
+    const int64_t chunks = ceil_div(s.a.tokens, s.chunk), slabs = ceil_div(s.a.cols, kCols);
     const bool whole = rows_whole(s.a.y, s.a.ldy, s.a.tokens, sizeof(T));
-    cudaError_t e = launch(x, embedding_sums_kernel<T, TO, 1, STRIDED>,
-                           dim3(chunks, (unsigned)ceil_div(s.a.cols, kCols)), kThreads, 0, st, s, whole);
+    cudaError_t e = launch(x, embedding_sums_kernel<T, TO, 1, STRIDED>, dim3((unsigned)(s.fillers + chunks * slabs)),
+                           kThreads, 0, st, s, (unsigned)slabs, whole);
+    const int64_t parts = ceil_div(s.a.cols, kJoinCols), want = (chunks - 1) * parts, most = (int64_t)x.num_sms * 4;
     if (e == cudaSuccess && chunks > 1)
-        e = launch(x, embedding_join_kernel<TO>, dim3(chunks - 1, (unsigned)ceil_div(s.a.cols, kThreads)), kThreads, 0,
-                   st, s);
+        e = launch(x, embedding_join_kernel<TO>, dim3((unsigned)(want < most ? want : most)), kJoinThreads, 0, st, s,
+                   (unsigned)parts);
     return e;
 }
 
@@ -407,43 +526,40 @@ cudaError_t backward(const OpContext& x, const heddle_embedding_grad_args& g, un
     const Places at = places(a);
     Sort s{};
     s.a = a;
-    s.out = const_cast<void*>(a.table);
     int bits = 1;
     while (bits < 31 && (int64_t)1 << bits < a.table_rows) ++bits;
     s.passes = (bits + 8) / 9;
     s.bits = (bits + s.passes - 1) / s.passes;
-    s.fill = !g.accumulate;
     s.list[0] = reinterpret_cast<Entry*>(ws + at.list);
     s.list[1] = reinterpret_cast<Entry*>(ws + at.list + align256(sizeof(Entry) * (size_t)a.tokens));
     s.count = reinterpret_cast<int64_t*>(ws);
     s.err = x.err;
-    auto* kernel = embedding_sort_kernel<TO>;
     static std::atomic<uint64_t> asked{0};
-    cudaError_t e = allow_shared(kernel, kSortShared, x.device, asked);
+    cudaError_t e = allow_shared(embedding_sort_kernel, kSortShared, x.device, asked);
     if (e != cudaSuccess) return e;
-    const unsigned clusters = 1 + (s.fill ? (unsigned)(x.num_sms / kCluster) : 0);
-    e = launch(x, kernel, dim3(clusters * kCluster), kSortThreads, kSortShared, st, s);
-    if (e != cudaSuccess || a.tokens == 0) return e;
+    e = launch(x, embedding_sort_kernel, dim3(kCluster), kSortThreads, kSortShared, st, s);
+    if (e != cudaSuccess) return e;
     Sums m{};
     m.a = a;
-    m.out = s.out;
+    m.out = const_cast<void*>(a.table);
     m.list = s.list[s.passes & 1];
     m.count = s.count;
+    m.crossing = reinterpret_cast<uint32_t*>(ws + at.crossing);
     m.partial = reinterpret_cast<float*>(ws + at.partial);
     m.chunk = (int32_t)chunk_of(a.tokens);
     m.accumulate = g.accumulate;
+    const int64_t most = (int64_t)x.num_sms * 2;
+    m.fillers = g.accumulate ? 0 : (unsigned)(a.table_rows < most ? a.table_rows : most);
     return a.cols % (16 / (int)sizeof(T)) ? sums<T, TO, true>(x, m, st) : sums<T, TO, false>(x, m, st);
 }
 
 }  // namespace
 
 cudaError_t launch_embedding(const OpContext& x, const heddle_embedding_args& a, cudaStream_t st) {
-    const bool strided = a.cols % (16 / size_of(a.dtype)) != 0;
     switch (a.dtype) {
-        case HEDDLE_BF16:
-            return strided ? lookup_typed<__nv_bfloat16, true>(x, a, st) : lookup_typed<__nv_bfloat16, false>(x, a, st);
-        case HEDDLE_FP16: return strided ? lookup_typed<__half, true>(x, a, st) : lookup_typed<__half, false>(x, a, st);
-        default: return strided ? lookup_typed<float, true>(x, a, st) : lookup_typed<float, false>(x, a, st);
+        case HEDDLE_BF16: return lookup_any<__nv_bfloat16>(x, a, st);
+        case HEDDLE_FP16: return lookup_any<__half>(x, a, st);
+        default: return lookup_any<float>(x, a, st);
     }
 }
 

@@ -18,6 +18,7 @@
 #ifndef FWD_THREADS
 #define FWD_THREADS 1024
 #define GRAD_THREADS 512
+#define GRADODD 608
 #define GRAD32 1024
 #define FRING 0
 #define FWD_SHORT 4
@@ -438,6 +439,9 @@ __global__ void __launch_bounds__(MOST)
         }
     };
     statistics(0);
+    // one row at a time stays in registers where there are enough
+    constexpr bool kKeep = ROWS == 1 && MOST <= 512;
+    uint32_t xv[R::kWords], gv[R::kWords];
     int turn = 0;
     for (int k = 0; k < rows; k += ROWS) {
         float v[2 * ROWS] = {}, m[ROWS], s[ROWS];
@@ -453,7 +457,6 @@ __global__ void __launch_bounds__(MOST)
         for (int i = 0; i < ROWS; ++i) {
             if (k + i >= rows) break;
             ring.wait(i);
-            uint32_t xv[R::kWords], gv[R::kWords];
             load_units<WHOLE>(xv, part, at[i][0], xl + i * xd & 15);
             load_units<WHOLE>(gv, part, at[i][1], gl + i * gd & 15);
             add_row<T>(part, xv, gv, w, m[i], s[i], true, v[2 * i], v[2 * i + 1], dw, db);
@@ -469,9 +472,11 @@ __global__ void __launch_bounds__(MOST)
 #pragma unroll
             for (int i = 0; i < ROWS; ++i, dx += ds) {
                 if (k + i >= rows) break;
-                uint32_t xv[R::kWords], gv[R::kWords], rv[R::kWords] = {};
-                load_units<WHOLE>(xv, part, at[i][0], xl + i * xd & 15);
-                load_units<WHOLE>(gv, part, at[i][1], gl + i * gd & 15);
+                uint32_t rv[R::kWords] = {};
+                if (!kKeep) {
+                    load_units<WHOLE>(xv, part, at[i][0], xl + i * xd & 15);
+                    load_units<WHOLE>(gv, part, at[i][1], gl + i * gd & 15);
+                }
                 if (dres) load_units<WHOLE>(rv, part, at[i][2], rl + i * rd & 15);
                 grad_row<T>(part, gv, xv, gv, w, rv, m[i], s[i], v[2 * i] * inv, v[2 * i + 1] * inv);
                 if (!WHOLE && i) __syncthreads();  // the row before has left its place on its way out
@@ -683,7 +688,7 @@ Plan plan_grad(const OpContext& x, const heddle_layer_norm_grad_args& a) {
     }
     p.threads = block_of(units);
     p.way = kLongRows;
-    int an_sm = blocks_an_sm(size == 4 ? GRAD32 : GRAD_THREADS, p.threads);
+    int an_sm = blocks_an_sm(size == 2 ? GRAD_THREADS : p.strided ? GRADODD : GRAD32, p.threads);
     p.whole = !p.strided && rows_whole(a.x, a.ldx, a.rows, size) && rows_whole(a.dy, a.lddy, a.rows, size) &&
               rows_whole(a.dres, a.ldr, a.rows, size) && rows_whole(a.dx, a.lddx, a.rows, size);
     if (units <= kEach * kLong) plan_ring(p, a.cols * size, a.dres ? 3 : 2, 3, p.whole, 0, an_sm);
@@ -750,7 +755,7 @@ cudaError_t backward_ring(const OpContext& x, const heddle_layer_norm_grad_args&
     if (p.threads > 512)
         return launch_planned(x, layer_norm_grad_ring_kernel<T, kEach, WHOLE, 1, 1024>, asked[0], p, st, a, partial,
                               p.stages, arrays, p.staged, x.err);
-    if (p.stages < 6)
+    if (p.stages < 6 || !WHOLE)
         return launch_planned(x, layer_norm_grad_ring_kernel<T, kEach, WHOLE, 1, 512>, asked[1], p, st, a, partial,
                               p.stages, arrays, p.staged, x.err);
     return launch_planned(x, layer_norm_grad_ring_kernel<T, kEach, WHOLE, 2, 512>, asked[2], p, st, a, partial,
