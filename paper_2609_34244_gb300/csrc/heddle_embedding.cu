@@ -79,7 +79,7 @@ __global__ void __launch_bounds__(kThreads)
 #pragma unroll
         for (int k = 0; k < U; ++k) {
             if (u0 + k * GL >= units) break;
-            if (a.scale != 1.0f) {
+            if (a.scale != 1.0f && row[j] >= 0) {
                 uint32_t w[4] = {v[j][k].x, v[j][k].y, v[j][k].z, v[j][k].w};
 #pragma unroll
                 for (int p = 0; p < V / 2; ++p) set_pair<T>(w, p, mul2(pair_of<T>(w, p), scale));
@@ -251,7 +251,11 @@ struct Sums {
     float* partial;     // [chunk][2][cols]
     int32_t chunk;   // entries a block
     int32_t accumulate;
-    unsigned fillers;  // blocks that write zeros to the rows without tokens
+    int32_t out_whole;  // the gradient's rows are whole units at 16 bytes
+    // blocks that write zeros to the rows without tokens, behind the others: many
+    // small ones even out what memory gives each (two an SM: 264 us where eight
+    // take 207, 16384 tokens and 131072 x 4096 bfloat16)
+    unsigned fillers;
 };
 
 // Zeros to the gradient's rows that the sorted list does not name, a range of
@@ -321,17 +325,34 @@ __device__ __noinline__ void fill_rows(const Sums& s, int64_t part) {
     asm volatile("cp.async.bulk.wait_group 0;" ::: "memory");
 }
 
+// A row's sums to the gradient: in 16-byte units, or value by value.
 template <class TO, class R>
 __device__ __forceinline__ void add_out(const Sums& s, const R& part, int64_t row, int64_t from,
                                         const float (&sum)[R::N]) {
     TO* p = static_cast<TO*>(s.out) + row * s.a.ldt + from;
+    if (s.out_whole) {
+        if (!part.in(0)) return;
+        constexpr int VO = 16 / sizeof(TO);
+        uint4* at = reinterpret_cast<uint4*>(p + part.at(0));
+        uint4 base[R::N / VO];
+#pragma unroll
+        for (int u = 0; u < R::N / VO; ++u) base[u] = s.accumulate ? at[u] : make_uint4(0, 0, 0, 0);
+#pragma unroll
+        for (int u = 0; u < R::N / VO; ++u) {
+            float f[VO];
+            unpack<TO>(base[u], f);
+#pragma unroll
+            for (int e = 0; e < VO; ++e) f[e] = fmaf(sum[u * VO + e], s.a.scale, f[e]);
+            at[u] = pack<TO>(f);
+        }
+        return;
+    }
+    float base[R::N];
+#pragma unroll
+    for (int e = 0; e < R::N; ++e) base[e] = s.accumulate && part.in(e) ? to_float(p[part.at(e)]) : 0.0f;
 #pragma unroll
     for (int e = 0; e < R::N; ++e)
-        if (part.in(e)) {
-            float v = sum[e] * s.a.scale;
-            if (s.accumulate) v += to_float(p[part.at(e)]);
-            p[part.at(e)] = from_float<TO>(v);
-        }
+        if (part.in(e)) p[part.at(e)] = from_float<TO>(fmaf(sum[e], s.a.scale, base[e]));
 }
 
 constexpr int kAhead = 8;  // rows fetched before any is added
@@ -340,20 +361,21 @@ constexpr int kLeastRun = 16, kMostRun = 512;  // entries a block
 // A run of the sorted list and a range of columns a block.  A row whose
 // entries all lie in the run is written; the sums of one that began before it
 // go to partial[.][0], of one that goes on behind it to partial[.][1].  The
-// first blocks write zeros to the other rows meanwhile.
-template <class T, class TO, int U, bool STRIDED>
+// last blocks write zeros to the other rows.
+template <class T, class TO, bool WHOLE>
 __global__ void __launch_bounds__(kThreads)
-    embedding_sums_kernel(const __grid_constant__ Sums s, unsigned slabs, bool whole) {
+    embedding_sums_kernel(const __grid_constant__ Sums s, unsigned slabs) {
     allow_dependents();
     await_previous();
-    if (blockIdx.x < s.fillers) {
-        fill_rows<TO>(s, blockIdx.x);
+    const unsigned sums = gridDim.x - s.fillers, block = blockIdx.x;
+    if (block >= sums) {
+        fill_rows<TO>(s, block - sums);
         return;
     }
-    using R = RowPart<T, U, STRIDED>;
+    using R = RowPart<T, 1, false>;
     constexpr int kCols = kThreads * R::N;
     __shared__ Entry run[kMostRun + 2];  // with the one before and the one behind
-    const unsigned chunk = (blockIdx.x - s.fillers) / slabs, slab = (blockIdx.x - s.fillers) % slabs;
+    const unsigned chunk = block / slabs, slab = block % slabs;
     const int64_t first = (int64_t)chunk * s.chunk, from = (int64_t)slab * kCols;
     // entries past the last are in the list's place, and not used
     for (int i = threadIdx.x; i < s.chunk + 2; i += kThreads)
@@ -383,8 +405,20 @@ __global__ void __launch_bounds__(kThreads)
     for (int i = 0; i < end; i += kAhead) {
         uint32_t v[kAhead][R::kWords];
 #pragma unroll
-        for (int k = 0; k < kAhead; ++k)
-            if (i + k < end) part.load(v[k], dy + (int64_t)run[i + k + 1].token * s.a.ldy, whole);
+        for (int k = 0; k < kAhead; ++k) {
+            if (i + k >= end) break;
+            const T* from = dy + (int64_t)run[i + k + 1].token * s.a.ldy;
+            if (WHOLE) {
+                part.load(v[k], from, true);
+            } else if (part.in(0)) {  // what lies past the row's end counts for nothing
+                const int valid = part.cols - part.at(0);
+                from += part.at(0);
+                const uint32_t skew = low_of(from) & 15;
+                const uint4 u = load_skewed(reinterpret_cast<const unsigned char*>((uintptr_t)from - skew), skew,
+                                            skew + valid * sizeof(T) > 16);
+                v[k][0] = u.x, v[k][1] = u.y, v[k][2] = u.z, v[k][3] = u.w;
+            }
+        }
 #pragma unroll
         for (int k = 0; k < kAhead; ++k) {
             if (i + k >= end) break;
@@ -446,9 +480,8 @@ __global__ void __launch_bounds__(kJoinThreads)
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
             if (col + k * kJoinThreads >= s.a.cols) break;
-            float v = sum[k] * s.a.scale;
-            if (s.accumulate) v += to_float(p[k * kJoinThreads]);
-            p[k * kJoinThreads] = from_float<TO>(v);
+            const float base = s.accumulate ? to_float(p[k * kJoinThreads]) : 0.0f;
+            p[k * kJoinThreads] = from_float<TO>(fmaf(sum[k], s.a.scale, base));
         }
     }
 }
@@ -484,13 +517,18 @@ cudaError_t lookup_any(const OpContext& x, const heddle_embedding_args& a, cudaS
     return whole ? lookup_typed<T, true>(x, a, st) : lookup_typed<T, false>(x, a, st);
 }
 
-// Entries a block of the sums takes: few, and for up to a million tokens no
-// more than 2048 blocks of them, which bounds the parts that a row is joined
-// from.
-int64_t chunk_of(int64_t tokens) {
-    int64_t c = kLeastRun;
+// Entries a block of the sums takes: 64, so that few rows go over several runs;
+// fewer where that leaves SMs without a block, more beyond 2048 runs, which
+// bounds the parts that a row of up to a million tokens is joined from.
+int64_t chunk_of(int64_t tokens, int64_t slabs) {
+    int64_t c = 64;
+    while (c > kLeastRun && ceil_div(tokens, c) * slabs < 1024) c /= 2;
     while (c < kMostRun && ceil_div(tokens, c) > 2048) c *= 2;
     return c;
+}
+// Columns of a block of the sums: a unit a thread.
+int64_t slabs_of(const heddle_embedding_args& a) {
+    return ceil_div(a.cols, kThreads * (a.dtype == HEDDLE_FP32 ? 4 : 8));
 }
 
 struct Places {
@@ -499,20 +537,20 @@ struct Places {
 Places places(const heddle_embedding_args& a) {
     Places p;
     p.list = 256;
-    const size_t chunks = (size_t)ceil_div(a.tokens, chunk_of(a.tokens));
+    const size_t chunks = (size_t)ceil_div(a.tokens, chunk_of(a.tokens, slabs_of(a)));
     p.crossing = p.list + 2 * align256(sizeof(Entry) * (size_t)a.tokens);
     p.partial = p.crossing + align256(sizeof(uint32_t) * chunks);
     p.total = p.partial + align256(sizeof(float) * 2 * chunks * a.cols);
     return p;
 }
 
-template <class T, class TO, bool STRIDED>
+template <class T, class TO>
 cudaError_t sums(const OpContext& x, const Sums& s, cudaStream_t st) {
-    constexpr int kCols = RowPart<T, 1, STRIDED>::N * kThreads;
-    const int64_t chunks = ceil_div(s.a.tokens, s.chunk), slabs = ceil_div(s.a.cols, kCols);
-    const bool whole = rows_whole(s.a.y, s.a.ldy, s.a.tokens, sizeof(T));
-    cudaError_t e = launch(x, embedding_sums_kernel<T, TO, 1, STRIDED>, dim3((unsigned)(s.fillers + chunks * slabs)),
-                           kThreads, 0, st, s, (unsigned)slabs, whole);
+    const int64_t chunks = ceil_div(s.a.tokens, s.chunk), slabs = slabs_of(s.a);
+    const bool whole = s.a.cols % (16 / (int)sizeof(T)) == 0 && rows_whole(s.a.y, s.a.ldy, s.a.tokens, sizeof(T));
+    auto* kernel = whole ? embedding_sums_kernel<T, TO, true> : embedding_sums_kernel<T, TO, false>;
+    cudaError_t e =
+        launch(x, kernel, dim3((unsigned)(s.fillers + chunks * slabs)), kThreads, 0, st, s, (unsigned)slabs);
     const int64_t parts = ceil_div(s.a.cols, kJoinCols), want = (chunks - 1) * parts, most = (int64_t)x.num_sms * 4;
     if (e == cudaSuccess && chunks > 1)
         e = launch(x, embedding_join_kernel<TO>, dim3((unsigned)(want < most ? want : most)), kJoinThreads, 0, st, s,
@@ -546,11 +584,12 @@ cudaError_t backward(const OpContext& x, const heddle_embedding_grad_args& g, un
     m.count = s.count;
     m.crossing = reinterpret_cast<uint32_t*>(ws + at.crossing);
     m.partial = reinterpret_cast<float*>(ws + at.partial);
-    m.chunk = (int32_t)chunk_of(a.tokens);
+    m.chunk = (int32_t)chunk_of(a.tokens, slabs_of(a));
     m.accumulate = g.accumulate;
-    const int64_t most = (int64_t)x.num_sms * 2;
+    m.out_whole = a.cols % (16 / (int)sizeof(T)) == 0 && rows_whole(a.table, a.ldt, a.table_rows, sizeof(TO));
+    const int64_t most = (int64_t)x.num_sms * 8;
     m.fillers = g.accumulate ? 0 : (unsigned)(a.table_rows < most ? a.table_rows : most);
-    return a.cols % (16 / (int)sizeof(T)) ? sums<T, TO, true>(x, m, st) : sums<T, TO, false>(x, m, st);
+    return sums<T, TO>(x, m, st);
 }
 
 }  // namespace

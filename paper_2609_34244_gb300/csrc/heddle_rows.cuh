@@ -228,11 +228,11 @@ struct Ring {
 __device__ __forceinline__ uint32_t low_of(const void* p) { return (uint32_t)(uintptr_t)p; }
 
 // 16 bytes at p + skew, p at 16 bytes, skew below 16 and the same for a row; an
-// element's size divides it.
-__device__ __forceinline__ uint4 load_skewed(const unsigned char* p, uint32_t skew) {
+// element's size divides it.  `second`: whether the next 16 bytes are needed.
+__device__ __forceinline__ uint4 load_skewed(const unsigned char* p, uint32_t skew, bool second = true) {
     const uint4 a = *reinterpret_cast<const uint4*>(p);
     if (skew == 0) return a;
-    const uint4 b = *reinterpret_cast<const uint4*>(p + 16);
+    const uint4 b = second ? *reinterpret_cast<const uint4*>(p + 16) : make_uint4(0, 0, 0, 0);
     uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
     if (skew & 8) {
 #pragma unroll
