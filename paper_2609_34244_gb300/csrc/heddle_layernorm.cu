@@ -576,7 +576,8 @@ __global__ void __launch_bounds__(256)
 }
 
 // The blocks' sums, 32 columns of dw or dbias a block.
-constexpr int kJoin = 8;  // warps
+constexpr int kJoin = 8;     // warps
+constexpr int kAtOnce = 10;  // loads that a thread waits for together
 __global__ void __launch_bounds__(32 * kJoin)
     layer_norm_join_kernel(const float* partial, int blocks, int64_t cols, float* dw, float* dbias) {
     allow_dependents();
@@ -589,8 +590,13 @@ __global__ void __launch_bounds__(32 * kJoin)
     float v = 0.0f;
     if (i < cols) {
         const float* p = partial + (int64_t)blockIdx.y * blocks * cols + i;
-#pragma unroll 16
-        for (int b = warp; b < blocks; b += kJoin) v += p[b * cols];
+        for (int b0 = warp; b0 < blocks; b0 += kJoin * kAtOnce) {
+            float f[kAtOnce];
+#pragma unroll
+            for (int k = 0; k < kAtOnce; ++k) f[k] = b0 + k * kJoin < blocks ? p[(b0 + k * kJoin) * cols] : 0.0f;
+#pragma unroll
+            for (int k = 0; k < kAtOnce; ++k) v += f[k];
+        }
     }
     s[warp][lane] = v;
     __syncthreads();
