@@ -136,9 +136,16 @@ constexpr int kThreads = N > 8 || L == 8 ? 256 : N == 8 ? 768 : 1024;
 template <int L, int N>
 constexpr int kResident = L == 8 ? 4 : 1;  // blocks an SM
 
+// The loss from its sum over experts of choices times probabilities.
+__device__ __forceinline__ float balance(const heddle_router_args& a, float sum, int32_t tokens) {
+    const float n = (float)tokens;
+    return tokens ? sum * ((float)a.experts / (float)a.top_k) / n / n : 0.0f;
+}
+
 // Sums of a block: of probabilities and choices, sums[experts + 1][block], the
-// last of the tokens.
-template <class T, int L, int N>
+// last of the tokens.  With ONE block they are all, and it gives the results: a
+// second kernel would cost a few tokens as much as the first.
+template <class T, int L, int N, bool ONE>
 __global__ void __launch_bounds__(kThreads<L, N>, kResident<L, N>)
     router_kernel(const __grid_constant__ heddle_router_args a, float2* sums) {
     allow_dependents();
@@ -222,14 +229,30 @@ __global__ void __launch_bounds__(kThreads<L, N>, kResident<L, N>)
     }
     if (lane == 0 && tokens) atomicAdd(&csum[L * N], tokens);
     __syncthreads();
+    float loss = 0.0f;
     for (int i = threadIdx.x; i <= a.experts; i += kBlock) {
         float p = 0.0f;
         if (i < a.experts) {
 #pragma unroll 16
             for (int k = 0; k < kBlock / 32; ++k) p += psum[k][i];
         }
-        sums[(int64_t)i * gridDim.x + blockIdx.x] =
-            make_float2(p, __int_as_float(csum[i < a.experts ? i : L * N]));
+        const int32_t c = csum[i < a.experts ? i : L * N];
+        if (ONE) {
+            a.count[i] = c;
+            if (i < a.experts) loss = fmaf((float)c, p, loss);
+        } else {
+            sums[(int64_t)i * gridDim.x + blockIdx.x] = make_float2(p, __int_as_float(c));
+        }
+    }
+    if (ONE && a.loss) {
+        __shared__ float part[kBlock / 32];
+        loss = warp_sum(loss);
+        if (threadIdx.x % 32 == 0) part[threadIdx.x / 32] = loss;
+        __syncthreads();
+        if (threadIdx.x < 32) {
+            loss = warp_sum(threadIdx.x < kBlock / 32 ? part[threadIdx.x] : 0.0f);
+            if (threadIdx.x == 0) *a.loss = balance(a, loss, csum[L * N]);
+        }
     }
 }
 
@@ -298,10 +321,7 @@ __global__ void __launch_bounds__(kJoin)
         }
         tc::cluster_sync();  // the others' memory is read
     }
-    if (rank == 0 && threadIdx.x == 0) {
-        const float n = (float)tokens;
-        *a.loss = tokens ? loss * ((float)a.experts / (float)a.top_k) / n / n : 0.0f;
-    }
+    if (rank == 0 && threadIdx.x == 0) *a.loss = balance(a, loss, tokens);
 }
 
 template <class T, int L, int N>
@@ -408,17 +428,24 @@ int64_t blocks_of(const OpContext& x, const heddle_router_args& a) {
     });
 }
 
+// Whether one block does it all: for up to two rounds of its groups.
+bool one_block(const heddle_router_args& a) {
+    return with_split(a.experts, [&](auto l, auto n) {
+        return a.tokens <= 2 * kThreads<l.value, n.value> / l.value;
+    });
+}
+
 template <class T>
 cudaError_t forward(const OpContext& x, const heddle_router_args& a, unsigned char* ws, cudaStream_t st) {
-    const int64_t blocks = blocks_of(x, a);
     float2* sums = reinterpret_cast<float2*>(ws);
-    cudaError_t e = cudaSuccess;
-    if (blocks)
-        e = with_split(a.experts, [&](auto l, auto n) {
-            constexpr int threads = kThreads<l.value, n.value>;
-            return launch(x, router_kernel<T, l.value, n.value>, dim3((unsigned)blocks), threads, 0, st, a, sums);
-        });
-    if (e != cudaSuccess) return e;
+    const bool one = one_block(a);
+    const int64_t blocks = one ? 1 : blocks_of(x, a);
+    const cudaError_t e = with_split(a.experts, [&](auto l, auto n) {
+        constexpr int threads = kThreads<l.value, n.value>;
+        auto* kernel = one ? router_kernel<T, l.value, n.value, true> : router_kernel<T, l.value, n.value, false>;
+        return launch(x, kernel, dim3((unsigned)blocks), threads, 0, st, a, sums);
+    });
+    if (e != cudaSuccess || one) return e;
     cudaLaunchAttribute attr[2] = {};
     attr[0].id = cudaLaunchAttributeClusterDimension;
     attr[0].val.clusterDim = {kJoinCluster, 1, 1};
@@ -447,7 +474,7 @@ cudaError_t backward(const OpContext& x, const heddle_router_grad_args& g, cudaS
 }  // namespace
 
 size_t router_scratch(const OpContext& x, const heddle_router_args& a) {
-    return align256(sizeof(float2) * (size_t)blocks_of(x, a) * (a.experts + 1));
+    return one_block(a) ? 0 : align256(sizeof(float2) * (size_t)blocks_of(x, a) * (a.experts + 1));
 }
 
 cudaError_t launch_router(const OpContext& x, const heddle_router_args& a, unsigned char* ws, cudaStream_t st) {

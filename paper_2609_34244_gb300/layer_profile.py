@@ -12,11 +12,17 @@ the degree -- and its forward and backward passes are timed together:
   f = act(y w_gate^T) (y w_up^T)    heddle_gated_ffn
   z = f w_down^T + y                heddle_linear
 
-The norms of the hidden state that models have ahead of attention and of the
-feed-forward block are not part of it, nor are experts: the entries are those
-of the products, attention and norms per head of a dense layer, and too small
-by two passes over the hidden state in either direction.  The backward pass
-adds the two residual gradients with torch.
+With ``norms`` a layer norm of the hidden state precedes attention and the
+feed-forward block (heddle_layer_norm, whose gradient takes in the residual
+path's), and with ``dropout`` both blocks' results pass through dropout on
+their way into the residual stream (heddle_dropout):
+
+  y = x + dropout(attention(norm(x)) w_o^T),  z = y + dropout(ffn(norm(y)) w_down^T)
+
+Without ``norms`` the entries are those of the products, attention and norms
+per head alone, too small by two passes over the hidden state in either
+direction, and the backward pass adds the two residual gradients with torch.
+Experts are not part of it.
 
 ``python -m paper_2609_34244_gb300.layer_profile`` measures a layer, loads the
 profile beside a cluster of this GPU and slower types, and prices candidates.
@@ -49,6 +55,8 @@ class LayerShape:
     sinks: int = 0
     act: str = "silu"
     dtype: str = "bfloat16"
+    norms: bool = False    # of the hidden state, ahead of attention and the feed-forward block
+    dropout: float = 0.0   # of both blocks' results
 
     def shard(self, degree: int) -> tuple:
         """(query heads, key heads, feed-forward columns) of one of `degree`
@@ -105,6 +113,20 @@ class Layer:
         self.d_f, self.d_y, self.d_a = buf(n, self.ffn), buf(n, hid), buf(n, self.hq, d)
         self.d_q, self.d_k = buf(n, self.hq, d), buf(n, self.hk, d)
         self.d_qkv, self.d_x = buf(n, self.hq + 2 * self.hk, d), buf(n, hid)
+        if shape.norms:
+            for i in "12":
+                for name, t in (("norm", torch.ones(hid, dtype=self.dtype, device=device)),
+                                ("norm_bias", torch.zeros(hid, dtype=self.dtype, device=device))):
+                    setattr(self, name + i, t)
+                    self.grads[name + i] = buf(hid, dtype=torch.float32)
+            self.n1, self.n2 = buf(n, hid), buf(n, hid)
+            self.stats1, self.stats2 = (dict(mean=buf(n, dtype=torch.float32), rstd=buf(n, dtype=torch.float32))
+                                        for _ in range(2))
+        if shape.dropout:
+            self.block, self.d_block = buf(n, hid), buf(n, hid)
+            self.seed = seed
+            # the masks' step: a training loop adds one to it after each backward pass
+            self.step = torch.zeros(1, dtype=torch.int64, device=device)
 
     def _sequences(self, t):
         return t.view(self.shape.microbatch, self.shape.seq, *t.shape[1:])
@@ -113,27 +135,65 @@ class Layer:
         v = self.qkv[:, self.hq + self.hk:]
         return [self._sequences(t) for t in (self.q, self.k, v, self.a)]
 
+    def _project(self, a, w, out, residual, mask):
+        """out = residual + a w^T, the product dropped by the mask of that number."""
+        if not self.shape.dropout:
+            h.heddle_linear(self.ctx, a, w, out, residual=residual)
+            return
+        h.heddle_linear(self.ctx, a, w, self.block)
+        h.heddle_dropout(self.ctx, self.block, out, self.shape.dropout, self.seed, offset=mask << 32, step=self.step,
+                         residual=residual)
+
+    def _block_grad(self, d_out, mask):
+        """The gradient of the product in _project from that of its result."""
+        if not self.shape.dropout:
+            return d_out
+        h.heddle_dropout_backward(self.ctx, d_out, self.d_block, self.shape.dropout, self.seed, offset=mask << 32,
+                                  step=self.step)
+        return self.d_block
+
+    def _norm(self, i, x):
+        """The norm ahead of block i ("1": attention, "2": feed-forward)."""
+        if not self.shape.norms:
+            return x
+        out = getattr(self, "n" + i)
+        h.heddle_layer_norm(self.ctx, x, getattr(self, "norm" + i), getattr(self, "norm_bias" + i), out,
+                            **getattr(self, "stats" + i))
+        return out
+
+    def _norm_grad(self, i, d_in, x, d_residual):
+        """The gradient of x from that of its norm, in whose place it comes,
+        and that of the residual path."""
+        if not self.shape.norms:
+            return d_in.add_(d_residual)
+        h.heddle_layer_norm_backward(self.ctx, d_in, x, getattr(self, "norm" + i), **getattr(self, "stats" + i),
+                                     dx=d_in, dw=self.grads["norm" + i], dbias=self.grads["norm_bias" + i],
+                                     dres=d_residual)
+        return d_in
+
     def forward(self, x):
         """z of x ([microbatch * seq][hidden]); the buffers keep what backward reads."""
         hq, hk, n = self.hq, self.hk, x.shape[0]
-        h.heddle_linear(self.ctx, x, self.w_qkv, self.qkv.view(n, -1))
+        h.heddle_linear(self.ctx, self._norm("1", x), self.w_qkv, self.qkv.view(n, -1))
         h.heddle_qk_norm_rope(self.ctx, self.qkv[:, :hq], self.qkv[:, hq:hq + hk], self.wq, self.wk, self.q, self.k,
                               **self.rope)
         h.heddle_attention(self.ctx, *self._attention(), self.lse, window=self.shape.window, sinks=self.shape.sinks)
-        h.heddle_linear(self.ctx, self.a.view(n, -1), self.w_o, self.y, residual=x)
-        h.heddle_gated_ffn(self.ctx, self.y, self.w_gate, self.w_up, self.f, act=self.act, gate=self.gate, up=self.up)
-        h.heddle_linear(self.ctx, self.f, self.w_down, self.z, residual=self.y)
+        self._project(self.a.view(n, -1), self.w_o, self.y, x, 0)
+        h.heddle_gated_ffn(self.ctx, self._norm("2", self.y), self.w_gate, self.w_up, self.f, act=self.act,
+                           gate=self.gate, up=self.up)
+        self._project(self.f, self.w_down, self.z, self.y, 1)
         return self.z
 
     def backward(self, x, dz):
         """The gradient of x from that of z; the weights' are in ``grads``."""
         hq, hk, n, g = self.hq, self.hk, x.shape[0], self.grads
-        h.heddle_linear_backward(self.ctx, dz, self.f, self.w_down, dx=self.d_f, dw=g["w_down"])
-        h.heddle_gated_ffn_backward(self.ctx, self.d_f, self.y, self.w_gate, self.w_up, self.gate, self.up,
+        n1, n2 = (self.n1, self.n2) if self.shape.norms else (x, self.y)
+        h.heddle_linear_backward(self.ctx, self._block_grad(dz, 1), self.f, self.w_down, dx=self.d_f, dw=g["w_down"])
+        h.heddle_gated_ffn_backward(self.ctx, self.d_f, n2, self.w_gate, self.w_up, self.gate, self.up,
                                     act=self.act, dx=self.d_y, dwg=g["w_gate"], dwu=g["w_up"])
-        self.d_y.add_(dz)
-        h.heddle_linear_backward(self.ctx, self.d_y, self.a.view(n, -1), self.w_o, dx=self.d_a.view(n, -1),
-                                 dw=g["w_o"])
+        self._norm_grad("2", self.d_y, self.y, dz)
+        h.heddle_linear_backward(self.ctx, self._block_grad(self.d_y, 0), self.a.view(n, -1), self.w_o,
+                                 dx=self.d_a.view(n, -1), dw=g["w_o"])
         h.heddle_attention_backward(self.ctx, self._sequences(self.d_a), *self._attention(), self.lse,
                                     self._sequences(self.d_q), self._sequences(self.d_k),
                                     self._sequences(self.d_qkv[:, hq + hk:]), window=self.shape.window,
@@ -141,8 +201,8 @@ class Layer:
         h.heddle_qk_norm_rope_backward(self.ctx, self.d_q, self.d_k, self.qkv[:, :hq], self.qkv[:, hq:hq + hk],
                                        self.wq, self.wk, self.d_qkv[:, :hq], self.d_qkv[:, hq:hq + hk], g["wq"],
                                        g["wk"], **self.rope)
-        h.heddle_linear_backward(self.ctx, self.d_qkv.view(n, -1), x, self.w_qkv, dx=self.d_x, dw=g["w_qkv"])
-        return self.d_x.add_(self.d_y)
+        h.heddle_linear_backward(self.ctx, self.d_qkv.view(n, -1), n1, self.w_qkv, dx=self.d_x, dw=g["w_qkv"])
+        return self._norm_grad("1", self.d_x, x, self.d_y)
 
 
 def measure_layer(ctx, shape: LayerShape, degree: int = 1, reps: int = 5, warmup: int = 3) -> float:
@@ -222,9 +282,12 @@ def main(argv=None):
     ap.add_argument("--microbatch", type=int, default=1)
     ap.add_argument("--window", type=int, default=0)
     ap.add_argument("--sinks", type=int, default=0)
+    ap.add_argument("--norms", action="store_true", help="layer norms of the hidden state")
+    ap.add_argument("--dropout", type=float, default=0.0, help="of both blocks' results")
     ap.add_argument("--candidates", type=int, default=100_000)
     a = ap.parse_args(argv)
-    shape = LayerShape(a.hidden, a.heads, a.kv_heads, a.ffn, a.seq, a.microbatch, window=a.window, sinks=a.sinks)
+    shape = LayerShape(a.hidden, a.heads, a.kv_heads, a.ffn, a.seq, a.microbatch, window=a.window, sinks=a.sinks,
+                       norms=a.norms, dropout=a.dropout)
     w = W.make_workload("dense32", seed=0, n=a.candidates)
     n_layers = len(w.model["flops"])
     ctx = h.heddle_create(0)
