@@ -15,14 +15,6 @@
 
 #include "heddle_rows.cuh"
 
-#ifndef FWD_THREADS
-#define FWD_THREADS 1024
-#define GRAD_THREADS 512
-#define GRADODD 608
-#define GRAD32 1024
-#define FRING 0
-#define FWD_SHORT 4
-#endif
 namespace hd {
 namespace {
 
@@ -145,7 +137,7 @@ __device__ __forceinline__ float squares_of(const R& part, const uint32_t (&r)[R
         if (ENDS) {
             const float2 d = make_float2(part.in(2 * p) ? v[p].x : 0.0f, part.in(2 * p + 1) ? v[p].y : 0.0f);
             s = fma2(d, d, s);
-        } else if (part.in(2 * p)) {
+        } else if (part.in(2 * p / R::V * R::V)) {  // a unit is in or out as a whole
             s = fma2(v[p], v[p], s);
         }
     }
@@ -221,11 +213,11 @@ struct Total {
 template <>
 struct Total<0> : BlockSum {};
 
-constexpr int kShort = 256;  // threads a block of short rows
+constexpr int kShort = 256, kShortResident = 4;  // threads a block of short rows, and its blocks an SM
 
 // GL lanes a row; GL 0: the block.
 template <class T, int GL, int U, bool STRIDED, int MOST>
-__global__ void __launch_bounds__(MOST, GL ? FWD_SHORT : 1024 / MOST)
+__global__ void __launch_bounds__(MOST, GL ? kShortResident : MOST == 256 ? 3 : 1024 / MOST)
     layer_norm_kernel(const __grid_constant__ heddle_layer_norm_args a, bool whole) {
     extern __shared__ __align__(128) unsigned char shared[];
     allow_dependents();
@@ -262,13 +254,13 @@ __global__ void __launch_bounds__(MOST, GL ? FWD_SHORT : 1024 / MOST)
 
 // The same by a block for rows that do not lie at 16 bytes: through the ring,
 // read from and written to memory in units all the same.
-template <class T, int U, int MOST>
+template <class T, int U, bool STRIDED, int MOST>
 __global__ void __launch_bounds__(MOST, 1024 / MOST)
     layer_norm_ring_kernel(const __grid_constant__ heddle_layer_norm_args a, int stages, bool staged, uint32_t* err) {
     extern __shared__ __align__(128) unsigned char shared[];
     allow_dependents();
     await_previous();
-    using R = RowPart<T, U, false>;
+    using R = RowPart<T, U, STRIDED>;
     const R part{(int)threadIdx.x, (int)blockDim.x, (int)a.cols};
     const float cols = (float)a.cols, inv = 1.0f / cols;
     const T* x = static_cast<const T*>(a.x);
@@ -396,14 +388,14 @@ __global__ void __launch_bounds__(kShort, 2)
 // for the sums and once more for dx.  ROWS at a time between two barriers: two
 // where that leaves four ahead (26214 x 5120 bfloat16: 165 us, one at a time
 // 182), one where the slots are few (16384 x 8192: 168 us, two 189).
-template <class T, int U, bool WHOLE, int ROWS, int MOST>
+template <class T, int U, bool WHOLE, bool STRIDED, int ROWS, int MOST>
 __global__ void __launch_bounds__(MOST)
     layer_norm_grad_ring_kernel(const __grid_constant__ heddle_layer_norm_grad_args a, float* partial, int stages,
                                 int arrays, bool staged, uint32_t* err) {
     extern __shared__ __align__(128) unsigned char shared[];
     allow_dependents();
     await_previous();
-    using R = RowPart<T, U, false>;
+    using R = RowPart<T, U, STRIDED>;
     const R part{(int)threadIdx.x, (int)blockDim.x, (int)a.cols};
     const float inv = 1.0f / (float)a.cols;
     const T *x = static_cast<const T*>(a.x), *dy = static_cast<const T*>(a.dy),
@@ -489,9 +481,9 @@ __global__ void __launch_bounds__(MOST)
         float *pw = partial + (int64_t)blockIdx.x * a.cols, *pb = pw + (int64_t)gridDim.x * a.cols;
 #pragma unroll
         for (int p = 0; p < R::N / 2; ++p) {
-            const int i = part.at(2 * p);
+            const int i = part.at(2 * p), j = part.at(2 * p + 1);
             if (i < a.cols) pw[i] = dw[p].x, pb[i] = db[p].x;
-            if (i + 1 < a.cols) pw[i + 1] = dw[p].y, pb[i + 1] = db[p].y;
+            if (j < a.cols) pw[j] = dw[p].y, pb[j] = db[p].y;
         }
     }
     ring.leave(err);
@@ -619,10 +611,13 @@ constexpr int kShared = 208 * 1024;  // of an SM's, shared by the blocks that it
 enum Way { kLanes, kBlocks, kRing, kLongRows };
 struct Plan {
     Way way;
-    bool strided;      // a short row's values are dealt out one by one
+    // rows of no whole units, whose values are dealt out one by one; but not in a
+    // block's forward pass over 16-bit ones (65568 x 2047 bfloat16: units put
+    // together from two 153 us, value by value 175; backward 236 and 220)
+    bool strided;
     bool whole;        // whole units at 16 bytes throughout
     bool staged;       // rows leave by way of shared memory
-    int lanes, units;  // of a short row: lanes, units each
+    int lanes, units;  // of a short row: lanes; units a lane, or a thread of a block, holds
     int threads, stages;
     size_t shared;
     int64_t blocks;
@@ -639,14 +634,14 @@ void plan_short(const OpContext& x, Plan& p, int64_t rows, int64_t units, int th
 
 // `arrays` of rows through the ring, by up to `an_sm` blocks an SM: as many as
 // leave each three slots of `most` arrays.  `fixed`: shared memory beside it.
-void plan_ring(Plan& p, int64_t row_bytes, int arrays, int most, bool whole, int fixed, int& an_sm) {
+void plan_ring(Plan& p, int64_t row_bytes, int arrays, int most, bool whole, bool direct, int fixed, int& an_sm) {
     const int64_t place = row_place(row_bytes);
     auto stages = [&](int n, bool out) {
         return (kShared / an_sm - (int64_t)sizeof(RingBars) - fixed - (out ? place : 0)) / (n * place);
     };
     while (an_sm > 1 && stages(most, true) < 3) --an_sm;
     p.way = stages(most, false) >= 2 ? kRing : kLongRows;
-    p.staged = !whole && stages(arrays, true) >= 2;
+    p.staged = !whole && !direct && stages(arrays, true) >= 2;
     p.stages = (int)at_most(stages(arrays, p.staged), kRingStages);
     p.shared = sizeof(RingBars) + fixed + (p.stages * arrays + p.staged) * place;
 }
@@ -665,15 +660,24 @@ Plan plan_forward(const OpContext& x, const heddle_layer_norm_args& a) {
     const int64_t units = ceil_div(a.cols, V);
     p.strided = a.cols % V != 0;
     if (units <= 64) {
-        plan_short(x, p, a.rows, units, 256 * FWD_SHORT);
+        plan_short(x, p, a.rows, units, kShort * kShortResident);
         return p;
     }
     const bool whole = !p.strided && rows_whole(a.x, a.ldx, a.rows, size) && rows_whole(a.y, a.ldy, a.rows, size);
     p.threads = block_of(units);
+    p.units = kEach;
     p.way = units > kEach * kLong ? kLongRows : kBlocks;
-    p.shared = affine_bytes<T>(p.threads, kEach);
-    int an_sm = blocks_an_sm(FWD_THREADS, p.threads);
-    if (p.way == kBlocks && !whole) plan_ring(p, a.cols * size, 1, 1, false, (int)p.shared, an_sm);
+    int an_sm = blocks_an_sm(1024, p.threads);
+    // rows of 512 to 1024 units of 16-bit values by smaller blocks, three an SM:
+    // 16384 x 8192 bfloat16 takes 86 us, two units a thread 98 (26214 x 5120: 86
+    // and 96; 32768 x 4096 the other way round, 91 and 100)
+    if (whole && size == 2 && units > 512 && units <= 1024) {
+        p.units = 4;
+        p.threads = (int)ceil_div(ceil_div(units, 4), 32) * 32;
+        an_sm = blocks_an_sm(768, p.threads);
+    }
+    p.shared = affine_bytes<T>(p.threads, p.units);
+    if (p.way == kBlocks && !whole) plan_ring(p, a.cols * size, 1, 1, false, size == 4 && p.strided, (int)p.shared, an_sm);
     if (p.way == kLongRows) p.threads = kLong, an_sm = 2;
     p.blocks = at_most(a.rows, (int64_t)x.num_sms * an_sm);
     return p;
@@ -694,10 +698,11 @@ Plan plan_grad(const OpContext& x, const heddle_layer_norm_grad_args& a) {
     }
     p.threads = block_of(units);
     p.way = kLongRows;
-    int an_sm = blocks_an_sm(size == 2 ? GRAD_THREADS : p.strided ? GRADODD : GRAD32, p.threads);
+    // threads an SM, by the registers that each takes
+    int an_sm = blocks_an_sm(size == 2 ? 512 : p.strided ? 608 : 1024, p.threads);
     p.whole = !p.strided && rows_whole(a.x, a.ldx, a.rows, size) && rows_whole(a.dy, a.lddy, a.rows, size) &&
               rows_whole(a.dres, a.ldr, a.rows, size) && rows_whole(a.dx, a.lddx, a.rows, size);
-    if (units <= kEach * kLong) plan_ring(p, a.cols * size, a.dres ? 3 : 2, 3, p.whole, 0, an_sm);
+    if (units <= kEach * kLong) plan_ring(p, a.cols * size, a.dres ? 3 : 2, 3, p.whole, p.strided, 0, an_sm);
     if (p.way == kLongRows) p.threads = kLong, an_sm = 2;
     p.blocks = at_most(a.rows, (int64_t)x.num_sms * an_sm);
     return p;
@@ -725,10 +730,16 @@ cudaError_t forward_short(const OpContext& x, const heddle_layer_norm_args& a, c
 
 template <class T, int MOST>
 cudaError_t forward_blocks(const OpContext& x, const heddle_layer_norm_args& a, const Plan& p, cudaStream_t st) {
-    static std::atomic<uint64_t> asked[2];
-    if (p.way == kRing)
-        return launch_planned(x, layer_norm_ring_kernel<T, kEach, MOST>, asked[0], p, st, a, p.stages, p.staged, x.err);
-    return launch_planned(x, layer_norm_kernel<T, 0, kEach, false, MOST>, asked[1], p, st, a, true);
+    static std::atomic<uint64_t> asked[4];
+    if (p.way == kRing) {
+        auto* kernel = layer_norm_ring_kernel<T, kEach, false, MOST>;
+        if constexpr (sizeof(T) == 4)
+            if (p.strided) kernel = layer_norm_ring_kernel<T, kEach, true, MOST>;
+        return launch_planned(x, kernel, asked[p.strided], p, st, a, p.stages, p.staged, x.err);
+    }
+    if (p.units == 4)
+        return launch_planned(x, layer_norm_kernel<T, 0, 4, false, 256>, asked[2], p, st, a, true);
+    return launch_planned(x, layer_norm_kernel<T, 0, kEach, false, MOST>, asked[3], p, st, a, true);
 }
 
 template <class T>
@@ -753,18 +764,18 @@ cudaError_t backward_short(const OpContext& x, const heddle_layer_norm_grad_args
     return launch(x, kernel, dim3((unsigned)p.blocks), kShort, 0, st, a, partial, whole);
 }
 
-template <class T, bool WHOLE>
+template <class T, bool WHOLE, bool STRIDED>
 cudaError_t backward_ring(const OpContext& x, const heddle_layer_norm_grad_args& a, const Plan& p, float* partial,
                           cudaStream_t st) {
     static std::atomic<uint64_t> asked[3];
     const int arrays = a.dres ? 3 : 2;
     if (p.threads > 512)
-        return launch_planned(x, layer_norm_grad_ring_kernel<T, kEach, WHOLE, 1, 1024>, asked[0], p, st, a, partial,
-                              p.stages, arrays, p.staged, x.err);
+        return launch_planned(x, layer_norm_grad_ring_kernel<T, kEach, WHOLE, STRIDED, 1, 1024>, asked[0], p, st, a,
+                              partial, p.stages, arrays, p.staged, x.err);
     if (p.stages < 6 || !WHOLE)
-        return launch_planned(x, layer_norm_grad_ring_kernel<T, kEach, WHOLE, 1, 512>, asked[1], p, st, a, partial,
-                              p.stages, arrays, p.staged, x.err);
-    return launch_planned(x, layer_norm_grad_ring_kernel<T, kEach, WHOLE, 2, 512>, asked[2], p, st, a, partial,
+        return launch_planned(x, layer_norm_grad_ring_kernel<T, kEach, WHOLE, STRIDED, 1, 512>, asked[1], p, st, a,
+                              partial, p.stages, arrays, p.staged, x.err);
+    return launch_planned(x, layer_norm_grad_ring_kernel<T, kEach, true, false, 2, 512>, asked[2], p, st, a, partial,
                           p.stages, arrays, p.staged, x.err);
 }
 
@@ -774,7 +785,9 @@ cudaError_t backward_rows(const OpContext& x, const heddle_layer_norm_grad_args&
     if (p.way == kLanes)
         return p.strided ? backward_short<T, true>(x, a, p, partial, st)
                          : backward_short<T, false>(x, a, p, partial, st);
-    return p.whole ? backward_ring<T, true>(x, a, p, partial, st) : backward_ring<T, false>(x, a, p, partial, st);
+    if (p.strided) return backward_ring<T, false, true>(x, a, p, partial, st);
+    return p.whole ? backward_ring<T, true, false>(x, a, p, partial, st)
+                   : backward_ring<T, false, false>(x, a, p, partial, st);
 }
 
 template <class T>

@@ -249,15 +249,14 @@ __device__ __forceinline__ uint4 load_skewed(const unsigned char* p, uint32_t sk
     return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
-// The units of a row that lies in shared memory, `skew` bytes into its place;
-// the last one's values past the row's end are zeros.  WHOLE: no skew, and
-// whole units alone.
-template <bool WHOLE, class T, int U>
-__device__ __forceinline__ void load_units(uint32_t (&r)[4 * U], const RowPart<T, U, false>& part,
+// A row that lies in shared memory, `skew` bytes into its place; values past the
+// row's end are zeros.  WHOLE: no skew, and whole units alone.
+template <bool WHOLE, class T, int U, bool STRIDED>
+__device__ __forceinline__ void load_units(uint32_t (&r)[4 * U], const RowPart<T, U, STRIDED>& part,
                                            const unsigned char* place, uint32_t skew) {
     constexpr int V = 16 / sizeof(T);
-    if constexpr (WHOLE) {
-        part.load(r, reinterpret_cast<const T*>(place), true);
+    if constexpr (WHOLE || STRIDED) {
+        part.load(r, reinterpret_cast<const T*>(place + (WHOLE ? 0 : skew)), WHOLE);
     } else {
 #pragma unroll
         for (int u = 0; u < U; ++u) {
@@ -278,8 +277,8 @@ __device__ __forceinline__ void load_units(uint32_t (&r)[4 * U], const RowPart<T
 // of its own at 16 bytes), whole units and the ends value by value; value by
 // value where there is no place.  The block calls it together; between two
 // calls it meets at a barrier.
-template <bool WHOLE, class T, int U>
-__device__ __forceinline__ void store_units(T* dst, const RowPart<T, U, false>& part, const uint32_t (&r)[4 * U],
+template <bool WHOLE, class T, int U, bool STRIDED>
+__device__ __forceinline__ void store_units(T* dst, const RowPart<T, U, STRIDED>& part, const uint32_t (&r)[4 * U],
                                             unsigned char* place) {
     constexpr int V = 16 / sizeof(T);
     if (WHOLE) {
@@ -292,11 +291,16 @@ __device__ __forceinline__ void store_units(T* dst, const RowPart<T, U, false>& 
         part.store(dst, r, off == 0 && cols % V == 0);
         return;
     }
+    // its last unit whole: the place has room for it
+    if constexpr (STRIDED) {
+        part.store(reinterpret_cast<T*>(place), r, false);
+    } else {
 #pragma unroll
-    for (int u = 0; u < U; ++u)
-        if (part.in(u * V))
-            *reinterpret_cast<uint4*>(place + part.at(u * V) * sizeof(T)) =
-                make_uint4(r[4 * u], r[4 * u + 1], r[4 * u + 2], r[4 * u + 3]);
+        for (int u = 0; u < U; ++u)
+            if (part.in(u * V))
+                *reinterpret_cast<uint4*>(place + part.at(u * V) * sizeof(T)) =
+                    make_uint4(r[4 * u], r[4 * u + 1], r[4 * u + 2], r[4 * u + 3]);
+    }
     __syncthreads();
     const int skip = off / sizeof(T), head = skip ? (V - skip < cols ? V - skip : cols) : 0;
     const T* src = reinterpret_cast<const T*>(place);
