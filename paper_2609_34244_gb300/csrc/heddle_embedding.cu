@@ -39,43 +39,49 @@ __global__ void __launch_bounds__(kThreads)
     const int lane = threadIdx.x % GL, cols = (int)a.cols, u0 = blockIdx.y * GL * U + lane;
     const int64_t t0 = (int64_t)blockIdx.x * kGroups * TOKENS + threadIdx.x / GL;
     const float2 scale = both(a.scale);
-    int64_t row[TOKENS];
+    const T* table = static_cast<const T*>(a.table);
+    T* const y = static_cast<T*>(a.y) + t0 * a.ldy;
+    const int64_t y_step = kGroups * a.ldy;
+    int row[TOKENS], head[TOKENS];  // the values before the output's first unit
 #pragma unroll
     for (int j = 0; j < TOKENS; ++j) {
         const int64_t t = t0 + j * kGroups;
         bool past = false;
-        row[j] = t < a.tokens ? row_of(a, t, past) : -1;
+        row[j] = t < a.tokens ? (int)row_of(a, t, past) : -1;
         if (past && blockIdx.y == 0 && lane == 0) atomicOr(err, kErrOpToken);
+        head[j] = 0;
+        if (!WHOLE) {
+            head[j] = (0 - (low_of(y) + (uint32_t)(j * y_step * sizeof(T))) & 15) / (uint32_t)sizeof(T);
+            head[j] = head[j] < cols ? head[j] : cols;
+        }
     }
     uint4 v[TOKENS][U];
-    auto head_of = [&](const T* dst) {
-        const int head = WHOLE ? 0 : (int)((16 - ((uintptr_t)dst & 15)) & 15) / (int)sizeof(T);
-        return head < cols ? head : cols;
-    };
 #pragma unroll
     for (int j = 0; j < TOKENS; ++j) {
-        const int64_t t = t0 + j * kGroups;
-        const int head = head_of(static_cast<T*>(a.y) + t * a.ldy);
-        const T* src = static_cast<const T*>(a.table) + row[j] * a.ldt + head;
+        const T* src = table + (row[j] * a.ldt + head[j]);
         const uint32_t skew = WHOLE ? 0 : low_of(src) & 15;
-        const unsigned char* from = reinterpret_cast<const unsigned char*>((uintptr_t)src - skew);
-        const int units = row[j] >= 0 ? (cols - head) / V : 0;
+        const unsigned char* from = reinterpret_cast<const unsigned char*>(src) - skew + u0 * 16;
+        const int units = row[j] >= 0 ? (cols - head[j]) / V : 0;
 #pragma unroll
         for (int k = 0; k < U; ++k)
-            v[j][k] = u0 + k * GL < units ? load_skewed(from + (u0 + k * GL) * 16, skew) : make_uint4(0, 0, 0, 0);
+            v[j][k] = u0 + k * GL < units ? load_skewed(from + k * GL * 16, skew) : make_uint4(0, 0, 0, 0);
+    }
+    if (!WHOLE && blockIdx.y == 0 && lane < V) {  // the rows' ends: at most V - 1 values on either side
+#pragma unroll
+        for (int j = 0; j < TOKENS; ++j) {
+            if (t0 + j * kGroups >= a.tokens) break;
+            const int tail = head[j] + (cols - head[j]) / V * V + lane;
+            const T* src = table + row[j] * a.ldt;
+            T* dst = y + j * y_step;
+            if (lane < head[j]) dst[lane] = from_float<T>(row[j] >= 0 ? to_float(src[lane]) * a.scale : 0.0f);
+            if (tail < cols) dst[tail] = from_float<T>(row[j] >= 0 ? to_float(src[tail]) * a.scale : 0.0f);
+        }
     }
 #pragma unroll
     for (int j = 0; j < TOKENS; ++j) {
-        const int64_t t = t0 + j * kGroups;
-        if (t >= a.tokens) break;
-        T* dst = static_cast<T*>(a.y) + t * a.ldy;
-        const int head = head_of(dst), units = (cols - head) / V, tail = head + units * V;
-        if (!WHOLE && blockIdx.y == 0) {
-            const T* src = static_cast<const T*>(a.table) + row[j] * a.ldt;
-            auto one = [&](int i) { dst[i] = from_float<T>(row[j] >= 0 ? to_float(src[i]) * a.scale : 0.0f); };
-            if (lane < head) one(lane);
-            if (tail + lane < cols) one(tail + lane);
-        }
+        if (t0 + j * kGroups >= a.tokens) break;
+        T* dst = y + j * y_step + head[j] + u0 * V;
+        const int units = (cols - head[j]) / V;
 #pragma unroll
         for (int k = 0; k < U; ++k) {
             if (u0 + k * GL >= units) break;
@@ -85,7 +91,7 @@ __global__ void __launch_bounds__(kThreads)
                 for (int p = 0; p < V / 2; ++p) set_pair<T>(w, p, mul2(pair_of<T>(w, p), scale));
                 v[j][k] = make_uint4(w[0], w[1], w[2], w[3]);
             }
-            *reinterpret_cast<uint4*>(dst + head + (u0 + k * GL) * V) = v[j][k];
+            *reinterpret_cast<uint4*>(dst + k * GL * V) = v[j][k];
         }
     }
 }
@@ -356,7 +362,7 @@ __device__ __forceinline__ void add_out(const Sums& s, const R& part, int64_t ro
 }
 
 constexpr int kAhead = 8;  // rows fetched before any is added
-constexpr int kLeastRun = 16, kMostRun = 512;  // entries a block
+constexpr int kLeastRun = 8, kMostRun = 512;  // entries a block
 
 // A run of the sorted list and a range of columns a block.  A row whose
 // entries all lie in the run is written; the sums of one that began before it
@@ -517,18 +523,25 @@ cudaError_t lookup_any(const OpContext& x, const heddle_embedding_args& a, cudaS
     return whole ? lookup_typed<T, true>(x, a, st) : lookup_typed<T, false>(x, a, st);
 }
 
-// Entries a block of the sums takes: 64, so that few rows go over several runs;
-// fewer where that leaves SMs without a block, more beyond 2048 runs, which
-// bounds the parts that a row of up to a million tokens is joined from.
-int64_t chunk_of(int64_t tokens, int64_t slabs) {
-    int64_t c = 64;
-    while (c > kLeastRun && ceil_div(tokens, c) * slabs < 1024) c /= 2;
-    while (c < kMostRun && ceil_div(tokens, c) > 2048) c *= 2;
-    return c;
-}
 // Columns of a block of the sums: a unit a thread.
 int64_t slabs_of(const heddle_embedding_args& a) {
     return ceil_div(a.cols, kThreads * (a.dtype == HEDDLE_FP32 ? 4 : 8));
+}
+
+// Entries a block of the sums takes: 64, so that few rows go over several runs,
+// or fewer, so that the table's share of the tokens keeps the SMs busy; more
+// beyond 8192 runs, which bounds the parts that a row of up to four million
+// tokens is joined from.  (32771 tokens, an eighth of them of the table, 1023
+// values, added to what is there: 43 us with 32 a block, 31 with 8; 16384 tokens
+// of 4096 values, all of the table: their joining took 42 us with 16 a block, 13
+// with 64.)
+int64_t chunk_of(const heddle_embedding_args& a) {
+    const int64_t slabs = slabs_of(a);
+    const int64_t own = (int64_t)((double)a.tokens * ((double)a.table_rows / (double)a.vocab));
+    int64_t c = 64;
+    while (c > kLeastRun && ceil_div(own, c) * slabs < 1024) c /= 2;
+    while (c < kMostRun && ceil_div(a.tokens, c) > 8192) c *= 2;
+    return c;
 }
 
 struct Places {
@@ -537,7 +550,7 @@ struct Places {
 Places places(const heddle_embedding_args& a) {
     Places p;
     p.list = 256;
-    const size_t chunks = (size_t)ceil_div(a.tokens, chunk_of(a.tokens, slabs_of(a)));
+    const size_t chunks = (size_t)ceil_div(a.tokens, chunk_of(a));
     p.crossing = p.list + 2 * align256(sizeof(Entry) * (size_t)a.tokens);
     p.partial = p.crossing + align256(sizeof(uint32_t) * chunks);
     p.total = p.partial + align256(sizeof(float) * 2 * chunks * a.cols);
@@ -551,7 +564,7 @@ cudaError_t sums(const OpContext& x, const Sums& s, cudaStream_t st) {
     auto* kernel = whole ? embedding_sums_kernel<T, TO, true> : embedding_sums_kernel<T, TO, false>;
     cudaError_t e =
         launch(x, kernel, dim3((unsigned)(s.fillers + chunks * slabs)), kThreads, 0, st, s, (unsigned)slabs);
-    const int64_t parts = ceil_div(s.a.cols, kJoinCols), want = (chunks - 1) * parts, most = (int64_t)x.num_sms * 4;
+    const int64_t parts = ceil_div(s.a.cols, kJoinCols), want = (chunks - 1) * parts, most = (int64_t)x.num_sms * 8;
     if (e == cudaSuccess && chunks > 1)
         e = launch(x, embedding_join_kernel<TO>, dim3((unsigned)(want < most ? want : most)), kJoinThreads, 0, st, s,
                    (unsigned)parts);
@@ -584,7 +597,7 @@ cudaError_t backward(const OpContext& x, const heddle_embedding_grad_args& g, un
     m.count = s.count;
     m.crossing = reinterpret_cast<uint32_t*>(ws + at.crossing);
     m.partial = reinterpret_cast<float*>(ws + at.partial);
-    m.chunk = (int32_t)chunk_of(a.tokens, slabs_of(a));
+    m.chunk = (int32_t)chunk_of(a);
     m.accumulate = g.accumulate;
     m.out_whole = a.cols % (16 / (int)sizeof(T)) == 0 && rows_whole(a.table, a.ldt, a.table_rows, sizeof(TO));
     const int64_t most = (int64_t)x.num_sms * 8;

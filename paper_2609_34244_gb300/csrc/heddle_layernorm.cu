@@ -677,7 +677,8 @@ Plan plan_forward(const OpContext& x, const heddle_layer_norm_args& a) {
         an_sm = blocks_an_sm(768, p.threads);
     }
     p.shared = affine_bytes<T>(p.threads, p.units);
-    if (p.way == kBlocks && !whole) plan_ring(p, a.cols * size, 1, 1, false, size == 4 && p.strided, (int)p.shared, an_sm);
+    if (p.way == kBlocks && !whole)
+        plan_ring(p, a.cols * size, 1, 1, false, size == 4 && p.strided, (int)p.shared, an_sm);
     if (p.way == kLongRows) p.threads = kLong, an_sm = 2;
     p.blocks = at_most(a.rows, (int64_t)x.num_sms * an_sm);
     return p;
