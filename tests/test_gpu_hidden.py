@@ -101,6 +101,32 @@ def test_layer_norm_backward(lib, m, n, dt):
             assert torch.equal(dy, dx)
 
 
+@pytest.mark.parametrize("dt", ["bf16", "fp32"])
+@pytest.mark.parametrize("m,n", [(20000, 520), (9000, 1031), (20000, 1032), (2000, 5121), (3000, 8192), (1200, 8190),
+                                 (700, 9000), (500, 16380)])
+def test_layer_norm_of_many_rows_a_block(lib, m, n, dt):
+    """More rows than a block holds ahead: places of the ring are taken again
+    and again."""
+    h, ctx = lib
+    dt = TYPES[dt]
+    g = gen(m + n)
+    x, dy, dres = (rand(g, m, n, dt=dt) for _ in range(3))
+    w, b = 1 + rand(g, n, dt=dt, std=0.3), rand(g, n, dt=dt)
+    y, dx, mean, rstd, dw, db = torch.empty_like(x), torch.empty_like(x), floats(m), floats(m), floats(n), floats(n)
+    h.heddle_layer_norm(ctx, x, w, b, y, mean=mean, rstd=rstd)
+    (_, _), (_, _), (wy, ey) = H.layer_norm(x, w, b, 1e-5)
+    close(y, wy, ey, "y")
+    del wy, ey
+    h.heddle_layer_norm_backward(ctx, dy, x, w, mean, rstd, dx=dx, dw=dw, dbias=db, dres=dres)
+    (wx, ex), (ww, ew), (wb, eb) = H.layer_norm_grads(dy, x, w, mean, rstd, dres)
+    close(dx, wx, ex, "dx")
+    close(dw, ww, ew, "dw")
+    close(db, wb, eb, "dbias")
+    again = [torch.empty_like(dx), floats(n), floats(n)]
+    h.heddle_layer_norm_backward(ctx, dy, x, w, mean, rstd, dx=again[0], dw=again[1], dbias=again[2], dres=dres)
+    assert torch.equal(again[0], dx) and torch.equal(again[1], dw) and torch.equal(again[2], db)
+
+
 def test_layer_norm_large_means_and_values_that_are_not_finite(lib):
     h, ctx = lib
     g = gen(3)
@@ -256,7 +282,7 @@ def token_list(g, t, vocab, kind):
 LOOKUPS = [  # tokens, vocabulary, shards, columns
     (1, 1, 1, 1), (1, 100, 1, 64), (16, 32000, 1, 4096), (5, 40, 4, 7), (300, 1000, 1, 136), (1000, 600, 3, 513),
     (2100, 70, 1, 1023), (4097, 5000, 2, 200), (40000, 300000, 1, 24), (33000, 4096, 1, 40), (3000, 1 << 20, 1, 8),
-    (70001, 33, 1, 130), (600, 1200, 1, 5000),
+    (70001, 33, 1, 130), (600, 1200, 1, 5000), (600000, 50, 1, 8), (9000, 900, 1, 1040),
 ]
 
 
@@ -403,6 +429,7 @@ def check_router(h, ctx, logits, k, valid, normalize, g, pad=0, skip=0):
 ROUTERS = [  # tokens, experts, chosen
     (1, 1, 1), (1, 64, 2), (5, 2, 2), (16, 64, 2), (33, 7, 3), (100, 64, 8), (70, 60, 32), (301, 65, 4), (3000, 8, 2),
     (40, 128, 8), (77, 250, 8), (64, 256, 32), (19, 512, 6), (9, 1000, 5), (6, 1024, 32), (20001, 16, 2),
+    (64, 64, 2), (65, 64, 2), (200, 1024, 32), (100, 512, 6), (5000, 250, 8), (33, 100, 1),
 ]
 
 
