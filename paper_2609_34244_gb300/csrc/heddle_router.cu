@@ -181,7 +181,7 @@ __global__ void __launch_bounds__(kThreads<L, N>, kResident<L, N>)
             if (!s.sound) key[j] = 0;
         }
         // the chosen ones: lane j % L keeps the j-th
-        float mine_p[kRounds] = {}, chosen = 0.0f;
+        float value[kRounds] = {}, chosen = 0.0f;
         int mine[kRounds];
 #pragma unroll
         for (int q = 0; q < kRounds; ++q) {
@@ -193,31 +193,40 @@ __global__ void __launch_bounds__(kThreads<L, N>, kResident<L, N>)
                 best = g.largest(best);
                 if (best <= kLowest<T>) break;  // none is left
                 int at;
-                float e;
                 if constexpr (kPacked) {
-                    at = 0xffff - (int)(best & 0xffffu), e = packed_value<T>(best);
+                    at = 0xffff - (int)(best & 0xffffu);
 #pragma unroll
                     for (int i = 0; i < N; ++i) key[i] = key[i] == best ? 0 : key[i];
                 } else {
-                    at = INT32_MAX, e = value_of(best);
+                    at = INT32_MAX;
 #pragma unroll
                     for (int i = N - 1; i >= 0; --i) at = key[i] == best ? lane + i * L : at;
                     at = g.least(at);
 #pragma unroll
                     for (int i = 0; i < N; ++i) key[i] = at == lane + i * L ? 0 : key[i];
                 }
-                e = expf(e - s.top);
-                chosen += e;
-                if (j == lane) mine[q] = at, mine_p[q] = e;
+                if (j == lane) mine[q] = at, value[q] = __uint_as_float(best);
             }
         }
+#pragma unroll
+        for (int q = 0; q < kRounds; ++q) {
+            const uint32_t key_q = __float_as_uint(value[q]);
+            float v_q;
+            if constexpr (kPacked)
+                v_q = packed_value<T>(key_q);
+            else
+                v_q = value_of(key_q);
+            value[q] = mine[q] >= 0 ? expf(v_q - s.top) : 0.0f;
+            chosen += value[q];
+        }
+        chosen = g.sum(chosen);
         const float over = !a.normalize ? s.inv : chosen > 0.0f ? 1.0f / chosen : 0.0f;
 #pragma unroll
         for (int q = 0; q < kRounds; ++q) {
             if (q * L + lane >= a.top_k) break;
             if (mine[q] >= 0) atomicAdd(&csum[mine[q]], 1);  // whole numbers
             a.expert[t * a.top_k + q * L + lane] = mine[q];
-            a.weight[t * a.top_k + q * L + lane] = s.sound ? mine_p[q] * over : NAN;
+            a.weight[t * a.top_k + q * L + lane] = s.sound ? value[q] * over : NAN;
         }
     }
     // a warp's groups, then the block's warps
