@@ -1,11 +1,12 @@
 // heddle_embedding.cu -- the embedding and the gradient of its table.
 //
 // Bound by memory: rows are copied, and the gradient's rows are written once
-// each.  The gradient sorts (row, token) pairs, so that a row's terms lie
-// together in the order of their tokens: one cluster of CTAs sorts while the
-// others write zeros to the rows that have no token.  Then blocks add up runs
-// of the sorted list, and the sums of rows that go over several blocks' parts
-// are joined in order.
+// each.  The gradient sorts (row, token) pairs, by one cluster of CTAs, so that
+// a row's terms lie together in the order of their tokens; then blocks add up
+// runs of the sorted list, others write zeros to the rows that have no token,
+// and the sums of rows that go over several runs are joined in order.
+// 16384 tokens, 131072 rows of 4096 bfloat16 values: 28 us for the rows, 17 to
+// sort, 176 for sums and zeros (1.2 GB), 10 to join.
 
 #include <atomic>
 
@@ -27,7 +28,7 @@ constexpr int kThreads = 128;
 
 // GL threads a token's row, U units of 16 bytes a thread: those that the
 // output's row is made of; TOKENS of them one after the other, their loads
-// together (32771 tokens of 1023 values, one at a time: 35 us, mostly waits).
+// together.
 // WHOLE: rows of whole units at 16 bytes; else units are put together from the
 // two of the table that hold them, and the row's ends go value by value.
 template <class T, int GL, int U, int TOKENS, bool WHOLE>
@@ -252,10 +253,10 @@ struct Sums {
     heddle_embedding_args a;  // y: the gradient in
     void* out;
     const Entry* list;
-    int64_t* count;     // of entries, and of rows that go over several runs
+    int64_t* count;      // of entries, and of rows that go over several runs
     uint32_t* crossing;  // the runs that these begin in
-    float* partial;     // [chunk][2][cols]
-    int32_t chunk;   // entries a block
+    float* partial;      // [chunk][2][cols]
+    int32_t chunk;       // entries a block
     int32_t accumulate;
     int32_t out_whole;  // the gradient's rows are whole units at 16 bytes
     // blocks that write zeros to the rows without tokens, behind the others: many
@@ -266,8 +267,27 @@ struct Sums {
 
 // Zeros to the gradient's rows that the sorted list does not name, a range of
 // rows a block: kWindow of them are marked at a time, the others written by
-// bulk copies out of shared memory where they lie at 16 bytes.
+// bulk copies out of shared memory where they lie at 16 bytes.  Entries of the
+// window are gone through, or, where they are many for its rows (padding tokens
+// of one row), searched for each: 262144 tokens of one row, 32000 rows, took
+// 2.9 ms with one thread after the other in place of 0.7.
 constexpr int kWindow = 8192, kZeros = 8192;
+constexpr int kScan = 8;  // entries of the list that a thread waits for together
+
+// The first entry of lo .. hi whose row is `row` or behind it, hi if there is
+// none: 32 probes at a time, by a whole warp.
+__device__ __forceinline__ int64_t first_of(const Entry* list, int64_t lo, int64_t hi, int64_t row) {
+    const int lane = threadIdx.x % 32;
+    while (lo < hi) {
+        const int64_t step = ceil_div(hi - lo, 32), at = lo + step * lane;
+        const int below = __popc(__ballot_sync(~0u, at < hi && list[at].row < row));
+        if (below == 0) break;
+        hi = lo + step * below < hi ? lo + step * below : hi;
+        lo += step * (below - 1) + 1;
+    }
+    return lo;
+}
+
 template <class TO>
 __device__ __noinline__ void fill_rows(const Sums& s, int64_t part) {
     __shared__ uint32_t marks[kWindow / 32];
@@ -286,18 +306,36 @@ __device__ __noinline__ void fill_rows(const Sums& s, int64_t part) {
         __syncthreads();
         for (int i = threadIdx.x; i < ceil_div(to - from, 32); i += kThreads) marks[i] = 0;
         __syncthreads();
-        int64_t lo = 0, hi = n;  // the first entry from `from` on, 32 probes at a time
-        while (lo < hi) {
-            const int64_t step = ceil_div(hi - lo, 32), at = lo + step * lane;
-            const int below = __popc(__ballot_sync(~0u, at < hi && s.list[at].row < from));
-            if (below == 0) break;
-            hi = lo + step * below < hi ? lo + step * below : hi;
-            lo += step * (below - 1) + 1;
-        }
-        for (int64_t i = lo + threadIdx.x; i < n; i += kThreads) {
-            const int64_t row = s.list[i].row;
-            if (row >= to) break;
-            atomicOr(&marks[(row - from) / 32], 1u << ((row - from) % 32));
+        // its entries; few are gone through, many are searched for its rows
+        const int64_t lo = first_of(s.list, 0, n, from), hi = first_of(s.list, lo, n, to);
+        auto mark = [&](int64_t row) {
+            const uint32_t bit = 1u << ((row - from) % 32);
+            uint32_t& word = marks[(row - from) / 32];
+            if (!(*(volatile uint32_t*)&word & bit)) atomicOr(&word, bit);
+        };
+        const int64_t a_row = 64 - __clzll(hi - lo);
+        if (ceil_div(hi - lo, kScan * kThreads) <= ceil_div(to - from, kThreads) * a_row) {
+            for (int64_t i = lo + threadIdx.x; i < hi; i += kScan * kThreads) {
+                uint32_t rows[kScan];
+#pragma unroll
+                for (int k = 0; k < kScan; ++k)
+                    if (i + k * kThreads < hi) rows[k] = s.list[i + k * kThreads].row;
+#pragma unroll
+                for (int k = 0; k < kScan; ++k)
+                    if (i + k * kThreads < hi) mark(rows[k]);
+            }
+        } else {
+            for (int64_t row = from + threadIdx.x; row < to; row += kThreads) {
+                int64_t i = lo, end = hi;
+                while (i < end) {
+                    const int64_t mid = (i + end) / 2;
+                    if (s.list[mid].row < row)
+                        i = mid + 1;
+                    else
+                        end = mid;
+                }
+                if (i < hi && s.list[i].row == row) mark(row);
+            }
         }
         __syncthreads();
         if (bulk) {  // a row a thread
@@ -446,10 +484,13 @@ __global__ void __launch_bounds__(kThreads)
         s.crossing[atomicAdd(reinterpret_cast<unsigned long long*>(s.count + 1), 1ull)] = chunk;
 }
 
-// Rows that go over several runs, 1024 columns of one a block at a time.  (A
-// block for every run, most of which have nothing to do, took 40 us for 16384
-// tokens; narrow slabs, each with the search and its waits, 36.)
+// Rows that go over several runs, 1024 columns of one a block at a time: 262144
+// tokens of 1024 values, half of one row, take 238 us, 346 with the runs' parts
+// fetched one after the other.  (A block for every run, most of which have
+// nothing to do, took 40 us for 16384 tokens where this takes 10; narrow slabs,
+// each with the search and its waits, 36.)
 constexpr int kJoinThreads = 256, kJoinCols = 4 * kJoinThreads;
+constexpr int kJoinAhead = 16;  // runs that a thread waits for together
 template <class TO>
 __global__ void __launch_bounds__(kJoinThreads)
     embedding_join_kernel(const __grid_constant__ Sums s, unsigned slabs) {
@@ -475,12 +516,20 @@ __global__ void __launch_bounds__(kJoinThreads)
 #pragma unroll
         for (int k = 0; k < 4; ++k)
             sum[k] = col + k * kJoinThreads < s.a.cols ? from[s.a.cols + k * kJoinThreads] : 0.0f;
-#pragma unroll 8
-        for (int64_t p = begin + 1; p <= last; ++p) {
-            from += 2 * s.a.cols;
+        for (int64_t p = begin + 1; p <= last; p += kJoinAhead) {
+            float v[kJoinAhead][4];
 #pragma unroll
-            for (int k = 0; k < 4; ++k)
-                if (col + k * kJoinThreads < s.a.cols) sum[k] += from[k * kJoinThreads];
+            for (int j = 0; j < kJoinAhead; ++j) {
+                from += 2 * s.a.cols;
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+                    v[j][k] = p + j <= last && col + k * kJoinThreads < s.a.cols ? from[k * kJoinThreads] : 0.0f;
+            }
+#pragma unroll
+            for (int j = 0; j < kJoinAhead; ++j) {
+#pragma unroll
+                for (int k = 0; k < 4; ++k) sum[k] += v[j][k];
+            }
         }
         TO* p = static_cast<TO*>(s.out) + row * s.a.ldt + col;
 #pragma unroll
@@ -501,10 +550,16 @@ cudaError_t lookup(const OpContext& x, const heddle_embedding_args& a, cudaStrea
     return launch(x, embedding_kernel<T, GL, U, TOKENS, WHOLE>, grid, kThreads, 0, st, a, x.err);
 }
 
+// Threads a token, units a thread and tokens at a time.  Few tokens take a unit
+// a thread (64 of 1024 bfloat16 values: 1.5 us, and 1.9 by four at a time), so
+// that more SMs take part.  Others keep several loads of a thread on their way:
+// 16384 tokens of 1024 values take 10.3 us, one at a time 17.5; beyond 128 units
+// those of one token (512 of 4096 values 2.3 us, four tokens at a time 2.6;
+// 16384 of them 39.2 and 37.9).
 template <class T, bool WHOLE>
 cudaError_t lookup_typed(const OpContext& x, const heddle_embedding_args& a, cudaStream_t st) {
     const int64_t units = ceil_div(a.cols, 16 / (int)sizeof(T));
-    if (a.tokens * units < (int64_t)x.num_sms * 1024)  // a unit a thread, so that more SMs take part
+    if (a.tokens * units < (int64_t)x.num_sms * 1024)
         return units <= 16   ? lookup<T, 16, 1, 1, WHOLE>(x, a, st)
                : units <= 32 ? lookup<T, 32, 1, 1, WHOLE>(x, a, st)
                              : lookup<T, 128, 1, 1, WHOLE>(x, a, st);
@@ -528,17 +583,16 @@ int64_t slabs_of(const heddle_embedding_args& a) {
     return ceil_div(a.cols, kThreads * (a.dtype == HEDDLE_FP32 ? 4 : 8));
 }
 
-// Entries a block of the sums takes: 64, so that few rows go over several runs,
-// or fewer, so that the table's share of the tokens keeps the SMs busy; more
-// beyond 8192 runs, which bounds the parts that a row of up to four million
-// tokens is joined from.  (32771 tokens, an eighth of them of the table, 1023
-// values, added to what is there: 43 us with 32 a block, 31 with 8; 16384 tokens
-// of 4096 values, all of the table: their joining took 42 us with 16 a block, 13
-// with 64.)
+// Entries a block of the sums takes: as many as leave 1024 blocks for the
+// table's share of the tokens, so that few rows go over several runs.  (16384
+// tokens of 4096 bfloat16 values, half of them of one row, into 32000 rows of
+// 32 bits: 142 us, 2048 blocks 159, 512 137; 262144 tokens of 1024 values, any
+// row: 217, 227 and 237.)  More beyond 8192 runs, which bounds the parts that a
+// row of up to four million tokens is joined from.
 int64_t chunk_of(const heddle_embedding_args& a) {
     const int64_t slabs = slabs_of(a);
     const int64_t own = (int64_t)((double)a.tokens * ((double)a.table_rows / (double)a.vocab));
-    int64_t c = 64;
+    int64_t c = kMostRun;
     while (c > kLeastRun && ceil_div(own, c) * slabs < 1024) c /= 2;
     while (c < kMostRun && ceil_div(a.tokens, c) > 8192) c *= 2;
     return c;
