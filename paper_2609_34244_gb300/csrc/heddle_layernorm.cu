@@ -1,15 +1,16 @@
 // heddle_layernorm.cu -- layer norm and its gradients.
 //
-// Bound by memory.  A row is held by a group of threads, two 16-byte units each at most:
-// its mean first, then the squares of its deviations from it, so that a large
-// mean costs no digits and nothing is read from memory twice.  Short rows take
-// 4 to 32 lanes of a warp, others a block, which walks over rows.  Gradients of
-// such rows are read through a ring in shared memory that bulk copies fill
-// ahead; the weights' sums over rows stay in registers, one set a block, and a
-// second kernel adds the sets in order.  Arithmetic runs on two values at a
-// time, and 16-bit values are taken out of their words in pairs: one by one,
-// bfloat16 was bound by instructions (16384 x 8192: forward 149 us, backward
-// 350).
+// Bound by memory.  A row is held by a group of threads, a few 16-byte units
+// each: its mean first, then the squares of its deviations from it, so that a
+// large mean costs no digits and nothing is read from memory twice.  Short rows
+// take 4 to 32 lanes of a warp, others a block, which walks over rows.
+// Gradients of such rows are read through a ring in shared memory that bulk
+// copies fill ahead; the weights' sums over rows stay in registers, one set a
+// block, and a second kernel adds the sets in order.  Arithmetic runs on two
+// values at a time, and 16-bit values are used as they lie in their words:
+// 16384 x 8192 bfloat16 takes 86 us forward (6.2 TB/s) and 169 backward (6.4,
+// with the join); taken out one by one they were bound by instructions, 149
+// and 350.
 
 #include <atomic>
 
@@ -213,11 +214,19 @@ struct Total {
 template <>
 struct Total<0> : BlockSum {};
 
-constexpr int kShort = 256, kShortResident = 4;  // threads a block of short rows, and its blocks an SM
+constexpr int kShort = 256;  // threads a block of short rows
+// Its blocks an SM, by the registers of U units a thread.  (2^20 x 64 floats
+// forward: 89 us by six, 102 by four; 262144 x 512 bfloat16: 88 by three, 91 by
+// four, 166 by six.  2^20 x 128 bfloat16 backward: 174 by four, 230 by two, 272
+// by five.)
+template <class T, int U>
+constexpr int kShortResident = U == 1 ? (sizeof(T) == 4 ? 6 : 4) : sizeof(T) == 4 ? 4 : 3;
+template <int U>
+constexpr int kShortGradResident = U == 1 ? 4 : 2;
 
 // GL lanes a row; GL 0: the block.
 template <class T, int GL, int U, bool STRIDED, int MOST>
-__global__ void __launch_bounds__(MOST, GL ? kShortResident : MOST == 256 ? 3 : 1024 / MOST)
+__global__ void __launch_bounds__(MOST, GL ? kShortResident<T, U> : MOST == 256 ? 3 : 1024 / MOST)
     layer_norm_kernel(const __grid_constant__ heddle_layer_norm_args a, bool whole) {
     extern __shared__ __align__(128) unsigned char shared[];
     allow_dependents();
@@ -334,7 +343,7 @@ __device__ __forceinline__ void grad_row(const R&, uint32_t (&out)[R::kWords], c
 
 // With the sums over rows, partial[dw, db][block][cols].
 template <class T, int GL, int U, bool STRIDED>
-__global__ void __launch_bounds__(kShort, 2)
+__global__ void __launch_bounds__(kShort, kShortGradResident<U>)
     layer_norm_grad_kernel(const __grid_constant__ heddle_layer_norm_grad_args a, float* partial, bool whole) {
     allow_dependents();
     await_previous();
@@ -471,7 +480,6 @@ __global__ void __launch_bounds__(MOST)
                 }
                 if (dres) load_units<WHOLE>(rv, part, at[i][2], rl + i * rd & 15);
                 grad_row<T>(part, gv, xv, gv, w, rv, m[i], s[i], v[2 * i] * inv, v[2 * i + 1] * inv);
-                if (!WHOLE && i) __syncthreads();  // the row before has left its place on its way out
                 store_units<WHOLE>(dx, part, gv, staged ? out : nullptr);
             }
         }
@@ -624,12 +632,15 @@ struct Plan {
 };
 
 // Short rows: up to 64 units, of which a lane has one, or two of 32 lanes.
-void plan_short(const OpContext& x, Plan& p, int64_t rows, int64_t units, int threads_an_sm) {
+// (2^20 x 128 bfloat16 by 16 lanes: 101 us, by 32 167; 262144 x 512 by two units
+// a lane or by blocks: forward 88 and 92, backward 175 and 182; 522247 x 257: 228
+// and 389.)
+void plan_short(const OpContext& x, Plan& p, int64_t rows, int64_t units, int by_one, int by_two) {
     p.way = kLanes;
     p.lanes = units <= 4 ? 4 : units <= 8 ? 8 : units <= 16 ? 16 : 32;
     p.units = units <= 32 ? 1 : 2;
     p.threads = kShort;
-    p.blocks = at_most(ceil_div(rows, kShort / p.lanes), (int64_t)x.num_sms * (threads_an_sm / kShort));
+    p.blocks = at_most(ceil_div(rows, kShort / p.lanes), (int64_t)x.num_sms * (p.units == 1 ? by_one : by_two));
 }
 
 // `arrays` of rows through the ring, by up to `an_sm` blocks an SM: as many as
@@ -660,7 +671,7 @@ Plan plan_forward(const OpContext& x, const heddle_layer_norm_args& a) {
     const int64_t units = ceil_div(a.cols, V);
     p.strided = a.cols % V != 0;
     if (units <= 64) {
-        plan_short(x, p, a.rows, units, kShort * kShortResident);
+        plan_short(x, p, a.rows, units, kShortResident<T, 1>, kShortResident<T, 2>);
         return p;
     }
     const bool whole = !p.strided && rows_whole(a.x, a.ldx, a.rows, size) && rows_whole(a.y, a.ldy, a.rows, size);
@@ -694,12 +705,13 @@ Plan plan_grad(const OpContext& x, const heddle_layer_norm_grad_args& a) {
     const int64_t units = ceil_div(a.cols, V);
     p.strided = a.cols % V != 0;
     if (units <= 64) {
-        plan_short(x, p, a.rows, units, 512);
+        plan_short(x, p, a.rows, units, kShortGradResident<1>, kShortGradResident<2>);
         return p;
     }
     p.threads = block_of(units);
     p.way = kLongRows;
-    // threads an SM, by the registers that each takes
+    // threads an SM, by the registers that each takes (131072 x 1024 bfloat16:
+    // 174 us by 512, 211 by 1024)
     int an_sm = blocks_an_sm(size == 2 ? 512 : p.strided ? 608 : 1024, p.threads);
     p.whole = !p.strided && rows_whole(a.x, a.ldx, a.rows, size) && rows_whole(a.dy, a.lddy, a.rows, size) &&
               rows_whole(a.dres, a.ldr, a.rows, size) && rows_whole(a.dx, a.lddx, a.rows, size);
@@ -738,8 +750,8 @@ cudaError_t forward_blocks(const OpContext& x, const heddle_layer_norm_args& a, 
             if (p.strided) kernel = layer_norm_ring_kernel<T, kEach, true, MOST>;
         return launch_planned(x, kernel, asked[p.strided], p, st, a, p.stages, p.staged, x.err);
     }
-    if (p.units == 4)
-        return launch_planned(x, layer_norm_kernel<T, 0, 4, false, 256>, asked[2], p, st, a, true);
+    if constexpr (sizeof(T) == 2)
+        if (p.units == 4) return launch_planned(x, layer_norm_kernel<T, 0, 4, false, 256>, asked[2], p, st, a, true);
     return launch_planned(x, layer_norm_kernel<T, 0, kEach, false, MOST>, asked[3], p, st, a, true);
 }
 
