@@ -823,7 +823,8 @@ typedef struct {
 heddle_status heddle_layer_norm_backward(heddle_ctx* ctx, const heddle_layer_norm_grad_args* args, void* stream);
 
 /* Dropout, its result added to the residual stream:
- *   y = (u < D ? 0 : x s) + residual,  D = p 2^32 rounded,  s = 2^32 / (2^32 - D)
+ *   y = (u < D ? 0 : x s) + residual,  D = p 2^32 rounded (below 2^32),
+ *   s = 2^32 / (2^32 - D)
  * The number u of element i = row * cols + col (whatever the strides) is word
  * i % 4 of Philox4x32-10 with the key `seed` (low word first) and the counter
  * (i / 4, offset + *step), 64 bits each, low words first: the mask is never

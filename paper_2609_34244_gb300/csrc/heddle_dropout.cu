@@ -5,7 +5,8 @@
 // "Parallel random numbers: as easy as 1, 2, 3", 2011): ten rounds of two
 // 32 x 32 products and exclusive ors over a counter of 128 bits, four words a
 // counter, one a value.  They cost about 60 instructions for four values, and
-// memory brings four 16-bit values to an SM in a cycle.
+// memory brings four 16-bit values to an SM in a cycle.  16384 x 8192 bfloat16
+// with the residual, forward and backward: 227 us, 5.9 TB/s.
 
 #include "heddle_rows.cuh"
 
@@ -66,7 +67,7 @@ __device__ __forceinline__ float kept(const Dropout& d, uint32_t u, float x, flo
 constexpr int kThreads = 256;
 // Blocks an SM: as many as the numbers' registers allow without spilling, in
 // four rounds (a unit a thread in more or fewer registers, two units at a
-// time, the next unit fetched ahead: 228 to 290 us where this takes 224).
+// time, the next unit fetched ahead: 230 to 298 us where this takes 227).
 constexpr int kResident = 6, kTurns = 4;
 
 // Whole 16-byte units.  FLAT: rows follow each other and are taken as one,
