@@ -548,7 +548,12 @@ PyObject* bind(PyObject*, PyObject* const* v, Py_ssize_t count) {
     return guarded<3>(count, [&] {
         void* found[kEntries + 1];
         for (int i = 0; i <= kEntries; ++i) {
-            PyObject* p = PyMapping_GetItemString(v[0], i < kEntries ? kNames[i] : "heddle_device");
+            const char* name = i < kEntries ? kNames[i] : "heddle_device";
+            if (i >= kLayerNorm && i < kEntries && !PyMapping_HasKeyString(v[0], name)) {
+                found[i] = functions[i];  // stays as it is
+                continue;
+            }
+            PyObject* p = PyMapping_GetItemString(v[0], name);
             if (!p) throw PythonError();
             found[i] = PyLong_AsVoidPtr(p);
             Py_DECREF(p);

@@ -538,9 +538,9 @@ def heddle_get_search(ctx) -> int:
 
 _ops = None
 _OP_NAMES = ("heddle_linear", "heddle_linear_backward", "heddle_gated_ffn", "heddle_gated_ffn_backward",
-             "heddle_qk_norm_rope", "heddle_qk_norm_rope_backward", "heddle_attention", "heddle_attention_backward",
-             "heddle_layer_norm", "heddle_layer_norm_backward", "heddle_dropout", "heddle_dropout_backward",
-             "heddle_embedding", "heddle_embedding_backward", "heddle_router", "heddle_router_backward")
+             "heddle_qk_norm_rope", "heddle_qk_norm_rope_backward", "heddle_attention", "heddle_attention_backward")
+_HIDDEN_NAMES = ("heddle_layer_norm", "heddle_layer_norm_backward", "heddle_dropout", "heddle_dropout_backward",
+                 "heddle_embedding", "heddle_embedding_backward", "heddle_router", "heddle_router_backward")
 
 
 def _op_setup():
@@ -554,8 +554,8 @@ def _op_setup():
     L = load_library()
     stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or \
         (lambda device: torch.cuda.current_stream(device).cuda_stream)
-    _heddle_ops.bind({n: C.cast(getattr(L, n), C.c_void_p).value for n in _OP_NAMES + ("heddle_device",)},
-                     HeddleError, stream)
+    names = _OP_NAMES + _HIDDEN_NAMES + ("heddle_device",)
+    _heddle_ops.bind({n: C.cast(getattr(L, n), C.c_void_p).value for n in names}, HeddleError, stream)
     _ops = _heddle_ops
     return _ops
 

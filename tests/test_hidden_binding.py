@@ -62,11 +62,11 @@ def test_refused_calls_keep_no_reference(ops):
     _, h = ops
     x = torch.zeros(4, 8, dtype=torch.bfloat16)
     for f, args in _calls(h, x):
-        before = [sys.getrefcount(a) for a in args]
+        before = sys.getrefcount(x)  # numbers are shared with whatever else holds them
         for _ in range(50):
             with pytest.raises(h.HeddleError):
                 f(*args)
-        assert [sys.getrefcount(a) for a in args][1:] == before[1:]
+        assert sys.getrefcount(x) == before
 
 
 def test_struct_layouts_match_header(heddle_lib, tmp_path):
