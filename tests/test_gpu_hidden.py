@@ -103,7 +103,7 @@ def test_layer_norm_backward(lib, m, n, dt):
 
 @pytest.mark.parametrize("dt", ["bf16", "fp32"])
 @pytest.mark.parametrize("m,n", [(20000, 520), (9000, 1031), (20000, 1032), (2000, 5121), (3000, 8192), (1200, 8190),
-                                 (700, 9000), (500, 16380)])
+                                 (700, 9000), (500, 16380), (60000, 64), (90000, 9), (20000, 257), (30000, 500)])
 def test_layer_norm_of_many_rows_a_block(lib, m, n, dt):
     """More rows than a block holds ahead: places of the ring are taken again
     and again."""
@@ -390,6 +390,24 @@ def test_embedding_tables_past_32_bits(lib):
     assert not table.any()
 
 
+@pytest.mark.parametrize("n,dt", [(4, "fp32"), (3, "bf16")])
+@pytest.mark.parametrize("t", [50, 70000])
+def test_embedding_gradient_of_many_rows(lib, t, n, dt):
+    # more rows a block than it marks at a time; with many tokens half of one row
+    h, ctx = lib
+    g, rows, dt = gen(t + n), 20_000_003, TYPES[dt]
+    tokens = torch.randint(0, rows, (t,), generator=g, device="cuda")
+    if t > 100:
+        tokens[torch.rand(t, generator=g, device="cuda") < 0.5] = 8200
+    dy, d = rand(g, t, n, dt=dt), torch.full((rows, n), 3.0, dtype=dt, device="cuda")
+    h.heddle_embedding_backward(ctx, tokens, dy, d)
+    own, at = torch.unique(tokens, return_inverse=True)
+    want, bound = H.embedding_grad(at, dy, len(own), 1.0, 0, None)
+    close(d[own], want, bound, "dtable")
+    d[own] = 0
+    assert not d.any()
+
+
 # -------------------------------------------------------------------- router
 
 def routed(h, ctx, logits, k, valid, normalize, loss=True):
@@ -665,6 +683,49 @@ def test_calls_on_two_streams_take_turns_at_the_scratch(lib):
 
 
 # ------------------------------------------------------------------- refusals
+
+def test_tensors_of_another_device_are_refused(lib):
+    """A stand-in reports the context's device: no operator's function may be
+    entered where it is not the tensors'; names left out stay bound."""
+    import ctypes
+    h, ctx = lib
+    native, entered = h._op_setup(), []
+
+    @ctypes.CFUNCTYPE(ctypes.c_int32, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p)
+    def operator(c, a, s):
+        entered.append(c)
+        return 0
+
+    @ctypes.CFUNCTYPE(ctypes.c_int32, ctypes.c_void_p)
+    def device(c):
+        return where
+
+    address = lambda f: ctypes.cast(f, ctypes.c_void_p).value
+    x, v, w = torch.zeros(4, 8, device="cuda"), torch.zeros(4, device="cuda"), torch.zeros(4, 2, device="cuda")
+    t, e, c = (torch.zeros(*n, dtype=torch.int32, device="cuda") for n in ((4,), (4, 2), (9,)))
+    calls = [(h.heddle_layer_norm, (x, None, None, x)), (h.heddle_layer_norm_backward, (x, x, None, v, v, x)),
+             (h.heddle_dropout, (x, x, 0.5, 1)), (h.heddle_dropout_backward, (x, x, 0.5, 1)),
+             (h.heddle_embedding, (t, x, x)), (h.heddle_embedding_backward, (t, x, x)),
+             (h.heddle_router, (x, e, w, c)), (h.heddle_router_backward, (x, e, w, c, x))]
+    assert len(calls) == len(h._HIDDEN_NAMES)
+    old = dict.fromkeys(h._OP_NAMES, address(operator))
+    old["heddle_device"] = address(device)
+    try:
+        for names in ({**old, **dict.fromkeys(h._HIDDEN_NAMES, address(operator))}, old):
+            native.bind(names, h.HeddleError, lambda index: 0)
+            for where in (torch.cuda.current_device(), torch.cuda.current_device() + 1):
+                for f, args in calls:
+                    entered.clear()
+                    if where == torch.cuda.current_device():
+                        f(ctx, *args)
+                        assert len(entered) == 1
+                    else:
+                        with pytest.raises(h.HeddleError, match="the context is of") as err:
+                            f(ctx, *args)
+                        assert err.value.status == h.E_ARG and not entered
+    finally:
+        h._op_setup()
+
 
 def test_refusals(lib):
     h, ctx = lib
