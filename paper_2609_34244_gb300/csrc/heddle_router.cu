@@ -9,8 +9,8 @@
 // over all tokens of its warp, then over the block's warps, then over blocks by
 // a second kernel, always in order.  The backward pass computes the
 // probabilities again.  16384 tokens of 64 bfloat16 logits, two chosen: 9.5 us
-// forward, 6.3 backward; 32771 of 250 floats, eight chosen: 33 and 21 us (its
-// 69 MB take 10), the integer units busy 78 % of the time.
+// forward, 6.3 backward; 32771 of 250 floats, eight chosen: 29 and 21 us (their
+// 69 MB take 10).
 
 #include <string.h>
 
@@ -91,6 +91,86 @@ struct Softmax {
     }
 };
 
+// A token's keys, the largest one after the other, and the first of equal ones.
+// Up to four a lane stay in registers and are all compared for each choice; more
+// lie in shared memory as lists.  (32771 tokens of 250 floats, eight chosen: 29
+// us, from registers 34; 16384 of 64: 14.6 and 12.2.)
+template <class T, int N, bool LISTS = (N > 4)>
+struct Search;
+template <class T, int N>
+struct Search<T, N, false> {
+    static constexpr int kPlaces = 32 * N;
+    uint32_t (&key)[N];
+    int lane;
+    __device__ __forceinline__ Search(uint32_t (&k)[N], uint32_t*, int l) : key(k), lane(l) {}
+    __device__ __forceinline__ uint32_t next(int& at) {
+        uint32_t best = key[0];
+#pragma unroll
+        for (int i = 1; i < N; ++i) best = key[i] > best ? key[i] : best;
+        best = __reduce_max_sync(~0u, best);
+        if constexpr (sizeof(T) == 2) {
+            at = 0xffff - (int)(best & 0xffffu);
+#pragma unroll
+            for (int i = 0; i < N; ++i) key[i] = key[i] == best ? 0 : key[i];
+        } else {
+            at = INT32_MAX;
+#pragma unroll
+            for (int i = N - 1; i >= 0; --i) at = key[i] == best ? lane + i * 32 : at;
+            at = __reduce_min_sync(~0u, at);
+#pragma unroll
+            for (int i = 0; i < N; ++i) key[i] = at == lane + i * 32 ? 0 : key[i];
+        }
+        return best;
+    }
+};
+// Every lane knows its largest, and the list of the lane that has the largest of
+// all is gone through by the warp, a lane a key.
+template <class T, int N>
+struct Search<T, N, true> {
+    static constexpr int kEach = N + 1, kPlaces = 32 * kEach;  // an odd distance between lists
+    uint32_t* list;
+    int lane;
+    uint32_t most = 0;
+    __device__ __forceinline__ Search(const uint32_t (&key)[N], uint32_t* at, int l) : list(at), lane(l) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            list[lane * kEach + i] = key[i];
+            most = key[i] > most ? key[i] : most;
+        }
+        __syncwarp();
+    }
+    __device__ __forceinline__ uint32_t next(int& at) {
+        const uint32_t best = __reduce_max_sync(~0u, most);
+        int slot, owner;
+        uint32_t v;
+        if constexpr (sizeof(T) == 2) {
+            at = 0xffff - (int)(best & 0xffffu);
+            slot = at / 32, owner = at % 32;
+            v = lane < N ? list[owner * kEach + lane] : 0;
+        } else {
+            const uint32_t who = __ballot_sync(~0u, most == best);
+            if (who & (who - 1)) {  // equal ones in several lanes
+                at = INT32_MAX;
+#pragma unroll
+                for (int i = N - 1; i >= 0; --i) at = list[lane * kEach + i] == best ? lane + i * 32 : at;
+                at = __reduce_min_sync(~0u, at);
+                slot = at / 32, owner = at % 32;
+                v = lane < N ? list[owner * kEach + lane] : 0;
+            } else {
+                owner = __ffs(who) - 1;
+                v = lane < N ? list[owner * kEach + lane] : 0;
+                slot = __ffs(__ballot_sync(~0u, v == best)) - 1;
+                at = owner + slot * 32;
+            }
+        }
+        if (lane == slot) v = list[owner * kEach + slot] = 0;
+        v = __reduce_max_sync(~0u, v);
+        if (lane == owner) most = v;
+        __syncwarp();
+        return best;
+    }
+};
+
 // Threads a block, one an SM: those that the registers allow.
 template <int N>
 constexpr int kThreads = N == 32 ? 256 : N == 16 ? 512 : N == 8 ? 768 : 1024;
@@ -109,7 +189,9 @@ __global__ void __launch_bounds__(kThreads<N>, 1)
     allow_dependents();
     await_previous();
     constexpr int kBlock = kThreads<N>, kWarps = kBlock / 32;
-    __shared__ float psum[kWarps][32 * N];
+    using Lists = Search<T, N>;
+    // a warp's list, then its sums
+    __shared__ uint32_t own_of[kWarps][Lists::kPlaces];
     __shared__ int32_t csum[32 * N + 1];
     const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
     float psums[N] = {}, v[N], next[N];
@@ -138,27 +220,13 @@ __global__ void __launch_bounds__(kThreads<N>, 1)
             if (!s.sound) key[j] = 0;
         }
         // the chosen ones: lane j keeps the j-th
+        Lists search(key, own_of[warp], lane);
         uint32_t own = 0;
         int mine = -1;
         for (int j = 0; j < a.top_k; ++j) {
-            uint32_t best = key[0];
-#pragma unroll
-            for (int i = 1; i < N; ++i) best = key[i] > best ? key[i] : best;
-            best = __reduce_max_sync(~0u, best);
-            if (best <= kLowest<T>) break;  // none is left
             int at;
-            if constexpr (kPacked) {
-                at = 0xffff - (int)(best & 0xffffu);
-#pragma unroll
-                for (int i = 0; i < N; ++i) key[i] = key[i] == best ? 0 : key[i];
-            } else {
-                at = INT32_MAX;
-#pragma unroll
-                for (int i = N - 1; i >= 0; --i) at = key[i] == best ? lane + i * 32 : at;
-                at = __reduce_min_sync(~0u, at);
-#pragma unroll
-                for (int i = 0; i < N; ++i) key[i] = at == lane + i * 32 ? 0 : key[i];
-            }
+            const uint32_t best = search.next(at);
+            if (best <= kLowest<T>) break;  // none is left
             if (j == lane) mine = at, own = best;
         }
         float value;
@@ -176,7 +244,7 @@ __global__ void __launch_bounds__(kThreads<N>, 1)
         }
     }
 #pragma unroll
-    for (int j = 0; j < N; ++j) psum[warp][lane + j * 32] = psums[j];
+    for (int j = 0; j < N; ++j) own_of[warp][lane + j * 32] = __float_as_uint(psums[j]);
     if (lane == 0 && tokens) atomicAdd(&csum[32 * N], tokens);
     __syncthreads();
     float loss = 0.0f;
@@ -184,7 +252,7 @@ __global__ void __launch_bounds__(kThreads<N>, 1)
         float p = 0.0f;
         if (i < a.experts) {
 #pragma unroll 16
-            for (int k = 0; k < kWarps; ++k) p += psum[k][i];
+            for (int k = 0; k < kWarps; ++k) p += __uint_as_float(own_of[k][i]);
         }
         const int32_t c = csum[i < a.experts ? i : 32 * N];
         if (ONE) {

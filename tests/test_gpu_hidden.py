@@ -482,6 +482,18 @@ def test_router_equal_logits_go_by_index(lib):
             assert counts[n] == 3 and counts[:n].sum() == 3 * k
 
 
+@pytest.mark.parametrize("n,k", [(60, 5), (100, 8), (250, 16), (500, 7), (1000, 32)])
+def test_router_few_values(lib, n, k):
+    h, ctx = lib
+    for dt in TYPES.values():
+        logits = torch.randint(-2, 3, (999, n), generator=gen(n), device="cuda").to(dt)
+        logits[::5, 3:] = float("-inf")  # three are left
+        experts, _, _, _ = routed(h, ctx, logits, k, None, True)
+        want = torch.sort(logits.float(), dim=1, descending=True, stable=True).indices[:, :k]
+        want[::5, 3:] = -1
+        assert torch.equal(experts.long(), want)
+
+
 def test_router_values_that_are_not_finite(lib):
     h, ctx = lib
     for n, k in ((8, 2), (64, 3), (200, 8)):
