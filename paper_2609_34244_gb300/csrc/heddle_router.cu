@@ -171,7 +171,8 @@ struct Search<T, N, true> {
     }
 };
 
-// Threads a block, one an SM: those that the registers allow.
+// Threads a block, one an SM: those that the registers allow.  (Two blocks of 1024
+// for 64 experts: 16384 tokens 10.4 us, one 9.6.)
 template <int N>
 constexpr int kThreads = N == 32 ? 256 : N == 16 ? 512 : N == 8 ? 768 : 1024;
 
