@@ -587,13 +587,17 @@ int64_t slabs_of(const heddle_embedding_args& a) {
 // table's share of the tokens, so that few rows go over several runs.  (16384
 // tokens of 4096 bfloat16 values, half of them of one row, into 32000 rows of
 // 32 bits: 142 us, 2048 blocks 159, 512 137; 262144 tokens of 1024 values, any
-// row: 217, 227 and 237.)  More beyond 8192 runs, which bounds the parts that a
-// row of up to four million tokens is joined from.
+// row: 217, 227 and 237.)  At least 8, and more from 6400 tokens on, whose
+// joining grows with the runs (with the lookup, 12867 tokens of 256 float16
+// values, 687 rows: 29 us by 16, 34 by 8; 4096 of 1023, 6251 rows: 52 and 50).
+// More beyond 8192 runs, which bounds the parts that a row of up to four million
+// tokens is joined from.
 int64_t chunk_of(const heddle_embedding_args& a) {
     const int64_t slabs = slabs_of(a);
     const int64_t own = (int64_t)((double)a.tokens * ((double)a.table_rows / (double)a.vocab));
-    int64_t c = kMostRun;
-    while (c > kLeastRun && ceil_div(own, c) * slabs < 1024) c /= 2;
+    int64_t c = kMostRun, least = kLeastRun;
+    while (least < kMostRun && 100 * least * least <= own) least *= 2;
+    while (c > least && ceil_div(own, c) * slabs < 1024) c /= 2;
     while (c < kMostRun && ceil_div(a.tokens, c) > 8192) c *= 2;
     return c;
 }
