@@ -1,7 +1,7 @@
 // heddle_embedding.cu -- the embedding and the gradient of its table.
 //
 // Bound by memory: rows are copied, and the gradient's rows are written once
-// each.  The gradient sorts (row, token) pairs, by one cluster of CTAs, so that
+// each.  The gradient sorts (row, token) pairs, by one CTA or a cluster, so that
 // a row's terms lie together in the order of their tokens; then blocks add up
 // runs of the sorted list, others write zeros to the rows that have no token,
 // and the sums of rows that go over several runs are joined in order.
@@ -99,7 +99,6 @@ __global__ void __launch_bounds__(kThreads)
 
 // -------------------------------------------------------------------- sorting
 
-constexpr int kCluster = 8;
 constexpr int kSortThreads = 1024, kSortWarps = kSortThreads / 32;
 constexpr int kDigits = 512;
 
@@ -121,18 +120,27 @@ __device__ __forceinline__ uint32_t load_of_rank(const uint32_t* p, uint32_t ran
     return v;
 }
 
+template <int CTAS>
+__device__ __forceinline__ void meet() {
+    if constexpr (CTAS > 1)
+        tc::cluster_sync();
+    else
+        __syncthreads();
+}
+
 // A stable sort by the row, `bits` bits a pass from the lowest.  Each warp of
 // the cluster has a run of the list: it counts its digits, its places in the
 // result follow from the counts of all warps before it, and it walks over its
 // run again in order.
+template <int CTAS>
 __device__ __forceinline__ void sort_pass(const Sort& s, int pass, int64_t n, uint32_t (*counts)[kDigits],
                                           uint32_t* total, uint32_t* base, uint32_t* scan) {
     const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
-    const uint32_t rank = tc::cluster_rank();
+    const uint32_t rank = CTAS > 1 ? tc::cluster_rank() : 0;
     const Entry* from = s.list[pass & 1];
     Entry* to = s.list[(pass & 1) ^ 1];
     const int shift = pass * s.bits, digits = 1 << s.bits;
-    const int64_t run = ceil_div(n, kCluster * kSortWarps), first = (rank * kSortWarps + warp) * run;
+    const int64_t run = ceil_div(n, CTAS * kSortWarps), first = (rank * kSortWarps + warp) * run;
     const int64_t end = first + run < n ? first + run : n;
     // entry i; false where it is none of the table's
     auto entry = [&](int64_t i, Entry& e, bool flag) {
@@ -174,16 +182,20 @@ __device__ __forceinline__ void sort_pass(const Sort& s, int pass, int64_t n, ui
         }
         total[d] = sum;
     }
-    tc::cluster_sync();
+    meet<CTAS>();
     // before this CTA: all of the smaller digits, and this digit's of the CTAs before
     uint32_t all = 0, before = 0;
     const int d = threadIdx.x;
     if (d < digits) {
+        if constexpr (CTAS > 1) {
 #pragma unroll
-        for (uint32_t r = 0; r < kCluster; ++r) {
-            const uint32_t c = load_of_rank(total + d, r);
-            before += r < rank ? c : 0;
-            all += c;
+            for (int r = 0; r < CTAS; ++r) {
+                const uint32_t c = load_of_rank(total + d, r);
+                before += r < (int)rank ? c : 0;
+                all += c;
+            }
+        } else {
+            all = total[d];
         }
     }
     uint32_t up = all;  // inclusive, over the warp, then over warps
@@ -229,10 +241,11 @@ __device__ __forceinline__ void sort_pass(const Sort& s, int pass, int64_t n, ui
         const bool is = entry(i0 + lane, e, false);
         place(e, is);
     }
-    tc::cluster_sync();  // the next pass reads what all wrote, and its counts take these ones' place
+    meet<CTAS>();  // the next pass reads what all wrote, and its counts take these ones' place
 }
 
-__global__ void __launch_bounds__(kSortThreads) __cluster_dims__(kCluster, 1, 1)
+template <int CTAS>
+__global__ void __launch_bounds__(kSortThreads) __cluster_dims__(CTAS, 1, 1)
     embedding_sort_kernel(const __grid_constant__ Sort s) {
     allow_dependents();
     await_previous();
@@ -241,7 +254,7 @@ __global__ void __launch_bounds__(kSortThreads) __cluster_dims__(kCluster, 1, 1)
     uint32_t *total = shared + kSortWarps * kDigits, *base = total + kDigits, *scan = base + kDigits;
     int64_t n = s.a.tokens;
     for (int pass = 0; pass < s.passes; ++pass) {
-        sort_pass(s, pass, n, counts, total, base, scan);
+        sort_pass<CTAS>(s, pass, n, counts, total, base, scan);
         if (pass == 0) n = *s.count;
     }
 }
@@ -629,6 +642,18 @@ cudaError_t sums(const OpContext& x, const Sums& s, cudaStream_t st) {
     return e;
 }
 
+// Up to so many are sorted by one CTA, others by a cluster of eight (the gradient
+// of 256 bfloat16 values, 1000 rows: 128 tokens 9.6 us, by a cluster 12.3; 512:
+// 12.9 and 14.3; 2048: 17.4 and 16.9).
+constexpr int64_t kFewTokens = 512;
+template <int CTAS>
+cudaError_t sort(const OpContext& x, const Sort& s, cudaStream_t st) {
+    static std::atomic<uint64_t> asked{0};
+    const cudaError_t e = allow_shared(embedding_sort_kernel<CTAS>, kSortShared, x.device, asked);
+    if (e != cudaSuccess) return e;
+    return launch(x, embedding_sort_kernel<CTAS>, dim3(CTAS), kSortThreads, kSortShared, st, s);
+}
+
 template <class T, class TO>
 cudaError_t backward(const OpContext& x, const heddle_embedding_grad_args& g, unsigned char* ws, cudaStream_t st) {
     const heddle_embedding_args& a = g.fwd;
@@ -643,10 +668,7 @@ cudaError_t backward(const OpContext& x, const heddle_embedding_grad_args& g, un
     s.list[1] = reinterpret_cast<Entry*>(ws + at.list + align256(sizeof(Entry) * (size_t)a.tokens));
     s.count = reinterpret_cast<int64_t*>(ws);
     s.err = x.err;
-    static std::atomic<uint64_t> asked{0};
-    cudaError_t e = allow_shared(embedding_sort_kernel, kSortShared, x.device, asked);
-    if (e != cudaSuccess) return e;
-    e = launch(x, embedding_sort_kernel, dim3(kCluster), kSortThreads, kSortShared, st, s);
+    cudaError_t e = a.tokens <= kFewTokens ? sort<1>(x, s, st) : sort<8>(x, s, st);
     if (e != cudaSuccess) return e;
     Sums m{};
     m.a = a;

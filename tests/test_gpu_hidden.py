@@ -283,6 +283,7 @@ LOOKUPS = [  # tokens, vocabulary, shards, columns
     (1, 1, 1, 1), (1, 100, 1, 64), (16, 32000, 1, 4096), (5, 40, 4, 7), (300, 1000, 1, 136), (1000, 600, 3, 513),
     (2100, 70, 1, 1023), (4097, 5000, 2, 200), (40000, 300000, 1, 24), (33000, 4096, 1, 40), (3000, 1 << 20, 1, 8),
     (70001, 33, 1, 130), (600, 1200, 1, 5000), (600000, 50, 1, 8), (9000, 900, 1, 1040),
+    (512, 30000, 1, 40), (513, 30000, 1, 40), (500, 1 << 20, 1, 4),
 ]
 
 
