@@ -8,7 +8,7 @@
 // copies fill ahead; the weights' sums over rows stay in registers, one set a
 // block, and a second kernel adds the sets in order.  Arithmetic runs on two
 // values at a time, and 16-bit values are used as they lie in their words:
-// 16384 x 8192 bfloat16 takes 86 us forward (6.2 TB/s) and 169 backward (6.4,
+// 16384 x 8192 bfloat16 takes 86 us forward (6.2 TB/s) and 167 backward (6.4,
 // with the join); taken out one by one they were bound by instructions, 149
 // and 350.
 
