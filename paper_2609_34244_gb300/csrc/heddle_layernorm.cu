@@ -195,12 +195,48 @@ struct Shared {
         }
     }
 };
+// 16-bit ones as they lie in their words, beside a ring: taking them out costs
+// less than the second block an SM that the floats leave no room for (16384 x
+// 8192 bfloat16 one element off 16 bytes: 143 us, floats 209; the same bits).
+template <class T, class R>
+struct Packed {
+    const uint4 *w, *b;
+    int threads;
+    __device__ __forceinline__ Packed(const R& part, const heddle_layer_norm_args& a, float4* place)
+        : threads(blockDim.x) {
+        uint4* at = reinterpret_cast<uint4*>(place);
+        w = at, b = at + threads * (R::N / R::V);
+        uint32_t r[R::kWords];
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            load_vector<T>(part, r, k ? a.bias : a.weight, k ? 0.0f : 1.0f);
+#pragma unroll
+            for (int u = 0; u < R::N / R::V; ++u)
+                at[(k * (R::N / R::V) + u) * threads + threadIdx.x] =
+                    make_uint4(r[4 * u], r[4 * u + 1], r[4 * u + 2], r[4 * u + 3]);
+        }
+    }
+    __device__ __forceinline__ void scale(const R&, uint32_t (&out)[R::kWords], const float2 (&v)[R::N / 2],
+                                          float rstd) const {
+        const float2 s = both(rstd);
+#pragma unroll
+        for (int u = 0; u < R::N / R::V; ++u) {
+            const uint4 wv = w[u * threads + threadIdx.x], bv = b[u * threads + threadIdx.x];
+            const uint32_t wr[4] = {wv.x, wv.y, wv.z, wv.w}, br[4] = {bv.x, bv.y, bv.z, bv.w};
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int p = 4 * u + i;
+                set_pair<T>(out, p, fma2(mul2(v[p], s), pair_of<T>(wr, i), pair_of<T>(br, i)));
+            }
+        }
+    }
+};
 // 32-bit ones need no taking out and stay in registers.
 template <class T, class R, int GL>
 using Affine = typename std::conditional<GL != 0 || sizeof(T) == 4, Held<T, R>, Shared<T, R>>::type;
 template <class T>
-int affine_bytes(int threads, int units) {
-    return sizeof(T) == 4 ? 0 : 2 * threads * units * 16 * 2;
+int affine_bytes(int threads, int units, bool packed) {
+    return sizeof(T) == 4 ? 0 : 2 * threads * units * 16 * (packed ? 1 : 2);
 }
 
 template <int GL>
@@ -264,7 +300,7 @@ __global__ void __launch_bounds__(MOST, GL ? kShortResident<T, U> : MOST == 256 
 // The same by a block for rows that do not lie at 16 bytes: through the ring,
 // read from and written to memory in units all the same.
 template <class T, int U, bool STRIDED, int MOST>
-__global__ void __launch_bounds__(MOST, 1024 / MOST)
+__global__ void __launch_bounds__(MOST, MOST == 256 ? 2 : 1024 / MOST)
     layer_norm_ring_kernel(const __grid_constant__ heddle_layer_norm_args a, int stages, bool staged, uint32_t* err) {
     extern __shared__ __align__(128) unsigned char shared[];
     allow_dependents();
@@ -285,7 +321,8 @@ __global__ void __launch_bounds__(MOST, 1024 / MOST)
         ahead += step;
     };
     for (int k = 0; k < stages - 1; ++k) fetch(k);
-    const Affine<T, R, 0> affine(part, a, reinterpret_cast<float4*>(out + (staged ? ring.place : 0)));
+    using Vectors = typename std::conditional<U == 4, Packed<T, R>, Affine<T, R, 0>>::type;
+    const Vectors affine(part, a, reinterpret_cast<float4*>(out + (staged ? ring.place : 0)));
     T* y = static_cast<T*>(a.y) + blockIdx.x * a.ldy;
     BlockSum total;
     for (int k = 0; k < rows; ++k, x += step, y += gridDim.x * a.ldy) {
@@ -691,12 +728,12 @@ Plan plan_forward(const OpContext& x, const heddle_layer_norm_args& a) {
     // rows of 512 to 1024 units of 16-bit values by smaller blocks, three an SM:
     // 16384 x 8192 bfloat16 takes 86 us, two units a thread 98 (26214 x 5120: 86
     // and 96; 32768 x 4096 the other way round, 91 and 100)
-    if (whole && size == 2 && units > 512 && units <= 1024) {
+    if (!p.strided && size == 2 && units > 512 && units <= 1024) {
         p.units = 4;
         p.threads = (int)ceil_div(ceil_div(units, 4), 32) * 32;
         an_sm = blocks_an_sm(768, p.threads);
     }
-    p.shared = affine_bytes<T>(p.threads, p.units);
+    p.shared = affine_bytes<T>(p.threads, p.units, !whole && p.units == 4);
     if (p.way == kBlocks && !whole)
         plan_ring(p, a.cols * size, 1, 1, false, size == 4 && p.strided, (int)p.shared, an_sm);
     if (p.way == kLongRows) p.threads = kLong, an_sm = 2;
@@ -752,11 +789,15 @@ cudaError_t forward_short(const OpContext& x, const heddle_layer_norm_args& a, c
 
 template <class T, int MOST>
 cudaError_t forward_blocks(const OpContext& x, const heddle_layer_norm_args& a, const Plan& p, cudaStream_t st) {
-    static std::atomic<uint64_t> asked[4];
+    static std::atomic<uint64_t> asked[5];
     if (p.way == kRing) {
         auto* kernel = layer_norm_ring_kernel<T, kEach, false, MOST>;
         if constexpr (sizeof(T) == 4)
             if (p.strided) kernel = layer_norm_ring_kernel<T, kEach, true, MOST>;
+        if constexpr (sizeof(T) == 2)
+            if (p.units == 4)
+                return launch_planned(x, layer_norm_ring_kernel<T, 4, false, 256>, asked[4], p, st, a, p.stages,
+                                      p.staged, x.err);
         return launch_planned(x, kernel, asked[p.strided], p, st, a, p.stages, p.staged, x.err);
     }
     if constexpr (sizeof(T) == 2)
