@@ -777,9 +777,12 @@ heddle_status heddle_attention_backward(heddle_ctx* ctx, const heddle_attention_
  *   y = (x - mean) rstd weight + bias
  * weight, bias: [cols], of the same type, each nullable (1 and 0).  mean, rstd
  * (float [rows], nullable together): receive the statistics for the backward
- * pass.  Deviations from the mean are squared, not values: a large mean costs
- * no digits.  y may be x itself (same stride).  A row with a value that is not
- * finite gets NaN. */
+ * pass.  Deviations from the mean are squared, not values, and what the mean is
+ * rounded by is taken out of them: a large mean costs y and rstd no digits (mean
+ * as it is saved is a float; n in the gradients is off by its rounding times
+ * rstd).  Sums are floats: where that of the squares is beyond them, y is bias,
+ * and where it is below, eps is all that is left.  y may be x itself (same
+ * stride).  A row with a value that is not finite gets NaN. */
 typedef struct {
     int64_t rows, cols;
     int32_t dtype;

@@ -1,16 +1,16 @@
 // heddle_layernorm.cu -- layer norm and its gradients.
 //
 // Bound by memory.  A row is held by a group of threads, a few 16-byte units
-// each: its mean first, then the squares of its deviations from it, so that a
-// large mean costs no digits and nothing is read from memory twice.  Short rows
-// take 4 to 32 lanes of a warp, others a block, which walks over rows.
-// Gradients of such rows are read through a ring in shared memory that bulk
-// copies fill ahead; the weights' sums over rows stay in registers, one set a
-// block, and a second kernel adds the sets in order.  Arithmetic runs on two
-// values at a time, and 16-bit values are used as they lie in their words:
-// 16384 x 8192 bfloat16 takes 86 us forward (6.2 TB/s) and 167 backward (6.4,
-// with the join); taken out one by one they were bound by instructions, 149
-// and 350.
+// each: its mean first, in two floats, then the squares of its deviations from
+// it, so that a large mean costs no digits and nothing is read from memory
+// twice.  Short rows take 4 to 32 lanes of a warp, others a block, which walks
+// over rows.  Gradients of such rows are read through a ring in shared memory
+// that bulk copies fill ahead; the weights' sums over rows stay in registers,
+// one set a block, and a second kernel adds the sets in order.  Arithmetic runs
+// on two values at a time, and 16-bit values are used as they lie in their
+// words: 16384 x 8192 bfloat16 takes 87 us forward (6.2 TB/s) and 168 backward
+// (6.4, with the join); taken out one by one they were bound by instructions,
+// 149 and 350.
 
 #include <atomic>
 
@@ -87,13 +87,18 @@ __device__ __forceinline__ void block_sums(float (&v)[4], int& turn) {
     turn ^= 1;
 }
 
-// sum / cols, inv = 1 / cols: the product and one correction by its remainder
-// (exact where the quotient is a float: a row of one value has no variance).
-// A division would take a dozen instructions of every thread.
-__device__ __forceinline__ float over(float sum, float cols, float inv) {
-    const float q = sum * inv;
-    return fmaf(fmaf(-q, cols, sum), inv, q);
-}
+// sum / cols in two floats, inv = 1 / cols: the product, corrected by its
+// remainder (exact where the quotient is a float: a row of one value has no
+// variance), and what then remains.  A division would take a dozen
+// instructions of every thread.
+struct Mean {
+    float value, left;
+    __device__ __forceinline__ Mean(float sum, float cols, float inv) {
+        const float q = sum * inv;
+        value = fmaf(fmaf(-q, cols, sum), inv, q);
+        left = fmaf(-value, cols, sum) * inv;
+    }
+};
 
 // Of GL lanes of a warp, all of which take part.
 template <int GL, int N>
@@ -125,24 +130,56 @@ __device__ __forceinline__ float sum_of(const R&, const uint32_t (&r)[R::kWords]
     s[0] = add2(s[0], s[1]);
     return s[0].x + s[0].y;
 }
-// Their deviations from the mean, and the sum of these' squares.  ENDS: the
-// row's end may lie in a unit.
+// Their deviations from the mean's first part, and the sum of these' squares.
+// ENDS: the row's end may lie in a unit.
+//
+// What a mean is off by reaches every y times rstd, and beside large means it is
+// not small: its rounding is taken out as its second part, `left`.  Sums of
+// 16-bit values around a large mean are exact for thousands of them; those of
+// 32 bits are not, so the deviations are added up as well and tell what is left
+// (32768 x 2048 floats: 87.3 us, 86.5 without; 8192 x 8192: 98.2 and 94.6; 16384
+// x 8192 bfloat16 would take 106 for 87).
+template <class T>
+constexpr bool kLeft = sizeof(T) == 4;
 template <class T, bool ENDS, class R>
-__device__ __forceinline__ float squares_of(const R& part, const uint32_t (&r)[R::kWords], float2 (&v)[R::N / 2],
-                                            float mean) {
-    float2 s = both(0.0f);
+__device__ __forceinline__ float2 deviations_of(const R& part, const uint32_t (&r)[R::kWords], float2 (&v)[R::N / 2],
+                                                float mean) {
+    float2 d = both(0.0f), s = both(0.0f);
     const float2 m = both(-mean);
 #pragma unroll
     for (int p = 0; p < R::N / 2; ++p) {
         v[p] = plus<T>(r, p, m);
         if (ENDS) {
-            const float2 d = make_float2(part.in(2 * p) ? v[p].x : 0.0f, part.in(2 * p + 1) ? v[p].y : 0.0f);
-            s = fma2(d, d, s);
+            const float2 f = make_float2(part.in(2 * p) ? v[p].x : 0.0f, part.in(2 * p + 1) ? v[p].y : 0.0f);
+            if (kLeft<T>) d = add2(d, f);
+            s = fma2(f, f, s);
         } else if (part.in(2 * p / R::V * R::V)) {  // a unit is in or out as a whole
+            if (kLeft<T>) d = add2(d, v[p]);
             s = fma2(v[p], v[p], s);
         }
     }
-    return s.x + s.y;
+    return make_float2(d.x + d.y, s.x + s.y);
+}
+// What is left of the mean, and 1 / sqrt(variance + eps).
+struct Spread {
+    float left, rstd;
+    // Of the two sums: the variance is the squares' mean less the square of what
+    // is left.
+    __device__ __forceinline__ Spread(float2 sums, float inv, float eps) : left(sums.x * inv) {
+        const float var = fmaf(-left, left, sums.y * inv);
+        rstd = inv_sqrt((var < 0.0f ? 0.0f : var) + eps);
+    }
+    // Of the mean and the squares: half a unit of the mean's last place, whose
+    // square is nothing beside a variance of 16-bit values.
+    __device__ __forceinline__ Spread(const Mean& mean, float squares, float inv, float eps)
+        : left(mean.left), rstd(inv_sqrt(fmaf(squares, inv, eps))) {}
+};
+template <class T, class S>
+__device__ __forceinline__ Spread spread_of(S& total, const Mean& mean, float2 sums, float inv, float eps) {
+    if constexpr (kLeft<T>)
+        return Spread(total(sums), inv, eps);
+    else
+        return Spread(mean, total(sums.y), inv, eps);
 }
 
 // Weight and bias of a lane as floats in its registers.
@@ -159,10 +196,10 @@ struct Held {
         for (int p = 0; p < R::N / 2; ++p) b[p] = pair_of<T>(r, p);
     }
     __device__ __forceinline__ void scale(const R&, uint32_t (&out)[R::kWords], const float2 (&v)[R::N / 2],
-                                          float rstd) const {
-        const float2 s = both(rstd);
+                                          const Spread& spread) const {
+        const float2 s = both(spread.rstd), o = both(-spread.left * spread.rstd);
 #pragma unroll
-        for (int p = 0; p < R::N / 2; ++p) set_pair<T>(out, p, fma2(mul2(v[p], s), w[p], b[p]));
+        for (int p = 0; p < R::N / 2; ++p) set_pair<T>(out, p, fma2(fma2(v[p], s, o), w[p], b[p]));
     }
 };
 // Those of a block as floats in shared memory, each thread its own, four values
@@ -185,13 +222,13 @@ struct Shared {
         }
     }
     __device__ __forceinline__ void scale(const R&, uint32_t (&out)[R::kWords], const float2 (&v)[R::N / 2],
-                                          float rstd) const {
-        const float2 s = both(rstd);
+                                          const Spread& spread) const {
+        const float2 s = both(spread.rstd), o = both(-spread.left * spread.rstd);
 #pragma unroll
         for (int q = 0; q < R::N / 4; ++q) {
             const float4 wv = w[q * threads + threadIdx.x], bv = b[q * threads + threadIdx.x];
-            set_pair<T>(out, 2 * q, fma2(mul2(v[2 * q], s), make_float2(wv.x, wv.y), make_float2(bv.x, bv.y)));
-            set_pair<T>(out, 2 * q + 1, fma2(mul2(v[2 * q + 1], s), make_float2(wv.z, wv.w), make_float2(bv.z, bv.w)));
+            set_pair<T>(out, 2 * q, fma2(fma2(v[2 * q], s, o), make_float2(wv.x, wv.y), make_float2(bv.x, bv.y)));
+            set_pair<T>(out, 2 * q + 1, fma2(fma2(v[2 * q + 1], s, o), make_float2(wv.z, wv.w), make_float2(bv.z, bv.w)));
         }
     }
 };
@@ -217,8 +254,8 @@ struct Packed {
         }
     }
     __device__ __forceinline__ void scale(const R&, uint32_t (&out)[R::kWords], const float2 (&v)[R::N / 2],
-                                          float rstd) const {
-        const float2 s = both(rstd);
+                                          const Spread& spread) const {
+        const float2 s = both(spread.rstd), o = both(-spread.left * spread.rstd);
 #pragma unroll
         for (int u = 0; u < R::N / R::V; ++u) {
             const uint4 wv = w[u * threads + threadIdx.x], bv = b[u * threads + threadIdx.x];
@@ -226,7 +263,7 @@ struct Packed {
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const int p = 4 * u + i;
-                set_pair<T>(out, p, fma2(mul2(v[p], s), pair_of<T>(wr, i), pair_of<T>(br, i)));
+                set_pair<T>(out, p, fma2(fma2(v[p], s, o), pair_of<T>(wr, i), pair_of<T>(br, i)));
             }
         }
     }
@@ -239,6 +276,7 @@ int affine_bytes(int threads, int units, bool packed) {
     return sizeof(T) == 4 ? 0 : 2 * threads * units * 16 * (packed ? 1 : 2);
 }
 
+// A row's sums over GL lanes, GL 0: over the block.
 template <int GL>
 struct Total {
     __device__ __forceinline__ float operator()(float v) const {
@@ -246,9 +284,45 @@ struct Total {
         lanes_sum<GL>(one);
         return one[0];
     }
+    __device__ __forceinline__ float2 operator()(float2 v) const {
+        float two[2] = {v.x, v.y};
+        lanes_sum<GL>(two);
+        return make_float2(two[0], two[1]);
+    }
 };
 template <>
 struct Total<0> : BlockSum {};
+// Two of a block at once: the lower half of a warp's lanes goes on with the
+// first, the upper half with the second.  Only where they are asked for: with
+// 512 bytes more, 16-bit rows' blocks would not fit three an SM.
+struct BlockPairs : BlockSum {
+    float* pairs;  // [2][2][32], by the same turns
+    __device__ __forceinline__ BlockPairs() {
+        __shared__ float all[2][2][32];
+        pairs = all[0][0];
+        if (threadIdx.x < 64) pairs[threadIdx.x] = pairs[64 + threadIdx.x] = 0.0f;
+        __syncthreads();
+    }
+    using BlockSum::operator();
+    __device__ __forceinline__ float2 operator()(float2 f) {
+        const bool up = threadIdx.x & 16;
+        float* at = pairs + 2 * turn + (threadIdx.x & 16) * 2;
+        float v = (up ? f.y : f.x) + __shfl_xor_sync(~0u, up ? f.x : f.y, 16);
+#pragma unroll
+        for (int o = 8; o; o >>= 1) v += __shfl_xor_sync(~0u, v, o);
+        if (threadIdx.x % 16 == 0) at[threadIdx.x / 32] = v;
+        __syncthreads();
+        v = at[threadIdx.x & 15 & (lanes - 1)];
+        if (lanes == 32) v += at[16 + threadIdx.x % 16];
+#pragma unroll
+        for (int o = 8; o; o >>= 1)
+            if (o < lanes) v += __shfl_xor_sync(~0u, v, o);
+        const float w = __shfl_xor_sync(~0u, v, 16);
+        return up ? make_float2(w, v) : make_float2(v, w);
+    }
+};
+template <class T, int GL>
+using RowTotal = typename std::conditional<GL == 0 && kLeft<T>, BlockPairs, Total<GL>>::type;
 
 constexpr int kShort = 256;  // threads a block of short rows
 // Its blocks an SM, by the registers of U units a thread.  (2^20 x 64 floats
@@ -280,7 +354,7 @@ __global__ void __launch_bounds__(MOST, GL ? kShortResident<T, U> : MOST == 256 
     x += (r < a.rows ? r : a.rows - 1) * a.ldx;
     part.load(next, x, whole);
     const Affine<T, R, GL> affine(part, a, reinterpret_cast<float4*>(shared));
-    Total<GL> total;
+    RowTotal<T, GL> total;
     // a warp's groups go round together
     for (int64_t first = (int64_t)blockIdx.x * groups; first < a.rows; first += step, r += step, y += step * a.ldy) {
         float2 v[R::N / 2];
@@ -288,11 +362,12 @@ __global__ void __launch_bounds__(MOST, GL ? kShortResident<T, U> : MOST == 256 
         for (int i = 0; i < R::kWords; ++i) now[i] = next[i];
         if (r + step < a.rows) x += step * a.ldx;
         if (first + step < a.rows) part.load(next, x, whole);
-        const float mean = over(total(sum_of<T>(part, now)), cols, inv);
-        const float rstd = inv_sqrt(fmaf(total(squares_of<T, STRIDED>(part, now, v, mean)), inv, a.eps));
+        const Mean mean(total(sum_of<T>(part, now)), cols, inv);
+        const Spread spread =
+            spread_of<T>(total, mean, deviations_of<T, STRIDED>(part, now, v, mean.value), inv, a.eps);
         if (r >= a.rows) continue;
-        if (a.mean && part.lane == 0) a.mean[r] = mean, a.rstd[r] = rstd;
-        affine.scale(part, now, v, rstd);
+        if (a.mean && part.lane == 0) a.mean[r] = mean.value + spread.left, a.rstd[r] = spread.rstd;
+        affine.scale(part, now, v, spread);
         part.store(y, now, whole);
     }
 }
@@ -324,21 +399,22 @@ __global__ void __launch_bounds__(MOST, MOST == 256 ? 2 : 1024 / MOST)
     using Vectors = typename std::conditional<U == 4, Packed<T, R>, Affine<T, R, 0>>::type;
     const Vectors affine(part, a, reinterpret_cast<float4*>(out + (staged ? ring.place : 0)));
     T* y = static_cast<T*>(a.y) + blockIdx.x * a.ldy;
-    BlockSum total;
+    RowTotal<T, 0> total;
     for (int k = 0; k < rows; ++k, x += step, y += gridDim.x * a.ldy) {
         uint32_t words[R::kWords];
         float2 v[R::N / 2];
         ring.wait(0);
         load_units<false>(words, part, ring.row(0, 0), low_of(x) & 15);
-        const float mean = over(total(sum_of<T>(part, words)), cols, inv);
+        const Mean mean(total(sum_of<T>(part, words)), cols, inv);
         fetch(k + stages - 1);  // all have read the row before this one
         ring.advance(1);
-        const float rstd = inv_sqrt(fmaf(total(squares_of<T, true>(part, words, v, mean)), inv, a.eps));
+        const Spread spread =
+            spread_of<T>(total, mean, deviations_of<T, true>(part, words, v, mean.value), inv, a.eps);
         if (a.mean && threadIdx.x == 0) {
             const int64_t r = blockIdx.x + (int64_t)k * gridDim.x;
-            a.mean[r] = mean, a.rstd[r] = rstd;
+            a.mean[r] = mean.value + spread.left, a.rstd[r] = spread.rstd;
         }
-        affine.scale(part, words, v, rstd);
+        affine.scale(part, words, v, spread);
         store_units<false>(y, part, words, staged ? out : nullptr);
     }
     ring.leave(err);
@@ -541,28 +617,30 @@ __global__ void __launch_bounds__(MOST)
 
 // ------------------------------------------- rows beyond registers or the ring
 
-constexpr int kLong = 1024;
+constexpr int kLong = 1024;  // two blocks an SM (1024 x 20000 floats: 55 us, by one 71)
 
 template <class T>
-__global__ void __launch_bounds__(kLong) layer_norm_long_kernel(const __grid_constant__ heddle_layer_norm_args a) {
+__global__ void __launch_bounds__(kLong, 2) layer_norm_long_kernel(const __grid_constant__ heddle_layer_norm_args a) {
     allow_dependents();
     await_previous();
     const float cols = (float)a.cols, inv = 1.0f / cols;
-    BlockSum total;
+    BlockPairs total;
     for (int64_t r = blockIdx.x; r < a.rows; r += gridDim.x) {
         const T* x = static_cast<const T*>(a.x) + r * a.ldx;
         T* y = static_cast<T*>(a.y) + r * a.ldy;
-        float sum = 0.0f, sq = 0.0f;
+        float sum = 0.0f;
+        float2 sums = both(0.0f);
         for (int64_t i = threadIdx.x; i < a.cols; i += kLong) sum += to_float(x[i]);
-        const float mean = over(total(sum), cols, inv);
+        const Mean mean(total(sum), cols, inv);
         for (int64_t i = threadIdx.x; i < a.cols; i += kLong) {
-            const float d = to_float(x[i]) - mean;
-            sq = fmaf(d, d, sq);
+            const float d = to_float(x[i]) - mean.value;
+            sums = make_float2(sums.x + d, fmaf(d, d, sums.y));
         }
-        const float rstd = inv_sqrt(fmaf(total(sq), inv, a.eps));
-        if (a.mean && threadIdx.x == 0) a.mean[r] = mean, a.rstd[r] = rstd;
+        const Spread spread(total(sums), inv, a.eps);
+        const float rstd = spread.rstd, o = -spread.left * rstd;
+        if (a.mean && threadIdx.x == 0) a.mean[r] = mean.value + spread.left, a.rstd[r] = rstd;
         for (int64_t i = threadIdx.x; i < a.cols; i += kLong) {
-            const float n = (to_float(x[i]) - mean) * rstd;
+            const float n = fmaf(to_float(x[i]) - mean.value, rstd, o);
             y[i] = from_float<T>(fmaf(n, a.weight ? to_float(static_cast<const T*>(a.weight)[i]) : 1.0f,
                                       a.bias ? to_float(static_cast<const T*>(a.bias)[i]) : 0.0f));
         }

@@ -64,3 +64,78 @@ def test_layer_norm_results_do_not_depend_on_addresses(lib, m, n, dt):
         want = want or got
         for name in want:
             assert torch.equal(got[name], want[name]), "%s of layout %d" % (name, i)
+
+
+def far_from_zero(x, w, b, eps):
+    """(mean, bound), (rstd, bound), (y, bound) where the deviations are taken
+    from a 32-bit number near the mean, and their own mean is taken out again.
+
+    That number, m, is off by em as in H.layer_norm.  v = x - m is off by e |v|;
+    the mean of v by its additions and v's errors, ed; so v minus it, in one
+    rounding, by e |v| + ed + e |mean of v| and its own rounding.
+
+    For 16-bit values the mean of v is what the sum of x leaves beyond m.  That
+    sum is exact while it stays below 2^24 times the last place of the row's
+    smallest value, of which all values and sums are multiples; else it is off
+    by its additions, em."""
+    e, last = H.e, torch.finfo(x.dtype).eps
+    x = x.double()
+    n = x.shape[1]
+    many = H.depth(n) + 5
+    mean = x.mean(1, keepdim=True)
+    em = (H.depth(n) + 3) * e * x.abs().mean(1, keepdim=True)
+    d = x - mean
+    var = d.square().mean(1, keepdim=True)
+    size = d.abs().mean(1, keepdim=True) + em        # of v, on average; |mean of v| <= em
+    ed = many * e * size
+    # mean v^2 = var + (mean v)^2 <= var + em^2, off by its additions and v's errors
+    ev = (many + 6) * e * (var + em ** 2) + 2 * em * ed + 4 * e * em ** 2
+    rstd = (var + eps) ** -0.5
+    rel = (ev + e * eps) / (var + eps) + 6 * e
+    assert rel.max() < 0.5
+    v = d * rstd
+    wd = 1.0 if w is None else w.double()
+    bd = 0.0 if b is None else b.double()
+    y = v * wd + bd
+    if last > 1e-6:
+        last = last * 2.0 ** torch.floor(torch.log2(x.abs().amin(1, keepdim=True).clamp(min=1e-30)))
+        ed = ed + em * (x.abs().sum(1, keepdim=True) > 2.0 ** 24 * last)
+    lost = (e * (d.abs() + em) + ed + 3 * e * em) * rstd * (1 + rel) + v.abs() * (rel + 2 * e)
+    ey = lost * (wd if w is None else wd.abs()) + 2 * e * (y.abs() + (v * wd).abs())
+    return (mean[:, 0], (ed + 2 * e * em + e * mean.abs())[:, 0]), (rstd[:, 0], (rstd * rel)[:, 0]), (y, ey)
+
+
+@pytest.mark.parametrize("dt", ["fp32", "fp16", "bf16"])
+@pytest.mark.parametrize("n", [5, 64, 100, 257, 300, 512, 1023, 2047, 4096, 4100, 8192, 12288, 20000])
+@pytest.mark.parametrize("center", [0.0, 300.0, -4096.0, 1e5])
+def test_layer_norm_of_large_means(lib, n, center, dt):
+    """The mean's rounding, up to 2^-24 of it, does not reach y: with a mean of
+    100000 and deviations of 1 it was off by 0.004 from that alone."""
+    h, ctx = lib
+    dt = TYPES[dt]
+    if abs(center) > 60000 and dt == torch.float16:
+        center = 30000.0
+    g = gen(n)
+    x = (rand(g, 40, n, dt=torch.float32) * (1 if dt == torch.float32 else max(1.0, abs(center) / 64)) + center).to(dt)
+    for pad, skip in PLACES[:4]:
+        w, b = (None, None) if skip == 8 else (1 + rand(g, n, dt=dt, std=0.3), rand(g, n, dt=dt))
+        y, mean, rstd = torch.empty_like(x), floats(40), floats(40)
+        h.heddle_layer_norm(ctx, laid(x, pad, skip), w, b, y, mean=mean, rstd=rstd)
+        (wm, em), (wr, er), (wy, ey) = far_from_zero(x, w, b, 1e-5)
+        close(mean, wm, em, "mean")
+        close(rstd, wr, er, "rstd")
+        close(y, wy, ey, "y")
+
+
+@pytest.mark.parametrize("n", [64, 100, 1000, 2047, 8192, 20000])
+def test_layer_norm_of_squares_beyond_32_bits(lib, n):
+    """Their sum past the largest float: y is the bias; below the smallest: eps
+    alone is the variance, and eps 0 is not asked for."""
+    h, ctx = lib
+    sign = 1.0 - 2.0 * (torch.arange(n, device="cuda") % 2)
+    x = torch.stack((sign * 1e25, sign * 1e-30))
+    b, y, mean, rstd = torch.full((n,), 0.25, device="cuda"), torch.empty_like(x), floats(2), floats(2)
+    h.heddle_layer_norm(ctx, x, None, b, y, mean=mean, rstd=rstd, eps=0.25)
+    assert (y[0] == 0.25).all() and rstd[0] == 0
+    assert torch.equal(y[1], x[1] * 2 + 0.25) and rstd[1] == 2
+    assert mean[0].abs() <= 1.01e25 / n and mean[1].abs() <= 1.01e-30 / n
