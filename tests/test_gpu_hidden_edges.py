@@ -1,4 +1,5 @@
-"""Layer norm where 32 bits are short, and what its results may not depend on."""
+"""The hidden state's operators where 32 bits are short, and what their results
+may not depend on."""
 
 import pytest
 
@@ -139,3 +140,56 @@ def test_layer_norm_of_squares_beyond_32_bits(lib, n):
     assert (y[0] == 0.25).all() and rstd[0] == 0
     assert torch.equal(y[1], x[1] * 2 + 0.25) and rstd[1] == 2
     assert mean[0].abs() <= 1.01e25 / n and mean[1].abs() <= 1.01e-30 / n
+
+
+FAR = 2 ** 30 + 24  # elements between rows: the third begins past 2^31
+
+
+def far(t, skip):
+    v = torch.empty(skip + 2 * FAR + t.shape[1] + 16, dtype=t.dtype, device="cuda")[skip:]
+    v = v.as_strided(t.shape, (FAR, 1))
+    v.copy_(t)
+    return v
+
+
+@pytest.mark.parametrize("n", [64, 2047, 4096, 8192, 20000])
+@pytest.mark.parametrize("skip", [0, 3])
+def test_layer_norm_and_dropout_of_rows_far_apart(lib, n, skip):
+    """The same bits as of rows that follow each other."""
+    h, ctx = lib
+    g = gen(n)
+    x, dy, dres = (rand(g, 3, n, dt=torch.bfloat16) for _ in range(3))
+    w, b = 1 + rand(g, n, dt=torch.bfloat16, std=0.3), rand(g, n, dt=torch.bfloat16)
+    got = []
+    for place in (lambda t: t, lambda t: far(t, skip)):
+        xi, dyi, dri = (place(t) for t in (x, dy, dres))
+        y, dx, d = (place(torch.zeros_like(x)) for _ in range(3))
+        mean, rstd, dw, db = floats(3), floats(3), floats(n), floats(n)
+        h.heddle_layer_norm(ctx, xi, w, b, y, mean=mean, rstd=rstd)
+        h.heddle_layer_norm_backward(ctx, dyi, xi, w, mean, rstd, dx=dx, dw=dw, dbias=db, dres=dri)
+        h.heddle_dropout(ctx, xi, d, 0.3, 5, residual=dri)
+        got.append([t.clone() for t in (y, mean, rstd, dx, dw, db, d)])
+    for one, other in zip(*got):
+        assert torch.equal(one, other)
+
+
+@pytest.mark.parametrize("skip", [0, 3])
+def test_embedding_and_router_of_rows_far_apart(lib, skip):
+    h, ctx = lib
+    g = gen(skip)
+    n, e, k = 1000, 250, 4
+    table, dy = rand(g, 3, n, dt=torch.float16), rand(g, 3, n, dt=torch.float16)
+    logits, dweights = rand(g, 3, e, dt=torch.float16), rand(g, 3, k, dt=torch.float32)
+    tokens = torch.tensor([2, 0, 2], device="cuda")
+    got = []
+    for place in (lambda t: t, lambda t: far(t, skip)):
+        y, dtable, dlogits = place(torch.zeros_like(dy)), place(torch.ones_like(table)), place(torch.zeros_like(logits))
+        experts, weights = torch.empty(3, k, dtype=torch.int32, device="cuda"), torch.empty(3, k, device="cuda")
+        counts, loss = torch.empty(e + 1, dtype=torch.int32, device="cuda"), floats(1)
+        h.heddle_embedding(ctx, tokens, place(table), y, scale=3.0)
+        h.heddle_embedding_backward(ctx, tokens, place(dy), dtable, scale=3.0)
+        h.heddle_router(ctx, place(logits), experts, weights, counts, loss=loss)
+        h.heddle_router_backward(ctx, place(logits), experts, weights, counts, dlogits, dweights=dweights, dloss=loss)
+        got.append([t.clone() for t in (y, dtable, experts, weights, counts, loss, dlogits)])
+    for one, other in zip(*got):
+        assert torch.equal(one, other)
