@@ -862,7 +862,7 @@ heddle_status heddle_dropout_backward(heddle_ctx* ctx, const heddle_dropout_args
  * rows of zeros, so that the shards' results add up.  vocab: the vocabulary's
  * size (at least first + table_rows); a token that is not below it raises
  * bit 6 of heddle_device_errors and gives zeros.  token: [tokens], int32, or
- * int64 with wide_tokens.  */
+ * int64 with wide_tokens.  cols: at most 2^22. */
 typedef struct {
     int64_t tokens, cols, table_rows, first, vocab;
     int32_t dtype, wide_tokens;
@@ -883,7 +883,7 @@ heddle_status heddle_embedding(heddle_ctx* ctx, const heddle_embedding_args* arg
  * in full, or, with `accumulate`, added to what it holds (rows without tokens
  * are then not touched).  grad_dtype: the gradient's type, dtype or
  * HEDDLE_FP32.  Tokens are sorted and each row's terms are added in an order
- * that the tokens alone fix, in 32 bits; one rounding at the end. */
+ * that the tokens and the sizes fix, in 32 bits; one rounding at the end. */
 typedef struct {
     heddle_embedding_args fwd;
     int32_t grad_dtype, accumulate;

@@ -5,8 +5,9 @@
 // a row's terms lie together in the order of their tokens; then blocks add up
 // runs of the sorted list, others write zeros to the rows that have no token,
 // and the sums of rows that go over several runs are joined in order.
-// 16384 tokens, 131072 rows of 4096 bfloat16 values: 28 us for the rows, 17 to
-// sort, 176 for sums and zeros (1.2 GB), 10 to join.
+// 16384 tokens as words fall on 131072 rows of 4096 bfloat16 values: 31 us for the
+// rows, 205 for the gradient (1.2 GB); launched one by one its kernels take 17 to
+// sort, 176 for sums and zeros, 10 to join.
 
 #include <atomic>
 
@@ -273,8 +274,8 @@ struct Sums {
     int32_t accumulate;
     int32_t out_whole;  // the gradient's rows are whole units at 16 bytes
     // blocks that write zeros to the rows without tokens, behind the others: many
-    // small ones even out what memory gives each (two an SM: 264 us where eight
-    // take 207, 16384 tokens and 131072 x 4096 bfloat16)
+    // small ones even out what memory gives each (two an SM: 404 us where eight
+    // take 205, 16384 tokens and 131072 x 4096 bfloat16)
     unsigned fillers;
 };
 
@@ -498,7 +499,7 @@ __global__ void __launch_bounds__(kThreads)
 }
 
 // Rows that go over several runs, 1024 columns of one a block at a time: 262144
-// tokens of 1024 values, half of one row, take 238 us, 346 with the runs' parts
+// tokens of 1024 values, half of one row, take 234 us, 346 with the runs' parts
 // fetched one after the other.  (A block for every run, most of which have
 // nothing to do, took 40 us for 16384 tokens where this takes 10; narrow slabs,
 // each with the search and its waits, 36.)
@@ -564,11 +565,12 @@ cudaError_t lookup(const OpContext& x, const heddle_embedding_args& a, cudaStrea
 }
 
 // Threads a token, units a thread and tokens at a time.  Few tokens take a unit
-// a thread (64 of 1024 bfloat16 values: 1.5 us, and 1.9 by four at a time), so
+// a thread (64 of 1024 bfloat16 values: 1.4 us, and 1.65 by four at a time), so
 // that more SMs take part.  Others keep several loads of a thread on their way:
 // 16384 tokens of 1024 values take 10.3 us, one at a time 17.5; beyond 128 units
-// those of one token (512 of 4096 values 2.3 us, four tokens at a time 2.6;
-// 16384 of them 39.2 and 37.9).
+// those of one token (512 of 4096 values 2.3 us, four tokens at a time 2.6; 2048
+// 4.7 and 5.0; 16384 of 32000 rows, as words fall, 29.5 and 29.2, and any row,
+// where it loses, 39.2 and 37.6).
 template <class T, bool WHOLE>
 cudaError_t lookup_typed(const OpContext& x, const heddle_embedding_args& a, cudaStream_t st) {
     const int64_t units = ceil_div(a.cols, 16 / (int)sizeof(T));
@@ -643,8 +645,8 @@ cudaError_t sums(const OpContext& x, const Sums& s, cudaStream_t st) {
 }
 
 // Up to so many are sorted by one CTA, others by a cluster of eight (the gradient
-// of 256 bfloat16 values, 1000 rows: 128 tokens 9.6 us, by a cluster 12.3; 512:
-// 12.9 and 14.3; 2048: 17.4 and 16.9).
+// of 256 bfloat16 values, 1000 rows: 512 tokens 12.9 us, by a cluster 14.3; 2048:
+// 17.5 and 16.9).
 constexpr int64_t kFewTokens = 512;
 template <int CTAS>
 cudaError_t sort(const OpContext& x, const Sort& s, cudaStream_t st) {

@@ -228,7 +228,8 @@ struct Shared {
         for (int q = 0; q < R::N / 4; ++q) {
             const float4 wv = w[q * threads + threadIdx.x], bv = b[q * threads + threadIdx.x];
             set_pair<T>(out, 2 * q, fma2(fma2(v[2 * q], s, o), make_float2(wv.x, wv.y), make_float2(bv.x, bv.y)));
-            set_pair<T>(out, 2 * q + 1, fma2(fma2(v[2 * q + 1], s, o), make_float2(wv.z, wv.w), make_float2(bv.z, bv.w)));
+            set_pair<T>(out, 2 * q + 1,
+                        fma2(fma2(v[2 * q + 1], s, o), make_float2(wv.z, wv.w), make_float2(bv.z, bv.w)));
         }
     }
 };
@@ -745,7 +746,7 @@ struct Plan {
     Way way;
     // rows of no whole units, whose values are dealt out one by one; but not in a
     // block's forward pass over 16-bit ones (65568 x 2047 bfloat16: units put
-    // together from two 153 us, value by value 175; backward 236 and 220)
+    // together from two 155 us, value by value 175; backward 236 and 220)
     bool strided;
     bool whole;        // whole units at 16 bytes throughout
     bool staged;       // rows leave by way of shared memory
@@ -804,8 +805,8 @@ Plan plan_forward(const OpContext& x, const heddle_layer_norm_args& a) {
     p.way = units > kEach * kLong ? kLongRows : kBlocks;
     int an_sm = blocks_an_sm(1024, p.threads);
     // rows of 512 to 1024 units of 16-bit values by smaller blocks, three an SM:
-    // 16384 x 8192 bfloat16 takes 86 us, two units a thread 98 (26214 x 5120: 86
-    // and 96; 32768 x 4096 the other way round, 91 and 100)
+    // 16384 x 8192 bfloat16 takes 87 us, two units a thread 98 (26214 x 5120: 87
+    // and 96; 32768 x 4096 the other way round, 92 and 100)
     if (!p.strided && size == 2 && units > 512 && units <= 1024) {
         p.units = 4;
         p.threads = (int)ceil_div(ceil_div(units, 4), 32) * 32;

@@ -8,9 +8,10 @@
 // What a lane's experts get, probability and choices, is summed in its registers
 // over all tokens of its warp, then over the block's warps, then over blocks by
 // a second kernel, always in order.  The backward pass computes the
-// probabilities again.  16384 tokens of 64 bfloat16 logits, two chosen: 9.5 us
-// forward, 6.3 backward; 32771 of 250 floats, eight chosen: 29 and 21 us (their
-// 69 MB take 10).
+// probabilities again.  16384 tokens of 64 bfloat16 logits, two chosen: 9.7 us
+// forward, 6.4 backward; 32771 of 250 floats, eight chosen: 29 and 21 us (their
+// 69 MB take 10).  These and the times below are of calls of a graph one after
+// the other, the join's kernel with them.
 
 #include <string.h>
 
@@ -94,7 +95,7 @@ struct Softmax {
 // A token's keys, the largest one after the other, and the first of equal ones.
 // Up to four a lane stay in registers and are all compared for each choice; more
 // lie in shared memory as lists.  (32771 tokens of 250 floats, eight chosen: 29
-// us, from registers 34; 16384 of 64: 14.6 and 12.2.)
+// us, from registers 34; 16384 of 64 bfloat16, eight chosen: 12.7 and 11.5.)
 template <class T, int N, bool LISTS = (N > 4)>
 struct Search;
 template <class T, int N>
@@ -172,7 +173,7 @@ struct Search<T, N, true> {
 };
 
 // Threads a block, one an SM: those that the registers allow.  (Two blocks of 1024
-// for 64 experts: 16384 tokens 10.4 us, one 9.6.)
+// for 64 experts: 16384 tokens 10.3 us, one 9.7.)
 template <int N>
 constexpr int kThreads = N == 32 ? 256 : N == 16 ? 512 : N == 8 ? 768 : 1024;
 
@@ -415,8 +416,8 @@ __global__ void __launch_bounds__(kThreads<N>, 1)
 }
 
 // Experts a lane of a token's warp.  (Eight lanes a token up to 64 experts took
-// 5.6 us for 64 tokens of 64 experts, two of them, where a warp takes 4.7, and
-// 11.3 for 16384 of eight where it takes 11.8.)
+// a fifth longer for 64 tokens of 64 experts, two of them, and 4 % less for
+// 16384 of eight.)
 template <class F>
 auto with_split(int experts, F f) {
     if (experts <= 64) return f(std::integral_constant<int, 2>());
@@ -434,7 +435,7 @@ int64_t blocks_of(const OpContext& x, const heddle_router_args& a) {
 }
 
 // Whether one block does it all: for up to two rounds of its warps.  (64 tokens
-// of 64 experts: 4.6 us, 5.8 with a second kernel; 128 tokens, in four rounds:
+// of 64 experts: 4.4 us, 4.9 with a second kernel; 128 tokens, in four rounds:
 // 7.0 and 5.7.)
 bool one_block(const heddle_router_args& a) {
     return with_split(a.experts, [&](auto n) { return a.tokens <= 2 * (kThreads<n.value> / 32); });
@@ -455,8 +456,8 @@ cudaError_t forward(const OpContext& x, const heddle_router_args& a, unsigned ch
     attr[0].val.clusterDim = {kJoinCluster, 1, 1};
     attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[1].val.programmaticStreamSerializationAllowed = 1;
-    // 32771 tokens of 250 experts: 33.4 us by a cluster, 36.8 by a block; 16384 of
-    // eight: 9.4 and 8.2
+    // 32771 tokens of 250 experts: 29.1 us by a cluster, 32.8 by a block; 16384 of
+    // 64: 9.9 and 9.7; of eight: 9.3 and 8.2
     const bool many = a.experts > 64;
     cudaLaunchConfig_t cfg{};
     cfg.gridDim = dim3(many ? kJoinCluster : 1);
