@@ -883,7 +883,8 @@ heddle_status heddle_embedding(heddle_ctx* ctx, const heddle_embedding_args* arg
  * in full, or, with `accumulate`, added to what it holds (rows without tokens
  * are then not touched).  grad_dtype: the gradient's type, dtype or
  * HEDDLE_FP32.  Tokens are sorted and each row's terms are added in an order
- * that the tokens and the sizes fix, in 32 bits; one rounding at the end. */
+ * that the tokens and the sizes fix, in 32 bits; one rounding at the end.  Takes
+ * scratch of 16 bytes a token and two rows of floats for every 8 to 512 tokens. */
 typedef struct {
     heddle_embedding_args fwd;
     int32_t grad_dtype, accumulate;

@@ -19,6 +19,9 @@ their way into the residual stream (heddle_dropout):
 
   y = x + dropout(attention(norm(x)) w_o^T),  z = y + dropout(ffn(norm(y)) w_down^T)
 
+These norms have means and biases, which models with a gated block and rotation
+leave out: a stand-in that moves a vector more, with more operations a value.
+
 Without ``norms`` the entries are those of the products, attention and norms
 per head alone, too small by two passes over the hidden state in either
 direction, and the backward pass adds the two residual gradients with torch.
